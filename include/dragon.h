@@ -49,7 +49,9 @@ enum {
   DRAGON_ERR_TIMEOUT = -10       /* a bounded device-side wait ran out (reported by dragon_function_status) */
 };
 
-enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2 };
+/* F8E4M3: one byte per element, 1 sign, 4 exponent (bias 7) and 3 mantissa bits, largest magnitude 448, no
+ * infinities; made by DRAGON_OP_QUANTIZE or fed, read by DRAGON_OP_SCALED_INNER_PRODUCT. */
+enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2, DRAGON_F8E4M3 = 3 };
 
 /* Operator types.  The paper names Sigmoid, Tanh, ReLU (Sec. 2.4) and uses mul, add, sin in
  * its example (Sec. 2.2); the remaining semantics are this library's:
@@ -66,6 +68,31 @@ enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2 };
  *   SOFTMAX_CROSS_ENTROPY(Z, labels)  scalar -(1/M) sum_m log softmax(Z[m,:])[labels[m]],
  *                          labels int32 in [0, N); an out-of-range label contributes 0 and
  *                          sets the function status to DRAGON_ERR_INVALID_ARG (no fault)
+ *
+ * Operators of language models (attrs: the operator's numbers, passed to dragon_add_op):
+ *   RMS_NORM(h, g) attrs {eps = 1e-6}    y[r,c] = h[r,c] / sqrt(mean_c(h[r,:]^2) + eps) * g[c]; h [R,C] or [C], g [C].
+ *                          An Add in front of it (the residual's addition) runs in the same pass, and so do a BlockScale
+ *                          and a Quantize behind it.  Statistics in fp32 on the values of h in its declared type.
+ *   BLOCK_SCALE(x) attrs {rows = 1}      s = max(amax / 448, 2^-126) of every block of rows x 128 elements of x [R,C]
+ *                          (rows 1 or 128, the last blocks may be ragged); s f32 [ceil(R / rows), ceil(C / 128)].  A NaN
+ *                          in a block makes its scale NaN.
+ *   QUANTIZE(x, s)         q[r,c] = e4m3(x[r,c] * (1 / s)), nearest, ties to even, magnitudes beyond 448 become 448, NaN stays
+ *                          NaN; s the scales of 1 x 128 or 128 x 128 blocks; the result's type is F8E4M3.
+ *   SCALED_INNER_PRODUCT(Xq, sx, Wq, sw)  Y[m,n] = sum_b sx[m,b] sw[n/128,b] sum_{k in block b} Xq[m,k] Wq[n,k] with
+ *                          blocks of 128 along K; Xq F8E4M3 [M,K], sx f32 [M, ceil(K/128)], Wq F8E4M3 [N,K], sw f32
+ *                          [ceil(N/128), ceil(K/128)], K a multiple of 16; fp32 accumulation; Y f32 or bf16.
+ *   GLOBAL_NORM(t0, t1, ...)  scalar sqrt(sum of the squares of all elements of all operands), any shapes.
+ *   CLIP_BY_NORM(t, norm) attrs {limit}   t * min(1, limit / norm), norm an f32 scalar (NaN makes everything NaN), limit > 0.
+ *                          The fetched ones of a norm run as one launch over all tensors; one that an operator
+ *                          consumes (an updater) is a factor in that operator's pass.
+ *   GATED_SCAN(gate, x [, h0] [, reset]) attrs {sequences = 1}   h[t] = f h[t-1] + (1 - f) x[t], f = sigmoid(gate[t]), per
+ *                          column; the rows of gate and x [T,C] are `sequences` sequences of T / sequences rows one after
+ *                          another, each starting from its row of h0 (f32/bf16 [sequences, C]) or from zero; reset (int32
+ *                          [T]): a row with a value other than 0 starts from zero whatever came before (packed documents).
+ *                          The state is kept in fp32 between rows.  One row per sequence is a decoding step.
+ * RMS_NORM and GATED_SCAN have gradients (with respect to h, g; gate, x, h0).  A gradient chain through BLOCK_SCALE,
+ * QUANTIZE, SCALED_INNER_PRODUCT, GLOBAL_NORM or CLIP_BY_NORM is DRAGON_ERR_UNSUPPORTED at dragon_function.
+ *
  *   OPAQUE                 an operator the library knows only as an edge set: any number of inputs
  *                          and of outputs (Sec. 2.2: an edge from every input to every output), output
  *                          shapes as declared.  Both prunes treat it like any other operator; a
@@ -78,7 +105,10 @@ enum {
   DRAGON_OP_RELU = 8, DRAGON_OP_SUM = 9, DRAGON_OP_MEAN = 10,
   DRAGON_OP_INNER_PRODUCT = 11, DRAGON_OP_BIAS_ADD = 12, DRAGON_OP_SOFTMAX_CROSS_ENTROPY = 13,
   DRAGON_OP_SQRT = 14, DRAGON_OP_RECIPROCAL = 15, DRAGON_OP_OPAQUE = 16,
-  DRAGON_OP_COUNT_ = 17
+  DRAGON_OP_RMS_NORM = 17, DRAGON_OP_BLOCK_SCALE = 18, DRAGON_OP_QUANTIZE = 19,
+  DRAGON_OP_SCALED_INNER_PRODUCT = 20, DRAGON_OP_GLOBAL_NORM = 21, DRAGON_OP_CLIP_BY_NORM = 22,
+  DRAGON_OP_GATED_SCAN = 23,
+  DRAGON_OP_COUNT_ = 24
 };
 
 /* ---- graph capture (Sec. 2.1: tensors are nodes; an operator connects each of its inputs
@@ -95,7 +125,8 @@ dragon_id dragon_add_tensor(dragon_graph_t* g, const char* name, int dtype, int 
  * have no producer yet, must not be among the inputs and must not have been read already; its
  * declared shape must equal the inferred one (Sec. 4.3: a mistaken shape is caught before
  * executing).  Every executable operator type has exactly one output; DRAGON_OP_OPAQUE takes
- * n_out >= 1.  attrs is reserved (pass NULL, 0).  Returns the operator id. */
+ * n_out >= 1.  attrs: host array of the operator's numbers as listed above (NULL, 0 for an operator
+ * without any, or for the defaults).  Returns the operator id. */
 dragon_id dragon_add_op(dragon_graph_t* g, int op_type, const dragon_id* in, int n_in,
                         const dragon_id* out, int n_out, const double* attrs, int n_attrs);
 
@@ -151,7 +182,9 @@ int dragon_function_workspace_tensors(const dragon_function_t* f, int64_t* out, 
 /* In-place use.  The updater graphs of Sec. 3.2 overwrite their state (W, momentum, second moment), and
  * Sec. 2.4 is about operators that write over their input.  Returns 1 if fetch position `output` may be
  * given the very same device pointer as feed position `input` in dragon_run(), 0 if not, a negative
- * code for bad positions.  It is 1 exactly when the function is a single elementwise launch over a
+ * code for bad positions.  It is 1 when the function is nothing but GlobalNorm and one norm's ClipByNorm, `input` is a tensor
+ * that is clipped once and `output` its clipped form of the same type (the launch that overwrites it is behind the
+ * one that sums it).  Otherwise it is 1 exactly when the function is a single elementwise launch over a
  * flat domain, both tensors have the domain's shape and the same type, and the program reads the
  * input for the last time before it first writes the output: every thread then overwrites only
  * elements it has already read (the copy of a tile that is fetched ahead of time is never a tile that

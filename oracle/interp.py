@@ -18,6 +18,12 @@ tensor per operator, no fusion, no reordering.
                      contraction consumes bf16), products and sums are wide
   BiasAdd(Y, b)      Y[m,n] + b[n]
   SoftmaxCrossEntropy(Z, labels)  scalar  -(1/M) sum_m log softmax(Z[m,:])[labels[m]]
+  RMSNorm(h, g)      h / sqrt(mean(h^2) + eps) * g over rows
+  BlockScale(x)      max(amax / 448, 2^-126) over blocks of rows x 128
+  Quantize(x, s)     nearest e4m3 value (ties to even, magnitudes capped at 448) of x / s
+  ScaledInnerProduct(Xq, sx, Wq, sw)  (Xq * sx) @ (Wq * sw)^T with the scales spread over their blocks
+  GlobalNorm(t...)   sqrt of the sum of all squares; ClipByNorm(t, norm) = t * min(1, limit / norm)
+  GatedScan(gate, x [, h0] [, reset])  row by row h = f*h + (1-f)*x, f = sigmoid(gate)
 
 Gradient rules (dy = gradient of the output): Add (dy,dy); Sub (dy,-dy);
 Mul (dy*b, dy*a); Div (dy/(1+|b|), -dy*a*sgn(b)/(1+|b|)^2) with sgn(0)=0;
@@ -47,7 +53,7 @@ def round_bf16(a):
     nan = np.isnan(f)
     out = r.astype(np.uint32).view(np.float32)
     out = np.where(nan, np.float32(np.nan), out)
-    return out.astype(a.dtype if a.dtype.kind == "f" else np.float32)
+    return out.astype(a.dtype if a.dtype.kind == "f" else np.float32).reshape(a.shape)      # a scalar stays one
 
 
 def _unbroadcast(g, shape):
@@ -61,8 +67,72 @@ def _unbroadcast(g, shape):
     return g.reshape(shape)
 
 
+def round_e4m3(a):
+    """Nearest e4m3 value, ties to even: steps of 2^(e-3) with e >= -6, magnitudes capped at 448, NaN kept."""
+    a = np.asarray(a, dtype=np.float64)
+    _, e = np.frexp(a)
+    step = np.exp2(np.maximum(e - 1, -6) - 3.0)
+    with np.errstate(invalid="ignore"):
+        return np.clip(np.rint(a / step) * step, -448.0, 448.0)
+
+
+def _attr(op, default=None):
+    return op["attrs"][0] if op.get("attrs") else default
+
+
+def _spread(s, shape, rows):
+    """Scales of rows x 128 blocks, one per element of a tensor of ``shape``."""
+    return np.repeat(np.repeat(s, rows, axis=0)[:shape[0]], 128, axis=1)[:, :shape[1]]
+
+
+def _scan_operands(op, ins):
+    seqs = int(_attr(op, 1))
+    rows, cols = ins[0].shape
+    h0 = next((a for a in ins[2:] if a.dtype.kind == "f"), None)
+    reset = next((a for a in ins[2:] if a.dtype.kind != "f"), None)
+    length = rows // seqs
+    shape = (seqs, length, cols)
+    fresh = np.zeros((seqs, length), dtype=bool) if reset is None else (reset.reshape(seqs, length) != 0)
+    start = np.zeros((seqs, cols), dtype=ins[0].dtype) if h0 is None else h0
+    f = 1 / (1 + np.exp(-ins[0].reshape(shape)))
+    keep = 1 / (1 + np.exp(ins[0].reshape(shape)))
+    return f, keep, ins[1].reshape(shape), start, fresh
+
+
+def _scan(op, ins):
+    """(states, state in front of every row), both [sequences, rows, columns]."""
+    f, keep, x, h, fresh = _scan_operands(op, ins)
+    out, before = np.empty_like(x), np.empty_like(x)
+    for t in range(x.shape[1]):
+        before[:, t] = np.where(fresh[:, t, None], 0.0, h)
+        h = f[:, t] * before[:, t] + keep[:, t] * x[:, t]
+        out[:, t] = h
+    return out, before
+
+
 def _forward(op, ins, dtype, bf16_contraction=True):
     t = op["type"]
+    if t == "RMSNorm":
+        return ins[0] / np.sqrt((ins[0] ** 2).mean(axis=-1, keepdims=True) + _attr(op, 1e-6)) * ins[1]
+    if t == "BlockScale":
+        rows = int(_attr(op, 1))
+        R, C = ins[0].shape
+        s = np.empty((-(-R // rows), -(-C // 128)), dtype=dtype)
+        for i in range(s.shape[0]):
+            for j in range(s.shape[1]):
+                s[i, j] = max(np.abs(ins[0][i * rows:(i + 1) * rows, j * 128:(j + 1) * 128]).max() / 448, 2.0 ** -126)
+        return s
+    if t == "Quantize":
+        return round_e4m3(ins[0] / _spread(ins[1], ins[0].shape, 1 if ins[1].shape[0] == ins[0].shape[0] else 128))
+    if t == "ScaledInnerProduct":
+        return (ins[0] * _spread(ins[1], ins[0].shape, 1)) @ (ins[2] * _spread(ins[3], ins[2].shape, 128)).T
+    if t == "GlobalNorm":
+        return np.asarray(np.sqrt(sum(float((a.astype(np.float64) ** 2).sum()) for a in ins)), dtype=dtype)
+    if t == "ClipByNorm":
+        limit = _attr(op)
+        return ins[0] * (limit / ins[1] if ins[1] > limit else 1.0)
+    if t == "GatedScan":
+        return _scan(op, ins)[0].reshape(ins[0].shape)
     if t == "Add":
         return ins[0] + ins[1]
     if t == "Sub":
@@ -106,7 +176,28 @@ def _backward(op, ins, out, dy, pos, bf16_contraction=True):
     """Gradients with respect to the operand positions in ``pos`` (un-reduced, operand-broadcast)."""
     t = op["type"]
     g = {}
-    if t == "Add":
+    if t == "RMSNorm":
+        h, gain = ins
+        r = 1 / np.sqrt((h ** 2).mean(axis=-1, keepdims=True) + _attr(op, 1e-6))
+        for p in pos:
+            d = dy * gain
+            g[p] = r * d - h * r ** 3 * (d * h).mean(axis=-1, keepdims=True) if p == 0 else dy * h * r
+    elif t == "GatedScan":
+        f, keep, x, _, fresh = _scan_operands(op, ins)
+        before = _scan(op, ins)[1]
+        dh, total = dy.reshape(x.shape), np.empty_like(x)
+        d = np.zeros_like(x[:, 0])
+        for k in reversed(range(x.shape[1])):
+            total[:, k] = dh[:, k] + d
+            d = np.where(fresh[:, k, None], 0.0, total[:, k] * f[:, k])
+        for p in pos:
+            if p == 0:
+                g[p] = (total * (before - x) * f * keep).reshape(ins[0].shape)
+            elif p == 1:
+                g[p] = (total * keep).reshape(ins[0].shape)
+            else:
+                g[p] = d
+    elif t == "Add":
         for p in pos:
             g[p] = dy
     elif t == "Sub":

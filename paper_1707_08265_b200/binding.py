@@ -14,11 +14,12 @@ LIB_PATH = os.environ.get("DRAGON_LIB") or os.path.join(HERE, "libdragon.so")
 OK = 0
 ERR_INVALID_ARG, ERR_SHAPE, ERR_DTYPE, ERR_NOT_SSA, ERR_MISSING_INPUT = -1, -2, -3, -4, -5
 ERR_NO_PATH, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = -6, -7, -8, -9, -10
-F32, BF16, I32 = 0, 1, 2
-DTYPES = {"f32": F32, "bf16": BF16, "i32": I32}
+F32, BF16, I32, F8E4M3 = 0, 1, 2, 3
+DTYPES = {"f32": F32, "bf16": BF16, "i32": I32, "f8e4m3": F8E4M3}
 OPS = {"Add": 0, "Sub": 1, "Mul": 2, "Div": 3, "Sin": 4, "Exp": 5, "Tanh": 6, "Sigmoid": 7, "ReLU": 8,
        "Sum": 9, "Mean": 10, "InnerProduct": 11, "BiasAdd": 12, "SoftmaxCrossEntropy": 13, "Sqrt": 14,
-       "Reciprocal": 15, "Opaque": 16}
+       "Reciprocal": 15, "Opaque": 16, "RMSNorm": 17, "BlockScale": 18, "Quantize": 19, "ScaledInnerProduct": 20,
+       "GlobalNorm": 21, "ClipByNorm": 22, "GatedScan": 23}
 
 _lib = None
 
@@ -124,8 +125,10 @@ class Graph:
             raise DragonError(r, "dragon_add_tensor")
         return r
 
-    def add_op(self, op_type, ins, outs):
-        r = lib().dragon_add_op(self.h, op_type, _ids(ins), len(ins), _ids(outs), len(outs), None, 0)
+    def add_op(self, op_type, ins, outs, attrs=()):
+        """attrs: the operator's numbers (include/dragon.h), or nothing for their defaults."""
+        nums = (_c.c_double * len(attrs))(*attrs) if len(attrs) else None
+        r = lib().dragon_add_op(self.h, op_type, _ids(ins), len(ins), _ids(outs), len(outs), nums, len(attrs))
         if r < 0:
             raise DragonError(r, "dragon_add_op")
         return r
@@ -170,7 +173,7 @@ class Graph:
             # operators whose outputs are all declared can be appended now (creation order)
             while next_op < len(desc["ops"]) and max(desc["ops"][next_op]["out"]) <= t:
                 op = desc["ops"][next_op]
-                oid = g.add_op(OPS[op["type"]], op["in"], op["out"])
+                oid = g.add_op(OPS[op["type"]], op["in"], op["out"], op.get("attrs", ()))
                 assert oid == next_op
                 next_op += 1
         assert next_op == len(desc["ops"])

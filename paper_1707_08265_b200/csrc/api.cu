@@ -2,8 +2,10 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
+#include <limits>
 #include <new>
 
 #include "plan.h"
@@ -23,6 +25,15 @@ cudaError_t launch_transpose16(const void* in, void* out, int rows, int cols, cu
 int launch_gemm_bf16(const void* A, const void* B, void* C, int c_dtype, int M, int N, int K, bool a_mn, bool b_mn, int* status,
                      cudaStream_t st, const void* bias, int bias_dtype, bool relu, const void* mask,
                      const std::vector<EpiSpec>& epi, const std::vector<MemRef>& mems, void* const* mem_ptr, float* colpart);
+cudaError_t launch_norm(const StepRun& r);
+cudaError_t launch_norm_bwd(const StepRun& r);
+cudaError_t launch_quant(const StepRun& r);
+cudaError_t launch_global_norm(const StepRun& r);
+cudaError_t launch_clip_factor(const StepRun& r);
+cudaError_t launch_clip(const StepRun& r);
+cudaError_t launch_scan(const StepRun& r);
+cudaError_t launch_scan_bwd(const StepRun& r);
+int launch_gemm_e4m3(const StepRun& r);   // a DRAGON_* code, message set
 }  // namespace dragon
 
 using namespace dragon;
@@ -31,7 +42,23 @@ namespace {
 
 bool valid_tensor(const dragon_graph_t* g, dragon_id t) { return t >= 0 && t < (int)g->g.tensors.size(); }
 
-int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, Shape* out) {
+// The operator's number from dragon_add_op's attrs: its default where none is given, checked for its range
+int resolve_attr(int type, const double* attrs, int n_attrs, double* out) {
+  *out = type == DRAGON_OP_RMS_NORM ? 1e-6 : (type == DRAGON_OP_BLOCK_SCALE || type == DRAGON_OP_GATED_SCAN) ? 1.0 : 0.0;
+  const bool takes = type == DRAGON_OP_RMS_NORM || type == DRAGON_OP_BLOCK_SCALE || type == DRAGON_OP_GATED_SCAN || type == DRAGON_OP_CLIP_BY_NORM;
+  if (!takes) return DRAGON_OK;            // an operator without a number ignores attrs
+  if (n_attrs > 1 || (n_attrs == 1 && !attrs)) { set_error("dragon_add_op: this operator takes one number"); return DRAGON_ERR_INVALID_ARG; }
+  if (n_attrs == 1) *out = attrs[0];
+  bool ok = std::isfinite(*out);
+  if (type == DRAGON_OP_RMS_NORM) ok = ok && *out >= 0.0 && (float)*out <= std::numeric_limits<float>::max();
+  if (type == DRAGON_OP_BLOCK_SCALE) ok = ok && (*out == 1.0 || *out == 128.0);
+  if (type == DRAGON_OP_GATED_SCAN) ok = ok && *out >= 1.0 && *out <= 2147483647.0 && *out == std::floor(*out);
+  if (type == DRAGON_OP_CLIP_BY_NORM) ok = ok && n_attrs == 1 && (float)*out >= std::numeric_limits<float>::min() && *out <= (double)std::numeric_limits<float>::max();
+  if (!ok) { set_error("dragon_add_op: the number of operator type %d is missing or out of range", type); return DRAGON_ERR_INVALID_ARG; }
+  return DRAGON_OK;
+}
+
+int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, double attr, Shape* out) {
   auto T = [&](int p) -> const TensorInfo& { return g.tensors[in[p]]; };
   auto is_float = [&](int p) { return T(p).dtype == DRAGON_F32 || T(p).dtype == DRAGON_BF16; };
   switch (type) {
@@ -66,6 +93,83 @@ int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, Shape* 
       if (T(0).shape.rank != 2 || T(1).shape.rank != 1 || T(0).shape.d[0] != T(1).shape.d[0]) { set_error("SoftmaxCrossEntropy needs Z[M,N], labels[M]"); return DRAGON_ERR_SHAPE; }
       *out = Shape();
       return DRAGON_OK;
+    case DRAGON_OP_RMS_NORM:
+      if (n_in != 2) { set_error("RMSNorm takes 2 inputs"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || !is_float(1)) { set_error("RMSNorm takes f32/bf16 tensors"); return DRAGON_ERR_DTYPE; }
+      if (T(0).shape.rank < 1 || T(1).shape.rank != 1 || T(1).shape.d[0] != T(0).shape.cols()) { set_error("RMSNorm needs h[R,C] or h[C], g[C]"); return DRAGON_ERR_SHAPE; }
+      if (T(0).shape.rows() > 0x7fffffffLL || T(0).shape.cols() > kMaxRowLength) { set_error("RMSNorm: too many rows or columns"); return DRAGON_ERR_UNSUPPORTED; }
+      *out = T(0).shape;
+      return DRAGON_OK;
+    case DRAGON_OP_BLOCK_SCALE:
+      if (n_in != 1) { set_error("BlockScale takes 1 input"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0)) { set_error("BlockScale takes an f32/bf16 tensor"); return DRAGON_ERR_DTYPE; }
+      if (T(0).shape.rank != 2) { set_error("BlockScale needs x[R,C]"); return DRAGON_ERR_SHAPE; }
+      if (T(0).shape.d[0] > 0x7fffffffLL || T(0).shape.d[1] > kMaxRowLength) { set_error("BlockScale: too many rows or columns"); return DRAGON_ERR_UNSUPPORTED; }
+      out->rank = 2; out->d[0] = (T(0).shape.d[0] + (int64_t)attr - 1) / (int64_t)attr; out->d[1] = (T(0).shape.d[1] + 127) / 128;
+      return DRAGON_OK;
+    case DRAGON_OP_QUANTIZE: {
+      if (n_in != 2) { set_error("Quantize takes 2 inputs"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || T(1).dtype != DRAGON_F32) { set_error("Quantize takes an f32/bf16 tensor and f32 scales"); return DRAGON_ERR_DTYPE; }
+      const Shape &x = T(0).shape, &s = T(1).shape;
+      if (x.rank != 2 || s.rank != 2 || s.d[1] != (x.d[1] + 127) / 128 || (s.d[0] != x.d[0] && s.d[0] != (x.d[0] + 127) / 128)) {
+        set_error("Quantize needs x[R,C] and scales [R or ceil(R/128), ceil(C/128)]");
+        return DRAGON_ERR_SHAPE;
+      }
+      if (x.d[0] > 0x7fffffffLL || x.d[1] > kMaxRowLength) { set_error("Quantize: too many rows or columns"); return DRAGON_ERR_UNSUPPORTED; }
+      *out = x;
+      return DRAGON_OK;
+    }
+    case DRAGON_OP_SCALED_INNER_PRODUCT: {
+      if (n_in != 4) { set_error("ScaledInnerProduct takes 4 inputs"); return DRAGON_ERR_INVALID_ARG; }
+      if (T(0).dtype != DRAGON_F8E4M3 || T(2).dtype != DRAGON_F8E4M3 || T(1).dtype != DRAGON_F32 || T(3).dtype != DRAGON_F32) {
+        set_error("ScaledInnerProduct takes e4m3 operands and f32 scales");
+        return DRAGON_ERR_DTYPE;
+      }
+      const Shape &x = T(0).shape, &sx = T(1).shape, &w = T(2).shape, &sw = T(3).shape;
+      if (x.rank != 2 || w.rank != 2 || sx.rank != 2 || sw.rank != 2 || x.d[1] != w.d[1]) { set_error("ScaledInnerProduct needs X[M,K], sx, W[N,K], sw"); return DRAGON_ERR_SHAPE; }
+      const int64_t kb = (x.d[1] + 127) / 128;
+      if (sx.d[0] != x.d[0] || sx.d[1] != kb || sw.d[0] != (w.d[0] + 127) / 128 || sw.d[1] != kb) {
+        set_error("ScaledInnerProduct: scales must be sx[M, ceil(K/128)] and sw[ceil(N/128), ceil(K/128)]");
+        return DRAGON_ERR_SHAPE;
+      }
+      if (x.d[1] & 15) { set_error("ScaledInnerProduct: K must be a multiple of 16"); return DRAGON_ERR_UNSUPPORTED; }
+      if (x.d[0] > kMaxProductExtent || w.d[0] > kMaxProductExtent || x.d[1] > kMaxProductExtent) { set_error("ScaledInnerProduct: an extent is too large"); return DRAGON_ERR_UNSUPPORTED; }
+      out->rank = 2; out->d[0] = x.d[0]; out->d[1] = w.d[0];
+      return DRAGON_OK;
+    }
+    case DRAGON_OP_GLOBAL_NORM:
+      for (int p = 0; p < n_in; ++p)
+        if (!is_float(p)) { set_error("GlobalNorm takes f32/bf16 tensors"); return DRAGON_ERR_DTYPE; }
+      *out = Shape();
+      return DRAGON_OK;
+    case DRAGON_OP_CLIP_BY_NORM:
+      if (n_in != 2) { set_error("ClipByNorm takes 2 inputs"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || T(1).dtype != DRAGON_F32) { set_error("ClipByNorm takes an f32/bf16 tensor and an f32 norm"); return DRAGON_ERR_DTYPE; }
+      if (T(1).shape.rank != 0) { set_error("ClipByNorm: the norm must be a scalar"); return DRAGON_ERR_SHAPE; }
+      *out = T(0).shape;
+      return DRAGON_OK;
+    case DRAGON_OP_GATED_SCAN: {
+      if (n_in < 2 || n_in > 4) { set_error("GatedScan takes gate, x and optionally h0 and reset"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || !is_float(1)) { set_error("GatedScan takes f32/bf16 tensors"); return DRAGON_ERR_DTYPE; }
+      const Shape &a = T(0).shape, &x = T(1).shape;
+      const int64_t seqs = (int64_t)attr;
+      if (a.rank != 2 || x != a || a.d[0] % seqs) { set_error("GatedScan needs gate[T,C] and x[T,C] with T a multiple of the number of sequences"); return DRAGON_ERR_SHAPE; }
+      if (a.d[0] > 0x7fffffffLL - kScanTileRows || a.d[1] > kMaxRowLength) { set_error("GatedScan: too many rows or columns"); return DRAGON_ERR_UNSUPPORTED; }
+      int p = 2;
+      if (p < n_in && T(p).dtype != DRAGON_I32) {
+        if (!is_float(p)) { set_error("GatedScan: h0 must be an f32/bf16 tensor"); return DRAGON_ERR_DTYPE; }
+        if (T(p).shape.rank != 2 || T(p).shape.d[0] != seqs || T(p).shape.d[1] != a.d[1]) { set_error("GatedScan: h0 must be [sequences, C]"); return DRAGON_ERR_SHAPE; }
+        ++p;
+      }
+      if (p < n_in) {
+        if (T(p).dtype != DRAGON_I32) { set_error("GatedScan: reset must be an int32 tensor behind h0"); return DRAGON_ERR_DTYPE; }
+        if (T(p).shape.rank != 1 || T(p).shape.d[0] != a.d[0]) { set_error("GatedScan: reset must be [T]"); return DRAGON_ERR_SHAPE; }
+        ++p;
+      }
+      if (p != n_in) { set_error("GatedScan takes gate, x and optionally h0 and reset, in this order"); return DRAGON_ERR_INVALID_ARG; }
+      *out = a;
+      return DRAGON_OK;
+    }
     default:
       set_error("unknown operator type %d", type);
       return DRAGON_ERR_INVALID_ARG;
@@ -92,7 +196,7 @@ void dragon_graph_destroy(dragon_graph_t* g) { delete g; }
 
 dragon_id dragon_add_tensor(dragon_graph_t* g, const char* name, int dtype, int rank, const int64_t* shape) {
   if (!g || !name || rank < 0 || rank > 2 || (rank > 0 && !shape)) { set_error("dragon_add_tensor: bad argument"); return DRAGON_ERR_INVALID_ARG; }
-  if (dtype != DRAGON_F32 && dtype != DRAGON_BF16 && dtype != DRAGON_I32) { set_error("dragon_add_tensor: unknown dtype %d", dtype); return DRAGON_ERR_DTYPE; }
+  if (dtype != DRAGON_F32 && dtype != DRAGON_BF16 && dtype != DRAGON_I32 && dtype != DRAGON_F8E4M3) { set_error("dragon_add_tensor: unknown dtype %d", dtype); return DRAGON_ERR_DTYPE; }
   TensorInfo t;
   t.name = name;
   t.dtype = dtype;
@@ -108,7 +212,6 @@ dragon_id dragon_add_tensor(dragon_graph_t* g, const char* name, int dtype, int 
 
 dragon_id dragon_add_op(dragon_graph_t* g, int op_type, const dragon_id* in, int n_in, const dragon_id* out, int n_out,
                         const double* attrs, int n_attrs) {
-  (void)attrs;
   if (!g || !in || !out || n_in <= 0 || n_out <= 0 || n_attrs < 0) { set_error("dragon_add_op: bad argument"); return DRAGON_ERR_INVALID_ARG; }
   for (int i = 0; i < n_in; ++i)
     if (!valid_tensor(g, in[i])) { set_error("dragon_add_op: input id %d is not a tensor", in[i]); return DRAGON_ERR_INVALID_ARG; }
@@ -128,17 +231,22 @@ dragon_id dragon_add_op(dragon_graph_t* g, int op_type, const dragon_id* in, int
     if (to.consumed) { set_error("dragon_add_op: tensor '%s' is already read by an earlier operator", to.name.c_str()); return DRAGON_ERR_NOT_SSA; }
     if (to.dtype == DRAGON_I32) { set_error("dragon_add_op: operators produce f32/bf16 tensors"); return DRAGON_ERR_DTYPE; }
   }
+  double attr = 0.0;
   if (op_type != DRAGON_OP_OPAQUE) {
     const TensorInfo& to = g->g.tensors[out[0]];
     Shape s;
-    int rc = infer_shape(g->g, op_type, in, n_in, &s);
+    int rc = resolve_attr(op_type, attrs, n_attrs, &attr);
+    if (rc == DRAGON_OK) rc = infer_shape(g->g, op_type, in, n_in, attr, &s);
     if (rc != DRAGON_OK) return rc;
+    if ((op_type == DRAGON_OP_QUANTIZE) != (to.dtype == DRAGON_F8E4M3)) { set_error("dragon_add_op: Quantize, and nothing else, produces an e4m3 tensor"); return DRAGON_ERR_DTYPE; }
+    if ((op_type == DRAGON_OP_BLOCK_SCALE || op_type == DRAGON_OP_GLOBAL_NORM) && to.dtype != DRAGON_F32) { set_error("dragon_add_op: scales and norms are f32 tensors"); return DRAGON_ERR_DTYPE; }
     if (s != to.shape) { set_error("dragon_add_op: declared shape of '%s' differs from the inferred one", to.name.c_str()); return DRAGON_ERR_SHAPE; }
   }
   OpInfo op;
   op.type = op_type;
   op.in.assign(in, in + n_in);
   op.out.assign(out, out + n_out);
+  op.attr = attr;
   g->g.ops.push_back(op);
   for (int i = 0; i < n_in; ++i) g->g.tensors[in[i]].consumed = true;
   for (int j = 0; j < n_out; ++j) g->g.tensors[out[j]].producer = (int)g->g.ops.size() - 1;
@@ -151,12 +259,12 @@ int dragon_add_grad(dragon_graph_t* g, const dragon_id* objs, int n_obj, const d
   GradStage st;
   for (int i = 0; i < n_obj; ++i) {
     if (!valid_tensor(g, objs[i]) || g->g.tensors[objs[i]].grad_stage >= 0) { set_error("dragon_add_grad: bad objective id %d", objs[i]); return DRAGON_ERR_INVALID_ARG; }
-    if (g->g.tensors[objs[i]].dtype == DRAGON_I32) { set_error("dragon_add_grad: objective must be a float tensor"); return DRAGON_ERR_DTYPE; }
+    if ((g->g.tensors[objs[i]].dtype == DRAGON_I32 || g->g.tensors[objs[i]].dtype == DRAGON_F8E4M3)) { set_error("dragon_add_grad: objective must be a float tensor"); return DRAGON_ERR_DTYPE; }
     st.objs.push_back(objs[i]);
   }
   for (int i = 0; i < n_wrt; ++i) {
     if (!valid_tensor(g, wrts[i]) || g->g.tensors[wrts[i]].grad_stage >= 0) { set_error("dragon_add_grad: bad derivative target id %d", wrts[i]); return DRAGON_ERR_INVALID_ARG; }
-    if (g->g.tensors[wrts[i]].dtype == DRAGON_I32) { set_error("dragon_add_grad: derivative target must be a float tensor"); return DRAGON_ERR_DTYPE; }
+    if ((g->g.tensors[wrts[i]].dtype == DRAGON_I32 || g->g.tensors[wrts[i]].dtype == DRAGON_F8E4M3)) { set_error("dragon_add_grad: derivative target must be a float tensor"); return DRAGON_ERR_DTYPE; }
     st.wrts.push_back(wrts[i]);
   }
   std::vector<uint8_t> G = backward_chain_marks(g->g, st.objs, st.wrts);
@@ -273,7 +381,22 @@ int dragon_function_used_inputs(const dragon_function_t* f, uint8_t* flags, int 
 int dragon_function_can_alias(const dragon_function_t* f, int input, int output) {
   if (!f || input < 0 || input >= f->n_in || output < 0 || output >= f->n_out) { set_error("dragon_function_can_alias: bad argument"); return DRAGON_ERR_INVALID_ARG; }
   const Plan& P = f->plan;
-  if (!f->not_executable.empty() || P.steps.size() != 1 || P.steps[0].kind != ST_VM) return 0;
+  if (!f->not_executable.empty()) return 0;
+  if (!P.steps.empty() && P.steps.back().kind == ST_CLIP) {
+    // the sums read every tensor in launches of their own; the clipping launch then reads and writes element by element
+    for (size_t k = 0; k + 1 < P.steps.size(); ++k)
+      if (P.steps[k].kind != ST_GNORM) return 0;
+    const Step& cs = P.steps.back();
+    int reads = 0, pairs = 0;
+    for (size_t k = 0; k < cs.wr.size(); ++k) {
+      const MemRef &mi = P.mems[cs.rd[cl::FIRST + k]], &mo = P.mems[cs.wr[k]];
+      if (mi.where != MEM_FEED || mi.index != input) continue;
+      ++reads;
+      pairs += mo.where == MEM_FETCH && mo.index == output && mo.dtype == mi.dtype;
+    }
+    return reads == 1 && pairs == 1 ? 1 : 0;
+  }
+  if (P.steps.size() != 1 || P.steps[0].kind != ST_VM) return 0;
   const VmSegment& sg = P.segs[P.steps[0].seg];
   if (sg.row_mode) return 0;
   const std::vector<VmAccess> acc = vm_operand_accesses(sg);
@@ -326,6 +449,9 @@ int dragon_function_num_launches(const dragon_function_t* f) {
   for (const Step& st : f->plan.steps) {
     if (st.kind == ST_VM) n += 1 + (f->plan.segs[st.seg].finish.empty() ? 0 : 1);
     else if (st.kind == ST_SCE_FWD) n += 2 + (st.mF >= 0 ? 1 : 0);
+    else if (st.kind == ST_NORM_BWD) n += 1 + (st.wr[nb::DGAIN] >= 0 ? 1 : 0);
+    else if (st.kind == ST_GNORM) n += launches_of_tensors((int)st.rd.size());
+    else if (st.kind == ST_CLIP) n += launches_of_tensors((int)st.wr.size());
     else if (st.kind != ST_COPY) n += 1 + (st.mF >= 0 ? 1 : 0);
   }
   return n;
@@ -541,6 +667,24 @@ int dragon_run(dragon_function_t* f, const void* const* feeds, void* const* fetc
       case ST_COPY:
         e = cudaMemcpyAsync(ptr[s.mC], ptr[s.mA], P.mems[s.mA].bytes(), cudaMemcpyDeviceToDevice, st);
         break;
+      default: {
+        const StepRun r{s, P.mems, ptr.data(), ws, status, next_cleared ? nullptr : status_next, reinterpret_cast<unsigned*>(word0 + 32), P.sm_count, cuda_stream};
+        next_cleared = true;
+        switch (s.kind) {
+          case ST_NORM: e = launch_norm(r); break;
+          case ST_NORM_BWD: e = launch_norm_bwd(r); break;
+          case ST_QUANT: e = launch_quant(r); break;
+          case ST_GNORM: e = launch_global_norm(r); break;
+          case ST_FACTOR: e = launch_clip_factor(r); break;
+          case ST_CLIP: e = launch_clip(r); break;
+          case ST_SCAN: e = launch_scan(r); break;
+          case ST_SCAN_BWD: e = launch_scan_bwd(r); break;
+          default: {
+            const int rc = launch_gemm_e4m3(r);
+            if (rc != DRAGON_OK) { f->status_ready = false; return rc; }
+          }
+        }
+      }
     }
     if (prof) {
       if (s.kind != ST_VM) cudaEventRecord(reinterpret_cast<cudaEvent_t>(f->prof_ev[2 * f->prof_used + 1]), st);

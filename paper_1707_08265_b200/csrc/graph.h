@@ -38,7 +38,17 @@ struct TensorInfo {
 struct OpInfo {
   int type = 0;
   std::vector<int> in, out;
+  double attr = 0.0;      // the operator's number (dragon.h: attrs), its default filled in
 };
+
+// bytes of one element of a tensor type
+inline size_t dtype_bytes(int dtype) { return dtype == DRAGON_F8E4M3 ? 1 : dtype == DRAGON_BF16 ? 2 : 4; }
+
+// operators through which no gradient is generated
+inline bool has_no_gradient(int type) {
+  return type == DRAGON_OP_BLOCK_SCALE || type == DRAGON_OP_QUANTIZE || type == DRAGON_OP_SCALED_INNER_PRODUCT ||
+         type == DRAGON_OP_GLOBAL_NORM || type == DRAGON_OP_CLIP_BY_NORM;
+}
 
 struct GradStage {
   std::vector<int> objs, wrts, grad_ids;

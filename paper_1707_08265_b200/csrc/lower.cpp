@@ -28,6 +28,8 @@ struct Lowerer {
   std::map<std::pair<int, int>, int> materialised;   // (value, dtype) -> memref
   std::vector<std::map<int, int>> pending;    // per stage: tensor -> gradient contributions still to come
   std::map<int, int> def_item;                // value -> index of the micro-operation that defines it
+  std::map<int, int> writer;                  // memory -> index of the item of a kind from IT_NORM on that writes it
+  std::map<int, int> scan_item;               // GatedScan operator -> its item
   int err = DRAGON_OK;
 
   Lowerer(const Graph& g_, const PruneResult& pr_, Plan* p) : g(g_), pr(pr_), plan(p) {}
@@ -202,6 +204,159 @@ struct Lowerer {
     else accum(v, m);
   }
 
+  // ---- operators of language models: one item each, or a place in an item that is there already -------------
+  int add_item(int kind, std::vector<int> rd, std::vector<int> wr, double attr) {
+    Item x; x.kind = kind; x.rd = std::move(rd); x.wr = std::move(wr); x.attr = attr;
+    items.push_back(x);
+    const int i = (int)items.size() - 1;
+    for (int m : items[i].wr) if (m >= 0) writer[m] = i;
+    return i;
+  }
+  // memory of an operator's result: the fetch buffer, or a workspace tensor
+  int out_mem(int o) {
+    const TensorInfo& t = g.tensors[o];
+    return new_mem(fetch_of[o] >= 0 ? MEM_FETCH : MEM_WORK, fetch_of[o], t.dtype, t.shape);
+  }
+  int in_mem(int t, int dtype = -1) {
+    const int v = fval[t];
+    if (fetch_of[t] >= 0 && vals[v].kind == VK_OP && (dtype < 0 || dtype == g.tensors[t].dtype))
+      for (const Item& s : items)      // a fetched tensor's buffer is an image of it
+        if (s.kind == IT_MOP && s.opc == M_STORE && s.a == v && plan->mems[s.mem].where == MEM_FETCH) return s.mem;
+    return materialise(v, dtype, g.tensors[t].dtype);
+  }
+  // the item of the given kind that writes memory m at position pos of its results, or null
+  Item* writer_of(int m, int kind, int pos) {
+    auto it = writer.find(m);
+    if (it == writer.end()) return nullptr;
+    Item& x = items[it->second];
+    return x.kind == kind && x.wr[pos] == m ? &x : nullptr;
+  }
+  // The residual's addition in front of a norm: h is the value of an Add of two tensors in memory of h's shape (rounded
+  // or not) of which no image has been made yet.  The norm's kernel then adds, and writes h if anything needs it.
+  bool sum_in_memory(int t, int* mX, int* mR) {
+    const int v = fval[t], p = g.tensors[t].producer;
+    if (p < 0 || g.ops[p].type != DRAGON_OP_ADD || vals[v].kind != VK_OP || materialised.count({v, g.tensors[t].dtype})) return false;
+    auto it = def_item.find(v);
+    if (it == def_item.end()) return false;
+    const Item* d = &items[it->second];
+    if (d->opc == M_RBF16) {
+      it = def_item.find(d->a);
+      if (it == def_item.end()) return false;
+      d = &items[it->second];
+    }
+    if (d->opc != M_ADD) return false;
+    for (int o : {d->a, d->b})
+      if (vals[o].kind != VK_MEM || vals[o].shape != g.tensors[t].shape || plan->mems[vals[o].mem].shape != g.tensors[t].shape) return false;
+    // the sum with a contraction's fp32 product is better off in that contraction's epilogue: the product never reaches memory
+    for (int o : {d->a, d->b})
+      for (const Item& x : items)
+        if (x.kind == IT_GEMM && x.mC == vals[o].mem && plan->mems[x.mC].where == MEM_WORK && plan->mems[x.mC].dtype == DRAGON_F32) return false;
+    *mX = vals[d->a].mem;
+    *mR = vals[d->b].mem;
+    return true;
+  }
+
+  void lower_norm(const OpInfo& op) {
+    const int th = op.in[0], o = op.out[0];
+    int mX = -1, mR = -1, mH = -1;
+    if (sum_in_memory(th, &mX, &mR)) {
+      const int v = fval[th];
+      for (Item& s : items)      // the store of a fetched h moves into the norm's kernel
+        if (s.kind == IT_MOP && s.opc == M_STORE && s.a == v && plan->mems[s.mem].where == MEM_FETCH) { mH = s.mem; s.opc = -1; }
+      if (mH < 0) mH = new_mem(MEM_WORK, -1, g.tensors[th].dtype, g.tensors[th].shape);
+      fval[th] = new_val(VK_MEM, g.tensors[th].shape, mH);
+    } else {
+      mX = in_mem(th);
+    }
+    const int mG = in_mem(op.in[1]), mY = out_mem(o);
+    const int i = add_item(IT_NORM, {mX, mR, mG}, {mH, mY, -1, -1}, op.attr);
+    items[i].sum_dtype = g.tensors[th].dtype;
+    items[i].round_dtype = g.tensors[o].dtype;
+    fval[o] = new_val(VK_MEM, g.tensors[o].shape, mY);
+  }
+
+  // scales of x: in the pass of the norm that makes x, otherwise a pass of their own
+  void lower_block_scale(const OpInfo& op) {
+    const int o = op.out[0], mX = in_mem(op.in[0]), mS = out_mem(o);
+    Item* norm = op.attr == 1.0 ? writer_of(mX, IT_NORM, nm::Y) : nullptr;
+    if (norm && norm->wr[nm::S] < 0) {
+      norm->wr[nm::S] = mS;
+      writer[mS] = writer[mX];
+    } else {
+      add_item(IT_QUANT, {mX, -1}, {mS, -1}, op.attr);
+    }
+    fval[o] = new_val(VK_MEM, g.tensors[o].shape, mS);
+  }
+  void lower_quantize(const OpInfo& op) {
+    const int o = op.out[0], mX = in_mem(op.in[0]), mS = in_mem(op.in[1], DRAGON_F32), mQ = out_mem(o);
+    Item *norm = writer_of(mS, IT_NORM, nm::S), *quant = writer_of(mS, IT_QUANT, qt::S);
+    if (norm && norm->wr[nm::Y] == mX && norm->wr[nm::Q] < 0) { norm->wr[nm::Q] = mQ; writer[mQ] = writer[mS]; }
+    else if (quant && quant->rd[qt::X] == mX && quant->wr[qt::Q] < 0) { quant->wr[qt::Q] = mQ; writer[mQ] = writer[mS]; }
+    else add_item(IT_QUANT, {mX, mS}, {-1, mQ}, plan->mems[mS].shape.d[0] == plan->mems[mX].shape.d[0] ? 1.0 : 128.0);
+    fval[o] = new_val(VK_MEM, g.tensors[o].shape, mQ);
+  }
+
+  // A fetched clipped tensor joins the one launch of its norm and limit; one that only operators read is a factor
+  // (a scalar in memory, written behind the norm) in their program.
+  void lower_clip(const OpInfo& op) {
+    const int o = op.out[0];
+    const TensorInfo& to = g.tensors[o];
+    const int mN = in_mem(op.in[1], DRAGON_F32);
+    if (fetch_of[o] >= 0) {
+      const int mT = in_mem(op.in[0]), mC = out_mem(o);
+      fval[o] = new_val(VK_MEM, to.shape, mC);
+      if (plan->mems[mT].where == MEM_FEED)      // in memory before everything else
+        for (int i = 0; i < (int)items.size(); ++i)
+          if (items[i].kind == IT_CLIP && items[i].rd[cl::NORM] == mN && items[i].attr == op.attr) {
+            items[i].rd.push_back(mT);
+            items[i].wr.push_back(mC);
+            writer[mC] = i;
+            return;
+          }
+      add_item(IT_CLIP, {mN, mT}, {mC}, op.attr);
+      return;
+    }
+    int mF = -1;
+    for (Item& x : items)
+      if (x.kind == IT_FACTOR && x.rd[0] == mN && x.attr == op.attr) mF = x.wr[0];
+    Item* norm = writer_of(mN, IT_GNORM, gn::NORM);
+    if (mF < 0 && norm && norm->wr[gn::FACTOR] >= 0 && norm->attr == op.attr) mF = norm->wr[gn::FACTOR];
+    if (mF < 0) {
+      mF = new_mem(MEM_WORK, -1, DRAGON_F32, Shape());
+      if (norm && norm->wr[gn::FACTOR] < 0) { norm->wr[gn::FACTOR] = mF; norm->attr = op.attr; writer[mF] = writer[mN]; }
+      else add_item(IT_FACTOR, {mN}, {mF}, op.attr);
+    }
+    int v = mop(M_MUL, fval[op.in[0]], new_val(VK_MEM, Shape(), mF));
+    if (to.dtype == DRAGON_BF16) v = mop(M_RBF16, v);
+    fval[o] = v;
+  }
+
+  void lower_scan(int k, const OpInfo& op) {
+    const int o = op.out[0];
+    const Shape& s = g.tensors[o].shape;
+    int mH0 = -1, mReset = -1;
+    for (size_t p = 2; p < op.in.size(); ++p) (g.tensors[op.in[p]].dtype == DRAGON_I32 ? mReset : mH0) = in_mem(op.in[p]);
+    Shape tiles; tiles.rank = 2; tiles.d[0] = (s.d[0] + kScanTileRows - 1) / kScanTileRows; tiles.d[1] = s.d[1];
+    const int mG = in_mem(op.in[0]), mX = in_mem(op.in[1]), mH = out_mem(o), mCarry = new_mem(MEM_WORK, -1, DRAGON_F32, tiles);
+    scan_item[k] = add_item(IT_SCAN, {mG, mX, mH0, mReset}, {mH, mCarry}, op.attr);
+    fval[o] = new_val(VK_MEM, s, mH);
+  }
+
+  // whether the gradient of tensor t reaches a derivative target unchanged (through additions): it is then kept in f32
+  bool reaches_target(int s, int t) const {
+    const auto& wr = g.stages[s].wrts;
+    if (std::find(wr.begin(), wr.end(), t) != wr.end()) return true;
+    const int p = g.tensors[t].producer;
+    if (p < 0 || (g.ops[p].type != DRAGON_OP_ADD && g.ops[p].type != DRAGON_OP_SUB && g.ops[p].type != DRAGON_OP_BIAS_ADD)) return false;
+    for (int i : g.ops[p].in)
+      if (pr.in_G[s][i] && reaches_target(s, i)) return true;
+    return false;
+  }
+  int grad_mem(int s, int t) {   // memory of the gradient with respect to t, as an operator's kernel writes it
+    const TensorInfo& ti = g.tensors[t];
+    return new_mem(MEM_WORK, -1, ti.dtype == DRAGON_BF16 && !reaches_target(s, t) ? DRAGON_BF16 : DRAGON_F32, ti.shape);
+  }
+
   void lower_forward(int k) {
     const OpInfo& op = g.ops[k];
     const int o = op.out[0];
@@ -241,6 +396,26 @@ struct Lowerer {
         fval[o] = new_val(VK_MEM, to.shape, mC);
         return;
       }
+      case DRAGON_OP_RMS_NORM: lower_norm(op); return;
+      case DRAGON_OP_BLOCK_SCALE: lower_block_scale(op); return;
+      case DRAGON_OP_QUANTIZE: lower_quantize(op); return;
+      case DRAGON_OP_SCALED_INNER_PRODUCT: {
+        std::vector<int> rd = {in_mem(op.in[0]), in_mem(op.in[1], DRAGON_F32), in_mem(op.in[2]), in_mem(op.in[3], DRAGON_F32)};
+        const int mY = out_mem(o);
+        add_item(IT_GEMM8, rd, {mY}, 0.0);
+        fval[o] = new_val(VK_MEM, to.shape, mY);
+        return;
+      }
+      case DRAGON_OP_GLOBAL_NORM: {
+        std::vector<int> rd;
+        for (int t : op.in) rd.push_back(in_mem(t));
+        const int mN = out_mem(o);
+        add_item(IT_GNORM, rd, {mN, -1}, 0.0);
+        fval[o] = new_val(VK_MEM, to.shape, mN);
+        return;
+      }
+      case DRAGON_OP_CLIP_BY_NORM: lower_clip(op); return;
+      case DRAGON_OP_GATED_SCAN: lower_scan(k, op); return;
       default:
         set_error("operator type %d cannot be lowered", op.type);
         err = DRAGON_ERR_UNSUPPORTED;
@@ -324,6 +499,36 @@ struct Lowerer {
         else x.mD = materialise(dy, DRAGON_F32, DRAGON_F32);
         items.push_back(x);
         add(0, new_val(VK_MEM, tz.shape, mdZ));
+        break;
+      }
+      case DRAGON_OP_RMS_NORM: {
+        // a contribution to dh that is there already (the residual branch's) is added in the same pass
+        int mSkip = -1;
+        auto have = gval[s].find(op.in[0]);
+        if (want[0] && op.in[0] != op.in[1] && have != gval[s].end() && vals[have->second].kind == VK_MEM &&
+            vals[have->second].shape == g.tensors[op.in[0]].shape)
+          mSkip = vals[have->second].mem;
+        const int mH = in_mem(op.in[0]), mdY = materialise(dy, -1, DRAGON_F32), mG = in_mem(op.in[1]);
+        const int mdH = want[0] ? grad_mem(s, op.in[0]) : -1, mdG = want[1] ? new_mem(MEM_WORK, -1, DRAGON_F32, g.tensors[op.in[1]].shape) : -1;
+        add_item(IT_NORM_BWD, {mH, mdY, mG, mSkip}, {mdH, mdG}, op.attr);
+        if (want[0]) {
+          const int v = new_val(VK_MEM, g.tensors[op.in[0]].shape, mdH);
+          if (mSkip >= 0) gval[s][op.in[0]] = v;
+          else add(0, v);
+        }
+        if (want[1]) add(1, new_val(VK_MEM, g.tensors[op.in[1]].shape, mdG));
+        break;
+      }
+      case DRAGON_OP_GATED_SCAN: {
+        const Item fwd = items[scan_item[r.op]];
+        const int mdY = materialise(dy, -1, DRAGON_F32);
+        const int pH0 = op.in.size() > 2 && g.tensors[op.in[2]].dtype != DRAGON_I32 ? 2 : -1;
+        const int mdG = want[0] ? grad_mem(s, op.in[0]) : -1, mdX = want[1] ? grad_mem(s, op.in[1]) : -1;
+        const int mdH0 = pH0 >= 0 && want[pH0] ? grad_mem(s, op.in[pH0]) : -1;
+        add_item(IT_SCAN_BWD, {fwd.rd[sc::GATE], fwd.rd[sc::X], fwd.rd[sc::H0], fwd.rd[sc::RESET], mdY, fwd.wr[sc::CARRY]}, {mdG, mdX, mdH0}, op.attr);
+        if (want[0]) add(0, new_val(VK_MEM, g.tensors[op.in[0]].shape, mdG));
+        if (want[1]) add(1, new_val(VK_MEM, g.tensors[op.in[1]].shape, mdX));
+        if (mdH0 >= 0) add(pH0, new_val(VK_MEM, g.tensors[op.in[pH0]].shape, mdH0));
         break;
       }
       default:
@@ -484,7 +689,8 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     if (mems[src].dtype != mems[dst].dtype || mems[src].shape != mems[dst].shape) continue;
     int writers = 0;
     for (const Item& w : items)
-      if ((w.kind != IT_MOP && w.mC == src) || (w.kind == IT_MOP && (w.opc == M_STORE || w.opc == M_ACCUM) && w.mem == src)) ++writers;
+      if ((w.kind != IT_MOP && (w.mC == src || std::count(w.wr.begin(), w.wr.end(), src))) ||
+          (w.kind == IT_MOP && (w.opc == M_STORE || w.opc == M_ACCUM) && w.mem == src)) ++writers;
     if (writers != 1) continue;
     mems[src].where = MEM_FETCH;
     mems[src].index = mems[dst].index;
@@ -506,6 +712,15 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       if (it.opc == M_STORE || it.opc == M_ACCUM) it.live = mems[it.mem].live;
       else it.live = val_live[it.dst] != 0;
       if (it.live) { use_val(it.a); use_val(it.b); }
+    } else if (it.kind >= IT_NORM) {
+      it.live = false;
+      for (int& m : it.wr) {
+        if (m >= 0 && !mems[m].live) m = -1;     // a result that nobody needs is not written
+        it.live |= m >= 0;
+      }
+      if (it.live)
+        for (int m : it.rd)
+          if (m >= 0) mems[m].live = true;
     } else {
       it.live = mems[it.mC].live;
       if (it.live)
@@ -594,7 +809,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     for (int i = 0; i < (int)items.size(); ++i) {
       const Item& it = items[i];
       if (!it.live) continue;
-      if (it.kind != IT_MOP) { if (it.mC == m || (it.kind == IT_SCE_FWD && it.mD == m)) w = std::max(w, i); }
+      if (it.kind != IT_MOP) { if (it.mC == m || (it.kind == IT_SCE_FWD && it.mD == m) || std::count(it.wr.begin(), it.wr.end(), m)) w = std::max(w, i); }
       else if ((it.opc == M_STORE || it.opc == M_ACCUM) && it.mem == m) w = std::max(w, runs_at(i));
     }
     return w;
@@ -645,7 +860,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       const Item& it = items[i];
       if (!it.live) continue;
       if (it.kind == IT_GEMM && it.mC == mP) producer = i;
-      if (it.kind != IT_MOP) { readers += (it.mA == mP) + (it.mB == mP) + (it.mD == mP); continue; }
+      if (it.kind != IT_MOP) { readers += (it.mA == mP) + (it.mB == mP) + (it.mD == mP) + (int)std::count(it.rd.begin(), it.rd.end(), mP); continue; }
       if (it.opc == M_WIDEN) continue;
       for (int v : {it.a, it.b})
         if (v >= 0 && root(v) >= 0 && vals[root(v)].kind == VK_MEM && vals[root(v)].mem == mP) ++readers;
@@ -698,7 +913,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       const Item& it = items[i];
       if (!it.live) continue;
       if (it.kind == IT_GEMM && it.mC == mP) producer = i;
-      if (it.kind != IT_MOP) { readers += (it.mA == mP) + (it.mB == mP) + (it.mD == mP) + (it.mE == mP); continue; }
+      if (it.kind != IT_MOP) { readers += (it.mA == mP) + (it.mB == mP) + (it.mD == mP) + (it.mE == mP) + (int)std::count(it.rd.begin(), it.rd.end(), mP); continue; }
       if (it.opc == M_WIDEN) continue;
       for (int v : {it.a, it.b})
         if (v >= 0 && root(v) >= 0 && vals[root(v)].kind == VK_MEM && vals[root(v)].mem == mP) ++readers;
@@ -810,7 +1025,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       if (!it.live) continue;
       if (it.kind == IT_GEMM && it.mC == mP) producer = i;
       if (it.kind != IT_MOP) {
-        readers += (it.mA == mP) + (it.mB == mP) + (it.mD == mP) + (it.mE == mP);
+        readers += (it.mA == mP) + (it.mB == mP) + (it.mD == mP) + (it.mE == mP) + (int)std::count(it.rd.begin(), it.rd.end(), mP);
         continue;
       }
       if (it.opc == M_WIDEN) continue;
@@ -878,7 +1093,8 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     }
     Step st;
     st.kind = it.kind == IT_GEMM ? ST_GEMM : it.kind == IT_TRANSPOSE ? ST_TRANSPOSE : it.kind == IT_SCE_FWD ? ST_SCE_FWD
-              : it.kind == IT_SCE_BWD ? ST_SCE_BWD : ST_COPY;
+              : it.kind == IT_SCE_BWD ? ST_SCE_BWD : it.kind == IT_COPY ? ST_COPY : ST_NORM + (it.kind - IT_NORM);
+    st.rd = it.rd; st.wr = it.wr; st.attr = it.attr; st.sum_dtype = it.sum_dtype; st.round_dtype = it.round_dtype;
     st.mA = it.mA; st.mB = it.mB; st.mC = it.mC; st.mD = it.mD; st.mE = it.mE; st.scale = it.scale; st.tA = it.tA; st.tB = it.tB;
     st.relu = it.relu;
     st.epi = it.epi;
@@ -926,6 +1142,16 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     sg.scalpart_off = take((size_t)kHostChunks * sg.n_scalacc * sg.grid * sizeof(double));   // a set per chunk of a chunked host run
   }
   for (auto& st : plan->steps) {
+    if (st.kind == ST_NORM_BWD && st.wr[nb::DGAIN] >= 0) {
+      const Shape& sh = mems[st.rd[nb::H]].shape;
+      st.n_colpart = norm_bwd_partials(sh.rows(), sh.cols(), sm_count);
+      st.colpart_off = take((size_t)st.n_colpart * sh.cols() * sizeof(float));
+    }
+    if (st.kind == ST_GNORM) st.scratch_off = take(global_norm_scratch_bytes((int)st.rd.size(), sm_count));
+    if (st.kind == ST_SCAN || st.kind == ST_SCAN_BWD) {
+      const Shape& sh = mems[st.rd[sc::GATE]].shape;
+      st.scratch_off = take(scan_scratch_bytes(sh.d[0], sh.d[1]));
+    }
     if (st.kind == ST_SCE_FWD) st.scratch_off = take((size_t)mems[st.mA].shape.d[0] * sizeof(float));
     if (st.mF >= 0) {   // partial column sums: one row per 32 output rows of a contraction, one per CTA of the softmax kernel
       const Shape& sc = mems[st.kind == ST_SCE_FWD ? st.mD : st.mC].shape;
@@ -968,6 +1194,8 @@ static size_t share_workspace(Plan* plan, size_t off) {
       if (st.kind == ST_SCE_FWD) touch(si, st.mD, true);
       touch(si, st.mC, true);
       touch(si, st.mF, true);
+      for (int m : st.rd) touch(si, m, false);
+      for (int m : st.wr) touch(si, m, true);
       continue;
     }
     const VmSegment& sg = plan->segs[st.seg];
@@ -1102,6 +1330,31 @@ std::string describe_plan(const Plan& p) {
         break;
       case ST_SCE_FWD: snprintf(buf, sizeof(buf), st.mD >= 0 ? "softmax_ce_fwd+bwd%s\n" : "softmax_ce_fwd%s\n", st.mF >= 0 ? " +colsum" : ""); break;
       case ST_SCE_BWD: snprintf(buf, sizeof(buf), "softmax_ce_bwd%s\n", st.mF >= 0 ? " +colsum" : ""); break;
+      case ST_NORM:
+        snprintf(buf, sizeof(buf), "rms_norm[%lldx%lld%s%s%s%s%s]\n", (long long)p.mems[st.rd[nm::X]].shape.rows(), (long long)p.mems[st.rd[nm::X]].shape.cols(),
+                 st.rd[nm::R] >= 0 ? " +residual" : "", st.wr[nm::H] >= 0 ? " ->sum" : "", st.wr[nm::Y] >= 0 ? " ->y" : "",
+                 st.wr[nm::S] >= 0 ? " ->scales" : "", st.wr[nm::Q] >= 0 ? " ->e4m3" : "");
+        break;
+      case ST_NORM_BWD:
+        snprintf(buf, sizeof(buf), "rms_norm_bwd[%lldx%lld%s%s%s]\n", (long long)p.mems[st.rd[nb::H]].shape.rows(), (long long)p.mems[st.rd[nb::H]].shape.cols(),
+                 st.rd[nb::SKIP] >= 0 ? " +residual gradient" : "", st.wr[nb::DH] >= 0 ? " ->dh" : "", st.wr[nb::DGAIN] >= 0 ? " ->dg" : "");
+        break;
+      case ST_QUANT:
+        snprintf(buf, sizeof(buf), "quantize[%lldx%lld blocks %dx128%s%s]\n", (long long)p.mems[st.rd[qt::X]].shape.d[0], (long long)p.mems[st.rd[qt::X]].shape.d[1],
+                 (int)st.attr, st.wr[qt::S] >= 0 ? " ->scales" : "", st.wr[qt::Q] >= 0 ? " ->e4m3" : "");
+        break;
+      case ST_GEMM8:
+        snprintf(buf, sizeof(buf), "gemm_e4m3[%lldx%lldx%lld -> %s]\n", (long long)p.mems[st.wr[g8::Y]].shape.d[0], (long long)p.mems[st.wr[g8::Y]].shape.d[1],
+                 (long long)p.mems[st.rd[g8::XQ]].shape.d[1], p.mems[st.wr[g8::Y]].dtype == DRAGON_BF16 ? "bf16" : "f32");
+        break;
+      case ST_GNORM: snprintf(buf, sizeof(buf), "global_norm[%d tensors%s]\n", (int)st.rd.size(), st.wr[gn::FACTOR] >= 0 ? " ->factor" : ""); break;
+      case ST_FACTOR: snprintf(buf, sizeof(buf), "clip_factor\n"); break;
+      case ST_CLIP: snprintf(buf, sizeof(buf), "clip_by_norm[%d tensors]\n", (int)st.wr.size()); break;
+      case ST_SCAN: case ST_SCAN_BWD:
+        snprintf(buf, sizeof(buf), "gated_scan%s[%lldx%lld, %d sequences%s%s%s]\n", st.kind == ST_SCAN ? "" : "_bwd", (long long)p.mems[st.rd[sc::GATE]].shape.d[0],
+                 (long long)p.mems[st.rd[sc::GATE]].shape.d[1], (int)st.attr, st.rd[sc::H0] >= 0 ? " +h0" : "", st.rd[sc::RESET] >= 0 ? " +reset" : "",
+                 st.kind == ST_SCAN && st.wr[sc::H] < 0 ? " states only" : "");
+        break;
       default: snprintf(buf, sizeof(buf), "copy\n");
     }
     s += buf;

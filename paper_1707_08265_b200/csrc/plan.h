@@ -36,7 +36,7 @@ struct MemRef {
   bool live = false;
   int first_step = -1, last_step = -1;   // plan steps that touch it first and last (MEM_WORK)
   int shares_input = 0;  // 1: written in place over an input of its producing step that dies there (Sec. 2.4)
-  size_t bytes() const { return (size_t)shape.numel() * (dtype == DRAGON_BF16 ? 2 : 4); }
+  size_t bytes() const { return (size_t)shape.numel() * dtype_bytes(dtype); }
 };
 
 enum MOpc {
@@ -73,7 +73,16 @@ struct EpiSpec {
 };
 constexpr int kMaxEpiOps = 8;
 
-enum ItemKind { IT_MOP, IT_GEMM, IT_TRANSPOSE, IT_SCE_FWD, IT_SCE_BWD, IT_COPY };
+enum ItemKind { IT_MOP, IT_GEMM, IT_TRANSPOSE, IT_SCE_FWD, IT_SCE_BWD, IT_COPY,
+                IT_NORM, IT_NORM_BWD, IT_QUANT, IT_GEMM8, IT_GNORM, IT_FACTOR, IT_CLIP, IT_SCAN, IT_SCAN_BWD };
+// Memory operands of the kinds from IT_NORM on, by position in Item::rd and Item::wr (-1: absent, or a result nobody needs)
+namespace nm { enum { X, R, GAIN }; enum { H, Y, S, Q }; }                        // IT_NORM: h = x + r (r absent: h = x), y; s, q of y
+namespace nb { enum { H, DY, GAIN, SKIP }; enum { DH, DGAIN }; }                  // IT_NORM_BWD: dh = skip + the norm's gradient
+namespace qt { enum { X, SIN }; enum { S, Q }; }                                  // IT_QUANT: scales of x, and x in them (or in given ones)
+namespace g8 { enum { XQ, SX, WQ, SW }; enum { Y }; }                             // IT_GEMM8
+namespace gn { enum { NORM, FACTOR }; }                                           // IT_GNORM: rd = the tensors; factor = min(1, attr / norm)
+namespace cl { enum { NORM, FIRST }; }                                            // IT_CLIP: rd = norm, tensors; wr = the clipped tensors
+namespace sc { enum { GATE, X, H0, RESET, DH, CARRY_IN }; enum { H, CARRY }; enum { DGATE, DX, DH0 }; }   // IT_SCAN, IT_SCAN_BWD
 struct Item {
   int kind = IT_MOP;
   // IT_MOP
@@ -87,6 +96,10 @@ struct Item {
   bool tA = false, tB = false;             // GEMM: operand given transposed ([K, M] / [K, N] row-major)
   bool relu = false;                       // GEMM: max(., 0) in the epilogue
   std::vector<EpiSpec> epi;                // GEMM: further elementwise operations on the accumulator, in order
+  std::vector<int> rd, wr;                 // memory operands of the kinds from IT_NORM on (positions: see there)
+  double attr = 0.0;                       // their number: eps, block rows, limit, sequences
+  int sum_dtype = DRAGON_F32;              // IT_NORM: the declared types of h and of y: both are rounded to them whether or not they are
+  int round_dtype = DRAGON_F32;            //   written (the norm reads the rounded h, the scales and e4m3 values are of the rounded y)
   bool live = false;
   int segment = -1;
 };
@@ -121,7 +134,8 @@ struct VmSegment {
   std::string spec_log;             // why it failed
 };
 
-enum StepKind { ST_VM, ST_GEMM, ST_TRANSPOSE, ST_SCE_FWD, ST_SCE_BWD, ST_COPY };
+enum StepKind { ST_VM, ST_GEMM, ST_TRANSPOSE, ST_SCE_FWD, ST_SCE_BWD, ST_COPY,
+                ST_NORM, ST_NORM_BWD, ST_QUANT, ST_GEMM8, ST_GNORM, ST_FACTOR, ST_CLIP, ST_SCAN, ST_SCAN_BWD };
 struct Step {
   int kind;
   int seg = -1;                          // ST_VM
@@ -133,8 +147,20 @@ struct Step {
   int mF = -1;                           // ST_GEMM / ST_SCE_*: row vector receiving the column sums of the written tensor
   int n_colpart = 0;                     // ... partial rows the kernel writes for it (fixed by the launch shape)
   size_t colpart_off = 0;                // ... and where: float [n_colpart][cols] in the workspace
-  size_t scratch_off = 0;                // SCE_FWD: per-row losses
+  size_t scratch_off = 0;                // SCE_FWD: per-row losses; GNORM: partial sums; SCAN: what tiles hand on
+  std::vector<int> rd, wr;               // kinds from ST_NORM on: as in Item
+  double attr = 0.0;
+  int sum_dtype = DRAGON_F32, round_dtype = DRAGON_F32;
 };
+
+// Scratch sizes and launch shapes of the language-model kernels (their .cu files) that the workspace layout needs
+constexpr int64_t kMaxRowLength = 1 << 26, kMaxProductExtent = 1 << 26;   // what the kernels' 32-bit column and row indices hold
+constexpr int kScanTileRows = 128;       // rows of one tile of GatedScan; the gradient reads the state in front of each
+int norm_bwd_partials(int64_t rows, int64_t cols, int sm_count);   // rows of partial gain gradients that the norm's gradient leaves
+size_t global_norm_scratch_bytes(int n_tensors, int sm_count);
+size_t scan_scratch_bytes(int64_t rows, int64_t cols);
+constexpr int kTensorsPerLaunch = 256;   // tensors that one launch of GlobalNorm or ClipByNorm takes in its parameters
+inline int launches_of_tensors(int n) { return (n + kTensorsPerLaunch - 1) / kTensorsPerLaunch; }
 
 struct Plan {
   std::vector<MemRef> mems;
@@ -143,6 +169,24 @@ struct Plan {
   size_t workspace_bytes = 0;
   size_t status_off = 0;
   int sm_count = kDefaultSmCount;
+};
+
+// What the launcher of a step of the kinds from ST_NORM on gets: the step, where its memory is, the run's status
+// word and (for the first kernel of a run that clears it) the next run's.
+struct StepRun {
+  const Step& s;
+  const std::vector<MemRef>& mems;
+  void* const* ptr;
+  char* ws;
+  int* status;
+  int* status_clear;
+  unsigned* counter;      // a word that is zero before and after every kernel (grid-wide "last block" tickets)
+  int sm_count;
+  void* stream;
+  void* rd(int i) const { return s.rd[i] >= 0 ? ptr[s.rd[i]] : nullptr; }
+  void* wr(int i) const { return s.wr[i] >= 0 ? ptr[s.wr[i]] : nullptr; }
+  int rd_type(int i) const { return s.rd[i] >= 0 ? mems[s.rd[i]].dtype : DRAGON_F32; }
+  int wr_type(int i) const { return s.wr[i] >= 0 ? mems[s.wr[i]].dtype : DRAGON_F32; }
 };
 
 int lower_function(const Graph& g, const PruneResult& pr, const std::vector<int>& inputs,

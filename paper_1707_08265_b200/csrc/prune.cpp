@@ -154,6 +154,15 @@ int prune_function(const Graph& g, const std::vector<int>& inputs, const std::ve
     for (int o : g.ops[k].out) keep |= out->marked[o] != 0;
     if (keep) out->fwd_ops.push_back(k);
   }
+  for (int s = 0; s < n_st; ++s)     // a wanted gradient that would have to pass an operator without one
+    for (int k = 0; k < n_ops; ++k) {
+      if (!gop[s][k] || !has_no_gradient(g.ops[k].type)) continue;
+      for (int i : g.ops[k].in)
+        if (out->in_G[s][i] && out->gmark[s][i]) {
+          set_error("the gradient with respect to '%s' would have to pass operator %d, which has none", g.tensors[i].name.c_str(), k);
+          return DRAGON_ERR_UNSUPPORTED;
+        }
+    }
   out->grad_ops.clear();
   for (int s = 0; s < n_st; ++s)
     for (int k = n_ops - 1; k >= 0; --k) {

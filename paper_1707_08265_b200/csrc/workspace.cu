@@ -10,6 +10,7 @@
 
 #include "plan.h"
 
+using dragon::dtype_bytes;
 using dragon::set_error;
 
 namespace {
@@ -21,8 +22,6 @@ struct Entry {
   void* ptr = nullptr;    // current contents
   void* spare = nullptr;  // second buffer of a tensor that a function overwrites but cannot update in place
 };
-
-size_t dtype_bytes(int dtype) { return dtype == DRAGON_BF16 ? 2 : 4; }
 
 }  // namespace
 
@@ -92,7 +91,7 @@ size_t dragon_workspace_bytes(const dragon_workspace_t* w) { return w ? w->bytes
 int dragon_workspace_feed(dragon_workspace_t* w, const char* name, int dtype, int rank, const int64_t* shape, const void* src,
                           void* cuda_stream) {
   if (!w || !name || rank < 0 || rank > 2 || (rank > 0 && !shape)) { set_error("dragon_workspace_feed: bad argument"); return DRAGON_ERR_INVALID_ARG; }
-  if (dtype != DRAGON_F32 && dtype != DRAGON_BF16 && dtype != DRAGON_I32) { set_error("dragon_workspace_feed: unknown type %d", dtype); return DRAGON_ERR_DTYPE; }
+  if (dtype != DRAGON_F32 && dtype != DRAGON_BF16 && dtype != DRAGON_I32 && dtype != DRAGON_F8E4M3) { set_error("dragon_workspace_feed: unknown type %d", dtype); return DRAGON_ERR_DTYPE; }
   dragon::Shape s;
   s.rank = rank;
   for (int i = 0; i < rank; ++i) {

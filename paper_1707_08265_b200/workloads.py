@@ -27,7 +27,8 @@ class GraphDesc:
     """Builder of the neutral graph description.
 
     ``desc`` = {"tensors": [{"name","dtype","shape"}], "ops": [{"type","in","out"}],
-    "grads": [{"objs","wrts","grad_ids"}]}; ids are list positions (creation order).
+    "grads": [{"objs","wrts","grad_ids"}]}; ids are list positions (creation order).  An operator
+    with numbers of its own (eps, block rows, limit, sequences) has them as "attrs".
     """
 
     def __init__(self):
@@ -40,11 +41,13 @@ class GraphDesc:
     def shape(self, t):
         return self.desc["tensors"][t]["shape"]
 
-    def op(self, type_, ins, out_name, out_shape=None, out_dtype="f32"):
+    def op(self, type_, ins, out_name, out_shape=None, out_dtype="f32", attrs=()):
         if out_shape is None:
             out_shape = _broadcast_shape([self.shape(i) for i in ins])
         o = self.tensor(out_name, out_shape, out_dtype)
         self.desc["ops"].append({"type": type_, "in": [int(i) for i in ins], "out": [o]})
+        if attrs:
+            self.desc["ops"][-1]["attrs"] = [float(a) for a in attrs]
         return o
 
     def grad(self, objs, wrts):
