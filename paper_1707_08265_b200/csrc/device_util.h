@@ -1,16 +1,22 @@
 // Device helpers of the language-model kernels: 8 elements at a time in any float type, e4m3 rounding, reductions.
 #pragma once
+#include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 #include "../../include/dragon.h"
-#include "vm_math.h"
 
 namespace dragon {
 
 __device__ __forceinline__ float bf16_low(unsigned w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ unsigned bf16_pair(float lo, float hi) { return vmmath::bf16_bits(lo) | (vmmath::bf16_bits(hi) << 16); }
+// nearest bf16, ties to even, by the conversion instruction
+__device__ __forceinline__ unsigned bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const unsigned*>(&v);
+}
+__device__ __forceinline__ unsigned short bf16_one(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+__device__ __forceinline__ float bf16_rounded(float v) { return bf16_low(bf16_one(v)); }
 
 // V consecutive elements (V = 8: 16-byte aligned, or V = 1) as they are in memory, so that loads can be issued
 // together and converted later
@@ -65,7 +71,7 @@ template <int V> __device__ __forceinline__ void store_any(void* p, int dtype, s
     }
   } else {
     if (dtype == DRAGON_F32) reinterpret_cast<float*>(p)[i] = v[0];
-    else reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)vmmath::bf16_bits(v[0]);
+    else reinterpret_cast<unsigned short*>(p)[i] = bf16_one(v[0]);
   }
 }
 

@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_kernel(const NormArgs a) 
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         if (RDT >= 0) h[k][e] += r[e];
-        if (a.sum_dt == DRAGON_BF16) h[k][e] = vmmath::round_bf16(h[k][e]);
+        if (a.sum_dt == DRAGON_BF16) h[k][e] = bf16_rounded(h[k][e]);
         sum.x += h[k][e] * h[k][e];
       }
       if (a.h) store_any<V>(a.h, a.sum_dt, base + j, h[k]);
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_kernel(const NormArgs a) 
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       y[e] = mine ? h[k][e] * rstd * g[k][e] : 0.f;
-      if (a.ydt == DRAGON_BF16) y[e] = vmmath::round_bf16(y[e]);
+      if (a.ydt == DRAGON_BF16) y[e] = bf16_rounded(y[e]);
       m = max(m, magnitude(y[e]));
     }
     if (mine && a.y) store_any<V>(a.y, a.ydt, base + j, y);
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_loop_kernel(const NormArg
     float h, r = 0.f;
     load_any<1>(a.x, a.xdt, base + j, &h);
     if (a.r) { load_any<1>(a.r, a.rdt, base + j, &r); h += r; }
-    return a.sum_dt == DRAGON_BF16 ? vmmath::round_bf16(h) : h;
+    return a.sum_dt == DRAGON_BF16 ? bf16_rounded(h) : h;
   };
   float2 sum = make_float2(0.f, 0.f);
   for (int j = threadIdx.x; j < a.cols; j += kMaxRowThreads) {
@@ -162,7 +162,7 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_loop_kernel(const NormArg
         float g;
         load_any<1>(a.gain, a.gdt, j, &g);
         y[e] = sum_at(j) * rstd * g;
-        if (a.ydt == DRAGON_BF16) y[e] = vmmath::round_bf16(y[e]);
+        if (a.ydt == DRAGON_BF16) y[e] = bf16_rounded(y[e]);
         if (a.y) store_any<1>(a.y, a.ydt, base + j, &y[e]);
       }
       m = max(m, magnitude(y[e]));

@@ -155,7 +155,7 @@ struct Step {
 
 // Scratch sizes and launch shapes of the language-model kernels (their .cu files) that the workspace layout needs
 constexpr int64_t kMaxRowLength = 1 << 26, kMaxProductExtent = 1 << 26;   // what the kernels' 32-bit column and row indices hold
-constexpr int kScanTileRows = 128;       // rows of one tile of GatedScan; the gradient reads the state in front of each
+constexpr int kScanTileRows = 64;       // rows of one tile of GatedScan; the gradient reads the state in front of each
 int norm_bwd_partials(int64_t rows, int64_t cols, int sm_count);   // rows of partial gain gradients that the norm's gradient leaves
 size_t global_norm_scratch_bytes(int n_tensors, int sm_count);
 size_t scan_scratch_bytes(int64_t rows, int64_t cols);
