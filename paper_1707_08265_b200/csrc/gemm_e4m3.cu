@@ -1,60 +1,475 @@
 // ScaledInnerProduct  Y[m,n] = sum_b sx[m,b] sw[n/128,b] sum_{k in block b} Xq[m,k] Wq[n,k]: e4m3 operands with a scale for
-// each block of 128 along K, fp32 accumulation, fp32 or bf16 output.
+// each block of 128 along K, fp32 accumulation, fp32 or bf16 output.  Hand-written for sm_100a.
+//
+// The scales change every 128 elements of K, so the tensor unit may accumulate over one block only (four
+// tcgen05.mma.kind::f8f6f4 of K = 32).  Two TMEM accumulators alternate: while the tensor unit works on block b + 1, the
+// epilogue warps read block b's sums with tcgen05.ld and add them, times their scale, to fp32 registers (packed FMAs).
+// A tile of 128 x 256 costs the tensor unit 512 cycles a block and the epilogue 64 packed FMAs a thread and a block, so
+// the addition hides behind the products.  One block is one TMA stage (128-byte rows, 128-byte swizzle).
+//
+//   gemm_e4m3_kernel      many rows: tiles of 128 rows of X x 256 rows of W; a thread holds one row of Y, its scale is one number
+//                         a block; persistent CTAs in an L2-friendly tile order; bound by the tensor unit
+//   gemm_e4m3_few_kernel  few rows: the operands change places (128 rows of W x 16..128 rows of X), so that the tile's height is
+//                         filled by weights and hardly any product is wasted; the K blocks of a tile are split over the
+//                         CTAs of a cluster, whose partial sums meet in shared memory in a fixed order; bound by the bytes of W
+// Every wait is bounded; when one runs out the kernel records DRAGON_ERR_TIMEOUT, lets its copies and products in flight
+// land, frees its TMEM and returns.
 #include <algorithm>
+#include <cstdlib>
 
 #include "device_util.h"
 #include "plan.h"
+#include "tcgen05_util.h"
 
 namespace dragon {
 namespace {
 
-struct Gemm8Args {
-  const unsigned char *x, *w;
-  const float *sx, *sw;
-  void* y;
-  int ydt, M, N, K, kb;
-  int* status_clear;
-};
+constexpr int kBlockK = 128;        // one scale block = one 128-byte swizzle row of e4m3 = one stage
+constexpr int kUmmaK = 32;
 
-__device__ __forceinline__ float e4m3_value(unsigned char b) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(b, __NV_E4M3)));
+// instruction descriptor of kind::f8f6f4: D = f32, A = B = e4m3 (both codes 0), K-major, M x N
+constexpr uint32_t idesc_e4m3(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+
+__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// acc (two neighbouring columns) += v * s
+__device__ __forceinline__ void fma_pair(float2& acc, uint32_t v0, uint32_t v1, float s0, float s1) {
+  unsigned long long a, v, s;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "f"(acc.x), "f"(acc.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(v0), "r"(v1));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(s) : "f"(s0), "f"(s1));
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(v), "l"(s));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(acc.x), "=f"(acc.y) : "l"(a));
 }
 
-// 32 x 32 outputs per CTA, one per thread
-__global__ void __launch_bounds__(1024) gemm_e4m3_simple_kernel(const Gemm8Args g) {
-  __shared__ float xs[32][33], ws[32][33];
-  if (g.status_clear && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *g.status_clear = 0;
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const long long m = (long long)blockIdx.y * 32 + ty;
-  const int n = blockIdx.x * 32 + tx;
-  float acc = 0.f;
-  for (int b = 0; b < g.kb; ++b) {
-    float part = 0.f;
-    for (int k0 = b * 128; k0 < std::min(g.K, (b + 1) * 128); k0 += 32) {
-      const int k = k0 + tx;
-      const int wn = blockIdx.x * 32 + ty;
-      xs[ty][tx] = m < g.M && k < g.K ? e4m3_value(g.x[(size_t)m * g.K + k]) : 0.f;
-      ws[ty][tx] = wn < g.N && k < g.K ? e4m3_value(g.w[(size_t)wn * g.K + k]) : 0.f;
-      __syncthreads();
-      for (int i = 0; i < 32; ++i) part += xs[ty][i] * ws[tx][i];
-      __syncthreads();
-    }
-    if (m < g.M && n < g.N) acc += part * (g.sx[(size_t)m * g.kb + b] * g.sw[(size_t)(n >> 7) * g.kb + b]);
+struct Gemm8Args {
+  const float *sx, *sw;
+  void* y;
+  int ydt, M, N, K, kb;        // kb: blocks along K
+  int tiles_m, tiles_n;
+  int split;                   // few rows: CTAs of a cluster that share a tile's blocks
+  int* status;
+  int* status_clear;
+  long long wait_budget;
+  int drop_first_load;         // failure-detection test: the first stage's signal never comes
+};
+
+// barriers and flags of a CTA, behind its stages
+struct Sync {
+  uint32_t full, empty, part_full, part_empty, drain;
+  uint32_t* tmem_slot;
+  volatile int* abort_flag;
+};
+__device__ __forceinline__ Sync sync_area(unsigned char* p, int stages) {
+  uint64_t* bars = reinterpret_cast<uint64_t*>(p);
+  Sync s;
+  s.full = smem_u32(bars);
+  s.empty = s.full + 8 * stages;
+  s.part_full = s.empty + 8 * stages;
+  s.part_empty = s.part_full + 16;
+  s.drain = s.part_empty + 16;
+  s.tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * stages + 5);
+  s.abort_flag = reinterpret_cast<volatile int*>(s.tmem_slot + 1);
+  return s;
+}
+__device__ __forceinline__ void sync_init(const Sync& s, int stages, int epilogue_warps) {
+  for (int i = 0; i < stages; ++i) { mbar_init(s.full + 8 * i, 1); mbar_init(s.empty + 8 * i, 1); }
+  for (int b = 0; b < 2; ++b) { mbar_init(s.part_full + 8 * b, 1); mbar_init(s.part_empty + 8 * b, epilogue_warps); }
+  mbar_init(s.drain, 1);
+  s.abort_flag[0] = 0;
+  s.abort_flag[1] = 0;         // nobody sets this one: for waits that must not be cut short
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
+__device__ __forceinline__ bool wait_or_abort(const Sync& s, const Gemm8Args& g, uint32_t bar, uint32_t parity) {
+  if (mbar_wait(bar, parity, s.abort_flag, g.wait_budget)) return true;
+  *s.abort_flag = 1;
+  atomicExch(g.status, DRAGON_ERR_TIMEOUT);
+  return false;
+}
+// the copies that nobody consumed must land before the shared memory goes away (full budget, whatever the pipeline's is)
+__device__ __forceinline__ void drain_copies(const Sync& s, int first, int issued, int stages) {
+  for (int i = max(first, issued > stages ? issued - stages : 0); i < issued; ++i) mbar_wait(s.full + 8 * (i % stages), (i / stages) & 1, s.abort_flag + 1);
+}
+
+// ... and the products in flight (the thread that issued them) before their operands and the TMEM do
+__device__ __forceinline__ void drain_products(const Sync& s) {
+  umma_commit(s.drain);
+  mbar_wait(s.drain, 0, s.abort_flag + 1);
+}
+
+// The MMA issuer's work on one block: wait for an accumulator and the stage, four products, hand both on
+__device__ __forceinline__ bool issue_block(const Sync& s, const Gemm8Args& g, int it, int stages, uint32_t a_addr, uint32_t b_addr, uint32_t tmem, int columns, uint32_t idesc) {
+  const int buf = it & 1, st = it % stages;
+  if (!wait_or_abort(s, g, s.part_empty + 8 * buf, ((it >> 1) & 1) ^ 1)) return false;
+  if (!wait_or_abort(s, g, s.full + 8 * st, (it / stages) & 1)) return false;
+  fence_after();
+  const uint64_t a = make_smem_desc(a_addr), b = make_smem_desc(b_addr);
+#pragma unroll
+  for (int k = 0; k < kBlockK / kUmmaK; ++k) umma_e4m3(tmem + buf * columns, a + 2 * k, b + 2 * k, idesc, k > 0 ? 1u : 0u);   // 32 bytes along the swizzle row
+  umma_commit(s.empty + 8 * st);
+  umma_commit(s.part_full + 8 * buf);
+  return true;
+}
+
+// ---- many rows ------------------------------------------------------------------------------------------------
+
+constexpr int kTileM = 128, kTileN = 256, kStages = 4;
+constexpr int kThreads = 320;                                   // TMA, MMA, 8 epilogue warps
+constexpr uint32_t kBytesA = kTileM * kBlockK, kBytesB = kTileN * kBlockK, kStageBytes = kBytesA + kBytesB;
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 256;
+
+__global__ void __launch_bounds__(kThreads, 1)
+gemm_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const Gemm8Args g) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), tiles = (raw + 1023u) & ~1023u;
+  const Sync s = sync_area(smem_raw + (tiles - raw) + (size_t)kStages * kStageBytes, kStages);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n_tiles = g.tiles_m * g.tiles_n;
+  if (threadIdx.x == 0) {
+    sync_init(s, kStages, 8);
+    if (g.status_clear && blockIdx.x == 0) *g.status_clear = 0;
   }
-  if (m < g.M && n < g.N) store_any<1>(g.y, g.ydt, (size_t)m * g.N + n, &acc);
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s.tmem_slot)), "r"((uint32_t)(2 * kTileN)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *s.tmem_slot;
+  int issued = 0, first_issued = 0;
+  if (warp == 0) {
+    if (lane == 0) {
+      bool ok = true;
+      for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x) {
+        int tm, tn;
+        tile_coords(t, g.tiles_m, g.tiles_n, &tm, &tn);
+        for (int b = 0; b < g.kb; ++b, ++issued) {
+          const int st = issued % kStages;
+          if (!wait_or_abort(s, g, s.empty + 8 * st, ((issued / kStages) & 1) ^ 1)) { ok = false; break; }
+          if (g.drop_first_load && issued == 0) { first_issued = 1; continue; }
+          const uint32_t dst = tiles + (uint32_t)st * kStageBytes;
+          mbar_expect_tx(s.full + 8 * st, kStageBytes);
+          tma_load_2d(dst, &tmap_x, b * kBlockK, tm * kTileM, s.full + 8 * st);
+          tma_load_2d(dst + kBytesA, &tmap_w, b * kBlockK, tn * kTileN, s.full + 8 * st);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int it = 0;
+      bool ok = true;
+      for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x)
+        for (int b = 0; b < g.kb && ok; ++b, ++it) {
+          const uint32_t a = tiles + (uint32_t)(it % kStages) * kStageBytes;
+          ok = issue_block(s, g, it, kStages, a, a + kBytesA, tmem, kTileN, idesc_e4m3(kTileM, kTileN));
+        }
+    }
+  } else {
+    // warp w reads TMEM lanes 32 (w % 4) .. + 31 (rows of the tile) and one half of the columns (one 128-row block of W)
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    int it = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x) {
+      int tm, tn;
+      tile_coords(t, g.tiles_m, g.tiles_n, &tm, &tn);
+      const int row = tm * kTileM + q * 32 + lane, col0 = tn * kTileN + half * 128;
+      const float* sx = g.sx + (size_t)min(row, g.M - 1) * g.kb;
+      const float* sw = g.sw + (size_t)min(col0 / 128, (g.N - 1) / 128) * g.kb;
+      float2 acc[64];
+#pragma unroll
+      for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
+      float sc = __ldg(sx) * __ldg(sw);
+      for (int b = 0; b < g.kb; ++b, ++it) {
+        const int buf = it & 1;
+        const int ahead = min(b + 1, g.kb - 1);
+        const float next_x = __ldg(sx + ahead), next_w = __ldg(sw + ahead);
+        ok = __all_sync(0xffffffffu, mbar_wait(s.part_full + 8 * buf, (it >> 1) & 1, s.abort_flag, g.wait_budget));
+        if (!ok) { if (lane == 0) { *s.abort_flag = 1; atomicExch(g.status, DRAGON_ERR_TIMEOUT); } break; }
+        fence_after();
+        const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * kTileN + half * 128);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t v[32];
+          tmem_ld32(from + 32 * c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) fma_pair(acc[16 * c + j], v[2 * j], v[2 * j + 1], sc, sc);
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s.part_empty + 8 * buf);
+        sc = next_x * next_w;
+      }
+      if (!ok || row >= g.M) continue;
+      if (g.ydt == DRAGON_F32) {
+        float* out = reinterpret_cast<float*>(g.y) + (size_t)row * g.N + col0;
+        if ((g.N & 3) == 0 && col0 + 128 <= g.N) {
+#pragma unroll
+          for (int j = 0; j < 64; j += 2) *reinterpret_cast<float4*>(out + 2 * j) = make_float4(acc[j].x, acc[j].y, acc[j + 1].x, acc[j + 1].y);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 64; ++j) {
+            if (col0 + 2 * j < g.N) out[2 * j] = acc[j].x;
+            if (col0 + 2 * j + 1 < g.N) out[2 * j + 1] = acc[j].y;
+          }
+        }
+      } else {
+        unsigned short* out = reinterpret_cast<unsigned short*>(g.y) + (size_t)row * g.N + col0;
+        if ((g.N & 7) == 0 && col0 + 128 <= g.N) {
+#pragma unroll
+          for (int j = 0; j < 64; j += 4)
+            *reinterpret_cast<uint4*>(out + 2 * j) = make_uint4(bf16_pair(acc[j].x, acc[j].y), bf16_pair(acc[j + 1].x, acc[j + 1].y),
+                                                                bf16_pair(acc[j + 2].x, acc[j + 2].y), bf16_pair(acc[j + 3].x, acc[j + 3].y));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 64; ++j) {
+            if (col0 + 2 * j < g.N) out[2 * j] = bf16_one(acc[j].x);
+            if (col0 + 2 * j + 1 < g.N) out[2 * j + 1] = bf16_one(acc[j].y);
+          }
+        }
+      }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (*s.abort_flag) {
+    if (threadIdx.x == 0) drain_copies(s, first_issued, issued, kStages);
+    if (threadIdx.x == 32) drain_products(s);
+    __syncthreads();
+  }
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * kTileN)) : "memory");
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------------
+
+constexpr int kFewThreads = 192;                                // TMA, MMA, 4 epilogue warps
+constexpr int few_stages(int nt) { return nt <= 32 ? 5 : nt == 64 ? 4 : 3; }      // two CTAs fit an SM
+constexpr uint32_t few_stage_bytes(int nt) { return (128 + nt) * kBlockK; }
+constexpr size_t few_smem(int nt) { return 1024 + (size_t)few_stages(nt) * few_stage_bytes(nt) + 256 + 2 * nt * sizeof(float); }
+
+template <int NT>
+__global__ void __launch_bounds__(kFewThreads, 2)
+gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const Gemm8Args g) {
+  constexpr int kSt = few_stages(NT);
+  constexpr uint32_t kSB = few_stage_bytes(NT), kColumns = 2 * NT < 32 ? 32 : 2 * NT;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), tiles = (raw + 1023u) & ~1023u;
+  unsigned char* base = smem_raw + (tiles - raw);
+  const Sync s = sync_area(base + (size_t)kSt * kSB, kSt);
+  float* scales = reinterpret_cast<float*>(base + (size_t)kSt * kSB + 256);      // two blocks' scales of the NT rows of X
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n0 = blockIdx.x * 128, m0 = blockIdx.y * NT, part = blockIdx.z;
+  const int b0 = (int)((long long)g.kb * part / g.split), b1 = (int)((long long)g.kb * (part + 1) / g.split);
+  if (threadIdx.x == 0) {
+    sync_init(s, kSt, 4);
+    if (g.status_clear && blockIdx.x == 0 && blockIdx.y == 0 && part == 0) *g.status_clear = 0;
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s.tmem_slot)), "r"(kColumns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *s.tmem_slot;
+  int issued = 0, first_issued = 0;
+  float2 acc[NT / 2];          // epilogue: row n0 + its TMEM lane of W, NT rows of X
+#pragma unroll
+  for (int j = 0; j < NT / 2; ++j) acc[j] = make_float2(0.f, 0.f);
+  const int q = warp & 3, e = q * 32 + lane;      // epilogue warps 2..5: quadrants 2, 3, 0, 1
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int b = b0; b < b1; ++b, ++issued) {
+        const int st = issued % kSt;
+        if (!wait_or_abort(s, g, s.empty + 8 * st, ((issued / kSt) & 1) ^ 1)) break;
+        if (g.drop_first_load && issued == 0) { first_issued = 1; continue; }
+        const uint32_t dst = tiles + (uint32_t)st * kSB;
+        mbar_expect_tx(s.full + 8 * st, kSB);
+        tma_load_2d(dst, &tmap_w, b * kBlockK, n0, s.full + 8 * st);
+        tma_load_2d(dst + 128 * kBlockK, &tmap_x, b * kBlockK, m0, s.full + 8 * st);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      bool ok = true;
+      for (int it = 0; it < b1 - b0 && ok; ++it) {
+        const uint32_t a = tiles + (uint32_t)(it % kSt) * kSB;
+        ok = issue_block(s, g, it, kSt, a, a + 128 * kBlockK, tmem, NT, idesc_e4m3(128, NT));
+      }
+    }
+  } else {
+    const float* sw = g.sw + (size_t)blockIdx.x * g.kb;
+    const bool has_scale = e < NT && m0 + e < g.M;
+    const float* sx = g.sx + (size_t)(has_scale ? m0 + e : 0) * g.kb;
+    float mine = has_scale ? __ldg(sx + b0) * __ldg(sw + b0) : 0.f;
+    if (e < NT) scales[e] = mine;
+    bool ok = true;
+    for (int it = 0; it < b1 - b0; ++it) {
+      const int buf = it & 1, ahead = min(b0 + it + 1, b1 - 1);
+      if (has_scale) mine = __ldg(sx + ahead) * __ldg(sw + ahead);
+      asm volatile("bar.sync 1, 128;" ::: "memory");       // this block's scales are there, the other buffer is free
+      ok = __all_sync(0xffffffffu, ok && mbar_wait(s.part_full + 8 * buf, (it >> 1) & 1, s.abort_flag, g.wait_budget));
+      if (!ok) {                                           // (the barrier above counts every warp in every turn)
+        if (lane == 0) { *s.abort_flag = 1; atomicExch(g.status, DRAGON_ERR_TIMEOUT); }
+        continue;
+      }
+      fence_after();
+      const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * NT);
+      const float4* sc = reinterpret_cast<const float4*>(scales + buf * NT);
+#pragma unroll
+      for (int c = 0; c < NT / 16; ++c) {
+        uint32_t v[16];
+        tmem_ld16(from + 16 * c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float4 f = sc[4 * c + j];
+          fma_pair(acc[8 * c + 2 * j], v[4 * j], v[4 * j + 1], f.x, f.y);
+          fma_pair(acc[8 * c + 2 * j + 1], v[4 * j + 2], v[4 * j + 3], f.z, f.w);
+        }
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(s.part_empty + 8 * buf);
+      if (e < NT) scales[(buf ^ 1) * NT + e] = mine;
+    }
+    if (g.split == 1) {
+      if (ok && n0 + e < g.N)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const float v = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+          if (m0 + j < g.M) store_any<1>(g.y, g.ydt, (size_t)(m0 + j) * g.N + n0 + e, &v);
+        }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (*s.abort_flag) {
+    if (threadIdx.x == 0) drain_copies(s, first_issued, issued, kSt);
+    if (threadIdx.x == 32) drain_products(s);
+    __syncthreads();
+  }
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kColumns) : "memory");
+  if (g.split == 1) return;
+  // the cluster's partial sums: each CTA lays its own down (the stages are free now), then sums a share of the rows of X
+  float* sums = reinterpret_cast<float*>(base);
+  if (warp >= 2) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) sums[j * 128 + e] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+  }
+  cluster_sync_all();
+  if (warp >= 2) {
+    const uint32_t mine = smem_u32(sums);
+    for (int j = part; j < NT && m0 + j < g.M; j += g.split) {
+      float v = 0.f;
+      for (int p = 0; p < g.split; ++p) {
+        float w;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(map_to_cta(mine + (uint32_t)(j * 128 + e) * 4, (uint32_t)p)) : "memory");
+        v += w;
+      }
+      if (n0 + e < g.N) store_any<1>(g.y, g.ydt, (size_t)(m0 + j) * g.N + n0 + e, &v);
+    }
+  }
+  cluster_sync_all();          // nobody leaves while its sums are read
+}
+
+// ---- host side ------------------------------------------------------------------------------------------------
+
+// row-major e4m3 [rows, K] with boxes of box_rows x 128 bytes; outside the tensor a copy reads zeros
+bool make_tmap8(CUtensorMap* map, const void* ptr, int64_t rows, int64_t k, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)k};
+  cuuint32_t box[2] = {(cuuint32_t)kBlockK, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// once per device and kernel: the shared-memory attribute
+cudaError_t allow_smem(const void* kern, size_t bytes, int variant) {
+  static std::mutex mu;
+  static bool done[64][5] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(mu);
+  if (done[dev][variant]) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) done[dev][variant] = true;
+  return e;
+}
+
+template <int NT>
+cudaError_t launch_few(const CUtensorMap& tx, const CUtensorMap& tw, const Gemm8Args& g, int variant, cudaStream_t st) {
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(gemm_e4m3_few_kernel<NT>), few_smem(NT), variant);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((g.N + 127) / 128, (g.M + NT - 1) / NT, g.split);
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = few_smem(NT);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = g.split;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, gemm_e4m3_few_kernel<NT>, tx, tw, g);
 }
 
 }  // namespace
 
 int launch_gemm_e4m3(const StepRun& r) {
   const Shape &sx = r.mems[r.s.rd[g8::XQ]].shape, &sw = r.mems[r.s.rd[g8::WQ]].shape;
-  Gemm8Args g{reinterpret_cast<const unsigned char*>(r.rd(g8::XQ)), reinterpret_cast<const unsigned char*>(r.rd(g8::WQ)),
-              reinterpret_cast<const float*>(r.rd(g8::SX)), reinterpret_cast<const float*>(r.rd(g8::SW)), r.wr(g8::Y), r.wr_type(g8::Y),
-              (int)sx.d[0], (int)sw.d[0], (int)sx.d[1], (int)((sx.d[1] + 127) / 128), r.status_clear};
-  dim3 grid((g.N + 31) / 32, (g.M + 31) / 32);
-  if (grid.y > 65535) { set_error("ScaledInnerProduct: too many rows"); return DRAGON_ERR_UNSUPPORTED; }
-  gemm_e4m3_simple_kernel<<<grid, 1024, 0, reinterpret_cast<cudaStream_t>(r.stream)>>>(g);
-  const cudaError_t e = cudaGetLastError();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
+  Gemm8Args g{reinterpret_cast<const float*>(r.rd(g8::SX)), reinterpret_cast<const float*>(r.rd(g8::SW)), r.wr(g8::Y), r.wr_type(g8::Y),
+              (int)sx.d[0], (int)sw.d[0], (int)sx.d[1], (int)((sx.d[1] + 127) / 128), 0, 0, 1, r.status, r.status_clear, kWaitBudgetCycles, 0};
+  // failure-detection test only, as for InnerProduct: a short budget and a first wait for a signal that nothing sends
+  if (const char* e = std::getenv("DRAGON_GEMM_WAIT_BUDGET")) { const long long b = std::atoll(e); if (b > 0) g.wait_budget = std::min(b, kWaitBudgetCycles); }
+  if (const char* e = std::getenv("DRAGON_GEMM_DROP_FIRST_LOAD")) g.drop_first_load = e[0] == '1';
+  const int64_t tiles_m = (g.M + kTileM - 1) / kTileM, tiles_n = (g.N + kTileN - 1) / kTileN;
+  if (tiles_m * tiles_n > 0x3fffffffLL) { set_error("ScaledInnerProduct: too many tiles"); return DRAGON_ERR_UNSUPPORTED; }
+  g.tiles_m = (int)tiles_m;
+  g.tiles_n = (int)tiles_n;
+  // The large tiles wherever they give every SM one; otherwise the small ones, their blocks split while CTAs find room
+  const bool few = tiles_m * tiles_n < r.sm_count;
+  const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
+  CUtensorMap tx, tw;
+  if (!make_tmap8(&tx, r.rd(g8::XQ), g.M, g.K, few ? nt : kTileM) || !make_tmap8(&tw, r.rd(g8::WQ), g.N, g.K, few ? 128 : kTileN)) {
+    set_error("ScaledInnerProduct: cannot encode the TMA descriptors (no CUDA driver?)");
+    return DRAGON_ERR_CUDA;
+  }
+  cudaError_t e;
+  if (few) {
+    const int64_t ctas = (int64_t)((g.N + 127) / 128) * ((g.M + nt - 1) / nt);
+    while (g.split < 8 && ctas * g.split * 2 <= 2 * r.sm_count && g.kb >= 4 * g.split) g.split *= 2;
+    e = nt == 16 ? launch_few<16>(tx, tw, g, 1, st) : nt == 32 ? launch_few<32>(tx, tw, g, 2, st)
+        : nt == 64 ? launch_few<64>(tx, tw, g, 3, st) : launch_few<128>(tx, tw, g, 4, st);
+  } else {
+    e = allow_smem(reinterpret_cast<const void*>(gemm_e4m3_kernel), kSmem, 0);
+    if (e == cudaSuccess) {
+      gemm_e4m3_kernel<<<std::min(g.tiles_m * g.tiles_n, r.sm_count), kThreads, kSmem, st>>>(tx, tw, g);
+      e = cudaGetLastError();
+    }
+  }
   if (e != cudaSuccess) { set_error("ScaledInnerProduct: launch failed: %s", cudaGetErrorString(e)); return DRAGON_ERR_CUDA; }
   return DRAGON_OK;
 }

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from lm_cases import (U16, U32, as_type, e4m3_half_step, norm_graph, normals, run_gpu, scan_bounds, scan_graph)
+from lm_cases import (U16, U32, as_type, e4m3_half_step, norm_graph, normals, run_gpu, scan_bounds, scan_graph, to_gpu)
 from oracle import interp
 from paper_1707_08265_b200 import workloads as wl
 
@@ -166,7 +166,9 @@ def product_case(M, N, K, out, seed):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 64, 128), (2, 129, 144), (5, 256, 4096), (8, 1000, 272), (16, 512, 2048), (17, 136, 1040), (33, 384, 512), (64, 128, 128),
-                                   (65, 300, 400), (128, 256, 128), (129, 257, 384), (200, 1024, 1024), (300, 520, 2064), (512, 768, 640), (1000, 1000, 1008)])
+                                   (65, 300, 400), (128, 256, 128), (129, 257, 384), (200, 1024, 1024), (300, 520, 2064), (512, 768, 640), (1000, 1000, 1008),
+                                   # enough tiles of 128 x 256 for every SM: the kernel of many rows, ragged in every extent, more tiles than SMs
+                                   (2433, 2049, 272), (2400, 2056, 128), (4900, 1000, 400), (19000, 96, 16)])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_scaled_product(M, N, K, out):
     g, t, y, feeds = product_case(M, N, K, out, M * 7 + N * 3 + K)
@@ -186,6 +188,30 @@ def test_scaled_product_keeps_non_finite_values_where_they_are():
     assert np.isnan(got[3]).all() and not np.isfinite(got[9]).any()
     rest = np.delete(got, [3, 9], axis=0)
     assert np.isfinite(rest).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 300, 1024), (100, 128, 640), (2432, 2048, 1024)])
+def test_scaled_product_wait_that_runs_out_is_reported(M, N, K, monkeypatch):
+    """Failure detection without a fault: the producer leaves out its first stage, the first wait for it runs out on a short
+    budget, the kernel reports DRAGON_ERR_TIMEOUT and returns by itself; the next run of the same function is correct."""
+    from paper_1707_08265_b200 import binding as B
+    import torch
+    g, t, y, feeds = product_case(M, N, K, "f32", 5)
+    f = B.Graph.from_desc(g.desc).function(t, [y])
+    dev = [to_gpu(a, g.desc["tensors"][i]["dtype"]) for a, i in zip(feeds, t)]
+    out = torch.empty(M, N, device="cuda")
+    monkeypatch.setenv("DRAGON_GEMM_WAIT_BUDGET", "2000000")
+    monkeypatch.setenv("DRAGON_GEMM_DROP_FIRST_LOAD", "1")
+    f.run_torch(dev, [out])
+    assert f.status() == B.ERR_TIMEOUT
+    monkeypatch.delenv("DRAGON_GEMM_WAIT_BUDGET")
+    monkeypatch.delenv("DRAGON_GEMM_DROP_FIRST_LOAD")
+    run_gpu(g.desc, t, [y], feeds, f)
+    f.run_torch(dev, [out])
+    assert f.status() == 0
+    want = interp.run_function(g.desc, t, [y], feeds)[0]
+    mag = (np.abs(feeds[0]) * interp._spread(feeds[1], (M, K), 1)) @ (np.abs(feeds[2]) * interp._spread(feeds[3], (N, K), 128)).T
+    close(out.double().cpu().numpy(), want, (128 + -(-K // 128) + 2) * U32 * mag, "f32", "y")
 
 
 # ---- norm over many tensors and clipping --------------------------------------------------------------------
