@@ -2,7 +2,7 @@
 //   norm = sqrt(sum_i sum_e t_i[e]^2),  c_i = t_i * (norm > limit ? limit / norm : 1)
 // Bound: bytes (every tensor read for the norm, then read and written).  All tensors are one list of chunks that
 // persistent CTAs walk, so that a launch takes any mix of sizes; the addresses travel in the launch's parameters.
-// Squares are added in fp32 over the 32 elements a thread holds at a time and in fp64 beyond; elements whose squares
+// Squares are added in fp32 over the 16 or 32 elements a thread holds at a time and in fp64 beyond; elements whose squares
 // could leave fp32's range are squared in fp64.  The order of the sums is fixed, so the norm is the same in every run.
 #include <algorithm>
 
@@ -13,8 +13,9 @@ namespace dragon {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 8192;                       // elements: 32 per thread
+constexpr int kChunkBytes = 4 * 16 * kThreads;     // four accesses of 16 bytes a thread
 constexpr int kCtasPerSm = 4;
+__host__ __device__ constexpr int chunk_elements(bool f32) { return kChunkBytes / (f32 ? 4 : 2); }
 
 struct TensorList {
   const void* src[kTensorsPerLaunch];
@@ -36,46 +37,94 @@ struct NormOut {
   int* status_clear;
 };
 
-__device__ __forceinline__ int tensor_of_chunk(const TensorList& t, int c) {
-  int lo = 0, hi = t.count - 1;                    // the last tensor whose first chunk is not behind c
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.first[mid] <= c) lo = mid; else hi = mid - 1;
+// A CTA's chunks are one run of the list, so that the tensor of the next chunk is this one or the next.  Walked upwards by
+// the norm and downwards by the clipping: what the norm read last is what L2 still holds.
+struct Walk {
+  int c, end, k, dir;
+  __device__ __forceinline__ Walk(const TensorList& t, int dir_) : dir(dir_) {
+    const long long n = t.first[t.count];
+    const int c0 = (int)(n * blockIdx.x / gridDim.x), c1 = (int)(n * (blockIdx.x + 1) / gridDim.x);
+    c = dir > 0 ? c0 : c1 - 1;
+    end = dir > 0 ? c1 : c0 - 1;
+    int lo = 0, hi = t.count - 1;                  // the last tensor whose first chunk is not behind c
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (t.first[mid] <= c) lo = mid; else hi = mid - 1;
+    }
+    k = lo;
   }
-  return lo;
+  __device__ __forceinline__ bool more() const { return c != end; }
+  __device__ __forceinline__ long long element(const TensorList& t) const { return (long long)(c - t.first[k]) * chunk_elements((t.dtype[k] & 15) == DRAGON_F32); }
+  __device__ __forceinline__ void next(const TensorList& t) {
+    c += dir;
+    if (!more()) return;
+    while (dir > 0 ? t.first[k + 1] <= c : t.first[k] > c) k += dir;
+  }
+};
+
+// A chunk of a tensor as it is in memory: four accesses of 16 bytes a thread, 4 or 8 elements each.  What is behind the
+// tensor's last whole access reads as zeros and is handled by itself.
+struct Chunk {
+  uint4 u[4];
+  template <bool kKeep> __device__ __forceinline__ void load(const void* src, bool f32, long long first, long long n) {
+    const int per = f32 ? 4 : 8;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const long long i = first + (k * kThreads + (int)threadIdx.x) * per;
+      u[k] = make_uint4(0, 0, 0, 0);
+      if (i + per <= n) {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(src) + i * (f32 ? 4 : 2));
+        u[k] = kKeep ? __ldg(p) : __ldcs(p);
+      }
+    }
+  }
+};
+__device__ __forceinline__ void values_of(uint4 a, float (&v)[4]) { v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w); }
+__device__ __forceinline__ void values_of(uint4 a, float (&v)[8]) {
+  v[0] = bf16_low(a.x); v[1] = bf16_high(a.x); v[2] = bf16_low(a.y); v[3] = bf16_high(a.y);
+  v[4] = bf16_low(a.z); v[5] = bf16_high(a.z); v[6] = bf16_low(a.w); v[7] = bf16_high(a.w);
+}
+// the elements behind the last whole access of a tensor, if the chunk that starts at `first` holds them: this thread's, or none
+__device__ __forceinline__ bool tail_element(bool f32, long long first, long long n, long long* i) {
+  const int per = f32 ? 4 : 8;
+  *i = n / per * per + threadIdx.x;
+  return *i < n && *i >= first && *i < first + chunk_elements(f32);
 }
 
 __device__ __forceinline__ float factor_of(float norm, float limit) { return norm > limit ? limit / norm : (norm == norm ? 1.f : norm); }
 
-template <int DT>
-__device__ __forceinline__ double chunk_squares(const void* src, long long first, long long n) {
-  float v[32];
-  Raw<DT, 8> raw[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const long long i = first + (k * kThreads + (int)threadIdx.x) * 8;
-    if (i + 8 <= n) raw[k].load(src, i);
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const long long i = first + (k * kThreads + (int)threadIdx.x) * 8;
-    if (i + 8 <= n) raw[k].get(v + 8 * k);
-    else
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[8 * k + e] = 0.f;
-        if (i + e < n) { Raw<DT, 1> one; one.load(src, i + e); one.get(v + 8 * k + e); }
-      }
-  }
+// sum of the squares of N values
+template <int N> __device__ __forceinline__ double squares(const float* v) {
   unsigned m = 0;
   float s = 0.f;
 #pragma unroll
-  for (int e = 0; e < 32; ++e) { m = max(m, magnitude(v[e])); s += v[e] * v[e]; }
+  for (int e = 0; e < N; ++e) { m = max(m, magnitude(v[e])); s += v[e] * v[e]; }
   // the largest magnitude in [2^-40, 2^60]: no square overflows, and one that underflows is below 2^-46 of the sum
   if (m == 0 || (m >= 0x2b800000u && m <= 0x5d800000u)) return (double)s;
   double d = 0.0;
 #pragma unroll
-  for (int e = 0; e < 32; ++e) d += (double)v[e] * (double)v[e];
+  for (int e = 0; e < N; ++e) d += (double)v[e] * (double)v[e];
+  return d;
+}
+__device__ __forceinline__ double chunk_squares(const Chunk& ch, const void* src, bool f32, long long first, long long n) {
+  double d;
+  if (f32) {
+    float v[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) values_of(ch.u[j], v[j]);
+    d = squares<16>(v[0]);
+  } else {
+    float v[4][8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) values_of(ch.u[j], v[j]);
+    d = squares<32>(v[0]);
+  }
+  long long i;
+  if (tail_element(f32, first, n, &i)) {
+    float x;
+    load_any<1>(src, f32 ? DRAGON_F32 : DRAGON_BF16, i, &x);
+    d += squares<1>(&x);
+  }
   return d;
 }
 
@@ -91,16 +140,20 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
   return r;
 }
 
-__global__ void __launch_bounds__(kThreads) global_norm_kernel(const __grid_constant__ TensorList t, const NormOut o) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) global_norm_kernel(const __grid_constant__ TensorList t, const NormOut o) {
   __shared__ double sh[kThreads / 32];
   __shared__ bool last;
   if (o.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *o.status_clear = 0;
   double sum = 0.0;
-  const int n_chunks = t.first[t.count];
-  for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-    const int k = tensor_of_chunk(t, c);
-    const long long first = (long long)(c - t.first[k]) * kChunk;
-    sum += t.dtype[k] == DRAGON_F32 ? chunk_squares<DRAGON_F32>(t.src[k], first, t.n[k]) : chunk_squares<DRAGON_BF16>(t.src[k], first, t.n[k]);
+  Walk w(t, 1);
+  Chunk next;
+  if (w.more()) next.load<true>(t.src[w.k], t.dtype[w.k] == DRAGON_F32, w.element(t), t.n[w.k]);
+  while (w.more()) {
+    const Chunk now = next;
+    const Walk here = w;
+    w.next(t);
+    if (w.more()) next.load<true>(t.src[w.k], t.dtype[w.k] == DRAGON_F32, w.element(t), t.n[w.k]);
+    sum += chunk_squares(now, t.src[here.k], t.dtype[here.k] == DRAGON_F32, here.element(t), t.n[here.k]);
   }
   sum = block_sum(sum, sh);
   if (threadIdx.x == 0) {
@@ -123,59 +176,51 @@ __global__ void __launch_bounds__(kThreads) global_norm_kernel(const __grid_cons
   }
 }
 
-template <int DT>
-__device__ __forceinline__ void clip_chunk(const void* src, void* dst, long long first, long long n, float f) {
-  Raw<DT, 8> raw[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const long long i = first + (k * kThreads + (int)threadIdx.x) * 8;
-    if (i + 8 <= n) raw[k].load(src, i);
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const long long i = first + (k * kThreads + (int)threadIdx.x) * 8;
-    if (i + 8 <= n) {
-      float v[8];
-      raw[k].get(v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= f;
-      store_any<8>(dst, DT, i, v);
-    } else {
-      for (int e = 0; e < 8; ++e)
-        if (i + e < n) {
-          float v;
-          Raw<DT, 1> one;
-          one.load(src, i + e);
-          one.get(&v);
-          v *= f;
-          store_any<1>(dst, DT, i + e, &v);
-        }
-    }
-  }
-}
-// the clipped tensor's type may differ from the tensor's
-__device__ __forceinline__ void clip_chunk_converting(const void* src, int sdt, void* dst, int ddt, long long first, long long n, float f) {
-  for (long long i = first + threadIdx.x; i < n && i < first + kChunk; i += kThreads) {
-    float v;
-    load_any<1>(src, sdt, i, &v);
-    v *= f;
-    store_any<1>(dst, ddt, i, &v);
-  }
-}
-
-__global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ TensorList t, const float* norm, float limit, int* status_clear) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) clip_kernel(const __grid_constant__ TensorList t, const float* norm, float limit, int* status_clear) {
   if (status_clear && blockIdx.x == 0 && threadIdx.x == 0) *status_clear = 0;
   const float f = factor_of(__ldg(norm), limit);
-  const int n_chunks = t.first[t.count];
-  // from the last chunk to the first: what the norm's launch read last is still in L2
-  for (int c = n_chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-    const int k = tensor_of_chunk(t, c);
-    const long long first = (long long)(c - t.first[k]) * kChunk;
-    const int sdt = t.dtype[k] & 15, ddt = t.dtype[k] >> 4;
+  Walk w(t, -1);
+  Chunk next;
+  auto load = [&] {
+    if (w.more() && !(f == 1.f && t.src[w.k] == t.dst[w.k])) next.load<false>(t.src[w.k], (t.dtype[w.k] & 15) == DRAGON_F32, w.element(t), t.n[w.k]);
+  };
+  load();
+  while (w.more()) {
+    const Chunk now = next;
+    const int k = w.k, sdt = t.dtype[k] & 15, ddt = t.dtype[k] >> 4;
+    const bool f32 = sdt == DRAGON_F32;
+    const long long first = w.element(t), n = t.n[k];
+    w.next(t);
+    load();
     if (f == 1.f && t.src[k] == t.dst[k]) continue;      // in place and nothing to change
-    if (sdt != ddt) clip_chunk_converting(t.src[k], sdt, t.dst[k], ddt, first, t.n[k], f);
-    else if (sdt == DRAGON_F32) clip_chunk<DRAGON_F32>(t.src[k], t.dst[k], first, t.n[k], f);
-    else clip_chunk<DRAGON_BF16>(t.src[k], t.dst[k], first, t.n[k], f);
+    if (f32) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const long long i = first + (j * kThreads + (int)threadIdx.x) * 4;
+        float v[4];
+        values_of(now.u[j], v);
+        if (i + 4 > n) continue;
+        if (ddt == DRAGON_F32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(t.dst[k]) + i) = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+        else *reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(t.dst[k]) + i) = make_uint2(bf16_pair(v[0] * f, v[1] * f), bf16_pair(v[2] * f, v[3] * f));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const long long i = first + (j * kThreads + (int)threadIdx.x) * 8;
+        float v[8];
+        values_of(now.u[j], v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= f;
+        if (i + 8 <= n) store_any<8>(t.dst[k], ddt, i, v);
+      }
+    }
+    long long i;
+    if (tail_element(f32, first, n, &i)) {
+      float v;
+      load_any<1>(t.src[k], sdt, i, &v);
+      v *= f;
+      store_any<1>(t.dst[k], ddt, i, &v);
+    }
   }
 }
 
@@ -187,7 +232,8 @@ __global__ void clip_factor_kernel(const float* norm, float limit, float* factor
 // chunk table of tensors [k0, k1); false if a launch cannot hold it
 bool add_tensor(TensorList* t, const void* src, void* dst, int sdt, int ddt, int64_t n) {
   const int i = t->count;
-  const int64_t chunks = (n + kChunk - 1) / kChunk;
+  const int per = chunk_elements(sdt == DRAGON_F32);
+  const int64_t chunks = (n + per - 1) / per;
   if ((int64_t)t->first[i] + chunks > 0x3fffffffLL) return false;
   t->src[i] = src;
   t->dst[i] = dst;

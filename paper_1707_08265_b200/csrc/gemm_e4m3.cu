@@ -376,14 +376,27 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
   cluster_sync_all();
   if (warp >= 2) {
     const uint32_t mine = smem_u32(sums);
-    for (int j = part; j < NT && m0 + j < g.M; j += g.split) {
-      float v = 0.f;
+    // eight rows at a time: their loads from the other CTAs' shared memory are in flight together
+    for (int j0 = part; j0 < NT && m0 + j0 < g.M; j0 += 8 * g.split) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
       for (int p = 0; p < g.split; ++p) {
-        float w;
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(map_to_cta(mine + (uint32_t)(j * 128 + e) * 4, (uint32_t)p)) : "memory");
-        v += w;
+        const uint32_t from = map_to_cta(mine, (uint32_t)p) + (uint32_t)e * 4;
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int j = min(j0 + i * g.split, NT - 1);
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w[i]) : "r"(from + (uint32_t)j * 512) : "memory");
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += w[i];
       }
-      if (n0 + e < g.N) store_any<1>(g.y, g.ydt, (size_t)(m0 + j) * g.N + n0 + e, &v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int j = j0 + i * g.split;
+        if (j < NT && m0 + j < g.M && n0 + e < g.N) store_any<1>(g.y, g.ydt, (size_t)(m0 + j) * g.N + n0 + e, &v[i]);
+      }
     }
   }
   cluster_sync_all();          // nobody leaves while its sums are read

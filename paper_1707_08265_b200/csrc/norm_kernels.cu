@@ -14,22 +14,24 @@ namespace {
 constexpr int kMaxRowThreads = 512;
 
 struct RowShape {
-  int threads, rows;   // threads per row (a power of two, at least 32), rows per CTA
+  int threads, rows;   // threads per row (whole warps), rows per CTA
   int vec, per;        // elements per access (8 or 1), accesses per thread
   bool in_registers;
 };
 
-// Threads per row and accesses per thread: 8 elements (16 bytes of bf16) per access where rows are 16-byte aligned
-// (a length that is a multiple of 8), single elements otherwise; rows beyond 16384 (single elements: 8192) do not fit.
-RowShape row_shape(int64_t cols) {
+// Threads per row and accesses per thread: 8 elements (16 bytes of bf16) per access where rows are 16-byte aligned (a length
+// that is a multiple of 8), pairs for other even lengths, single elements for odd ones; rows beyond 16384 (8192) do not fit.
+// With many rows a thread takes up to four accesses of 8, so that a row is few warps and an SM holds many rows in flight;
+// with fewer rows than two per SM there is nothing else to run, and a row is spread over as many threads as it can use.
+RowShape row_shape(int64_t rows, int64_t cols) {
   RowShape s;
-  s.vec = cols % 8 == 0 ? 8 : 1;
+  s.vec = cols % 8 == 0 ? 8 : cols % 2 == 0 ? 2 : 1;
   const int64_t n = cols / s.vec;
-  s.per = s.vec == 1 ? 16 : n <= 512 ? 1 : n <= 1024 ? 2 : 4;
+  if (s.vec == 8) s.per = n <= 256 || (rows <= 256 && n <= kMaxRowThreads) ? 1 : n <= 512 || (rows <= 256 && n <= 2 * kMaxRowThreads) ? 2 : 4;
+  else s.per = n <= 2 * 256 ? 2 : n <= 8 * 256 || s.vec == 2 ? 8 : 16;
   s.in_registers = n <= (int64_t)s.per * kMaxRowThreads;
-  s.threads = 32;
-  while (s.threads < kMaxRowThreads && (int64_t)s.threads * s.per < n) s.threads *= 2;
-  s.rows = s.threads < 128 ? 128 / s.threads : 1;
+  s.threads = (int)std::min<int64_t>(kMaxRowThreads, ((n + s.per - 1) / s.per + 31) / 32 * 32);
+  s.rows = s.threads <= 64 ? 128 / s.threads : 1;
   return s;
 }
 
@@ -43,7 +45,8 @@ struct NormArgs {
   int* status_clear;
 };
 
-// sums over the `threads` threads of a row (threads / 32 warps); every thread of the CTA takes part
+// sums over the `threads` threads of a row (threads / 32 warps); every thread of the CTA takes part.  Scratch is written
+// once per call in alternating halves, so that one barrier is enough.
 __device__ __forceinline__ float2 row_sum2(float2 v, int threads, float2* sh) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -56,47 +59,54 @@ __device__ __forceinline__ float2 row_sum2(float2 v, int threads, float2* sh) {
   __syncthreads();
   float2 t = sh[first];
   for (int i = 1; i < per_row; ++i) { t.x += sh[first + i].x; t.y += sh[first + i].y; }
-  __syncthreads();
   return t;
 }
 
-template <int XDT, int RDT, int V, int PER>
-__global__ void __launch_bounds__(kMaxRowThreads) norm_kernel(const NormArgs a) {
+// DT: the type of x, r and h (-1: they differ); RDT: that of r, or -2 without a residual
+template <int DT, int RDT, int V, int PER>
+__global__ void __launch_bounds__(kMaxRowThreads, DT == DRAGON_BF16 && V == 8 && PER <= 2 ? 3 : 2) norm_kernel(const NormArgs a) {
   __shared__ float2 sh[kMaxRowThreads / 32];
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
-  const int t = threadIdx.x & (a.threads - 1);
-  const int rows_per_cta = blockDim.x / a.threads;
-  const long long row = (long long)blockIdx.x * rows_per_cta + threadIdx.x / a.threads;
+  const int slot = threadIdx.x / a.threads, t = threadIdx.x - slot * a.threads;
+  const long long row = (long long)blockIdx.x * (blockDim.x / a.threads) + slot;
   const bool in = row < a.rows;
   const size_t base = (size_t)(in ? row : 0) * a.cols;
-  Raw<XDT, V> rx[PER];
-  Raw<RDT, V> rr[PER];
+  Raw<DT, V> h[PER];
+  {
+    Raw<RDT, V> r[PER];
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int j = (t + k * a.threads) * V;
-    if (in && j < a.cols) { rx[k].load(a.x, base + j); rr[k].load(a.r, base + j); }
+    for (int k = 0; k < PER; ++k) {
+      const int j = (t + k * a.threads) * V;
+      if (in && j < a.cols) { h[k].load(a.x, a.xdt, base + j); r[k].load(a.r, a.rdt, base + j); }
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int j = (t + k * a.threads) * V;
+      if (RDT != -2 && in && j < a.cols) {
+        float u[V], w[V];
+        h[k].get(u);
+        r[k].get(w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) u[e] += w[e];
+        h[k].set(u);
+      }
+    }
   }
-  float h[PER][V], g[PER][V];
   float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int j = (t + k * a.threads) * V;
-    if (j < a.cols) load_any<V>(a.gain, a.gdt, j, g[k]);
-  }
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int j = (t + k * a.threads) * V;
     if (in && j < a.cols) {
-      float r[V];
-      rx[k].get(h[k]);
-      rr[k].get(r);
+      float u[V];
+      h[k].get(u);
+      if (DT == -1 && a.sum_dt == DRAGON_BF16) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        if (RDT >= 0) h[k][e] += r[e];
-        if (a.sum_dt == DRAGON_BF16) h[k][e] = bf16_rounded(h[k][e]);
-        sum.x += h[k][e] * h[k][e];
+        for (int e = 0; e < V; ++e) u[e] = bf16_rounded(u[e]);
+        h[k].set(u);
       }
-      if (a.h) store_any<V>(a.h, a.sum_dt, base + j, h[k]);
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum.x += u[e] * u[e];
+      if (a.h) h[k].store(a.h, a.sum_dt, base + j);
     }
   }
   sum = row_sum2(sum, a.threads, sh);
@@ -108,24 +118,25 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_kernel(const NormArgs a) 
     float y[V];
     unsigned m = 0;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      y[e] = mine ? h[k][e] * rstd * g[k][e] : 0.f;
-      if (a.ydt == DRAGON_BF16) y[e] = bf16_rounded(y[e]);
-      m = max(m, magnitude(y[e]));
+    for (int e = 0; e < V; ++e) y[e] = 0.f;
+    if (mine) {
+      float g[V];
+      load_any<V>(a.gain, a.gdt, j, g);
+      h[k].get(y);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        y[e] = y[e] * rstd * g[e];
+        if (a.ydt == DRAGON_BF16) y[e] = bf16_rounded(y[e]);
+        m = max(m, magnitude(y[e]));
+      }
+      if (a.y) store_any<V>(a.y, a.ydt, base + j, y);
     }
-    if (mine && a.y) store_any<V>(a.y, a.ydt, base + j, y);
     if (V == 8 && (a.s || a.q)) {       // 16 neighbouring threads hold a block of 128
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
       const float s = scale_of(m);
-      if (mine && a.s && (threadIdx.x & 15) == 0) a.s[(size_t)row * ((a.cols + 127) / 128) + j / 128] = s;
-      if (mine && a.q) {
-        const float inv = __frcp_rn(s);
-        uint2 w;
-        w.x = e4m3_pair(y[0] * inv, y[1 % V] * inv) | (e4m3_pair(y[2 % V] * inv, y[3 % V] * inv) << 16);
-        w.y = e4m3_pair(y[4 % V] * inv, y[5 % V] * inv) | (e4m3_pair(y[6 % V] * inv, y[7 % V] * inv) << 16);
-        *reinterpret_cast<uint2*>(reinterpret_cast<unsigned char*>(a.q) + base + j) = w;
-      }
+      if (mine && a.s && (t & 15) == 0) a.s[(size_t)row * ((a.cols + 127) / 128) + j / 128] = s;
+      if (mine && a.q) store_e4m3<V>(reinterpret_cast<unsigned char*>(a.q) + base + j, y, __frcp_rn(s));
     }
   }
 }
@@ -190,15 +201,18 @@ struct NormBwdArgs {
 };
 
 // Persistent: a row slot (the threads of one row) walks the rows with the grid's stride, so that every thread keeps the
-// running sums of dg for its own columns and writes them once.
-template <int HDT, int DYDT, int SDT, int V, int PER>
-__global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_kernel(const NormBwdArgs a) {
-  __shared__ float2 sh[kMaxRowThreads / 32];
+// running sums of dg for its own columns and writes them once.  DT: the type of h and dy (-1: they differ), SDT: that of
+// the residual branch's gradient (-2: none).
+template <int DT, int SDT, int V, int PER> constexpr int norm_bwd_ctas() { return V * PER <= 8 ? 2 : 1; }      // of 512 threads, by registers
+template <int DT, int SDT, int V, int PER>
+__global__ void __launch_bounds__(kMaxRowThreads, norm_bwd_ctas<DT, SDT, V, PER>()) norm_bwd_kernel(const NormBwdArgs a) {
+  constexpr bool kAhead = DT == DRAGON_BF16 && SDT != -1 && V == 8 && PER == 2;      // the next row's loads go out before this row's sums
+  __shared__ float2 sh[2][kMaxRowThreads / 32];
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
-  const int t = threadIdx.x & (a.threads - 1);
+  const int slot_in = threadIdx.x / a.threads, t = threadIdx.x - slot_in * a.threads;
   const int rows_per_cta = blockDim.x / a.threads;
-  const long long slot = (long long)blockIdx.x * rows_per_cta + threadIdx.x / a.threads, step = (long long)gridDim.x * rows_per_cta;
-  const long long passes = (a.rows + step - 1) / step;     // the same number for every thread of the CTA (barriers)
+  const long long slot = (long long)blockIdx.x * rows_per_cta + slot_in, step = (long long)gridDim.x * rows_per_cta;
+  const int passes = (int)((a.rows + step - 1) / step);     // the same number for every thread of the CTA (barriers)
   float g[PER][V], dg[PER][V];
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
@@ -208,31 +222,41 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_kernel(const NormBwdA
     for (int e = 0; e < V; ++e) dg[k][e] = 0.f;
   }
   const float inv_cols = 1.f / (float)a.cols;
-  for (long long pass = 0; pass < passes; ++pass) {
-    const long long row = slot + pass * step;
-    const bool in = row < a.rows;
-    const size_t base = (size_t)(in ? row : 0) * a.cols;
-    Raw<HDT, V> rh[PER];
-    Raw<DYDT, V> ry[PER];
-    Raw<SDT, V> rs[PER];
+  Raw<DT, V> rh[PER], ry[PER];
+  Raw<SDT, V> rs[PER];
+  auto load = [&](long long row) {
+    if (row >= a.rows) return;
+    const size_t base = (size_t)row * a.cols;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int j = (t + k * a.threads) * V;
-      if (in && j < a.cols) { rh[k].load(a.h, base + j); ry[k].load(a.dy, base + j); rs[k].load(a.skip, base + j); }
+      if (j < a.cols) { rh[k].load(a.h, a.hdt, base + j); ry[k].load(a.dy, a.dydt, base + j); rs[k].load(a.skip, a.sdt, base + j); }
     }
+  };
+  if (kAhead) load(slot);
+  for (int pass = 0; pass < passes; ++pass) {
+    const long long row = slot + pass * step;
+    const bool in = row < a.rows;
+    const size_t base = (size_t)(in ? row : 0) * a.cols;
+    if (!kAhead) load(row);
+    Raw<DT, V> ch[PER], cy[PER];
+    Raw<SDT, V> cs[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) { ch[k] = rh[k]; cy[k] = ry[k]; cs[k] = rs[k]; }
+    if (kAhead) load(row + step);
     float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int j = (t + k * a.threads) * V;
       if (in && j < a.cols) {
         float h[V], dy[V];
-        rh[k].get(h);
-        ry[k].get(dy);
+        ch[k].get(h);
+        cy[k].get(dy);
 #pragma unroll
         for (int e = 0; e < V; ++e) { sum.x += h[e] * h[e]; sum.y += dy[e] * g[k][e] * h[e]; }
       }
     }
-    sum = row_sum2(sum, a.threads, sh);
+    sum = row_sum2(sum, a.threads, sh[pass & 1]);
     const float rstd = rsqrtf(sum.x * inv_cols + a.eps);
     const float c = rstd * rstd * (sum.y * inv_cols);
 #pragma unroll
@@ -240,9 +264,9 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_kernel(const NormBwdA
       const int j = (t + k * a.threads) * V;
       if (in && j < a.cols) {
         float h[V], dy[V], s[V], o[V];
-        rh[k].get(h);
-        ry[k].get(dy);
-        rs[k].get(s);
+        ch[k].get(h);
+        cy[k].get(dy);
+        cs[k].get(s);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           o[e] = s[e] + rstd * (dy[e] * g[k][e] - h[e] * c);
@@ -263,9 +287,10 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_kernel(const NormBwdA
 
 // any row length: two passes over the row; the running sums of dg stay in memory (each column belongs to one thread)
 __global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_loop_kernel(const NormBwdArgs a) {
-  __shared__ float2 sh[kMaxRowThreads / 32];
+  __shared__ float2 sh[2][kMaxRowThreads / 32];
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
   bool first = true;
+  int half = 0;
   for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, first = false) {
     const size_t base = (size_t)row * a.cols;
     float2 sum = make_float2(0.f, 0.f);
@@ -277,7 +302,8 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_loop_kernel(const Nor
       sum.x += h * h;
       sum.y += dy * g * h;
     }
-    sum = row_sum2(sum, kMaxRowThreads, sh);
+    sum = row_sum2(sum, kMaxRowThreads, sh[half]);
+    half ^= 1;
     const float rstd = rsqrtf(sum.x / (float)a.cols + a.eps);
     const float c = rstd * rstd * (sum.y / (float)a.cols);
     for (int j = threadIdx.x; j < a.cols; j += kMaxRowThreads) {
@@ -296,27 +322,41 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_loop_kernel(const Nor
   }
 }
 
+// row slots of the gradient's grid: enough CTAs to fill the SMs at the kernel's occupancy
 int norm_bwd_grid(int64_t rows, const RowShape& s, int sm_count) {
   const int64_t ctas = (rows + s.rows - 1) / s.rows;
-  return (int)std::min<int64_t>(ctas, (int64_t)sm_count * (s.threads * s.rows > 256 ? 2 : 4));
+  const int per_sm = std::max(1, (s.vec * s.per <= 8 ? 1024 : 512) / (s.threads * s.rows));
+  return (int)std::min<int64_t>(ctas, (int64_t)sm_count * per_sm);
 }
 
-template <int XDT, int RDT>
+template <int DT, int RDT>
 cudaError_t launch_norm_typed(const NormArgs& a, const RowShape& s, int grid, cudaStream_t st) {
   const int block = s.threads * s.rows;
-  if (s.vec == 1) norm_kernel<XDT, RDT, 1, 16><<<grid, block, 0, st>>>(a);
-  else if (s.per == 1) norm_kernel<XDT, RDT, 8, 1><<<grid, block, 0, st>>>(a);
-  else if (s.per == 2) norm_kernel<XDT, RDT, 8, 2><<<grid, block, 0, st>>>(a);
-  else norm_kernel<XDT, RDT, 8, 4><<<grid, block, 0, st>>>(a);
+  if (s.vec == 2) {
+    if (s.per == 2) norm_kernel<DT, RDT, 2, 2><<<grid, block, 0, st>>>(a);
+    else norm_kernel<DT, RDT, 2, 8><<<grid, block, 0, st>>>(a);
+  } else if (s.vec == 1) {
+    if (s.per == 2) norm_kernel<DT, RDT, 1, 2><<<grid, block, 0, st>>>(a);
+    else if (s.per == 8) norm_kernel<DT, RDT, 1, 8><<<grid, block, 0, st>>>(a);
+    else norm_kernel<DT, RDT, 1, 16><<<grid, block, 0, st>>>(a);
+  } else if (s.per == 1) norm_kernel<DT, RDT, 8, 1><<<grid, block, 0, st>>>(a);
+  else if (s.per == 2) norm_kernel<DT, RDT, 8, 2><<<grid, block, 0, st>>>(a);
+  else norm_kernel<DT, RDT, 8, 4><<<grid, block, 0, st>>>(a);
   return cudaGetLastError();
 }
-template <int HDT, int DYDT, int SDT>
+template <int DT, int SDT>
 cudaError_t launch_norm_bwd_typed(const NormBwdArgs& a, const RowShape& s, int grid, cudaStream_t st) {
   const int block = s.threads * s.rows;
-  if (s.vec == 1) norm_bwd_kernel<HDT, DYDT, SDT, 1, 16><<<grid, block, 0, st>>>(a);
-  else if (s.per == 1) norm_bwd_kernel<HDT, DYDT, SDT, 8, 1><<<grid, block, 0, st>>>(a);
-  else if (s.per == 2) norm_bwd_kernel<HDT, DYDT, SDT, 8, 2><<<grid, block, 0, st>>>(a);
-  else norm_bwd_kernel<HDT, DYDT, SDT, 8, 4><<<grid, block, 0, st>>>(a);
+  if (s.vec == 2) {
+    if (s.per == 2) norm_bwd_kernel<DT, SDT, 2, 2><<<grid, block, 0, st>>>(a);
+    else norm_bwd_kernel<DT, SDT, 2, 8><<<grid, block, 0, st>>>(a);
+  } else if (s.vec == 1) {
+    if (s.per == 2) norm_bwd_kernel<DT, SDT, 1, 2><<<grid, block, 0, st>>>(a);
+    else if (s.per == 8) norm_bwd_kernel<DT, SDT, 1, 8><<<grid, block, 0, st>>>(a);
+    else norm_bwd_kernel<DT, SDT, 1, 16><<<grid, block, 0, st>>>(a);
+  } else if (s.per == 1) norm_bwd_kernel<DT, SDT, 8, 1><<<grid, block, 0, st>>>(a);
+  else if (s.per == 2) norm_bwd_kernel<DT, SDT, 8, 2><<<grid, block, 0, st>>>(a);
+  else norm_bwd_kernel<DT, SDT, 8, 4><<<grid, block, 0, st>>>(a);
   return cudaGetLastError();
 }
 
@@ -361,48 +401,114 @@ __global__ void __launch_bounds__(256) quant_row_kernel(const QuantArgs a) {
   }
 }
 
-// 128 x 128 blocks: a CTA per block, which stays in registers between the maximum and the rounding (16 rows a warp)
-__global__ void __launch_bounds__(256) quant_tile_kernel(const QuantArgs a) {
-  __shared__ unsigned sh[8];
+// The same for rows of a multiple of 8 elements: 16 lanes a block, 8 elements a lane, four blocks of a warp half in flight.
+// kWhole: the length is a multiple of 128, so block i is elements 128 i .. 128 i + 127 of the tensor.
+template <int DT, bool kWhole>
+__global__ void __launch_bounds__(256) quant_row_vec_kernel(const QuantArgs a) {
+  constexpr int kAhead = 4;
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long tile_row = blockIdx.x / a.col_blocks;
-  const int b = (int)(blockIdx.x - tile_row * a.col_blocks);
-  float v[16][4];
-  unsigned m = 0;
+  const int l = threadIdx.x & 15;
+  const long long step = (long long)gridDim.x * 16;
+  for (long long i0 = (long long)blockIdx.x * 16 + (threadIdx.x >> 4); i0 - (threadIdx.x >> 4 & 1) < a.n_blocks; i0 += kAhead * step) {   // both halves of a warp stay
+    Raw<DT, 8> raw[kAhead];
+    size_t at[kAhead];
+    float given[kAhead];
+    bool in[kAhead];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const long long row = tile_row * 128 + i * 8 + warp;
+    for (int k = 0; k < kAhead; ++k) {
+      const long long i = i0 + k * step;
+      in[k] = i < a.n_blocks;
+      at[k] = (size_t)i * 128 + l * 8;
+      long long row = 0;
+      int b = 0;
+      if (!kWhole || a.s_in) {
+        row = i >> 31 ? i / a.col_blocks : (long long)((unsigned)i / (unsigned)a.col_blocks);
+        b = (int)(i - row * a.col_blocks);
+      }
+      if (!kWhole) {
+        in[k] = in[k] && b * 128 + l * 8 < a.cols;
+        at[k] = (size_t)row * a.cols + b * 128 + l * 8;
+      }
+      given[k] = 1.f;
+      if (in[k]) {
+        raw[k].load(a.x, a.xdt, at[k]);
+        if (a.s_in) given[k] = __ldg(a.s_in + (size_t)(a.block_rows == 1 ? row : row >> 7) * a.col_blocks + b);
+      }
+    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = b * 128 + e * 32 + lane;
-      v[i][e] = 0.f;
-      if (row < a.rows && j < a.cols) load_any<1>(a.x, a.xdt, (size_t)row * a.cols + j, &v[i][e]);
-      m = max(m, magnitude(v[i][e]));
+    for (int k = 0; k < kAhead; ++k) {
+      const long long i = i0 + k * step;
+      float v[8];
+      unsigned m = 0;
+      if (in[k]) {
+        raw[k].get(v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, magnitude(v[e]));
+      }
+      float s = given[k];
+      if (!a.s_in) {
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        s = scale_of(m);
+      }
+      if (a.s && l == 0 && i < a.n_blocks) a.s[i] = s;
+      if (a.q && in[k]) store_e4m3<8>(a.q + at[k], v, __frcp_rn(s));
     }
   }
+}
+
+// 128 x 128 blocks: a CTA per block, which stays in registers between the maximum and the rounding.  V = 8: 16 lanes a row,
+// 16 rows at a time; V = 1 (rows that are not 16-byte aligned): a warp a row, four elements a lane.
+template <int DT, int V>
+__global__ void __launch_bounds__(256) quant_tile_kernel(const QuantArgs a) {
+  constexpr int kLanes = V == 8 ? 16 : 32, kCells = V == 8 ? 1 : 4, kPer = 128 * kLanes / 256;     // rows per thread
+  __shared__ unsigned sh[8];
+  if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
+  const int lane = threadIdx.x % kLanes, line = threadIdx.x / kLanes;
+  const long long tile_row = blockIdx.x / a.col_blocks;
+  const int b = (int)(blockIdx.x - tile_row * a.col_blocks);
+  Raw<DT, V> raw[kPer][kCells];
+  auto inside = [&](int i, int e) { return tile_row * 128 + i * (256 / kLanes) + line < a.rows && b * 128 + (e * kLanes + lane) * V < a.cols; };
+  auto place = [&](int i, int e) { return (size_t)(tile_row * 128 + i * (256 / kLanes) + line) * a.cols + b * 128 + (e * kLanes + lane) * V; };
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int e = 0; e < kCells; ++e)
+      if (inside(i, e)) raw[i][e].load(a.x, a.xdt, place(i, e));
+  unsigned m = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+#pragma unroll
+    for (int e = 0; e < kCells; ++e)
+      if (inside(i, e)) {
+        float v[V];
+        raw[i][e].get(v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) m = max(m, magnitude(v[k]));
+      }
   m = __reduce_max_sync(0xffffffffu, m);
-  if (lane == 0) sh[warp] = m;
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
   __syncthreads();
+#pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, sh[i]);
   const float s = scale_of(m), inv = __frcp_rn(s);
   if (a.s && threadIdx.x == 0) a.s[blockIdx.x] = s;
   if (!a.q) return;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const long long row = tile_row * 128 + i * 8 + warp;
+  for (int i = 0; i < kPer; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = b * 128 + e * 32 + lane;
-      if (row < a.rows && j < a.cols) a.q[(size_t)row * a.cols + j] = e4m3_of(v[i][e] * inv);
-    }
-  }
+    for (int e = 0; e < kCells; ++e)
+      if (inside(i, e)) {
+        float v[V];
+        raw[i][e].get(v);
+        store_e4m3<V>(a.q + place(i, e), v, inv);
+      }
 }
 
 }  // namespace
 
 int norm_bwd_partials(int64_t rows, int64_t cols, int sm_count) {
-  const RowShape s = row_shape(cols);
+  const RowShape s = row_shape(rows, cols);
   if (!s.in_registers) return (int)std::min<int64_t>(rows, (int64_t)sm_count * 2);
   return norm_bwd_grid(rows, s, sm_count) * s.rows;
 }
@@ -413,19 +519,17 @@ cudaError_t launch_norm(const StepRun& r) {
   NormArgs a{r.rd(nm::X), r.rd(nm::R), r.rd(nm::GAIN), r.wr(nm::H), r.wr(nm::Y), r.wr(nm::Q), reinterpret_cast<float*>(r.wr(nm::S)),
              r.rd_type(nm::X), r.rd_type(nm::R), r.rd_type(nm::GAIN), r.s.sum_dtype, r.s.round_dtype, (int)sh.rows(), (int)sh.cols(), 0,
              (float)r.s.attr, r.status_clear};
-  const RowShape s = row_shape(a.cols);
-  if (!s.in_registers || (s.vec == 1 && (a.s || a.q))) {
+  const RowShape s = row_shape(a.rows, a.cols);
+  if (!s.in_registers || (s.vec != 8 && (a.s || a.q))) {
     norm_loop_kernel<<<a.rows, kMaxRowThreads, 0, st>>>(a);
     return cudaGetLastError();
   }
   a.threads = s.threads;
   const int grid = (int)(((int64_t)a.rows + s.rows - 1) / s.rows);
-  const int rdt = a.r ? a.rdt : -1;
-  if (a.xdt == DRAGON_F32)
-    return rdt < 0 ? launch_norm_typed<DRAGON_F32, -1>(a, s, grid, st) : rdt == DRAGON_F32 ? launch_norm_typed<DRAGON_F32, DRAGON_F32>(a, s, grid, st)
-                                                                         : launch_norm_typed<DRAGON_F32, DRAGON_BF16>(a, s, grid, st);
-  return rdt < 0 ? launch_norm_typed<DRAGON_BF16, -1>(a, s, grid, st) : rdt == DRAGON_F32 ? launch_norm_typed<DRAGON_BF16, DRAGON_F32>(a, s, grid, st)
-                                                                        : launch_norm_typed<DRAGON_BF16, DRAGON_BF16>(a, s, grid, st);
+  const bool same = a.xdt == a.sum_dt && (!a.r || a.rdt == a.xdt);
+  if (!same) return a.r ? launch_norm_typed<-1, -1>(a, s, grid, st) : launch_norm_typed<-1, -2>(a, s, grid, st);
+  if (a.xdt == DRAGON_F32) return a.r ? launch_norm_typed<DRAGON_F32, DRAGON_F32>(a, s, grid, st) : launch_norm_typed<DRAGON_F32, -2>(a, s, grid, st);
+  return a.r ? launch_norm_typed<DRAGON_BF16, DRAGON_BF16>(a, s, grid, st) : launch_norm_typed<DRAGON_BF16, -2>(a, s, grid, st);
 }
 
 cudaError_t launch_colsum_finish(const float* part, int n_part, int cols, void* out, int dtype, cudaStream_t st);
@@ -437,7 +541,7 @@ cudaError_t launch_norm_bwd(const StepRun& r) {
   NormBwdArgs a{r.rd(nb::H), r.rd(nb::DY), r.rd(nb::GAIN), r.rd(nb::SKIP), r.wr(nb::DH), dg ? reinterpret_cast<float*>(r.ws + r.s.colpart_off) : nullptr,
                 r.rd_type(nb::H), r.rd_type(nb::DY), r.rd_type(nb::GAIN), r.rd_type(nb::SKIP), r.wr_type(nb::DH), (int)sh.rows(), (int)sh.cols(), 0,
                 (float)r.s.attr, r.status_clear};
-  const RowShape s = row_shape(a.cols);
+  const RowShape s = row_shape(a.rows, a.cols);
   cudaError_t e;
   if (!s.in_registers) {
     norm_bwd_loop_kernel<<<(int)std::min<int64_t>(a.rows, (int64_t)r.sm_count * 2), kMaxRowThreads, 0, st>>>(a);
@@ -445,12 +549,10 @@ cudaError_t launch_norm_bwd(const StepRun& r) {
   } else {
     a.threads = s.threads;
     const int grid = norm_bwd_grid(a.rows, s, r.sm_count);
-    const int sdt = a.skip ? a.sdt : -1;
-#define DRAGON_NB(H, D) (sdt < 0 ? launch_norm_bwd_typed<H, D, -1>(a, s, grid, st) : sdt == DRAGON_F32 ? launch_norm_bwd_typed<H, D, DRAGON_F32>(a, s, grid, st) \
-                                                                                     : launch_norm_bwd_typed<H, D, DRAGON_BF16>(a, s, grid, st))
-    if (a.hdt == DRAGON_F32) e = a.dydt == DRAGON_F32 ? DRAGON_NB(DRAGON_F32, DRAGON_F32) : DRAGON_NB(DRAGON_F32, DRAGON_BF16);
-    else e = a.dydt == DRAGON_F32 ? DRAGON_NB(DRAGON_BF16, DRAGON_F32) : DRAGON_NB(DRAGON_BF16, DRAGON_BF16);
-#undef DRAGON_NB
+    const bool same = a.hdt == a.dydt && (!a.skip || a.sdt == a.hdt);
+    if (!same) e = a.skip ? launch_norm_bwd_typed<-1, -1>(a, s, grid, st) : launch_norm_bwd_typed<-1, -2>(a, s, grid, st);
+    else if (a.hdt == DRAGON_F32) e = a.skip ? launch_norm_bwd_typed<DRAGON_F32, DRAGON_F32>(a, s, grid, st) : launch_norm_bwd_typed<DRAGON_F32, -2>(a, s, grid, st);
+    else e = a.skip ? launch_norm_bwd_typed<DRAGON_BF16, DRAGON_BF16>(a, s, grid, st) : launch_norm_bwd_typed<DRAGON_BF16, -2>(a, s, grid, st);
   }
   if (e != cudaSuccess || !dg) return e;
   return launch_colsum_finish(a.part, r.s.n_colpart, a.cols, dg, r.wr_type(nb::DGAIN), st);
@@ -461,13 +563,22 @@ cudaError_t launch_quant(const StepRun& r) {
   const Shape& sh = r.mems[r.s.rd[qt::X]].shape;
   QuantArgs a{r.rd(qt::X), reinterpret_cast<const float*>(r.rd(qt::SIN)), reinterpret_cast<float*>(r.wr(qt::S)), reinterpret_cast<unsigned char*>(r.wr(qt::Q)),
               r.rd_type(qt::X), (int)r.s.attr, (int)sh.d[0], (int)sh.d[1], (int)((sh.d[1] + 127) / 128), 0, r.status_clear};
+  const bool vec = a.cols % 8 == 0, f32 = a.xdt == DRAGON_F32;
   if (a.block_rows == 128 && !a.s_in) {
     const int64_t tiles = (sh.d[0] + 127) / 128 * a.col_blocks;
     if (tiles > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    quant_tile_kernel<<<(unsigned)tiles, 256, 0, st>>>(a);
+    if (vec) f32 ? quant_tile_kernel<DRAGON_F32, 8><<<(unsigned)tiles, 256, 0, st>>>(a) : quant_tile_kernel<DRAGON_BF16, 8><<<(unsigned)tiles, 256, 0, st>>>(a);
+    else f32 ? quant_tile_kernel<DRAGON_F32, 1><<<(unsigned)tiles, 256, 0, st>>>(a) : quant_tile_kernel<DRAGON_BF16, 1><<<(unsigned)tiles, 256, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  a.n_blocks = (long long)sh.d[0] * a.col_blocks;
+  const unsigned most = (unsigned)r.sm_count * 8;
+  if (vec) {
+    const unsigned grid = (unsigned)std::min<long long>((a.n_blocks + 15) / 16, most);
+    if (a.cols % 128 == 0) f32 ? quant_row_vec_kernel<DRAGON_F32, true><<<grid, 256, 0, st>>>(a) : quant_row_vec_kernel<DRAGON_BF16, true><<<grid, 256, 0, st>>>(a);
+    else f32 ? quant_row_vec_kernel<DRAGON_F32, false><<<grid, 256, 0, st>>>(a) : quant_row_vec_kernel<DRAGON_BF16, false><<<grid, 256, 0, st>>>(a);
   } else {
-    a.n_blocks = (long long)sh.d[0] * a.col_blocks;
-    quant_row_kernel<<<(unsigned)std::min<long long>((a.n_blocks + 7) / 8, (long long)r.sm_count * 8), 256, 0, st>>>(a);
+    quant_row_kernel<<<(unsigned)std::min<long long>((a.n_blocks + 7) / 8, most), 256, 0, st>>>(a);
   }
   return cudaGetLastError();
 }
