@@ -103,6 +103,13 @@ def _ids(seq):
     return arr
 
 
+def _current_stream():
+    """Handle of torch's current stream, without the Stream object around it where torch offers that (3 us a call)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+
+
 class Graph:
     """dragon_graph_t: tensors and operators in creation order."""
 
@@ -191,9 +198,10 @@ class Function:
         if not self.h:
             raise DragonError(-1, "dragon_function")
         self._ws = None
+        self._feeds_t, self._fetches_t = _c.c_void_p * max(1, self.n_in), _c.c_void_p * max(1, self.n_out)
 
     def close(self):
-        if self.h:
+        if self.h and lib is not None:      # (at the interpreter's exit the module may be gone before its objects)
             lib().dragon_function_destroy(self.h)
             self.h = None
 
@@ -296,9 +304,7 @@ class Function:
             raise DragonError(r, "dragon_function_set_workspace")
 
     def run(self, feed_ptrs, fetch_ptrs, stream=0):
-        feeds = (_c.c_void_p * max(1, self.n_in))(*[p or None for p in feed_ptrs])
-        fetches = (_c.c_void_p * max(1, self.n_out))(*fetch_ptrs)
-        r = lib().dragon_run(self.h, feeds, fetches, stream)
+        r = lib().dragon_run(self.h, self._feeds_t(*feed_ptrs), self._fetches_t(*fetch_ptrs), stream)      # (a 0 is a NULL)
         if r < 0:
             raise DragonError(r, "dragon_run")
 
@@ -338,10 +344,10 @@ class Function:
 
     def run_torch(self, feeds, fetches, stream=None):
         """feeds / fetches: lists of CUDA torch tensors (None for a pruned input)."""
-        import torch
-        self.ensure_workspace()
-        s = stream if stream is not None else torch.cuda.current_stream()
-        self.run([0 if t is None else t.data_ptr() for t in feeds], [t.data_ptr() for t in fetches], s.cuda_stream)
+        if self._ws is None:
+            self.ensure_workspace()
+        s = _current_stream() if stream is None else stream.cuda_stream
+        self.run([0 if t is None else t.data_ptr() for t in feeds], [t.data_ptr() for t in fetches], s)
 
 
 class Workspace:

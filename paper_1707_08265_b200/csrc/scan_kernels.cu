@@ -549,6 +549,32 @@ __global__ void __launch_bounds__(kBwdWarps * 32, kBwdCtas) scan_bwd_kernel(cons
   }
 }
 
+// One row per sequence (a decoding step): nothing to scan, every element by itself
+template <int DT, int CH>
+__global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
+  if (a.status_clear && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status_clear = 0;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * CH;
+  if (c >= a.cols) return;
+  for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    const size_t at = (size_t)row * a.cols + c;
+    Cell<DT, CH> z, x;
+    Cell<-1, CH> h0;
+    z.load(reinterpret_cast<const char*>(a.gate) + at * element_bytes<DT>(a.gdt), a.gdt);
+    x.load(reinterpret_cast<const char*>(a.x) + at * element_bytes<DT>(a.xdt), a.xdt);
+    if (a.h0) h0.load(reinterpret_cast<const char*>(a.h0) + at * element_bytes<-1>(a.h0dt), a.h0dt);
+    const bool from_h0 = a.h0 && !(a.reset && __ldg(a.reset + row) != 0);
+    float h[CH];
+#pragma unroll
+    for (int e = 0; e < CH; ++e) {
+      float f, keep;
+      gate_of(z.get(e), &f, &keep);
+      h[e] = keep * x.get(e);
+      if (from_h0) h[e] = fmaf(f, h0.get(e), h[e]);
+    }
+    store_cell<DT, CH>(reinterpret_cast<char*>(a.h) + at * element_bytes<DT>(a.hdt), a.hdt, h);
+  }
+}
+
 int columns_per_lane(int64_t cols) { return cols % 2 == 0 ? 2 : 1; }    // pairs of columns are aligned in every row
 
 struct Scratch { size_t pair, end, bytes; };
@@ -597,6 +623,13 @@ cudaError_t scan_args(const StepRun& r, bool backward, ScanArgs* out) {
 
 template <int DT>
 void launch_fwd(const ScanArgs& a, int sm_count, cudaStream_t st) {
+  if (a.length == 1 && !a.carry) {
+    const int per = columns_per_lane(a.cols);
+    const dim3 grid((a.cols + 256 * per - 1) / (256 * per), std::min(a.rows, 32768));
+    if (per == 2) scan_step_kernel<DT, 2><<<grid, 256, 0, st>>>(a);
+    else scan_step_kernel<DT, 1><<<grid, 256, 0, st>>>(a);
+    return;
+  }
   const unsigned grid = std::min((unsigned)a.tiles * a.groups, (unsigned)(sm_count * kFwdCtas));
   if (columns_per_lane(a.cols) == 2) scan_kernel<DT, 2><<<grid, kFwdWarps * 32, 0, st>>>(a);
   else scan_kernel<DT, 1><<<grid, kFwdWarps * 32, 0, st>>>(a);
