@@ -2,13 +2,18 @@
 // each block of 128 along K, fp32 accumulation, fp32 or bf16 output.  Hand-written for sm_100a.
 //
 // The scales change every 128 elements of K, so the tensor unit may accumulate over one block only (four
-// tcgen05.mma.kind::f8f6f4 of K = 32).  Two TMEM accumulators alternate: while the tensor unit works on block b + 1, the
-// epilogue warps read block b's sums with tcgen05.ld and add them, times their scale, to fp32 registers (packed FMAs).
-// A tile of 128 x 256 costs the tensor unit 512 cycles a block and the epilogue 64 packed FMAs a thread and a block, so
-// the addition hides behind the products.  One block is one TMA stage (128-byte rows, 128-byte swizzle).
+// tcgen05.mma.kind::f8f6f4 of K = 32).  TMEM accumulators take turns: while the tensor unit works on the next block, the
+// epilogue warps read this block's sums with tcgen05.ld and add them, times their scale, to fp32 registers (packed FMAs).
+// One block is one TMA stage (128-byte rows, 128-byte swizzle).
 //
-//   gemm_e4m3_kernel      many rows: tiles of 128 rows of X x 256 rows of W; a thread holds one row of Y, its scale is one number
-//                         a block; persistent CTAs in an L2-friendly tile order; bound by the tensor unit
+//   gemm_e4m3_kernel      many rows: two CTAs of a cluster work on one tile of 256 rows of X x 256 rows of W
+//                         (tcgen05.mma.cta_group::2), so that a CTA copies 32 KB a block instead of the 48 KB of a 128 x 256 tile
+//                         of its own.  A thread holds one row of Y and 64 columns, its scale is one number a block; persistent
+//                         pairs in an L2-friendly tile order.  Measured, 8192 x 8192 x 4096: 320 us by itself, 361 us in a loop
+//                         under the power limit (1.52 PFLOP/s).  With parts left out: products alone 136 us, with their copies
+//                         195 (11 TB/s out of L2), with the hand-over of the accumulators but no work on them 269; what
+//                         bounds is that hand-over (TMEM holds two blocks' sums, and commit, wake-up and release across two
+//                         SMs take longer than one block's products).
 //   gemm_e4m3_few_kernel  few rows: the operands change places (128 rows of W x 16..128 rows of X), so that the tile's height is
 //                         filled by weights and hardly any product is wasted; the K blocks of a tile are split over the
 //                         CTAs of a cluster, whose partial sums meet in shared memory in a fixed order; bound by the bytes of W
@@ -26,6 +31,7 @@ namespace {
 
 constexpr int kBlockK = 128;        // one scale block = one 128-byte swizzle row of e4m3 = one stage
 constexpr int kUmmaK = 32;
+constexpr int kBufs = 4;            // accumulators in TMEM that take turns
 
 // instruction descriptor of kind::f8f6f4: D = f32, A = B = e4m3 (both codes 0), K-major, M x N
 constexpr uint32_t idesc_e4m3(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
@@ -47,14 +53,23 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* v) {
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// acc (two neighbouring columns) += v * s
-__device__ __forceinline__ void fma_pair(float2& acc, uint32_t v0, uint32_t v1, float s0, float s1) {
-  unsigned long long a, v, s;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "f"(acc.x), "f"(acc.y));
+// two neighbouring columns' sums as one 64-bit register: acc += v * s
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pack(float lo, float hi) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi)); return p; }
+__device__ __forceinline__ float2 unpack(Pair p) { float2 v; asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p)); return v; }
+__device__ __forceinline__ void fma_pair(Pair& acc, uint32_t v0, uint32_t v1, Pair s) {
+  Pair v;
   asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(v0), "r"(v1));
-  asm("mov.b64 %0, {%1, %2};" : "=l"(s) : "f"(s0), "f"(s1));
-  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(v), "l"(s));
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(acc.x), "=f"(acc.y) : "l"(a));
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(v), "l"(s));
+}
+
+// the same by a pair: 256 rows of A and N columns over both CTAs' shared memory and TMEM
+__device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
 struct Gemm8Args {
@@ -81,15 +96,15 @@ __device__ __forceinline__ Sync sync_area(unsigned char* p, int stages) {
   s.full = smem_u32(bars);
   s.empty = s.full + 8 * stages;
   s.part_full = s.empty + 8 * stages;
-  s.part_empty = s.part_full + 16;
-  s.drain = s.part_empty + 16;
-  s.tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * stages + 5);
+  s.part_empty = s.part_full + 8 * kBufs;
+  s.drain = s.part_empty + 8 * kBufs;
+  s.tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * stages + 2 * kBufs + 1);
   s.abort_flag = reinterpret_cast<volatile int*>(s.tmem_slot + 1);
   return s;
 }
 __device__ __forceinline__ void sync_init(const Sync& s, int stages, int epilogue_warps) {
   for (int i = 0; i < stages; ++i) { mbar_init(s.full + 8 * i, 1); mbar_init(s.empty + 8 * i, 1); }
-  for (int b = 0; b < 2; ++b) { mbar_init(s.part_full + 8 * b, 1); mbar_init(s.part_empty + 8 * b, epilogue_warps); }
+  for (int b = 0; b < kBufs; ++b) { mbar_init(s.part_full + 8 * b, 1); mbar_init(s.part_empty + 8 * b, epilogue_warps); }
   mbar_init(s.drain, 1);
   s.abort_flag[0] = 0;
   s.abort_flag[1] = 0;         // nobody sets this one: for waits that must not be cut short
@@ -114,8 +129,8 @@ __device__ __forceinline__ void drain_products(const Sync& s) {
 
 // The MMA issuer's work on one block: wait for an accumulator and the stage, four products, hand both on
 __device__ __forceinline__ bool issue_block(const Sync& s, const Gemm8Args& g, int it, int stages, uint32_t a_addr, uint32_t b_addr, uint32_t tmem, int columns, uint32_t idesc) {
-  const int buf = it & 1, st = it % stages;
-  if (!wait_or_abort(s, g, s.part_empty + 8 * buf, ((it >> 1) & 1) ^ 1)) return false;
+  const int buf = it % kBufs, st = it % stages;
+  if (!wait_or_abort(s, g, s.part_empty + 8 * buf, ((it / kBufs) & 1) ^ 1)) return false;
   if (!wait_or_abort(s, g, s.full + 8 * st, (it / stages) & 1)) return false;
   fence_after();
   const uint64_t a = make_smem_desc(a_addr), b = make_smem_desc(b_addr);
@@ -128,10 +143,33 @@ __device__ __forceinline__ bool issue_block(const Sync& s, const Gemm8Args& g, i
 
 // ---- many rows ------------------------------------------------------------------------------------------------
 
-constexpr int kTileM = 128, kTileN = 256, kStages = 4;
-constexpr int kThreads = 320;                                   // TMA, MMA, 8 epilogue warps
-constexpr uint32_t kBytesA = kTileM * kBlockK, kBytesB = kTileN * kBlockK, kStageBytes = kBytesA + kBytesB;
-constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 256;
+constexpr int kTileM = 256, kTileN = 256, kStages = 6;          // of a pair; a CTA holds 128 rows of X and 128 of W
+constexpr int kEpiWarps = 16, kEpiThreads = 32 * kEpiWarps;     // four warps a quarter of the lanes: one's loads from TMEM hide behind the others' sums
+constexpr int kFetchWarps = 2;
+constexpr int kThreads = 64 + kEpiThreads + 32 * kFetchWarps;   // TMA, MMA, epilogue, scales
+constexpr int kTileBufs = 2;                                    // accumulators that take turns: all of TMEM
+constexpr int kEpiCols = kTileN * 4 / kEpiWarps;                // columns of a warp
+constexpr uint32_t kHalfBytes = 128 * kBlockK, kStageBytes = 2 * kHalfBytes;
+constexpr int kScaleBlocks = 16;                                // blocks whose scales are fetched together
+// scales of kScaleBlocks blocks: of this CTA's 128 rows of X, and of the tile's two 128-row blocks of W; two sets
+struct TileScales { float x[kScaleBlocks][128]; float w[2][kScaleBlocks]; };
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 256 + 2 * sizeof(TileScales);
+
+__device__ __forceinline__ void copy_async4(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+// the fetching threads copy the scales of blocks b0.. of the tile at (row0, n-block nb0); what is outside repeats the last
+__device__ __forceinline__ void fetch_scales(const Gemm8Args& g, TileScales& to, int tid, int row0, int nb0, int b0) {
+  for (int r = tid; r < 128; r += 32 * kFetchWarps) {
+    const float* sx = g.sx + (size_t)min(row0 + r, g.M - 1) * g.kb;
+#pragma unroll
+    for (int b = 0; b < kScaleBlocks; ++b) copy_async4(&to.x[b][r], sx + min(b0 + b, g.kb - 1));
+  }
+  for (int i = tid; i < 2 * kScaleBlocks; i += 32 * kFetchWarps) {
+    const int h = i / kScaleBlocks, b = i % kScaleBlocks;
+    copy_async4(&to.w[h][b], g.sw + (size_t)min(nb0 + h, (g.N - 1) / 128) * g.kb + min(b0 + b, g.kb - 1));
+  }
+}
 
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const Gemm8Args g) {
@@ -139,145 +177,177 @@ gemm_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
   const uint32_t raw = smem_u32(smem_raw), tiles = (raw + 1023u) & ~1023u;
   const Sync s = sync_area(smem_raw + (tiles - raw) + (size_t)kStages * kStageBytes, kStages);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_tiles = g.tiles_m * g.tiles_n;
+  const int n_tiles = g.tiles_m * g.tiles_n, n_units = (int)(gridDim.x >> 1), unit = (int)(blockIdx.x >> 1);
+  const uint32_t rank = cluster_ctarank();
   if (threadIdx.x == 0) {
-    sync_init(s, kStages, 8);
+    sync_init(s, kStages, 2 * kEpiWarps);                       // (both CTAs' epilogue warps; only the first CTA's part_empty is used)
     if (g.status_clear && blockIdx.x == 0) *g.status_clear = 0;
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s.tmem_slot)), "r"((uint32_t)(2 * kTileN)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s.tmem_slot)), "r"((uint32_t)(2 * kTileN)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = *s.tmem_slot;
-  int issued = 0, first_issued = 0;
+  cluster_sync_all();                                           // nobody signals a barrier of the other CTA before it is initialised
+  const uint32_t full_first = map_to_cta(s.full, 0);            // the pair counts its copies on the first CTA's barriers
   if (warp == 0) {
     if (lane == 0) {
       bool ok = true;
-      for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x) {
+      int issued = 0;
+      for (int t = unit; t < n_tiles && ok; t += n_units) {
         int tm, tn;
         tile_coords(t, g.tiles_m, g.tiles_n, &tm, &tn);
         for (int b = 0; b < g.kb; ++b, ++issued) {
           const int st = issued % kStages;
           if (!wait_or_abort(s, g, s.empty + 8 * st, ((issued / kStages) & 1) ^ 1)) { ok = false; break; }
-          if (g.drop_first_load && issued == 0) { first_issued = 1; continue; }
+          if (g.drop_first_load && issued == 0) continue;
           const uint32_t dst = tiles + (uint32_t)st * kStageBytes;
-          mbar_expect_tx(s.full + 8 * st, kStageBytes);
-          tma_load_2d(dst, &tmap_x, b * kBlockK, tm * kTileM, s.full + 8 * st);
-          tma_load_2d(dst + kBytesA, &tmap_w, b * kBlockK, tn * kTileN, s.full + 8 * st);
+          if (rank == 0) mbar_expect_tx(s.full + 8 * st, 2 * kStageBytes);
+          tma_load_2d_pair(dst, &tmap_x, b * kBlockK, tm * kTileM + (int)rank * 128, full_first + 8 * st);
+          tma_load_2d_pair(dst + kHalfBytes, &tmap_w, b * kBlockK, tn * kTileN + (int)rank * 128, full_first + 8 * st);
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       int it = 0;
       bool ok = true;
-      for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x)
+      for (int t = unit; t < n_tiles && ok; t += n_units)
         for (int b = 0; b < g.kb && ok; ++b, ++it) {
-          const uint32_t a = tiles + (uint32_t)(it % kStages) * kStageBytes;
-          ok = issue_block(s, g, it, kStages, a, a + kBytesA, tmem, kTileN, idesc_e4m3(kTileM, kTileN));
+          const int st = it % kStages;
+          const int buf = it % kTileBufs;
+          ok = wait_or_abort(s, g, s.part_empty + 8 * buf, ((it / kTileBufs) & 1) ^ 1) && wait_or_abort(s, g, s.full + 8 * st, (it / kStages) & 1);
+          if (!ok) break;
+          fence_after();
+          const uint32_t at = tiles + (uint32_t)st * kStageBytes;
+          const uint64_t da = make_smem_desc(at), db = make_smem_desc(at + kHalfBytes);
+#pragma unroll
+          for (int k = 0; k < kBlockK / kUmmaK; ++k) umma_e4m3_pair(tmem + buf * kTileN, da + 2 * k, db + 2 * k, idesc_e4m3(kTileM, kTileN), k > 0 ? 1u : 0u);
+          umma_commit_pair(s.empty + 8 * st);
+          umma_commit_pair(s.part_full + 8 * buf);
         }
     }
-  } else {
-    // warp w reads TMEM lanes 32 (w % 4) .. + 31 (rows of the tile) and one half of the columns (one 128-row block of W)
-    const int q = warp & 3, half = (warp - 2) >> 2;
-    int it = 0;
-    bool ok = true;
-    for (int t = blockIdx.x; t < n_tiles && ok; t += gridDim.x) {
+  } else if (warp >= 2 + kEpiWarps) {
+    // scales, kScaleBlocks blocks at a time: a set is filled while the epilogue works with the other one, and handed over
+    // at a barrier that says both "it is filled" and "the other one is free"
+    TileScales* scales = reinterpret_cast<TileScales*>(smem_raw + (tiles - raw) + (size_t)kStages * kStageBytes + 256);
+    int set = 0;
+    for (int t = unit; t < n_tiles; t += n_units) {
       int tm, tn;
       tile_coords(t, g.tiles_m, g.tiles_n, &tm, &tn);
-      const int row = tm * kTileM + q * 32 + lane, col0 = tn * kTileN + half * 128;
-      const float* sx = g.sx + (size_t)min(row, g.M - 1) * g.kb;
-      const float* sw = g.sw + (size_t)min(col0 / 128, (g.N - 1) / 128) * g.kb;
-      float2 acc[64];
-#pragma unroll
-      for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
-      float sc = __ldg(sx) * __ldg(sw);
-      for (int b = 0; b < g.kb; ++b, ++it) {
-        const int buf = it & 1;
-        const int ahead = min(b + 1, g.kb - 1);
-        const float next_x = __ldg(sx + ahead), next_w = __ldg(sw + ahead);
-        ok = __all_sync(0xffffffffu, mbar_wait(s.part_full + 8 * buf, (it >> 1) & 1, s.abort_flag, g.wait_budget));
-        if (!ok) { if (lane == 0) { *s.abort_flag = 1; atomicExch(g.status, DRAGON_ERR_TIMEOUT); } break; }
-        fence_after();
-        const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * kTileN + half * 128);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t v[32];
-          tmem_ld32(from + 32 * c, v);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 16; ++j) fma_pair(acc[16 * c + j], v[2 * j], v[2 * j + 1], sc, sc);
-        }
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(s.part_empty + 8 * buf);
-        sc = next_x * next_w;
+      for (int b0 = 0; b0 < g.kb; b0 += kScaleBlocks, set ^= 1) {
+        fetch_scales(g, scales[set], (int)threadIdx.x - 64 - kEpiThreads, tm * kTileM + (int)rank * 128, tn * 2, b0);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads + 32 * kFetchWarps) : "memory");
       }
+    }
+  } else {
+    // warp w reads TMEM lanes 32 (w % 4) .. + 31 (rows of this CTA's half of the tile) and kEpiCols columns (inside one
+    // 128-row block of W)
+    const int q = warp & 3, first_col = ((warp - 2) >> 2) * kEpiCols;
+    const uint32_t part_empty_first = map_to_cta(s.part_empty, 0);
+    const TileScales* scales = reinterpret_cast<const TileScales*>(smem_raw + (tiles - raw) + (size_t)kStages * kStageBytes + 256);
+    const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)first_col;
+    int it = 0, set = 0;
+    bool ok = true;
+    for (int t = unit; t < n_tiles; t += n_units) {
+      Pair acc[kEpiCols / 2];
+#pragma unroll
+      for (int j = 0; j < kEpiCols / 2; ++j) acc[j] = 0;
+      for (int b0 = 0; b0 < g.kb; b0 += kScaleBlocks, set ^= 1) {
+        asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads + 32 * kFetchWarps) : "memory");
+        const float* xs = &scales[set].x[0][q * 32 + lane];
+        const float* ws = scales[set].w[first_col / 128];
+        const int n = min(kScaleBlocks, g.kb - b0);
+#pragma unroll 1
+        for (int i = 0; i < n && ok; ++i, ++it) {
+          const float s1 = xs[i * 128] * ws[i];
+          const Pair sc = pack(s1, s1);
+          const int buf = it % kTileBufs;
+          ok = __all_sync(0xffffffffu, mbar_wait(s.part_full + 8 * buf, (it / kTileBufs) & 1, s.abort_flag, g.wait_budget));
+          if (!ok) { if (lane == 0) { *s.abort_flag = 1; atomicExch(g.status, DRAGON_ERR_TIMEOUT); } break; }
+          fence_after();
+#pragma unroll
+          for (int c = 0; c < kEpiCols; c += 16) {
+            uint32_t v[16];
+            tmem_ld16(from + (uint32_t)(buf * kTileN + c), v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) fma_pair(acc[c / 2 + j], v[2 * j], v[2 * j + 1], sc);
+          }
+          fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            if (rank == 0) mbar_arrive(s.part_empty + 8 * buf);
+            else mbar_arrive_remote_relaxed(part_empty_first + 8 * buf);
+          }
+        }
+      }
+      int tm, tn;
+      tile_coords(t, g.tiles_m, g.tiles_n, &tm, &tn);
+      const int row = tm * kTileM + (int)rank * 128 + q * 32 + lane;
       if (!ok || row >= g.M) continue;
-      if (g.ydt == DRAGON_F32) {
-        float* out = reinterpret_cast<float*>(g.y) + (size_t)row * g.N + col0;
-        if ((g.N & 3) == 0 && col0 + 128 <= g.N) {
+      const int col0 = tn * kTileN + first_col;
+      const size_t at = (size_t)row * g.N + col0;
+      const bool whole = (g.N & 7) == 0 && col0 + kEpiCols <= g.N;
 #pragma unroll
-          for (int j = 0; j < 64; j += 2) *reinterpret_cast<float4*>(out + 2 * j) = make_float4(acc[j].x, acc[j].y, acc[j + 1].x, acc[j + 1].y);
-        } else {
+      for (int j = 0; j < kEpiCols / 2; j += 4) {
+        float v[8];
 #pragma unroll
-          for (int j = 0; j < 64; ++j) {
-            if (col0 + 2 * j < g.N) out[2 * j] = acc[j].x;
-            if (col0 + 2 * j + 1 < g.N) out[2 * j + 1] = acc[j].y;
-          }
-        }
-      } else {
-        unsigned short* out = reinterpret_cast<unsigned short*>(g.y) + (size_t)row * g.N + col0;
-        if ((g.N & 7) == 0 && col0 + 128 <= g.N) {
+        for (int i = 0; i < 4; ++i) { const float2 p = unpack(acc[j + i]); v[2 * i] = p.x; v[2 * i + 1] = p.y; }
+        if (whole) store_any<8>(g.y, g.ydt, at + 2 * j, v);
+        else
 #pragma unroll
-          for (int j = 0; j < 64; j += 4)
-            *reinterpret_cast<uint4*>(out + 2 * j) = make_uint4(bf16_pair(acc[j].x, acc[j].y), bf16_pair(acc[j + 1].x, acc[j + 1].y),
-                                                                bf16_pair(acc[j + 2].x, acc[j + 2].y), bf16_pair(acc[j + 3].x, acc[j + 3].y));
-        } else {
-#pragma unroll
-          for (int j = 0; j < 64; ++j) {
-            if (col0 + 2 * j < g.N) out[2 * j] = bf16_one(acc[j].x);
-            if (col0 + 2 * j + 1 < g.N) out[2 * j + 1] = bf16_one(acc[j].y);
-          }
-        }
+          for (int i = 0; i < 8; ++i)
+            if (col0 + 2 * j + i < g.N) store_any<1>(g.y, g.ydt, at + 2 * j + i, v + i);
       }
     }
   }
   fence_before();
   __syncthreads();
   if (*s.abort_flag) {
-    if (threadIdx.x == 0) drain_copies(s, first_issued, issued, kStages);
-    if (threadIdx.x == 32) drain_products(s);
+    if (threadIdx.x == 0) {   // the copies are counted on the first CTA's barriers: give them time instead (they take microseconds)
+      const long long t0 = clock64();
+      while (clock64() - t0 < 20000000LL) { }
+    }
+    if (threadIdx.x == 32 && rank == 0) {
+      umma_commit_pair(s.drain);
+      mbar_wait(s.drain, 0, s.abort_flag + 1);
+    }
     __syncthreads();
   }
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * kTileN)) : "memory");
+  cluster_sync_all();          // neither CTA leaves while the other may still signal its barriers or read its tiles
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)(2 * kTileN)) : "memory");
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------
 
-constexpr int kFewThreads = 192;                                // TMA, MMA, 4 epilogue warps
-constexpr int few_stages(int nt) { return nt <= 32 ? 5 : nt == 64 ? 4 : 3; }      // two CTAs fit an SM
+// NT rows of X a tile; from 64 on more epilogue warps share its columns, 32 each
+constexpr int few_warps(int nt) { return nt == 128 ? 16 : nt == 64 ? 8 : 4; }
+constexpr int few_threads(int nt) { return 64 + 32 * few_warps(nt); }             // TMA, MMA, epilogue
+constexpr int few_ctas(int nt) { return nt == 128 ? 1 : 2; }                      // per SM
+constexpr int few_stages(int nt) { return nt <= 32 ? 5 : nt == 64 ? 4 : 6; }
 constexpr uint32_t few_stage_bytes(int nt) { return (128 + nt) * kBlockK; }
-constexpr size_t few_smem(int nt) { return 1024 + (size_t)few_stages(nt) * few_stage_bytes(nt) + 256 + 2 * nt * sizeof(float); }
+constexpr size_t few_smem(int nt) { return 1024 + (size_t)few_stages(nt) * few_stage_bytes(nt) + 256 + kScaleBlocks * nt * sizeof(float); }
 
 template <int NT>
-__global__ void __launch_bounds__(kFewThreads, 2)
+__global__ void __launch_bounds__(few_threads(NT), few_ctas(NT))
 gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const Gemm8Args g) {
-  constexpr int kSt = few_stages(NT);
-  constexpr uint32_t kSB = few_stage_bytes(NT), kColumns = 2 * NT < 32 ? 32 : 2 * NT;
+  constexpr int kSt = few_stages(NT), kWarps = few_warps(NT), kCols = NT * 4 / kWarps;      // columns (rows of X) of a warp
+  constexpr uint32_t kSB = few_stage_bytes(NT), kColumns = kBufs * NT;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), tiles = (raw + 1023u) & ~1023u;
   unsigned char* base = smem_raw + (tiles - raw);
   const Sync s = sync_area(base + (size_t)kSt * kSB, kSt);
-  float* scales = reinterpret_cast<float*>(base + (size_t)kSt * kSB + 256);      // two blocks' scales of the NT rows of X
+  float* scales = reinterpret_cast<float*>(base + (size_t)kSt * kSB + 256);      // [kScaleBlocks][NT]: scale of X times scale of W
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n0 = blockIdx.x * 128, m0 = blockIdx.y * NT, part = blockIdx.z;
   const int b0 = (int)((long long)g.kb * part / g.split), b1 = (int)((long long)g.kb * (part + 1) / g.split);
   if (threadIdx.x == 0) {
-    sync_init(s, kSt, 4);
+    sync_init(s, kSt, kWarps);
     if (g.status_clear && blockIdx.x == 0 && blockIdx.y == 0 && part == 0) *g.status_clear = 0;
   }
   if (warp == 1) {
@@ -289,10 +359,11 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
   fence_after();
   const uint32_t tmem = *s.tmem_slot;
   int issued = 0, first_issued = 0;
-  float2 acc[NT / 2];          // epilogue: row n0 + its TMEM lane of W, NT rows of X
+  Pair acc[kCols / 2];         // epilogue: row n0 + its TMEM lane of W, kCols rows of X from c0 on
 #pragma unroll
-  for (int j = 0; j < NT / 2; ++j) acc[j] = make_float2(0.f, 0.f);
-  const int q = warp & 3, e = q * 32 + lane;      // epilogue warps 2..5: quadrants 2, 3, 0, 1
+  for (int j = 0; j < kCols / 2; ++j) acc[j] = 0;
+  const int q = warp & 3, e = q * 32 + lane;      // epilogue warps 2..: quadrants 2, 3, 0, 1
+  const int c0 = ((warp - 2) >> 2) * kCols, tid = (warp - 2) * 32 + lane;
   if (warp == 0) {
     if (lane == 0) {
       for (int b = b0; b < b1; ++b, ++issued) {
@@ -314,47 +385,61 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
       }
     }
   } else {
+    // kScaleBlocks blocks' scales at a time: the next ones are in registers before they are needed
+    constexpr int kThreadsE = 32 * kWarps, kPer = kScaleBlocks * NT / kThreadsE;
     const float* sw = g.sw + (size_t)blockIdx.x * g.kb;
-    const bool has_scale = e < NT && m0 + e < g.M;
-    const float* sx = g.sx + (size_t)(has_scale ? m0 + e : 0) * g.kb;
-    float mine = has_scale ? __ldg(sx + b0) * __ldg(sw + b0) : 0.f;
-    if (e < NT) scales[e] = mine;
+    float next_x[kPer], next_w[kPer];
+    auto fetch = [&](int b) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int k = i * kThreadsE + tid, row = m0 + k % NT, at = min(b + k / NT, b1 - 1);
+        next_x[i] = row < g.M ? __ldg(g.sx + (size_t)row * g.kb + at) : 0.f;
+        next_w[i] = __ldg(sw + at);
+      }
+    };
+    fetch(b0);
     bool ok = true;
     for (int it = 0; it < b1 - b0; ++it) {
-      const int buf = it & 1, ahead = min(b0 + it + 1, b1 - 1);
-      if (has_scale) mine = __ldg(sx + ahead) * __ldg(sw + ahead);
-      asm volatile("bar.sync 1, 128;" ::: "memory");       // this block's scales are there, the other buffer is free
-      ok = __all_sync(0xffffffffu, ok && mbar_wait(s.part_full + 8 * buf, (it >> 1) & 1, s.abort_flag, g.wait_budget));
-      if (!ok) {                                           // (the barrier above counts every warp in every turn)
+      const int buf = it % kBufs;
+      if (it % kScaleBlocks == 0) {
+        if (it) asm volatile("bar.sync 1, %0;" ::"n"(kThreadsE) : "memory");      // everyone is done with the last ones
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) scales[i * kThreadsE + tid] = next_x[i] * next_w[i];
+        if (it + kScaleBlocks < b1 - b0) fetch(b0 + it + kScaleBlocks);
+        asm volatile("bar.sync 1, %0;" ::"n"(kThreadsE) : "memory");
+      }
+      ok = __all_sync(0xffffffffu, ok && mbar_wait(s.part_full + 8 * buf, (it / kBufs) & 1, s.abort_flag, g.wait_budget));
+      if (!ok) {                                           // (the barriers above count every warp)
         if (lane == 0) { *s.abort_flag = 1; atomicExch(g.status, DRAGON_ERR_TIMEOUT); }
         continue;
       }
       fence_after();
-      const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * NT);
-      const float4* sc = reinterpret_cast<const float4*>(scales + buf * NT);
+      const uint32_t from = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * NT + c0);
+      const float4* sc = reinterpret_cast<const float4*>(scales + it % kScaleBlocks * NT + c0);
+      constexpr int kChunk = kCols < 32 ? kCols : 32;
 #pragma unroll
-      for (int c = 0; c < NT / 16; ++c) {
-        uint32_t v[16];
-        tmem_ld16(from + 16 * c, v);
+      for (int c = 0; c < kCols / kChunk; ++c) {
+        uint32_t v[kChunk];
+        if (kChunk == 16) tmem_ld16(from, v);
+        else tmem_ld32(from + 32 * c, v);
         tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float4 f = sc[4 * c + j];
-          fma_pair(acc[8 * c + 2 * j], v[4 * j], v[4 * j + 1], f.x, f.y);
-          fma_pair(acc[8 * c + 2 * j + 1], v[4 * j + 2], v[4 * j + 3], f.z, f.w);
+        for (int j = 0; j < kChunk / 4; ++j) {
+          const float4 f = sc[kChunk / 4 * c + j];
+          fma_pair(acc[kChunk / 2 * c + 2 * j], v[4 * j], v[4 * j + 1], pack(f.x, f.y));
+          fma_pair(acc[kChunk / 2 * c + 2 * j + 1], v[4 * j + 2], v[4 * j + 3], pack(f.z, f.w));
         }
       }
       fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(s.part_empty + 8 * buf);
-      if (e < NT) scales[(buf ^ 1) * NT + e] = mine;
     }
     if (g.split == 1) {
       if (ok && n0 + e < g.N)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const float v = j & 1 ? acc[j / 2].y : acc[j / 2].x;
-          if (m0 + j < g.M) store_any<1>(g.y, g.ydt, (size_t)(m0 + j) * g.N + n0 + e, &v);
+        for (int j = 0; j < kCols; ++j) {
+          const float v = j & 1 ? unpack(acc[j / 2]).y : unpack(acc[j / 2]).x;
+          if (m0 + c0 + j < g.M) store_any<1>(g.y, g.ydt, (size_t)(m0 + c0 + j) * g.N + n0 + e, &v);
         }
     }
   }
@@ -371,13 +456,14 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
   float* sums = reinterpret_cast<float*>(base);
   if (warp >= 2) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) sums[j * 128 + e] = j & 1 ? acc[j / 2].y : acc[j / 2].x;
+    for (int j = 0; j < kCols; ++j) sums[(c0 + j) * 128 + e] = j & 1 ? unpack(acc[j / 2]).y : unpack(acc[j / 2]).x;
   }
   cluster_sync_all();
   if (warp >= 2) {
     const uint32_t mine = smem_u32(sums);
+    const int step = g.split * (kWarps / 4);      // rows of X go round the CTAs and their groups of four warps
     // eight rows at a time: their loads from the other CTAs' shared memory are in flight together
-    for (int j0 = part; j0 < NT && m0 + j0 < g.M; j0 += 8 * g.split) {
+    for (int j0 = part + g.split * ((warp - 2) >> 2); j0 < NT && m0 + j0 < g.M; j0 += 8 * step) {
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = 0.f;
@@ -386,7 +472,7 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
         float w[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int j = min(j0 + i * g.split, NT - 1);
+          const int j = min(j0 + i * step, NT - 1);
           asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w[i]) : "r"(from + (uint32_t)j * 512) : "memory");
         }
 #pragma unroll
@@ -394,7 +480,7 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int j = j0 + i * g.split;
+        const int j = j0 + i * step;
         if (j < NT && m0 + j < g.M && n0 + e < g.N) store_any<1>(g.y, g.ydt, (size_t)(m0 + j) * g.N + n0 + e, &v[i]);
       }
     }
@@ -437,7 +523,7 @@ cudaError_t launch_few(const CUtensorMap& tx, const CUtensorMap& tw, const Gemm8
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((g.N + 127) / 128, (g.M + NT - 1) / NT, g.split);
-  cfg.blockDim = dim3(kFewThreads);
+  cfg.blockDim = dim3(few_threads(NT));
   cfg.dynamicSmemBytes = few_smem(NT);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -462,25 +548,36 @@ int launch_gemm_e4m3(const StepRun& r) {
   if (tiles_m * tiles_n > 0x3fffffffLL) { set_error("ScaledInnerProduct: too many tiles"); return DRAGON_ERR_UNSUPPORTED; }
   g.tiles_m = (int)tiles_m;
   g.tiles_n = (int)tiles_n;
-  // The large tiles wherever they give every SM one; otherwise the small ones, their blocks split while CTAs find room
-  const bool few = tiles_m * tiles_n < r.sm_count;
+  // The large tiles wherever they give every pair of SMs one; otherwise the small ones, their blocks split while CTAs find room
+  const int pairs = r.sm_count / 2;
+  const bool few = tiles_m * tiles_n < pairs || g.M <= 128;
   const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
   CUtensorMap tx, tw;
-  if (!make_tmap8(&tx, r.rd(g8::XQ), g.M, g.K, few ? nt : kTileM) || !make_tmap8(&tw, r.rd(g8::WQ), g.N, g.K, few ? 128 : kTileN)) {
+  if (!make_tmap8(&tx, r.rd(g8::XQ), g.M, g.K, few ? nt : 128) || !make_tmap8(&tw, r.rd(g8::WQ), g.N, g.K, 128)) {
     set_error("ScaledInnerProduct: cannot encode the TMA descriptors (no CUDA driver?)");
     return DRAGON_ERR_CUDA;
   }
   cudaError_t e;
   if (few) {
     const int64_t ctas = (int64_t)((g.N + 127) / 128) * ((g.M + nt - 1) / nt);
-    while (g.split < 8 && ctas * g.split * 2 <= 2 * r.sm_count && g.kb >= 4 * g.split) g.split *= 2;
+    if ((g.M + nt - 1) / nt > 65535) { set_error("ScaledInnerProduct: too many rows"); return DRAGON_ERR_UNSUPPORTED; }
+    while (g.split < 8 && ctas * g.split * 2 <= few_ctas(nt) * r.sm_count && g.kb >= 4 * g.split) g.split *= 2;
     e = nt == 16 ? launch_few<16>(tx, tw, g, 1, st) : nt == 32 ? launch_few<32>(tx, tw, g, 2, st)
         : nt == 64 ? launch_few<64>(tx, tw, g, 3, st) : launch_few<128>(tx, tw, g, 4, st);
   } else {
     e = allow_smem(reinterpret_cast<const void*>(gemm_e4m3_kernel), kSmem, 0);
     if (e == cudaSuccess) {
-      gemm_e4m3_kernel<<<std::min(g.tiles_m * g.tiles_n, r.sm_count), kThreads, kSmem, st>>>(tx, tw, g);
-      e = cudaGetLastError();
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(2 * std::min(g.tiles_m * g.tiles_n, pairs));
+      cfg.blockDim = dim3(kThreads);
+      cfg.dynamicSmemBytes = kSmem;
+      cfg.stream = st;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      e = cudaLaunchKernelEx(&cfg, gemm_e4m3_kernel, tx, tw, g);
     }
   }
   if (e != cudaSuccess) { set_error("ScaledInnerProduct: launch failed: %s", cudaGetErrorString(e)); return DRAGON_ERR_CUDA; }
