@@ -6,12 +6,14 @@
 // Bound: bytes.  A recurrence h -> f h + b composes: rows r..s act on the state in front of them as h -> A h + B with A the
 // product of the f and B the state they reach from 0.  A tile is kScanTileRows rows x 64 columns; each warp of a CTA folds
 // its rows into (A, B) from registers, the warps' pairs are folded through shared memory, and the state in front of the
-// tile comes from the tiles before it: a tile publishes its (A, B) as soon as it has it and its end state once it knows its
-// start; a tile looks back over published pairs until it meets an end state.  Everything is read once and written once,
-// whatever the number of sequences: a long one is spread over the whole GPU.  Tiles are handed out by a counter in time
-// order, so a tile waits only for tiles that are running or done; the wait is bounded (DRAGON_ERR_TIMEOUT).
-// Published words need no flags and no fences: the exchange area is filled with a bit pattern that no arithmetic
-// produces (a NaN other than the canonical one) before the launch, and a word that differs from it is there.
+// tile comes from the tiles before it.  Tiles form runs of 32: every tile publishes its (A, B) as soon as it has it; a tile
+// reads those of the tiles before it in its run (the warps share them, all loads in flight together), and the state in front
+// of the run, which the last tile of the run before published.  What is added to what is fixed by the tile's place alone, so
+// every run of the kernel gives the same bits; a long sequence passes 1/32 of its tiles one after another.  Everything is
+// read once and written once, whatever the number of sequences: a long one is spread over the whole GPU.  Tiles are handed
+// out by a counter in the order of the chain, so a tile waits only for tiles that are running or done; the wait is bounded
+// (DRAGON_ERR_TIMEOUT).  Published words need no flags and no fences: the exchange area is filled with a bit pattern that no
+// arithmetic produces (a NaN other than the canonical one) before the launch, and a word that differs from it is there.
 // A row that starts afresh cuts the chain by selection, not by a factor of 0: what is in front of it cannot reach it, NaN
 // or not.  The state is fp32; the gradient recomputes it from the state in front of each tile, which the forward keeps.
 #include <algorithm>
@@ -22,13 +24,16 @@
 namespace dragon {
 namespace {
 
-// The forward folds 16 rows a warp (4 CTAs of 4 warps per SM, next tile's rows loading), the gradient, which holds three
-// tensors' rows and five values per element, 8 (2 CTAs of 8 warps).  Measured on 65536 x 1024 bf16: forward 4 x 16 rows
-// 160 us, 8 x 8 178, 8 x 16 (tiles of 128) 154; gradient 8 x 8 320, 16 x 8 (tiles of 128) 347.
+// The forward folds 16 rows a warp (4 CTAs of 4 warps per SM, the next tile's rows on their way), the gradient, which holds
+// three tensors' rows and three values per element, 8 (2 CTAs of 8 warps).  Measured on 65536 x 1024 bf16, one sequence (and
+// 1024 of them, where no tile needs another): forward 4 x 16 rows 175 us (112), 8 x 8 199 (117), folding one tile ahead of the
+// one that waits 242 (143: the second tile's registers cost more than the wait); gradient 337 (258).  The bytes alone: 61, 143.
 constexpr int kFwdWarps = 4, kBwdWarps = 8, kFwdCtas = 4, kBwdCtas = 2;
 template <int W> constexpr int rows_per_warp() { return kScanTileRows / W; }
 constexpr long long kWaitBudgetCycles = 4000000000LL;   // about two seconds
 constexpr unsigned kAbsent = 0xffffffffu;          // an exchange word that has not been written
+constexpr unsigned kClosed = 0xfffffffeu;          // in the place of A: a row of the tile starts afresh, its end state is B whatever comes in
+constexpr int kRun = 32;                           // tiles of a run
 
 struct ScanArgs {
   const void *gate, *x, *h0, *dh;
@@ -39,8 +44,8 @@ struct ScanArgs {
   int rows, cols, length;  // length: rows per sequence
   int tiles, groups;       // tiles of kScanTileRows rows, groups of 32 * CH columns
   unsigned* counter;       // tickets (starts at kAbsent)
-  uint4* pair;             // exchange area: per tile and group 32 lanes' pairs (A, A', B, B'), null if no tile needs another
-  uint2* end;              // ... and end states
+  uint4* pair;             // exchange area: per tile (in the chain's order) and group 32 lanes' pairs (A, A', B, B'), null if no tile needs another
+  uint2* start;            // ... and per run and group the state in front of it
   int *status, *status_clear;
 };
 
@@ -92,13 +97,41 @@ template <int DT, int CH> __device__ __forceinline__ void store_cell(char* p, in
   }
 }
 
+// CH neighbouring columns' values; pairs go through the packed instructions (each half rounded as the scalar one rounds)
+template <int CH> struct Vec { float v[CH]; };
+template <int CH> __device__ __forceinline__ Vec<CH> splat(float x) { Vec<CH> r; for (int e = 0; e < CH; ++e) r.v[e] = x; return r; }
+__device__ __forceinline__ unsigned long long packed(const Vec<2>& a) { unsigned long long r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.v[0]), "f"(a.v[1])); return r; }
+__device__ __forceinline__ Vec<2> unpacked(unsigned long long a) { Vec<2> r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.v[0]), "=f"(r.v[1]) : "l"(a)); return r; }
+__device__ __forceinline__ Vec<2> mul(const Vec<2>& a, const Vec<2>& b) { unsigned long long r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(packed(a)), "l"(packed(b))); return unpacked(r); }
+__device__ __forceinline__ Vec<2> add(const Vec<2>& a, const Vec<2>& b) { unsigned long long r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(packed(a)), "l"(packed(b))); return unpacked(r); }
+__device__ __forceinline__ Vec<2> fma(const Vec<2>& a, const Vec<2>& b, const Vec<2>& c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(packed(a)), "l"(packed(b)), "l"(packed(c)));
+  return unpacked(r);
+}
+__device__ __forceinline__ Vec<1> mul(const Vec<1>& a, const Vec<1>& b) { return {{__fmul_rn(a.v[0], b.v[0])}}; }
+__device__ __forceinline__ Vec<1> add(const Vec<1>& a, const Vec<1>& b) { return {{__fadd_rn(a.v[0], b.v[0])}}; }
+__device__ __forceinline__ Vec<1> fma(const Vec<1>& a, const Vec<1>& b, const Vec<1>& c) { return {{__fmaf_rn(a.v[0], b.v[0], c.v[0])}}; }
+
 // f and 1 - f = exp(-z) f, each to full relative precision (two units or so); exp(-z) is kept finite, a NaN stays one
 __device__ __forceinline__ void gate_of(float z, float* f, float* keep) {
   float u = -z * 1.4426950408889634f, t;
   asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(u) : "f"(u));      // 126
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(u));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(*f) : "f"(1.f + t));
-  *keep = t * *f;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(*f) : "f"(__fadd_rn(1.f, t)));
+  *keep = __fmul_rn(t, *f);
+}
+template <int CH> __device__ __forceinline__ void gate_of(const Vec<CH>& z, Vec<CH>* f, Vec<CH>* keep) {
+  Vec<CH> u = mul(z, splat<CH>(-1.4426950408889634f)), t;
+#pragma unroll
+  for (int e = 0; e < CH; ++e) {
+    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(u.v[e]) : "f"(u.v[e]));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.v[e]) : "f"(u.v[e]));
+  }
+  u = add(t, splat<CH>(1.f));
+#pragma unroll
+  for (int e = 0; e < CH; ++e) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f->v[e]) : "f"(u.v[e]));
+  *keep = mul(t, *f);
 }
 
 // which of a warp's rows exist, start afresh, and start from h0: lane r looks at row r
@@ -144,88 +177,103 @@ __device__ __forceinline__ uint2 look(const uint2* p) {
 // Every value that is published goes through this: an arithmetic result is never kAbsent (NaNs come out canonical)
 __device__ __forceinline__ float computed(float v) { return __fadd_rn(v, 0.f); }
 
-// What one warp (2 columns a lane) hands on for its tile, and what it finds in front of it.  dir -1: the state, from the
-// tiles before it; +1: the gradient, from the tiles behind it.  `closed`: a row of the tile starts afresh, so the end
-// state is B whatever comes in.
-__device__ __forceinline__ size_t slot_of(const ScanArgs& a, int tile, int group, int lane) { return ((size_t)tile * a.groups + group) * 32 + lane; }
-__device__ __forceinline__ void publish_pair(const ScanArgs& a, int tile, int group, int lane, float4 ab, bool closed, int last) {
-  const size_t s = slot_of(a, tile, group, lane);
-  if (closed || tile == last) put(a.end + s, make_float2(computed(ab.z), computed(ab.w)));
-  else put(a.pair + s, make_float4(computed(ab.x), computed(ab.y), computed(ab.z), computed(ab.w)));
+// `order`: a tile's place in the chain (its number, or counted from the end for the gradient)
+__device__ __forceinline__ size_t slot_of(const ScanArgs& a, int order, int group, int lane) { return ((size_t)order * a.groups + group) * 32 + lane; }
+__device__ __forceinline__ void publish_pair(const ScanArgs& a, int order, int group, int lane, float4 ab, bool closed) {
+  const float none = __uint_as_float(kClosed);
+  put(a.pair + slot_of(a, order, group, lane), make_float4(closed ? none : computed(ab.x), closed ? none : computed(ab.y), computed(ab.z), computed(ab.w)));
 }
-__device__ __forceinline__ float2 look_back(const ScanArgs& a, int tile, int group, int lane, int dir, int last) {
-  constexpr int kAhead = 4;                        // tiles looked at together
-  float2 in = make_float2(0.f, 0.f);
-  float4 acc = make_float4(1.f, 1.f, 0.f, 0.f);    // the tiles between the one looked at and this one
-  int at = tile + dir;
-  const long long t0 = clock64();
-  for (bool done = tile == last; !done;) {
-    uint4 p[kAhead];
-    uint2 e[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const int t = dir < 0 ? max(at - i, last) : min(at + i, last);
-      const size_t s = slot_of(a, t, group, lane);
-      p[i] = look(a.pair + s);
-      e[i] = look(a.end + s);
-    }
-    bool moving = true;
-    int moved = 0;
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const bool has_end = e[i].x != kAbsent && e[i].y != kAbsent;
-      const bool has_pair = p[i].x != kAbsent && p[i].y != kAbsent && p[i].z != kAbsent && p[i].w != kAbsent;
-      if (moving && !done && has_end) {
-        in = make_float2(fmaf(acc.x, __uint_as_float(e[i].x), acc.z), fmaf(acc.y, __uint_as_float(e[i].y), acc.w));
-        done = true;
-      }
-      moving = moving && !done && has_pair;        // (the last tile has an end state and no pair: nothing moves past it)
-      if (moving) {
-        acc.z = fmaf(acc.x, __uint_as_float(p[i].z), acc.z);
-        acc.w = fmaf(acc.y, __uint_as_float(p[i].w), acc.w);
-        acc.x *= __uint_as_float(p[i].x);
-        acc.y *= __uint_as_float(p[i].y);
-        ++moved;
-      }
-    }
-    at += dir * moved;
-    if (!done && moved == 0 && clock64() - t0 > kWaitBudgetCycles) {
-      atomicExch(a.status, DRAGON_ERR_TIMEOUT);
-      done = true;
-    }
-  }
-  __syncwarp();
-  return in;
+// the state behind a run's last tile, for the next run
+__device__ __forceinline__ void publish_start(const ScanArgs& a, int order, int group, int lane, float2 v) {
+  if (order % kRun == kRun - 1) put(a.start + slot_of(a, order / kRun + 1, group, lane), make_float2(computed(v.x), computed(v.y)));
 }
-__device__ __forceinline__ void publish_end(const ScanArgs& a, int tile, int group, int lane, float4 ab, float2 in) {
-  put(a.end + slot_of(a, tile, group, lane), make_float2(computed(fmaf(ab.x, in.x, ab.z)), computed(fmaf(ab.y, in.y, ab.w))));
+__device__ __forceinline__ bool out_of_time(const ScanArgs& a, long long t0) {
+  if (clock64() - t0 <= kWaitBudgetCycles) return false;
+  atomicExch(a.status, DRAGON_ERR_TIMEOUT);
+  return true;
 }
 
-template <int W> struct TileShared {
-  float4 ab[W][32];          // each warp's pair (A, A', B, B')
-  unsigned fresh[W];         // whether one of its rows starts afresh
-  float2 in[32];             // the state in front of the tile
-  unsigned ticket;
+// what the warps of a CTA exchange; kCopies: tiles whose pairs are alive at a time
+template <int W, int kCopies> struct TileShared {
+  float4 ab[kCopies][W][32];     // each warp's pair (A, A', B, B')
+  unsigned fresh[kCopies][W];    // its rows that start afresh
+  unsigned ticket[kCopies];
+  float4 seg[W][32];             // the pairs of the run's tiles in front of this one, folded by each warp's share
+  bool seg_closed[W];
 };
 
+// This warp's share of the run's tiles in front of tile `order`: their pairs, folded in order (waits for them)
+template <int W, int K> __device__ __forceinline__ void fold_run(const ScanArgs& a, TileShared<W, K>& sh, int order, int group, int warp, int lane) {
+  constexpr int kShare = kRun / W;
+  const int first = order / kRun * kRun + warp * kShare, n = min(kShare, order - first);
+  float4 ab = make_float4(1.f, 1.f, 0.f, 0.f);
+  bool closed = false;
+  constexpr int kAhead = 4;                        // loads in flight together
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += kAhead) {
+    uint4 p[kAhead];
+    const long long t0 = clock64();
+    for (;;) {
+      bool all = true;
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) p[i] = look(a.pair + slot_of(a, first + min(i0 + i, n - 1), group, lane));
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) all = all && p[i].x != kAbsent && p[i].y != kAbsent && p[i].z != kAbsent && p[i].w != kAbsent;
+      if (__all_sync(0xffffffffu, all) || out_of_time(a, t0)) break;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i0 + i < n) {
+        const float4 q = make_float4(__uint_as_float(p[i].x), __uint_as_float(p[i].y), __uint_as_float(p[i].z), __uint_as_float(p[i].w));
+        if (p[i].x == kClosed) { ab = q; closed = true; }      // (closed for all columns or for none)
+        else ab = make_float4(ab.x * q.x, ab.y * q.y, fmaf(q.x, ab.z, q.z), fmaf(q.y, ab.w, q.w));
+      }
+  }
+  sh.seg[warp][lane] = ab;
+  if (lane == 0) sh.seg_closed[warp] = closed;
+}
+// ... and, after a barrier, the state in front of tile `order`
+template <int W, int K> __device__ __forceinline__ float2 state_in_front(const ScanArgs& a, const TileShared<W, K>& sh, int order, int group, int lane) {
+  float2 v = make_float2(0.f, 0.f);
+  const int run = order / kRun;
+  bool cut = run == 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) cut = cut || sh.seg_closed[w];
+  if (!cut) {
+    const uint2* from = a.start + slot_of(a, run, group, lane);
+    uint2 u = look(from);
+    const long long t0 = clock64();
+    while ((u.x == kAbsent || u.y == kAbsent) && !out_of_time(a, t0)) u = look(from);
+    __syncwarp();
+    v = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+  }
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float4 p = sh.seg[w][lane];
+    v = sh.seg_closed[w] ? make_float2(p.z, p.w) : make_float2(fmaf(p.x, v.x, p.z), fmaf(p.y, v.y, p.w));
+  }
+  return v;
+}
+
 // fold of warps [w0, w1) in time order (dir 1) or against it, applied to `in`
-template <int W> __device__ __forceinline__ float2 through(const TileShared<W>& sh, int lane, int w0, int w1, int dir, float2 in) {
+__device__ __forceinline__ float2 through(const float4 (*ab)[32], const unsigned* fresh, int lane, int w0, int w1, int dir, float2 in) {
 #pragma unroll 4
   for (int w = w0; w != w1; w += dir) {
-    const float4 p = sh.ab[w][lane];
-    in = sh.fresh[w] ? make_float2(p.z, p.w) : make_float2(fmaf(p.x, in.x, p.z), fmaf(p.y, in.y, p.w));
+    const float4 p = ab[w][lane];
+    in = fresh[w] ? make_float2(p.z, p.w) : make_float2(fmaf(p.x, in.x, p.z), fmaf(p.y, in.y, p.w));
   }
   return in;
 }
 // the tile's own pair and whether it is closed
-template <int W> __device__ __forceinline__ float4 fold_tile(const TileShared<W>& sh, int lane, int dir, bool* closed) {
+template <int W> __device__ __forceinline__ float4 fold_tile(const float4 (*abs)[32], const unsigned* fresh, int lane, int dir, bool* closed) {
   float4 ab = make_float4(1.f, 1.f, 0.f, 0.f);
   *closed = false;
-#pragma unroll 8
+#pragma unroll
   for (int i = 0; i < W; ++i) {
     const int w = dir > 0 ? i : W - 1 - i;
-    const float4 p = sh.ab[w][lane];
-    if (sh.fresh[w]) { ab = make_float4(0.f, 0.f, p.z, p.w); *closed = true; }
+    const float4 p = abs[w][lane];
+    if (fresh[w]) { ab = make_float4(0.f, 0.f, p.z, p.w); *closed = true; }
     else ab = make_float4(ab.x * p.x, ab.y * p.y, fmaf(p.x, ab.z, p.z), fmaf(p.y, ab.w, p.w));
   }
   return ab;
@@ -233,27 +281,33 @@ template <int W> __device__ __forceinline__ float4 fold_tile(const TileShared<W>
 
 // Tiles in the order they are handed out.  With an exchange area the counter decides (it starts at kAbsent, so the first
 // ticket is 0 after the increment); without one any order will do.
-__device__ __forceinline__ unsigned next_ticket(const ScanArgs& a, unsigned now) { return a.pair ? atomicAdd(a.counter, 1u) + 1u : now + gridDim.x; }
+__device__ __forceinline__ unsigned take_tickets(const ScanArgs& a, unsigned count) { return atomicAdd(a.counter, count) + 1u; }
 
-// initial states of the rows that start a sequence: h0v[r] for the bits of m.from_h0
+// initial states of the rows that start a sequence: v[r] for the bits of m.from_h0, else 0
 template <int CH, int kRows>
-__device__ __forceinline__ void load_h0(const ScanArgs& a, const RowMarks& m, int c, float (*v)[CH]) {
+__device__ __forceinline__ void load_h0(const ScanArgs& a, const RowMarks& m, int c, Vec<CH> (&v)[kRows]) {
 #pragma unroll
   for (int r = 0; r < kRows; ++r) {
     const size_t at = (size_t)__shfl_sync(0xffffffffu, m.seq, r) * a.cols + c;
-    const bool want = m.from_h0 >> r & 1;
+    const bool want = a.h0 && (m.from_h0 >> r & 1);
 #pragma unroll
     for (int e = 0; e < CH; ++e) {
-      v[r][e] = 0.f;
-      if (want && a.h0dt == DRAGON_F32) v[r][e] = __ldg(reinterpret_cast<const float*>(a.h0) + at + e);
-      if (want && a.h0dt == DRAGON_BF16) v[r][e] = bf16_low(__ldg(reinterpret_cast<const unsigned short*>(a.h0) + at + e));
+      v[r].v[e] = 0.f;
+      if (want && a.h0dt == DRAGON_F32) v[r].v[e] = __ldg(reinterpret_cast<const float*>(a.h0) + at + e);
+      if (want && a.h0dt == DRAGON_BF16) v[r].v[e] = bf16_low(__ldg(reinterpret_cast<const unsigned short*>(a.h0) + at + e));
     }
   }
 }
 
-// One tile's rows of one warp as they come from memory; rows behind the tensor repeat its last one
+// One tile's rows of one warp, of N tensors, as they come from memory; rows behind the tensor repeat its last one
 template <int DT, int CH, int N, int kRows> struct TileRows {
   Cell<DT, CH> v[N][kRows];
+  __device__ __forceinline__ Vec<CH> get(int k, int r) const {
+    Vec<CH> x;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) x.v[e] = v[k][r].get(e);
+    return x;
+  }
   __device__ __forceinline__ void load(const ScanArgs& a, int row0, int c) {
     const void* src[3] = {a.gate, a.x, a.dh};
     const int dt[3] = {a.gdt, a.xdt, a.dhdt};
@@ -284,135 +338,153 @@ struct Place {
   }
 };
 
-// Persistent CTAs.  While a tile's warp 0 looks back, the next tile's rows are on their way.
+// A tile between its fold and its output: f and b = (1 - f) x (+ f h0 where a sequence starts) of a thread's rows
+template <int CH, int kRows> struct Folded {
+  Vec<CH> f[kRows], b[kRows];
+  unsigned fresh;      // rows that start afresh
+  int n;               // rows inside the tensor
+  Place at;
+};
+
+// Persistent CTAs.  While a tile waits for what is in front of it, the next tile's rows are on their way.
 template <int DT, int CH>
 __global__ void __launch_bounds__(kFwdWarps * 32, kFwdCtas) scan_kernel(const ScanArgs a) {
-  constexpr int kRows = rows_per_warp<kFwdWarps>(), kThreads = kFwdWarps * 32;
-  __shared__ TileShared<kFwdWarps> sh;
+  constexpr int W = kFwdWarps, kRows = rows_per_warp<W>();
+  __shared__ TileShared<W, 3> sh;
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned n = (unsigned)a.tiles * a.groups;
-  unsigned ticket = blockIdx.x;
+  unsigned ticket = blockIdx.x;          // of the tile whose rows are on their way
   if (a.pair) {
-    if (threadIdx.x == 0) sh.ticket = next_ticket(a, 0);
+    if (threadIdx.x == 0) sh.ticket[0] = take_tickets(a, 1);
     __syncthreads();
-    ticket = sh.ticket;
+    ticket = sh.ticket[0];
+    __syncthreads();
   }
   TileRows<DT, CH, 2, kRows> rows;
-  Place next = Place::of<false>(a, ticket);
-  auto load_next = [&] { rows.load(a, next.tile * kScanTileRows + warp * kRows, min((next.group * 32 + lane) * CH, a.cols - CH)); };
-  if (ticket < n) load_next();
-  while (ticket < n) {
-    const int tile = next.tile, group = next.group;
-    const int c0 = (group * 32 + lane) * CH, row0 = tile * kScanTileRows + warp * kRows;
-    const bool mine = c0 < a.cols;
-    const int c = min(c0, a.cols - CH);
-    const RowMarks m = row_marks<kFwdWarps>(a, row0, lane);
-    float f[kRows][CH], b[kRows][CH];
+  auto load = [&] {
+    if (ticket >= n) return;
+    const Place p = Place::of<false>(a, ticket);
+    rows.load(a, p.tile * kScanTileRows + warp * kRows, min((p.group * 32 + lane) * CH, a.cols - CH));
+  };
+  auto column = [&](const Place& p) { return min((p.group * 32 + lane) * CH, a.cols - CH); };
+  // the rows that have come become a folded tile; the next ones are sent for
+  auto fold = [&](Folded<CH, kRows>& o, int copy) {
+    o.at = Place::of<false>(a, ticket);
+    const RowMarks m = row_marks<W>(a, o.at.tile * kScanTileRows + warp * kRows, lane);
+    o.fresh = m.fresh;
+    o.n = m.n;
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-#pragma unroll
-      for (int e = 0; e < CH; ++e) {
-        float keep;
-        gate_of(rows.v[0][r].get(e), &f[r][e], &keep);
-        b[r][e] = keep * rows.v[1][r].get(e);
-      }
+    for (int r = 0; r < kRows; ++r) {
+      Vec<CH> keep;
+      gate_of(rows.get(0, r), &o.f[r], &keep);
+      o.b[r] = mul(keep, rows.get(1, r));
+    }
     if (m.n < kRows) {       // rows behind the tensor pass the state on
 #pragma unroll
       for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e)
-          if (r >= m.n) { f[r][e] = 1.f; b[r][e] = 0.f; }
+        if (r >= m.n) { o.f[r] = splat<CH>(1.f); o.b[r] = splat<CH>(0.f); }
     }
     if (a.h0 && m.from_h0) {
-      float v[kRows][CH];
-      load_h0<CH, kRows>(a, m, c, v);
+      Vec<CH> v[kRows];
+      load_h0<CH, kRows>(a, m, column(o.at), v);
 #pragma unroll
       for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e)
-          if (m.from_h0 >> r & 1) b[r][e] = fmaf(f[r][e], v[r][e], b[r][e]);
+        if (m.from_h0 >> r & 1) o.b[r] = fma(o.f[r], v[r], o.b[r]);
     }
-    float A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f};
+    Vec<CH> A = splat<CH>(1.f), B = splat<CH>(0.f);
     if (m.fresh == 0) {
 #pragma unroll
-      for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e) { A[e] *= f[r][e]; B[e] = fmaf(f[r][e], B[e], b[r][e]); }
+      for (int r = 0; r < kRows; ++r) { A = mul(A, o.f[r]); B = fma(o.f[r], B, o.b[r]); }
     } else {
 #pragma unroll
-      for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e) B[e] = (m.fresh >> r & 1) ? b[r][e] : fmaf(f[r][e], B[e], b[r][e]);
+      for (int r = 0; r < kRows; ++r) B = (m.fresh >> r & 1) ? o.b[r] : fma(o.f[r], B, o.b[r]);
     }
-    sh.ab[warp][lane] = make_float4(A[0], A[1], B[0], B[1]);
-    if (lane == 0) sh.fresh[warp] = m.fresh;
-    if (threadIdx.x == kThreads - 1) sh.ticket = next_ticket(a, ticket);
+    sh.ab[copy][warp][lane] = make_float4(A.v[0], A.v[CH - 1], B.v[0], B.v[CH - 1]);
+    if (lane == 0) sh.fresh[copy][warp] = m.fresh;
+    if (threadIdx.x == W * 32 - 1) sh.ticket[copy] = a.pair ? take_tickets(a, 1) : ticket + gridDim.x;
     __syncthreads();
-    ticket = sh.ticket;
-    next = Place::of<false>(a, ticket);
-    bool closed = true;
-    float4 ab;
-    if (warp == 0 && a.pair) {
-      ab = fold_tile(sh, lane, 1, &closed);
-      publish_pair(a, tile, group, lane, ab, closed, 0);
+    ticket = sh.ticket[copy];
+    load();
+    if (a.pair && warp == 0) {
+      bool closed;
+      const float4 ab = fold_tile<W>(sh.ab[copy], sh.fresh[copy], lane, 1, &closed);
+      publish_pair(a, o.at.tile, o.at.group, lane, ab, closed);
+      if (closed) publish_start(a, o.at.tile, o.at.group, lane, make_float2(ab.z, ab.w));
     }
-    if (ticket < n) load_next();
-    if (warp == 0) {
-      float2 in = make_float2(0.f, 0.f);
-      if (a.pair && !(m.fresh & 1)) in = look_back(a, tile, group, lane, -1, 0);
-      if (a.pair && !closed && tile != 0) publish_end(a, tile, group, lane, ab, in);
-      sh.in[lane] = in;
-      if (a.carry && mine) {
-        float* p = a.carry + (size_t)tile * a.cols + c;
-        p[0] = in.x;
-        if (CH == 2) p[1] = in.y;
+  };
+  // a folded tile's state in front, end state and output
+  auto finish = [&](const Folded<CH, kRows>& o, int copy) {
+    float2 front = make_float2(0.f, 0.f);
+    if (a.pair) {
+      const bool open = !(sh.fresh[copy][0] & 1);         // the tile's first row goes on from the tile before
+      if (open) {
+        fold_run(a, sh, o.at.tile, o.at.group, warp, lane);
+        __syncthreads();
+        front = state_in_front(a, sh, o.at.tile, o.at.group, lane);
+      }
+      if (warp == 0 && o.at.tile % kRun == kRun - 1) {
+        bool closed;
+        const float4 ab = fold_tile<W>(sh.ab[copy], sh.fresh[copy], lane, 1, &closed);
+        if (!closed) publish_start(a, o.at.tile, o.at.group, lane, make_float2(fmaf(ab.x, front.x, ab.z), fmaf(ab.y, front.y, ab.w)));
       }
     }
-    __syncthreads();
-    if (a.h) {
-      const float2 in = through(sh, lane, 0, warp, 1, sh.in[lane]);
-      float h[2] = {in.x, in.y};
-      const int es = element_bytes<DT>(a.hdt);
-      char* p = reinterpret_cast<char*>(a.h) + ((size_t)row0 * a.cols + c) * es;
-      const size_t step = (size_t)a.cols * es;
-      if (m.fresh == 0 && m.n == kRows) {
+    const int c = column(o.at), row0 = o.at.tile * kScanTileRows + warp * kRows;
+    const bool mine = (o.at.group * 32 + lane) * CH < a.cols;
+    if (warp == 0 && a.carry && mine) {
+      float* p = a.carry + (size_t)o.at.tile * a.cols + c;
+      p[0] = front.x;
+      if (CH == 2) p[1] = front.y;
+    }
+    if (!a.h) return;
+    const float2 in = through(sh.ab[copy], sh.fresh[copy], lane, 0, warp, 1, front);
+    Vec<CH> h;
+    h.v[0] = in.x;
+    h.v[CH - 1] = CH == 2 ? in.y : in.x;
+    const int es = element_bytes<DT>(a.hdt);
+    char* p = reinterpret_cast<char*>(a.h) + ((size_t)row0 * a.cols + c) * es;
+    const size_t step = (size_t)a.cols * es;
+    if (o.fresh == 0 && o.n == kRows) {
 #pragma unroll
-        for (int r = 0; r < kRows; ++r, p += step) {
+      for (int r = 0; r < kRows; ++r, p += step) {
+        h = fma(o.f[r], h, o.b[r]);
+        if (mine) store_cell<DT, CH>(p, a.hdt, h.v);
+      }
+    } else {
 #pragma unroll
-          for (int e = 0; e < CH; ++e) h[e] = fmaf(f[r][e], h[e], b[r][e]);
-          if (mine) store_cell<DT, CH>(p, a.hdt, h);
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < kRows; ++r, p += step) {
-#pragma unroll
-          for (int e = 0; e < CH; ++e) h[e] = (m.fresh >> r & 1) ? b[r][e] : fmaf(f[r][e], h[e], b[r][e]);
-          if (mine && r < m.n) store_cell<DT, CH>(p, a.hdt, h);
-        }
+      for (int r = 0; r < kRows; ++r, p += step) {
+        h = (o.fresh >> r & 1) ? o.b[r] : fma(o.f[r], h, o.b[r]);
+        if (mine && r < o.n) store_cell<DT, CH>(p, a.hdt, h.v);
       }
     }
-    __syncthreads();         // the pairs and the state have been read
+  };
+  // three copies of the pairs in turn: a copy is written again only behind two barriers that follow its last use
+  load();
+  Folded<CH, kRows> tile;
+  for (int copy = 0; ticket < n; copy = copy == 2 ? 0 : copy + 1) {
+    fold(tile, copy);
+    finish(tile, copy);
   }
 }
 
 template <int DT, int CH>
 __global__ void __launch_bounds__(kBwdWarps * 32, kBwdCtas) scan_bwd_kernel(const ScanArgs a) {
-  constexpr int kWarps = kBwdWarps, kRows = rows_per_warp<kBwdWarps>();
-  __shared__ TileShared<kBwdWarps> sh, back;
+  constexpr int W = kBwdWarps, kRows = rows_per_warp<W>();
+  __shared__ TileShared<W, 2> sh;        // copy 0: the state's pairs, copy 1: the gradient's
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned n = (unsigned)a.tiles * a.groups;
+  const bool plain_out = a.dx && a.dgate && a.dxdt == DRAGON_F32 && a.dgdt == DRAGON_F32;
   unsigned ticket = blockIdx.x;
   if (a.pair) {
-    if (threadIdx.x == 0) sh.ticket = next_ticket(a, 0);
+    if (threadIdx.x == 0) sh.ticket[0] = take_tickets(a, 1);
     __syncthreads();
-    ticket = sh.ticket;
+    ticket = sh.ticket[0];
+    __syncthreads();
   }
-  const bool plain_out = a.dx && a.dgate && a.dxdt == DRAGON_F32 && a.dgdt == DRAGON_F32;
   while (ticket < n) {
     const Place at = Place::of<true>(a, ticket);      // tickets against time
-    const int tile = at.tile, group = at.group;
+    const int tile = at.tile, group = at.group, order = a.tiles - 1 - tile;
     const int c0 = (group * 32 + lane) * CH, row0 = tile * kScanTileRows + warp * kRows;
     const bool mine = c0 < a.cols;
     const int c = min(c0, a.cols - CH);
@@ -421,127 +493,106 @@ __global__ void __launch_bounds__(kBwdWarps * 32, kBwdCtas) scan_bwd_kernel(cons
     float carry[2] = {0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < CH; ++e) carry[e] = __ldg(a.carry + (size_t)tile * a.cols + c + e);
-    const RowMarks m = row_marks<kBwdWarps>(a, row0, lane);
+    const RowMarks m = row_marks<W>(a, row0, lane);
     const bool plain = m.n == kRows && m.fresh == 0;
-    float f[kRows][CH], keep[kRows][CH], hp[kRows][CH];      // hp: the state in front of the row
+    Vec<CH> f[kRows], keep[kRows], hp[kRows];      // hp: the state in front of the row
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-#pragma unroll
-      for (int e = 0; e < CH; ++e) gate_of(rows.v[0][r].get(e), &f[r][e], &keep[r][e]);
+    for (int r = 0; r < kRows; ++r) gate_of(rows.get(0, r), &f[r], &keep[r]);
     if (m.n < kRows) {       // rows behind the tensor pass the state and the gradient on
 #pragma unroll
       for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e)
-          if (r >= m.n) { f[r][e] = 1.f; keep[r][e] = 0.f; }
+        if (r >= m.n) { f[r] = splat<CH>(1.f); keep[r] = splat<CH>(0.f); }
     }
     // pairs of the state and of the gradient e -> f (dh + e)
-    float A[2] = {1.f, 1.f}, B[2] = {0.f, 0.f}, E[2] = {0.f, 0.f};
+    Vec<CH> A = splat<CH>(1.f), B = splat<CH>(0.f), E = splat<CH>(0.f);
     if (plain) {
 #pragma unroll
-      for (int r = 0; r < kRows; ++r)
+      for (int r = 0; r < kRows; ++r) { A = mul(A, f[r]); B = fma(f[r], B, mul(keep[r], rows.get(1, r))); }
 #pragma unroll
-        for (int e = 0; e < CH; ++e) { A[e] *= f[r][e]; B[e] = fmaf(f[r][e], B[e], keep[r][e] * rows.v[1][r].get(e)); }
-#pragma unroll
-      for (int r = kRows - 1; r >= 0; --r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e) E[e] = f[r][e] * (rows.v[2][r].get(e) + E[e]);
+      for (int r = kRows - 1; r >= 0; --r) E = mul(f[r], add(rows.get(2, r), E));
     } else {
+      load_h0<CH, kRows>(a, m, c, hp);         // for now: h0 where a sequence starts
 #pragma unroll
-      for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e) hp[r][e] = 0.f;         // for now: h0 where a sequence starts
-      if (a.h0 && m.from_h0) load_h0<CH, kRows>(a, m, c, hp);
-#pragma unroll
-      for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-          A[e] *= f[r][e];
-          const float kx = r < m.n ? keep[r][e] * rows.v[1][r].get(e) : 0.f;
-          B[e] = fmaf(f[r][e], (m.fresh >> r & 1) ? hp[r][e] : B[e], kx);
-        }
-#pragma unroll
-      for (int r = kRows - 1; r >= 0; --r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-          const float g = f[r][e] * (rows.v[2][r].get(e) + E[e]);
-          E[e] = r >= m.n || (m.fresh >> r & 1) ? 0.f : g;
-        }
-    }
-    sh.ab[warp][lane] = make_float4(A[0], A[1], B[0], B[1]);
-    back.ab[warp][lane] = make_float4(A[0], A[1], E[0], E[1]);
-    if (lane == 0) sh.fresh[warp] = back.fresh[warp] = m.fresh;
-    if (threadIdx.x == 0) sh.ticket = next_ticket(a, ticket);
-    __syncthreads();
-    ticket = sh.ticket;
-    if (warp == kWarps - 1) {
-      float2 in = make_float2(0.f, 0.f);
-      if (a.pair) {
-        bool closed;
-        const float4 ab = fold_tile(back, lane, -1, &closed);
-        publish_pair(a, tile, group, lane, ab, closed, a.tiles - 1);
-        in = look_back(a, tile, group, lane, 1, a.tiles - 1);
-        if (!closed && tile != a.tiles - 1) publish_end(a, tile, group, lane, ab, in);
+      for (int r = 0; r < kRows; ++r) {
+        A = mul(A, f[r]);
+        B = fma(f[r], (m.fresh >> r & 1) ? hp[r] : B, r < m.n ? mul(keep[r], rows.get(1, r)) : splat<CH>(0.f));
       }
-      back.in[lane] = in;
+#pragma unroll
+      for (int r = kRows - 1; r >= 0; --r) {
+        if (r < m.n) E = mul(f[r], add(rows.get(2, r), E));
+        if (m.fresh >> r & 1) E = splat<CH>(0.f);
+      }
+    }
+    sh.ab[0][warp][lane] = make_float4(A.v[0], A.v[CH - 1], B.v[0], B.v[CH - 1]);
+    sh.ab[1][warp][lane] = make_float4(A.v[0], A.v[CH - 1], E.v[0], E.v[CH - 1]);
+    if (lane == 0) sh.fresh[0][warp] = m.fresh;
+    if (threadIdx.x == 0) sh.ticket[0] = a.pair ? take_tickets(a, 1) : ticket + gridDim.x;
+    __syncthreads();
+    ticket = sh.ticket[0];
+    bool closed = false;
+    float4 ab;
+    if (a.pair) {
+      if (warp == W - 1) {
+        ab = fold_tile<W>(sh.ab[1], sh.fresh[0], lane, -1, &closed);
+        publish_pair(a, order, group, lane, ab, closed);
+        if (closed) publish_start(a, order, group, lane, make_float2(ab.z, ab.w));
+      }
+      fold_run(a, sh, order, group, warp, lane);
     }
     {
-      const float2 in = through(sh, lane, 0, warp, 1, make_float2(carry[0], carry[1]));
-      float h[2] = {in.x, in.y};
+      const float2 in = through(sh.ab[0], sh.fresh[0], lane, 0, warp, 1, make_float2(carry[0], carry[1]));
+      Vec<CH> h;
+      h.v[0] = in.x;
+      h.v[CH - 1] = CH == 2 ? in.y : in.x;
 #pragma unroll
-      for (int r = 0; r < kRows; ++r)
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-          if (!plain && (m.fresh >> r & 1)) h[e] = hp[r][e];
-          hp[r][e] = h[e];
-          h[e] = fmaf(f[r][e], h[e], keep[r][e] * rows.v[1][r].get(e));
-        }
+      for (int r = 0; r < kRows; ++r) {
+        if (!plain && (m.fresh >> r & 1)) h = hp[r];
+        hp[r] = h;
+        h = fma(f[r], h, mul(keep[r], rows.get(1, r)));
+      }
     }
-    __syncthreads();
-    const float2 in = through(back, lane, kWarps - 1, warp, -1, back.in[lane]);
-    float d[2] = {in.x, in.y};
+    float2 front = make_float2(0.f, 0.f);
+    if (a.pair) {
+      __syncthreads();
+      front = state_in_front(a, sh, order, group, lane);
+      if (warp == W - 1 && !closed) publish_start(a, order, group, lane, make_float2(fmaf(ab.x, front.x, ab.z), fmaf(ab.y, front.y, ab.w)));
+    }
+    const float2 in = through(sh.ab[1], sh.fresh[0], lane, W - 1, warp, -1, front);
+    Vec<CH> d;
+    d.v[0] = in.x;
+    d.v[CH - 1] = CH == 2 ? in.y : in.x;
+    const Vec<CH> minus = splat<CH>(-1.f);
     if (plain && plain_out) {
       const size_t step = (size_t)a.cols * 4, at_last = ((size_t)(row0 + kRows - 1) * a.cols + c) * 4;
       char *px = reinterpret_cast<char*>(a.dx) + at_last, *pg = reinterpret_cast<char*>(a.dgate) + at_last;
 #pragma unroll
       for (int r = kRows - 1; r >= 0; --r, px -= step, pg -= step) {
-        float dx[2], dz[2];
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-          d[e] += rows.v[2][r].get(e);
-          dx[e] = d[e] * keep[r][e];
-          d[e] *= f[r][e];
-          dz[e] = dx[e] * f[r][e] * (hp[r][e] - rows.v[1][r].get(e));
-        }
-        if (mine) { store_cell<DRAGON_F32, CH>(px, DRAGON_F32, dx); store_cell<DRAGON_F32, CH>(pg, DRAGON_F32, dz); }
+        d = add(d, rows.get(2, r));
+        const Vec<CH> dx = mul(d, keep[r]), dz = mul(mul(dx, f[r]), fma(rows.get(1, r), minus, hp[r]));
+        d = mul(d, f[r]);
+        if (mine) { store_cell<DRAGON_F32, CH>(px, DRAGON_F32, dx.v); store_cell<DRAGON_F32, CH>(pg, DRAGON_F32, dz.v); }
       }
     } else {
 #pragma unroll
       for (int r = kRows - 1; r >= 0; --r) {
         if (r >= m.n) continue;
-        float dx[2], dz[2];
-#pragma unroll
-        for (int e = 0; e < CH; ++e) {
-          d[e] += rows.v[2][r].get(e);
-          dx[e] = d[e] * keep[r][e];
-          d[e] *= f[r][e];
-          dz[e] = dx[e] * f[r][e] * (hp[r][e] - rows.v[1][r].get(e));
-        }
+        d = add(d, rows.get(2, r));
+        const Vec<CH> dx = mul(d, keep[r]), dz = mul(mul(dx, f[r]), fma(rows.get(1, r), minus, hp[r]));
+        d = mul(d, f[r]);
         if (mine) {
           const size_t i = (size_t)(row0 + r) * a.cols + c;
-          if (a.dx) store_cell<-1, CH>(reinterpret_cast<char*>(a.dx) + i * element_bytes<-1>(a.dxdt), a.dxdt, dx);
-          if (a.dgate) store_cell<-1, CH>(reinterpret_cast<char*>(a.dgate) + i * element_bytes<-1>(a.dgdt), a.dgdt, dz);
+          if (a.dx) store_cell<-1, CH>(reinterpret_cast<char*>(a.dx) + i * element_bytes<-1>(a.dxdt), a.dxdt, dx.v);
+          if (a.dgate) store_cell<-1, CH>(reinterpret_cast<char*>(a.dgate) + i * element_bytes<-1>(a.dgdt), a.dgdt, dz.v);
         }
         if (m.fresh >> r & 1) {
           if (a.dh0) {
             const int row = row0 + r, seq = row / a.length;
             if (row - seq * a.length == 0) {         // a sequence's first row: what reaches its initial state (nothing past a reset)
-              const bool reaches = m.from_h0 >> r & 1;
-              float g[2] = {reaches ? d[0] : 0.f, reaches ? d[1] : 0.f};
-              if (mine) store_cell<-1, CH>(reinterpret_cast<char*>(a.dh0) + ((size_t)seq * a.cols + c) * element_bytes<-1>(a.dh0dt), a.dh0dt, g);
+              const Vec<CH> g = (m.from_h0 >> r & 1) ? d : splat<CH>(0.f);
+              if (mine) store_cell<-1, CH>(reinterpret_cast<char*>(a.dh0) + ((size_t)seq * a.cols + c) * element_bytes<-1>(a.dh0dt), a.dh0dt, g.v);
             }
           }
-          d[0] = d[1] = 0.f;
+          d = splat<CH>(0.f);
         }
       }
     }
@@ -577,13 +628,13 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
 
 int columns_per_lane(int64_t cols) { return cols % 2 == 0 ? 2 : 1; }    // pairs of columns are aligned in every row
 
-struct Scratch { size_t pair, end, bytes; };
+struct Scratch { size_t pair, start, bytes; };
 Scratch scratch_layout(int64_t rows, int64_t cols) {
-  const int64_t slots = (rows + kScanTileRows - 1) / kScanTileRows * ((cols + 32 * columns_per_lane(cols) - 1) / (32 * columns_per_lane(cols)));
+  const int64_t tiles = (rows + kScanTileRows - 1) / kScanTileRows, per_group = 32 * columns_per_lane(cols), groups = (cols + per_group - 1) / per_group;
   Scratch s;
   s.pair = 256;            // the counter stands in front
-  s.end = s.pair + (size_t)slots * 32 * sizeof(uint4);
-  s.bytes = s.end + (size_t)slots * 32 * sizeof(uint2);
+  s.start = s.pair + (size_t)(tiles * groups) * 32 * sizeof(uint4);
+  s.bytes = s.start + (size_t)((tiles / kRun + 1) * groups) * 32 * sizeof(uint2);
   return s;
 }
 
@@ -617,28 +668,29 @@ cudaError_t scan_args(const StepRun& r, bool backward, ScanArgs* out) {
   char* p = r.ws + r.s.scratch_off;
   a.counter = reinterpret_cast<unsigned*>(p);
   a.pair = reinterpret_cast<uint4*>(p + s.pair);
-  a.end = reinterpret_cast<uint2*>(p + s.end);
+  a.start = reinterpret_cast<uint2*>(p + s.start);
   return cudaMemsetAsync(p, 0xff, s.bytes, reinterpret_cast<cudaStream_t>(r.stream));
 }
 
-template <int DT>
-void launch_fwd(const ScanArgs& a, int sm_count, cudaStream_t st) {
+template <int DT> cudaError_t launch_fwd(const ScanArgs& a, int sm_count, cudaStream_t st) {
+  const bool two = columns_per_lane(a.cols) == 2;
   if (a.length == 1 && !a.carry) {
-    const int per = columns_per_lane(a.cols);
+    const int per = two ? 2 : 1;
     const dim3 grid((a.cols + 256 * per - 1) / (256 * per), std::min(a.rows, 32768));
-    if (per == 2) scan_step_kernel<DT, 2><<<grid, 256, 0, st>>>(a);
+    if (two) scan_step_kernel<DT, 2><<<grid, 256, 0, st>>>(a);
     else scan_step_kernel<DT, 1><<<grid, 256, 0, st>>>(a);
-    return;
+    return cudaGetLastError();
   }
   const unsigned grid = std::min((unsigned)a.tiles * a.groups, (unsigned)(sm_count * kFwdCtas));
-  if (columns_per_lane(a.cols) == 2) scan_kernel<DT, 2><<<grid, kFwdWarps * 32, 0, st>>>(a);
+  if (two) scan_kernel<DT, 2><<<grid, kFwdWarps * 32, 0, st>>>(a);
   else scan_kernel<DT, 1><<<grid, kFwdWarps * 32, 0, st>>>(a);
+  return cudaGetLastError();
 }
-template <int DT>
-void launch_bwd(const ScanArgs& a, int sm_count, cudaStream_t st) {
+template <int DT> cudaError_t launch_bwd(const ScanArgs& a, int sm_count, cudaStream_t st) {
   const unsigned grid = std::min((unsigned)a.tiles * a.groups, (unsigned)(sm_count * kBwdCtas));
   if (columns_per_lane(a.cols) == 2) scan_bwd_kernel<DT, 2><<<grid, kBwdWarps * 32, 0, st>>>(a);
   else scan_bwd_kernel<DT, 1><<<grid, kBwdWarps * 32, 0, st>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -651,10 +703,7 @@ cudaError_t launch_scan(const StepRun& r) {
   const cudaError_t e = scan_args(r, false, &a);
   if (e != cudaSuccess) return e;
   const bool same = a.gdt == a.xdt && (!a.h || a.hdt == a.gdt);
-  if (!same) launch_fwd<-1>(a, r.sm_count, st);
-  else if (a.gdt == DRAGON_F32) launch_fwd<DRAGON_F32>(a, r.sm_count, st);
-  else launch_fwd<DRAGON_BF16>(a, r.sm_count, st);
-  return cudaGetLastError();
+  return !same ? launch_fwd<-1>(a, r.sm_count, st) : a.gdt == DRAGON_F32 ? launch_fwd<DRAGON_F32>(a, r.sm_count, st) : launch_fwd<DRAGON_BF16>(a, r.sm_count, st);
 }
 
 cudaError_t launch_scan_bwd(const StepRun& r) {
@@ -663,10 +712,7 @@ cudaError_t launch_scan_bwd(const StepRun& r) {
   const cudaError_t e = scan_args(r, true, &a);
   if (e != cudaSuccess) return e;
   const bool same = a.gdt == a.xdt && a.dhdt == a.gdt;
-  if (!same) launch_bwd<-1>(a, r.sm_count, st);
-  else if (a.gdt == DRAGON_F32) launch_bwd<DRAGON_F32>(a, r.sm_count, st);
-  else launch_bwd<DRAGON_BF16>(a, r.sm_count, st);
-  return cudaGetLastError();
+  return !same ? launch_bwd<-1>(a, r.sm_count, st) : a.gdt == DRAGON_F32 ? launch_bwd<DRAGON_F32>(a, r.sm_count, st) : launch_bwd<DRAGON_BF16>(a, r.sm_count, st);
 }
 
 }  // namespace dragon

@@ -315,6 +315,17 @@ def test_scan_and_gradient(seqs, length, cols, types, reset):
     assert np.array_equal(dx_alone, got[ids["dx"]])
 
 
+@pytest.mark.parametrize("seqs,length,cols,dtype", [(1, 20000, 64, "bf16"), (1, 9000, 33, "f32"), (3, 5000, 200, "f32")])
+def test_scan_gives_the_same_bits_every_time(seqs, length, cols, dtype):
+    """Tiles of a long sequence hand their states on while they run in any order; what is added to what does not depend on it."""
+    g, ids, inputs, outputs = scan_graph(seqs, length, cols, dtype, dtype, "f32", "f32", False, True, dtype)
+    feeds = normals(g.desc, inputs, 6, {"gate": 2.0})
+    first, f = run_gpu(g.desc, inputs, outputs, feeds)
+    for _ in range(10):
+        again, _ = run_gpu(g.desc, inputs, outputs, feeds, f)
+        assert all(np.array_equal(a, b) for a, b in zip(first, again))
+
+
 def test_scan_extreme_gates():
     g, ids, inputs, outputs = scan_graph(1, 300, 8, "f32", "f32", "f32", "f32", grad=True)
     feeds = normals(g.desc, inputs, 3)
