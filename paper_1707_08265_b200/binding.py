@@ -103,11 +103,17 @@ def _ids(seq):
     return arr
 
 
+_raw_stream = None
+
+
 def _current_stream():
     """Handle of torch's current stream, without the Stream object around it where torch offers that (3 us a call)."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        _raw_stream = (lambda: raw(device())) if raw and device else (lambda: torch.cuda.current_stream().cuda_stream)
+    return _raw_stream()
 
 
 class Graph:

@@ -346,8 +346,22 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int n0 = blockIdx.x * 128, m0 = blockIdx.y * NT, part = blockIdx.z;
   const int b0 = (int)((long long)g.kb * part / g.split), b1 = (int)((long long)g.kb * (part + 1) / g.split);
+  int issued = 0, first_issued = 0;
+  auto copy_block = [&](int b) {
+    const uint32_t bar = s.full + 8 * (issued % kSt), dst = tiles + (uint32_t)(issued % kSt) * kSB;
+    mbar_expect_tx(bar, kSB);
+    tma_load_2d(dst, &tmap_w, b * kBlockK, n0, bar);
+    tma_load_2d(dst + 128 * kBlockK, &tmap_x, b * kBlockK, m0, bar);
+  };
   if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_w) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_x) : "memory");
     sync_init(s, kSt, kWarps);
+    // the first copies go out at once: the stages are free, and nobody else touches their barriers before the one below
+    for (; issued < kSt && b0 + issued < b1; ++issued) {
+      if (g.drop_first_load && issued == 0) { first_issued = 1; continue; }
+      copy_block(b0 + issued);
+    }
     if (g.status_clear && blockIdx.x == 0 && blockIdx.y == 0 && part == 0) *g.status_clear = 0;
   }
   if (warp == 1) {
@@ -358,7 +372,6 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
   __syncthreads();
   fence_after();
   const uint32_t tmem = *s.tmem_slot;
-  int issued = 0, first_issued = 0;
   Pair acc[kCols / 2];         // epilogue: row n0 + its TMEM lane of W, kCols rows of X from c0 on
 #pragma unroll
   for (int j = 0; j < kCols / 2; ++j) acc[j] = 0;
@@ -366,14 +379,9 @@ gemm_e4m3_few_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
   const int c0 = ((warp - 2) >> 2) * kCols, tid = (warp - 2) * 32 + lane;
   if (warp == 0) {
     if (lane == 0) {
-      for (int b = b0; b < b1; ++b, ++issued) {
-        const int st = issued % kSt;
-        if (!wait_or_abort(s, g, s.empty + 8 * st, ((issued / kSt) & 1) ^ 1)) break;
-        if (g.drop_first_load && issued == 0) { first_issued = 1; continue; }
-        const uint32_t dst = tiles + (uint32_t)st * kSB;
-        mbar_expect_tx(s.full + 8 * st, kSB);
-        tma_load_2d(dst, &tmap_w, b * kBlockK, n0, s.full + 8 * st);
-        tma_load_2d(dst + 128 * kBlockK, &tmap_x, b * kBlockK, m0, s.full + 8 * st);
+      for (; b0 + issued < b1; ++issued) {
+        if (!wait_or_abort(s, g, s.empty + 8 * (issued % kSt), ((issued / kSt) & 1) ^ 1)) break;
+        copy_block(b0 + issued);
       }
     }
   } else if (warp == 1) {
