@@ -31,6 +31,7 @@ cudaError_t launch_quant(const StepRun& r);
 cudaError_t launch_global_norm(const StepRun& r);
 cudaError_t launch_clip_factor(const StepRun& r);
 cudaError_t launch_clip(const StepRun& r);
+cudaError_t launch_norm_and_clip(const StepRun& r);
 cudaError_t launch_scan(const StepRun& r);
 cudaError_t launch_scan_bwd(const StepRun& r);
 int launch_gemm_e4m3(const StepRun& r);   // a DRAGON_* code, message set
@@ -382,6 +383,18 @@ int dragon_function_can_alias(const dragon_function_t* f, int input, int output)
   if (!f || input < 0 || input >= f->n_in || output < 0 || output >= f->n_out) { set_error("dragon_function_can_alias: bad argument"); return DRAGON_ERR_INVALID_ARG; }
   const Plan& P = f->plan;
   if (!f->not_executable.empty()) return 0;
+  if (P.steps.size() == 1 && P.steps[0].kind == ST_NORM_CLIP) {
+    // every tensor is in registers before the first element is written
+    const Step& cs = P.steps[0];
+    int reads = 0, pairs = 0;
+    for (size_t k = 0; k < cs.rd.size(); ++k) {
+      const MemRef &mi = P.mems[cs.rd[k]], &mo = P.mems[cs.wr[gn::CLIPPED + k]];
+      if (mi.where != MEM_FEED || mi.index != input) continue;
+      ++reads;
+      pairs += mo.where == MEM_FETCH && mo.index == output && mo.dtype == mi.dtype;
+    }
+    return reads == 1 && pairs == 1 ? 1 : 0;
+  }
   if (!P.steps.empty() && P.steps.back().kind == ST_CLIP) {
     // the sums read every tensor in launches of their own; the clipping launch then reads and writes element by element
     for (size_t k = 0; k + 1 < P.steps.size(); ++k)
@@ -677,6 +690,7 @@ int dragon_run(dragon_function_t* f, const void* const* feeds, void* const* fetc
           case ST_GNORM: e = launch_global_norm(r); break;
           case ST_FACTOR: e = launch_clip_factor(r); break;
           case ST_CLIP: e = launch_clip(r); break;
+          case ST_NORM_CLIP: e = launch_norm_and_clip(r); break;
           case ST_SCAN: e = launch_scan(r); break;
           case ST_SCAN_BWD: e = launch_scan_bwd(r); break;
           default: {

@@ -1,6 +1,7 @@
 // The 2-norm over many tensors, and every tensor times min(1, limit / norm).
 //   norm = sqrt(sum_i sum_e t_i[e]^2),  c_i = t_i * (norm > limit ? limit / norm : 1)
-// Bound: bytes (every tensor read for the norm, then read and written).  All tensors are one list of chunks that
+// Bound: bytes (every tensor read for the norm, then read and written; read once where all of them fit the registers of the
+// GPU, 19 MB).  All tensors are one list of chunks that
 // persistent CTAs walk, so that a launch takes any mix of sizes; the addresses travel in the launch's parameters.
 // Squares are added in fp32 over the 16 or 32 elements a thread holds at a time and in fp64 beyond; elements whose squares
 // could leave fp32's range are squared in fp64.  The order of the sums is fixed, so the norm is the same in every run.
@@ -17,14 +18,16 @@ constexpr int kChunkBytes = 4 * 16 * kThreads;     // four accesses of 16 bytes 
 constexpr int kCtasPerSm = 4;
 __host__ __device__ constexpr int chunk_elements(bool f32) { return kChunkBytes / (f32 ? 4 : 2); }
 
-struct TensorList {
-  const void* src[kTensorsPerLaunch];
-  void* dst[kTensorsPerLaunch];
-  long long n[kTensorsPerLaunch];
-  int first[kTensorsPerLaunch + 1];                // first chunk of each tensor
-  unsigned char dtype[kTensorsPerLaunch];
+// the tensors of a launch, in its parameters; a short form for few tensors (parameters are copied at every launch)
+template <int kMost> struct TensorListOf {
+  const void* src[kMost];
+  void* dst[kMost];
+  long long n[kMost];
+  int first[kMost + 1];                            // first chunk of each tensor
+  unsigned char dtype[kMost];
   int count;
 };
+constexpr int kFewTensors = 24;
 
 struct NormOut {
   double* part;                                    // one partial sum per CTA of every launch
@@ -41,7 +44,7 @@ struct NormOut {
 // the norm and downwards by the clipping: what the norm read last is what L2 still holds.
 struct Walk {
   int c, end, k, dir;
-  __device__ __forceinline__ Walk(const TensorList& t, int dir_) : dir(dir_) {
+  template <typename TensorList> __device__ __forceinline__ Walk(const TensorList& t, int dir_) : dir(dir_) {
     const long long n = t.first[t.count];
     const int c0 = (int)(n * blockIdx.x / gridDim.x), c1 = (int)(n * (blockIdx.x + 1) / gridDim.x);
     c = dir > 0 ? c0 : c1 - 1;
@@ -54,8 +57,8 @@ struct Walk {
     k = lo;
   }
   __device__ __forceinline__ bool more() const { return c != end; }
-  __device__ __forceinline__ long long element(const TensorList& t) const { return (long long)(c - t.first[k]) * chunk_elements((t.dtype[k] & 15) == DRAGON_F32); }
-  __device__ __forceinline__ void next(const TensorList& t) {
+  template <typename TensorList> __device__ __forceinline__ long long element(const TensorList& t) const { return (long long)(c - t.first[k]) * chunk_elements((t.dtype[k] & 15) == DRAGON_F32); }
+  template <typename TensorList> __device__ __forceinline__ void next(const TensorList& t) {
     c += dir;
     if (!more()) return;
     while (dir > 0 ? t.first[k + 1] <= c : t.first[k] > c) k += dir;
@@ -140,7 +143,7 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
   return r;
 }
 
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) global_norm_kernel(const __grid_constant__ TensorList t, const NormOut o) {
+template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtasPerSm) global_norm_kernel(const __grid_constant__ TensorList t, const NormOut o) {
   __shared__ double sh[kThreads / 32];
   __shared__ bool last;
   if (o.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *o.status_clear = 0;
@@ -176,7 +179,99 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) global_norm_kernel(const
   }
 }
 
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) clip_kernel(const __grid_constant__ TensorList t, const float* norm, float limit, int* status_clear) {
+// a chunk times f, in the type of its destination
+__device__ __forceinline__ void store_clipped(const Chunk& now, const void* src, int sdt, void* dst, int ddt, long long first, long long n, float f) {
+  const bool f32 = sdt == DRAGON_F32;
+  if (f32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long long i = first + (j * kThreads + (int)threadIdx.x) * 4;
+      float v[4];
+      values_of(now.u[j], v);
+      if (i + 4 > n) continue;
+      if (ddt == DRAGON_F32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(dst) + i) = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+      else *reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(dst) + i) = make_uint2(bf16_pair(v[0] * f, v[1] * f), bf16_pair(v[2] * f, v[3] * f));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long long i = first + (j * kThreads + (int)threadIdx.x) * 8;
+      float v[8];
+      values_of(now.u[j], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= f;
+      if (i + 8 <= n) store_any<8>(dst, ddt, i, v);
+    }
+  }
+  long long i;
+  if (tail_element(f32, first, n, &i)) {
+    float v;
+    load_any<1>(src, sdt, i, &v);
+    v *= f;
+    store_any<1>(dst, ddt, i, &v);
+  }
+}
+
+// Norm and clipping in one launch, for tensors of which every CTA holds its whole share (kHeld chunks) in registers: read
+// once, summed, and after a grid-wide barrier scaled and written.  Launched cooperatively, so that all CTAs run; the wait is
+// bounded all the same.  Two words, zero before and after: CTAs that have left their sum, CTAs that have seen them all.
+constexpr int kHeld = 2;
+template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtasPerSm) norm_and_clip_kernel(const __grid_constant__ TensorList t, const NormOut o, int* status) {
+  __shared__ double sh[kThreads / 32];
+  if (o.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *o.status_clear = 0;
+  Chunk held[kHeld];
+  Walk w(t, 1);
+  int tensor[kHeld];
+  long long first[kHeld];
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h) {
+    tensor[h] = -1;
+    if (!w.more()) continue;
+    tensor[h] = w.k;
+    first[h] = w.element(t);
+    held[h].load<false>(t.src[w.k], (t.dtype[w.k] & 15) == DRAGON_F32, first[h], t.n[w.k]);
+    w.next(t);
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h)
+    if (tensor[h] >= 0) sum += chunk_squares(held[h], t.src[tensor[h]], (t.dtype[tensor[h]] & 15) == DRAGON_F32, first[h], t.n[tensor[h]]);
+  // the elements behind the last whole access are read again when they are written: before the barrier nobody writes
+  sum = block_sum(sum, sh);
+  if (threadIdx.x == 0) {
+    __stcg(o.part + blockIdx.x, sum);
+    __threadfence();
+    atomicAdd(o.counter, 1u);
+    const long long t0 = clock64();
+    for (;;) {
+      unsigned there;
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(there) : "l"(o.counter) : "memory");
+      if (there >= gridDim.x) break;
+      if (clock64() - t0 > 4000000000LL) { atomicExch(status, DRAGON_ERR_TIMEOUT); break; }
+    }
+    __threadfence();
+  }
+  __syncthreads();
+  double total = 0.0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) total += __ldcg(o.part + i);
+  total = block_sum(total, sh);
+  const float norm = (float)sqrt(total), f = factor_of(norm, o.limit);
+  if (threadIdx.x == 0) {
+    if (blockIdx.x == 0) {
+      *o.norm = norm;
+      if (o.factor) *o.factor = f;
+    }
+    if (atomicAdd(o.counter + 1, 1u) == gridDim.x - 1) { o.counter[0] = 0; o.counter[1] = 0; }
+  }
+#pragma unroll
+  for (int h = 0; h < kHeld; ++h) {
+    const int k = tensor[h];
+    if (k < 0 || (f == 1.f && t.src[k] == t.dst[k])) continue;
+    store_clipped(held[h], t.src[k], t.dtype[k] & 15, t.dst[k], t.dtype[k] >> 4, first[h], t.n[k], f);
+  }
+}
+
+template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtasPerSm) clip_kernel(const __grid_constant__ TensorList t, const float* norm, float limit, int* status_clear) {
   if (status_clear && blockIdx.x == 0 && threadIdx.x == 0) *status_clear = 0;
   const float f = factor_of(__ldg(norm), limit);
   Walk w(t, -1);
@@ -188,39 +283,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) clip_kernel(const __grid
   while (w.more()) {
     const Chunk now = next;
     const int k = w.k, sdt = t.dtype[k] & 15, ddt = t.dtype[k] >> 4;
-    const bool f32 = sdt == DRAGON_F32;
     const long long first = w.element(t), n = t.n[k];
     w.next(t);
     load();
     if (f == 1.f && t.src[k] == t.dst[k]) continue;      // in place and nothing to change
-    if (f32) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const long long i = first + (j * kThreads + (int)threadIdx.x) * 4;
-        float v[4];
-        values_of(now.u[j], v);
-        if (i + 4 > n) continue;
-        if (ddt == DRAGON_F32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(t.dst[k]) + i) = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-        else *reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(t.dst[k]) + i) = make_uint2(bf16_pair(v[0] * f, v[1] * f), bf16_pair(v[2] * f, v[3] * f));
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const long long i = first + (j * kThreads + (int)threadIdx.x) * 8;
-        float v[8];
-        values_of(now.u[j], v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= f;
-        if (i + 8 <= n) store_any<8>(t.dst[k], ddt, i, v);
-      }
-    }
-    long long i;
-    if (tail_element(f32, first, n, &i)) {
-      float v;
-      load_any<1>(t.src[k], sdt, i, &v);
-      v *= f;
-      store_any<1>(t.dst[k], ddt, i, &v);
-    }
+    store_clipped(now, t.src[k], sdt, t.dst[k], ddt, first, n, f);
   }
 }
 
@@ -230,7 +297,7 @@ __global__ void clip_factor_kernel(const float* norm, float limit, float* factor
 }
 
 // chunk table of tensors [k0, k1); false if a launch cannot hold it
-bool add_tensor(TensorList* t, const void* src, void* dst, int sdt, int ddt, int64_t n) {
+template <typename TensorList> bool add_tensor(TensorList* t, const void* src, void* dst, int sdt, int ddt, int64_t n) {
   const int i = t->count;
   const int per = chunk_elements(sdt == DRAGON_F32);
   const int64_t chunks = (n + per - 1) / per;
@@ -248,13 +315,24 @@ bool add_tensor(TensorList* t, const void* src, void* dst, int sdt, int ddt, int
 
 size_t global_norm_scratch_bytes(int n_tensors, int sm_count) { return (size_t)launches_of_tensors(n_tensors) * sm_count * kCtasPerSm * sizeof(double); }
 
-cudaError_t launch_global_norm(const StepRun& r) {
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
+bool norm_and_clip_fit_one_launch(const std::vector<int64_t>& numel, const std::vector<int>& dtype, int sm_count) {
+  if ((int)numel.size() > kTensorsPerLaunch) return false;
+  int64_t chunks = 0;
+  for (size_t i = 0; i < numel.size(); ++i) {
+    const int per = chunk_elements(dtype[i] == DRAGON_F32);
+    chunks += (numel[i] + per - 1) / per;
+  }
+  return chunks <= (int64_t)sm_count * kCtasPerSm * kHeld;
+}
+
+namespace {
+
+template <int kMost> cudaError_t global_norm_of(const StepRun& r, cudaStream_t st) {
   const int n = (int)r.s.rd.size(), launches = launches_of_tensors(n);
   NormOut o{reinterpret_cast<double*>(r.ws + r.s.scratch_off), 0, 0, false, reinterpret_cast<float*>(r.wr(gn::NORM)), reinterpret_cast<float*>(r.wr(gn::FACTOR)),
             (float)r.s.attr, r.counter, r.status_clear};
   for (int l = 0; l < launches; ++l) {
-    TensorList t;
+    TensorListOf<kMost> t;
     t.count = 0;
     t.first[0] = 0;
     for (int k = l * kTensorsPerLaunch; k < std::min(n, (l + 1) * kTensorsPerLaunch); ++k)
@@ -269,17 +347,11 @@ cudaError_t launch_global_norm(const StepRun& r) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_clip_factor(const StepRun& r) {
-  clip_factor_kernel<<<1, 1, 0, reinterpret_cast<cudaStream_t>(r.stream)>>>(reinterpret_cast<const float*>(r.rd(0)), (float)r.s.attr, reinterpret_cast<float*>(r.wr(0)), r.status_clear);
-  return cudaGetLastError();
-}
-
-cudaError_t launch_clip(const StepRun& r) {
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
+template <int kMost> cudaError_t clip_of(const StepRun& r, cudaStream_t st) {
   const int n = (int)r.s.wr.size();
   int* clear = r.status_clear;
   for (int k0 = 0; k0 < n; k0 += kTensorsPerLaunch) {
-    TensorList t;
+    TensorListOf<kMost> t;
     t.count = 0;
     t.first[0] = 0;
     for (int k = k0; k < std::min(n, k0 + kTensorsPerLaunch); ++k) {
@@ -291,6 +363,49 @@ cudaError_t launch_clip(const StepRun& r) {
     clear = nullptr;
   }
   return cudaGetLastError();
+}
+
+template <int kMost> cudaError_t norm_and_clip_of(const StepRun& r, cudaStream_t st) {
+  TensorListOf<kMost> t;
+  t.count = 0;
+  t.first[0] = 0;
+  for (int k = 0; k < (int)r.s.rd.size(); ++k)
+    if (!add_tensor(&t, r.rd(k), r.wr(gn::CLIPPED + k), r.rd_type(k), r.wr_type(gn::CLIPPED + k), r.mems[r.s.rd[k]].shape.numel())) return cudaErrorInvalidValue;
+  const NormOut o{reinterpret_cast<double*>(r.ws + r.s.scratch_off), 0, 0, true, reinterpret_cast<float*>(r.wr(gn::NORM)), reinterpret_cast<float*>(r.wr(gn::FACTOR)),
+                  (float)r.s.attr, r.counter, r.status_clear};
+  cudaLaunchConfig_t cfg = {};
+  // no more CTAs than hold their share: at most kHeld chunks each, and all of them on the GPU at once
+  cfg.gridDim = dim3(std::min(t.first[t.count], r.sm_count * kCtasPerSm));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, norm_and_clip_kernel<TensorListOf<kMost>>, t, o, r.status);
+}
+
+}  // namespace
+
+cudaError_t launch_global_norm(const StepRun& r) {
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
+  return r.s.rd.size() <= kFewTensors ? global_norm_of<kFewTensors>(r, st) : global_norm_of<kTensorsPerLaunch>(r, st);
+}
+
+cudaError_t launch_clip_factor(const StepRun& r) {
+  clip_factor_kernel<<<1, 1, 0, reinterpret_cast<cudaStream_t>(r.stream)>>>(reinterpret_cast<const float*>(r.rd(0)), (float)r.s.attr, reinterpret_cast<float*>(r.wr(0)), r.status_clear);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_clip(const StepRun& r) {
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
+  return r.s.wr.size() <= kFewTensors ? clip_of<kFewTensors>(r, st) : clip_of<kTensorsPerLaunch>(r, st);
+}
+
+cudaError_t launch_norm_and_clip(const StepRun& r) {
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
+  return r.s.rd.size() <= kFewTensors ? norm_and_clip_of<kFewTensors>(r, st) : norm_and_clip_of<kTensorsPerLaunch>(r, st);
 }
 
 }  // namespace dragon

@@ -1116,6 +1116,22 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     }
     plan->steps.push_back(st);
   }
+  // A norm and the clipping of exactly its tensors that fit the GPU's registers run as one launch: every tensor is read once
+  for (size_t i = 0; i + 1 < plan->steps.size(); ++i) {
+    Step &nst = plan->steps[i], &cst = plan->steps[i + 1];
+    if (nst.kind != ST_GNORM || cst.kind != ST_CLIP || nst.wr[gn::NORM] < 0 || cst.rd[cl::NORM] != nst.wr[gn::NORM]) continue;
+    if (!std::equal(nst.rd.begin(), nst.rd.end(), cst.rd.begin() + cl::FIRST, cst.rd.end()) || std::count(cst.wr.begin(), cst.wr.end(), -1)) continue;
+    if (nst.wr[gn::FACTOR] >= 0 && nst.attr != cst.attr) continue;
+    std::vector<int64_t> numel;
+    std::vector<int> dtype;
+    for (int m : nst.rd) { numel.push_back(mems[m].shape.numel()); dtype.push_back(mems[m].dtype); }
+    if (!norm_and_clip_fit_one_launch(numel, dtype, sm_count)) continue;
+    nst.kind = ST_NORM_CLIP;
+    nst.attr = cst.attr;
+    nst.wr.insert(nst.wr.end(), cst.wr.begin(), cst.wr.end());
+    plan->steps.erase(plan->steps.begin() + i + 1);
+    // (steps of VM segments name their segment, so nothing else refers to a step's position)
+  }
   for (size_t s = 0; s < seg_items.size(); ++s) {
     if (seg_items[s].empty()) continue;   // ran in a product's epilogue
     int rc = codegen_segment(items, seg_items[s], vals, mems, sm_count, &plan->segs[s]);
@@ -1147,7 +1163,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       st.n_colpart = norm_bwd_partials(sh.rows(), sh.cols(), sm_count);
       st.colpart_off = take((size_t)st.n_colpart * sh.cols() * sizeof(float));
     }
-    if (st.kind == ST_GNORM) st.scratch_off = take(global_norm_scratch_bytes((int)st.rd.size(), sm_count));
+    if (st.kind == ST_GNORM || st.kind == ST_NORM_CLIP) st.scratch_off = take(global_norm_scratch_bytes((int)st.rd.size(), sm_count));
     if (st.kind == ST_SCAN || st.kind == ST_SCAN_BWD) {
       const Shape& sh = mems[st.rd[sc::GATE]].shape;
       st.scratch_off = take(scan_scratch_bytes(sh.d[0], sh.d[1]));
@@ -1348,6 +1364,7 @@ std::string describe_plan(const Plan& p) {
                  (long long)p.mems[st.rd[g8::XQ]].shape.d[1], p.mems[st.wr[g8::Y]].dtype == DRAGON_BF16 ? "bf16" : "f32");
         break;
       case ST_GNORM: snprintf(buf, sizeof(buf), "global_norm[%d tensors%s]\n", (int)st.rd.size(), st.wr[gn::FACTOR] >= 0 ? " ->factor" : ""); break;
+      case ST_NORM_CLIP: snprintf(buf, sizeof(buf), "global_norm+clip_by_norm[%d tensors%s]\n", (int)st.rd.size(), st.wr[gn::FACTOR] >= 0 ? " ->factor" : ""); break;
       case ST_FACTOR: snprintf(buf, sizeof(buf), "clip_factor\n"); break;
       case ST_CLIP: snprintf(buf, sizeof(buf), "clip_by_norm[%d tensors]\n", (int)st.wr.size()); break;
       case ST_SCAN: case ST_SCAN_BWD:

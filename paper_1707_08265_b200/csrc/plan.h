@@ -80,7 +80,7 @@ namespace nm { enum { X, R, GAIN }; enum { H, Y, S, Q }; }                      
 namespace nb { enum { H, DY, GAIN, SKIP }; enum { DH, DGAIN }; }                  // IT_NORM_BWD: dh = skip + the norm's gradient
 namespace qt { enum { X, SIN }; enum { S, Q }; }                                  // IT_QUANT: scales of x, and x in them (or in given ones)
 namespace g8 { enum { XQ, SX, WQ, SW }; enum { Y }; }                             // IT_GEMM8
-namespace gn { enum { NORM, FACTOR }; }                                           // IT_GNORM: rd = the tensors; factor = min(1, attr / norm)
+namespace gn { enum { NORM, FACTOR, CLIPPED }; }                                  // IT_GNORM: rd = the tensors; factor = min(1, attr / norm)
 namespace cl { enum { NORM, FIRST }; }                                            // IT_CLIP: rd = norm, tensors; wr = the clipped tensors
 namespace sc { enum { GATE, X, H0, RESET, DH, CARRY_IN }; enum { H, CARRY }; enum { DGATE, DX, DH0 }; }   // IT_SCAN, IT_SCAN_BWD
 struct Item {
@@ -135,7 +135,8 @@ struct VmSegment {
 };
 
 enum StepKind { ST_VM, ST_GEMM, ST_TRANSPOSE, ST_SCE_FWD, ST_SCE_BWD, ST_COPY,
-                ST_NORM, ST_NORM_BWD, ST_QUANT, ST_GEMM8, ST_GNORM, ST_FACTOR, ST_CLIP, ST_SCAN, ST_SCAN_BWD };
+                ST_NORM, ST_NORM_BWD, ST_QUANT, ST_GEMM8, ST_GNORM, ST_FACTOR, ST_CLIP, ST_SCAN, ST_SCAN_BWD,
+                ST_NORM_CLIP };   // (GNORM and the CLIP of all its tensors in one launch: rd = tensors, wr = norm, factor, clipped tensors)
 struct Step {
   int kind;
   int seg = -1;                          // ST_VM
@@ -158,6 +159,7 @@ constexpr int64_t kMaxRowLength = 1 << 26, kMaxProductExtent = 1 << 26;   // wha
 constexpr int kScanTileRows = 64;       // rows of one tile of GatedScan; the gradient reads the state in front of each
 int norm_bwd_partials(int64_t rows, int64_t cols, int sm_count);   // rows of partial gain gradients that the norm's gradient leaves
 size_t global_norm_scratch_bytes(int n_tensors, int sm_count);
+bool norm_and_clip_fit_one_launch(const std::vector<int64_t>& numel, const std::vector<int>& dtype, int sm_count);
 size_t scan_scratch_bytes(int64_t rows, int64_t cols);
 constexpr int kTensorsPerLaunch = 256;   // tensors that one launch of GlobalNorm or ClipByNorm takes in its parameters
 inline int launches_of_tensors(int n) { return (n + kTensorsPerLaunch - 1) / kTensorsPerLaunch; }

@@ -180,7 +180,14 @@ def test_clipped_tensors_share_a_launch_and_an_updater_takes_the_factor():
     c = [g.op("ClipByNorm", [a, n], "c%d" % i, attrs=[1.0], out_shape=[i + 1, 3]) for i, a in enumerate(t)]
     w2 = g.op("Sub", [w, c[0]], "w2", [1, 3])
     lines = B.Graph.from_desc(g.desc).function(t, [n] + c).describe().splitlines()
-    assert lines == ["global_norm[5 tensors]", "clip_by_norm[5 tensors]"]
+    assert lines == ["global_norm+clip_by_norm[5 tensors]"]              # small: one launch that reads every tensor once
+    big = wl.GraphDesc()
+    t2 = [big.tensor("a", [4096, 1024]), big.tensor("b", [4096, 1024], "bf16")]
+    n2 = big.op("GlobalNorm", t2, "n", [])
+    c2 = [big.op("ClipByNorm", [x, n2], "c%d" % i, [4096, 1024], attrs=[1.0]) for i, x in enumerate(t2)]
+    f = B.Graph.from_desc(big.desc)
+    assert f.function(t2, [n2] + c2).describe().splitlines() == ["global_norm[2 tensors]", "clip_by_norm[2 tensors]"]
+    assert f.function(t2, [n2] + c2[:1]).describe().splitlines() == ["global_norm[2 tensors]", "clip_by_norm[1 tensors]"]
     lines = B.Graph.from_desc(g.desc).function(t + [w], [w2]).describe().splitlines()
     assert lines[0] == "global_norm[5 tensors ->factor]" and lines[1].startswith("vm[flat") and len([s for s in lines if s[0] != " "]) == 2
 
