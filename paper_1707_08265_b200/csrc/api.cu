@@ -610,7 +610,10 @@ int dragon_run(dragon_function_t* f, const void* const* feeds, void* const* fetc
   cudaError_t e = cudaSuccess;
   if (!f->status_ready) {
     e = cudaMemsetAsync(word0, 0, 256, st);
-    f->status_ready = true;
+    // a run that is only captured into a graph has not cleared anything yet: the next run, captured or not, clears again
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &capturing) != cudaSuccess) cudaGetLastError();
+    f->status_ready = capturing == cudaStreamCaptureStatusNone;
     f->run_parity = 0;
   }
   int* const status = word0 + 16 * f->run_parity;

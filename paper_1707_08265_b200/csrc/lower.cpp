@@ -345,11 +345,17 @@ struct Lowerer {
   // whether the gradient of tensor t reaches a derivative target unchanged (through additions): it is then kept in f32
   bool reaches_target(int s, int t) const {
     const auto& wr = g.stages[s].wrts;
-    if (std::find(wr.begin(), wr.end(), t) != wr.end()) return true;
-    const int p = g.tensors[t].producer;
-    if (p < 0 || (g.ops[p].type != DRAGON_OP_ADD && g.ops[p].type != DRAGON_OP_SUB && g.ops[p].type != DRAGON_OP_BIAS_ADD)) return false;
-    for (int i : g.ops[p].in)
-      if (pr.in_G[s][i] && reaches_target(s, i)) return true;
+    std::set<int> seen = {t};
+    std::vector<int> todo = {t};
+    while (!todo.empty()) {
+      const int x = todo.back();
+      todo.pop_back();
+      if (std::find(wr.begin(), wr.end(), x) != wr.end()) return true;
+      const int p = g.tensors[x].producer;
+      if (p < 0 || (g.ops[p].type != DRAGON_OP_ADD && g.ops[p].type != DRAGON_OP_SUB && g.ops[p].type != DRAGON_OP_BIAS_ADD)) continue;
+      for (int i : g.ops[p].in)
+        if (pr.in_G[s][i] && seen.insert(i).second) todo.push_back(i);
+    }
     return false;
   }
   int grad_mem(int s, int t) {   // memory of the gradient with respect to t, as an operator's kernel writes it

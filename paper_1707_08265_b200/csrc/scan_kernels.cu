@@ -17,6 +17,7 @@
 // A row that starts afresh cuts the chain by selection, not by a factor of 0: what is in front of it cannot reach it, NaN
 // or not.  The state is fp32; the gradient recomputes it from the state in front of each tile, which the forward keeps.
 #include <algorithm>
+#include <cstdlib>
 
 #include "device_util.h"
 #include "plan.h"
@@ -47,6 +48,8 @@ struct ScanArgs {
   uint4* pair;             // exchange area: per tile (in the chain's order) and group 32 lanes' pairs (A, A', B, B'), null if no tile needs another
   uint2* start;            // ... and per run and group the state in front of it
   int *status, *status_clear;
+  long long wait_budget;   // clock cycles
+  int withhold;            // failure-detection test: the chain's first tile publishes nothing
 };
 
 // CH neighbouring columns as they are in memory; DT -1: a type known at run time
@@ -180,6 +183,7 @@ __device__ __forceinline__ float computed(float v) { return __fadd_rn(v, 0.f); }
 // `order`: a tile's place in the chain (its number, or counted from the end for the gradient)
 __device__ __forceinline__ size_t slot_of(const ScanArgs& a, int order, int group, int lane) { return ((size_t)order * a.groups + group) * 32 + lane; }
 __device__ __forceinline__ void publish_pair(const ScanArgs& a, int order, int group, int lane, float4 ab, bool closed) {
+  if (a.withhold && order == 0) return;
   const float none = __uint_as_float(kClosed);
   put(a.pair + slot_of(a, order, group, lane), make_float4(closed ? none : computed(ab.x), closed ? none : computed(ab.y), computed(ab.z), computed(ab.w)));
 }
@@ -188,7 +192,7 @@ __device__ __forceinline__ void publish_start(const ScanArgs& a, int order, int 
   if (order % kRun == kRun - 1) put(a.start + slot_of(a, order / kRun + 1, group, lane), make_float2(computed(v.x), computed(v.y)));
 }
 __device__ __forceinline__ bool out_of_time(const ScanArgs& a, long long t0) {
-  if (clock64() - t0 <= kWaitBudgetCycles) return false;
+  if (clock64() - t0 <= a.wait_budget) return false;
   atomicExch(a.status, DRAGON_ERR_TIMEOUT);
   return true;
 }
@@ -651,6 +655,10 @@ cudaError_t scan_args(const StepRun& r, bool backward, ScanArgs* out) {
   const int per_group = 32 * columns_per_lane(a.cols);
   a.groups = (a.cols + per_group - 1) / per_group;
   a.status = r.status;
+  a.wait_budget = kWaitBudgetCycles;
+  // failure-detection test only: a short budget and a first tile that publishes nothing
+  if (const char* e = std::getenv("DRAGON_SCAN_WAIT_BUDGET")) { const long long b = std::atoll(e); if (b > 0) a.wait_budget = std::min(b, kWaitBudgetCycles); }
+  if (const char* e = std::getenv("DRAGON_SCAN_WITHHOLD")) a.withhold = e[0] == '1';
   a.status_clear = r.status_clear;
   if (backward) {
     a.dh = r.rd(sc::DH); a.dhdt = r.rd_type(sc::DH);

@@ -366,3 +366,188 @@ def test_scan_reset_stops_non_finite_states():
     assert np.isfinite(dx[:200, 9]).all() and np.isfinite(dx[301:, 9]).all()
     ok = ~expect_bad
     assert np.abs(h - want[ids["h"]])[ok].max() < 1e-5
+
+
+def test_scan_wait_that_runs_out_is_reported(monkeypatch):
+    """Failure detection without a fault: the chain's first tile publishes nothing, the tiles behind it give up on a short
+    budget, the kernel ends and reports DRAGON_ERR_TIMEOUT; the next run of the same function is correct."""
+    from paper_1707_08265_b200 import binding as B
+    g, ids, inputs, outputs = scan_graph(1, 1000, 64, "f32", "f32", "f32", "f32", False, True)
+    feeds = normals(g.desc, inputs, 6)
+    want, f = run_gpu(g.desc, inputs, outputs, feeds)
+    import torch
+    dev = [to_gpu(a, g.desc["tensors"][t]["dtype"]) for a, t in zip(feeds, inputs)]
+    outs = [torch.empty(g.shape(t), device="cuda") for t in outputs]
+    monkeypatch.setenv("DRAGON_SCAN_WAIT_BUDGET", "2000000")
+    monkeypatch.setenv("DRAGON_SCAN_WITHHOLD", "1")
+    f.run_torch(dev, outs)
+    assert f.status() == B.ERR_TIMEOUT
+    monkeypatch.delenv("DRAGON_SCAN_WAIT_BUDGET")
+    monkeypatch.delenv("DRAGON_SCAN_WITHHOLD")
+    again, _ = run_gpu(g.desc, inputs, outputs, feeds, f)
+    assert all(np.array_equal(a, b) for a, b in zip(want, again))
+
+
+@pytest.mark.parametrize("seqs,length", [(1, 70), (5, 1)])
+def test_scan_of_one_tensor_in_two_places(seqs, length):
+    """gate and x are the same tensor, or x and h0 (one row per sequence): the gradient sums both places."""
+    g = wl.GraphDesc()
+    rows = seqs * length
+    x, d = g.tensor("x", [rows, 6]), g.tensor("d", [rows, 6])
+    h = g.op("GatedScan", [x, x] if length > 1 else [x, x, x], "h", [rows, 6], attrs=[seqs])
+    dx, = g.grad([g.op("Mul", [h, d], "along")], [x])
+    feeds = normals(g.desc, [x, d], 3)
+    got, _ = run_gpu(g.desc, [x, d], [h, dx], feeds)
+    for o, p in zip(got, interp.run_function(g.desc, [x, d], [h, dx], feeds)):
+        assert np.abs(o - p).max() <= 1e-5 * max(1.0, np.abs(p).max())
+
+
+# ---- how functions of these operators are run --------------------------------------------------------------------
+
+def mixed_functions():
+    """One function of each kind of kernel (norm, gradient, quantisation, product of many and few rows, clipping, scan over many tiles)."""
+    out = []
+    out.append(norm_graph(70, 264, grad=True, skip="bf16"))
+    out.append(norm_graph(70, 300, eight_bit=True))
+    g, t, y, _ = product_case(40, 300, 400, "bf16", 1)
+    out.append((g, {}, t, [y]))
+    g, t, y, _ = product_case(2600, 2100, 144, "f32", 1)
+    out.append((g, {}, t, [y]))
+    g, t, n, c = clip_graph([[100, 33], [7]], ["f32", "bf16"], 0.5)
+    out.append((g, {}, t, [n] + c))
+    g, t, n, c = clip_graph([[4096, 3000], [7]], ["bf16", "f32"], 0.5)
+    out.append((g, {}, t, [n] + c))
+    out.append(scan_graph(2, 1000, 66, reset=True, grad=True))
+    return out
+
+
+def feeds_of(g, inputs, seed):
+    out = []
+    for a, t in zip(normals(g.desc, inputs, seed), inputs):
+        out.append((np.abs(a) < 0.05).astype(np.int32) if g.desc["tensors"][t]["dtype"] == "i32" else a)
+    return out
+
+
+@pytest.mark.parametrize("k", range(7))
+@pytest.mark.parametrize("eager_first", [True, False])
+def test_captured_and_replayed(k, eager_first):
+    """A run captured into a CUDA graph before or after a first eager one, two graphs of one function (one workspace), replays
+    in any order and eager runs between them, with inputs that change in place: always the bits of a plain run."""
+    import torch
+    from paper_1707_08265_b200 import binding as B
+    g, _, inputs, outputs = mixed_functions()[k]
+    f = B.Graph.from_desc(g.desc).function(inputs, outputs)
+    f.ensure_workspace()
+    f._ws.fill_(0xA5)
+    sets = [feeds_of(g, inputs, s) for s in (1, 2)]
+    plain = [run_gpu(g.desc, inputs, outputs, s)[0] for s in sets]
+    dev = [[to_gpu(a, g.desc["tensors"][t]["dtype"]) for a, t in zip(s, inputs)] for s in sets]
+    feeds = [t.clone() for t in dev[0]]
+    outs = [torch.empty(g.shape(t), dtype={"f32": torch.float32, "bf16": torch.bfloat16, "f8e4m3": torch.float8_e4m3fn}[g.desc["tensors"][t]["dtype"]], device="cuda")
+            for t in outputs]
+
+    def check(which):
+        torch.cuda.synchronize()
+        for o, p in zip(outs, plain[which]):
+            assert np.array_equal(o.double().cpu().numpy(), p)
+
+    def load(which):
+        for a, b in zip(feeds, dev[which]):
+            a.copy_(b)
+        for o in outs:
+            o.reshape(-1).view(torch.uint8).fill_(0x7F)
+
+    if eager_first:
+        f.run_torch(feeds, outs)
+        check(0)
+    graphs = []
+    for _ in range(2):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            f.run_torch(feeds, outs)
+        graphs.append(gr)
+    for which, step in ((1, graphs[1]), (0, graphs[0]), (1, None), (0, graphs[1]), (1, graphs[0]), (0, graphs[0])):
+        load(which)
+        step.replay() if step else f.run_torch(feeds, outs)
+        check(which)
+
+
+def test_two_streams_and_two_functions_at_once():
+    """Functions with workspaces of their own on streams of their own, many runs in flight."""
+    import torch
+    from paper_1707_08265_b200 import binding as B
+    jobs = []
+    for k, (g, _, inputs, outputs) in enumerate(mixed_functions()):
+        feeds = feeds_of(g, inputs, 9)
+        plain = run_gpu(g.desc, inputs, outputs, feeds)[0]
+        f = B.Graph.from_desc(g.desc).function(inputs, outputs)
+        f.ensure_workspace()
+        dev = [to_gpu(a, g.desc["tensors"][t]["dtype"]) for a, t in zip(feeds, inputs)]
+        from lm_cases import torch_type
+        outs = [torch.empty(g.shape(t), dtype=torch_type(g.desc["tensors"][t]["dtype"]), device="cuda") for t in outputs]
+        jobs.append((f, dev, outs, plain, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for f, dev, outs, _, st in jobs:
+            f.run_torch(dev, outs, st)
+    torch.cuda.synchronize()
+    for f, _, outs, plain, _ in jobs:
+        assert f.status() == 0
+        for o, p in zip(outs, plain):
+            assert np.array_equal(o.double().cpu().numpy(), p)
+
+
+@pytest.mark.parametrize("big", [False, True])
+def test_clip_over_its_own_tensors(big):
+    """dragon_function_can_alias: the clipped tensors may be the tensors; one that is below the limit stays as it is."""
+    import torch
+    from paper_1707_08265_b200 import binding as B
+    g, t, n, c = clip_graph([[4096, 2100], [4096, 300], [77]] if big else [[1000, 30], [513], [77]], ["bf16", "f32", "f32"], 2.0)
+    feeds = normals(g.desc, t, 3)
+    want = run_gpu(g.desc, t, [n] + c, feeds)[0]
+    f = B.Graph.from_desc(g.desc).function(t, [n] + c)
+    assert all(f.can_alias(i, i + 1) for i in range(3)) and not f.can_alias(0, 2)
+    dev = [to_gpu(a, g.desc["tensors"][x]["dtype"]) for a, x in zip(feeds, t)]
+    norm = torch.empty((), device="cuda")
+    f.run_torch(dev, [norm] + dev)
+    for o, p in zip([norm] + dev, want):
+        assert np.array_equal(o.double().cpu().numpy(), p)
+    clipped = [x.clone() for x in dev]
+    f.run_torch(dev, [norm] + dev)            # the norm is the limit now, up to rounding
+    assert abs(float(norm) - 2.0) < 1e-2
+    for o, p in zip(dev, clipped):
+        assert (o.float() - p.float()).abs().max() <= 2 * U16 * p.float().abs().max()
+
+
+def test_host_buffers_and_named_tensors():
+    """The same functions through dragon_run_host and through a workspace of named tensors (e4m3 among them)."""
+    import torch
+    from lm_cases import torch_type
+    from paper_1707_08265_b200 import binding as B
+    for g, _, inputs, outputs in mixed_functions():
+        feeds = feeds_of(g, inputs, 4)
+        plain, f = run_gpu(g.desc, inputs, outputs, feeds)
+        host = [to_gpu(a, g.desc["tensors"][t]["dtype"]).cpu().pin_memory() for a, t in zip(feeds, inputs)]
+        outs = [torch.empty(g.shape(t), dtype=torch_type(g.desc["tensors"][t]["dtype"])).pin_memory() for t in outputs]
+        staging = torch.empty(f.staging_bytes() + 256, dtype=torch.uint8, device="cuda")
+        base = (staging.data_ptr() + 255) & ~255
+        f.run_host([h.data_ptr() for h in host], [o.data_ptr() for o in outs], base, f.staging_bytes(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        for o, p in zip(outs, plain):
+            assert np.array_equal(o.double().numpy(), p)
+        ws = B.Workspace()
+        f2 = B.Graph.from_desc(g.desc).function(inputs, outputs)
+        for h, t in zip(host, inputs):
+            info = g.desc["tensors"][t]
+            ws.feed(info["name"], B.DTYPES[info["dtype"]], info["shape"], h.data_ptr())
+        for _ in range(2):
+            ws.run(f2)
+        torch.cuda.synchronize()
+        for t, p in zip(outputs, plain):
+            info = g.desc["tensors"][t]
+            o = torch.empty(info["shape"], dtype=torch_type(info["dtype"]))
+            ws.fetch(info["name"], o.data_ptr(), o.numel() * o.element_size())
+            torch.cuda.synchronize()
+            assert np.array_equal(o.double().numpy(), p)
+        f2.close()
+        ws.close()
