@@ -13,6 +13,11 @@ Workloads (sizes are arguments so that tests can shrink them):
                       with an unused Tanh side branch and gradients for weights and biases
   random_row_dag      random broadcast/row-reduction DAG over [R,C] and [C] tensors, with
                       gradients for every input
+  recurrent_layer     RMSNorm / InnerProduct / GatedScan / InnerProduct with a residual stream, RMSNorm, InnerProduct,
+                      SoftmaxCrossEntropy, with gradients for every weight (a language model's layer and its loss)
+  recurrent_step      the same layer one row per sequence with its weights in e4m3 (RMSNorm with 8-bit output,
+                      ScaledInnerProduct, GatedScan from fed states): a decoding step
+  clipped_updater     W' = W - lr * clipped gradient for several weights under one global norm
 """
 import numpy as np
 
@@ -234,4 +239,69 @@ def updater(shape, kind="sgd"):
     else:
         raise ValueError(kind)
     ids["W_new"] = g.op("Sub", [ids["W"], step], "W_new")
+    return g, ids
+
+
+def recurrent_layer(seqs, length, width, inner, vocab, resets=False):
+    """One layer over ``seqs`` sequences of ``length`` rows and the loss behind it:
+      y = RMSNorm(r; g1),  h = GatedScan(y Wf^T, y Wx^T; h0),  r2 = r + h Wo^T,  z = RMSNorm(r2; g2) Wv^T,  loss(z, labels)
+    r: the residual stream, bf16 [rows, width].  Returns (graph, ids); ids["grads"]: gradients of (Wf, Wx, Wo, Wv, g1, g2, h0)."""
+    g, rows = GraphDesc(), seqs * length
+    ids = {"r": g.tensor("r", [rows, width], "bf16"), "h0": g.tensor("h0", [seqs, inner])}
+    if resets:
+        ids["reset"] = g.tensor("reset", [rows], "i32")
+    for n, sh in (("Wf", [inner, width]), ("Wx", [inner, width]), ("Wo", [width, inner]), ("Wv", [vocab, width])):
+        ids[n] = g.tensor(n, sh, "bf16")
+    ids["g1"], ids["g2"] = g.tensor("gain1", [width]), g.tensor("gain2", [width])
+    ids["labels"] = g.tensor("labels", [rows], "i32")
+    y = g.op("RMSNorm", [ids["r"], ids["g1"]], "y", [rows, width], "bf16")
+    f = g.op("InnerProduct", [y, ids["Wf"]], "f", [rows, inner], "bf16")
+    x = g.op("InnerProduct", [y, ids["Wx"]], "x", [rows, inner], "bf16")
+    h = g.op("GatedScan", [f, x, ids["h0"]] + ([ids["reset"]] if resets else []), "h", [rows, inner], "bf16", attrs=[seqs])
+    o = g.op("InnerProduct", [h, ids["Wo"]], "o", [rows, width])
+    ids["r2"] = g.op("Add", [o, ids["r"]], "r2", [rows, width], "bf16")
+    y2 = g.op("RMSNorm", [ids["r2"], ids["g2"]], "y2", [rows, width], "bf16")
+    z = g.op("InnerProduct", [y2, ids["Wv"]], "z", [rows, vocab])
+    ids["loss"] = g.op("SoftmaxCrossEntropy", [z, ids["labels"]], "loss", [])
+    ids["weights"] = [ids[n] for n in ("Wf", "Wx", "Wo", "Wv", "g1", "g2", "h0")]
+    ids["grads"] = g.grad([ids["loss"]], ids["weights"])
+    return g, ids
+
+
+def recurrent_step(seqs, width, inner):
+    """One decoding step of the layer for ``seqs`` sequences, its weights in e4m3 with scales of 128 x 128 blocks:
+    r2 = r + GatedScan(y Wf^T, y Wx^T; states) Wo^T with y and the new states in e4m3 with scales of 1 x 128 blocks."""
+    g = GraphDesc()
+
+    def blocks(n):
+        return -(-n // 128)
+
+    ids = {"r": g.tensor("r", [seqs, width], "bf16"), "g1": g.tensor("gain1", [width]), "states": g.tensor("states", [seqs, inner])}
+    for n, sh in (("Wf", [inner, width]), ("Wx", [inner, width]), ("Wo", [width, inner])):
+        ids[n], ids["s" + n] = g.tensor(n, sh, "f8e4m3"), g.tensor("s" + n, [blocks(sh[0]), blocks(sh[1])])
+
+    def product(x, out):
+        s = g.op("BlockScale", [x], "s_" + out, [seqs, blocks(g.shape(x)[1])])
+        q = g.op("Quantize", [x, s], "q_" + out, g.shape(x), "f8e4m3")
+        return lambda n, o, dt: g.op("ScaledInnerProduct", [q, s, ids[n], ids["s" + n]], o, [seqs, g.shape(ids[n])[0]], dt)
+
+    y = g.op("RMSNorm", [ids["r"], ids["g1"]], "y", [seqs, width])
+    of_y = product(y, "y")
+    f, x = of_y("Wf", "f", "f32"), of_y("Wx", "x", "f32")
+    ids["new_states"] = g.op("GatedScan", [f, x, ids["states"]], "new_states", [seqs, inner], attrs=[seqs])
+    o = product(ids["new_states"], "h")("Wo", "o", "f32")
+    ids["r2"] = g.op("Add", [ids["r"], o], "r2", [seqs, width], "bf16")
+    return g, ids
+
+
+def clipped_updater(shapes, limit):
+    """W_i' = W_i - lr * g_i * min(1, limit / norm(g_1, g_2, ...)) for every shape: the norm and the factor are one launch, the
+    clipping is part of every update's own pass.  Returns (graph, ids) with lists W, g, W_new and the norm."""
+    g = GraphDesc()
+    ids = {"W": [g.tensor("W%d" % i, s) for i, s in enumerate(shapes)], "g": [g.tensor("g%d" % i, s) for i, s in enumerate(shapes)], "lr": g.tensor("lr", [])}
+    ids["norm"] = g.op("GlobalNorm", ids["g"], "norm", [])
+    ids["W_new"] = []
+    for i, (w, d, s) in enumerate(zip(ids["W"], ids["g"], shapes)):
+        c = g.op("ClipByNorm", [d, ids["norm"]], "clipped%d" % i, s, attrs=[limit])
+        ids["W_new"].append(g.op("Sub", [w, g.op("Mul", [ids["lr"], c], "step%d" % i, s)], "W_new%d" % i, s))
     return g, ids

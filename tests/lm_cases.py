@@ -20,7 +20,7 @@ def to_gpu(a, dtype):
     import torch
     if dtype == "i32":
         return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
-    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda().to(torch_type(dtype))
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32).reshape(np.shape(a))).cuda().to(torch_type(dtype))
 
 
 def run_gpu(desc, inputs, outputs, feeds, function=None, fill=True):
