@@ -25,11 +25,14 @@
 namespace dragon {
 namespace {
 
-// The forward folds 16 rows a warp (4 CTAs of 4 warps per SM, the next tile's rows on their way), the gradient, which holds
-// three tensors' rows and three values per element, 8 (2 CTAs of 8 warps).  Measured on 65536 x 1024 bf16, one sequence (and
-// 1024 of them, where no tile needs another): forward 4 x 16 rows 175 us (112), 8 x 8 199 (117), folding one tile ahead of the
-// one that waits 242 (143: the second tile's registers cost more than the wait); gradient 337 (258).  The bytes alone: 61, 143.
-constexpr int kFwdWarps = 4, kBwdWarps = 8, kFwdCtas = 4, kBwdCtas = 2;
+// The forward folds 16 rows a warp (3 CTAs of 4 warps per SM, the next tile's rows on their way in registers), the gradient,
+// which holds three tensors' rows and three values per element, 8 (2 CTAs of 8 warps; the next tile's rows on their way to
+// L2).  Measured on 65536 x 1024 bf16, one sequence (and 1024 of them, where no tile needs another): forward 164 us (98),
+// with 4 CTAs and their spills 175 (112), 8 x 8 rows 199 (117), folding one tile ahead of the one that waits 242 (143: the
+// second tile's registers cost more than the wait); gradient 295 (241), without the next tile asked for 337 (258).  The bytes
+// alone: 61, 143.
+constexpr int kFwdWarps = 4, kBwdWarps = 8, kBwdCtas = 2;
+template <int CH> constexpr int kFwdCtas = CH == 2 ? 3 : 4;      // per SM, as registers allow
 template <int W> constexpr int rows_per_warp() { return kScanTileRows / W; }
 constexpr long long kWaitBudgetCycles = 4000000000LL;   // about two seconds
 constexpr unsigned kAbsent = 0xffffffffu;          // an exchange word that has not been written
@@ -207,12 +210,12 @@ template <int W, int kCopies> struct TileShared {
 };
 
 // This warp's share of the run's tiles in front of tile `order`: their pairs, folded in order (waits for them)
-template <int W, int K> __device__ __forceinline__ void fold_run(const ScanArgs& a, TileShared<W, K>& sh, int order, int group, int warp, int lane) {
+// kAhead: loads in flight together (the forward over fp32 rows has registers for half of them: 95 us for 107 on 16384 x 2048)
+template <int kAhead, int W, int K> __device__ __forceinline__ void fold_run(const ScanArgs& a, TileShared<W, K>& sh, int order, int group, int warp, int lane) {
   constexpr int kShare = kRun / W;
   const int first = order / kRun * kRun + warp * kShare, n = min(kShare, order - first);
   float4 ab = make_float4(1.f, 1.f, 0.f, 0.f);
   bool closed = false;
-  constexpr int kAhead = 4;                        // loads in flight together
 #pragma unroll 1
   for (int i0 = 0; i0 < n; i0 += kAhead) {
     uint4 p[kAhead];
@@ -237,8 +240,12 @@ template <int W, int K> __device__ __forceinline__ void fold_run(const ScanArgs&
   sh.seg[warp][lane] = ab;
   if (lane == 0) sh.seg_closed[warp] = closed;
 }
-// ... and, after a barrier, the state in front of tile `order`
-template <int W, int K> __device__ __forceinline__ float2 state_in_front(const ScanArgs& a, const TileShared<W, K>& sh, int order, int group, int lane) {
+// the first look at the state in front of the run, sent for before the pairs
+__device__ __forceinline__ uint2 early_start(const ScanArgs& a, int order, int group, int lane) {
+  return order < kRun ? make_uint2(0, 0) : look(a.start + slot_of(a, order / kRun, group, lane));
+}
+// ... and, after a barrier, the state in front of tile `order` (u: the first look)
+template <int W, int K> __device__ __forceinline__ float2 state_in_front(const ScanArgs& a, const TileShared<W, K>& sh, int order, int group, int lane, uint2 u) {
   float2 v = make_float2(0.f, 0.f);
   const int run = order / kRun;
   bool cut = run == 0;
@@ -246,7 +253,6 @@ template <int W, int K> __device__ __forceinline__ float2 state_in_front(const S
   for (int w = 0; w < W; ++w) cut = cut || sh.seg_closed[w];
   if (!cut) {
     const uint2* from = a.start + slot_of(a, run, group, lane);
-    uint2 u = look(from);
     const long long t0 = clock64();
     while ((u.x == kAbsent || u.y == kAbsent) && !out_of_time(a, t0)) u = look(from);
     __syncwarp();
@@ -312,6 +318,19 @@ template <int DT, int CH, int N, int kRows> struct TileRows {
     for (int e = 0; e < CH; ++e) x.v[e] = v[k][r].get(e);
     return x;
   }
+  // asks L2 for the warp's rows of a tile that comes later: columns [c0, c0 + 32 CH) of kRows rows, in quarters
+  static __device__ __forceinline__ void ask(const ScanArgs& a, int row0, int c0, int lane) {
+    const void* src[3] = {a.gate, a.x, a.dh};
+    const int dt[3] = {a.gdt, a.xdt, a.dhdt};
+    const int c = min(c0 + (lane & 3) * 8 * CH, a.cols - 1);
+#pragma unroll
+    for (int r0 = 0; r0 < kRows; r0 += 8) {
+      const size_t at = (size_t)min(row0 + r0 + (lane >> 2), a.rows - 1) * a.cols + c;
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(src[k]) + at * element_bytes<DT>(dt[k])));
+    }
+  }
   __device__ __forceinline__ void load(const ScanArgs& a, int row0, int c) {
     const void* src[3] = {a.gate, a.x, a.dh};
     const int dt[3] = {a.gdt, a.xdt, a.dhdt};
@@ -352,7 +371,7 @@ template <int CH, int kRows> struct Folded {
 
 // Persistent CTAs.  While a tile waits for what is in front of it, the next tile's rows are on their way.
 template <int DT, int CH>
-__global__ void __launch_bounds__(kFwdWarps * 32, kFwdCtas) scan_kernel(const ScanArgs a) {
+__global__ void __launch_bounds__(kFwdWarps * 32, kFwdCtas<CH>) scan_kernel(const ScanArgs a) {
   constexpr int W = kFwdWarps, kRows = rows_per_warp<W>();
   __shared__ TileShared<W, 3> sh;
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
@@ -423,9 +442,10 @@ __global__ void __launch_bounds__(kFwdWarps * 32, kFwdCtas) scan_kernel(const Sc
     if (a.pair) {
       const bool open = !(sh.fresh[copy][0] & 1);         // the tile's first row goes on from the tile before
       if (open) {
-        fold_run(a, sh, o.at.tile, o.at.group, warp, lane);
+        const uint2 u = early_start(a, o.at.tile, o.at.group, lane);
+        fold_run<DT == DRAGON_BF16 ? kRun / W : kRun / W / 2>(a, sh, o.at.tile, o.at.group, warp, lane);
         __syncthreads();
-        front = state_in_front(a, sh, o.at.tile, o.at.group, lane);
+        front = state_in_front(a, sh, o.at.tile, o.at.group, lane, u);
       }
       if (warp == 0 && o.at.tile % kRun == kRun - 1) {
         bool closed;
@@ -533,15 +553,21 @@ __global__ void __launch_bounds__(kBwdWarps * 32, kBwdCtas) scan_bwd_kernel(cons
     if (threadIdx.x == 0) sh.ticket[0] = a.pair ? take_tickets(a, 1) : ticket + gridDim.x;
     __syncthreads();
     ticket = sh.ticket[0];
+    if (ticket < n) {        // (registers hold one tile only: the next one comes as far as L2)
+      const Place next = Place::of<true>(a, ticket);
+      TileRows<DT, CH, 3, kRows>::ask(a, next.tile * kScanTileRows + warp * kRows, next.group * 32 * CH, lane);
+    }
     bool closed = false;
     float4 ab;
+    uint2 u = make_uint2(0, 0);
     if (a.pair) {
+      u = early_start(a, order, group, lane);
       if (warp == W - 1) {
         ab = fold_tile<W>(sh.ab[1], sh.fresh[0], lane, -1, &closed);
         publish_pair(a, order, group, lane, ab, closed);
         if (closed) publish_start(a, order, group, lane, make_float2(ab.z, ab.w));
       }
-      fold_run(a, sh, order, group, warp, lane);
+      fold_run<kRun / W>(a, sh, order, group, warp, lane);
     }
     {
       const float2 in = through(sh.ab[0], sh.fresh[0], lane, 0, warp, 1, make_float2(carry[0], carry[1]));
@@ -558,7 +584,7 @@ __global__ void __launch_bounds__(kBwdWarps * 32, kBwdCtas) scan_bwd_kernel(cons
     float2 front = make_float2(0.f, 0.f);
     if (a.pair) {
       __syncthreads();
-      front = state_in_front(a, sh, order, group, lane);
+      front = state_in_front(a, sh, order, group, lane, u);
       if (warp == W - 1 && !closed) publish_start(a, order, group, lane, make_float2(fmaf(ab.x, front.x, ab.z), fmaf(ab.y, front.y, ab.w)));
     }
     const float2 in = through(sh.ab[1], sh.fresh[0], lane, W - 1, warp, -1, front);
@@ -689,9 +715,9 @@ template <int DT> cudaError_t launch_fwd(const ScanArgs& a, int sm_count, cudaSt
     else scan_step_kernel<DT, 1><<<grid, 256, 0, st>>>(a);
     return cudaGetLastError();
   }
-  const unsigned grid = std::min((unsigned)a.tiles * a.groups, (unsigned)(sm_count * kFwdCtas));
-  if (two) scan_kernel<DT, 2><<<grid, kFwdWarps * 32, 0, st>>>(a);
-  else scan_kernel<DT, 1><<<grid, kFwdWarps * 32, 0, st>>>(a);
+  const unsigned n = (unsigned)a.tiles * a.groups;
+  if (two) scan_kernel<DT, 2><<<std::min(n, (unsigned)(sm_count * kFwdCtas<2>)), kFwdWarps * 32, 0, st>>>(a);
+  else scan_kernel<DT, 1><<<std::min(n, (unsigned)(sm_count * kFwdCtas<1>)), kFwdWarps * 32, 0, st>>>(a);
   return cudaGetLastError();
 }
 template <int DT> cudaError_t launch_bwd(const ScanArgs& a, int sm_count, cudaStream_t st) {
