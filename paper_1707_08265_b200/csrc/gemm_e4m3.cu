@@ -144,7 +144,7 @@ __device__ __forceinline__ bool issue_block(const Sync& s, const Gemm8Args& g, i
 // ---- many rows ------------------------------------------------------------------------------------------------
 
 constexpr int kTileM = 256, kTileN = 256, kStages = 6;          // of a pair; a CTA holds 128 rows of X and 128 of W
-constexpr int kEpiWarps = 16, kEpiThreads = 32 * kEpiWarps;     // four warps a quarter of the lanes: one's loads from TMEM hide behind the others' sums
+constexpr int kEpiWarps = 8, kEpiThreads = 32 * kEpiWarps;      // two warps a quarter of the lanes, 128 columns of it each: all the registers there are
 constexpr int kFetchWarps = 2;
 constexpr int kThreads = 64 + kEpiThreads + 32 * kFetchWarps;   // TMA, MMA, epilogue, scales
 constexpr int kTileBufs = 2;                                    // accumulators that take turns: all of TMEM
@@ -171,6 +171,61 @@ __device__ __forceinline__ void fetch_scales(const Gemm8Args& g, TileScales& to,
   }
 }
 
+// A warp holds 32 rows, a row to a lane; written like that, every 16 bytes would be half a sector of its own (a tile of bf16
+// took 5 us; with the exchanges below 2).  Eight neighbouring lanes exchange pieces of 16 bytes: piece u of lane p becomes
+// piece p of lane u.
+__device__ __forceinline__ void exchange(uint32_t& lo, uint32_t& hi, int lane, int b) {
+  const uint32_t got = __shfl_xor_sync(0xffffffffu, lane & b ? lo : hi, b);
+  if (lane & b) lo = got; else hi = got;
+}
+__device__ __forceinline__ void exchange_pieces(uint32_t (&v)[32], int lane) {
+#pragma unroll
+  for (int b = 1; b < 8; b <<= 1)
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (!(u & b))
+#pragma unroll
+        for (int i = 0; i < 4; ++i) exchange(v[4 * u + i], v[4 * (u | b) + i], lane, b);
+}
+// 32 rows' lines of 128 bytes (of 16-byte pieces whose first column is below `cols`), each written as a whole by 8 lanes
+template <bool kF32>
+__device__ __forceinline__ void store_lines(char* y, size_t row_bytes, int rows_left, int col0, int cols, uint32_t (&v)[32], int lane) {
+  exchange_pieces(v, lane);
+  if (col0 + (lane & 7) * (kF32 ? 4 : 8) >= cols) return;
+  char* at = y + (lane & 24) * row_bytes + (lane & 7) * 16;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if ((lane & 24) + i < rows_left) *reinterpret_cast<uint4*>(kF32 ? at : at + i * row_bytes) = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    if (kF32) at += row_bytes;           // (one address in registers, where four parts of a row would spill them)
+  }
+}
+// ... and where rows do not start at 16-byte boundaries: word u of lane p becomes word p of lane u, and the warp writes one
+// row after another
+template <bool kF32>
+__device__ __forceinline__ void store_words(char* y, size_t row_bytes, int rows_left, int col0, int cols, uint32_t (&v)[32], int lane) {
+#pragma unroll
+  for (int b = 1; b < 32; b <<= 1)
+#pragma unroll
+    for (int u = 0; u < 32; ++u)
+      if (!(u & b)) exchange(v[u], v[u | b], lane, b);
+  const int left = cols - col0 - (kF32 ? lane : 2 * lane);
+  char* at = y + 4 * lane;
+#pragma unroll
+  for (int r = 0; r < 32; ++r, at += row_bytes) {
+    if (r >= rows_left) break;
+    if (kF32) {
+      if (left > 0) *reinterpret_cast<uint32_t*>(at) = v[r];
+    } else if (cols % 2 == 0) {
+      if (left > 0) *reinterpret_cast<uint32_t*>(at) = v[r];
+    } else {
+      if (left > 0) *reinterpret_cast<unsigned short*>(at) = (unsigned short)v[r];
+      if (left > 1) *reinterpret_cast<unsigned short*>(at + 2) = (unsigned short)(v[r] >> 16);
+    }
+  }
+}
+
+// One kernel for each way to write a tile: with all of them in one the registers spill (285 us instead of 260).
+template <bool kF32, bool kLines>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_w, const Gemm8Args g) {
   extern __shared__ unsigned char smem_raw[];
@@ -288,21 +343,24 @@ gemm_e4m3_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_consta
       }
       int tm, tn;
       tile_coords(t, g.tiles_m, g.tiles_n, &tm, &tn);
-      const int row = tm * kTileM + (int)rank * 128 + q * 32 + lane;
-      if (!ok || row >= g.M) continue;
+      if (!ok) continue;
+      const int row0 = tm * kTileM + (int)rank * 128 + q * 32;
+      constexpr int kCols = kF32 ? 32 : 64, kBytes = kF32 ? 4 : 2;         // 128 bytes of a row at a time
+      const size_t row_bytes = (size_t)g.N * kBytes;
       const int col0 = tn * kTileN + first_col;
-      const size_t at = (size_t)row * g.N + col0;
-      const bool whole = (g.N & 7) == 0 && col0 + kEpiCols <= g.N;
+      char* y = static_cast<char*>(g.y) + (size_t)row0 * row_bytes + (size_t)col0 * kBytes;
 #pragma unroll
-      for (int j = 0; j < kEpiCols / 2; j += 4) {
-        float v[8];
+      for (int h = 0; h < kEpiCols / kCols; ++h) {
+        if (!kLines) asm volatile("" ::: "memory");     // (one part after another, or registers spill)
+        uint32_t v[32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 p = unpack(acc[j + i]); v[2 * i] = p.x; v[2 * i + 1] = p.y; }
-        if (whole) store_any<8>(g.y, g.ydt, at + 2 * j, v);
-        else
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (col0 + 2 * j + i < g.N) store_any<1>(g.y, g.ydt, at + 2 * j + i, v + i);
+        for (int j = 0; j < kCols / 2; ++j) {
+          const float2 p = unpack(acc[kCols / 2 * h + j]);
+          if (kF32) { v[2 * j] = __float_as_uint(p.x); v[2 * j + 1] = __float_as_uint(p.y); }
+          else v[j] = bf16_pair(p.x, p.y);
+        }
+        if (kLines) store_lines<kF32>(y + 128 * h, row_bytes, g.M - row0, col0 + kCols * h, g.N, v, lane);
+        else store_words<kF32>(y + 128 * h, row_bytes, g.M - row0, col0 + kCols * h, g.N, v, lane);
       }
     }
   }
@@ -513,7 +571,7 @@ bool make_tmap8(CUtensorMap* map, const void* ptr, int64_t rows, int64_t k, int 
 // once per device and kernel: the shared-memory attribute
 cudaError_t allow_smem(const void* kern, size_t bytes, int variant) {
   static std::mutex mu;
-  static bool done[64][5] = {};
+  static bool done[64][8] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
@@ -541,6 +599,22 @@ cudaError_t launch_few(const CUtensorMap& tx, const CUtensorMap& tw, const Gemm8
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, gemm_e4m3_few_kernel<NT>, tx, tw, g);
 }
+template <bool kF32, bool kLines>
+cudaError_t launch_pairs(const CUtensorMap& tx, const CUtensorMap& tw, const Gemm8Args& g, int pairs, int variant, cudaStream_t st) {
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(gemm_e4m3_kernel<kF32, kLines>), kSmem, variant);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * std::min(g.tiles_m * g.tiles_n, pairs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, gemm_e4m3_kernel<kF32, kLines>, tx, tw, g);
+}
 
 }  // namespace
 
@@ -556,9 +630,11 @@ int launch_gemm_e4m3(const StepRun& r) {
   if (tiles_m * tiles_n > 0x3fffffffLL) { set_error("ScaledInnerProduct: too many tiles"); return DRAGON_ERR_UNSUPPORTED; }
   g.tiles_m = (int)tiles_m;
   g.tiles_n = (int)tiles_n;
-  // The large tiles wherever they give every pair of SMs one; otherwise the small ones, their blocks split while CTAs find room
+  // The small tiles where rows are few or the GPU holds all of them at once, their blocks split while CTAs find room; otherwise
+  // the large ones.  Small and large: 777 x 2056 x 2064 18.7 us and 20.8, 256 x 2048 x 8192 21 and 39, 256 x 8192 x 4096 28 and
+  // 27, 512 x 8192 x 4096 49 and 28, 2048 x 2048 x 2048 31 and 20.
   const int pairs = r.sm_count / 2;
-  const bool few = tiles_m * tiles_n < pairs || g.M <= 128;
+  const bool few = g.M <= 128 || ((g.M + 127) / 128) * (int64_t)((g.N + 127) / 128) <= r.sm_count;
   const int nt = g.M <= 16 ? 16 : g.M <= 32 ? 32 : g.M <= 64 ? 64 : 128;
   CUtensorMap tx, tw;
   if (!make_tmap8(&tx, r.rd(g8::XQ), g.M, g.K, few ? nt : 128) || !make_tmap8(&tw, r.rd(g8::WQ), g.N, g.K, 128)) {
@@ -573,20 +649,9 @@ int launch_gemm_e4m3(const StepRun& r) {
     e = nt == 16 ? launch_few<16>(tx, tw, g, 1, st) : nt == 32 ? launch_few<32>(tx, tw, g, 2, st)
         : nt == 64 ? launch_few<64>(tx, tw, g, 3, st) : launch_few<128>(tx, tw, g, 4, st);
   } else {
-    e = allow_smem(reinterpret_cast<const void*>(gemm_e4m3_kernel), kSmem, 0);
-    if (e == cudaSuccess) {
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(2 * std::min(g.tiles_m * g.tiles_n, pairs));
-      cfg.blockDim = dim3(kThreads);
-      cfg.dynamicSmemBytes = kSmem;
-      cfg.stream = st;
-      cudaLaunchAttribute attr[1];
-      attr[0].id = cudaLaunchAttributeClusterDimension;
-      attr[0].val.clusterDim.x = 2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-      cfg.attrs = attr;
-      cfg.numAttrs = 1;
-      e = cudaLaunchKernelEx(&cfg, gemm_e4m3_kernel, tx, tw, g);
-    }
+    const bool lines = g.N % (g.ydt == DRAGON_F32 ? 4 : 8) == 0;
+    if (g.ydt == DRAGON_F32) e = lines ? launch_pairs<true, true>(tx, tw, g, pairs, 0, st) : launch_pairs<true, false>(tx, tw, g, pairs, 5, st);
+    else e = lines ? launch_pairs<false, true>(tx, tw, g, pairs, 6, st) : launch_pairs<false, false>(tx, tw, g, pairs, 7, st);
   }
   if (e != cudaSuccess) { set_error("ScaledInnerProduct: launch failed: %s", cudaGetErrorString(e)); return DRAGON_ERR_CUDA; }
   return DRAGON_OK;
