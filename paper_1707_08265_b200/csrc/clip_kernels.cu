@@ -1,8 +1,10 @@
 // The 2-norm over many tensors, and every tensor times min(1, limit / norm).
 //   norm = sqrt(sum_i sum_e t_i[e]^2),  c_i = t_i * (norm > limit ? limit / norm : 1)
 // Bound: bytes (every tensor read for the norm, then read and written; read once where all of them fit the registers of the
-// GPU, 19 MB).  All tensors are one list of chunks that
-// persistent CTAs walk, so that a launch takes any mix of sizes; the addresses travel in the launch's parameters.
+// GPU, 19 MB).  All tensors are one list of chunks that persistent CTAs walk, so that a launch takes any mix of sizes; the
+// addresses travel in the launch's parameters.  Measured, 393M bf16 in 49 tensors: norm 144 us (5.5 TB/s read), clipping 259 us
+// (6.1 TB/s, what L2 holds of the norm's last reads included); 0.65M fp32 in 5 tensors, both in one launch: 8 us, of which the
+// launch and the barrier are nearly all.
 // Squares are added in fp32 over the 16 or 32 elements a thread holds at a time and in fp64 beyond; elements whose squares
 // could leave fp32's range are squared in fp64.  The order of the sums is fixed, so the norm is the same in every run.
 #include <algorithm>
@@ -40,28 +42,48 @@ struct NormOut {
   int* status_clear;
 };
 
-// A CTA's chunks are one run of the list, so that the tensor of the next chunk is this one or the next.  Walked upwards by
-// the norm and downwards by the clipping: what the norm read last is what L2 still holds.
+// A CTA takes every gridDim.x-th chunk of the list, so that the CTAs together read one place after another.  Walked upwards
+// by the norm and downwards by the clipping: what the norm read last is what L2 still holds.  What the chunk's tensor is like
+// is looked up when the walk comes to another tensor.
 struct Walk {
-  int c, end, k, dir;
-  template <typename TensorList> __device__ __forceinline__ Walk(const TensorList& t, int dir_) : dir(dir_) {
-    const long long n = t.first[t.count];
-    const int c0 = (int)(n * blockIdx.x / gridDim.x), c1 = (int)(n * (blockIdx.x + 1) / gridDim.x);
-    c = dir > 0 ? c0 : c1 - 1;
-    end = dir > 0 ? c1 : c0 - 1;
-    int lo = 0, hi = t.count - 1;                  // the last tensor whose first chunk is not behind c
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (t.first[mid] <= c) lo = mid; else hi = mid - 1;
+  int c, left, step;           // chunk, chunks that come after it plus one, distance of the next
+  int k, lo, hi;               // its tensor, that tensor's chunks
+  const void* src;
+  void* dst;
+  long long n, first;          // the tensor's elements, the chunk's first one
+  int sdt, ddt;
+  template <typename TensorList> __device__ __forceinline__ Walk(const TensorList& t, int dir) {
+    const int chunks = t.first[t.count], mine = (int)blockIdx.x < chunks ? (chunks - 1 - (int)blockIdx.x) / (int)gridDim.x + 1 : 0;
+    left = mine;
+    step = dir * (int)gridDim.x;
+    c = (int)blockIdx.x + (dir > 0 ? 0 : max(mine - 1, 0) * (int)gridDim.x);
+    int a = 0, b = t.count - 1;                    // the last tensor whose first chunk is not behind c
+    while (a < b) {
+      const int mid = (a + b + 1) >> 1;
+      if (t.first[mid] <= c) a = mid; else b = mid - 1;
     }
-    k = lo;
+    k = a;
+    look_up(t);
   }
-  __device__ __forceinline__ bool more() const { return c != end; }
-  template <typename TensorList> __device__ __forceinline__ long long element(const TensorList& t) const { return (long long)(c - t.first[k]) * chunk_elements((t.dtype[k] & 15) == DRAGON_F32); }
+  template <typename TensorList> __device__ __forceinline__ void look_up(const TensorList& t) {
+    lo = t.first[k];
+    hi = t.first[k + 1];
+    src = t.src[k];
+    dst = t.dst[k];
+    n = t.n[k];
+    sdt = t.dtype[k] & 15;
+    ddt = t.dtype[k] >> 4;
+    first = (long long)(c - lo) * chunk_elements(f32());
+  }
+  __device__ __forceinline__ bool f32() const { return sdt == DRAGON_F32; }
+  __device__ __forceinline__ bool more() const { return left > 0; }
   template <typename TensorList> __device__ __forceinline__ void next(const TensorList& t) {
-    c += dir;
-    if (!more()) return;
-    while (dir > 0 ? t.first[k + 1] <= c : t.first[k] > c) k += dir;
+    c += step;
+    if (--left <= 0) return;
+    if (c >= lo && c < hi) { first += (long long)step * chunk_elements(f32()); return; }
+    while (c >= t.first[k + 1]) ++k;
+    while (c < t.first[k]) --k;
+    look_up(t);
   }
 };
 
@@ -109,6 +131,27 @@ template <int N> __device__ __forceinline__ double squares(const float* v) {
   for (int e = 0; e < N; ++e) d += (double)v[e] * (double)v[e];
   return d;
 }
+// ... of 32 bf16 in 16 words, two at a time
+__device__ __forceinline__ double squares_of_bf16(const uint4 (&u)[4]) {
+  const unsigned* w = reinterpret_cast<const unsigned*>(u);
+  unsigned m = 0;
+  unsigned long long s = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+    unsigned long long v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(bf16_low(w[i])), "f"(bf16_high(w[i])));
+    asm("fma.rn.f32x2 %0, %1, %1, %0;" : "+l"(s) : "l"(v));
+  }
+  m = max(m & 0xffffu, m >> 16);
+  float a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(s));
+  if (m == 0 || (m >= 0x2b80u && m <= 0x5d80u)) return (double)(a + b);
+  double d = 0.0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) d += (double)bf16_low(w[i]) * (double)bf16_low(w[i]) + (double)bf16_high(w[i]) * (double)bf16_high(w[i]);
+  return d;
+}
 __device__ __forceinline__ double chunk_squares(const Chunk& ch, const void* src, bool f32, long long first, long long n) {
   double d;
   if (f32) {
@@ -117,10 +160,7 @@ __device__ __forceinline__ double chunk_squares(const Chunk& ch, const void* src
     for (int j = 0; j < 4; ++j) values_of(ch.u[j], v[j]);
     d = squares<16>(v[0]);
   } else {
-    float v[4][8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) values_of(ch.u[j], v[j]);
-    d = squares<32>(v[0]);
+    d = squares_of_bf16(ch.u);
   }
   long long i;
   if (tail_element(f32, first, n, &i)) {
@@ -150,13 +190,13 @@ template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtas
   double sum = 0.0;
   Walk w(t, 1);
   Chunk next;
-  if (w.more()) next.load<true>(t.src[w.k], t.dtype[w.k] == DRAGON_F32, w.element(t), t.n[w.k]);
+  if (w.more()) next.load<true>(w.src, w.f32(), w.first, w.n);
   while (w.more()) {
     const Chunk now = next;
     const Walk here = w;
     w.next(t);
-    if (w.more()) next.load<true>(t.src[w.k], t.dtype[w.k] == DRAGON_F32, w.element(t), t.n[w.k]);
-    sum += chunk_squares(now, t.src[here.k], t.dtype[here.k] == DRAGON_F32, here.element(t), t.n[here.k]);
+    if (w.more()) next.load<true>(w.src, w.f32(), w.first, w.n);
+    sum += chunk_squares(now, here.src, here.f32(), here.first, here.n);
   }
   sum = block_sum(sum, sh);
   if (threadIdx.x == 0) {
@@ -228,8 +268,8 @@ template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtas
     tensor[h] = -1;
     if (!w.more()) continue;
     tensor[h] = w.k;
-    first[h] = w.element(t);
-    held[h].load<false>(t.src[w.k], (t.dtype[w.k] & 15) == DRAGON_F32, first[h], t.n[w.k]);
+    first[h] = w.first;
+    held[h].load<false>(w.src, w.f32(), w.first, w.n);
     w.next(t);
   }
   double sum = 0.0;
@@ -277,17 +317,16 @@ template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtas
   Walk w(t, -1);
   Chunk next;
   auto load = [&] {
-    if (w.more() && !(f == 1.f && t.src[w.k] == t.dst[w.k])) next.load<false>(t.src[w.k], (t.dtype[w.k] & 15) == DRAGON_F32, w.element(t), t.n[w.k]);
+    if (w.more() && !(f == 1.f && w.src == w.dst)) next.load<false>(w.src, w.f32(), w.first, w.n);
   };
   load();
   while (w.more()) {
     const Chunk now = next;
-    const int k = w.k, sdt = t.dtype[k] & 15, ddt = t.dtype[k] >> 4;
-    const long long first = w.element(t), n = t.n[k];
+    const Walk here = w;
     w.next(t);
     load();
-    if (f == 1.f && t.src[k] == t.dst[k]) continue;      // in place and nothing to change
-    store_clipped(now, t.src[k], sdt, t.dst[k], ddt, first, n, f);
+    if (f == 1.f && here.src == here.dst) continue;      // in place and nothing to change
+    store_clipped(now, here.src, here.sdt, here.dst, here.ddt, here.first, here.n, f);
   }
 }
 
