@@ -125,6 +125,19 @@ template <int V> __device__ __forceinline__ void store_e4m3(unsigned char* p, co
 
 // Largest magnitude of a block as the integer that orders floats of one sign: a NaN is larger than everything and stays
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+template <int DT> __device__ __forceinline__ unsigned largest_magnitude(const Raw<DT, 8>& r) {
+  float v[8];
+  r.get(v);
+  unsigned m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, magnitude(v[e]));
+  return m;
+}
+template <> __device__ __forceinline__ unsigned largest_magnitude<DRAGON_BF16>(const Raw<DRAGON_BF16, 8>& r) {      // two at a time
+  constexpr unsigned k = 0x7fff7fffu;
+  const unsigned m = __vmaxu2(__vmaxu2(r.u.x & k, r.u.y & k), __vmaxu2(r.u.z & k, r.u.w & k));
+  return max(m & 0xffff0000u, m << 16);
+}
 __device__ __forceinline__ float scale_of(unsigned magnitude_bits) {
   const float s = __fdiv_rn(__uint_as_float(magnitude_bits), 448.f);
   return s < 1.17549435e-38f ? 1.17549435e-38f : s;      // 2^-126; a comparison with NaN is false, so NaN stays
