@@ -646,7 +646,6 @@ int launch_gemm_e4m3(const StepRun& r) {
   cudaError_t e;
   if (few) {
     const int64_t ctas = (int64_t)((g.N + 127) / 128) * ((g.M + nt - 1) / nt);
-    if ((g.M + nt - 1) / nt > 65535) { set_error("ScaledInnerProduct: too many rows"); return DRAGON_ERR_UNSUPPORTED; }
     while (g.split < 8 && ctas * g.split * 2 <= few_ctas(nt) * r.sm_count && g.kb >= 4 * g.split) g.split *= 2;
     e = nt == 16 ? launch_few<16>(tx, tw, g, 1, st) : nt == 32 ? launch_few<32>(tx, tw, g, 2, st)
         : nt == 64 ? launch_few<64>(tx, tw, g, 3, st) : launch_few<128>(tx, tw, g, 4, st);

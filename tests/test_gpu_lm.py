@@ -168,7 +168,9 @@ def product_case(M, N, K, out, seed):
 @pytest.mark.parametrize("M,N,K", [(1, 1, 16), (1, 64, 128), (2, 129, 144), (5, 256, 4096), (8, 1000, 272), (16, 512, 2048), (17, 136, 1040), (33, 384, 512), (64, 128, 128),
                                    (65, 300, 400), (128, 256, 128), (129, 257, 384), (200, 1024, 1024), (300, 520, 2064), (512, 768, 640), (1000, 1000, 1008),
                                    # enough tiles of 128 x 256 for every SM: the kernel of many rows, ragged in every extent, more tiles than SMs
-                                   (2433, 2049, 272), (2400, 2056, 128), (4900, 1000, 400), (19000, 96, 16)])
+                                   (2433, 2049, 272), (2400, 2056, 128), (4900, 1000, 400), (19000, 96, 16),
+                                   # ... whose rows start at multiples of 4 and of 8 bytes
+                                   (2431, 2050, 160), (1301, 2052, 272)])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_scaled_product(M, N, K, out):
     g, t, y, feeds = product_case(M, N, K, out, M * 7 + N * 3 + K)
