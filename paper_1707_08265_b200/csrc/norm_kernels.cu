@@ -5,9 +5,10 @@
 //   gradient  dh = skip + rstd * (t - h * rstd^2 * mean(t h)),  t = dy g;   dg = sum over rows of dy h rstd
 // Bound: bytes.  A row stays in the registers of its threads between the reduction and the output, so everything is read
 // and written once; the statistics are fp32 sums.  Row lengths that do not fit take a second pass over the row.
-// Measured, bf16, the kernel by itself: norm with residual and sum 8192 x 4096 48 us (5.6 TB/s), 16384 x 4096 87 us (6.2); with
-// scales and e4m3 values for y 4099 x 5000 37 us (3.9: the divisions of the scales and a short launch), 16384 x 4096 93 us (5.1);
-// gradient with the residual branch's 8192 x 4096 64 us (5.2).
+// Measured, bf16, the kernel by itself: norm with residual and sum 8192 x 4096 48 us (5.6 TB/s), 16384 x 4096 87 us (6.2), in fp32
+// 8192 x 8192 210 us (5.1); with scales and e4m3 values for y 4099 x 5000 35 us (4.1), 16384 x 4096 88 us (5.3; a division for each
+// lane and access instead 93); rows of 5001 81 us (single elements), of 5002 58 (pairs), of 5000 36; gradient with the residual
+// branch's 8192 x 4096 64 us (5.2).
 #include "device_util.h"
 #include "plan.h"
 
@@ -114,33 +115,41 @@ __global__ void __launch_bounds__(kMaxRowThreads, DT == DRAGON_BF16 && V == 8 &&
   }
   sum = row_sum2(sum, a.threads, sh);
   const float rstd = rsqrtf(sum.x / (float)a.cols + a.eps);
+  float y[PER][V];
+  unsigned m = 0;
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int j = (t + k * a.threads) * V;
-    const bool mine = in && j < a.cols;
-    float y[V];
-    unsigned m = 0;
-#pragma unroll
-    for (int e = 0; e < V; ++e) y[e] = 0.f;
-    if (mine) {
+    unsigned mk = 0;
+    if (in && j < a.cols) {
       float g[V];
       load_any<V>(a.gain, a.gdt, j, g);
-      h[k].get(y);
+      h[k].get(y[k]);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        y[e] = y[e] * rstd * g[e];
-        if (a.ydt == DRAGON_BF16) y[e] = bf16_rounded(y[e]);
-        m = max(m, magnitude(y[e]));
+        y[k][e] = y[k][e] * rstd * g[e];
+        if (a.ydt == DRAGON_BF16) y[k][e] = bf16_rounded(y[k][e]);
+        mk = max(mk, magnitude(y[k][e]));
       }
-      if (a.y) store_any<V>(a.y, a.ydt, base + j, y);
+      if (a.y) store_any<V>(a.y, a.ydt, base + j, y[k]);
     }
-    if (V == 8 && (a.s || a.q)) {       // 16 neighbouring threads hold a block of 128
+    if (V == 8 && (a.s || a.q)) {       // 16 neighbouring threads hold a block of 128; lane l % PER of them keeps block k's maximum
 #pragma unroll
-      for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const float s = scale_of(m);
-      if (mine && a.s && (t & 15) == 0) a.s[(size_t)row * ((a.cols + 127) / 128) + j / 128] = s;
-      if (mine && a.q) store_e4m3<V>(reinterpret_cast<unsigned char*>(a.q) + base + j, y, __frcp_rn(s));
+      for (int o = 8; o > 0; o >>= 1) mk = max(mk, __shfl_xor_sync(0xffffffffu, mk, o));
+      if (t % PER == k) m = mk;
     }
+  }
+  if (V == 8 && (a.s || a.q)) {         // the scales, two correctly rounded divisions each, of PER blocks at once
+    const float s = scale_of(m), inv = __frcp_rn(s);
+    const int l = t & 15, first = (t - l + l * a.threads) * V;
+    if (a.s && in && l < PER && first < a.cols) a.s[(size_t)row * ((a.cols + 127) / 128) + first / 128] = s;
+    if (a.q)
+#pragma unroll
+      for (int k = 0; k < PER; ++k) {
+        const float inv_k = __shfl_sync(0xffffffffu, inv, (threadIdx.x & 16) + k);
+        const int j = (t + k * a.threads) * V;
+        if (in && j < a.cols) store_e4m3<V>(reinterpret_cast<unsigned char*>(a.q) + base + j, y[k], inv_k);
+      }
   }
 }
 
