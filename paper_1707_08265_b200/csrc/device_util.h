@@ -143,4 +143,98 @@ __device__ __forceinline__ float scale_of(unsigned magnitude_bits) {
   return s < 1.17549435e-38f ? 1.17549435e-38f : s;      // 2^-126; a comparison with NaN is false, so NaN stays
 }
 
+// Four consecutive elements for each lane of a warp, lane after lane, from an element on that is no multiple of 4: every lane
+// reads the aligned vector that its first element lies in, and takes the rest from the next lane's.
+template <int DT> struct Quad;
+template <> struct Quad<DRAGON_BF16> {
+  typedef uint2 Vec;
+  uint2 u;
+  __device__ __forceinline__ void get(float* v) const { v[0] = bf16_low(u.x); v[1] = bf16_high(u.x); v[2] = bf16_low(u.y); v[3] = bf16_high(u.y); }
+  static __device__ __forceinline__ uint2 part(const char* p, int n) {      // the first n of an aligned vector's elements (n < 4)
+    const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+    uint2 v = make_uint2(0, 0);
+    if (n > 0) v.x = __ldg(q);
+    if (n > 1) v.x |= (unsigned)__ldg(q + 1) << 16;
+    if (n > 2) v.y = __ldg(q + 2);
+    return v;
+  }
+  static __device__ __forceinline__ uint2 next_lane(uint2 v) { return make_uint2(__shfl_down_sync(0xffffffffu, v.x, 1), __shfl_down_sync(0xffffffffu, v.y, 1)); }
+  static __device__ __forceinline__ uint2 of_lane(uint2 v, int l) { return make_uint2(__shfl_sync(0xffffffffu, v.x, l), __shfl_sync(0xffffffffu, v.y, l)); }
+  static __device__ __forceinline__ uint2 join(uint2 v, uint2 n, int lead) {      // elements lead .. lead + 3 of the two
+    if (lead & 2) { v.x = v.y; v.y = n.x; n.x = n.y; }
+    if (lead & 1) { v.x = __funnelshift_r(v.x, v.y, 16); v.y = __funnelshift_r(v.y, n.x, 16); }
+    return v;
+  }
+};
+template <> struct Quad<DRAGON_F32> {
+  typedef uint4 Vec;
+  uint4 u;
+  __device__ __forceinline__ void get(float* v) const { v[0] = __uint_as_float(u.x); v[1] = __uint_as_float(u.y); v[2] = __uint_as_float(u.z); v[3] = __uint_as_float(u.w); }
+  static __device__ __forceinline__ uint4 part(const char* p, int n) {
+    const unsigned* q = reinterpret_cast<const unsigned*>(p);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (n > 0) v.x = __ldg(q);
+    if (n > 1) v.y = __ldg(q + 1);
+    if (n > 2) v.z = __ldg(q + 2);
+    return v;
+  }
+  static __device__ __forceinline__ uint4 next_lane(uint4 v) {
+    return make_uint4(__shfl_down_sync(0xffffffffu, v.x, 1), __shfl_down_sync(0xffffffffu, v.y, 1), __shfl_down_sync(0xffffffffu, v.z, 1), 0);
+  }
+  static __device__ __forceinline__ uint4 of_lane(uint4 v, int l) {
+    return make_uint4(__shfl_sync(0xffffffffu, v.x, l), __shfl_sync(0xffffffffu, v.y, l), __shfl_sync(0xffffffffu, v.z, l), 0);
+  }
+  static __device__ __forceinline__ uint4 join(uint4 v, uint4 n, int lead) {
+    if (lead & 2) { v = make_uint4(v.z, v.w, n.x, n.y); n.x = n.z; }
+    if (lead & 1) v = make_uint4(v.y, v.z, v.w, n.x);
+    return v;
+  }
+};
+// In two steps, so that the loads of several such pieces are in flight together.  i0: the first lane's first element; left: how
+// many elements the tensor has from it on (what is behind them reads as 0, what is behind the piece as it is: the caller masks).
+// First every lane's vector, and by some lane the one behind the last lane's; then, by the whole warp, the elements.
+template <int DT> __device__ __forceinline__ typename Quad<DT>::Vec vector_from(const void* p, size_t i0, long long left, int at) {
+  const int lead = (int)(i0 & 3);
+  const char* q = static_cast<const char*>(p) + (i0 - lead + 4 * at) * (DT == DRAGON_F32 ? 4 : 2);
+  if (left >= 132) return __ldg(reinterpret_cast<const typename Quad<DT>::Vec*>(q));
+  const int room = (int)left + lead - 4 * at;        // elements from this vector on
+  return room >= 4 ? __ldg(reinterpret_cast<const typename Quad<DT>::Vec*>(q)) : Quad<DT>::part(q, room);
+}
+template <int DT> __device__ __forceinline__ Quad<DT> quads_of(typename Quad<DT>::Vec own, typename Quad<DT>::Vec behind, int holder, size_t i0, int lane) {
+  Quad<DT> q;
+  typename Quad<DT>::Vec next = Quad<DT>::next_lane(own), last = Quad<DT>::of_lane(behind, holder);
+  q.u = Quad<DT>::join(own, lane == 31 ? last : next, (int)(i0 & 3));
+  return q;
+}
+// Four bytes for each lane, likewise; the first n of the warp's 128 are written.
+__device__ __forceinline__ void store_byte_quads(unsigned char* p, size_t i0, int n, unsigned w, int lane) {
+  const int lead = (int)(i0 & 3), first = 4 * lane - lead;         // of the aligned word of this lane, counted from i0
+  unsigned char* at = p + i0;
+  if (lead == 0 && n == 128) { *reinterpret_cast<unsigned*>(at + first) = w; return; }
+  const unsigned before = __shfl_up_sync(0xffffffffu, w, 1), head = __shfl_sync(0xffffffffu, w, 0), tail = __shfl_sync(0xffffffffu, w, 31);
+  const unsigned word = __funnelshift_l(before, w, 8 * lead);
+  // the first 4 - lead bytes and the last lead ones are no whole word: one byte each for four lanes
+  const int edge = lane < 4 - lead ? lane : 124 + lane;
+  if (lane < 4 && edge < n) at[edge] = (unsigned char)((edge < 4 ? head : tail) >> (8 * lane));
+  if (lane == 0) return;
+  if (first + 4 <= n) *reinterpret_cast<unsigned*>(at + first) = word;
+  else
+    for (int e = 0; first + e < n; ++e) at[first + e] = (unsigned char)(word >> (8 * e));
+}
+template <int DT> __device__ __forceinline__ unsigned largest_magnitude(const Quad<DT>& q, int n) {      // of its first n elements
+  float v[4];
+  q.get(v);
+  if (n >= 4) return max(max(magnitude(v[0]), magnitude(v[1])), max(magnitude(v[2]), magnitude(v[3])));
+  unsigned m = 0;
+#pragma unroll
+  for (int e = 0; e < 3; ++e)
+    if (e < n) m = max(m, magnitude(v[e]));
+  return m;
+}
+template <int DT> __device__ __forceinline__ unsigned e4m3_of(const Quad<DT>& q, float inv) {
+  float v[4];
+  q.get(v);
+  return e4m3_pair(v[0] * inv, v[1] * inv) | (e4m3_pair(v[2] * inv, v[3] * inv) << 16);
+}
+
 }  // namespace dragon

@@ -383,32 +383,53 @@ struct QuantArgs {
   int* status_clear;
 };
 
-// 1 x 128 blocks, or given scales of either kind: a warp per block of a row, four elements a lane
+// 1 x 128 blocks, or given scales of either kind, in rows of any length: a warp per block of a row, four elements a lane, four
+// blocks in flight (their scales as below).
+constexpr int kTogether = 4;
+template <int DT>
 __global__ void __launch_bounds__(256) quant_row_kernel(const QuantArgs a) {
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
   const int lane = threadIdx.x & 31;
-  for (long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); i < a.n_blocks; i += (long long)gridDim.x * 8) {
-    const long long row = i / a.col_blocks;
-    const int b = (int)(i - row * a.col_blocks);
-    const size_t base = (size_t)row * a.cols;
-    float v[4];
-    unsigned m = 0;
+  const long long total = (long long)a.rows * a.cols;
+  for (long long first = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * kTogether; first < a.n_blocks; first += (long long)gridDim.x * 8 * kTogether) {
+    typename Quad<DT>::Vec own[kTogether], behind = {};
+    Quad<DT> raw[kTogether];
+    size_t at[kTogether];
+    int n[kTogether];
+    float s = 1.f;
+    long long row = first >> 31 ? first / a.col_blocks : (long long)((unsigned)first / (unsigned)a.col_blocks);
+    int b = (int)(first - row * a.col_blocks);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = b * 128 + e * 32 + lane;
-      v[e] = 0.f;
-      if (j < a.cols) load_any<1>(a.x, a.xdt, base + j, &v[e]);
-      m = max(m, magnitude(v[e]));
+    for (int k = 0; k < kTogether; ++k, ++b) {
+      if (b == a.col_blocks) { b = 0; ++row; }
+      n[k] = 0;
+      at[k] = 0;
+      own[k] = {};
+      if (first + k >= a.n_blocks) continue;
+      at[k] = (size_t)row * a.cols + (size_t)b * 128;
+      n[k] = min(128, a.cols - b * 128);
+      own[k] = vector_from<DT>(a.x, at[k], total - (long long)at[k], lane);
+      if (lane == k) behind = vector_from<DT>(a.x, at[k], total - (long long)at[k], 32);
+      if (a.s_in && lane % kTogether == k) s = __ldg(a.s_in + (size_t)(a.block_rows == 1 ? row : row >> 7) * a.col_blocks + b);
     }
-    float s;
-    if (a.s_in) s = __ldg(a.s_in + (size_t)(row / a.block_rows) * a.col_blocks + b);
-    else s = scale_of(__reduce_max_sync(0xffffffffu, m));
-    if (a.s && lane == 0) a.s[i] = s;
+#pragma unroll
+    for (int k = 0; k < kTogether; ++k) raw[k] = quads_of<DT>(own[k], behind, k, at[k], lane);
+    if (!a.s_in) {
+      unsigned m = 0;
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) {
+        const unsigned mk = __reduce_max_sync(0xffffffffu, n[k] ? largest_magnitude(raw[k], n[k] - 4 * lane) : 0);
+        if (lane % kTogether == k) m = mk;
+      }
+      s = scale_of(m);
+    }
+    if (a.s && lane < kTogether && first + lane < a.n_blocks) a.s[first + lane] = s;
+    if (!a.q) continue;
     const float inv = __frcp_rn(s);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = b * 128 + e * 32 + lane;
-      if (a.q && j < a.cols) a.q[base + j] = e4m3_of(v[e] * inv);
+    for (int k = 0; k < kTogether; ++k) {
+      const float inv_k = __shfl_sync(0xffffffffu, inv, k);
+      if (n[k]) store_byte_quads(a.q, at[k], n[k], e4m3_of(raw[k], inv_k), lane);
     }
   }
 }
@@ -417,7 +438,7 @@ __global__ void __launch_bounds__(256) quant_row_kernel(const QuantArgs a) {
 // flight, whose scales (two correctly rounded divisions each) are computed by as many lanes at once.  kWhole: the length is a
 // multiple of 128, so block i is elements 128 i .. 128 i + 127 of the tensor.  16384 x 4096 bf16: 47 us (4.3 TB/s), with persistent
 // CTAs and a division per lane 61; bound by instructions.
-constexpr int kTogether = 4, kQuantBlocks = 16 * kTogether;      // blocks of a CTA
+constexpr int kQuantBlocks = 16 * kTogether;      // blocks of a CTA
 template <int DT, bool kWhole>
 __global__ void __launch_bounds__(256, 4) quant_row_vec_kernel(const QuantArgs a) {
   if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
@@ -472,52 +493,69 @@ __global__ void __launch_bounds__(256, 4) quant_row_vec_kernel(const QuantArgs a
   }
 }
 
-// 128 x 128 blocks (8192 x 8192 bf16: 38 us, 5.3 TB/s): a CTA per block, which stays in registers between the maximum and the rounding.  V = 8: 16 lanes a row,
-// 16 rows at a time; V = 1 (rows that are not 16-byte aligned): a warp a row, four elements a lane.
-template <int DT, int V>
-__global__ void __launch_bounds__(256) quant_tile_kernel(const QuantArgs a) {
-  constexpr int kLanes = V == 8 ? 16 : 32, kCells = V == 8 ? 1 : 4, kPer = 128 * kLanes / 256;     // rows per thread
-  __shared__ unsigned sh[8];
-  if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
-  const int lane = threadIdx.x % kLanes, line = threadIdx.x / kLanes;
-  const long long tile_row = blockIdx.x / a.col_blocks;
-  const int b = (int)(blockIdx.x - tile_row * a.col_blocks);
-  Raw<DT, V> raw[kPer][kCells];
-  auto inside = [&](int i, int e) { return tile_row * 128 + i * (256 / kLanes) + line < a.rows && b * 128 + (e * kLanes + lane) * V < a.cols; };
-  auto place = [&](int i, int e) { return (size_t)(tile_row * 128 + i * (256 / kLanes) + line) * a.cols + b * 128 + (e * kLanes + lane) * V; };
-#pragma unroll
-  for (int i = 0; i < kPer; ++i)
-#pragma unroll
-    for (int e = 0; e < kCells; ++e)
-      if (inside(i, e)) raw[i][e].load(a.x, a.xdt, place(i, e));
-  unsigned m = 0;
-#pragma unroll
-  for (int i = 0; i < kPer; ++i)
-#pragma unroll
-    for (int e = 0; e < kCells; ++e)
-      if (inside(i, e)) {
-        float v[V];
-        raw[i][e].get(v);
-#pragma unroll
-        for (int k = 0; k < V; ++k) m = max(m, magnitude(v[k]));
-      }
+// 128 x 128 blocks (8192 x 8192 bf16: 38 us, 5.3 TB/s): a CTA per block, which stays in registers between the maximum and the
+// rounding.  kVec: 16 lanes a row, 8 elements a lane, 16 rows at a time; otherwise (rows that are not 16-byte aligned) a warp a
+// row, four elements a lane.
+__device__ __forceinline__ float tile_scale(unsigned m, unsigned* sh) {
   m = __reduce_max_sync(0xffffffffu, m);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, sh[i]);
-  const float s = scale_of(m), inv = __frcp_rn(s);
-  if (a.s && threadIdx.x == 0) a.s[blockIdx.x] = s;
-  if (!a.q) return;
+  return scale_of(m);
+}
+template <int DT, bool kVec>
+__global__ void __launch_bounds__(256) quant_tile_kernel(const QuantArgs a) {
+  constexpr int kLanes = kVec ? 16 : 32, kPer = 128 * kLanes / 256;     // rows per thread
+  __shared__ unsigned sh[8];
+  if (a.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *a.status_clear = 0;
+  const int lane = threadIdx.x % kLanes, line = threadIdx.x / kLanes;
+  const long long tile_row = blockIdx.x / a.col_blocks;
+  const int b = (int)(blockIdx.x - tile_row * a.col_blocks);
+  const int rows = (int)min(128LL, a.rows - tile_row * 128), cols = min(128, a.cols - b * 128);      // of this block
+  const size_t first = (size_t)tile_row * 128 * a.cols + (size_t)b * 128;
+  unsigned m = 0;
+  if constexpr (kVec) {
+    Raw<DT, 8> raw[kPer];
+    const bool in = lane * 8 < cols;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i)
+    for (int i = 0; i < kPer; ++i)
+      if (in && i * 16 + line < rows) raw[i].load(a.x, a.xdt, first + (size_t)(i * 16 + line) * a.cols + lane * 8);
 #pragma unroll
-    for (int e = 0; e < kCells; ++e)
-      if (inside(i, e)) {
-        float v[V];
-        raw[i][e].get(v);
-        store_e4m3<V>(a.q + place(i, e), v, inv);
+    for (int i = 0; i < kPer; ++i)
+      if (in && i * 16 + line < rows) m = max(m, largest_magnitude(raw[i]));
+    const float s = tile_scale(m, sh), inv = __frcp_rn(s);
+    if (a.s && threadIdx.x == 0) a.s[blockIdx.x] = s;
+    if (!a.q) return;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (in && i * 16 + line < rows) {
+        float v[8];
+        raw[i].get(v);
+        store_e4m3<8>(a.q + first + (size_t)(i * 16 + line) * a.cols + lane * 8, v, inv);
       }
+  } else {
+    Quad<DT> raw[kPer];
+    typename Quad<DT>::Vec behind = {};
+    const long long total = (long long)a.rows * a.cols;
+    auto place = [&](int i) { return first + (size_t)(i * 8 + line) * a.cols; };
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i * 8 + line < rows) raw[i].u = vector_from<DT>(a.x, place(i), total - (long long)place(i), lane);
+    if (lane < kPer && lane * 8 + line < rows) behind = vector_from<DT>(a.x, place(lane), total - (long long)place(lane), 32);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i * 8 + line < rows) {
+        raw[i] = quads_of<DT>(raw[i].u, behind, i, place(i), lane);
+        m = max(m, largest_magnitude(raw[i], cols - 4 * lane));
+      }
+    const float s = tile_scale(m, sh), inv = __frcp_rn(s);
+    if (a.s && threadIdx.x == 0) a.s[blockIdx.x] = s;
+    if (!a.q) return;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i * 8 + line < rows) store_byte_quads(a.q, place(i), cols, e4m3_of(raw[i], inv), lane);
+  }
 }
 
 }  // namespace
@@ -582,8 +620,8 @@ cudaError_t launch_quant(const StepRun& r) {
   if (a.block_rows == 128 && !a.s_in) {
     const int64_t tiles = (sh.d[0] + 127) / 128 * a.col_blocks;
     if (tiles > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
-    if (vec) f32 ? quant_tile_kernel<DRAGON_F32, 8><<<(unsigned)tiles, 256, 0, st>>>(a) : quant_tile_kernel<DRAGON_BF16, 8><<<(unsigned)tiles, 256, 0, st>>>(a);
-    else f32 ? quant_tile_kernel<DRAGON_F32, 1><<<(unsigned)tiles, 256, 0, st>>>(a) : quant_tile_kernel<DRAGON_BF16, 1><<<(unsigned)tiles, 256, 0, st>>>(a);
+    if (vec) f32 ? quant_tile_kernel<DRAGON_F32, true><<<(unsigned)tiles, 256, 0, st>>>(a) : quant_tile_kernel<DRAGON_BF16, true><<<(unsigned)tiles, 256, 0, st>>>(a);
+    else f32 ? quant_tile_kernel<DRAGON_F32, false><<<(unsigned)tiles, 256, 0, st>>>(a) : quant_tile_kernel<DRAGON_BF16, false><<<(unsigned)tiles, 256, 0, st>>>(a);
     return cudaGetLastError();
   }
   a.n_blocks = (long long)sh.d[0] * a.col_blocks;
@@ -592,7 +630,8 @@ cudaError_t launch_quant(const StepRun& r) {
     if (a.cols % 128 == 0) f32 ? quant_row_vec_kernel<DRAGON_F32, true><<<grid, 256, 0, st>>>(a) : quant_row_vec_kernel<DRAGON_BF16, true><<<grid, 256, 0, st>>>(a);
     else f32 ? quant_row_vec_kernel<DRAGON_F32, false><<<grid, 256, 0, st>>>(a) : quant_row_vec_kernel<DRAGON_BF16, false><<<grid, 256, 0, st>>>(a);
   } else {
-    quant_row_kernel<<<(unsigned)std::min<long long>((a.n_blocks + 7) / 8, (long long)r.sm_count * 8), 256, 0, st>>>(a);
+    const unsigned grid = (unsigned)std::min<long long>((a.n_blocks + 8 * kTogether - 1) / (8 * kTogether), 0x7fffffffLL);
+    f32 ? quant_row_kernel<DRAGON_F32><<<grid, 256, 0, st>>>(a) : quant_row_kernel<DRAGON_BF16><<<grid, 256, 0, st>>>(a);
   }
   return cudaGetLastError();
 }
