@@ -384,7 +384,8 @@ struct QuantArgs {
 };
 
 // 1 x 128 blocks, or given scales of either kind, in rows of any length: a warp per block of a row, four elements a lane, four
-// blocks in flight (their scales as below).
+// blocks in flight (their scales as below).  8192 x 8191 bf16: 112 us (46 for 8192 columns), element by element 186; bound by
+// instructions (vectors joined across lanes, edges written by themselves).
 constexpr int kTogether = 4;
 template <int DT>
 __global__ void __launch_bounds__(256) quant_row_kernel(const QuantArgs a) {
@@ -495,7 +496,7 @@ __global__ void __launch_bounds__(256, 4) quant_row_vec_kernel(const QuantArgs a
 
 // 128 x 128 blocks (8192 x 8192 bf16: 38 us, 5.3 TB/s): a CTA per block, which stays in registers between the maximum and the
 // rounding.  kVec: 16 lanes a row, 8 elements a lane, 16 rows at a time; otherwise (rows that are not 16-byte aligned) a warp a
-// row, four elements a lane.
+// row, four elements a lane: 8192 x 8191 84 us, element by element 407.
 __device__ __forceinline__ float tile_scale(unsigned m, unsigned* sh) {
   m = __reduce_max_sync(0xffffffffu, m);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
