@@ -166,15 +166,15 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_loop_kernel(const NormArg
     return a.sum_dt == DRAGON_BF16 ? bf16_rounded(h) : h;
   };
   float2 sum = make_float2(0.f, 0.f);
-  for (int j = threadIdx.x; j < a.cols; j += kMaxRowThreads) {
+  for (int j = threadIdx.x; j < a.cols; j += blockDim.x) {
     const float h = sum_at(j);
     if (a.h) store_any<1>(a.h, a.sum_dt, base + j, &h);
     sum.x += h * h;
   }
-  sum = row_sum2(sum, kMaxRowThreads, sh);
+  sum = row_sum2(sum, blockDim.x, sh);
   const float rstd = rsqrtf(sum.x / (float)a.cols + a.eps);
   const int lane = threadIdx.x & 31, n_blocks = (a.cols + 127) / 128;
-  for (int b = threadIdx.x >> 5; b < n_blocks; b += kMaxRowThreads / 32) {
+  for (int b = threadIdx.x >> 5; b < n_blocks; b += blockDim.x >> 5) {
     float y[4];
     unsigned m = 0;
 #pragma unroll
@@ -213,7 +213,8 @@ struct NormBwdArgs {
 };
 
 // Persistent: a row slot (the threads of one row) walks the rows with the grid's stride, so that every thread keeps the
-// running sums of dg for its own columns and writes them once.  DT: the type of h and dy (-1: they differ), SDT: that of
+// running sums of dg for its own columns; a CTA's slots (short rows: up to 16) add theirs in their order and write one partial
+// row, so that two CTAs an SM leave no more than 296 for the sum that follows (14500 x 60: 61 us with a row for every slot, 17 so).  DT: the type of h and dy (-1: they differ), SDT: that of
 // the residual branch's gradient (-2: none).
 template <int DT, int SDT, int V, int PER> constexpr int norm_bwd_ctas() { return V * PER <= 8 ? 2 : 1; }      // of 512 threads, by registers
 template <int DT, int SDT, int V, int PER>
@@ -288,12 +289,26 @@ __global__ void __launch_bounds__(kMaxRowThreads, norm_bwd_ctas<DT, SDT, V, PER>
       }
     }
   }
-  if (a.part) {
+  if (a.part && rows_per_cta == 1) {
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
       const int j = (t + k * a.threads) * V;
-      if (j < a.cols) store_any<V>(a.part, DRAGON_F32, (size_t)slot * a.cols + j, dg[k]);
+      if (j < a.cols) store_any<V>(a.part, DRAGON_F32, (size_t)blockIdx.x * a.cols + j, dg[k]);
     }
+  } else if (a.part) {
+    extern __shared__ float total[];               // cols
+    for (int s = 0; s < rows_per_cta; ++s) {
+      if (slot_in == s)
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+          const int j = (t + k * a.threads) * V;
+          if (j < a.cols)
+#pragma unroll
+            for (int e = 0; e < V; ++e) total[j + e] = s ? total[j + e] + dg[k][e] : dg[k][e];
+        }
+      __syncthreads();
+    }
+    for (int j = threadIdx.x; j < a.cols; j += blockDim.x) a.part[(size_t)blockIdx.x * a.cols + j] = total[j];
   }
 }
 
@@ -334,7 +349,13 @@ __global__ void __launch_bounds__(kMaxRowThreads) norm_bwd_loop_kernel(const Nor
   }
 }
 
-// row slots of the gradient's grid: enough CTAs to fill the SMs at the kernel's occupancy
+// the gradient's CTAs take as many rows as fit 512 threads where rows are short; enough CTAs to fill the SMs at the kernel's
+// occupancy
+RowShape norm_bwd_shape(int64_t rows, int64_t cols) {
+  RowShape s = row_shape(rows, cols);
+  s.rows = s.threads <= 128 ? kMaxRowThreads / s.threads : 1;
+  return s;
+}
 int norm_bwd_grid(int64_t rows, const RowShape& s, int sm_count) {
   const int64_t ctas = (rows + s.rows - 1) / s.rows;
   const int per_sm = std::max(1, (s.vec * s.per <= 8 ? 1024 : 512) / (s.threads * s.rows));
@@ -359,16 +380,17 @@ cudaError_t launch_norm_typed(const NormArgs& a, const RowShape& s, int grid, cu
 template <int DT, int SDT>
 cudaError_t launch_norm_bwd_typed(const NormBwdArgs& a, const RowShape& s, int grid, cudaStream_t st) {
   const int block = s.threads * s.rows;
+  const size_t smem = s.rows > 1 ? (size_t)a.cols * sizeof(float) : 0;      // (at most 16 KB)
   if (s.vec == 2) {
-    if (s.per == 2) norm_bwd_kernel<DT, SDT, 2, 2><<<grid, block, 0, st>>>(a);
-    else norm_bwd_kernel<DT, SDT, 2, 8><<<grid, block, 0, st>>>(a);
+    if (s.per == 2) norm_bwd_kernel<DT, SDT, 2, 2><<<grid, block, smem, st>>>(a);
+    else norm_bwd_kernel<DT, SDT, 2, 8><<<grid, block, smem, st>>>(a);
   } else if (s.vec == 1) {
-    if (s.per == 2) norm_bwd_kernel<DT, SDT, 1, 2><<<grid, block, 0, st>>>(a);
-    else if (s.per == 8) norm_bwd_kernel<DT, SDT, 1, 8><<<grid, block, 0, st>>>(a);
-    else norm_bwd_kernel<DT, SDT, 1, 16><<<grid, block, 0, st>>>(a);
-  } else if (s.per == 1) norm_bwd_kernel<DT, SDT, 8, 1><<<grid, block, 0, st>>>(a);
-  else if (s.per == 2) norm_bwd_kernel<DT, SDT, 8, 2><<<grid, block, 0, st>>>(a);
-  else norm_bwd_kernel<DT, SDT, 8, 4><<<grid, block, 0, st>>>(a);
+    if (s.per == 2) norm_bwd_kernel<DT, SDT, 1, 2><<<grid, block, smem, st>>>(a);
+    else if (s.per == 8) norm_bwd_kernel<DT, SDT, 1, 8><<<grid, block, smem, st>>>(a);
+    else norm_bwd_kernel<DT, SDT, 1, 16><<<grid, block, smem, st>>>(a);
+  } else if (s.per == 1) norm_bwd_kernel<DT, SDT, 8, 1><<<grid, block, smem, st>>>(a);
+  else if (s.per == 2) norm_bwd_kernel<DT, SDT, 8, 2><<<grid, block, smem, st>>>(a);
+  else norm_bwd_kernel<DT, SDT, 8, 4><<<grid, block, smem, st>>>(a);
   return cudaGetLastError();
 }
 
@@ -562,9 +584,9 @@ __global__ void __launch_bounds__(256) quant_tile_kernel(const QuantArgs a) {
 }  // namespace
 
 int norm_bwd_partials(int64_t rows, int64_t cols, int sm_count) {
-  const RowShape s = row_shape(rows, cols);
+  const RowShape s = norm_bwd_shape(rows, cols);
   if (!s.in_registers) return (int)std::min<int64_t>(rows, (int64_t)sm_count * 2);
-  return norm_bwd_grid(rows, s, sm_count) * s.rows;
+  return norm_bwd_grid(rows, s, sm_count);
 }
 
 cudaError_t launch_norm(const StepRun& r) {
@@ -575,7 +597,7 @@ cudaError_t launch_norm(const StepRun& r) {
              (float)r.s.attr, r.status_clear};
   const RowShape s = row_shape(a.rows, a.cols);
   if (!s.in_registers || (s.vec != 8 && (a.s || a.q))) {
-    norm_loop_kernel<<<a.rows, kMaxRowThreads, 0, st>>>(a);
+    norm_loop_kernel<<<a.rows, std::min(kMaxRowThreads, (a.cols + 127) / 128 * 32), 0, st>>>(a);
     return cudaGetLastError();
   }
   a.threads = s.threads;
@@ -595,7 +617,7 @@ cudaError_t launch_norm_bwd(const StepRun& r) {
   NormBwdArgs a{r.rd(nb::H), r.rd(nb::DY), r.rd(nb::GAIN), r.rd(nb::SKIP), r.wr(nb::DH), dg ? reinterpret_cast<float*>(r.ws + r.s.colpart_off) : nullptr,
                 r.rd_type(nb::H), r.rd_type(nb::DY), r.rd_type(nb::GAIN), r.rd_type(nb::SKIP), r.wr_type(nb::DH), (int)sh.rows(), (int)sh.cols(), 0,
                 (float)r.s.attr, r.status_clear};
-  const RowShape s = row_shape(a.rows, a.cols);
+  const RowShape s = norm_bwd_shape(a.rows, a.cols);
   cudaError_t e;
   if (!s.in_registers) {
     norm_bwd_loop_kernel<<<(int)std::min<int64_t>(a.rows, (int64_t)r.sm_count * 2), kMaxRowThreads, 0, st>>>(a);
