@@ -585,21 +585,49 @@ cudaError_t allow_smem(const void* kern, size_t bytes, int variant) {
   return e;
 }
 
+struct FewConfig {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  FewConfig(int nt, dim3 grid, cudaStream_t st) {
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(few_threads(nt));
+    cfg.dynamicSmemBytes = few_smem(nt);
+    cfg.stream = st;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = grid.z;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+  }
+};
+// How many CTAs in clusters of `split` the GPU holds at once: fewer than its SMs suggest, as a cluster stays inside one group
+// of SMs (16 clusters of 8 do not fit: 2025 x 64 x 2912 took two waves, 30 us for 16)
+template <int NT> int few_capacity(int split, int sm_count) {
+  static std::mutex mu;
+  static int known[64][4] = {};
+  const int at = split == 1 ? 0 : split == 2 ? 1 : split == 4 ? 2 : 3;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  std::lock_guard<std::mutex> lock(mu);
+  if (!known[dev][at]) {
+    FewConfig c(NT, dim3(1, 1, split), nullptr);
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, gemm_e4m3_few_kernel<NT>, &c.cfg) != cudaSuccess || clusters < 1) {
+      (void)cudaGetLastError();
+      clusters = few_ctas(NT) * sm_count / split;
+    }
+    known[dev][at] = clusters * split;
+  }
+  return known[dev][at];
+}
+
 template <int NT>
-cudaError_t launch_few(const CUtensorMap& tx, const CUtensorMap& tw, const Gemm8Args& g, int variant, cudaStream_t st) {
+cudaError_t launch_few(const CUtensorMap& tx, const CUtensorMap& tw, Gemm8Args g, int variant, int sm_count, cudaStream_t st) {
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(gemm_e4m3_few_kernel<NT>), few_smem(NT), variant);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((g.N + 127) / 128, (g.M + NT - 1) / NT, g.split);
-  cfg.blockDim = dim3(few_threads(NT));
-  cfg.dynamicSmemBytes = few_smem(NT);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = g.split;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, gemm_e4m3_few_kernel<NT>, tx, tw, g);
+  const int64_t ctas = (int64_t)((g.N + 127) / 128) * ((g.M + NT - 1) / NT);
+  while (g.split < 8 && g.kb >= 4 * g.split && ctas * g.split * 2 <= few_capacity<NT>(2 * g.split, sm_count)) g.split *= 2;
+  FewConfig c(NT, dim3((g.N + 127) / 128, (g.M + NT - 1) / NT, g.split), st);
+  return cudaLaunchKernelEx(&c.cfg, gemm_e4m3_few_kernel<NT>, tx, tw, g);
 }
 template <bool kF32, bool kLines>
 cudaError_t launch_pairs(const CUtensorMap& tx, const CUtensorMap& tw, const Gemm8Args& g, int pairs, int variant, cudaStream_t st) {
@@ -645,10 +673,8 @@ int launch_gemm_e4m3(const StepRun& r) {
   }
   cudaError_t e;
   if (few) {
-    const int64_t ctas = (int64_t)((g.N + 127) / 128) * ((g.M + nt - 1) / nt);
-    while (g.split < 8 && ctas * g.split * 2 <= few_ctas(nt) * r.sm_count && g.kb >= 4 * g.split) g.split *= 2;
-    e = nt == 16 ? launch_few<16>(tx, tw, g, 1, st) : nt == 32 ? launch_few<32>(tx, tw, g, 2, st)
-        : nt == 64 ? launch_few<64>(tx, tw, g, 3, st) : launch_few<128>(tx, tw, g, 4, st);
+    e = nt == 16 ? launch_few<16>(tx, tw, g, 1, r.sm_count, st) : nt == 32 ? launch_few<32>(tx, tw, g, 2, r.sm_count, st)
+        : nt == 64 ? launch_few<64>(tx, tw, g, 3, r.sm_count, st) : launch_few<128>(tx, tw, g, 4, r.sm_count, st);
   } else {
     const bool lines = g.N % (g.ydt == DRAGON_F32 ? 4 : 8) == 0;
     if (g.ydt == DRAGON_F32) e = lines ? launch_pairs<true, true>(tx, tw, g, pairs, 0, st) : launch_pairs<true, false>(tx, tw, g, pairs, 5, st);
