@@ -17,8 +17,9 @@
 //                         release before the last sums (no gain).
 //   gemm_e4m3_few_kernel  few rows: the operands change places (128 rows of W x 16..128 rows of X), so that the tile's height is
 //                         filled by weights and hardly any product is wasted; the K blocks of a tile are split over the
-//                         CTAs of a cluster, whose partial sums meet in shared memory in a fixed order.  5 rows of 8192 x 4096: 8.7 us by itself for
-//                         34 MB of weights (5.1 at the measured bandwidth); 256 x 8192 x 16384: a block 0.5 us, copies out of L2
+//                         CTAs of a cluster, whose partial sums meet in shared memory in a fixed order.  5 x 8192 x 4096: 11.3 us, one call
+//                         after another (34 MB of weights: 5.1 us at the measured bandwidth; the rest is the first bytes' latency
+//                         and the join); 256 x 8192 x 16384: a block 0.5 us, copies out of L2
 // Every wait is bounded; when one runs out the kernel records DRAGON_ERR_TIMEOUT, lets its copies and products in flight
 // land, frees its TMEM and returns.
 #include <algorithm>
@@ -600,7 +601,7 @@ struct FewConfig {
   }
 };
 // How many CTAs in clusters of `split` the GPU holds at once: fewer than its SMs suggest, as a cluster stays inside one group
-// of SMs (16 clusters of 8 do not fit: 2025 x 64 x 2912 took two waves, 30 us for 16)
+// of SMs (16 clusters of 8 CTAs of an SM each do not fit: 2025 x 64 x 2912 took 30 us in two waves, in clusters of 4 16 us)
 template <int NT> int few_capacity(int split, int sm_count) {
   static std::mutex mu;
   static int known[64][4] = {};
@@ -627,7 +628,10 @@ cudaError_t launch_few(const CUtensorMap& tx, const CUtensorMap& tw, Gemm8Args g
   const int64_t ctas = (int64_t)((g.N + 127) / 128) * ((g.M + NT - 1) / NT);
   // eight parts pay for their join only where a tile is small: 1 x 512 x 4096 10.8 us for 12.2 with four, 128 x 128 x 2912 16.8 for 14.4
   const int most = NT == 128 ? 4 : 8;
-  while (g.split < most && g.kb >= 4 * g.split && ctas * g.split * 2 <= few_capacity<NT>(2 * g.split, sm_count)) g.split *= 2;
+  // where an SM holds one CTA all clusters must find room, a second wave costs more than longer parts; where it holds two, the
+  // clusters that do not fit start beside others (5 x 8192 x 4096: 64 clusters of 4 11.3 us, of 2 12.3)
+  auto room = [&](int split) { return few_ctas(NT) == 1 ? few_capacity<NT>(split, sm_count) : few_ctas(NT) * sm_count; };
+  while (g.split < most && g.kb >= 4 * g.split && ctas * g.split * 2 <= room(2 * g.split)) g.split *= 2;
   FewConfig c(NT, dim3((g.N + 127) / 128, (g.M + NT - 1) / NT, g.split), st);
   return cudaLaunchKernelEx(&c.cfg, gemm_e4m3_few_kernel<NT>, tx, tw, g);
 }
