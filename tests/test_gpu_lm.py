@@ -19,7 +19,7 @@ def close(got, want, bound, dtype, what):
 
 
 NORM_SIZES = [(1, 1), (3, 7), (2, 8), (5, 96), (4, 128), (9, 250), (130, 1000), (7, 1001), (600, 136), (3, 4096), (2, 5000), (2, 8200), (3, 8195),
-              (2, 16384), (2, 16392), (1, 20001)]
+              (2, 16384), (2, 16392), (1, 20001), (9700, 40)]
 # rstd: a sum of squares in at most 32 terms a thread and a tree (each rounding halved by the root), rsqrt to 2 units, two products
 NORM_REL = 32 * U32
 
