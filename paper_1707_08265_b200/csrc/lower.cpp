@@ -221,7 +221,11 @@ struct Lowerer {
     const int v = fval[t];
     if (fetch_of[t] >= 0 && vals[v].kind == VK_OP && (dtype < 0 || dtype == g.tensors[t].dtype))
       for (const Item& s : items)      // a fetched tensor's buffer is an image of it
-        if (s.kind == IT_MOP && s.opc == M_STORE && s.a == v && plan->mems[s.mem].where == MEM_FETCH) return s.mem;
+        if (s.kind == IT_MOP && s.opc == M_STORE && s.a == v && plan->mems[s.mem].where == MEM_FETCH) {
+          // recorded like any other image: from now on somebody reads it, so its store stays where it is (sum_in_memory)
+          materialised[{v, g.tensors[t].dtype}] = s.mem;
+          return s.mem;
+        }
     return materialise(v, dtype, g.tensors[t].dtype);
   }
   // the item of the given kind that writes memory m at position pos of its results, or null
@@ -556,6 +560,7 @@ bool join_domain(Shape* dom, bool* has_dom, const Shape& s) {
 }  // namespace
 
 static size_t share_workspace(Plan* plan, size_t off);
+static bool reads_follow_writes(const Plan& plan);
 
 // per operand of a VM program: position (index into the code) of its last load and of its first store
 std::vector<VmAccess> vm_operand_accesses(const VmSegment& sg) {
@@ -1153,6 +1158,8 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     if (rc) return rc;
   }
 
+  if (!reads_follow_writes(*plan)) return DRAGON_ERR_UNSUPPORTED;
+
   // workspace layout: the status word, live workspace tensors, then per-segment scratch
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
@@ -1185,6 +1192,50 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
   return DRAGON_OK;
 }
 
+// The memory that a step reads and writes, reads first (acc: vm_operand_accesses of a VM step's program)
+template <typename Fn> static void for_each_access(const Plan& plan, int si, const std::vector<VmAccess>& acc, Fn&& fn) {
+  const Step& st = plan.steps[si];
+  auto touch = [&](int m, bool w) { if (m >= 0) fn(m, w); };
+  if (st.kind != ST_VM) {
+    touch(st.mA, false); touch(st.mB, false);
+    if (st.kind == ST_SCE_BWD || st.kind == ST_GEMM) touch(st.mD, false);
+    if (st.kind == ST_GEMM) touch(st.mE, false);
+    if (st.kind == ST_GEMM)
+      for (const EpiSpec& e : st.epi) touch(e.mem, false);
+    for (int m : st.rd) touch(m, false);
+    if (st.kind == ST_SCE_FWD) touch(st.mD, true);
+    touch(st.mC, true);
+    touch(st.mF, true);
+    for (int m : st.wr) touch(m, true);
+    return;
+  }
+  const VmSegment& sg = plan.segs[st.seg];
+  for (size_t i = 0; i < sg.operand_mem.size(); ++i)
+    if (acc[i].last_load >= 0) touch(sg.operand_mem[i], false);
+  for (size_t i = 0; i < sg.operand_mem.size(); ++i)
+    if (acc[i].first_store < (1 << 30)) touch(sg.operand_mem[i], true);
+  for (const FinishJob& j : sg.finish) touch(j.mem, true);
+}
+
+// Whatever a step reads is a feed or has been written by a step before it.  A plan in which it is not would run on what
+// its buffers happen to hold: it is refused.
+static bool reads_follow_writes(const Plan& plan) {
+  std::vector<char> written(plan.mems.size(), 0);
+  for (int si = 0; si < (int)plan.steps.size(); ++si) {
+    std::vector<VmAccess> acc;
+    if (plan.steps[si].kind == ST_VM) acc = vm_operand_accesses(plan.segs[plan.steps[si].seg]);
+    std::vector<int> reads, writes;
+    for_each_access(plan, si, acc, [&](int m, bool w) { (w ? writes : reads).push_back(m); });
+    for (int m : reads)
+      if (plan.mems[m].where != MEM_FEED && !written[m]) {
+        set_error("internal: step %d of the plan reads memory that no step before it has written", si);
+        return false;
+      }
+    for (int m : writes) written[m] = 1;
+  }
+  return true;
+}
+
 // Memory sharing between the tensors that cross kernels (the purpose of Sec. 2.4, at the granularity of
 // plan steps).  Every workspace tensor lives from the first step that touches it to the last one.
 //  * In place (the paper's in-place structure): the output of an elementwise VM step takes the region
@@ -1197,36 +1248,16 @@ static size_t share_workspace(Plan* plan, size_t off) {
   std::vector<MemRef>& mems = plan->mems;
   const int n_steps = (int)plan->steps.size();
   std::vector<std::vector<int>> reads(n_steps), writes(n_steps);
-  auto touch = [&](int si, int m, bool w) {
-    if (m < 0 || mems[m].where != MEM_WORK || !mems[m].live) return;
-    (w ? writes : reads)[si].push_back(m);
-    if (mems[m].first_step < 0) mems[m].first_step = si;
-    mems[m].last_step = si;
-  };
   // positions of the last load and the first store of every operand of a VM program
   std::vector<std::vector<VmAccess>> acc(n_steps);
   for (int si = 0; si < n_steps; ++si) {
-    const Step& st = plan->steps[si];
-    if (st.kind != ST_VM) {
-      touch(si, st.mA, false); touch(si, st.mB, false);
-      if (st.kind == ST_SCE_BWD || st.kind == ST_GEMM) touch(si, st.mD, false);
-      if (st.kind == ST_GEMM) touch(si, st.mE, false);
-      if (st.kind == ST_GEMM)
-        for (const EpiSpec& e : st.epi) touch(si, e.mem, false);
-      if (st.kind == ST_SCE_FWD) touch(si, st.mD, true);
-      touch(si, st.mC, true);
-      touch(si, st.mF, true);
-      for (int m : st.rd) touch(si, m, false);
-      for (int m : st.wr) touch(si, m, true);
-      continue;
-    }
-    const VmSegment& sg = plan->segs[st.seg];
-    acc[si] = vm_operand_accesses(sg);
-    for (size_t i = 0; i < sg.operand_mem.size(); ++i) {
-      if (acc[si][i].last_load >= 0) touch(si, sg.operand_mem[i], false);
-      if (acc[si][i].first_store < (1 << 30)) touch(si, sg.operand_mem[i], true);
-    }
-    for (const FinishJob& j : sg.finish) touch(si, j.mem, true);
+    if (plan->steps[si].kind == ST_VM) acc[si] = vm_operand_accesses(plan->segs[plan->steps[si].seg]);
+    for_each_access(*plan, si, acc[si], [&](int m, bool w) {
+      if (mems[m].where != MEM_WORK || !mems[m].live) return;
+      (w ? writes : reads)[si].push_back(m);
+      if (mems[m].first_step < 0) mems[m].first_step = si;
+      mems[m].last_step = si;
+    });
   }
   std::vector<std::pair<size_t, size_t>> free_list;   // (offset, bytes), 256-byte granules
   auto round = [](size_t b) { return (b + 255) & ~(size_t)255; };

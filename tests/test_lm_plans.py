@@ -1,0 +1,30 @@
+"""Plans of the language-model operators among themselves and the older ones, without a GPU: what runs in which order."""
+import pytest
+
+from lm_cases import norm_graph
+from lm_mixed_cases import SUM_READERS, sum_read_before_its_norm
+from paper_1707_08265_b200 import binding as B
+
+
+def steps(desc, inputs, outputs):
+    return [s for s in B.Graph.from_desc(desc).function(inputs, outputs).describe().splitlines() if s[0] != " "]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("reader", SUM_READERS)
+def test_sum_that_is_read_before_its_norm_is_written_first(reader, dtype):
+    """The norm's kernel may write the sum in front of it only where nobody reads the sum before that kernel runs."""
+    g, inputs, outputs = sum_read_before_its_norm(reader, dtype)
+    lines = steps(g.desc, inputs, outputs)
+    assert lines[0].startswith("vm[") and lines[-1].startswith("rms_norm[") and "->sum" not in lines[-1] and "+residual" not in lines[-1]
+    # the same where the sum is not fetched
+    lines = steps(g.desc, inputs, outputs[1:])
+    assert lines[0].startswith("vm[") and "->sum" not in lines[-1] and "+residual" not in lines[-1]
+    # the reader alone is not wanted: the norm adds again
+    assert steps(g.desc, inputs, [outputs[0], outputs[-1]]) == [lines[-1].replace(" ->y", " +residual ->sum ->y")]
+
+
+def test_sum_whose_readers_come_behind_the_norm_stays_in_its_kernel():
+    g, ids, inputs, outputs = norm_graph(64, 256)
+    s = g.op("BlockScale", [ids["h"]], "s", [64, 2])
+    assert steps(g.desc, inputs, outputs + [s]) == ["rms_norm[64x256 +residual ->sum ->y]", "quantize[64x256 blocks 1x128 ->scales]"]
