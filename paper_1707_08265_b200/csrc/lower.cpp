@@ -191,6 +191,15 @@ struct Lowerer {
     return mC;
   }
 
+  // Gradient value v of a tensor of shape `want`, summed over what the tensor was broadcast along: for kernels, which take
+  // their extents from the tensor
+  int summed(int v, const Shape& want) {
+    v = widen(v, want);
+    if (vals[v].shape.numel() == want.numel()) return v;
+    const int m = new_mem(MEM_WORK, -1, DRAGON_F32, want);
+    accum(v, m);
+    return new_val(VK_MEM, want, m);
+  }
   void accumulate_grad(int s, int x, int contrib) {
     auto it = gval[s].find(x);
     if (it == gval[s].end()) gval[s][x] = contrib;
@@ -443,7 +452,10 @@ struct Lowerer {
     if (gy == gval[s].end()) return;  // no gradient reaches this operator
     // a gradient value stands for a tensor of at least the output's shape (a folded seed or a
     // scalar factor is narrower); sums over broadcast axes count every element of that shape
-    const int dy = widen(gy->second, g.tensors[o].shape);
+    int dy = widen(gy->second, g.tensors[o].shape);
+    // a kernel of its own reads dy with its output's extents: where that output is broadcast dy is summed first
+    if (op.type == DRAGON_OP_INNER_PRODUCT || op.type == DRAGON_OP_SOFTMAX_CROSS_ENTROPY || op.type == DRAGON_OP_RMS_NORM || op.type == DRAGON_OP_GATED_SCAN)
+      dy = summed(dy, g.tensors[o].shape);
     std::vector<bool> want(op.in.size(), false);
     for (size_t p = 0; p < op.in.size(); ++p)
       for (size_t q = 0; q < op.in.size(); ++q)
@@ -745,17 +757,21 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
   std::vector<std::vector<int>> seg_items;
   {
     Shape dom; bool has_dom = false; int cur = -1;
+    std::set<int> sums;      // memory that the current segment sums into: complete only behind it
+    auto reads_sum = [&](int v) { return v >= 0 && vals[v].kind == VK_MEM && sums.count(vals[v].mem) != 0; };
     for (int i = 0; i < (int)items.size(); ++i) {
       Item& it = items[i];
       if (!it.live) continue;
       if (it.kind != IT_MOP) { cur = -1; has_dom = false; continue; }
       Shape s = (it.opc == M_STORE || it.opc == M_ACCUM) ? vals[it.a].shape : vals[it.dst].shape;
-      if (cur < 0 || cuts.count(i) || !join_domain(&dom, &has_dom, s)) {
+      if (cur < 0 || cuts.count(i) || reads_sum(it.a) || reads_sum(it.b) || !join_domain(&dom, &has_dom, s)) {
         seg_items.emplace_back();
         cur = (int)seg_items.size() - 1;
         has_dom = false;
+        sums.clear();
         join_domain(&dom, &has_dom, s);
       }
+      if (it.opc == M_ACCUM) sums.insert(it.mem);
       it.segment = cur;
       seg_items[cur].push_back(i);
     }

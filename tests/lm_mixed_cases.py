@@ -36,3 +36,36 @@ def sum_read_before_its_norm(reader, dtype, rows=70, cols=264):
         read = [g.op("GatedScan", [z, h] if reader == "scan of it" else [h, z], "states", shape, dtype)]
     y = g.op("RMSNorm", [h, w], "y", shape, dtype)
     return g, inputs, [h] + read + [y]
+
+
+def broadcast_gradient(kind, dtype="f32", rows=37, cols=264):
+    """Gradients of tensors that a wider operator broadcasts: what reads them sums first.  Returns (graph, inputs, outputs)."""
+    g = wl.GraphDesc()
+    wide = g.tensor("M", [rows, cols])
+    if kind in ("norm of a vector", "norm of one row", "norm of a sum", "norm of a vector, constant"):
+        shape = [1, cols] if kind == "norm of one row" else [cols]
+        x, w = g.tensor("x", shape, dtype), g.tensor("w", [cols])
+        inputs, h = [x, w], x
+        if kind == "norm of a sum":
+            r = g.tensor("r", shape, dtype)
+            inputs.append(r)
+            h = g.op("Add", [x, r], "h", shape, dtype)
+        y = g.op("RMSNorm", [h, w], "y", shape, dtype)
+        objs = [g.op("Add" if kind.endswith("constant") else "Mul", [y, wide], "z")]
+    elif kind == "scan of one row":
+        x, gate, h0 = g.tensor("x", [1, cols], dtype), g.tensor("gate", [1, cols], dtype), g.tensor("h0", [1, cols])
+        inputs = [gate, x, h0]
+        objs = [g.op("Mul", [g.op("GatedScan", inputs, "h", [1, cols], dtype), wide], "z")]
+    elif kind == "product of one row":
+        x, w = g.tensor("x", [1, 64], "bf16"), g.tensor("w", [cols, 64], "bf16")
+        inputs = [x, w]
+        objs = [g.op("Mul", [g.op("InnerProduct", [x, w], "y", [1, cols]), wide], "z")]
+    elif kind == "loss":
+        x, labels = g.tensor("x", [6, 40]), g.tensor("labels", [6], "i32")
+        inputs = [x, labels]
+        objs = [g.op("Mul", [g.op("SoftmaxCrossEntropy", [x, labels], "loss", []), wide], "z")]
+    wrts = [t for t in inputs if g.desc["tensors"][t]["dtype"] != "i32"]
+    return g, inputs + [wide], objs + g.grad(objs, wrts)
+
+
+BROADCAST_KINDS = ("norm of a vector", "norm of one row", "norm of a sum", "norm of a vector, constant", "scan of one row", "product of one row", "loss")

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from lm_cases import U16, U32, normals, run_gpu
-from lm_mixed_cases import SUM_READERS, sum_read_before_its_norm
+from lm_mixed_cases import BROADCAST_KINDS, SUM_READERS, broadcast_gradient, sum_read_before_its_norm
 from oracle import interp
 
 pytestmark = pytest.mark.gpu
@@ -23,3 +23,21 @@ def test_sum_that_is_read_before_its_norm(reader, dtype):
         # here; a rounding to bf16 that may go the other way is a step of 2^-7 of the value at most, one to e4m3 a step of 2^-3
         step = {"f32": 0.0, "bf16": 2 * U16, "f8e4m3": 2.0 ** -3}[info["dtype"]]
         assert np.abs(a - b).max() <= (3100 * U32 + step) * np.abs(b).max(), info["name"]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", BROADCAST_KINDS)
+def test_gradient_of_a_broadcast_tensor(kind, dtype):
+    g, inputs, outputs = broadcast_gradient(kind, dtype)
+    feeds = normals(g.desc, inputs, 13)
+    for i, t in enumerate(inputs):
+        if g.desc["tensors"][t]["dtype"] == "i32":
+            feeds[i] = np.arange(6, dtype=np.int32) * 5
+    got, _ = run_gpu(g.desc, inputs, outputs, feeds)
+    want = interp.run_function(g.desc, inputs, outputs, feeds)
+    for t, a, b in zip(outputs, got, want):
+        info = g.desc["tensors"][t]
+        # of the largest value: sums of at most 10000 terms in trees of 64 or fewer roundings, and twice that for cancellation
+        # between them; every value may pass three roundings to bf16 that go the other way (of y, of dy and its own)
+        rounded = 0.0 if dtype == "f32" and kind != "product of one row" else 6 * U16
+        assert np.abs(a - b).max() <= (1000 * U32 + rounded) * max(np.abs(b).max(), 1e-30), info["name"]

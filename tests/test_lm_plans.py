@@ -2,7 +2,7 @@
 import pytest
 
 from lm_cases import norm_graph
-from lm_mixed_cases import SUM_READERS, sum_read_before_its_norm
+from lm_mixed_cases import BROADCAST_KINDS, SUM_READERS, broadcast_gradient, sum_read_before_its_norm
 from paper_1707_08265_b200 import binding as B
 
 
@@ -28,3 +28,17 @@ def test_sum_whose_readers_come_behind_the_norm_stays_in_its_kernel():
     g, ids, inputs, outputs = norm_graph(64, 256)
     s = g.op("BlockScale", [ids["h"]], "s", [64, 2])
     assert steps(g.desc, inputs, outputs + [s]) == ["rms_norm[64x256 +residual ->sum ->y]", "quantize[64x256 blocks 1x128 ->scales]"]
+
+
+@pytest.mark.parametrize("kind", BROADCAST_KINDS)
+def test_gradient_of_a_broadcast_tensor_is_summed_before_a_kernel_reads_it(kind):
+    g, inputs, outputs = broadcast_gradient(kind)
+    lines = steps(g.desc, inputs, outputs)
+    names = [s.split("[")[0] for s in lines]
+    summing = [i for i, s in enumerate(lines) if "colacc=1" in s or "scalacc=1" in s]
+    assert summing, lines
+    for i, n in enumerate(names):
+        if n in ("rms_norm_bwd", "gated_scan_bwd", "softmax_ce_bwd"):
+            assert min(summing) < i
+    if kind == "product of one row":          # no contraction over more rows than X has
+        assert [s for s in lines if s.startswith("gemm")] == ["gemm[1x264x64 -> f32]", "gemm[1x64x264 B^T -> f32]", "gemm[264x64x1 A^T B^T -> f32]"]
