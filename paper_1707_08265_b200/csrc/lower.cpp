@@ -192,7 +192,7 @@ struct Lowerer {
   }
 
   // Gradient value v of a tensor of shape `want`, summed over what the tensor was broadcast along: for kernels, which take
-  // their extents from the tensor
+  // their extents from the tensor, and for sums of contributions that do not have the same shape
   int summed(int v, const Shape& want) {
     v = widen(v, want);
     if (vals[v].shape.numel() == want.numel()) return v;
@@ -200,10 +200,17 @@ struct Lowerer {
     accum(v, m);
     return new_val(VK_MEM, want, m);
   }
+  // Contributions of one shape are added as they are.  Where shapes differ, a narrower value counts once for every element of
+  // the tensor, not for every element of the wider one: the wider one is summed first.
   void accumulate_grad(int s, int x, int contrib) {
     auto it = gval[s].find(x);
-    if (it == gval[s].end()) gval[s][x] = contrib;
-    else it->second = mop(M_ADD, it->second, contrib);
+    if (it == gval[s].end()) { gval[s][x] = contrib; return; }
+    const Shape& want = g.tensors[x].shape;
+    int a = it->second, b = contrib;
+    if (vals[a].shape != vals[b].shape)
+      for (int* v : {&a, &b})
+        if (vals[*v].shape.numel() > want.numel()) *v = summed(*v, want);
+    it->second = mop(M_ADD, a, b);
   }
 
   void store_fetch(int v, int tensor) {

@@ -56,6 +56,23 @@ def broadcast_gradient(kind, dtype="f32", rows=37, cols=264):
         x, gate, h0 = g.tensor("x", [1, cols], dtype), g.tensor("gate", [1, cols], dtype), g.tensor("h0", [1, cols])
         inputs = [gate, x, h0]
         objs = [g.op("Mul", [g.op("GatedScan", inputs, "h", [1, cols], dtype), wide], "z")]
+    elif kind == "gain of two uses":        # the gain's gradient is [cols] from the norm, [rows, cols] from the product
+        x, w = g.tensor("x", [5, cols], dtype), g.tensor("w", [cols])
+        inputs = [x, w]
+        objs = [g.op("RMSNorm", [x, w], "y", [5, cols], dtype), g.op("Mul", [wide, w], "z")]
+    elif kind == "vector of two uses":      # operators that are all in the graph VM
+        x = g.tensor("x", [cols], dtype)
+        inputs = [x]
+        objs = [g.op("Mul", [wide, x], "z"), g.op("Tanh", [x], "t")]
+    elif kind == "objective of two uses":   # an objective counts once for each of its own elements
+        x = g.tensor("x", [cols], dtype)
+        inputs = [x]
+        t = g.op("Tanh", [x], "t")
+        objs = [t, g.op("Mul", [wide, t], "z")]
+    elif kind == "scalar of two widths":    # gradients over two domains that do not broadcast against each other
+        a, v = g.tensor("a", []), g.tensor("v", [rows + 1])
+        inputs = [a, v]
+        objs = [g.op("Mul", [wide, a], "z"), g.op("Mul", [v, a], "u")]
     elif kind == "product of one row":
         x, w = g.tensor("x", [1, 64], "bf16"), g.tensor("w", [cols, 64], "bf16")
         inputs = [x, w]
@@ -68,4 +85,5 @@ def broadcast_gradient(kind, dtype="f32", rows=37, cols=264):
     return g, inputs + [wide], objs + g.grad(objs, wrts)
 
 
-BROADCAST_KINDS = ("norm of a vector", "norm of one row", "norm of a sum", "norm of a vector, constant", "scan of one row", "product of one row", "loss")
+BROADCAST_KINDS = ("norm of a vector", "norm of one row", "norm of a sum", "norm of a vector, constant", "scan of one row", "gain of two uses", "vector of two uses",
+                   "objective of two uses", "scalar of two widths", "product of one row", "loss")

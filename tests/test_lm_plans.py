@@ -4,6 +4,7 @@ import pytest
 from lm_cases import norm_graph
 from lm_mixed_cases import BROADCAST_KINDS, SUM_READERS, broadcast_gradient, sum_read_before_its_norm
 from paper_1707_08265_b200 import binding as B
+from paper_1707_08265_b200 import workloads as wl
 
 
 def steps(desc, inputs, outputs):
@@ -38,7 +39,21 @@ def test_gradient_of_a_broadcast_tensor_is_summed_before_a_kernel_reads_it(kind)
     summing = [i for i, s in enumerate(lines) if "colacc=1" in s or "scalacc=1" in s]
     assert summing, lines
     for i, n in enumerate(names):
-        if n in ("rms_norm_bwd", "gated_scan_bwd", "softmax_ce_bwd"):
+        if n in ("rms_norm_bwd", "gated_scan_bwd", "softmax_ce_bwd") and kind != "gain of two uses":
             assert min(summing) < i
     if kind == "product of one row":          # no contraction over more rows than X has
         assert [s for s in lines if s.startswith("gemm")] == ["gemm[1x264x64 -> f32]", "gemm[1x64x264 B^T -> f32]", "gemm[264x64x1 A^T B^T -> f32]"]
+    if kind in ("gain of two uses", "vector of two uses", "objective of two uses"):
+        # the two contributions meet behind the sum, over the vector's own elements
+        assert "colacc=0" in lines[-1] and "n=264 " in lines[-1] and max(summing) < len(lines) - 1
+    if kind == "scalar of two widths":
+        assert len(summing) == 2 and "n=1 " in lines[-1]
+
+
+def test_contributions_of_one_shape_stay_one_program():
+    g = wl.GraphDesc()
+    x, m = g.tensor("x", [264]), g.tensor("M", [37, 264])
+    objs = [g.op("Mul", [m, x], "z"), g.op("Mul", [g.op("Sin", [m], "sm"), x], "u")]
+    grads = g.grad(objs, [x])
+    lines = steps(g.desc, [x, m], objs + grads)
+    assert len(lines) == 1 and "colacc=1" in lines[0]
