@@ -183,8 +183,8 @@ int dragon_function_workspace_tensors(const dragon_function_t* f, int64_t* out, 
  * Sec. 2.4 is about operators that write over their input.  Returns 1 if fetch position `output` may be
  * given the very same device pointer as feed position `input` in dragon_run(), 0 if not, a negative
  * code for bad positions.  It is 1 when the function is nothing but GlobalNorm and one norm's ClipByNorm, `input` is a tensor
- * that is clipped once and `output` its clipped form of the same type (the launch that overwrites it is behind the
- * one that sums it).  Otherwise it is 1 exactly when the function is a single elementwise launch over a
+ * that is clipped once and is not the norm itself, and `output` its clipped form of the same type (the launch that
+ * overwrites it is behind the one that sums it).  Otherwise it is 1 exactly when the function is a single elementwise launch over a
  * flat domain, both tensors have the domain's shape and the same type, and the program reads the
  * input for the last time before it first writes the output: every thread then overwrites only
  * elements it has already read (the copy of a tile that is fetched ahead of time is never a tile that

@@ -400,6 +400,8 @@ int dragon_function_can_alias(const dragon_function_t* f, int input, int output)
     for (size_t k = 0; k + 1 < P.steps.size(); ++k)
       if (P.steps[k].kind != ST_GNORM) return 0;
     const Step& cs = P.steps.back();
+    const MemRef& norm = P.mems[cs.rd[cl::NORM]];
+    if (norm.where == MEM_FEED && norm.index == input) return 0;      // every CTA reads the norm, at a time of its own
     int reads = 0, pairs = 0;
     for (size_t k = 0; k < cs.wr.size(); ++k) {
       const MemRef &mi = P.mems[cs.rd[cl::FIRST + k]], &mo = P.mems[cs.wr[k]];

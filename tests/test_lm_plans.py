@@ -57,3 +57,15 @@ def test_contributions_of_one_shape_stay_one_program():
     grads = g.grad(objs, [x])
     lines = steps(g.desc, [x, m], objs + grads)
     assert len(lines) == 1 and "colacc=1" in lines[0]
+
+
+def test_a_norm_that_is_clipped_itself_is_not_overwritten():
+    """Every CTA of the clipping launch reads the norm: a tensor that is the norm as well has to stay while it runs."""
+    g = B.Graph()
+    n, a = g.add_tensor("n", B.F32, []), g.add_tensor("a", B.F32, [100])
+    cn, ca = g.add_tensor("cn", B.F32, []), g.add_tensor("ca", B.F32, [100])
+    g.add_op(B.OPS["ClipByNorm"], [n, n], [cn], [1.0])
+    g.add_op(B.OPS["ClipByNorm"], [a, n], [ca], [1.0])
+    f = g.function([n, a], [cn, ca])
+    assert not f.can_alias(0, 0) and not f.can_alias(0, 1) and f.can_alias(1, 1) and not f.can_alias(1, 0)
+    assert not g.function([n], [cn]).can_alias(0, 0)
