@@ -11,6 +11,10 @@ Which axis, for the five workloads:
   * the MLP (workload 4): the batch; weights and biases are replicated; the loss is a mean over the batch and
     every gradient descends from it, so a rank's results are weighted by its share of the batch and added
     -> all-reduce(sum) of loss, dW1, db1, dW2, db2 after scaling by rows_of_rank / rows.
+Of the language-model operators those that work on each row by itself run on shards of rows (RMSNorm, scales of 1 x 128
+blocks and Quantize in them, the rows of X in ScaledInnerProduct, ClipByNorm by a norm that every rank has); what mixes rows
+(GatedScan, scales of 128 x 128 blocks, GlobalNorm) is refused with a ValueError, and so is a result that only holds one
+rank's part going into any of them.
 Remote data always lands in local memory (the all-reduce's output) before any kernel reads it.
 """
 
@@ -29,8 +33,36 @@ def _has_extent(desc, t, extent):
     return bool(shp) and shp[0] == extent
 
 
+def _refuse_mixed_rows(desc, extent):
+    """Raises where a language-model operator would mix the rows of several shards, or where an operand that is no row of the
+    sharded tensors happens to have their leading extent and would be cut too."""
+    one_rank = set()      # tensors without the extent that were computed from one rank's rows
+    for op in desc["ops"]:
+        cut = [_has_extent(desc, t, extent) for t in op["in"]]
+        result = any(_has_extent(desc, t, extent) for t in op["out"])
+        if op["type"] == "RMSNorm":
+            ok = len(desc["tensors"][op["in"][0]]["shape"]) == 2 and not cut[1] if any(cut) else True
+        elif op["type"] == "BlockScale":
+            ok = cut[0] == result and not (cut[0] and op.get("attrs", [1])[0] != 1)
+        elif op["type"] == "Quantize":
+            ok = cut[0] == cut[1]
+        elif op["type"] == "ScaledInnerProduct":
+            ok = cut[0] == cut[1] and not cut[2] and not cut[3]
+        elif op["type"] in ("GlobalNorm", "GatedScan"):
+            ok = not any(cut)
+        elif op["type"] == "ClipByNorm":
+            ok = True
+        else:
+            ok = None
+        if ok is False or (ok and any(t in one_rank for t in op["in"])):
+            raise ValueError("%s of '%s' cannot run on shards of the leading extent %d" % (op["type"], desc["tensors"][op["out"][0]]["name"], extent))
+        if not result and (any(cut) or any(t in one_rank for t in op["in"])):
+            one_rank.update(op["out"])
+
+
 def shard_desc(desc, extent, new_extent):
     """The graph of one shard: every tensor whose leading extent is ``extent`` gets ``new_extent`` instead."""
+    _refuse_mixed_rows(desc, extent)
     out = {"tensors": [], "ops": desc["ops"], "grads": desc.get("grads", [])}
     for t in desc["tensors"]:
         shp = list(t["shape"])
@@ -49,6 +81,7 @@ def classify_outputs(desc, outputs, extent):
       MEAN   a batch mean (SoftmaxCrossEntropy of sharded logits) or a gradient that descends from one:
              the ranks' results are weighted by their share of the axis and added;
       SAME   a forward tensor without the leading extent: the same on every rank."""
+    _refuse_mixed_rows(desc, extent)
     producer = {}
     for op in desc["ops"]:
         for o in op["out"]:
