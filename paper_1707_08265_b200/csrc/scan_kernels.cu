@@ -27,7 +27,7 @@ namespace {
 
 // The forward folds 16 rows a warp (3 CTAs of 4 warps per SM, the next tile's rows on their way in registers), the gradient,
 // which holds three tensors' rows and three values per element, 8 (2 CTAs of 8 warps; the next tile's rows on their way to
-// L2).  Measured on 65536 x 1024 bf16, one sequence (and 1024 of them, where no tile needs another): forward 164 us (98),
+// L2).  Measured on 65536 x 1024 bf16, one sequence (and 1024 of them, where no tile needs another): forward 169 us (103),
 // with 4 CTAs and their spills 175 (112), 8 x 8 rows 199 (117), folding one tile ahead of the one that waits 242 (143: the
 // second tile's registers cost more than the wait); gradient 295 (241), without the next tile asked for 337 (258).  The bytes
 // alone: 61, 143.
@@ -119,24 +119,27 @@ __device__ __forceinline__ Vec<1> mul(const Vec<1>& a, const Vec<1>& b) { return
 __device__ __forceinline__ Vec<1> add(const Vec<1>& a, const Vec<1>& b) { return {{__fadd_rn(a.v[0], b.v[0])}}; }
 __device__ __forceinline__ Vec<1> fma(const Vec<1>& a, const Vec<1>& b, const Vec<1>& c) { return {{__fmaf_rn(a.v[0], b.v[0], c.v[0])}}; }
 
-// f and 1 - f = exp(-z) f, each to full relative precision (two units or so); exp(-z) is kept finite, a NaN stays one
-__device__ __forceinline__ void gate_of(float z, float* f, float* keep) {
-  float u = -z * 1.4426950408889634f, t;
-  asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(u) : "f"(u));      // 126
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(u));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(*f) : "f"(__fadd_rn(1.f, t)));
-  *keep = __fmul_rn(t, *f);
-}
-template <int CH> __device__ __forceinline__ void gate_of(const Vec<CH>& z, Vec<CH>* f, Vec<CH>* keep) {
-  Vec<CH> u = mul(z, splat<CH>(-1.4426950408889634f)), t;
+// f = 1 / (1 + exp(-z)) and 1 - f = exp(-z) f, each within 10 units of 2^-24 of itself: exp(-z) = 2^u (1 + w) with u the rounded
+// product -z log2(e) and w what it leaves out times ln 2 (its residue, exact, and z times the part of log2(e) that fp32 does
+// not hold; without it the error grows to |z| units); 2^u is good to 4 units, the reciprocal to 2, three more roundings.  z is
+// kept in [-87, 104], where exp(-z) and f are normal numbers or 0 and nothing is infinite; a NaN stays one.  Two columns at a
+// time this is three instructions an element more than the rounded product alone: 65536 x 1024 bf16 forward 169 us for 165,
+// forward and gradient 463 for 456.
+constexpr float kLog2eHi = 1.44269502162933349609375f, kLog2eLo = 1.9259629911266175e-8f, kLn2 = 0.693147180559945309f;
+template <int CH> __device__ __forceinline__ void gate_of(Vec<CH> z, Vec<CH>* f, Vec<CH>* keep) {
 #pragma unroll
   for (int e = 0; e < CH; ++e) {
-    asm("min.NaN.f32 %0, %1, 0f42FC0000;" : "=f"(u.v[e]) : "f"(u.v[e]));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.v[e]) : "f"(u.v[e]));
+    asm("max.NaN.f32 %0, %1, 0fC2AE0000;" : "=f"(z.v[e]) : "f"(z.v[e]));      // -87
+    asm("min.NaN.f32 %0, %1, 0f42D00000;" : "=f"(z.v[e]) : "f"(z.v[e]));      // 104
   }
-  u = add(t, splat<CH>(1.f));
+  const Vec<CH> u = mul(z, splat<CH>(-kLog2eHi)), w = fma(z, splat<CH>(kLog2eLo), fma(z, splat<CH>(kLog2eHi), u));
+  Vec<CH> t;
 #pragma unroll
-  for (int e = 0; e < CH; ++e) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f->v[e]) : "f"(u.v[e]));
+  for (int e = 0; e < CH; ++e) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.v[e]) : "f"(u.v[e]));
+  t = fma(t, mul(w, splat<CH>(-kLn2)), t);
+  const Vec<CH> d = add(t, splat<CH>(1.f));
+#pragma unroll
+  for (int e = 0; e < CH; ++e) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f->v[e]) : "f"(d.v[e]));
   *keep = mul(t, *f);
 }
 
@@ -645,12 +648,14 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
     if (a.h0) h0.load(reinterpret_cast<const char*>(a.h0) + at * element_bytes<-1>(a.h0dt), a.h0dt);
     const bool from_h0 = a.h0 && !(a.reset && __ldg(a.reset + row) != 0);
     float h[CH];
+    Vec<CH> v, f, keep;
+#pragma unroll
+    for (int e = 0; e < CH; ++e) v.v[e] = z.get(e);
+    gate_of(v, &f, &keep);
 #pragma unroll
     for (int e = 0; e < CH; ++e) {
-      float f, keep;
-      gate_of(z.get(e), &f, &keep);
-      h[e] = keep * x.get(e);
-      if (from_h0) h[e] = fmaf(f, h0.get(e), h[e]);
+      h[e] = keep.v[e] * x.get(e);
+      if (from_h0) h[e] = fmaf(f.v[e], h0.get(e), h[e]);
     }
     store_cell<DT, CH>(reinterpret_cast<char*>(a.h) + at * element_bytes<DT>(a.hdt), a.hdt, h);
   }
