@@ -81,6 +81,9 @@ enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2, DRAGON_F8E4M3 = 3 };
  *   SCALED_INNER_PRODUCT(Xq, sx, Wq, sw)  Y[m,n] = sum_b sx[m,b] sw[n/128,b] sum_{k in block b} Xq[m,k] Wq[n,k] with
  *                          blocks of 128 along K; Xq F8E4M3 [M,K], sx f32 [M, ceil(K/128)], Wq F8E4M3 [N,K], sw f32
  *                          [ceil(N/128), ceil(K/128)], K a multiple of 16; fp32 accumulation; Y f32 or bf16.
+ *                          A block's two scales are multiplied first, in fp32: a product below 2^-126 is off by up to
+ *                          2^-150, times the sum it scales (operands of magnitude 1e-18 on both sides), one beyond
+ *                          2^128 is infinite, and 0 times it NaN.
  *   GLOBAL_NORM(t0, t1, ...)  scalar sqrt(sum of the squares of all elements of all operands), any shapes.
  *   CLIP_BY_NORM(t, norm) attrs {limit}   t * min(1, limit / norm), norm an f32 scalar (NaN makes everything NaN), limit > 0.
  *                          The fetched ones of a norm run as one launch over all tensors; one that an operator

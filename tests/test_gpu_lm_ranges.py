@@ -47,3 +47,27 @@ def test_gates_at_the_ends_of_the_range():
     z = np.array([[np.inf, -np.inf, 3e38, -3e38, 1e-45, -0.0, np.nan, 104.5]])
     (got,), _ = run_gpu(g.desc, [gate, x, h0], [h], [z, np.full((1, 8), 3.0), np.full((1, 8), 5.0)])
     assert np.array_equal(got[0, :6], [5.0, 3.0, 5.0, 3.0, 4.0, 4.0]) and np.isnan(got[0, 6]) and got[0, 7] == 5.0
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 300, 4096), (20, 130, 272), (50, 257, 400), (100, 200, 2064), (300, 520, 640), (2433, 2049, 272), (2400, 2056, 144)])
+def test_scaled_product_whose_scales_multiply_to_a_denormal(M, N, K):
+    """Scales of 1e-21 on both sides: their product has its documented error, a denormal's half step, in both kernels; rows
+    whose scales multiply to a normal number have none of it, and a row of zeros stays zero."""
+    g, kb, nb = wl.GraphDesc(), -(-K // 128), -(-N // 128)
+    t = [g.tensor("xq", [M, K], "f8e4m3"), g.tensor("sx", [M, kb]), g.tensor("wq", [N, K], "f8e4m3"), g.tensor("sw", [nb, kb])]
+    y = g.op("ScaledInnerProduct", t, "y", [M, N])
+    rng = np.random.default_rng(M)
+    xq, wq = (interp.round_e4m3(rng.standard_normal((r, K)) * 120.0) for r in (M, N))
+    xq[0] = 0
+    sx, sw = ((1e-21 * np.exp(rng.standard_normal(shape) * 0.5)).astype(np.float32).astype(np.float64) for shape in ((M, kb), (nb, kb)))
+    sx[1::3] = np.float32(1e-10)
+    (got,), _ = run_gpu(g.desc, t, [y], [xq, sx, wq, sw])
+    want = interp.run_function(g.desc, t, [y], [xq, sx, wq, sw])[0]
+    plain = np.abs(xq) @ np.abs(wq).T
+    mag = (np.abs(xq) * interp._spread(sx, (M, K), 1)) @ (np.abs(wq) * interp._spread(sw, (N, K), 128)).T
+    assert (got[0] == 0).all() and np.isfinite(got).all()
+    # exact products, at most 128 additions in a block, a factor (half a unit, or half of 2^-149) and one addition a block
+    bound = (128 + kb + 2) * U32 * mag + kb * 2.0 ** -149
+    bound += np.where(np.arange(M)[:, None] % 3 == 1, 0, plain * 2.0 ** -150 * (1 + 200 * U32))
+    assert (np.abs(got - want) <= bound).all()
+    assert (np.abs(want[1::3]) > 2.0 ** -110).mean() > 0.9      # (ordinary numbers, for which 2^-149 is nothing)
