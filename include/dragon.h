@@ -249,7 +249,9 @@ int dragon_verify_vm_program(const uint32_t* code, int n_code, int loop_start, i
 
 /* Scratch memory (partial sums, tensors that cross kernels, spilled values, a status word).
  * dev_ptr: device memory, 256-byte aligned, at least dragon_function_workspace_bytes() long,
- * owned by the caller and not touched by anyone else while a run is in flight. */
+ * owned by the caller and not touched by anyone else while a run is in flight.  Between two runs it may serve
+ * something else, another function among them: no result depends on what is in it.  dragon_function_status then
+ * speaks of a run only if nothing else has written to the workspace since the run before it. */
 size_t dragon_function_workspace_bytes(const dragon_function_t* f);
 int dragon_function_set_workspace(dragon_function_t* f, void* dev_ptr, size_t bytes);
 

@@ -686,7 +686,7 @@ int dragon_run(dragon_function_t* f, const void* const* feeds, void* const* fetc
         e = cudaMemcpyAsync(ptr[s.mC], ptr[s.mA], P.mems[s.mA].bytes(), cudaMemcpyDeviceToDevice, st);
         break;
       default: {
-        const StepRun r{s, P.mems, ptr.data(), ws, status, next_cleared ? nullptr : status_next, reinterpret_cast<unsigned*>(word0 + 32), P.sm_count, cuda_stream};
+        const StepRun r{s, P.mems, ptr.data(), ws, status, next_cleared ? nullptr : status_next, P.sm_count, cuda_stream};
         next_cleared = true;
         switch (s.kind) {
           case ST_NORM: e = launch_norm(r); break;

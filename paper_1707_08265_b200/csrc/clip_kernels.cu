@@ -7,6 +7,8 @@
 // launch and the barrier are nearly all.
 // Squares are added in fp32 over the 16 or 32 elements a thread holds at a time and in fp64 beyond; elements whose squares
 // could leave fp32's range are squared in fp64.  The order of the sums is fixed, so the norm is the same in every run.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "device_util.h"
@@ -38,7 +40,6 @@ struct NormOut {
   float* norm;
   float* factor;
   float limit;
-  unsigned* counter;
   int* status_clear;
 };
 
@@ -183,9 +184,10 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
   return r;
 }
 
+// The grid-wide barriers here and in norm_and_clip_kernel are those of a cooperative launch: all CTAs run at once, so every wait
+// ends, and nothing in the caller's workspace has to be zero before a run (it may have served another function in between).
 template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtasPerSm) global_norm_kernel(const __grid_constant__ TensorList t, const NormOut o) {
   __shared__ double sh[kThreads / 32];
-  __shared__ bool last;
   if (o.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *o.status_clear = 0;
   double sum = 0.0;
   Walk w(t, 1);
@@ -199,15 +201,11 @@ template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtas
     sum += chunk_squares(now, here.src, here.f32(), here.first, here.n);
   }
   sum = block_sum(sum, sh);
-  if (threadIdx.x == 0) {
-    o.part[o.part_first + blockIdx.x] = sum;
-    __threadfence();
-    last = o.last_launch && atomicAdd(o.counter, 1u) == gridDim.x - 1;
-  }
-  __syncthreads();
-  if (!last) return;
-  // the last CTA to arrive adds all partial sums, in their order
-  __threadfence();
+  if (threadIdx.x == 0) __stcg(o.part + o.part_first + blockIdx.x, sum);
+  if (!o.last_launch) return;
+  cooperative_groups::this_grid().sync();
+  if (blockIdx.x != 0) return;
+  // one CTA adds all partial sums, in their order
   double total = 0.0;
   for (int i = threadIdx.x; i < o.part_total; i += kThreads) total += __ldcg(o.part + i);
   total = block_sum(total, sh);
@@ -215,7 +213,6 @@ template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtas
     const float norm = (float)sqrt(total);
     if (o.norm) *o.norm = norm;
     if (o.factor) *o.factor = factor_of(norm, o.limit);
-    *o.counter = 0;
   }
 }
 
@@ -252,11 +249,10 @@ __device__ __forceinline__ void store_clipped(const Chunk& now, const void* src,
   }
 }
 
-// Norm and clipping in one launch, for tensors of which every CTA holds its whole share (kHeld chunks) in registers: read
-// once, summed, and after a grid-wide barrier scaled and written.  Launched cooperatively, so that all CTAs run; the wait is
-// bounded all the same.  Two words, zero before and after: CTAs that have left their sum, CTAs that have seen them all.
+// Norm and clipping in one cooperative launch, for tensors of which every CTA holds its whole share (kHeld chunks) in
+// registers: read once, summed, and after a grid-wide barrier scaled and written.
 constexpr int kHeld = 2;
-template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtasPerSm) norm_and_clip_kernel(const __grid_constant__ TensorList t, const NormOut o, int* status) {
+template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtasPerSm) norm_and_clip_kernel(const __grid_constant__ TensorList t, const NormOut o) {
   __shared__ double sh[kThreads / 32];
   if (o.status_clear && blockIdx.x == 0 && threadIdx.x == 0) *o.status_clear = 0;
   Chunk held[kHeld];
@@ -278,30 +274,15 @@ template <typename TensorList> __global__ void __launch_bounds__(kThreads, kCtas
     if (tensor[h] >= 0) sum += chunk_squares(held[h], t.src[tensor[h]], (t.dtype[tensor[h]] & 15) == DRAGON_F32, first[h], t.n[tensor[h]]);
   // the elements behind the last whole access are read again when they are written: before the barrier nobody writes
   sum = block_sum(sum, sh);
-  if (threadIdx.x == 0) {
-    __stcg(o.part + blockIdx.x, sum);
-    __threadfence();
-    atomicAdd(o.counter, 1u);
-    const long long t0 = clock64();
-    for (;;) {
-      unsigned there;
-      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(there) : "l"(o.counter) : "memory");
-      if (there >= gridDim.x) break;
-      if (clock64() - t0 > 4000000000LL) { atomicExch(status, DRAGON_ERR_TIMEOUT); break; }
-    }
-    __threadfence();
-  }
-  __syncthreads();
+  if (threadIdx.x == 0) __stcg(o.part + blockIdx.x, sum);
+  cooperative_groups::this_grid().sync();
   double total = 0.0;
   for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) total += __ldcg(o.part + i);
   total = block_sum(total, sh);
   const float norm = (float)sqrt(total), f = factor_of(norm, o.limit);
-  if (threadIdx.x == 0) {
-    if (blockIdx.x == 0) {
-      *o.norm = norm;
-      if (o.factor) *o.factor = f;
-    }
-    if (atomicAdd(o.counter + 1, 1u) == gridDim.x - 1) { o.counter[0] = 0; o.counter[1] = 0; }
+  if (threadIdx.x == 0 && blockIdx.x == 0) {
+    *o.norm = norm;
+    if (o.factor) *o.factor = f;
   }
 #pragma unroll
   for (int h = 0; h < kHeld; ++h) {
@@ -366,10 +347,23 @@ bool norm_and_clip_fit_one_launch(const std::vector<int64_t>& numel, const std::
 
 namespace {
 
+template <typename TensorList> cudaError_t launch(void (*kernel)(TensorList, NormOut), int grid, bool cooperative, cudaStream_t st, const TensorList& t, const NormOut& o) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cooperative ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, t, o);
+}
+
 template <int kMost> cudaError_t global_norm_of(const StepRun& r, cudaStream_t st) {
   const int n = (int)r.s.rd.size(), launches = launches_of_tensors(n);
   NormOut o{reinterpret_cast<double*>(r.ws + r.s.scratch_off), 0, 0, false, reinterpret_cast<float*>(r.wr(gn::NORM)), reinterpret_cast<float*>(r.wr(gn::FACTOR)),
-            (float)r.s.attr, r.counter, r.status_clear};
+            (float)r.s.attr, r.status_clear};
   for (int l = 0; l < launches; ++l) {
     TensorListOf<kMost> t;
     t.count = 0;
@@ -380,10 +374,11 @@ template <int kMost> cudaError_t global_norm_of(const StepRun& r, cudaStream_t s
     o.part_first = o.part_total;
     o.part_total += grid;
     o.last_launch = l + 1 == launches;
-    global_norm_kernel<<<grid, kThreads, 0, st>>>(t, o);
+    const cudaError_t e = launch(global_norm_kernel<TensorListOf<kMost>>, grid, o.last_launch, st, t, o);
+    if (e != cudaSuccess) return e;
     o.status_clear = nullptr;
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 template <int kMost> cudaError_t clip_of(const StepRun& r, cudaStream_t st) {
@@ -411,18 +406,9 @@ template <int kMost> cudaError_t norm_and_clip_of(const StepRun& r, cudaStream_t
   for (int k = 0; k < (int)r.s.rd.size(); ++k)
     if (!add_tensor(&t, r.rd(k), r.wr(gn::CLIPPED + k), r.rd_type(k), r.wr_type(gn::CLIPPED + k), r.mems[r.s.rd[k]].shape.numel())) return cudaErrorInvalidValue;
   const NormOut o{reinterpret_cast<double*>(r.ws + r.s.scratch_off), 0, 0, true, reinterpret_cast<float*>(r.wr(gn::NORM)), reinterpret_cast<float*>(r.wr(gn::FACTOR)),
-                  (float)r.s.attr, r.counter, r.status_clear};
-  cudaLaunchConfig_t cfg = {};
+                  (float)r.s.attr, r.status_clear};
   // no more CTAs than hold their share: at most kHeld chunks each, and all of them on the GPU at once
-  cfg.gridDim = dim3(std::min(t.first[t.count], r.sm_count * kCtasPerSm));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeCooperative;
-  attr[0].val.cooperative = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, norm_and_clip_kernel<TensorListOf<kMost>>, t, o, r.status);
+  return launch(norm_and_clip_kernel<TensorListOf<kMost>>, std::min(t.first[t.count], r.sm_count * kCtasPerSm), true, st, t, o);
 }
 
 }  // namespace

@@ -182,7 +182,6 @@ struct StepRun {
   char* ws;
   int* status;
   int* status_clear;
-  unsigned* counter;      // a word that is zero before and after every kernel (grid-wide "last block" tickets)
   int sm_count;
   void* stream;
   void* rd(int i) const { return s.rd[i] >= 0 ? ptr[s.rd[i]] : nullptr; }
