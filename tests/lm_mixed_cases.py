@@ -1,4 +1,7 @@
 """Graphs in which the language-model operators meet each other and the older ones in orders other than a layer's own."""
+import random
+
+from oracle import prune
 from paper_1707_08265_b200 import workloads as wl
 
 SUM_READERS = ("scales of rows", "scales of tiles", "given scales", "norm over tensors", "clipped", "scan of it", "scan gated by it", "gain of another norm")
@@ -87,3 +90,68 @@ def broadcast_gradient(kind, dtype="f32", rows=37, cols=264):
 
 BROADCAST_KINDS = ("norm of a vector", "norm of one row", "norm of a sum", "norm of a vector, constant", "scan of one row", "gain of two uses", "vector of two uses",
                    "objective of two uses", "scalar of two widths", "product of one row", "loss")
+
+
+def random_mixture(seed, rows=37, cols=264, n_ops=14):
+    """A random graph of the language-model operators and the graph VM's over [rows, cols], [cols] and scalar tensors, all
+    f32, values kept near one; some tensors fetched, gradients of some with respect to some.  Returns (graph, inputs,
+    outputs, the outputs that are e4m3)."""
+    rng = random.Random(seed)
+    g = wl.GraphDesc()
+    big, vec = [rows, cols], [cols]
+    wide = [g.tensor("x%d" % i, big) for i in range(3)]
+    rowv = [g.tensor("v%d" % i, vec) for i in range(2)] + [g.tensor("one_row", [1, cols])]
+    h0 = g.tensor("h0", [1, cols])
+    inputs = wide + rowv + [h0]
+    smooth = list(inputs)                      # tensors through which gradients pass
+    made, eight, no_grad = [], [], []
+
+    def name(t):
+        return "%s_%d" % (t, len(made) + len(eight) + len(no_grad))
+
+    for _ in range(n_ops):
+        kind = rng.choice(["Add", "Add", "Mul", "Tanh", "Sin", "RMSNorm", "RMSNorm", "GatedScan", "GatedScan", "vector norm", "row scan", "scales", "tiles", "GlobalNorm", "Clip",
+                           "Sum", "InnerProduct"])
+        a, b, v = rng.choice(wide), rng.choice(wide), rng.choice(rowv)
+        if kind in ("Add", "Mul"):
+            b = rng.choice([b, b, v])
+            wide.append(g.op(kind, [a, b], name(kind), big))
+        elif kind in ("Tanh", "Sin"):
+            src = rng.choice([a, v])
+            t = g.op(kind, [src], name(kind), g.shape(src))
+            (wide if g.shape(src) == big else rowv).append(t)
+        elif kind == "RMSNorm":
+            gain = rng.choice([t for t in rowv if g.shape(t) == vec])
+            wide.append(g.op("RMSNorm", [a, gain], name(kind), big, attrs=[0.1]))
+        elif kind == "vector norm":
+            gain = rng.choice([t for t in rowv if g.shape(t) == vec])
+            rowv.append(g.op("RMSNorm", [v, gain], name("vnorm"), g.shape(v), attrs=[0.1]))
+        elif kind == "GatedScan":
+            ins = [a, b] + ([h0] if rng.random() < 0.5 else [])
+            wide.append(g.op("GatedScan", ins, name(kind), big, attrs=[1]))
+        elif kind == "row scan":
+            one = [t for t in rowv if g.shape(t) == [1, cols]]
+            rowv.append(g.op("GatedScan", [rng.choice(one), rng.choice(one), h0], name("rowscan"), [1, cols], attrs=[1]))
+        elif kind == "Sum":
+            wide.append(g.op("Mean", [a], name("mean"), big))
+        elif kind == "InnerProduct":
+            p = g.op("InnerProduct", [a, b], name("prod"), [rows, rows])
+            no_grad.append(p)
+        elif kind in ("scales", "tiles"):
+            r = 1 if kind == "scales" else 128
+            s = g.op("BlockScale", [a], name("s"), [-(-rows // r), -(-cols // 128)], attrs=[r])
+            no_grad.append(s)
+            eight.append(g.op("Quantize", [a, s], name("q"), big, "f8e4m3"))
+        elif kind == "GlobalNorm":
+            no_grad.append(g.op("GlobalNorm", rng.sample(wide, min(len(wide), 3)) + [v], name("norm"), []))
+        else:
+            n = g.op("GlobalNorm", [a, b], name("norm"), [])
+            no_grad.append(n)
+            c = g.op("ClipByNorm", [a, n], name("clip"), big, attrs=[20.0])
+            no_grad.append(c if rng.random() < 0.5 else g.op("Sub", [b, c], name("upd"), big))
+        made = [t for t in wide + rowv if t not in inputs]
+    objs = rng.sample(made, min(len(made), 2))
+    reached = [t for t in smooth if t in prune.backward_marks(g.desc, objs, smooth)]
+    grads = g.grad(objs, rng.sample(reached, min(len(reached), 4))) if reached else []
+    outputs = rng.sample(made, min(len(made), 3)) + rng.sample(no_grad, min(len(no_grad), 3)) + rng.sample(eight, min(len(eight), 1)) + grads
+    return g, inputs, outputs, eight

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from lm_cases import U16, U32, normals, run_gpu
-from lm_mixed_cases import BROADCAST_KINDS, SUM_READERS, broadcast_gradient, sum_read_before_its_norm
+from lm_mixed_cases import BROADCAST_KINDS, SUM_READERS, broadcast_gradient, random_mixture, sum_read_before_its_norm
 from oracle import interp
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +41,26 @@ def test_gradient_of_a_broadcast_tensor(kind, dtype):
         # between them; every value may pass three roundings to bf16 that go the other way (of y, of dy and its own)
         rounded = 0.0 if dtype == "f32" and kind != "product of one row" else 6 * U16
         assert np.abs(a - b).max() <= (1000 * U32 + rounded) * max(np.abs(b).max(), 1e-30), info["name"]
+
+
+# an operator's own error, relative to the largest value: the scan's 37 rows at (6 + |z|) 2^-23 with |z| <= 16, all others below;
+# up to 14 of them one behind another
+CHAIN = 14 * 37 * 22 * 2 * U32
+
+
+@pytest.mark.parametrize("seed", range(80))
+def test_random_mixture_of_operators(seed):
+    g, inputs, outputs, eight = random_mixture(seed)
+    feeds = normals(g.desc, inputs, seed)
+    want, val, _ = interp.run_function(g.desc, inputs, outputs, feeds, return_all=True)
+    got, f = run_gpu(g.desc, inputs, outputs, feeds)
+    by_output = {op["out"][0]: op for op in g.desc["ops"]}
+    for t, a, b in zip(outputs, got, want):
+        what = "%s of\n%s" % (g.desc["tensors"][t]["name"], f.describe())
+        if t in eight:            # a value next to a midpoint may become the neighbour: a step is an 8th of it at most, 2^-9 at least
+            assert (np.abs(a - b) <= np.maximum(np.abs(b) * 2.0 ** -3, 2.0 ** -9)).all(), what
+        elif t in by_output and by_output[t]["type"] == "InnerProduct":      # operands rounded to bf16, perhaps the other way
+            p, q = (np.abs(val[i]) for i in by_output[t]["in"])
+            assert (np.abs(a - b) <= (4 * U16 + 2 * CHAIN) * (p @ q.T)).all(), what
+        else:
+            assert np.abs(a - b).max() <= CHAIN * np.abs(b).max(), what

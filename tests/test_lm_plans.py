@@ -2,7 +2,7 @@
 import pytest
 
 from lm_cases import norm_graph
-from lm_mixed_cases import BROADCAST_KINDS, SUM_READERS, broadcast_gradient, sum_read_before_its_norm
+from lm_mixed_cases import BROADCAST_KINDS, SUM_READERS, broadcast_gradient, random_mixture, sum_read_before_its_norm
 from paper_1707_08265_b200 import binding as B
 from paper_1707_08265_b200 import workloads as wl
 
@@ -69,3 +69,11 @@ def test_a_norm_that_is_clipped_itself_is_not_overwritten():
     f = g.function([n, a], [cn, ca])
     assert not f.can_alias(0, 0) and not f.can_alias(0, 1) and f.can_alias(1, 1) and not f.can_alias(1, 0)
     assert not g.function([n], [cn]).can_alias(0, 0)
+
+
+def test_random_mixtures_compile():
+    """The library refuses a plan that reads memory before it is written; no mixture of operators makes one."""
+    for seed in range(300):
+        g, inputs, outputs, _ = random_mixture(seed)
+        f = B.Graph.from_desc(g.desc).function(inputs, outputs)
+        assert f.num_launches() > 0
