@@ -130,7 +130,7 @@ def _forward(op, ins, dtype, bf16_contraction=True):
         return np.asarray(np.sqrt(sum(float((a.astype(np.float64) ** 2).sum()) for a in ins)), dtype=dtype)
     if t == "ClipByNorm":
         limit = _attr(op)
-        return ins[0] * (limit / ins[1] if ins[1] > limit else 1.0)
+        return ins[0] * (1.0 if ins[1] <= limit else limit / ins[1])      # (a NaN norm makes everything NaN)
     if t == "GatedScan":
         return _scan(op, ins)[0].reshape(ins[0].shape)
     if t == "Add":
