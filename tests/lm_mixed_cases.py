@@ -92,16 +92,20 @@ BROADCAST_KINDS = ("norm of a vector", "norm of one row", "norm of a sum", "norm
                    "objective of two uses", "scalar of two widths", "product of one row", "loss")
 
 
-def random_mixture(seed, rows=37, cols=264, n_ops=14):
-    """A random graph of the language-model operators and the graph VM's over [rows, cols], [cols] and scalar tensors, all
-    f32, values kept near one; some tensors fetched, gradients of some with respect to some.  Returns (graph, inputs,
+def random_mixture(seed, rows=37, cols=264, n_ops=14, types=("f32",)):
+    """A random graph of the language-model operators and the graph VM's over [rows, cols], [cols] and scalar tensors of the
+    given types, values kept near one; some tensors fetched, gradients of some with respect to some.  Returns (graph, inputs,
     outputs, the outputs that are e4m3)."""
     rng = random.Random(seed)
     g = wl.GraphDesc()
+
+    def dt():
+        return types[0] if len(types) == 1 else rng.choice(types)
+
     big, vec = [rows, cols], [cols]
-    wide = [g.tensor("x%d" % i, big) for i in range(3)]
-    rowv = [g.tensor("v%d" % i, vec) for i in range(2)] + [g.tensor("one_row", [1, cols])]
-    h0 = g.tensor("h0", [1, cols])
+    wide = [g.tensor("x%d" % i, big, dt()) for i in range(3)]
+    rowv = [g.tensor("v%d" % i, vec, dt()) for i in range(2)] + [g.tensor("one_row", [1, cols], dt())]
+    h0 = g.tensor("h0", [1, cols], dt())
     inputs = wide + rowv + [h0]
     smooth = list(inputs)                      # tensors through which gradients pass
     made, eight, no_grad = [], [], []
@@ -109,33 +113,34 @@ def random_mixture(seed, rows=37, cols=264, n_ops=14):
     def name(t):
         return "%s_%d" % (t, len(made) + len(eight) + len(no_grad))
 
+    kinds = ["Add", "Add", "Mul", "Tanh", "Sin", "RMSNorm", "RMSNorm", "GatedScan", "GatedScan", "vector norm", "row scan", "scales", "tiles", "GlobalNorm", "Clip", "Sum"]
+    kinds += ["InnerProduct"] if cols % 8 == 0 else []      # (it takes rows of 16 bytes)
     for _ in range(n_ops):
-        kind = rng.choice(["Add", "Add", "Mul", "Tanh", "Sin", "RMSNorm", "RMSNorm", "GatedScan", "GatedScan", "vector norm", "row scan", "scales", "tiles", "GlobalNorm", "Clip",
-                           "Sum", "InnerProduct"])
+        kind = rng.choice(kinds)
         a, b, v = rng.choice(wide), rng.choice(wide), rng.choice(rowv)
         if kind in ("Add", "Mul"):
             b = rng.choice([b, b, v])
-            wide.append(g.op(kind, [a, b], name(kind), big))
+            wide.append(g.op(kind, [a, b], name(kind), big, dt()))
         elif kind in ("Tanh", "Sin"):
             src = rng.choice([a, v])
-            t = g.op(kind, [src], name(kind), g.shape(src))
+            t = g.op(kind, [src], name(kind), g.shape(src), dt())
             (wide if g.shape(src) == big else rowv).append(t)
         elif kind == "RMSNorm":
             gain = rng.choice([t for t in rowv if g.shape(t) == vec])
-            wide.append(g.op("RMSNorm", [a, gain], name(kind), big, attrs=[0.1]))
+            wide.append(g.op("RMSNorm", [a, gain], name(kind), big, dt(), attrs=[0.1]))
         elif kind == "vector norm":
             gain = rng.choice([t for t in rowv if g.shape(t) == vec])
-            rowv.append(g.op("RMSNorm", [v, gain], name("vnorm"), g.shape(v), attrs=[0.1]))
+            rowv.append(g.op("RMSNorm", [v, gain], name("vnorm"), g.shape(v), dt(), attrs=[0.1]))
         elif kind == "GatedScan":
             ins = [a, b] + ([h0] if rng.random() < 0.5 else [])
-            wide.append(g.op("GatedScan", ins, name(kind), big, attrs=[1]))
+            wide.append(g.op("GatedScan", ins, name(kind), big, dt(), attrs=[1]))
         elif kind == "row scan":
             one = [t for t in rowv if g.shape(t) == [1, cols]]
-            rowv.append(g.op("GatedScan", [rng.choice(one), rng.choice(one), h0], name("rowscan"), [1, cols], attrs=[1]))
+            rowv.append(g.op("GatedScan", [rng.choice(one), rng.choice(one), h0], name("rowscan"), [1, cols], dt(), attrs=[1]))
         elif kind == "Sum":
-            wide.append(g.op("Mean", [a], name("mean"), big))
+            wide.append(g.op("Mean", [a], name("mean"), big, dt()))
         elif kind == "InnerProduct":
-            p = g.op("InnerProduct", [a, b], name("prod"), [rows, rows])
+            p = g.op("InnerProduct", [a, b], name("prod"), [rows, rows], dt())
             no_grad.append(p)
         elif kind in ("scales", "tiles"):
             r = 1 if kind == "scales" else 128
@@ -147,8 +152,8 @@ def random_mixture(seed, rows=37, cols=264, n_ops=14):
         else:
             n = g.op("GlobalNorm", [a, b], name("norm"), [])
             no_grad.append(n)
-            c = g.op("ClipByNorm", [a, n], name("clip"), big, attrs=[20.0])
-            no_grad.append(c if rng.random() < 0.5 else g.op("Sub", [b, c], name("upd"), big))
+            c = g.op("ClipByNorm", [a, n], name("clip"), big, dt(), attrs=[20.0])
+            no_grad.append(c if rng.random() < 0.5 else g.op("Sub", [b, c], name("upd"), big, dt()))
         made = [t for t in wide + rowv if t not in inputs]
     objs = rng.sample(made, min(len(made), 2))
     reached = [t for t in smooth if t in prune.backward_marks(g.desc, objs, smooth)]

@@ -64,3 +64,16 @@ def test_random_mixture_of_operators(seed):
             assert (np.abs(a - b) <= (4 * U16 + 2 * CHAIN) * (p @ q.T)).all(), what
         else:
             assert np.abs(a - b).max() <= CHAIN * np.abs(b).max(), what
+
+
+@pytest.mark.parametrize("rows,cols", [(37, 264), (131, 130), (65, 33), (1, 1001)])
+@pytest.mark.parametrize("seed", range(12))
+def test_random_mixture_of_operators_and_types(seed, rows, cols):
+    """bf16 and f32 tensors among each other: up to 14 roundings to bf16 behind one another, each in two evaluations that may
+    round differently, bound the relative 2-norm."""
+    g, inputs, outputs, eight = random_mixture(1000 + seed, rows, cols, types=("f32", "bf16"))
+    feeds = normals(g.desc, inputs, seed)
+    got, f = run_gpu(g.desc, inputs, outputs, feeds)
+    for t, a, b in zip(outputs, got, interp.run_function(g.desc, inputs, outputs, feeds)):
+        assert np.linalg.norm(a - b) <= 14 * 2 * U16 * np.linalg.norm(b) + (2.0 ** -3 * np.linalg.norm(b) if t in eight else 0), "%s of\n%s" % (
+            g.desc["tensors"][t]["name"], f.describe())
