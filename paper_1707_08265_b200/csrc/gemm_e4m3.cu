@@ -11,16 +11,16 @@
 //
 //   gemm_e4m3_kernel      many rows: two CTAs of a cluster work on one tile of 256 rows of X x 256 rows of W
 //                         (tcgen05.mma.cta_group::2), so that a CTA copies 32 KB a block instead of the 48 KB of a 128 x 256 tile
-//                         of its own.  A thread holds one row of Y and 64 columns, its scale is one number a block; persistent
-//                         pairs in an L2-friendly tile order.  Measured, 8192 x 8192 x 4096: 260 us by itself (2.1 PFLOP/s), 310 us
-//                         in a loop under the power limit (1.8).  A block of a tile takes 0.52 us: its products alone 0.30, with
-//                         the copies 0.42 (12 TB/s out of L2), with the hand-over of the accumulators but no work on them 0.47.
+//                         of its own.  A thread holds one row of Y and 128 columns, its scale is one number a block; persistent
+//                         pairs in an L2-friendly tile order.  Measured, 8192 x 8192 x 4096: 250 us by itself (2.2 PFLOP/s), 308 us
+//                         in a loop under the power limit (1.8).  A block of a tile takes 0.52 us: its products alone 0.28, with
+//                         the copies 0.37 (13 TB/s out of L2), with the hand-over of the accumulators but no work on them 0.41.
 //                         TMEM holds two blocks' sums, so the products of a block wait for the work on the one before the last.
 //                         Slower: accumulators of half a tile (A is read twice), 16 epilogue warps of 64 columns (spills), a
 //                         release before the last sums (no gain).
 //   gemm_e4m3_few_kernel  few rows: the operands change places (128 rows of W x 16..128 rows of X), so that the tile's height is
 //                         filled by weights and hardly any product is wasted; the K blocks of a tile are split over the
-//                         CTAs of a cluster, whose partial sums meet in shared memory in a fixed order.  5 x 8192 x 4096: 11.3 us, one call
+//                         CTAs of a cluster, whose partial sums meet in shared memory in a fixed order.  5 x 8192 x 4096: 11.4 us, one call
 //                         after another (34 MB of weights: 5.1 us at the measured bandwidth; the rest is the first bytes' latency
 //                         and the join); 256 x 8192 x 16384: a block 0.5 us, copies out of L2
 // Every wait is bounded; when one runs out the kernel records DRAGON_ERR_TIMEOUT, lets its copies and products in flight

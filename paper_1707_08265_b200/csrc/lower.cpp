@@ -4,7 +4,8 @@
 // (Sec. 3.2).  A gradient operator reads forward values through its anchor (Sec. 3.3); inside
 // one fused segment those are simply values that stay live, across segments they are
 // workspace tensors.  Gradients with respect to broadcast operands are kept per domain element
-// (the reverse sweep is linear in dy) and summed once, where the gradient tensor is written.
+// (the reverse sweep is linear in dy) and summed once: where the gradient tensor is written, where a
+// kernel of its own reads them with its output's extents, or where a contribution of another shape is added.
 #include <algorithm>
 #include <cmath>
 #include <cstdio>

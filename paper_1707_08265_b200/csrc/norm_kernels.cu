@@ -7,8 +7,10 @@
 // and written once; the statistics are fp32 sums.  Row lengths that do not fit take a second pass over the row.
 // Measured, bf16, the kernel by itself: norm with residual and sum 8192 x 4096 48 us (5.6 TB/s), 16384 x 4096 87 us (6.2), in fp32
 // 8192 x 8192 210 us (5.1); with scales and e4m3 values for y 4099 x 5000 35 us (4.1), 16384 x 4096 88 us (5.3; a division for each
-// lane and access instead 93); rows of 5001 81 us (single elements), of 5002 58 (pairs), of 5000 36; gradient with the residual
-// branch's 8192 x 4096 64 us (5.2).
+// lane and access instead 93); rows of 5001 80 us (single elements), of 5002 57 (pairs), of 5000 36; gradient with the residual
+// branch's 8192 x 4096 64 us (5.2).  To 8 bits, rows that are not 16-byte aligned or do not fit take two passes by single elements:
+// 4099 x 5001 108 us (4.9 times its bytes at the copy rate), 5490 x 532 23 (7.2; in fp32 4.0).  Issue slots used and DRAM's share,
+// by ncu: 4099 x 5000 to 8 bits 0.63 and 0.42, 4099 x 5001 0.69 and 0.18, 5490 x 532 to 8 bits 0.68 and 0.07.
 #include "device_util.h"
 #include "plan.h"
 
@@ -410,7 +412,7 @@ struct QuantArgs {
 
 // 1 x 128 blocks, or given scales of either kind, in rows of any length: a warp per block of a row, four elements a lane, four
 // blocks in flight (their scales as below).  8192 x 8191 bf16: 112 us (46 for 8192 columns), element by element 186; bound by
-// instructions (vectors joined across lanes, edges written by themselves).
+// instructions (vectors joined across lanes, edges written by themselves: 0.76 of the issue slots used, DRAM 0.19, by ncu).
 constexpr int kTogether = 4;
 template <int DT>
 __global__ void __launch_bounds__(256) quant_row_kernel(const QuantArgs a) {
@@ -463,7 +465,7 @@ __global__ void __launch_bounds__(256) quant_row_kernel(const QuantArgs a) {
 // The same for rows of a multiple of 8 elements: 16 lanes a block, 8 elements a lane, kTogether blocks of a half warp in
 // flight, whose scales (two correctly rounded divisions each) are computed by as many lanes at once.  kWhole: the length is a
 // multiple of 128, so block i is elements 128 i .. 128 i + 127 of the tensor.  16384 x 4096 bf16: 47 us (4.3 TB/s), with persistent
-// CTAs and a division per lane 61; bound by instructions.
+// CTAs and a division per lane 61; instructions as much as bytes (0.63 of the issue slots used, DRAM 0.51, by ncu).
 constexpr int kQuantBlocks = 16 * kTogether;      // blocks of a CTA
 template <int DT, bool kWhole>
 __global__ void __launch_bounds__(256, 4) quant_row_vec_kernel(const QuantArgs a) {
@@ -521,7 +523,7 @@ __global__ void __launch_bounds__(256, 4) quant_row_vec_kernel(const QuantArgs a
 
 // 128 x 128 blocks (8192 x 8192 bf16: 38 us, 5.3 TB/s): a CTA per block, which stays in registers between the maximum and the
 // rounding.  kVec: 16 lanes a row, 8 elements a lane, 16 rows at a time; otherwise (rows that are not 16-byte aligned) a warp a
-// row, four elements a lane: 8192 x 8191 84 us, element by element 407.
+// row, four elements a lane: 8192 x 8191 85 us (0.70 of the issue slots, DRAM 0.24), element by element 407.
 __device__ __forceinline__ float tile_scale(unsigned m, unsigned* sh) {
   m = __reduce_max_sync(0xffffffffu, m);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = m;
@@ -600,7 +602,7 @@ cudaError_t launch_norm(const StepRun& r) {
              (float)r.s.attr, r.status_clear};
   const RowShape s = row_shape(a.rows, a.cols);
   if (!s.in_registers || (s.vec != 8 && (a.s || a.q))) {
-    if (a.cols <= 1024) norm_loop_kernel<128><<<a.rows, 128, 0, st>>>(a);      // 5490 x 532 to 8 bits 23 us, with 512 threads 31
+    if (a.cols <= 1024) norm_loop_kernel<128><<<a.rows, 128, 0, st>>>(a);      // 5490 x 532 bf16 to 8 bits 23 us, with 512 threads 31
     else norm_loop_kernel<kMaxRowThreads><<<a.rows, kMaxRowThreads, 0, st>>>(a);
     return cudaGetLastError();
   }

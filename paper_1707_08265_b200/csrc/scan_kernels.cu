@@ -27,10 +27,10 @@ namespace {
 
 // The forward folds 16 rows a warp (3 CTAs of 4 warps per SM, the next tile's rows on their way in registers), the gradient,
 // which holds three tensors' rows and three values per element, 8 (2 CTAs of 8 warps; the next tile's rows on their way to
-// L2).  Measured on 65536 x 1024 bf16, one sequence (and 1024 of them, where no tile needs another): forward 169 us (103),
-// with 4 CTAs and their spills 175 (112), 8 x 8 rows 199 (117), folding one tile ahead of the one that waits 242 (143: the
-// second tile's registers cost more than the wait); gradient 295 (241), without the next tile asked for 337 (258).  The bytes
-// alone: 61, 143.
+// L2).  Measured on 65536 x 1024 bf16, one sequence (and 1024 of them, where no tile needs another): forward 169 us (104),
+// gradient 295 (247); the bytes alone: 61, 143.  Other shapes, when the gate took three instructions less (forward 164 (98),
+// gradient 295 (241)): 4 CTAs and their spills 175 (112), 8 x 8 rows 199 (117), folding one tile ahead of the one that waits 242
+// (143: the second tile's registers cost more than the wait), the gradient without the next tile asked for 337 (258).
 constexpr int kFwdWarps = 4, kBwdWarps = 8, kBwdCtas = 2;
 template <int CH> constexpr int kFwdCtas = CH == 2 ? 3 : 4;      // per SM, as registers allow
 template <int W> constexpr int rows_per_warp() { return kScanTileRows / W; }
