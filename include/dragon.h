@@ -93,8 +93,44 @@ enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2, DRAGON_F8E4M3 = 3 };
  *                          another, each starting from its row of h0 (f32/bf16 [sequences, C]) or from zero; reset (int32
  *                          [T]): a row with a value other than 0 starts from zero whatever came before (packed documents).
  *                          The state is kept in fp32 between rows.  One row per sequence is a decoding step.
- * RMS_NORM and GATED_SCAN have gradients (with respect to h, g; gate, x, h0).  A gradient chain through BLOCK_SCALE,
- * QUANTIZE, SCALED_INNER_PRODUCT, GLOBAL_NORM or CLIP_BY_NORM is DRAGON_ERR_UNSUPPORTED at dragon_function.
+ *   HEAD_NORM(x, g) attrs {eps = 1e-6}   x [T, H*D] holds H heads of D elements (D the length of g, a multiple of 8, at most
+ *                          256) in every row; y = x / sqrt(mean of x^2 over its head + eps) * g, statistics in fp32.
+ *   ROTATE(x, positions) attrs {heads, dims = D, interleaved = 0, base = 10000, factor = 1, low = 0, high = 0, original = 0,
+ *                          amplitude = 1}   positions int32 [T]; the first dims elements (even) of every head of x
+ *                          [T, heads*D] are pairs (a, b), elements i and i + dims/2, or 2i and 2i + 1 if interleaved, and
+ *                          become amplitude (a cos t - b sin t), amplitude (b cos t + a sin t), t = positions[r] * f_i with
+ *                          f_i = base^(-2i/dims) * (k + (1 - k) / factor); k = 0 unless original > 0, then
+ *                          k = clamp((original * base^(-2i/dims) / 2 pi - low) / (high - low), 0, 1), a step at low where
+ *                          low = high (contexts longer than the original one: slow pairs are slowed by factor, fast ones
+ *                          kept).  Elements behind dims are copied.  Angles are exact to 2^-24 turns for every int32
+ *                          position.  D as for HEAD_NORM; a HEAD_NORM in front runs in the same pass.
+ *   ATTENTION(q, k, v [, starts]) attrs {heads, kv_heads = heads, causal = 1, window = 0, scale = 0, sequences = 1}
+ *                          q [T, heads*D], k, v [T, kv_heads*D], y like q; D a multiple of 8, at most 128.  Every row i of
+ *                          a query head sees the rows j of its sequence (causal: j <= i; window > 0, causal only:
+ *                          i - j < window) in key head h / (heads / kv_heads):
+ *                          y = sum_j softmax_j(scale q_i . k_j) v_j, scale 1/sqrt(D) where it is given as 0.  The rows are
+ *                          `sequences` sequences of equal length, or sequence s has rows starts[s] .. starts[s+1] - 1
+ *                          (starts int32 [S+1], ascending; sequences may be empty; rows of no sequence get 0 and pass no
+ *                          gradient; starts out of order or range are cut to it and set the function status to
+ *                          DRAGON_ERR_INVALID_ARG).  Operands are consumed as bf16, probabilities are rounded to bf16 for
+ *                          their product; statistics and sums are fp32.
+ *   CACHE_WRITE(cache, rows, pages, lengths [, starts]) attrs {page}   cache' = the cache with the rows of new tokens in their
+ *                          places.  cache [pages_in_pool * page, C], rows [T, C], the same type (f32 or bf16), C a multiple of 8; page a power of
+ *                          two of 16 or more; pages int32 [S, P], lengths int32 [S].  Sequence s has lengths[s] tokens, its
+ *                          new rows (rows s T/S .. of rows, or as `starts` says) are the last of them: row i of n has
+ *                          position p = lengths[s] - n + i and place pages[s, p / page] * page + p % page.  A negative
+ *                          position (padding in front) writes nothing; nor does a position behind P pages or a page
+ *                          number outside of the pool, which set the function status to DRAGON_ERR_INVALID_ARG.  Fetching
+ *                          cache' into the very memory that was fed as cache (dragon_function_can_alias) writes the rows
+ *                          in place; otherwise the cache is copied first.
+ *   PAGED_ATTENTION(q, kcache, vcache, pages, lengths [, starts]) attrs {heads, kv_heads = heads, page, window = 0, scale = 0}
+ *                          q [T, heads*D], kcache, vcache bf16 [pages_in_pool * page, kv_heads*D] that hold every token,
+ *                          the new ones too; the table as for CACHE_WRITE; y like q.  The row at position p sees positions
+ *                          0 .. p (window > 0: the last `window` of them); one at a negative position, or of no sequence,
+ *                          gets 0.  Pages outside of the pool count as zeros and set the status, as above.
+ * RMS_NORM, GATED_SCAN, HEAD_NORM, ROTATE and ATTENTION have gradients (with respect to h, g; gate, x, h0; x, g; x; q, k, v).  A
+ * gradient chain through BLOCK_SCALE, QUANTIZE, SCALED_INNER_PRODUCT, GLOBAL_NORM, CLIP_BY_NORM, CACHE_WRITE or PAGED_ATTENTION is
+ * DRAGON_ERR_UNSUPPORTED at dragon_function.
  *
  *   OPAQUE                 an operator the library knows only as an edge set: any number of inputs
  *                          and of outputs (Sec. 2.2: an edge from every input to every output), output
@@ -111,7 +147,9 @@ enum {
   DRAGON_OP_RMS_NORM = 17, DRAGON_OP_BLOCK_SCALE = 18, DRAGON_OP_QUANTIZE = 19,
   DRAGON_OP_SCALED_INNER_PRODUCT = 20, DRAGON_OP_GLOBAL_NORM = 21, DRAGON_OP_CLIP_BY_NORM = 22,
   DRAGON_OP_GATED_SCAN = 23,
-  DRAGON_OP_COUNT_ = 24
+  DRAGON_OP_HEAD_NORM = 24, DRAGON_OP_ROTATE = 25, DRAGON_OP_ATTENTION = 26,
+  DRAGON_OP_CACHE_WRITE = 27, DRAGON_OP_PAGED_ATTENTION = 28,
+  DRAGON_OP_COUNT_ = 29
 };
 
 /* ---- graph capture (Sec. 2.1: tensors are nodes; an operator connects each of its inputs
@@ -140,6 +178,13 @@ dragon_id dragon_add_op(dragon_graph_t* g, int op_type, const dragon_id* in, int
  * chain to any objective.  Gradient tensors can be fetched but not consumed by operators. */
 int dragon_add_grad(dragon_graph_t* g, const dragon_id* objs, int n_obj, const dragon_id* wrts, int n_wrt,
                     dragon_id* out_grad_tensor_ids);
+
+/* The same with a type for every gradient tensor: dtypes: host array of n_wrt types, DRAGON_F32 or DRAGON_BF16 (NULL: all
+ * DRAGON_F32, as dragon_add_grad).  A bf16 gradient is rounded once more where it is written: what an operator's own kernel
+ * computes in bf16 anyway (the gradients of InnerProduct's and Attention's activations on their way) then takes half the
+ * bytes. */
+int dragon_add_grad_typed(dragon_graph_t* g, const dragon_id* objs, int n_obj, const dragon_id* wrts, int n_wrt,
+                          const int* dtypes, dragon_id* out_grad_tensor_ids);
 
 int dragon_graph_num_tensors(const dragon_graph_t* g);
 int dragon_graph_num_ops(const dragon_graph_t* g);
@@ -187,7 +232,8 @@ int dragon_function_workspace_tensors(const dragon_function_t* f, int64_t* out, 
  * given the very same device pointer as feed position `input` in dragon_run(), 0 if not, a negative
  * code for bad positions.  It is 1 when the function is nothing but GlobalNorm and one norm's ClipByNorm, `input` is a tensor
  * that is clipped once and is not the norm itself, and `output` its clipped form of the same type (the launch that
- * overwrites it is behind the one that sums it).  Otherwise it is 1 exactly when the function is a single elementwise launch over a
+ * overwrites it is behind the one that sums it).  It is 1 when `input` is the cache of a CacheWrite, `output` its result, and nothing
+ * reads `input` from that step on (only the new rows are then written).  Otherwise it is 1 exactly when the function is a single elementwise launch over a
  * flat domain, both tensors have the domain's shape and the same type, and the program reads the
  * input for the last time before it first writes the output: every thread then overwrites only
  * elements it has already read (the copy of a tile that is fetched ahead of time is never a tile that

@@ -24,6 +24,11 @@ tensor per operator, no fusion, no reordering.
   ScaledInnerProduct(Xq, sx, Wq, sw)  (Xq * sx) @ (Wq * sw)^T with the scales spread over their blocks
   GlobalNorm(t...)   sqrt of the sum of all squares; ClipByNorm(t, norm) = t * min(1, limit / norm)
   GatedScan(gate, x [, h0] [, reset])  row by row h = f*h + (1-f)*x, f = sigmoid(gate)
+  HeadNorm(x, g)     every head of len(g) elements over its root mean square, times g
+  Rotate(x, positions)  pairs of every head turned by position * frequency (the numbers: include/dragon.h)
+  Attention(q, k, v [, starts])  softmax(scale q k^T) v inside every sequence, head by head (operands rounded to bf16)
+  CacheWrite(cache, rows, pages, lengths [, starts])  the cache with the new rows in their places
+  PagedAttention(q, kcache, vcache, pages, lengths [, starts])  the new rows of every sequence over its pages
 
 Gradient rules (dy = gradient of the output): Add (dy,dy); Sub (dy,-dy);
 Mul (dy*b, dy*a); Div (dy/(1+|b|), -dy*a*sgn(b)/(1+|b|)^2) with sgn(0)=0;
@@ -110,8 +115,125 @@ def _scan(op, ins):
     return out, before
 
 
+def _numbers(op, defaults):
+    given = list(op.get("attrs") or [])
+    return given + list(defaults)[len(given):]
+
+
+def rotation(op, cols, positions, dtype=np.float64):
+    """(cos, sin) [rows, pairs] with the amplitude, and the elements of a head that are first and second of a pair."""
+    heads, dims, interleaved, base, factor, low, high, original, amplitude = _numbers(op, [1, 0, 0, 10000.0, 1.0, 0.0, 0.0, 0.0, 1.0])
+    dims = int(dims) or cols // int(heads)
+    i = np.arange(dims // 2)
+    f = np.asarray(base, np.longdouble) ** (-2 * i.astype(np.longdouble) / dims)
+    keep = np.zeros(dims // 2)
+    if original > 0:
+        turns = original * f / (2 * np.pi)
+        keep = np.clip((turns - low) / (high - low), 0, 1) if high > low else (turns >= low).astype(np.float64)
+    angle = positions.astype(np.longdouble)[:, None] * (f * (keep + (1 - keep) / factor))
+    first = 2 * i if interleaved else i
+    second = first + 1 if interleaved else i + dims // 2
+    return (amplitude * np.cos(angle)).astype(dtype), (amplitude * np.sin(angle)).astype(dtype), first, second
+
+
+def _rotate(op, x, positions, back=False):
+    heads = int(op["attrs"][0])
+    c, s, first, second = rotation(op, x.shape[1], positions, x.dtype)
+    if back:
+        s = -s
+    h = x.reshape(x.shape[0], heads, -1)
+    out = h.copy()
+    a, b = h[..., first], h[..., second]
+    out[..., first] = a * c[:, None] - b * s[:, None]
+    out[..., second] = b * c[:, None] + a * s[:, None]
+    return out.reshape(x.shape)
+
+
+def sequence_rows(rows, sequences, starts):
+    """[first, last) of every sequence."""
+    if starts is None:
+        return [(s * (rows // sequences), (s + 1) * (rows // sequences)) for s in range(sequences)]
+    return [(int(a), int(b)) for a, b in zip(starts[:-1], starts[1:])]
+
+
+def attention_parts(op, ins, bf16=True):
+    """For every sequence and query head: (rows, columns of the head, columns of its key head, probabilities, scale)."""
+    heads, kv_heads, causal, window, scale, sequences = _numbers(op, [1, 0, 1, 0, 0.0, 1])
+    heads, kv_heads = int(heads), int(kv_heads) or int(heads)
+    q, k = ins[0], ins[1]
+    width = q.shape[1] // heads
+    scale = scale or 1 / np.sqrt(width)
+    for a, b in sequence_rows(q.shape[0], int(sequences), ins[3] if len(ins) > 3 else None):
+        i = np.arange(b - a)
+        seen = np.ones((b - a, b - a), bool)
+        if causal:
+            seen &= i[:, None] >= i
+        if window:
+            seen &= i[:, None] - i < window
+        for h in range(heads):
+            mine, theirs = slice(h * width, (h + 1) * width), slice(h // (heads // kv_heads) * width, (h // (heads // kv_heads) + 1) * width)
+            x = np.where(seen, scale * (q[a:b, mine] @ k[a:b, theirs].T), -np.inf)
+            e = np.exp(x - x.max(axis=1, keepdims=True)) if b > a else x
+            yield slice(a, b), mine, theirs, e / e.sum(axis=1, keepdims=True), scale
+
+
+def cache_places(page, rows, pool, pages, lengths, starts):
+    """For every row of the new tokens (sequence, position), and the row of the cache it has, -1 for none."""
+    out = [(-1, -1, -1)] * rows
+    for s, (a, b) in enumerate(sequence_rows(rows, len(lengths), starts)):
+        for r in range(a, b):
+            p = int(lengths[s]) - (b - a) + r - a
+            ok = 0 <= p < pages.shape[1] * page and 0 <= pages[s, p // page] < pool // page
+            out[r] = (s, p, int(pages[s, p // page]) * page + p % page if ok else -1)
+    return out
+
+
+def paged_parts(op, ins):
+    """For every new row and query head that sees anything: (row, columns, columns of the key head, rows of the cache, probabilities)."""
+    heads, kv_heads, page, window, scale = _numbers(op, [1, 0, 16, 0, 0.0])
+    heads, kv_heads, page = int(heads), int(kv_heads) or int(heads), int(page)
+    q, kc, pages, lengths = ins[0], ins[1], ins[3], ins[4]
+    width = q.shape[1] // heads
+    scale = scale or 1 / np.sqrt(width)
+    for r, (s, p, _) in enumerate(cache_places(page, q.shape[0], kc.shape[0], pages, lengths, ins[5] if len(ins) > 5 else None)):
+        if p < 0:
+            continue
+        j = np.arange(max(0, p - int(window) + 1) if window else 0, p + 1)
+        at = pages[s, j // page] * page + j % page
+        for h in range(heads):
+            mine, theirs = slice(h * width, (h + 1) * width), slice(h // (heads // kv_heads) * width, (h // (heads // kv_heads) + 1) * width)
+            x = scale * (kc[at, theirs] @ q[r, mine])
+            e = np.exp(x - x.max())
+            yield r, mine, theirs, at, e / e.sum()
+
+
 def _forward(op, ins, dtype, bf16_contraction=True):
     t = op["type"]
+    if t == "HeadNorm":
+        x = ins[0].reshape(ins[0].shape[0], -1, ins[1].shape[0])
+        return (x / np.sqrt((x ** 2).mean(axis=-1, keepdims=True) + _attr(op, 1e-6)) * ins[1]).reshape(ins[0].shape)
+    if t == "Rotate":
+        return _rotate(op, ins[0], ins[1])
+    if t == "Attention":
+        rb = round_bf16 if bf16_contraction else (lambda a: a)
+        ins = [rb(a) for a in ins[:3]] + list(ins[3:])
+        y = np.zeros_like(ins[0])
+        for rows, mine, theirs, p, _ in attention_parts(op, ins):
+            y[rows, mine] = p @ ins[2][rows, theirs]
+        return y
+    if t == "CacheWrite":
+        out = ins[0].copy()
+        places = cache_places(int(_attr(op)), ins[1].shape[0], out.shape[0], ins[2], ins[3], ins[4] if len(ins) > 4 else None)
+        for r, (_, _, at) in enumerate(places):
+            if at >= 0:
+                out[at] = ins[1][r]
+        return out
+    if t == "PagedAttention":
+        q = round_bf16(ins[0]) if bf16_contraction else ins[0]
+        y = np.zeros_like(q)
+        for r, mine, theirs, at, p in paged_parts(op, [q] + list(ins[1:])):
+            y[r, mine] = p @ ins[2][at, theirs]
+        return y
     if t == "RMSNorm":
         return ins[0] / np.sqrt((ins[0] ** 2).mean(axis=-1, keepdims=True) + _attr(op, 1e-6)) * ins[1]
     if t == "BlockScale":
@@ -176,7 +298,30 @@ def _backward(op, ins, out, dy, pos, bf16_contraction=True):
     """Gradients with respect to the operand positions in ``pos`` (un-reduced, operand-broadcast)."""
     t = op["type"]
     g = {}
-    if t == "RMSNorm":
+    if t == "HeadNorm":
+        x = ins[0].reshape(ins[0].shape[0], -1, ins[1].shape[0])
+        r = 1 / np.sqrt((x ** 2).mean(axis=-1, keepdims=True) + _attr(op, 1e-6))
+        dy = dy.reshape(x.shape)
+        for p in pos:
+            d = dy * ins[1]
+            g[p] = (r * d - x * r ** 3 * (d * x).mean(axis=-1, keepdims=True)).reshape(ins[0].shape) if p == 0 else (dy * x * r).sum(axis=(0, 1))
+    elif t == "Rotate":
+        g[0] = _rotate(op, dy, ins[1], back=True)
+    elif t == "Attention":
+        rb = round_bf16 if bf16_contraction else (lambda a: a)
+        q, k, v = (rb(a) for a in ins[:3])
+        dy = rb(dy)
+        d = [np.zeros_like(q), np.zeros_like(k), np.zeros_like(v)]
+        for rows, mine, theirs, p, scale in attention_parts(op, [q, k, v] + list(ins[3:])):
+            do = dy[rows, mine]
+            dp = do @ v[rows, theirs].T
+            ds = scale * p * (dp - (p * dp).sum(axis=1, keepdims=True))
+            d[0][rows, mine] = ds @ k[rows, theirs]
+            d[1][rows, theirs] += ds.T @ q[rows, mine]
+            d[2][rows, theirs] += p.T @ do
+        for p in pos:
+            g[p] = d[p]
+    elif t == "RMSNorm":
         h, gain = ins
         r = 1 / np.sqrt((h ** 2).mean(axis=-1, keepdims=True) + _attr(op, 1e-6))
         for p in pos:

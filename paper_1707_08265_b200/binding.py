@@ -19,7 +19,8 @@ DTYPES = {"f32": F32, "bf16": BF16, "i32": I32, "f8e4m3": F8E4M3}
 OPS = {"Add": 0, "Sub": 1, "Mul": 2, "Div": 3, "Sin": 4, "Exp": 5, "Tanh": 6, "Sigmoid": 7, "ReLU": 8,
        "Sum": 9, "Mean": 10, "InnerProduct": 11, "BiasAdd": 12, "SoftmaxCrossEntropy": 13, "Sqrt": 14,
        "Reciprocal": 15, "Opaque": 16, "RMSNorm": 17, "BlockScale": 18, "Quantize": 19, "ScaledInnerProduct": 20,
-       "GlobalNorm": 21, "ClipByNorm": 22, "GatedScan": 23}
+       "GlobalNorm": 21, "ClipByNorm": 22, "GatedScan": 23, "HeadNorm": 24, "Rotate": 25, "Attention": 26, "CacheWrite": 27,
+       "PagedAttention": 28}
 
 _lib = None
 
@@ -32,6 +33,8 @@ _SIGNATURES = {
                                    _c.c_int, _c.POINTER(_c.c_double), _c.c_int]),
     "dragon_add_grad": (_c.c_int, [_c.c_void_p, _c.POINTER(_c.c_int32), _c.c_int, _c.POINTER(_c.c_int32), _c.c_int,
                                    _c.POINTER(_c.c_int32)]),
+    "dragon_add_grad_typed": (_c.c_int, [_c.c_void_p, _c.POINTER(_c.c_int32), _c.c_int, _c.POINTER(_c.c_int32), _c.c_int,
+                                         _c.POINTER(_c.c_int), _c.POINTER(_c.c_int32)]),
     "dragon_graph_num_tensors": (_c.c_int, [_c.c_void_p]),
     "dragon_graph_num_ops": (_c.c_int, [_c.c_void_p]),
     "dragon_function": (_c.c_void_p, [_c.c_void_p, _c.POINTER(_c.c_int32), _c.c_int, _c.POINTER(_c.c_int32), _c.c_int]),
@@ -146,9 +149,13 @@ class Graph:
             raise DragonError(r, "dragon_add_op")
         return r
 
-    def add_grad(self, objs, wrts):
+    def add_grad(self, objs, wrts, dtypes=None):
+        """dtypes: the gradients' types (F32 or BF16), or None for F32 throughout."""
         out = (_c.c_int32 * max(1, len(wrts)))()
-        r = lib().dragon_add_grad(self.h, _ids(objs), len(objs), _ids(wrts), len(wrts), out)
+        if dtypes is not None and len(dtypes) != len(wrts):
+            raise ValueError("add_grad: one type for each derivative target")
+        types = None if dtypes is None else (_c.c_int * max(1, len(wrts)))(*dtypes)
+        r = lib().dragon_add_grad_typed(self.h, _ids(objs), len(objs), _ids(wrts), len(wrts), types, out)
         if r < 0:
             raise DragonError(r, "dragon_add_grad")
         return list(out[:len(wrts)])
@@ -178,7 +185,7 @@ class Graph:
             if t in grad_ids:
                 if t in stage_first:
                     st = stage_first[t]
-                    got = g.add_grad(st["objs"], st["wrts"])
+                    got = g.add_grad(st["objs"], st["wrts"], [DTYPES[desc["tensors"][i]["dtype"]] for i in st["grad_ids"]])
                     assert got == list(st["grad_ids"]), (got, st["grad_ids"])
                 continue
             tid = g.add_tensor(ti["name"], DTYPES[ti["dtype"]], ti["shape"])

@@ -35,6 +35,12 @@ cudaError_t launch_norm_and_clip(const StepRun& r);
 cudaError_t launch_scan(const StepRun& r);
 cudaError_t launch_scan_bwd(const StepRun& r);
 int launch_gemm_e4m3(const StepRun& r);   // a DRAGON_* code, message set
+cudaError_t launch_head(const StepRun& r);
+cudaError_t launch_head_bwd(const StepRun& r);
+cudaError_t launch_cache_write(const StepRun& r);
+int launch_attention(const StepRun& r);      // these three: a DRAGON_* code, message set
+int launch_attention_bwd(const StepRun& r);
+int launch_paged_attention(const StepRun& r);
 }  // namespace dragon
 
 using namespace dragon;
@@ -59,7 +65,47 @@ int resolve_attr(int type, const double* attrs, int n_attrs, double* out) {
   return DRAGON_OK;
 }
 
-int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, double attr, Shape* out) {
+// The numbers of an operator that takes several: those given, then the defaults (what depends on the operands' shapes is 0 until
+// infer_shape has seen them)
+int resolve_numbers(int type, const double* attrs, int n_attrs, std::vector<double>* num) {
+  int least = 0;
+  switch (type) {
+    case DRAGON_OP_HEAD_NORM: *num = {1e-6}; break;
+    case DRAGON_OP_ROTATE: *num = {0.0, 0.0, 0.0, 10000.0, 1.0, 0.0, 0.0, 0.0, 1.0}; least = 1; break;
+    case DRAGON_OP_ATTENTION: *num = {0.0, 0.0, 1.0, 0.0, 0.0, 1.0}; least = 1; break;
+    case DRAGON_OP_CACHE_WRITE: *num = {0.0}; least = 1; break;
+    case DRAGON_OP_PAGED_ATTENTION: *num = {0.0, 0.0, 0.0, 0.0, 0.0}; least = 3; break;
+    default: return DRAGON_OK;
+  }
+  if (n_attrs < least || n_attrs > (int)num->size() || (n_attrs > 0 && !attrs)) {
+    set_error("dragon_add_op: operator type %d takes %d to %d numbers", type, least, (int)num->size());
+    return DRAGON_ERR_INVALID_ARG;
+  }
+  for (int i = 0; i < n_attrs; ++i) (*num)[i] = attrs[i];
+  for (double v : *num)
+    if (!std::isfinite(v)) { set_error("dragon_add_op: a number of operator type %d is not finite", type); return DRAGON_ERR_INVALID_ARG; }
+  return DRAGON_OK;
+}
+
+bool whole(double v, double lo, double hi) { return v >= lo && v <= hi && v == std::floor(v); }
+
+// the table of a paged cache behind the first operands: pages [S,P], lengths [S] and, where given, starts [S+1]
+int check_table(const Graph& g, const char* who, const dragon_id* in, int n_in, int first, int64_t rows) {
+  auto T = [&](int p) -> const TensorInfo& { return g.tensors[in[p]]; };
+  if (n_in != first + 2 && n_in != first + 3) { set_error("%s takes pages, lengths and optionally starts behind its tensors", who); return DRAGON_ERR_INVALID_ARG; }
+  for (int p = first; p < n_in; ++p)
+    if (T(p).dtype != DRAGON_I32) { set_error("%s: pages, lengths and starts are int32", who); return DRAGON_ERR_DTYPE; }
+  const Shape &pages = T(first).shape, &lengths = T(first + 1).shape;
+  if (pages.rank != 2 || lengths.rank != 1 || lengths.d[0] != pages.d[0]) { set_error("%s needs pages[S,P] and lengths[S]", who); return DRAGON_ERR_SHAPE; }
+  if (n_in == first + 3 && (T(first + 2).shape.rank != 1 || T(first + 2).shape.d[0] != pages.d[0] + 1)) { set_error("%s: starts must be [S + 1]", who); return DRAGON_ERR_SHAPE; }
+  if (n_in == first + 2 && rows % pages.d[0]) { set_error("%s: without starts the rows are a multiple of the sequences", who); return DRAGON_ERR_SHAPE; }
+  if (pages.d[0] > (1 << 24) || pages.d[1] > (1 << 27) || rows > kMaxAttentionRows) { set_error("%s: too many sequences, pages or rows", who); return DRAGON_ERR_UNSUPPORTED; }
+  return DRAGON_OK;
+}
+
+bool valid_page(double page) { return whole(page, 16.0, 1 << 20) && ((int64_t)page & ((int64_t)page - 1)) == 0; }
+
+int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, double attr, std::vector<double>* num, Shape* out) {
   auto T = [&](int p) -> const TensorInfo& { return g.tensors[in[p]]; };
   auto is_float = [&](int p) { return T(p).dtype == DRAGON_F32 || T(p).dtype == DRAGON_BF16; };
   switch (type) {
@@ -171,6 +217,104 @@ int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, double 
       *out = a;
       return DRAGON_OK;
     }
+    case DRAGON_OP_HEAD_NORM: {
+      if (n_in != 2) { set_error("HeadNorm takes 2 inputs"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || !is_float(1)) { set_error("HeadNorm takes f32/bf16 tensors"); return DRAGON_ERR_DTYPE; }
+      const Shape &x = T(0).shape, &gain = T(1).shape;
+      if (x.rank != 2 || gain.rank != 1 || x.d[1] % gain.d[0]) { set_error("HeadNorm needs x[T,H*D] and g[D]"); return DRAGON_ERR_SHAPE; }
+      if ((*num)[0] < 0.0 || !((float)(*num)[0] <= std::numeric_limits<float>::max())) { set_error("HeadNorm: eps must not be negative"); return DRAGON_ERR_INVALID_ARG; }
+      if ((gain.d[0] & 7) || gain.d[0] > kMaxRotatedWidth || x.d[0] > kMaxAttentionRows || x.d[1] > kMaxRowLength) {
+        set_error("HeadNorm: heads are a multiple of 8 wide, at most %d, of at most %lld rows", kMaxRotatedWidth, (long long)kMaxAttentionRows);
+        return DRAGON_ERR_UNSUPPORTED;
+      }
+      *out = x;
+      return DRAGON_OK;
+    }
+    case DRAGON_OP_ROTATE: {
+      if (n_in != 2) { set_error("Rotate takes x and positions"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || T(1).dtype != DRAGON_I32) { set_error("Rotate takes an f32/bf16 tensor and int32 positions"); return DRAGON_ERR_DTYPE; }
+      const Shape &x = T(0).shape, &pos = T(1).shape;
+      std::vector<double>& n = *num;
+      if (!whole(n[0], 1.0, 65535.0)) { set_error("Rotate: the number of heads is missing or out of range"); return DRAGON_ERR_INVALID_ARG; }
+      if (x.rank != 2 || x.d[1] % (int64_t)n[0] || pos.rank != 1 || pos.d[0] != x.d[0]) { set_error("Rotate needs x[T,heads*D] and positions[T]"); return DRAGON_ERR_SHAPE; }
+      const int64_t width = x.d[1] / (int64_t)n[0];
+      if ((width & 7) || width > kMaxRotatedWidth || x.d[0] > kMaxAttentionRows || x.d[1] > kMaxRowLength) {
+        set_error("Rotate: heads are a multiple of 8 wide, at most %d, of at most %lld rows", kMaxRotatedWidth, (long long)kMaxAttentionRows);
+        return DRAGON_ERR_UNSUPPORTED;
+      }
+      if (n[1] == 0.0) n[1] = (double)width;
+      if (!whole(n[1] / 2, 1.0, (double)width / 2) || !whole(n[2], 0.0, 1.0) || n[3] < 1.0 || n[4] < 1.0 || n[5] < 0.0 || n[6] < n[5] || n[7] < 0.0 ||
+          std::fabs(n[8]) > std::numeric_limits<float>::max()) {
+        set_error("Rotate: dims even and within the head, interleaved 0 or 1, base and factor at least 1, 0 <= low <= high, original at least 0");
+        return DRAGON_ERR_INVALID_ARG;
+      }
+      *out = x;
+      return DRAGON_OK;
+    }
+    case DRAGON_OP_ATTENTION: {
+      if (n_in != 3 && n_in != 4) { set_error("Attention takes q, k, v and optionally starts"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || !is_float(1) || !is_float(2)) { set_error("Attention takes f32/bf16 tensors"); return DRAGON_ERR_DTYPE; }
+      if (n_in == 4 && T(3).dtype != DRAGON_I32) { set_error("Attention: starts are int32"); return DRAGON_ERR_DTYPE; }
+      const Shape &q = T(0).shape, &k = T(1).shape, &v = T(2).shape;
+      std::vector<double>& n = *num;
+      if (n[1] == 0.0) n[1] = n[0];
+      if (!whole(n[0], 1.0, 65535.0) || !whole(n[1], 1.0, n[0]) || (int64_t)n[0] % (int64_t)n[1] || !whole(n[2], 0.0, 1.0) || !whole(n[3], 0.0, 1 << 30) ||
+          (n[3] > 0.0 && n[2] == 0.0) || n[4] < 0.0 || !((float)n[4] <= std::numeric_limits<float>::max()) || !whole(n[5], 1.0, 2147483647.0) || (n_in == 4 && n[5] != 1.0)) {
+        set_error("Attention: heads a multiple of kv_heads, causal 0 or 1, a window only where causal, scale at least 0, sequences only without starts");
+        return DRAGON_ERR_INVALID_ARG;
+      }
+      if (q.rank != 2 || k.rank != 2 || v != k || k.d[0] != q.d[0] || q.d[1] % (int64_t)n[0] || k.d[1] != q.d[1] / (int64_t)n[0] * (int64_t)n[1] || q.d[0] % (int64_t)n[5]) {
+        set_error("Attention needs q[T,heads*D], k[T,kv_heads*D], v like k, with T a multiple of the number of sequences");
+        return DRAGON_ERR_SHAPE;
+      }
+      if (n_in == 4 && (T(3).shape.rank != 1 || T(3).shape.d[0] < 2)) { set_error("Attention: starts must be [S + 1]"); return DRAGON_ERR_SHAPE; }
+      const int64_t width = q.d[1] / (int64_t)n[0];
+      if ((width & 7) || width > kMaxHeadWidth || q.d[0] > kMaxAttentionRows || (n_in == 4 && T(3).shape.d[0] > (1 << 24))) {
+        set_error("Attention: heads are a multiple of 8 wide, at most %d, of at most %lld rows", kMaxHeadWidth, (long long)kMaxAttentionRows);
+        return DRAGON_ERR_UNSUPPORTED;
+      }
+      if (n[4] == 0.0) n[4] = 1.0 / std::sqrt((double)width);
+      *out = q;
+      return DRAGON_OK;
+    }
+    case DRAGON_OP_CACHE_WRITE: {
+      if (n_in < 4) { set_error("CacheWrite takes cache, rows, pages, lengths and optionally starts"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || T(1).dtype != T(0).dtype) { set_error("CacheWrite takes a cache and rows of one type, f32 or bf16"); return DRAGON_ERR_DTYPE; }
+      const Shape &cache = T(0).shape, &rows = T(1).shape;
+      if (!valid_page((*num)[0])) { set_error("CacheWrite: the page must be a power of two of 16 or more"); return DRAGON_ERR_INVALID_ARG; }
+      if (cache.rank != 2 || rows.rank != 2 || rows.d[1] != cache.d[1] || cache.d[0] % (int64_t)(*num)[0]) {
+        set_error("CacheWrite needs cache[pages*page,C] and rows[T,C]");
+        return DRAGON_ERR_SHAPE;
+      }
+      const int rc = check_table(g, "CacheWrite", in, n_in, 2, rows.d[0]);
+      if (rc != DRAGON_OK) return rc;
+      if ((cache.d[1] & 7) || cache.d[0] > 0x7fffffffLL - (1 << 20) || cache.d[1] > kMaxRowLength) { set_error("CacheWrite: rows are a multiple of 8 long, and at most 2^31 of them"); return DRAGON_ERR_UNSUPPORTED; }
+      *out = cache;
+      return DRAGON_OK;
+    }
+    case DRAGON_OP_PAGED_ATTENTION: {
+      if (n_in < 5) { set_error("PagedAttention takes q, kcache, vcache, pages, lengths and optionally starts"); return DRAGON_ERR_INVALID_ARG; }
+      if (!is_float(0) || T(1).dtype != DRAGON_BF16 || T(2).dtype != DRAGON_BF16) { set_error("PagedAttention takes an f32/bf16 tensor and bf16 caches"); return DRAGON_ERR_DTYPE; }
+      const Shape &q = T(0).shape, &k = T(1).shape, &v = T(2).shape;
+      std::vector<double>& n = *num;
+      if (n[1] == 0.0) n[1] = n[0];
+      if (!whole(n[0], 1.0, 65535.0) || !whole(n[1], 1.0, n[0]) || (int64_t)n[0] % (int64_t)n[1] || !valid_page(n[2]) || !whole(n[3], 0.0, 1 << 30) || n[4] < 0.0 ||
+          !((float)n[4] <= std::numeric_limits<float>::max())) {
+        set_error("PagedAttention: heads a multiple of kv_heads, page a power of two of 16 or more, window and scale at least 0");
+        return DRAGON_ERR_INVALID_ARG;
+      }
+      if (q.rank != 2 || k.rank != 2 || v != k || q.d[1] % (int64_t)n[0] || k.d[1] != q.d[1] / (int64_t)n[0] * (int64_t)n[1] || k.d[0] % (int64_t)n[2]) {
+        set_error("PagedAttention needs q[T,heads*D], kcache[pages*page,kv_heads*D], vcache like kcache");
+        return DRAGON_ERR_SHAPE;
+      }
+      const int rc = check_table(g, "PagedAttention", in, n_in, 3, q.d[0]);
+      if (rc != DRAGON_OK) return rc;
+      const int64_t width = q.d[1] / (int64_t)n[0];
+      if ((width & 7) || width > kMaxHeadWidth || k.d[0] > 0x7fffffffLL - (1 << 20)) { set_error("PagedAttention: heads are a multiple of 8 wide, at most %d, and a cache has at most 2^31 rows", kMaxHeadWidth); return DRAGON_ERR_UNSUPPORTED; }
+      if (n[4] == 0.0) n[4] = 1.0 / std::sqrt((double)width);
+      *out = q;
+      return DRAGON_OK;
+    }
     default:
       set_error("unknown operator type %d", type);
       return DRAGON_ERR_INVALID_ARG;
@@ -233,14 +377,17 @@ dragon_id dragon_add_op(dragon_graph_t* g, int op_type, const dragon_id* in, int
     if (to.dtype == DRAGON_I32) { set_error("dragon_add_op: operators produce f32/bf16 tensors"); return DRAGON_ERR_DTYPE; }
   }
   double attr = 0.0;
+  std::vector<double> num;
   if (op_type != DRAGON_OP_OPAQUE) {
     const TensorInfo& to = g->g.tensors[out[0]];
     Shape s;
     int rc = resolve_attr(op_type, attrs, n_attrs, &attr);
-    if (rc == DRAGON_OK) rc = infer_shape(g->g, op_type, in, n_in, attr, &s);
+    if (rc == DRAGON_OK) rc = resolve_numbers(op_type, attrs, n_attrs, &num);
+    if (rc == DRAGON_OK) rc = infer_shape(g->g, op_type, in, n_in, attr, &num, &s);
     if (rc != DRAGON_OK) return rc;
     if ((op_type == DRAGON_OP_QUANTIZE) != (to.dtype == DRAGON_F8E4M3)) { set_error("dragon_add_op: Quantize, and nothing else, produces an e4m3 tensor"); return DRAGON_ERR_DTYPE; }
     if ((op_type == DRAGON_OP_BLOCK_SCALE || op_type == DRAGON_OP_GLOBAL_NORM) && to.dtype != DRAGON_F32) { set_error("dragon_add_op: scales and norms are f32 tensors"); return DRAGON_ERR_DTYPE; }
+    if (op_type == DRAGON_OP_CACHE_WRITE && to.dtype != g->g.tensors[in[0]].dtype) { set_error("dragon_add_op: CacheWrite's result has the cache's type"); return DRAGON_ERR_DTYPE; }
     if (s != to.shape) { set_error("dragon_add_op: declared shape of '%s' differs from the inferred one", to.name.c_str()); return DRAGON_ERR_SHAPE; }
   }
   OpInfo op;
@@ -248,6 +395,7 @@ dragon_id dragon_add_op(dragon_graph_t* g, int op_type, const dragon_id* in, int
   op.in.assign(in, in + n_in);
   op.out.assign(out, out + n_out);
   op.attr = attr;
+  op.num = num;
   g->g.ops.push_back(op);
   for (int i = 0; i < n_in; ++i) g->g.tensors[in[i]].consumed = true;
   for (int j = 0; j < n_out; ++j) g->g.tensors[out[j]].producer = (int)g->g.ops.size() - 1;
@@ -256,6 +404,11 @@ dragon_id dragon_add_op(dragon_graph_t* g, int op_type, const dragon_id* in, int
 
 int dragon_add_grad(dragon_graph_t* g, const dragon_id* objs, int n_obj, const dragon_id* wrts, int n_wrt,
                     dragon_id* out_grad_tensor_ids) {
+  return dragon_add_grad_typed(g, objs, n_obj, wrts, n_wrt, nullptr, out_grad_tensor_ids);
+}
+
+int dragon_add_grad_typed(dragon_graph_t* g, const dragon_id* objs, int n_obj, const dragon_id* wrts, int n_wrt,
+                          const int* dtypes, dragon_id* out_grad_tensor_ids) {
   if (!g || !objs || !wrts || !out_grad_tensor_ids || n_obj <= 0 || n_wrt <= 0) { set_error("dragon_add_grad: bad argument"); return DRAGON_ERR_INVALID_ARG; }
   GradStage st;
   for (int i = 0; i < n_obj; ++i) {
@@ -266,6 +419,7 @@ int dragon_add_grad(dragon_graph_t* g, const dragon_id* objs, int n_obj, const d
   for (int i = 0; i < n_wrt; ++i) {
     if (!valid_tensor(g, wrts[i]) || g->g.tensors[wrts[i]].grad_stage >= 0) { set_error("dragon_add_grad: bad derivative target id %d", wrts[i]); return DRAGON_ERR_INVALID_ARG; }
     if ((g->g.tensors[wrts[i]].dtype == DRAGON_I32 || g->g.tensors[wrts[i]].dtype == DRAGON_F8E4M3)) { set_error("dragon_add_grad: derivative target must be a float tensor"); return DRAGON_ERR_DTYPE; }
+    if (dtypes && dtypes[i] != DRAGON_F32 && dtypes[i] != DRAGON_BF16) { set_error("dragon_add_grad: a gradient's type is f32 or bf16"); return DRAGON_ERR_DTYPE; }
     st.wrts.push_back(wrts[i]);
   }
   std::vector<uint8_t> G = backward_chain_marks(g->g, st.objs, st.wrts);
@@ -276,7 +430,7 @@ int dragon_add_grad(dragon_graph_t* g, const dragon_id* objs, int n_obj, const d
     TensorInfo t;
     t.name = "grad" + std::to_string(s) + "/" + g->g.tensors[wrts[i]].name;
     while (!g->g.names.insert(t.name).second) t.name += "'";
-    t.dtype = DRAGON_F32;
+    t.dtype = dtypes ? dtypes[i] : DRAGON_F32;
     t.shape = g->g.tensors[wrts[i]].shape;
     t.grad_stage = s;
     t.grad_wrt = wrts[i];
@@ -383,6 +537,7 @@ int dragon_function_can_alias(const dragon_function_t* f, int input, int output)
   if (!f || input < 0 || input >= f->n_in || output < 0 || output >= f->n_out) { set_error("dragon_function_can_alias: bad argument"); return DRAGON_ERR_INVALID_ARG; }
   const Plan& P = f->plan;
   if (!f->not_executable.empty()) return 0;
+  if (std::count(P.in_place.begin(), P.in_place.end(), std::make_pair(input, output))) return 1;
   if (P.steps.size() == 1 && P.steps[0].kind == ST_NORM_CLIP) {
     // every tensor is in registers before the first element is written
     const Step& cs = P.steps[0];
@@ -467,6 +622,9 @@ int dragon_function_num_launches(const dragon_function_t* f) {
     else if (st.kind == ST_NORM_BWD) n += 1 + (st.wr[nb::DGAIN] >= 0 ? 1 : 0);
     else if (st.kind == ST_GNORM) n += launches_of_tensors((int)st.rd.size());
     else if (st.kind == ST_CLIP) n += launches_of_tensors((int)st.wr.size());
+    else if (st.kind == ST_HEAD_BWD) n += 1 + (st.wr[hb::DGAIN] >= 0 ? 1 : 0);
+    else if (st.kind == ST_ATTN_BWD) n += attention_bwd_launches(st);
+    else if (st.kind == ST_PAGED) n += paged_launches(st, f->plan.mems);
     else if (st.kind != ST_COPY) n += 1 + (st.mF >= 0 ? 1 : 0);
   }
   return n;
@@ -698,8 +856,12 @@ int dragon_run(dragon_function_t* f, const void* const* feeds, void* const* fetc
           case ST_NORM_CLIP: e = launch_norm_and_clip(r); break;
           case ST_SCAN: e = launch_scan(r); break;
           case ST_SCAN_BWD: e = launch_scan_bwd(r); break;
+          case ST_HEAD: e = launch_head(r); break;
+          case ST_HEAD_BWD: e = launch_head_bwd(r); break;
+          case ST_CACHE_WRITE: e = launch_cache_write(r); break;
           default: {
-            const int rc = launch_gemm_e4m3(r);
+            const int rc = s.kind == ST_ATTN ? launch_attention(r) : s.kind == ST_ATTN_BWD ? launch_attention_bwd(r)
+                           : s.kind == ST_PAGED ? launch_paged_attention(r) : launch_gemm_e4m3(r);
             if (rc != DRAGON_OK) { f->status_ready = false; return rc; }
           }
         }

@@ -39,6 +39,7 @@ struct OpInfo {
   int type = 0;
   std::vector<int> in, out;
   double attr = 0.0;      // the operator's number (dragon.h: attrs), its default filled in
+  std::vector<double> num;   // the numbers of an operator that takes several (HeadNorm and later types), defaults filled in
 };
 
 // bytes of one element of a tensor type
@@ -47,7 +48,8 @@ inline size_t dtype_bytes(int dtype) { return dtype == DRAGON_F8E4M3 ? 1 : dtype
 // operators through which no gradient is generated
 inline bool has_no_gradient(int type) {
   return type == DRAGON_OP_BLOCK_SCALE || type == DRAGON_OP_QUANTIZE || type == DRAGON_OP_SCALED_INNER_PRODUCT ||
-         type == DRAGON_OP_GLOBAL_NORM || type == DRAGON_OP_CLIP_BY_NORM;
+         type == DRAGON_OP_GLOBAL_NORM || type == DRAGON_OP_CLIP_BY_NORM || type == DRAGON_OP_CACHE_WRITE ||
+         type == DRAGON_OP_PAGED_ATTENTION;
 }
 
 struct GradStage {

@@ -31,6 +31,7 @@ struct Lowerer {
   std::map<int, int> def_item;                // value -> index of the micro-operation that defines it
   std::map<int, int> writer;                  // memory -> index of the item of a kind from IT_NORM on that writes it
   std::map<int, int> scan_item;               // GatedScan operator -> its item
+  std::map<int, int> attn_item;               // Attention operator -> its item
   int err = DRAGON_OK;
 
   Lowerer(const Graph& g_, const PruneResult& pr_, Plan* p) : g(g_), pr(pr_), plan(p) {}
@@ -363,15 +364,88 @@ struct Lowerer {
     fval[o] = new_val(VK_MEM, s, mH);
   }
 
+  // HeadNorm, and Rotate in the pass of the HeadNorm that makes its operand
+  std::vector<double> head_numbers(const OpInfo& op) const {
+    std::vector<double> n(hn::COUNT, 0.0);
+    const int64_t cols = g.tensors[op.in[0]].shape.d[1];
+    if (op.type == DRAGON_OP_HEAD_NORM) {
+      n[hn::EPS] = op.num[0];
+      n[hn::WIDTH] = (double)g.tensors[op.in[1]].shape.d[0];
+    } else {
+      n[hn::WIDTH] = (double)(cols / (int64_t)op.num[0]);
+      std::copy(op.num.begin() + 1, op.num.end(), n.begin() + hn::DIMS);
+    }
+    return n;
+  }
+  void lower_head_norm(const OpInfo& op) {
+    const int o = op.out[0], mX = in_mem(op.in[0]), mG = in_mem(op.in[1]), mU = out_mem(o);
+    const int i = add_item(IT_HEAD, {mX, mG, -1}, {mU, -1}, 0.0);
+    items[i].num = head_numbers(op);
+    items[i].round_dtype = g.tensors[o].dtype;
+    fval[o] = new_val(VK_MEM, g.tensors[o].shape, mU);
+  }
+  void lower_rotate(const OpInfo& op) {
+    const int o = op.out[0], mX = in_mem(op.in[0]), mP = in_mem(op.in[1]), mY = out_mem(o);
+    const std::vector<double> num = head_numbers(op);
+    Item* norm = writer_of(mX, IT_HEAD, hd::U);
+    if (norm && norm->wr[hd::Y] < 0 && norm->num[hn::WIDTH] == num[hn::WIDTH]) {      // (positions are int32, so they are fed)
+      norm->rd[hd::POS] = mP;
+      norm->wr[hd::Y] = mY;
+      std::copy(num.begin() + hn::DIMS, num.end(), norm->num.begin() + hn::DIMS);
+      writer[mY] = writer[mX];
+    } else {
+      const int i = add_item(IT_HEAD, {mX, -1, mP}, {-1, mY}, 0.0);
+      items[i].num = num;
+    }
+    fval[o] = new_val(VK_MEM, g.tensors[o].shape, mY);
+  }
+
+  void lower_attention(int k, const OpInfo& op) {
+    const int o = op.out[0];
+    const Shape& s = g.tensors[o].shape;
+    Shape rows; rows.rank = 2; rows.d[0] = (int64_t)op.num[an::HEADS]; rows.d[1] = s.d[0];
+    std::vector<int> rd;
+    for (int p = 0; p < 3; ++p) rd.push_back(in_mem(op.in[p], DRAGON_BF16));
+    rd.push_back(op.in.size() > 3 ? in_mem(op.in[3]) : -1);
+    const int mY = out_mem(o), mLse = new_mem(MEM_WORK, -1, DRAGON_F32, rows);
+    attn_item[k] = add_item(IT_ATTN, rd, {mY, mLse}, 0.0);
+    items[attn_item[k]].num = op.num;
+    fval[o] = new_val(VK_MEM, s, mY);
+  }
+  void lower_cache_write(const OpInfo& op) {
+    const int o = op.out[0], dtype = g.tensors[o].dtype;
+    const int mC = in_mem(op.in[0], dtype), mR = in_mem(op.in[1], dtype), mO = out_mem(o);
+    const int i = add_item(IT_CACHE_WRITE, {in_mem(op.in[2]), in_mem(op.in[3]), op.in.size() > 4 ? in_mem(op.in[4]) : -1, mC, mR}, {mO}, 0.0);
+    items[i].num = op.num;
+    fval[o] = new_val(VK_MEM, g.tensors[o].shape, mO);
+  }
+  void lower_paged(const OpInfo& op) {
+    const int o = op.out[0];
+    std::vector<int> rd;
+    for (int p = 0; p < 3; ++p) rd.push_back(in_mem(op.in[p], DRAGON_BF16));
+    for (int p = 3; p < 6; ++p) rd.push_back(p < (int)op.in.size() ? in_mem(op.in[p]) : -1);
+    const int mY = out_mem(o);
+    const int i = add_item(IT_PAGED, rd, {mY}, 0.0);
+    items[i].num = op.num;
+    fval[o] = new_val(VK_MEM, g.tensors[o].shape, mY);
+  }
+
+  // whether a gradient of tensor t that the caller asked for is f32
+  bool wanted_in_f32(int s, int t) const {
+    const GradStage& st = g.stages[s];
+    for (size_t j = 0; j < st.wrts.size(); ++j)
+      if (st.wrts[j] == t && g.tensors[st.grad_ids[j]].dtype == DRAGON_F32) return true;
+    return false;
+  }
   // whether the gradient of tensor t reaches a derivative target unchanged (through additions): it is then kept in f32
+  // (unless the target's gradient is bf16 itself)
   bool reaches_target(int s, int t) const {
-    const auto& wr = g.stages[s].wrts;
     std::set<int> seen = {t};
     std::vector<int> todo = {t};
     while (!todo.empty()) {
       const int x = todo.back();
       todo.pop_back();
-      if (std::find(wr.begin(), wr.end(), x) != wr.end()) return true;
+      if (wanted_in_f32(s, x)) return true;
       const int p = g.tensors[x].producer;
       if (p < 0 || (g.ops[p].type != DRAGON_OP_ADD && g.ops[p].type != DRAGON_OP_SUB && g.ops[p].type != DRAGON_OP_BIAS_ADD)) continue;
       for (int i : g.ops[p].in)
@@ -443,6 +517,11 @@ struct Lowerer {
       }
       case DRAGON_OP_CLIP_BY_NORM: lower_clip(op); return;
       case DRAGON_OP_GATED_SCAN: lower_scan(k, op); return;
+      case DRAGON_OP_HEAD_NORM: lower_head_norm(op); return;
+      case DRAGON_OP_ROTATE: lower_rotate(op); return;
+      case DRAGON_OP_ATTENTION: lower_attention(k, op); return;
+      case DRAGON_OP_CACHE_WRITE: lower_cache_write(op); return;
+      case DRAGON_OP_PAGED_ATTENTION: lower_paged(op); return;
       default:
         set_error("operator type %d cannot be lowered", op.type);
         err = DRAGON_ERR_UNSUPPORTED;
@@ -462,7 +541,8 @@ struct Lowerer {
     // scalar factor is narrower); sums over broadcast axes count every element of that shape
     int dy = widen(gy->second, g.tensors[o].shape);
     // a kernel of its own reads dy with its output's extents: where that output is broadcast dy is summed first
-    if (op.type == DRAGON_OP_INNER_PRODUCT || op.type == DRAGON_OP_SOFTMAX_CROSS_ENTROPY || op.type == DRAGON_OP_RMS_NORM || op.type == DRAGON_OP_GATED_SCAN)
+    if (op.type == DRAGON_OP_INNER_PRODUCT || op.type == DRAGON_OP_SOFTMAX_CROSS_ENTROPY || op.type == DRAGON_OP_RMS_NORM || op.type == DRAGON_OP_GATED_SCAN ||
+        op.type == DRAGON_OP_HEAD_NORM || op.type == DRAGON_OP_ROTATE || op.type == DRAGON_OP_ATTENTION)
       dy = summed(dy, g.tensors[o].shape);
     std::vector<bool> want(op.in.size(), false);
     for (size_t p = 0; p < op.in.size(); ++p)
@@ -507,8 +587,7 @@ struct Lowerer {
           int mW = materialise(in(1), DRAGON_BF16, DRAGON_BF16);
           // the gradient of a bf16 activation is kept in bf16 (it feeds the next contraction);
           // a gradient that the caller asked for stays fp32
-          const auto& wr = g.stages[s].wrts;
-          const bool wanted = std::find(wr.begin(), wr.end(), op.in[0]) != wr.end();
+          const bool wanted = wanted_in_f32(s, op.in[0]);
           int mC = gemm(mdY, mW, MEM_WORK, -1,
                         (g.tensors[op.in[0]].dtype == DRAGON_BF16 && !wanted) ? DRAGON_BF16 : DRAGON_F32, false, true);
           add(0, new_val(VK_MEM, plan->mems[mC].shape, mC));
@@ -561,6 +640,42 @@ struct Lowerer {
         if (mdH0 >= 0) add(pH0, new_val(VK_MEM, g.tensors[op.in[pH0]].shape, mdH0));
         break;
       }
+      case DRAGON_OP_ROTATE: {      // the rotation backwards
+        const int mdY = materialise(dy, -1, DRAGON_F32), mdX = grad_mem(s, op.in[0]);
+        const int i = add_item(IT_HEAD_BWD, {-1, -1, in_mem(op.in[1]), mdY}, {mdX, -1}, 0.0);
+        items[i].num = head_numbers(op);
+        add(0, new_val(VK_MEM, g.tensors[op.in[0]].shape, mdX));
+        break;
+      }
+      case DRAGON_OP_HEAD_NORM: {
+        int mdY = materialise(dy, -1, DRAGON_F32), mP = -1;
+        std::vector<double> num = head_numbers(op);
+        // behind a Rotate: both in one pass (the gradient between the two is then dead unless somebody else reads it)
+        Item* rot = writer_of(mdY, IT_HEAD_BWD, hb::DX);
+        if (rot && rot->rd[hb::GAIN] < 0 && rot->num[hn::WIDTH] == num[hn::WIDTH]) {
+          std::copy(rot->num.begin() + hn::DIMS, rot->num.end(), num.begin() + hn::DIMS);
+          mP = rot->rd[hb::POS];
+          mdY = rot->rd[hb::DY];
+        }
+        const int mX = in_mem(op.in[0]), mG = in_mem(op.in[1]);
+        const int mdX = want[0] ? grad_mem(s, op.in[0]) : -1, mdG = want[1] ? new_mem(MEM_WORK, -1, DRAGON_F32, g.tensors[op.in[1]].shape) : -1;
+        const int i = add_item(IT_HEAD_BWD, {mX, mG, mP, mdY}, {mdX, mdG}, 0.0);
+        items[i].num = num;
+        if (want[0]) add(0, new_val(VK_MEM, g.tensors[op.in[0]].shape, mdX));
+        if (want[1]) add(1, new_val(VK_MEM, g.tensors[op.in[1]].shape, mdG));
+        break;
+      }
+      case DRAGON_OP_ATTENTION: {
+        const Item fwd = items[attn_item[r.op]];
+        const int mdY = materialise(dy, DRAGON_BF16, DRAGON_BF16);
+        int md[3];
+        for (int p = 0; p < 3; ++p) md[p] = want[p] ? grad_mem(s, op.in[p]) : -1;
+        const int i = add_item(IT_ATTN_BWD, {fwd.rd[at::Q], fwd.rd[at::K], fwd.rd[at::V], fwd.rd[at::STARTS], fwd.wr[at::Y], fwd.wr[at::LSE], mdY}, {md[0], md[1], md[2]}, 0.0);
+        items[i].num = op.num;
+        for (int p = 0; p < 3; ++p)
+          if (want[p]) add(p, new_val(VK_MEM, g.tensors[op.in[p]].shape, md[p]));
+        break;
+      }
       default:
         set_error("gradient of operator type %d cannot be lowered", op.type);
         err = DRAGON_ERR_UNSUPPORTED;
@@ -581,6 +696,7 @@ bool join_domain(Shape* dom, bool* has_dom, const Shape& s) {
 
 static size_t share_workspace(Plan* plan, size_t off);
 static bool reads_follow_writes(const Plan& plan);
+static void find_in_place_caches(Plan* plan);
 
 // per operand of a VM program: position (index into the code) of its last load and of its first store
 std::vector<VmAccess> vm_operand_accesses(const VmSegment& sg) {
@@ -1129,7 +1245,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     Step st;
     st.kind = it.kind == IT_GEMM ? ST_GEMM : it.kind == IT_TRANSPOSE ? ST_TRANSPOSE : it.kind == IT_SCE_FWD ? ST_SCE_FWD
               : it.kind == IT_SCE_BWD ? ST_SCE_BWD : it.kind == IT_COPY ? ST_COPY : ST_NORM + (it.kind - IT_NORM);
-    st.rd = it.rd; st.wr = it.wr; st.attr = it.attr; st.sum_dtype = it.sum_dtype; st.round_dtype = it.round_dtype;
+    st.rd = it.rd; st.wr = it.wr; st.attr = it.attr; st.num = it.num; st.sum_dtype = it.sum_dtype; st.round_dtype = it.round_dtype;
     st.mA = it.mA; st.mB = it.mB; st.mC = it.mC; st.mD = it.mD; st.mE = it.mE; st.scale = it.scale; st.tA = it.tA; st.tB = it.tB;
     st.relu = it.relu;
     st.epi = it.epi;
@@ -1167,6 +1283,18 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     plan->steps.erase(plan->steps.begin() + i + 1);
     // (steps of VM segments name their segment, so nothing else refers to a step's position)
   }
+  // Neighbouring writes by one table (keys and values) are one launch
+  for (size_t i = 0; i + 1 < plan->steps.size();) {
+    Step &a = plan->steps[i], &b = plan->steps[i + 1];
+    bool join = a.kind == ST_CACHE_WRITE && b.kind == ST_CACHE_WRITE && a.num == b.num && a.rd.size() < 2 * kCachesPerLaunch + cw::CACHE;
+    if (join) join = std::equal(a.rd.begin(), a.rd.begin() + cw::CACHE, b.rd.begin()) && mems[a.rd[cw::ROWS]].shape.d[0] == mems[b.rd[cw::ROWS]].shape.d[0] &&
+                     !std::count(a.wr.begin(), a.wr.end(), b.rd[cw::CACHE]) &&
+                     !std::count(a.wr.begin(), a.wr.end(), b.rd[cw::ROWS]);
+    if (!join) { ++i; continue; }
+    a.rd.insert(a.rd.end(), b.rd.begin() + cw::CACHE, b.rd.end());
+    a.wr.insert(a.wr.end(), b.wr.begin(), b.wr.end());
+    plan->steps.erase(plan->steps.begin() + i + 1);
+  }
   for (size_t s = 0; s < seg_items.size(); ++s) {
     if (seg_items[s].empty()) continue;   // ran in a product's epilogue
     int rc = codegen_segment(items, seg_items[s], vals, mems, sm_count, &plan->segs[s]);
@@ -1183,6 +1311,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
   }
 
   if (!reads_follow_writes(*plan)) return DRAGON_ERR_UNSUPPORTED;
+  find_in_place_caches(plan);
 
   // workspace layout: the status word, live workspace tensors, then per-segment scratch
   size_t off = 0;
@@ -1199,6 +1328,17 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       const Shape& sh = mems[st.rd[nb::H]].shape;
       st.n_colpart = norm_bwd_partials(sh.rows(), sh.cols(), sm_count);
       st.colpart_off = take((size_t)st.n_colpart * sh.cols() * sizeof(float));
+    }
+    if (st.kind == ST_HEAD_BWD && st.wr[hb::DGAIN] >= 0) {
+      const Shape& sh = mems[st.rd[hb::X]].shape;
+      st.n_colpart = head_bwd_partials(sh.d[0], sh.d[1] / (int64_t)st.num[hn::WIDTH], sm_count);
+      st.colpart_off = take((size_t)st.n_colpart * (size_t)st.num[hn::WIDTH] * sizeof(float));
+    }
+    if (st.kind == ST_ATTN_BWD) st.scratch_off = take(attention_bwd_scratch_bytes(mems[st.rd[at::Q]].shape.d[0], (int64_t)st.num[an::HEADS]));
+    if (st.kind == ST_PAGED) {
+      const Shape& sh = mems[st.rd[pa::Q]].shape;
+      st.scratch_off = take(paged_scratch_bytes(sh.d[0], mems[st.rd[pa::PAGES]].shape.d[0], (int64_t)st.num[pn::HEADS], (int64_t)st.num[pn::KV_HEADS],
+                                                sh.d[1] / (int64_t)st.num[pn::HEADS], sm_count));
     }
     if (st.kind == ST_GNORM || st.kind == ST_NORM_CLIP) st.scratch_off = take(global_norm_scratch_bytes((int)st.rd.size(), sm_count));
     if (st.kind == ST_SCAN || st.kind == ST_SCAN_BWD) {
@@ -1258,6 +1398,27 @@ static bool reads_follow_writes(const Plan& plan) {
     for (int m : writes) written[m] = 1;
   }
   return true;
+}
+
+// A fed cache may be overwritten by the fetched result of its CacheWrite if nothing reads it from that step on, and that step reads
+// it once
+static void find_in_place_caches(Plan* plan) {
+  const int n_steps = (int)plan->steps.size();
+  for (int si = 0; si < n_steps; ++si) {
+    const Step& st = plan->steps[si];
+    if (st.kind != ST_CACHE_WRITE) continue;
+    for (size_t k = 0; k < st.wr.size(); ++k) {
+      const MemRef &in = plan->mems[st.rd[cw::CACHE + 2 * k]], &out = plan->mems[st.wr[k]];
+      if (in.where != MEM_FEED || out.where != MEM_FETCH) continue;
+      int reads = 0;
+      for (int sj = si; sj < n_steps; ++sj) {
+        std::vector<VmAccess> acc;
+        if (plan->steps[sj].kind == ST_VM) acc = vm_operand_accesses(plan->segs[plan->steps[sj].seg]);
+        for_each_access(*plan, sj, acc, [&](int m, bool w) { reads += !w && plan->mems[m].where == MEM_FEED && plan->mems[m].index == in.index; });
+      }
+      if (reads == 1) plan->in_place.emplace_back(in.index, out.index);
+    }
+  }
 }
 
 // Memory sharing between the tensors that cross kernels (the purpose of Sec. 2.4, at the granularity of
@@ -1432,6 +1593,25 @@ std::string describe_plan(const Plan& p) {
         snprintf(buf, sizeof(buf), "gated_scan%s[%lldx%lld, %d sequences%s%s%s]\n", st.kind == ST_SCAN ? "" : "_bwd", (long long)p.mems[st.rd[sc::GATE]].shape.d[0],
                  (long long)p.mems[st.rd[sc::GATE]].shape.d[1], (int)st.attr, st.rd[sc::H0] >= 0 ? " +h0" : "", st.rd[sc::RESET] >= 0 ? " +reset" : "",
                  st.kind == ST_SCAN && st.wr[sc::H] < 0 ? " states only" : "");
+        break;
+      case ST_HEAD: case ST_HEAD_BWD: {
+        const bool back = st.kind == ST_HEAD_BWD, norm = st.rd[hd::GAIN] >= 0, rot = st.rd[hd::POS] >= 0;
+        const Shape& sh = p.mems[st.rd[back ? (int)hb::DY : (int)hd::X]].shape;
+        snprintf(buf, sizeof(buf), "%s%s%s%s[%lldx%lld, heads of %d%s%s%s]\n", norm ? "head_norm" : "", norm && rot ? "+" : "", rot ? "rotate" : "", back ? "_bwd" : "",
+                 (long long)sh.d[0], (long long)sh.d[1], (int)st.num[hn::WIDTH],
+                 rot ? (st.num[hn::INTERLEAVED] != 0.0 ? " interleaved" : " halves") : "", !back && rot && st.wr[hd::U] >= 0 ? " ->normed" : "",
+                 back && st.wr[hb::DGAIN] >= 0 ? " ->dg" : "");
+        break;
+      }
+      case ST_ATTN: case ST_ATTN_BWD:
+        snprintf(buf, sizeof(buf), "attention%s[%lld rows, %d heads on %d, %s%s%s]\n", st.kind == ST_ATTN ? "" : "_bwd", (long long)p.mems[st.rd[at::Q]].shape.d[0],
+                 (int)st.num[an::HEADS], (int)st.num[an::KV_HEADS], st.num[an::CAUSAL] != 0.0 ? "causal" : "full", st.num[an::WINDOW] != 0.0 ? " window" : "",
+                 st.rd[at::STARTS] >= 0 ? " packed" : "");
+        break;
+      case ST_CACHE_WRITE: snprintf(buf, sizeof(buf), "cache_write[%d caches, pages of %d]\n", (int)st.wr.size(), (int)st.num[0]); break;
+      case ST_PAGED:
+        snprintf(buf, sizeof(buf), "paged_attention[%lld rows of %lld sequences, %d heads on %d, pages of %d%s]\n", (long long)p.mems[st.rd[pa::Q]].shape.d[0],
+                 (long long)p.mems[st.rd[pa::PAGES]].shape.d[0], (int)st.num[pn::HEADS], (int)st.num[pn::KV_HEADS], (int)st.num[pn::PAGE], st.num[pn::WINDOW] != 0.0 ? " window" : "");
         break;
       default: snprintf(buf, sizeof(buf), "copy\n");
     }

@@ -74,7 +74,8 @@ struct EpiSpec {
 constexpr int kMaxEpiOps = 8;
 
 enum ItemKind { IT_MOP, IT_GEMM, IT_TRANSPOSE, IT_SCE_FWD, IT_SCE_BWD, IT_COPY,
-                IT_NORM, IT_NORM_BWD, IT_QUANT, IT_GEMM8, IT_GNORM, IT_FACTOR, IT_CLIP, IT_SCAN, IT_SCAN_BWD };
+                IT_NORM, IT_NORM_BWD, IT_QUANT, IT_GEMM8, IT_GNORM, IT_FACTOR, IT_CLIP, IT_SCAN, IT_SCAN_BWD,
+                IT_HEAD, IT_HEAD_BWD, IT_ATTN, IT_ATTN_BWD, IT_CACHE_WRITE, IT_PAGED };
 // Memory operands of the kinds from IT_NORM on, by position in Item::rd and Item::wr (-1: absent, or a result nobody needs)
 namespace nm { enum { X, R, GAIN }; enum { H, Y, S, Q }; }                        // IT_NORM: h = x + r (r absent: h = x), y; s, q of y
 namespace nb { enum { H, DY, GAIN, SKIP }; enum { DH, DGAIN }; }                  // IT_NORM_BWD: dh = skip + the norm's gradient
@@ -83,6 +84,17 @@ namespace g8 { enum { XQ, SX, WQ, SW }; enum { Y }; }                           
 namespace gn { enum { NORM, FACTOR, CLIPPED }; }                                  // IT_GNORM: rd = the tensors; factor = min(1, attr / norm)
 namespace cl { enum { NORM, FIRST }; }                                            // IT_CLIP: rd = norm, tensors; wr = the clipped tensors
 namespace sc { enum { GATE, X, H0, RESET, DH, CARRY_IN }; enum { H, CARRY }; enum { DGATE, DX, DH0 }; }   // IT_SCAN, IT_SCAN_BWD
+// IT_HEAD: u = the norm of every head of x (gain absent: u = x), y = u rotated (positions absent: no rotation).  IT_HEAD_BWD: dy is y's
+// gradient (positions present) or u's.  Numbers: hn below.
+namespace hd { enum { X, GAIN, POS }; enum { U, Y }; }
+namespace hb { enum { X, GAIN, POS, DY }; enum { DX, DGAIN }; }
+namespace hn { enum { EPS, WIDTH, DIMS, INTERLEAVED, BASE, FACTOR, LOW, HIGH, ORIGINAL, AMPLITUDE, COUNT }; }
+// IT_ATTN, IT_ATTN_BWD: lse [heads, T] is log2 of every row's sum of exponentials (scaled), +inf for a row that sees nothing
+namespace at { enum { Q, K, V, STARTS, Y_IN, LSE_IN, DY }; enum { Y, LSE }; enum { DQ, DK, DV }; }
+namespace an { enum { HEADS, KV_HEADS, CAUSAL, WINDOW, SCALE, SEQUENCES }; }
+namespace cw { enum { PAGES, LENGTHS, STARTS, CACHE, ROWS }; }                    // IT_CACHE_WRITE: rd = table, then cache and rows of each; wr = the new caches
+namespace pa { enum { Q, K, V, PAGES, LENGTHS, STARTS }; enum { Y }; }            // IT_PAGED
+namespace pn { enum { HEADS, KV_HEADS, PAGE, WINDOW, SCALE }; }
 struct Item {
   int kind = IT_MOP;
   // IT_MOP
@@ -98,6 +110,7 @@ struct Item {
   std::vector<EpiSpec> epi;                // GEMM: further elementwise operations on the accumulator, in order
   std::vector<int> rd, wr;                 // memory operands of the kinds from IT_NORM on (positions: see there)
   double attr = 0.0;                       // their number: eps, block rows, limit, sequences
+  std::vector<double> num;                 // the numbers of the kinds from IT_HEAD on
   int sum_dtype = DRAGON_F32;              // IT_NORM: the declared types of h and of y: both are rounded to them whether or not they are
   int round_dtype = DRAGON_F32;            //   written (the norm reads the rounded h, the scales and e4m3 values are of the rounded y)
   bool live = false;
@@ -136,6 +149,7 @@ struct VmSegment {
 
 enum StepKind { ST_VM, ST_GEMM, ST_TRANSPOSE, ST_SCE_FWD, ST_SCE_BWD, ST_COPY,
                 ST_NORM, ST_NORM_BWD, ST_QUANT, ST_GEMM8, ST_GNORM, ST_FACTOR, ST_CLIP, ST_SCAN, ST_SCAN_BWD,
+                ST_HEAD, ST_HEAD_BWD, ST_ATTN, ST_ATTN_BWD, ST_CACHE_WRITE, ST_PAGED,
                 ST_NORM_CLIP };   // (GNORM and the CLIP of all its tensors in one launch: rd = tensors, wr = norm, factor, clipped tensors)
 struct Step {
   int kind;
@@ -151,6 +165,7 @@ struct Step {
   size_t scratch_off = 0;                // SCE_FWD: per-row losses; GNORM: partial sums; SCAN: what tiles hand on
   std::vector<int> rd, wr;               // kinds from ST_NORM on: as in Item
   double attr = 0.0;
+  std::vector<double> num;
   int sum_dtype = DRAGON_F32, round_dtype = DRAGON_F32;
 };
 
@@ -161,6 +176,14 @@ int norm_bwd_partials(int64_t rows, int64_t cols, int sm_count);   // rows of pa
 size_t global_norm_scratch_bytes(int n_tensors, int sm_count);
 bool norm_and_clip_fit_one_launch(const std::vector<int64_t>& numel, const std::vector<int>& dtype, int sm_count);
 size_t scan_scratch_bytes(int64_t rows, int64_t cols);
+constexpr int64_t kMaxAttentionRows = 1 << 30;   // rows of an attention operator's tensors: 32-bit row numbers with room for a tile
+constexpr int kMaxHeadWidth = 128, kMaxRotatedWidth = 256;
+int head_bwd_partials(int64_t rows, int64_t heads, int sm_count);   // rows of partial gain gradients that HeadNorm's gradient leaves
+size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads);
+int attention_bwd_launches(const Step& s);
+int paged_launches(const Step& s, const std::vector<MemRef>& mems);
+size_t paged_scratch_bytes(int64_t rows, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t width, int sm_count);
+constexpr int kCachesPerLaunch = 8;
 constexpr int kTensorsPerLaunch = 256;   // tensors that one launch of GlobalNorm or ClipByNorm takes in its parameters
 inline int launches_of_tensors(int n) { return (n + kTensorsPerLaunch - 1) / kTensorsPerLaunch; }
 
@@ -171,6 +194,7 @@ struct Plan {
   size_t workspace_bytes = 0;
   size_t status_off = 0;
   int sm_count = kDefaultSmCount;
+  std::vector<std::pair<int, int>> in_place;   // (feed, fetch) of a cache that CacheWrite may write in place
 };
 
 // What the launcher of a step of the kinds from ST_NORM on gets: the step, where its memory is, the run's status

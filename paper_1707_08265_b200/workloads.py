@@ -55,12 +55,13 @@ class GraphDesc:
             self.desc["ops"][-1]["attrs"] = [float(a) for a in attrs]
         return o
 
-    def grad(self, objs, wrts):
+    def grad(self, objs, wrts, dtypes=None):
+        """dtypes: the gradients' types, "f32" or "bf16" (None: "f32" throughout)."""
         gids = []
         s = len(self.desc["grads"])
-        for w in wrts:
+        for w, dt in zip(wrts, dtypes or ["f32"] * len(wrts)):
             t = self.desc["tensors"][w]
-            gids.append(self.tensor("grad%d/%s" % (s, t["name"]), t["shape"], "f32"))
+            gids.append(self.tensor("grad%d/%s" % (s, t["name"]), t["shape"], dt))
         self.desc["grads"].append({"objs": list(objs), "wrts": list(wrts), "grad_ids": gids})
         return gids
 
