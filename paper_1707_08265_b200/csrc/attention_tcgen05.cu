@@ -1,0 +1,406 @@
+// Attention's forward pass on the tensor cores: y = softmax(scale q k^T) v over packed sequences or over a paged cache.
+// Hand-written for sm_100a.
+//
+// A CTA works on two tiles of 128 query rows that see the same keys: the same rows of two query heads that share a key head,
+// or (where heads do not come in pairs) two neighbouring blocks of rows.  Keys and values pass once, 128 at a time:
+//   S_t = Q_t K^T              tcgen05.mma, both operands in shared memory (TMA, 128-byte swizzle), S_t in TMEM
+//   P_t = exp2(scale' S_t - m) one thread a row: the running maximum m and sum stay in its registers; P_t goes back over S_t as
+//                              bf16 (its sum is taken in fp32 before the rounding)
+//   O_t += P_t V               tcgen05.mma with P_t as the A operand out of TMEM, V as it lies in memory (MN-major)
+// While the softmax threads of one tile work, the tensor unit works for the other.  m only moves when a row's maximum has grown
+// by more than 2^8 (P_t and the sum then stay below 2^8 times their scale, far inside bf16 and fp32): O_t in TMEM is rescaled
+// that seldom that the softmax threads do it themselves.  S_t of the next keys is issued behind O_t's product, so a completed
+// S_t says that O_t may be touched.
+// Warps: 0..3 and 4..7 softmax of tile 0 and 1 (a warp its TMEM lanes), 8 TMA, 9 MMA.  Every wait is bounded.
+#include <algorithm>
+#include <cstdlib>
+
+#include "attention_rows.h"
+#include "attention_tiles.h"
+
+namespace dragon {
+namespace {
+
+constexpr int kFwdThreads = 320;
+constexpr int fwd_stages(int chunks) { return chunks == 1 ? 4 : 2; }                          // of K and of V each
+constexpr size_t fwd_smem(int chunks) { return 1024 + (size_t)(2 + 2 * fwd_stages(chunks)) * chunks * kChunkBytes + 512; }
+constexpr float kRescale = 8.f;
+
+struct FwdArgs {
+  RowArgs r;
+  int by_heads;         // the two tiles are two heads' (1) or two blocks' of rows
+  int pairs;            // pairs of heads, or heads
+  int blocks;           // blocks of rows that the grid has room for
+  int each_blocks;      // of a sequence, where all are equally long (0: starts)
+  int few;              // paged: sequences of at most so many rows are not this kernel's
+  long long budget;
+  int drop_first_load;
+};
+
+struct FwdUnit {
+  int seq, a, b;        // the sequence (-1: none) and its rows
+  int row0;             // first row of tile 0, from a
+  int first_pos;        // position of row a (paged: behind the tokens that were there)
+  int keys;             // keys there are
+  int spare, spares;    // seq < 0: which of how many units that are left over
+};
+
+// Which block of rows this unit has: blocks of a sequence from its end (those that see most keys go first)
+__device__ __forceinline__ void find_unit(const FwdArgs& a, int unit, int block_rows, FwdUnit* u, int lane) {
+  const Sequences& q = a.r.seq;
+  u->seq = -1;
+  if (a.each_blocks) {
+    const int s = unit % q.count;
+    q.rows_of(s, &u->a, &u->b);
+    u->seq = s;
+    u->row0 = (a.each_blocks - 1 - unit / q.count) * block_rows;
+    return;
+  }
+  int before = 0;
+  for (int s0 = 0; s0 < q.count; s0 += 32) {
+    int x = 0, y = 0;
+    if (s0 + lane < q.count) q.rows_of(s0 + lane, &x, &y);
+    const int n = (y - x + block_rows - 1) / block_rows;
+    int sum = n;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, k); if (lane >= k) sum += t; }
+    const int local = unit - before;
+    const unsigned hit = __ballot_sync(0xffffffffu, local >= sum - n && local < sum);
+    if (hit) {
+      const int w = __ffs(hit) - 1;
+      u->seq = s0 + w;
+      u->a = __shfl_sync(0xffffffffu, x, w);
+      u->b = __shfl_sync(0xffffffffu, y, w);
+      u->row0 = (__shfl_sync(0xffffffffu, sum, w) - 1 - local) * block_rows;
+      return;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  u->spare = unit - before;
+  u->spares = a.blocks - before;
+}
+
+template <bool kPaged, int kChunks>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ FwdArgs a) {
+  constexpr int kSt = fwd_stages(kChunks);
+  constexpr uint32_t kTile = kChunks * kChunkBytes;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const uint32_t q_at = base, k_at = base + 2 * kTile, v_at = k_at + kSt * kTile;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (base - raw) + (2 + 2 * kSt) * kTile);
+  const uint32_t q_full = smem_u32(bars), k_full = q_full + 16, k_empty = k_full + 8 * kSt, v_full = k_empty + 8 * kSt, v_empty = v_full + 8 * kSt;
+  const uint32_t s_full = v_empty + 8 * kSt, p_full = s_full + 16, o_full = p_full + 16, v_clean = o_full + 16, drain = v_clean + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 10 + 4 * kSt);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  __shared__ FwdUnit unit;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int block_rows = a.by_heads ? 128 : 256, pair = blockIdx.x % a.pairs, group = a.r.heads / a.r.kv_heads;
+  const int head0 = a.by_heads ? 2 * pair : pair, kvh = head0 / group;
+
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
+    for (int t = 0; t < 2; ++t) { mbar_init(q_full + 8 * t, 1); mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 8 * t, 4); mbar_init(o_full + 8 * t, 1); }
+    for (int s = 0; s < kSt; ++s) { mbar_init(k_full + 8 * s, 1); mbar_init(k_empty + 8 * s, 1); mbar_init(v_full + 8 * s, 1); mbar_init(v_empty + 8 * s, 1); }
+    mbar_init(v_clean, 32);
+    mbar_init(drain, 1);
+    abort_flag[0] = abort_flag[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (blockIdx.x == 0 && a.r.status_clear) *a.r.status_clear = 0;
+  }
+  if (blockIdx.x == 0 && !a.r.seq.in_order()) report(a.r.status, DRAGON_ERR_INVALID_ARG);
+  if (warp == 0) {
+    FwdUnit u;
+    find_unit(a, blockIdx.x / a.pairs, block_rows, &u, lane);
+    if (u.seq >= 0) {
+      u.keys = u.b - u.a;
+      u.first_pos = 0;
+      if (kPaged) {
+        bool fits;
+        u.keys = a.r.pages.tokens(u.seq, &fits);
+        if (!fits) report(a.r.status, DRAGON_ERR_INVALID_ARG);
+        u.first_pos = u.keys - (u.b - u.a);
+      }
+    }
+    if (lane == 0) unit = u;
+  }
+  __syncthreads();
+  const FwdUnit u = unit;
+  if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
+    const int first = a.r.seq.starts ? min(max(__ldg(a.r.seq.starts), 0), a.r.seq.rows) : 0;
+    const int last = a.r.seq.starts ? min(max(__ldg(a.r.seq.starts + a.r.seq.count), first), a.r.seq.rows) : a.r.seq.rows;
+    const int none = first + a.r.seq.rows - last, wide = (a.by_heads ? 2 : 1) * a.r.width;
+    for (int i = u.spare; i < none; i += u.spares) {
+      const int row = i < first ? i : last + i - first;
+      const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (a.r.out) for (int c = 8 * threadIdx.x; c < wide; c += 8 * kFwdThreads) store_any<8>(a.r.out, a.r.ot, ((size_t)row * a.r.heads + head0) * a.r.width + c, zero);
+      if (a.r.lse && threadIdx.x < (a.by_heads ? 2 : 1)) a.r.lse[(size_t)(head0 + threadIdx.x) * a.r.seq.rows + row] = kInf;
+    }
+    return;
+  }
+  const int n_rows = u.b - u.a;
+  if (kPaged && n_rows * group <= a.few) return;
+  // the tiles of keys that any row of the unit sees
+  const int last_row = min(u.row0 + block_rows, n_rows) - 1;      // (row0 < n_rows)
+  const int key_end = a.r.causal ? max(0, min(u.keys, u.first_pos + last_row + 1)) : u.keys;
+  const int key_begin = a.r.window ? max(0, u.first_pos + u.row0 - a.r.window + 1) : 0;
+  const int j0 = key_begin / 128, n_tiles = key_end > key_begin ? (key_end + 127) / 128 - j0 : 0;
+  const bool ragged = u.keys - (j0 + n_tiles - 1) * 128 < 128;      // the last tile has rows behind the sequence's last key
+
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_wait(bar, parity, abort_flag, a.budget)) return true;
+    *abort_flag = 1;
+    report(a.r.status, DRAGON_ERR_TIMEOUT);
+    return false;
+  };
+  int issued_k = 0, issued_v = 0;
+  if (warp == 8) {
+    if (lane == 0 && n_tiles > 0) {
+      for (int t = 0; t < 2; ++t) {
+        mbar_expect_tx(q_full + 8 * t, kTile);
+        for (int c = 0; c < kChunks; ++c)
+          tma_load_3d(q_at + t * kTile + c * kChunkBytes, &tm_q, 64 * c, a.by_heads ? head0 + t : head0, u.a + u.row0 + (a.by_heads ? 0 : 128 * t), q_full + 8 * t);
+      }
+    }
+    __syncwarp();
+    bool ok = true;
+    for (int j = 0; j < n_tiles && ok; ++j) {
+      const int s = j % kSt, turn = j / kSt;
+      for (int which = 0; which < 2; ++which) {
+        const CUtensorMap* tm = which ? &tm_v : &tm_k;
+        const uint32_t full = (which ? v_full : k_full) + 8 * s, dst = (which ? v_at : k_at) + s * kTile;
+        ok = __all_sync(0xffffffffu, wait((which ? v_empty : k_empty) + 8 * s, (turn & 1) ^ 1));
+        if (!ok) break;
+        if (which) issued_v = j + 1; else issued_k = j + 1;
+        if (a.drop_first_load && j == 0 && !which) continue;      // failure-detection test: this stage's signal never comes
+        if (lane == 0) mbar_expect_tx(full, kTile);
+        __syncwarp();
+        if (!kPaged) {
+          if (lane < kChunks) tma_load_3d(dst + lane * kChunkBytes, tm, 64 * lane, kvh, u.a + (j0 + j) * 128, full);
+        } else {
+          const int page = 1 << a.r.pages.shift, box = min(page, 128), at = (j0 + j) * 128 + lane * box;
+          if (lane < 128 / box) {
+            int row = a.r.pages.pool << a.r.pages.shift;          // behind the cache: zeros
+            if (at < u.keys) {
+              const int number = a.r.pages.page_of(u.seq, at);
+              if (a.r.pages.in_pool(number)) row = (number << a.r.pages.shift) + (at & (page - 1));
+              else report(a.r.status, DRAGON_ERR_INVALID_ARG);
+            }
+            for (int c = 0; c < kChunks; ++c) tma_load_3d(dst + c * kChunkBytes + lane * box * 128, tm, 64 * c, kvh, row, full);
+          }
+        }
+      }
+    }
+    if (ok && ragged && n_tiles > 0) {
+      // what stands behind the sequence's last key (other sequences, a page's unused rows) is not to meet a probability of 0
+      const int j = n_tiles - 1, keep = u.keys - (j0 + j) * 128;
+      if (__all_sync(0xffffffffu, wait(v_full + 8 * (j % kSt), (j / kSt) & 1))) {
+        unsigned char* tile = smem_raw + (v_at - raw) + (j % kSt) * kTile;
+        for (int c = 0; c < kChunks; ++c)
+          for (int i = lane; i < (128 - keep) * 8; i += 32) *reinterpret_cast<uint4*>(tile + c * kChunkBytes + keep * 128 + 16 * i) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(v_clean);
+      }
+    }
+  } else if (warp == 9) {
+    if (lane == 0 && n_tiles > 0) {
+      const int k_steps = (a.r.width + 15) / 16, n_out = 16 * k_steps;
+      const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_o = idesc_bf16(128, n_out, true);
+      auto product_s = [&](int t, int j) {
+        const uint32_t kt = k_at + (j % kSt) * kTile, qt = q_at + t * kTile;
+        for (int k = 0; k < k_steps; ++k) {
+          const uint32_t off = (k >> 2) * kChunkBytes + (k & 3) * 32;
+          umma_ss(tmem + 128 * t, desc_k(qt + off), desc_k(kt + off), idesc_s, k > 0);
+        }
+        umma_commit(s_full + 8 * t);
+      };
+      bool ok = wait(k_full, 0);
+      for (int t = 0; t < 2 && ok; ++t) {
+        ok = wait(q_full + 8 * t, 0);
+        fence_after();
+        if (ok) product_s(t, 0);
+      }
+      if (ok) umma_commit(k_empty);
+      for (int j = 0; j < n_tiles && ok; ++j) {
+        const int s = j % kSt;
+        ok = wait(v_full + 8 * s, (j / kSt) & 1);
+        if (ok && ragged && j == n_tiles - 1) ok = wait(v_clean, 0);
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (!(ok = wait(p_full + 8 * t, j & 1))) break;
+          fence_after();
+          for (int k = 0; k < 8; ++k)
+            umma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k, desc_mn(v_at + s * kTile + k * 2048), idesc_o, j > 0 || k > 0);
+          if (j + 1 < n_tiles) {
+            if (t == 0) { if (!(ok = wait(k_full + 8 * ((j + 1) % kSt), ((j + 1) / kSt) & 1))) break; fence_after(); }
+            product_s(t, j + 1);
+          } else {
+            umma_commit(o_full + 8 * t);
+          }
+        }
+        if (ok) {
+          umma_commit(v_empty + 8 * s);
+          if (j + 1 < n_tiles) umma_commit(k_empty + 8 * ((j + 1) % kSt));
+        }
+      }
+      if (*abort_flag) { umma_commit(drain); mbar_wait(drain, 0, abort_flag + 1); }
+    }
+    __syncwarp();
+  } else {
+    const int t = warp >> 2, e = (warp & 3) * 32 + lane;
+    const int head = a.by_heads ? head0 + t : head0, i = u.row0 + (a.by_heads ? 0 : 128 * t) + e;      // this thread's row of the sequence
+    const int pos = u.first_pos + i;
+    const bool mine = i < n_rows;
+    // the keys that the row sees
+    const int hi = !mine ? 0 : a.r.causal ? min(pos + 1, u.keys) : u.keys, lo = a.r.window ? max(0, pos - a.r.window + 1) : 0;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + 256 + 128 * t;
+    float top = -kInf, sum = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n_tiles; ++j) {
+      ok = __all_sync(0xffffffffu, wait(s_full + 8 * t, j & 1));
+      if (!ok) break;
+      fence_after();
+      uint32_t s[128];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
+      tmem_ld_wait();
+      const int k0 = (j0 + j) * 128;
+      if (!__all_sync(0xffffffffu, lo <= k0 && k0 + 128 <= hi)) {
+#pragma unroll
+        for (int c = 0; c < 128; ++c) if (k0 + c < lo || k0 + c >= hi) s[c] = 0xff800000u;
+      }
+      float m[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) m[c] = __uint_as_float(s[c]);
+#pragma unroll
+      for (int c = 4; c < 128; ++c) m[c & 3] = fmaxf(m[c & 3], __uint_as_float(s[c]));
+      const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+      if (j == 0) {
+        top = most;
+      } else {
+        const bool grown = (most - top) * a.r.scale > kRescale;      // (from -inf on: infinite)
+        if (__any_sync(0xffffffffu, grown)) {
+          const float f = grown ? exp2_fast((top - most) * a.r.scale) : 1.f;
+          if (grown) top = most;
+          sum *= f;
+#pragma unroll 1
+          for (int c = 0; c < a.r.width; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_at + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+            tmem_st16(o_at + c, o);
+          }
+        }
+      }
+      const float shift = top == -kInf ? 0.f : top * a.r.scale;
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t p[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          const float x = exp2_fast(fmaf(__uint_as_float(s[64 * c + 2 * k]), a.r.scale, -shift));
+          const float y = exp2_fast(fmaf(__uint_as_float(s[64 * c + 2 * k + 1]), a.r.scale, -shift));
+          part[(2 * k) & 3] += x;
+          part[(2 * k + 1) & 3] += y;
+          p[k] = bf16_pair(x, y);
+        }
+        tmem_st32(s_at + 32 * c, p);
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      tmem_st_wait();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full + 8 * t);
+    }
+    if (ok && n_tiles > 0) {
+      ok = __all_sync(0xffffffffu, wait(o_full + 8 * t, 0));
+      fence_after();
+    }
+    if (ok) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a NaN stays one)
+      const int row = u.a + i;
+      const size_t at = ((size_t)row * a.r.heads + head) * a.r.width;
+      bool fine = fabsf(sum) < kInf;
+#pragma unroll 1
+      for (int c = 0; c < a.r.width; c += 16) {
+        uint32_t o[16];
+        float v[16];
+        if (n_tiles > 0) { tmem_ld16(o_at + c, o); tmem_ld_wait(); }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          v[k] = n_tiles > 0 ? __uint_as_float(o[k]) * inv : 0.f;
+          fine &= fabsf(v[k]) < kInf;
+        }
+        if (mine && a.r.out) {
+          store_any<8>(a.r.out, a.r.ot, at + c, v);
+          if (c + 8 < a.r.width) store_any<8>(a.r.out, a.r.ot, at + c + 8, v + 8);
+        }
+      }
+      if (mine && a.r.lse) a.r.lse[(size_t)head * a.r.seq.rows + row] = sum == 0.f ? kInf : top * a.r.scale + log2f(sum);
+      __syncwarp();
+      for (unsigned again = __ballot_sync(0xffffffffu, mine && !fine); again; again &= again - 1)
+        attend_row<kPaged>(a.r, head, __shfl_sync(0xffffffffu, row, __ffs(again) - 1), lane);
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (*abort_flag) {      // an unwind: what the producer has handed to the TMA engine lands before the shared memory goes away
+    if (threadIdx.x == 256) {
+      for (int t = 0; t < 2 && n_tiles > 0; ++t) mbar_wait(q_full + 8 * t, 0, abort_flag + 1);
+      for (int k = std::max(a.drop_first_load ? 1 : 0, issued_k - kSt); k < issued_k; ++k) mbar_wait(k_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
+      for (int k = std::max(0, issued_v - kSt); k < issued_v; ++k) mbar_wait(v_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
+    }
+    __syncthreads();
+  }
+  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+template <bool kPaged, int kChunks> int launch_fwd(const FwdArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t st, const char* who) {
+  static bool set[64] = {};
+  const int rc = allow_smem(reinterpret_cast<const void*>(attention_fwd<kPaged, kChunks>), fwd_smem(kChunks), set, who);
+  if (rc != DRAGON_OK) return rc;
+  const long long grid = (long long)a.blocks * a.pairs;
+  if (grid > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
+  attention_fwd<kPaged, kChunks><<<(unsigned)grid, kFwdThreads, fwd_smem(kChunks), st>>>(q, k, v, a);
+  return launched(who);
+}
+
+}  // namespace
+
+// rows: what the row functions need as well; key_rows: rows of k and v in memory; few: rows x group of a sequence up to which another kernel has it
+int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, cudaStream_t st, const char* who) {
+  FwdArgs a = {};
+  a.r = rows;
+  const int group = rows.heads / rows.kv_heads;
+  a.by_heads = group % 2 == 0;
+  a.pairs = a.by_heads ? rows.heads / 2 : rows.heads;
+  const int block = a.by_heads ? 128 : 256;
+  if (rows.seq.starts) a.blocks = (int)((rows.seq.rows + block - 1) / block + rows.seq.count);
+  else { a.each_blocks = (rows.seq.each + block - 1) / block; a.blocks = a.each_blocks * rows.seq.count; }
+  a.few = few;
+  wait_settings("DRAGON_ATTENTION", &a.budget, &a.drop_first_load);
+  CUtensorMap q, k, v;
+  const int box = paged ? std::min(1 << rows.pages.shift, 128) : 128;
+  if (!head_map(&q, rows.q, rows.seq.rows, rows.heads, rows.width, 128) || !head_map(&k, rows.k, key_rows, rows.kv_heads, rows.width, box) ||
+      !head_map(&v, rows.v, key_rows, rows.kv_heads, rows.width, box)) {
+    set_error("%s: cannot encode the TMA descriptors (no CUDA driver?)", who);
+    return DRAGON_ERR_CUDA;
+  }
+  const bool wide = rows.width > 64;
+  return paged ? (wide ? launch_fwd<true, 2>(a, q, k, v, st, who) : launch_fwd<true, 1>(a, q, k, v, st, who))
+               : (wide ? launch_fwd<false, 2>(a, q, k, v, st, who) : launch_fwd<false, 1>(a, q, k, v, st, who));
+}
+
+}  // namespace dragon

@@ -110,17 +110,20 @@ def test_some_of_the_gradients(wanted):
 
 
 def test_infinities_and_nan_in_keys_that_nobody_sees():
-    """A causal row is untouched by what stands behind it, a window by what lies in front of it."""
+    """A causal row is untouched by what stands behind it, a window by what lies in front of it.  (A row whose tile held something
+    not finite is computed a second time, from fp32 probabilities: it is another rounding of the same formula, so both are held
+    to the formula's bound and not to each other's bits.)"""
     g, ids, inputs, outputs = attention_graph(300, 2, 1, 64, window=40)
     feeds = attention_feeds(g, inputs, 12)
-    clean, _ = run_gpu(g.desc, inputs, outputs, feeds)
+    clean = interp.run_function(g.desc, inputs, outputs, feeds)
+    bound = attention_bounds(g, inputs, outputs, feeds)["y"]
     for bad in (np.nan, np.inf):
         dirty = [f.copy() for f in feeds]
         dirty[1][150], dirty[2][150] = bad, bad
         got, _ = run_gpu(g.desc, inputs, outputs, dirty)
         seen = np.zeros(300, bool)
         seen[150:190] = True
-        assert np.array_equal(got[0][~seen], clean[0][~seen])
+        assert within(got[0][~seen], clean[0][~seen], bound[~seen], "bf16") <= 1
         assert not np.isfinite(got[0][seen]).all(axis=1).any() or bad == np.inf
 
 
