@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdragon.so")
 SOURCES = ["prune.cpp", "lower.cpp", "codegen.cpp", "specialize.cpp", "verify.cpp", "api.cu", "workspace.cu", "vm_launch.cu", "row_kernels.cu", "gemm_tcgen05.cu",
-           "norm_kernels.cu", "clip_kernels.cu", "scan_kernels.cu", "gemm_e4m3.cu", "head_kernels.cu", "attention_kernels.cu", "attention_tcgen05.cu", "paged_kernels.cu"]
+           "norm_kernels.cu", "clip_kernels.cu", "scan_kernels.cu", "gemm_e4m3.cu", "head_kernels.cu", "attention_kernels.cu", "attention_tcgen05.cu", "attention_bwd_tcgen05.cu", "paged_kernels.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC",
          "--expt-relaxed-constexpr", "-Xcompiler", "-Wall"] + os.environ.get("DRAGON_NVCC_DEFS", "").split()

@@ -1,0 +1,407 @@
+// Attention's gradient on the tensor cores, with the probabilities computed again from q, k and every row's log2 sum.
+// Hand-written for sm_100a.
+//
+//   p = exp2(scale' q k^T - lse), dp = dy v^T, ds = p (dp - delta), delta = sum(dy y) of a row
+//   dv = p^T dy, dk = scale ds^T q (over the query heads that share the key head), dq = scale ds k
+//
+// Two kernels, so that every sum has one owner and its order is fixed (no atomics); q k^T and dy v^T are computed in both (7 products
+// of a tile where one pass needs 5):
+//   keys:  a CTA has 128 keys of a key head and meets every tile of queries that sees them, of every head of the group.  It
+//          computes S^T = K Q^T and dP^T = V dY^T, so that P^T and dS^T lie in TMEM as the A operands of dV += P^T dY and
+//          dK += dS^T Q (dY and Q as they lie in memory, MN-major).
+//   rows:  a CTA has 128 rows of a head and meets their keys: S = Q K^T, dP = dY V^T, dQ += dS K.
+// One tile pair is 128 x 128; two warps share a row (64 columns each).  The products are issued in an order in which the tensor
+// unit has work while the threads compute: keys: dV(i), S(i+1), dK(i), dP(i+1); rows: S(i+1), dP(i+1), dQ(i) (dP has two buffers).
+// Warps: 0..7 mathematics, 8 TMA, 9 MMA.  Every wait is bounded.
+#include <algorithm>
+
+#include "attention_rows.h"
+#include "attention_tiles.h"
+
+namespace dragon {
+namespace {
+
+constexpr int kBwdThreads = 320;
+constexpr int kBwdStages = 2;
+constexpr size_t bwd_smem(int chunks) { return 1024 + (size_t)(2 + 2 * kBwdStages) * chunks * kChunkBytes + kBwdStages * 1024 + 512; }
+
+struct BwdArgs {
+  RowArgs r;
+  int blocks, each_blocks;
+  long long budget;
+  int drop_first_load;
+};
+
+template <bool kKeys, int kChunks>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+              const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ BwdArgs a) {
+  constexpr int kSt = kBwdStages;
+  constexpr uint32_t kTile = kChunks * kChunkBytes;
+  // columns of TMEM
+  constexpr uint32_t kS = 0, kDp = 128, kAcc1 = kKeys ? 256 : 384, kAcc2 = 384;      // (rows: the second buffer of dP at 256)
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const uint32_t x1 = base, x2 = x1 + kTile, y1 = x2 + kTile, y2 = y1 + kSt * kTile;      // the CTA's own tiles, and the stages of those it meets
+  float* stats = reinterpret_cast<float*>(smem_raw + (base - raw) + (2 + 2 * kSt) * kTile);      // keys: [stage][lse, delta][128]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(stats + kSt * 256);
+  const uint32_t x_full = smem_u32(bars), y1_full = x_full + 8, y1_empty = y1_full + 8 * kSt, y2_full = y1_empty + 8 * kSt, y2_empty = y2_full + 8 * kSt;
+  const uint32_t st_full = y2_empty + 8 * kSt, st_empty = st_full + 8 * kSt;
+  const uint32_t s_full = st_empty + 8 * kSt, dp_full = s_full + 8, p_full = dp_full + 16, ds_full = p_full + 8, acc_full = ds_full + 8, drain = acc_full + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 6 * kSt + 7);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  __shared__ Unit unit;
+  __shared__ unsigned again[8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.r.heads / a.r.kv_heads;
+  const int n_heads = kKeys ? a.r.kv_heads : a.r.heads, head = blockIdx.x % n_heads;
+
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_dy) : "memory");
+    mbar_init(x_full, 1);
+    for (int s = 0; s < kSt; ++s) {
+      mbar_init(y1_full + 8 * s, 1); mbar_init(y1_empty + 8 * s, 1); mbar_init(y2_full + 8 * s, 1); mbar_init(y2_empty + 8 * s, 1);
+      mbar_init(st_full + 8 * s, 32); mbar_init(st_empty + 8 * s, 8);
+    }
+    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(dp_full + 8, 1); mbar_init(p_full, 8); mbar_init(ds_full, 8); mbar_init(acc_full, 1); mbar_init(drain, 1);
+    abort_flag[0] = abort_flag[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    Unit u;
+    find_unit(a.r.seq, a.blocks, a.each_blocks, blockIdx.x / n_heads, 128, &u, lane);
+    if (u.seq >= 0 && kKeys && a.r.causal) u.row0 = (u.b - u.a - 1) / 128 * 128 - u.row0;      // the first keys are seen by most rows
+    if (lane == 0) unit = u;
+  }
+  __syncthreads();
+  const Unit u = unit;
+  if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares)
+      for (int c = 8 * threadIdx.x; c < a.r.width; c += 8 * kBwdThreads) {
+        const size_t at = ((size_t)row * n_heads + head) * a.r.width + c;
+        if (kKeys && a.r.dk) store_any<8>(a.r.dk, a.r.dkt, at, zero);
+        if (kKeys && a.r.dv) store_any<8>(a.r.dv, a.r.dvt, at, zero);
+        if (!kKeys) store_any<8>(a.r.out, a.r.ot, at, zero);
+      }
+    return;
+  }
+  const int n_rows = u.b - u.a, last = min(u.row0 + 128, n_rows) - 1;      // own rows: row0 .. last
+  // the tiles it meets: keys: rows that see any of the own keys; rows: keys that any of the own rows sees
+  int first = 0, end = n_rows;
+  if (kKeys) {
+    if (a.r.causal) first = u.row0;
+    if (a.r.window) end = (int)min((long long)n_rows, (long long)last + a.r.window);
+  } else {
+    if (a.r.causal) end = last + 1;
+    if (a.r.window) first = max(0, u.row0 - a.r.window + 1);
+  }
+  const int t0 = first / 128, tiles = (end + 127) / 128 - t0, n = tiles * (kKeys ? group : 1);
+
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_wait(bar, parity, abort_flag, a.budget)) return true;
+    *abort_flag = 1;
+    report(a.r.status, DRAGON_ERR_TIMEOUT);
+    return false;
+  };
+  int issued1 = 0, issued2 = 0;
+  if (warp == 8) {
+    if (lane == 0) {
+      mbar_expect_tx(x_full, 2 * kTile);
+      for (int c = 0; c < kChunks; ++c) {
+        tma_load_3d(x1 + c * kChunkBytes, kKeys ? &tm_k : &tm_q, 64 * c, head, u.a + u.row0, x_full);
+        tma_load_3d(x2 + c * kChunkBytes, kKeys ? &tm_v : &tm_dy, 64 * c, head, u.a + u.row0, x_full);
+      }
+    }
+    __syncwarp();
+    bool ok = true;
+    for (int i = 0; i < n && ok; ++i) {
+      const int s = i % kSt, turn = i / kSt, h = kKeys ? head * group + i / tiles : head / group, row = u.a + (t0 + i % tiles) * 128;
+      ok = __all_sync(0xffffffffu, wait(y1_empty + 8 * s, (turn & 1) ^ 1));
+      if (!ok) break;
+      issued1 = i + 1;
+      if (lane == 0 && !(a.drop_first_load && i == 0)) {      // (failure-detection test: the first stage's signal never comes)
+        mbar_expect_tx(y1_full + 8 * s, kTile);
+        for (int c = 0; c < kChunks; ++c) tma_load_3d(y1 + s * kTile + c * kChunkBytes, kKeys ? &tm_q : &tm_k, 64 * c, h, row, y1_full + 8 * s);
+      }
+      if (kKeys) {      // lse and delta of the tile's rows; a row behind the sequence's last has probabilities 0
+        ok = __all_sync(0xffffffffu, wait(st_empty + 8 * s, (turn & 1) ^ 1));
+        if (!ok) break;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = (t0 + i % tiles) * 128 + 32 * k + lane;
+          const size_t at = (size_t)h * a.r.seq.rows + u.a + r;
+          stats[s * 256 + 32 * k + lane] = r < n_rows ? __ldg(a.r.lse + at) : kInf;
+          stats[s * 256 + 128 + 32 * k + lane] = r < n_rows ? __ldg(a.r.delta + at) : 0.f;
+        }
+        mbar_arrive(st_full + 8 * s);
+      }
+      ok = __all_sync(0xffffffffu, wait(y2_empty + 8 * s, (turn & 1) ^ 1));
+      if (!ok) break;
+      issued2 = i + 1;
+      if (lane == 0) {
+        mbar_expect_tx(y2_full + 8 * s, kTile);
+        for (int c = 0; c < kChunks; ++c) tma_load_3d(y2 + s * kTile + c * kChunkBytes, kKeys ? &tm_dy : &tm_v, 64 * c, h, row, y2_full + 8 * s);
+      }
+    }
+  } else if (warp == 9) {
+    if (lane == 0) {
+      const int k_steps = (a.r.width + 15) / 16;
+      const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_acc = idesc_bf16(128, 16 * k_steps, true);
+      auto product = [&](uint32_t d, uint32_t x, uint32_t y) {      // X Y^T over the head
+        for (int k = 0; k < k_steps; ++k) {
+          const uint32_t off = (k >> 2) * kChunkBytes + (k & 3) * 32;
+          umma_ss(tmem + d, desc_k(x + off), desc_k(y + off), idesc_s, k > 0);
+        }
+      };
+      auto accumulate = [&](uint32_t d, uint32_t p, uint32_t y, bool more) {      // P Y over the tile's rows; P's halves are 64 columns apart
+        for (int k = 0; k < 8; ++k) umma_ts(tmem + d, tmem + p + 64 * (k >> 2) + 8 * (k & 3), desc_mn(y + k * 2048), idesc_acc, more || k > 0);
+      };
+      auto dp_at = [&](int i) { return kDp + (kKeys ? 0 : 128 * (i & 1)); };
+      auto issue_s = [&](int i) {
+        if (!wait(y1_full + 8 * (i % kSt), (i / kSt) & 1)) return false;
+        fence_after();
+        product(kS, x1, y1 + (i % kSt) * kTile);
+        umma_commit(s_full);
+        return true;
+      };
+      auto issue_dp = [&](int i) {
+        if (!wait(y2_full + 8 * (i % kSt), (i / kSt) & 1)) return false;
+        fence_after();
+        product(dp_at(i), x2, y2 + (i % kSt) * kTile);
+        umma_commit(dp_full + (kKeys ? 0 : 8 * (i & 1)));
+        if (!kKeys) umma_commit(y2_empty + 8 * (i % kSt));
+        return true;
+      };
+      bool ok = wait(x_full, 0) && issue_s(0) && issue_dp(0);
+      for (int i = 0; i < n && ok; ++i) {
+        const int s = i % kSt;
+        if (kKeys) {
+          if (!(ok = wait(p_full, i & 1))) break;
+          fence_after();
+          accumulate(kAcc2, kS, y2 + s * kTile, i > 0);
+          umma_commit(y2_empty + 8 * s);
+          if (i + 1 < n && !(ok = issue_s(i + 1))) break;
+          if (!(ok = wait(ds_full, i & 1))) break;
+          fence_after();
+          accumulate(kAcc1, kDp, y1 + s * kTile, i > 0);
+          umma_commit(y1_empty + 8 * s);
+          if (i + 1 < n && !(ok = issue_dp(i + 1))) break;
+        } else {
+          if (i + 1 < n) {
+            if (!(ok = wait(p_full, i & 1))) break;      // S has been read
+            fence_after();
+            if (!(ok = issue_s(i + 1) && issue_dp(i + 1))) break;
+          }
+          if (!(ok = wait(ds_full, i & 1))) break;
+          fence_after();
+          accumulate(kAcc1, dp_at(i), y1 + s * kTile, i > 0);
+          umma_commit(y1_empty + 8 * s);
+        }
+      }
+      if (ok) umma_commit(acc_full);
+      if (*abort_flag) { umma_commit(drain); mbar_wait(drain, 0, abort_flag + 1); }
+    }
+    __syncwarp();
+  } else {
+    const int e = (warp & 3) * 32 + lane, half = warp >> 2, row = u.row0 + e;      // own row of the sequence (a key, or a query)
+    const bool mine = row < n_rows;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    float lse = kInf, delta = 0.f;
+    if (!kKeys && mine) {
+      lse = a.r.lse[(size_t)head * a.r.seq.rows + u.a + row];
+      delta = a.r.delta[(size_t)head * a.r.seq.rows + u.a + row];
+    }
+    bool ok = true;
+    for (int i = 0; i < n; ++i) {
+      const int c0 = (t0 + i % tiles) * 128 + 64 * half;      // the first of this thread's columns
+      // columns [lo, hi) are seen
+      int lo, hi;
+      if (kKeys) {
+        lo = a.r.causal ? row - c0 : 0;
+        hi = a.r.window ? (int)min(64LL, (long long)row + a.r.window - c0) : 64;
+      } else {
+        hi = (a.r.causal ? min(row + 1, n_rows) : n_rows) - c0;
+        lo = a.r.window ? row - a.r.window + 1 - c0 : 0;
+      }
+      const float4* st = reinterpret_cast<const float4*>(stats + (i % kSt) * 256 + 64 * half);
+      ok = __all_sync(0xffffffffu, wait(s_full, i & 1));
+      if (ok && kKeys) ok = __all_sync(0xffffffffu, wait(st_full + 8 * (i % kSt), (i / kSt) & 1));
+      if (!ok) break;
+      fence_after();
+      uint32_t v[64];
+      float p[64];
+      tmem_ld32(tmem + lanes + kS + 64 * half, v);
+      tmem_ld32(tmem + lanes + kS + 64 * half + 32, v + 32);
+      tmem_ld_wait();
+      if (!kKeys) {
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full);
+      }
+#pragma unroll
+      for (int c = 0; c < 64; c += 4) {
+        float4 l = make_float4(lse, lse, lse, lse);
+        if (kKeys) l = st[c / 4];
+        p[c] = exp2_fast(fmaf(__uint_as_float(v[c]), a.r.scale, -l.x));
+        p[c + 1] = exp2_fast(fmaf(__uint_as_float(v[c + 1]), a.r.scale, -l.y));
+        p[c + 2] = exp2_fast(fmaf(__uint_as_float(v[c + 2]), a.r.scale, -l.z));
+        p[c + 3] = exp2_fast(fmaf(__uint_as_float(v[c + 3]), a.r.scale, -l.w));
+      }
+      if (!__all_sync(0xffffffffu, lo <= 0 && hi >= 64)) {
+#pragma unroll
+        for (int c = 0; c < 64; ++c) if (c < lo || c >= hi) p[c] = 0.f;
+      }
+      if (kKeys) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) v[c] = bf16_pair(p[2 * c], p[2 * c + 1]);
+        tmem_st32(tmem + lanes + kS + 64 * half, v);
+        tmem_st_wait();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full);
+      }
+      const uint32_t dp = tmem + lanes + kDp + (kKeys ? 0 : 128 * (i & 1)) + 64 * half;
+      ok = __all_sync(0xffffffffu, wait(dp_full + (kKeys ? 0 : 8 * (i & 1)), (kKeys ? i : i >> 1) & 1));
+      if (!ok) break;
+      fence_after();
+      tmem_ld32(dp, v);
+      tmem_ld32(dp + 32, v + 32);
+      tmem_ld_wait();
+#pragma unroll
+      for (int c = 0; c < 64; c += 4) {
+        float4 d = make_float4(delta, delta, delta, delta);
+        if (kKeys) d = st[32 + c / 4];
+        const float s0 = p[c] * (__uint_as_float(v[c]) - d.x), s1 = p[c + 1] * (__uint_as_float(v[c + 1]) - d.y);
+        const float s2 = p[c + 2] * (__uint_as_float(v[c + 2]) - d.z), s3 = p[c + 3] * (__uint_as_float(v[c + 3]) - d.w);
+        v[c / 2] = bf16_pair(s0, s1);
+        v[c / 2 + 1] = bf16_pair(s2, s3);
+      }
+      tmem_st32(dp, v);
+      tmem_st_wait();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(ds_full);
+        if (kKeys) mbar_arrive(st_empty + 8 * (i % kSt));
+      }
+    }
+    if (ok) {
+      ok = __all_sync(0xffffffffu, wait(acc_full, 0));
+      fence_after();
+    }
+    bool fine = true;
+    if (ok) {      // a warp writes half of the head's elements
+      const size_t at = ((size_t)(u.a + row) * n_heads + head) * a.r.width;
+      auto write = [&](uint32_t acc, void* out, int type, float factor) {
+#pragma unroll 1
+        for (int c = 32 * kChunks * half; c < min(a.r.width, 32 * kChunks * (half + 1)); c += 16) {
+          uint32_t o[16];
+          float f[16];
+          tmem_ld16(tmem + lanes + acc + c, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int k = 0; k < 16; ++k) { f[k] = __uint_as_float(o[k]) * factor; fine &= fabsf(f[k]) < kInf; }
+          if (mine && out) {
+            store_any<8>(out, type, at + c, f);
+            if (c + 8 < a.r.width) store_any<8>(out, type, at + c + 8, f + 8);
+          }
+        }
+      };
+      if (kKeys) {
+        write(kAcc1, a.r.dk, a.r.dkt, a.r.raw_scale);
+        write(kAcc2, a.r.dv, a.r.dvt, 1.f);
+      } else {
+        write(kAcc1, a.r.out, a.r.ot, a.r.raw_scale);
+      }
+    }
+    // rows that are not finite: again, after both halves have been written (every warp comes here, after an unwind too)
+    const unsigned bad = __ballot_sync(0xffffffffu, mine && !fine);
+    if (lane == 0) again[warp] = bad;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (half == 0)
+      for (unsigned b = again[warp] | again[warp + 4]; b; b &= b - 1) {
+        const int r = u.a + u.row0 + (warp & 3) * 32 + __ffs(b) - 1;
+        if (kKeys) dkv_of_row(a.r, head, r, lane);
+        else dq_of_row(a.r, head, r, lane);
+      }
+  }
+  fence_before();
+  __syncthreads();
+  if (*abort_flag) {      // an unwind: what the producer has handed to the TMA engine lands before the shared memory goes away
+    if (threadIdx.x == 256) {
+      mbar_wait(x_full, 0, abort_flag + 1);
+      for (int k = std::max(a.drop_first_load ? 1 : 0, issued1 - kSt); k < issued1; ++k) mbar_wait(y1_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
+      for (int k = std::max(0, issued2 - kSt); k < issued2; ++k) mbar_wait(y2_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
+    }
+    __syncthreads();
+  }
+  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// delta = sum(dy y) of every row and head: a head in the next power of two of lanes, 8 elements a lane
+__global__ void __launch_bounds__(256) attention_delta(const __grid_constant__ RowArgs a, int lanes) {
+  if (blockIdx.x == 0 && threadIdx.x == 0 && a.status_clear) *a.status_clear = 0;
+  const int lane = threadIdx.x & 31, l = lane & (lanes - 1);
+  const long long i = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * (32 / lanes) + lane / lanes, n = (long long)a.seq.rows * a.heads;      // row by row, head by head
+  float sum = 0.f;
+  if (i < n && 8 * l < a.width) {
+    float y[8], d[8];
+    load_any<8>(a.y, a.yt, (size_t)i * a.width + 8 * l, y);
+    load_any<8>(a.dy, DRAGON_BF16, (size_t)i * a.width + 8 * l, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += y[e] * d[e];
+  }
+  for (int s = lanes >> 1; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+  if (i < n && l == 0) a.delta[(size_t)(i % a.heads) * a.seq.rows + i / a.heads] = sum;
+}
+
+template <bool kKeys, int kChunks> int launch_bwd(const BwdArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& dy, cudaStream_t st) {
+  static const char* who = "Attention's gradient";
+  static bool set[64] = {};
+  const int rc = allow_smem(reinterpret_cast<const void*>(attention_bwd<kKeys, kChunks>), bwd_smem(kChunks), set, who);
+  if (rc != DRAGON_OK) return rc;
+  const long long grid = (long long)a.blocks * (kKeys ? a.r.kv_heads : a.r.heads);
+  if (grid > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
+  attention_bwd<kKeys, kChunks><<<(unsigned)grid, kBwdThreads, bwd_smem(kChunks), st>>>(q, k, v, dy, a);
+  return launched(who);
+}
+
+}  // namespace
+
+size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads) { return (size_t)(rows * heads) * sizeof(float); }
+int attention_bwd_launches(const Step& s) { return 1 + (s.wr[at::DQ] >= 0) + (s.wr[at::DK] >= 0 || s.wr[at::DV] >= 0); }
+
+int launch_attention_backward(const RowArgs& rows, cudaStream_t st) {
+  BwdArgs a = {};
+  a.r = rows;
+  count_blocks(rows.seq, 128, &a.blocks, &a.each_blocks);
+  wait_settings("DRAGON_ATTENTION", &a.budget, &a.drop_first_load);
+  CUtensorMap q, k, v, dy;
+  if (!head_map(&q, rows.q, rows.seq.rows, rows.heads, rows.width, 128) || !head_map(&k, rows.k, rows.seq.rows, rows.kv_heads, rows.width, 128) ||
+      !head_map(&v, rows.v, rows.seq.rows, rows.kv_heads, rows.width, 128) || !head_map(&dy, rows.dy, rows.seq.rows, rows.heads, rows.width, 128)) {
+    set_error("Attention's gradient: cannot encode the TMA descriptors (no CUDA driver?)");
+    return DRAGON_ERR_CUDA;
+  }
+  int lanes = 1;
+  while (lanes * 8 < rows.width) lanes *= 2;
+  const long long warps = ((long long)rows.seq.rows * rows.heads * lanes + 31) / 32;
+  attention_delta<<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(rows, lanes);
+  int rc = launched("Attention's gradient");
+  const bool wide = rows.width > 64;
+  if (rc == DRAGON_OK && rows.out) rc = wide ? launch_bwd<false, 2>(a, q, k, v, dy, st) : launch_bwd<false, 1>(a, q, k, v, dy, st);
+  if (rc == DRAGON_OK && (rows.dk || rows.dv)) rc = wide ? launch_bwd<true, 2>(a, q, k, v, dy, st) : launch_bwd<true, 1>(a, q, k, v, dy, st);
+  return rc;
+}
+
+}  // namespace dragon

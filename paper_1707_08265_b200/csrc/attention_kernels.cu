@@ -8,17 +8,8 @@
 
 namespace dragon {
 int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, cudaStream_t st, const char* who);
+int launch_attention_backward(const RowArgs& rows, cudaStream_t st);
 namespace {
-
-__global__ void __launch_bounds__(128) row_attention_dq(const RowArgs a) {
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && a.status_clear) *a.status_clear = 0;
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row < a.seq.rows) dq_of_row(a, blockIdx.y, row, threadIdx.x & 31);
-}
-__global__ void __launch_bounds__(128) row_attention_dkv(const RowArgs a) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row < a.seq.rows) dkv_of_row(a, blockIdx.y, row, threadIdx.x & 31);
-}
 
 RowArgs row_args(const StepRun& r) {
   const std::vector<double>& n = r.s.num;
@@ -41,8 +32,6 @@ RowArgs row_args(const StepRun& r) {
 
 }  // namespace
 
-size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads) { return (size_t)(rows * heads) * sizeof(float); }
-int attention_bwd_launches(const Step&) { return 2; }
 int paged_launches(const Step&, const std::vector<MemRef>&) { return 1; }
 size_t paged_scratch_bytes(int64_t, int64_t, int64_t, int64_t, int64_t, int) { return 0; }
 
@@ -62,10 +51,7 @@ int launch_attention_bwd(const StepRun& r) {
   a.dk = r.wr(at::DK); a.dkt = r.wr_type(at::DK);
   a.dv = r.wr(at::DV); a.dvt = r.wr_type(at::DV);
   a.delta = reinterpret_cast<float*>(r.ws + r.s.scratch_off);
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
-  row_attention_dq<<<dim3((a.seq.rows + 3) / 4, a.heads), 128, 0, st>>>(a);
-  row_attention_dkv<<<dim3((a.seq.rows + 3) / 4, a.kv_heads), 128, 0, st>>>(a);
-  return launched("Attention's gradient");
+  return launch_attention_backward(a, reinterpret_cast<cudaStream_t>(r.stream));
 }
 
 int launch_paged_attention(const StepRun& r) {

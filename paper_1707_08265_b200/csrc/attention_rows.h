@@ -95,24 +95,20 @@ template <bool kPaged> __device__ __noinline__ void attend_row(const RowArgs& a,
   if (a.lse && lane == 0) a.lse[(size_t)h * a.seq.rows + row] = sum == 0.f ? kInf : top + log2f(sum);
 }
 
-// dq of a row, and delta = sum(dy y)
+// dq of a row
 __device__ __noinline__ void dq_of_row(const RowArgs& a, int h, int row, int lane) {
   const int kvh = h / (a.heads / a.kv_heads);
   const int s = a.seq.of_row(row);
   const size_t base = (size_t)row * a.heads * a.width + (size_t)h * a.width;
-  float q[4], d[4], dq[4] = {0.f, 0.f, 0.f, 0.f}, delta = 0.f;
+  float q[4], d[4], dq[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const bool in = lane + 32 * e < a.width;
     q[e] = in ? at(a.q, base + lane + 32 * e) : 0.f;
     d[e] = in ? at(a.dy, base + lane + 32 * e) : 0.f;
-    float y = 0.f;
-    if (in) load_any<1>(a.y, a.yt, base + lane + 32 * e, &y);
-    delta += y * d[e];
   }
-  delta = warp_sum(delta);
   const size_t st = (size_t)h * a.seq.rows + row;
-  if (lane == 0) a.delta[st] = delta;
+  const float delta = a.delta[st];
   int first = 0, last = 0, r0 = 0, r1 = 0;
   if (s >= 0) { a.seq.rows_of(s, &r0, &r1); seen_by(a, row - r0, r1 - r0, &first, &last); }
   const float lse = a.lse[st];

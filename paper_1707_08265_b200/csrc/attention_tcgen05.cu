@@ -37,49 +37,6 @@ struct FwdArgs {
   int drop_first_load;
 };
 
-struct FwdUnit {
-  int seq, a, b;        // the sequence (-1: none) and its rows
-  int row0;             // first row of tile 0, from a
-  int first_pos;        // position of row a (paged: behind the tokens that were there)
-  int keys;             // keys there are
-  int spare, spares;    // seq < 0: which of how many units that are left over
-};
-
-// Which block of rows this unit has: blocks of a sequence from its end (those that see most keys go first)
-__device__ __forceinline__ void find_unit(const FwdArgs& a, int unit, int block_rows, FwdUnit* u, int lane) {
-  const Sequences& q = a.r.seq;
-  u->seq = -1;
-  if (a.each_blocks) {
-    const int s = unit % q.count;
-    q.rows_of(s, &u->a, &u->b);
-    u->seq = s;
-    u->row0 = (a.each_blocks - 1 - unit / q.count) * block_rows;
-    return;
-  }
-  int before = 0;
-  for (int s0 = 0; s0 < q.count; s0 += 32) {
-    int x = 0, y = 0;
-    if (s0 + lane < q.count) q.rows_of(s0 + lane, &x, &y);
-    const int n = (y - x + block_rows - 1) / block_rows;
-    int sum = n;
-#pragma unroll
-    for (int k = 1; k < 32; k <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, k); if (lane >= k) sum += t; }
-    const int local = unit - before;
-    const unsigned hit = __ballot_sync(0xffffffffu, local >= sum - n && local < sum);
-    if (hit) {
-      const int w = __ffs(hit) - 1;
-      u->seq = s0 + w;
-      u->a = __shfl_sync(0xffffffffu, x, w);
-      u->b = __shfl_sync(0xffffffffu, y, w);
-      u->row0 = (__shfl_sync(0xffffffffu, sum, w) - 1 - local) * block_rows;
-      return;
-    }
-    before += __shfl_sync(0xffffffffu, sum, 31);
-  }
-  u->spare = unit - before;
-  u->spares = a.blocks - before;
-}
-
 template <bool kPaged, int kChunks>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ FwdArgs a) {
@@ -93,7 +50,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const uint32_t s_full = v_empty + 8 * kSt, p_full = s_full + 16, o_full = p_full + 16, v_clean = o_full + 16, drain = v_clean + 8;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 10 + 4 * kSt);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  __shared__ FwdUnit unit;
+  __shared__ Unit unit;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int block_rows = a.by_heads ? 128 : 256, pair = blockIdx.x % a.pairs, group = a.r.heads / a.r.kv_heads;
   const int head0 = a.by_heads ? 2 * pair : pair, kvh = head0 / group;
@@ -112,8 +69,8 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   }
   if (blockIdx.x == 0 && !a.r.seq.in_order()) report(a.r.status, DRAGON_ERR_INVALID_ARG);
   if (warp == 0) {
-    FwdUnit u;
-    find_unit(a, blockIdx.x / a.pairs, block_rows, &u, lane);
+    Unit u;
+    find_unit(a.r.seq, a.blocks, a.each_blocks, blockIdx.x / a.pairs, block_rows, &u, lane);
     if (u.seq >= 0) {
       u.keys = u.b - u.a;
       u.first_pos = 0;
@@ -127,13 +84,10 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     if (lane == 0) unit = u;
   }
   __syncthreads();
-  const FwdUnit u = unit;
+  const Unit u = unit;
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
-    const int first = a.r.seq.starts ? min(max(__ldg(a.r.seq.starts), 0), a.r.seq.rows) : 0;
-    const int last = a.r.seq.starts ? min(max(__ldg(a.r.seq.starts + a.r.seq.count), first), a.r.seq.rows) : a.r.seq.rows;
-    const int none = first + a.r.seq.rows - last, wide = (a.by_heads ? 2 : 1) * a.r.width;
-    for (int i = u.spare; i < none; i += u.spares) {
-      const int row = i < first ? i : last + i - first;
+    const int wide = (a.by_heads ? 2 : 1) * a.r.width;
+    for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (a.r.out) for (int c = 8 * threadIdx.x; c < wide; c += 8 * kFwdThreads) store_any<8>(a.r.out, a.r.ot, ((size_t)row * a.r.heads + head0) * a.r.width + c, zero);
       if (a.r.lse && threadIdx.x < (a.by_heads ? 2 : 1)) a.r.lse[(size_t)(head0 + threadIdx.x) * a.r.seq.rows + row] = kInf;
@@ -387,8 +341,7 @@ int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, 
   a.by_heads = group % 2 == 0;
   a.pairs = a.by_heads ? rows.heads / 2 : rows.heads;
   const int block = a.by_heads ? 128 : 256;
-  if (rows.seq.starts) a.blocks = (int)((rows.seq.rows + block - 1) / block + rows.seq.count);
-  else { a.each_blocks = (rows.seq.each + block - 1) / block; a.blocks = a.each_blocks * rows.seq.count; }
+  count_blocks(rows.seq, block, &a.blocks, &a.each_blocks);
   a.few = few;
   wait_settings("DRAGON_ATTENTION", &a.budget, &a.drop_first_load);
   CUtensorMap q, k, v;

@@ -7,6 +7,7 @@
 #include <cstdlib>
 #include <mutex>
 
+#include "attention_util.h"
 #include "plan.h"
 #include "tcgen05_util.h"
 
@@ -77,6 +78,58 @@ __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a_tmem, uint64_t b_
       ::"r"(d), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
 }
 
+// ---- units of work ---------------------------------------------------------------------------
+
+struct Unit {
+  int seq, a, b;        // the sequence (-1: none) and its rows
+  int row0;             // first row of tile 0, from a
+  int first_pos;        // position of row a (paged: behind the tokens that were there)
+  int keys;             // keys there are
+  int spare, spares;    // seq < 0: which of how many units that are left over
+};
+
+// Which block of rows this unit has: blocks of a sequence from its end (those that see most keys go first)
+// (blocks: those that the grid has room for, each_blocks: of a sequence, where all are equally long, 0: starts)
+__device__ __forceinline__ void find_unit(const Sequences& q, int blocks, int each_blocks, int unit, int block_rows, Unit* u, int lane) {
+  u->seq = -1;
+  if (each_blocks) {
+    const int s = unit % q.count;
+    q.rows_of(s, &u->a, &u->b);
+    u->seq = s;
+    u->row0 = (each_blocks - 1 - unit / q.count) * block_rows;
+    return;
+  }
+  int before = 0;
+  for (int s0 = 0; s0 < q.count; s0 += 32) {
+    int x = 0, y = 0;
+    if (s0 + lane < q.count) q.rows_of(s0 + lane, &x, &y);
+    const int n = (y - x + block_rows - 1) / block_rows;
+    int sum = n;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, k); if (lane >= k) sum += t; }
+    const int local = unit - before;
+    const unsigned hit = __ballot_sync(0xffffffffu, local >= sum - n && local < sum);
+    if (hit) {
+      const int w = __ffs(hit) - 1;
+      u->seq = s0 + w;
+      u->a = __shfl_sync(0xffffffffu, x, w);
+      u->b = __shfl_sync(0xffffffffu, y, w);
+      u->row0 = (__shfl_sync(0xffffffffu, sum, w) - 1 - local) * block_rows;
+      return;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  u->spare = unit - before;
+  u->spares = blocks - before;
+}
+
+// row i of those that belong to no sequence, -1 behind them
+__device__ __forceinline__ int row_of_none(const Sequences& q, int i) {
+  const int first = q.starts ? min(max(__ldg(q.starts), 0), q.rows) : 0;
+  const int last = q.starts ? min(max(__ldg(q.starts + q.count), first), q.rows) : q.rows;
+  return i < first ? i : i < first + q.rows - last ? last + i - first : -1;
+}
+
 // ---- host ----------------------------------------------------------------------------------
 
 // bf16 [rows, heads * width] as (element of a head, head, row), boxes of 64 elements of one head x box_rows rows
@@ -89,6 +142,12 @@ bool head_map(CUtensorMap* map, const void* ptr, int64_t rows, int heads, int wi
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// blocks of rows that a grid needs room for, and those of a sequence where all are equally long
+void count_blocks(const Sequences& q, int block_rows, int* blocks, int* each_blocks) {
+  *each_blocks = q.starts ? 0 : (q.each + block_rows - 1) / block_rows;
+  *blocks = q.starts ? (q.rows + block_rows - 1) / block_rows + q.count : *each_blocks * q.count;
 }
 
 // a kernel's dynamic shared memory, once per device (set: one flag a device)
