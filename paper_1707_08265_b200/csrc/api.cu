@@ -624,7 +624,7 @@ int dragon_function_num_launches(const dragon_function_t* f) {
     else if (st.kind == ST_CLIP) n += launches_of_tensors((int)st.wr.size());
     else if (st.kind == ST_HEAD_BWD) n += 1 + (st.wr[hb::DGAIN] >= 0 ? 1 : 0);
     else if (st.kind == ST_ATTN_BWD) n += attention_bwd_launches(st);
-    else if (st.kind == ST_PAGED) n += paged_launches(st, f->plan.mems);
+    else if (st.kind == ST_PAGED) n += paged_launches(st, f->plan.mems, f->plan.sm_count);
     else if (st.kind != ST_COPY) n += 1 + (st.mF >= 0 ? 1 : 0);
   }
   return n;

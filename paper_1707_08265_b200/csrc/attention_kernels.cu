@@ -1,4 +1,4 @@
-// Attention over packed sequences, forward and backward, and over a paged cache: one warp for each row of a head.
+// Attention's steps of the plan: their operands for the kernels.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -25,15 +25,13 @@ RowArgs row_args(const StepRun& r) {
   a.seq.starts = reinterpret_cast<const int*>(r.rd(at::STARTS));
   a.seq.count = a.seq.starts ? (int)r.mems[r.s.rd[at::STARTS]].shape.d[0] - 1 : (int)n[an::SEQUENCES];
   a.seq.each = a.seq.rows / a.seq.count;
+  a.splits = 1;
   a.status = r.status;
   a.status_clear = r.status_clear;
   return a;
 }
 
 }  // namespace
-
-int paged_launches(const Step&, const std::vector<MemRef>&) { return 1; }
-size_t paged_scratch_bytes(int64_t, int64_t, int64_t, int64_t, int64_t, int) { return 0; }
 
 int launch_attention(const StepRun& r) {
   RowArgs a = row_args(r);
@@ -52,31 +50,6 @@ int launch_attention_bwd(const StepRun& r) {
   a.dv = r.wr(at::DV); a.dvt = r.wr_type(at::DV);
   a.delta = reinterpret_cast<float*>(r.ws + r.s.scratch_off);
   return launch_attention_backward(a, reinterpret_cast<cudaStream_t>(r.stream));
-}
-
-int launch_paged_attention(const StepRun& r) {
-  const std::vector<double>& n = r.s.num;
-  const Shape &sh = r.mems[r.s.rd[pa::Q]].shape, &tb = r.mems[r.s.rd[pa::PAGES]].shape;
-  RowArgs a = {};
-  a.q = reinterpret_cast<const unsigned short*>(r.rd(pa::Q));
-  a.k = reinterpret_cast<const unsigned short*>(r.rd(pa::K));
-  a.v = reinterpret_cast<const unsigned short*>(r.rd(pa::V));
-  a.out = r.wr(pa::Y); a.ot = r.wr_type(pa::Y);
-  a.heads = (int)n[pn::HEADS]; a.kv_heads = (int)n[pn::KV_HEADS]; a.width = (int)(sh.d[1] / a.heads);
-  a.causal = 1; a.window = (int)n[pn::WINDOW];
-  a.scale = (float)(n[pn::SCALE] * 1.4426950408889634);
-  a.seq.rows = (int)sh.d[0]; a.seq.count = (int)tb.d[0];
-  a.seq.starts = reinterpret_cast<const int*>(r.rd(pa::STARTS));
-  a.seq.each = a.seq.rows / a.seq.count;
-  a.pages.pages = reinterpret_cast<const int*>(r.rd(pa::PAGES));
-  a.pages.lengths = reinterpret_cast<const int*>(r.rd(pa::LENGTHS));
-  a.pages.most = (int)tb.d[1];
-  a.pages.shift = 0;
-  while ((1 << a.pages.shift) < (int)n[pn::PAGE]) ++a.pages.shift;
-  a.pages.pool = (int)(r.mems[r.s.rd[pa::K]].shape.d[0] >> a.pages.shift);
-  a.status = r.status;
-  a.status_clear = r.status_clear;
-  return launch_attention_forward(a, true, r.mems[r.s.rd[pa::K]].shape.d[0], 0, reinterpret_cast<cudaStream_t>(r.stream), "PagedAttention");
 }
 
 }  // namespace dragon

@@ -25,6 +25,9 @@ struct RowArgs {
   float raw_scale;
   Sequences seq;
   Pages pages;
+  // keys of a sequence split over `splits` CTAs: every part's result and the log2 of its sum (-inf: no keys), [split][row][head]
+  int splits;
+  float *part, *part_lse;
   int* status;
   int* status_clear;
 };

@@ -1,8 +1,9 @@
 // Attention's forward pass on the tensor cores: y = softmax(scale q k^T) v over packed sequences or over a paged cache.
 // Hand-written for sm_100a.
 //
-// A CTA works on two tiles of 128 query rows that see the same keys: the same rows of two query heads that share a key head,
-// or (where heads do not come in pairs) two neighbouring blocks of rows.  Keys and values pass once, 128 at a time:
+// A CTA works on two tiles of 128 query rows that see the same keys: where the heads of a group are a power of two, all of them
+// for 128 / group neighbouring rows of the sequence in each tile; otherwise the same 128 rows of two heads of a group, or 256 rows
+// of one head.  Keys and values pass once, 128 at a time:
 //   S_t = Q_t K^T              tcgen05.mma, both operands in shared memory (TMA, 128-byte swizzle), S_t in TMEM
 //   P_t = exp2(scale' S_t - m) one thread a row: the running maximum m and sum stay in its registers; P_t goes back over S_t as
 //                              bf16 (its sum is taken in fp32 before the rounding)
@@ -10,7 +11,7 @@
 // While the softmax threads of one tile work, the tensor unit works for the other.  m only moves when a row's maximum has grown
 // by more than 2^8 (P_t and the sum then stay below 2^8 times their scale, far inside bf16 and fp32): O_t in TMEM is rescaled
 // that seldom that the softmax threads do it themselves.  S_t of the next keys is issued behind O_t's product, so a completed
-// S_t says that O_t may be touched.
+// S_t says that O_t may be touched.  A paged cache's keys can be split over several CTAs (few rows, long contexts).
 // Warps: 0..3 and 4..7 softmax of tile 0 and 1 (a warp its TMEM lanes), 8 TMA, 9 MMA.  Every wait is bounded.
 #include <algorithm>
 #include <cstdlib>
@@ -28,8 +29,9 @@ constexpr float kRescale = 8.f;
 
 struct FwdArgs {
   RowArgs r;
-  int by_heads;         // the two tiles are two heads' (1) or two blocks' of rows
-  int pairs;            // pairs of heads, or heads
+  int pack_shift;       // log2 of the heads in a tile
+  int by_heads;         // (one head a tile) the two tiles are two heads' of the same rows, not two blocks of rows
+  int columns;          // units side by side: key heads (several heads a tile), pairs of heads, or heads
   int blocks;           // blocks of rows that the grid has room for
   int each_blocks;      // of a sequence, where all are equally long (0: starts)
   int few;              // paged: sequences of at most so many rows are not this kernel's
@@ -52,8 +54,9 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   __shared__ Unit unit;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int block_rows = a.by_heads ? 128 : 256, pair = blockIdx.x % a.pairs, group = a.r.heads / a.r.kv_heads;
-  const int head0 = a.by_heads ? 2 * pair : pair, kvh = head0 / group;
+  const int pack = 1 << a.pack_shift, tile_rows = 128 >> a.pack_shift, block_rows = a.by_heads ? 128 : 2 * tile_rows;      // rows: of the sequence
+  const int column = blockIdx.x % a.columns, group = a.r.heads / a.r.kv_heads, heads_here = a.by_heads ? 2 : pack;
+  const int head0 = column * heads_here, kvh = head0 / group;
 
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
@@ -65,12 +68,12 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     mbar_init(drain, 1);
     abort_flag[0] = abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    if (blockIdx.x == 0 && a.r.status_clear) *a.r.status_clear = 0;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && a.r.status_clear) *a.r.status_clear = 0;
   }
-  if (blockIdx.x == 0 && !a.r.seq.in_order()) report(a.r.status, DRAGON_ERR_INVALID_ARG);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && !a.r.seq.in_order()) report(a.r.status, DRAGON_ERR_INVALID_ARG);
   if (warp == 0) {
     Unit u;
-    find_unit(a.r.seq, a.blocks, a.each_blocks, blockIdx.x / a.pairs, block_rows, &u, lane);
+    find_unit(a.r.seq, a.blocks, a.each_blocks, blockIdx.x / a.columns, block_rows, &u, lane);
     if (u.seq >= 0) {
       u.keys = u.b - u.a;
       u.first_pos = 0;
@@ -86,11 +89,12 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   __syncthreads();
   const Unit u = unit;
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
-    const int wide = (a.by_heads ? 2 : 1) * a.r.width;
+    if (a.r.splits > 1) return;      // (where the parts are put together)
+    const int wide = heads_here * a.r.width;
     for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (a.r.out) for (int c = 8 * threadIdx.x; c < wide; c += 8 * kFwdThreads) store_any<8>(a.r.out, a.r.ot, ((size_t)row * a.r.heads + head0) * a.r.width + c, zero);
-      if (a.r.lse && threadIdx.x < (a.by_heads ? 2 : 1)) a.r.lse[(size_t)(head0 + threadIdx.x) * a.r.seq.rows + row] = kInf;
+      if (a.r.lse && threadIdx.x < heads_here) a.r.lse[(size_t)(head0 + threadIdx.x) * a.r.seq.rows + row] = kInf;
     }
     return;
   }
@@ -100,7 +104,12 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const int last_row = min(u.row0 + block_rows, n_rows) - 1;      // (row0 < n_rows)
   const int key_end = a.r.causal ? max(0, min(u.keys, u.first_pos + last_row + 1)) : u.keys;
   const int key_begin = a.r.window ? max(0, u.first_pos + u.row0 - a.r.window + 1) : 0;
-  const int j0 = key_begin / 128, n_tiles = key_end > key_begin ? (key_end + 127) / 128 - j0 : 0;
+  int j0 = key_begin / 128, n_tiles = key_end > key_begin ? (key_end + 127) / 128 - j0 : 0;
+  if (kPaged && a.r.splits > 1) {
+    const int each = (n_tiles + a.r.splits - 1) / a.r.splits, skip = min(n_tiles, (int)blockIdx.y * each);
+    j0 += skip;
+    n_tiles = min(each, n_tiles - skip);
+  }
   const bool ragged = u.keys - (j0 + n_tiles - 1) * 128 < 128;      // the last tile has rows behind the sequence's last key
 
   if (warp == 9) {
@@ -123,7 +132,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       for (int t = 0; t < 2; ++t) {
         mbar_expect_tx(q_full + 8 * t, kTile);
         for (int c = 0; c < kChunks; ++c)
-          tma_load_3d(q_at + t * kTile + c * kChunkBytes, &tm_q, 64 * c, a.by_heads ? head0 + t : head0, u.a + u.row0 + (a.by_heads ? 0 : 128 * t), q_full + 8 * t);
+          tma_load_3d(q_at + t * kTile + c * kChunkBytes, &tm_q, 64 * c, a.by_heads ? head0 + t : head0, u.a + u.row0 + (a.by_heads ? 0 : tile_rows * t), q_full + 8 * t);
       }
     }
     __syncwarp();
@@ -211,7 +220,8 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     __syncwarp();
   } else {
     const int t = warp >> 2, e = (warp & 3) * 32 + lane;
-    const int head = a.by_heads ? head0 + t : head0, i = u.row0 + (a.by_heads ? 0 : 128 * t) + e;      // this thread's row of the sequence
+    const int head = a.by_heads ? head0 + t : head0 + (e & (pack - 1));
+    const int i = u.row0 + (a.by_heads ? 0 : tile_rows * t) + (e >> a.pack_shift);      // this thread's row of the sequence
     const int pos = u.first_pos + i;
     const bool mine = i < n_rows;
     // the keys that the row sees
@@ -297,15 +307,25 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
           v[k] = n_tiles > 0 ? __uint_as_float(o[k]) * inv : 0.f;
           fine &= fabsf(v[k]) < kInf;
         }
-        if (mine && a.r.out) {
+        if (kPaged && a.r.splits > 1) {
+          float* to = a.r.part + ((size_t)blockIdx.y * a.r.seq.rows * a.r.heads * a.r.width + at + c);
+          if (mine && n_tiles > 0) {
+            store_any<8>(to, DRAGON_F32, 0, v);
+            if (c + 8 < a.r.width) store_any<8>(to, DRAGON_F32, 8, v + 8);
+          }
+        } else if (mine && a.r.out) {
           store_any<8>(a.r.out, a.r.ot, at + c, v);
           if (c + 8 < a.r.width) store_any<8>(a.r.out, a.r.ot, at + c + 8, v + 8);
         }
       }
+      if (kPaged && a.r.splits > 1) {      // (where the parts are put together a row that is not finite is computed again)
+        if (mine) a.r.part_lse[((size_t)blockIdx.y * a.r.seq.rows + row) * a.r.heads + head] = sum == 0.f ? -kInf : top * a.r.scale + log2f(sum);
+        fine = true;
+      }
       if (mine && a.r.lse) a.r.lse[(size_t)head * a.r.seq.rows + row] = sum == 0.f ? kInf : top * a.r.scale + log2f(sum);
       __syncwarp();
       for (unsigned again = __ballot_sync(0xffffffffu, mine && !fine); again; again &= again - 1)
-        attend_row<kPaged>(a.r, head, __shfl_sync(0xffffffffu, row, __ffs(again) - 1), lane);
+        attend_row<kPaged>(a.r, __shfl_sync(0xffffffffu, head, __ffs(again) - 1), __shfl_sync(0xffffffffu, row, __ffs(again) - 1), lane);
     }
   }
   fence_before();
@@ -325,28 +345,40 @@ template <bool kPaged, int kChunks> int launch_fwd(const FwdArgs& a, const CUten
   static bool set[64] = {};
   const int rc = allow_smem(reinterpret_cast<const void*>(attention_fwd<kPaged, kChunks>), fwd_smem(kChunks), set, who);
   if (rc != DRAGON_OK) return rc;
-  const long long grid = (long long)a.blocks * a.pairs;
+  const long long grid = (long long)a.blocks * a.columns;
   if (grid > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
-  attention_fwd<kPaged, kChunks><<<(unsigned)grid, kFwdThreads, fwd_smem(kChunks), st>>>(q, k, v, a);
+  attention_fwd<kPaged, kChunks><<<dim3((unsigned)grid, a.r.splits), kFwdThreads, fwd_smem(kChunks), st>>>(q, k, v, a);
   return launched(who);
 }
 
 }  // namespace
+
+// whether a tile holds all heads of a group
+static bool packs(int group) { return (group & (group - 1)) == 0 && group <= 128; }
+
+// units of work that the kernel has at least room for, without splits
+int64_t attention_units(int64_t rows, int64_t sequences, int heads, int kv_heads) {
+  const int group = heads / kv_heads;
+  const int64_t block = packs(group) ? 256 / group : group % 2 == 0 ? 128 : 256;
+  return std::max<int64_t>(sequences, (rows + block - 1) / block) * (packs(group) ? kv_heads : group % 2 == 0 ? heads / 2 : heads);
+}
 
 // rows: what the row functions need as well; key_rows: rows of k and v in memory; few: rows x group of a sequence up to which another kernel has it
 int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, cudaStream_t st, const char* who) {
   FwdArgs a = {};
   a.r = rows;
   const int group = rows.heads / rows.kv_heads;
-  a.by_heads = group % 2 == 0;
-  a.pairs = a.by_heads ? rows.heads / 2 : rows.heads;
-  const int block = a.by_heads ? 128 : 256;
+  const bool packed = packs(group);
+  while (packed && (1 << a.pack_shift) < group) ++a.pack_shift;
+  a.by_heads = !packed && group % 2 == 0;
+  a.columns = packed ? rows.kv_heads : a.by_heads ? rows.heads / 2 : rows.heads;
+  const int block = a.by_heads ? 128 : 256 >> a.pack_shift;
   count_blocks(rows.seq, block, &a.blocks, &a.each_blocks);
   a.few = few;
   wait_settings("DRAGON_ATTENTION", &a.budget, &a.drop_first_load);
   CUtensorMap q, k, v;
   const int box = paged ? std::min(1 << rows.pages.shift, 128) : 128;
-  if (!head_map(&q, rows.q, rows.seq.rows, rows.heads, rows.width, 128) || !head_map(&k, rows.k, key_rows, rows.kv_heads, rows.width, box) ||
+  if (!head_map(&q, rows.q, rows.seq.rows, rows.heads, rows.width, 128 >> a.pack_shift, 1 << a.pack_shift) || !head_map(&k, rows.k, key_rows, rows.kv_heads, rows.width, box) ||
       !head_map(&v, rows.v, key_rows, rows.kv_heads, rows.width, box)) {
     set_error("%s: cannot encode the TMA descriptors (no CUDA driver?)", who);
     return DRAGON_ERR_CUDA;

@@ -132,13 +132,13 @@ __device__ __forceinline__ int row_of_none(const Sequences& q, int i) {
 
 // ---- host ----------------------------------------------------------------------------------
 
-// bf16 [rows, heads * width] as (element of a head, head, row), boxes of 64 elements of one head x box_rows rows
-bool head_map(CUtensorMap* map, const void* ptr, int64_t rows, int heads, int width, int box_rows) {
+// bf16 [rows, heads * width] as (element of a head, head, row), boxes of 64 elements x box_heads heads x box_rows rows
+bool head_map(CUtensorMap* map, const void* ptr, int64_t rows, int heads, int width, int box_rows, int box_heads = 1) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)heads, (cuuint64_t)rows};
   cuuint64_t strides[2] = {(cuuint64_t)width * 2, (cuuint64_t)width * heads * 2};
-  cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
+  cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -1335,11 +1335,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       st.colpart_off = take((size_t)st.n_colpart * (size_t)st.num[hn::WIDTH] * sizeof(float));
     }
     if (st.kind == ST_ATTN_BWD) st.scratch_off = take(attention_bwd_scratch_bytes(mems[st.rd[at::Q]].shape.d[0], (int64_t)st.num[an::HEADS]));
-    if (st.kind == ST_PAGED) {
-      const Shape& sh = mems[st.rd[pa::Q]].shape;
-      st.scratch_off = take(paged_scratch_bytes(sh.d[0], mems[st.rd[pa::PAGES]].shape.d[0], (int64_t)st.num[pn::HEADS], (int64_t)st.num[pn::KV_HEADS],
-                                                sh.d[1] / (int64_t)st.num[pn::HEADS], sm_count));
-    }
+    if (st.kind == ST_PAGED) st.scratch_off = take(paged_scratch_bytes(st, mems, sm_count));
     if (st.kind == ST_GNORM || st.kind == ST_NORM_CLIP) st.scratch_off = take(global_norm_scratch_bytes((int)st.rd.size(), sm_count));
     if (st.kind == ST_SCAN || st.kind == ST_SCAN_BWD) {
       const Shape& sh = mems[st.rd[sc::GATE]].shape;

@@ -181,8 +181,8 @@ constexpr int kMaxHeadWidth = 128, kMaxRotatedWidth = 256;
 int head_bwd_partials(int64_t rows, int64_t heads, int sm_count);   // rows of partial gain gradients that HeadNorm's gradient leaves
 size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads);
 int attention_bwd_launches(const Step& s);
-int paged_launches(const Step& s, const std::vector<MemRef>& mems);
-size_t paged_scratch_bytes(int64_t rows, int64_t sequences, int64_t heads, int64_t kv_heads, int64_t width, int sm_count);
+int paged_launches(const Step& s, const std::vector<MemRef>& mems, int sm_count);
+size_t paged_scratch_bytes(const Step& s, const std::vector<MemRef>& mems, int sm_count);
 constexpr int kCachesPerLaunch = 8;
 constexpr int kTensorsPerLaunch = 256;   // tensors that one launch of GlobalNorm or ClipByNorm takes in its parameters
 inline int launches_of_tensors(int n) { return (n + kTensorsPerLaunch - 1) / kTensorsPerLaunch; }
