@@ -622,7 +622,11 @@ int dragon_function_num_launches(const dragon_function_t* f) {
     else if (st.kind == ST_NORM_BWD) n += 1 + (st.wr[nb::DGAIN] >= 0 ? 1 : 0);
     else if (st.kind == ST_GNORM) n += launches_of_tensors((int)st.rd.size());
     else if (st.kind == ST_CLIP) n += launches_of_tensors((int)st.wr.size());
-    else if (st.kind == ST_HEAD_BWD) n += 1 + (st.wr[hb::DGAIN] >= 0 ? 1 : 0);
+    else if (st.kind == ST_HEAD_BWD) {
+      bool sums = false;
+      for (size_t k = hb::DGAIN; k < st.wr.size(); k += hb::WRITES) sums |= st.wr[k] >= 0;
+      n += 1 + sums;
+    }
     else if (st.kind == ST_ATTN_BWD) n += attention_bwd_launches(st);
     else if (st.kind == ST_PAGED) n += paged_launches(st, f->plan.mems, f->plan.sm_count);
     else if (st.kind != ST_COPY) n += 1 + (st.mF >= 0 ? 1 : 0);

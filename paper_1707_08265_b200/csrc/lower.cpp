@@ -694,6 +694,24 @@ bool join_domain(Shape* dom, bool* has_dom, const Shape& s) {
 
 }  // namespace
 
+// Turns per position of every rotated pair as 64-bit fractions: position times fraction, modulo 2^64, is exact
+static std::vector<uint64_t> rotation_table(const std::vector<double>& n) {
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  const int dims = (int)n[hn::DIMS];
+  std::vector<uint64_t> table;
+  for (int i = 0; i < dims / 2; ++i) {
+    const long double f = std::pow((long double)n[hn::BASE], -2.0L * i / dims);
+    long double keep = 0.0L;
+    if (n[hn::ORIGINAL] > 0.0) {
+      const long double turns = n[hn::ORIGINAL] * f / two_pi;
+      keep = n[hn::HIGH] > n[hn::LOW] ? (turns - n[hn::LOW]) / (n[hn::HIGH] - n[hn::LOW]) : turns >= n[hn::LOW] ? 1.0L : 0.0L;
+      keep = std::min(1.0L, std::max(0.0L, keep));
+    }
+    table.push_back((uint64_t)(f * (keep + (1.0L - keep) / (long double)n[hn::FACTOR]) / two_pi * 18446744073709551616.0L));
+  }
+  return table;
+}
+
 static size_t share_workspace(Plan* plan, size_t off);
 static bool reads_follow_writes(const Plan& plan);
 static void find_in_place_caches(Plan* plan);
@@ -1265,6 +1283,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
         }
       }
     }
+    if (st.kind == ST_HEAD || st.kind == ST_HEAD_BWD) { st.head_eps = {(float)it.num[hn::EPS]}; st.head_round = {it.round_dtype}; }
     plan->steps.push_back(st);
   }
   // A norm and the clipping of exactly its tensors that fit the GPU's registers run as one launch: every tensor is read once
@@ -1282,6 +1301,24 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     nst.wr.insert(nst.wr.end(), cst.wr.begin(), cst.wr.end());
     plan->steps.erase(plan->steps.begin() + i + 1);
     // (steps of VM segments name their segment, so nothing else refers to a step's position)
+  }
+  // Neighbouring norms and rotations of the same rows by the same positions (queries and keys) are one launch
+  for (size_t i = 0; i + 1 < plan->steps.size();) {
+    Step &a = plan->steps[i], &b = plan->steps[i + 1];
+    const bool back = a.kind == ST_HEAD_BWD;
+    bool join = a.kind == b.kind && (back || a.kind == ST_HEAD) && a.head_eps.size() < kHeadsPerLaunch;
+    if (join) {
+      const int pos = back ? (int)hb::POS : (int)hd::POS, x = back ? (int)hb::DY : (int)hd::X, y = hd::Y;
+      join = a.rd[pos] == b.rd[pos] && std::equal(a.num.begin() + hn::WIDTH, a.num.end(), b.num.begin() + hn::WIDTH) &&
+             mems[a.rd[x]].shape.d[0] == mems[b.rd[x]].shape.d[0] && (back || (a.wr[y] < 0) == (b.wr[y] < 0));
+      for (int m : b.rd) join &= m < 0 || !std::count(a.wr.begin(), a.wr.end(), m);
+    }
+    if (!join) { ++i; continue; }
+    a.rd.insert(a.rd.end(), b.rd.begin(), b.rd.end());
+    a.wr.insert(a.wr.end(), b.wr.begin(), b.wr.end());
+    a.head_eps.push_back(b.head_eps[0]);
+    a.head_round.push_back(b.head_round[0]);
+    plan->steps.erase(plan->steps.begin() + i + 1);
   }
   // Neighbouring writes by one table (keys and values) are one launch
   for (size_t i = 0; i + 1 < plan->steps.size();) {
@@ -1329,10 +1366,11 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       st.n_colpart = norm_bwd_partials(sh.rows(), sh.cols(), sm_count);
       st.colpart_off = take((size_t)st.n_colpart * sh.cols() * sizeof(float));
     }
-    if (st.kind == ST_HEAD_BWD && st.wr[hb::DGAIN] >= 0) {
-      const Shape& sh = mems[st.rd[hb::X]].shape;
-      st.n_colpart = head_bwd_partials(sh.d[0], sh.d[1] / (int64_t)st.num[hn::WIDTH], sm_count);
-      st.colpart_off = take((size_t)st.n_colpart * (size_t)st.num[hn::WIDTH] * sizeof(float));
+    if ((st.kind == ST_HEAD || st.kind == ST_HEAD_BWD) && st.rd[hd::POS] >= 0) st.freq = rotation_table(st.num);
+    if (st.kind == ST_HEAD_BWD) {
+      const Shape& sh = mems[st.rd[hb::DY]].shape;
+      st.n_colpart = head_bwd_partials(sh.d[0], sm_count);
+      st.colpart_off = take(st.head_eps.size() * st.n_colpart * (size_t)st.num[hn::WIDTH] * sizeof(float));
     }
     if (st.kind == ST_ATTN_BWD) st.scratch_off = take(attention_bwd_scratch_bytes(mems[st.rd[at::Q]].shape.d[0], (int64_t)st.num[an::HEADS]));
     if (st.kind == ST_PAGED) st.scratch_off = take(paged_scratch_bytes(st, mems, sm_count));
@@ -1593,10 +1631,11 @@ std::string describe_plan(const Plan& p) {
       case ST_HEAD: case ST_HEAD_BWD: {
         const bool back = st.kind == ST_HEAD_BWD, norm = st.rd[hd::GAIN] >= 0, rot = st.rd[hd::POS] >= 0;
         const Shape& sh = p.mems[st.rd[back ? (int)hb::DY : (int)hd::X]].shape;
-        snprintf(buf, sizeof(buf), "%s%s%s%s[%lldx%lld, heads of %d%s%s%s]\n", norm ? "head_norm" : "", norm && rot ? "+" : "", rot ? "rotate" : "", back ? "_bwd" : "",
+        const std::string more = st.head_eps.size() > 1 ? ", " + std::to_string(st.head_eps.size()) + " tensors" : "";
+        snprintf(buf, sizeof(buf), "%s%s%s%s[%lldx%lld, heads of %d%s%s%s%s]\n", norm ? "head_norm" : "", norm && rot ? "+" : "", rot ? "rotate" : "", back ? "_bwd" : "",
                  (long long)sh.d[0], (long long)sh.d[1], (int)st.num[hn::WIDTH],
                  rot ? (st.num[hn::INTERLEAVED] != 0.0 ? " interleaved" : " halves") : "", !back && rot && st.wr[hd::U] >= 0 ? " ->normed" : "",
-                 back && st.wr[hb::DGAIN] >= 0 ? " ->dg" : "");
+                 back && st.wr[hb::DGAIN] >= 0 ? " ->dg" : "", more.c_str());
         break;
       }
       case ST_ATTN: case ST_ATTN_BWD:

@@ -300,34 +300,69 @@ template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps) 
     if (row_bad[r]) attend_row<true>(a, kvh * group + (first + r) % group, r0 + (first + r) / group, lane);
 }
 
-// The parts of every row put together; rows of no sequence get zeros.  A warp a row and head, 4 elements a lane.
-__global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArgs a, int few, int few_splits, int tile_splits) {
-  const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (i >= (long long)a.seq.rows * a.heads) return;
-  const int row = (int)(i / a.heads), head = (int)(i % a.heads), s = a.seq.of_row(row);
-  int splits = 0;
-  if (s >= 0) {
+// The parts of every row put together; rows of no sequence get zeros.  A row and head for `ways` warps (1 or 8), which share its
+// parts, 4 elements a lane.  by_sequence: only rows of sequences of few rows (the others have no parts).
+__global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArgs a, int few, int few_splits, int tile_splits, int ways, int by_sequence) {
+  __shared__ float sums[8][132];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = warp & (ways - 1), group = a.heads / a.kv_heads;
+  const long long item = ((long long)blockIdx.x * 8 + warp) / ways;
+  int row, head, s, splits = 0;
+  if (by_sequence) {
+    const int slots = a.kv_heads * few, slot = (int)(item % slots), r = slot % few;
+    s = (int)(item / slots);
+    if (s >= a.seq.count) return;
     int r0, r1;
     a.seq.rows_of(s, &r0, &r1);
-    splits = (r1 - r0) * (a.heads / a.kv_heads) <= few ? few_splits : tile_splits;
-    if (splits == 1) return;      // written already
+    if ((r1 - r0) * group > few || r >= (r1 - r0) * group) return;
+    row = r0 + r / group;
+    head = slot / few * group + r % group;
+    splits = few_splits;
+  } else {
+    if (item >= (long long)a.seq.rows * a.heads) return;
+    row = (int)(item / a.heads);
+    head = (int)(item % a.heads);
+    s = a.seq.of_row(row);
+    if (s >= 0) {
+      int r0, r1;
+      a.seq.rows_of(s, &r0, &r1);
+      splits = (r1 - r0) * group <= few ? few_splits : tile_splits;
+      if (splits == 1) return;      // written already
+    }
   }
-  const size_t stride = (size_t)a.seq.rows * a.heads;
+  const size_t i = (size_t)row * a.heads + head, stride = (size_t)a.seq.rows * a.heads;
   float most = -kInf;
   for (int p = lane; p < splits; p += 32) most = fmaxf(most, a.part_lse[p * stride + i]);
 #pragma unroll
   for (int k = 16; k; k >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, k));
   const float shift = most == -kInf ? 0.f : most;
   float total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < splits; ++p) {
-    const float l = a.part_lse[p * stride + i];
-    if (l == -kInf) continue;      // no keys: nothing was written
-    const float w = exp2f(l - shift);
-    total += w;
-    if (4 * lane < a.width) {
-      const float4 x = *reinterpret_cast<const float4*>(a.part + (p * stride + i) * a.width + 4 * lane);
-      v[0] += w * x.x; v[1] += w * x.y; v[2] += w * x.z; v[3] += w * x.w;
+  for (int p0 = way; p0 < splits; p0 += 4 * ways) {
+    float w[4];
+    float4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int p = p0 + k * ways;
+      const float l = p < splits ? a.part_lse[p * stride + i] : -kInf;
+      w[k] = exp2f(l - shift);
+      x[k] = make_float4(0.f, 0.f, 0.f, 0.f);      // (no keys: nothing was written)
+      if (l != -kInf && 4 * lane < a.width) x[k] = *reinterpret_cast<const float4*>(a.part + (p * stride + i) * a.width + 4 * lane);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      total += w[k];
+      v[0] += w[k] * x[k].x; v[1] += w[k] * x[k].y; v[2] += w[k] * x[k].z; v[3] += w[k] * x[k].w;
+    }
+  }
+  if (ways > 1) {      // (the CTA has one row and head: it came here as a whole)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[warp][4 * lane + e] = v[e];
+    if (lane == 0) sums[warp][128] = total;
+    __syncthreads();
+    if (warp) return;
+    for (int w = 1; w < 8; ++w) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += sums[w][4 * lane + e];
+      total += sums[w][128];
     }
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
@@ -479,8 +514,10 @@ int launch_paged_attention(const StepRun& r) {
     rc = launch_attention_forward(a, true, r.mems[r.s.rd[pa::K]].shape.d[0], p.most_few, st, "PagedAttention");
   }
   if (rc == DRAGON_OK && p.join) {
-    const long long warps = (long long)a.seq.rows * a.heads;
-    paged_join<<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(a, p.most_few, p.few_splits, p.tile_splits);
+    const bool by_sequence = a.seq.starts && p.tiles && p.tile_splits == 1;
+    const int ways = std::max(p.few_splits, p.tile_splits) > 8 ? 8 : 1;
+    const long long items = by_sequence ? (long long)a.seq.count * a.kv_heads * p.most_few : (long long)a.seq.rows * a.heads;
+    paged_join<<<(unsigned)((items * ways + 7) / 8), 256, 0, st>>>(a, p.most_few, p.few_splits, p.tile_splits, ways, by_sequence);
     rc = launched("PagedAttention");
   }
   return rc;

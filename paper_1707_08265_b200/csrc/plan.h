@@ -86,8 +86,8 @@ namespace cl { enum { NORM, FIRST }; }                                          
 namespace sc { enum { GATE, X, H0, RESET, DH, CARRY_IN }; enum { H, CARRY }; enum { DGATE, DX, DH0 }; }   // IT_SCAN, IT_SCAN_BWD
 // IT_HEAD: u = the norm of every head of x (gain absent: u = x), y = u rotated (positions absent: no rotation).  IT_HEAD_BWD: dy is y's
 // gradient (positions present) or u's.  Numbers: hn below.
-namespace hd { enum { X, GAIN, POS }; enum { U, Y }; }
-namespace hb { enum { X, GAIN, POS, DY }; enum { DX, DGAIN }; }
+namespace hd { enum { X, GAIN, POS, READS }; enum { U, Y, WRITES }; }      // (a step may hold several: READS operands and WRITES results each)
+namespace hb { enum { X, GAIN, POS, DY, READS }; enum { DX, DGAIN, WRITES }; }
 namespace hn { enum { EPS, WIDTH, DIMS, INTERLEAVED, BASE, FACTOR, LOW, HIGH, ORIGINAL, AMPLITUDE, COUNT }; }
 // IT_ATTN, IT_ATTN_BWD: lse [heads, T] is log2 of every row's sum of exponentials (scaled), +inf for a row that sees nothing
 namespace at { enum { Q, K, V, STARTS, Y_IN, LSE_IN, DY }; enum { Y, LSE }; enum { DQ, DK, DV }; }
@@ -166,6 +166,9 @@ struct Step {
   std::vector<int> rd, wr;               // kinds from ST_NORM on: as in Item
   double attr = 0.0;
   std::vector<double> num;
+  std::vector<float> head_eps;           // ST_HEAD, ST_HEAD_BWD: of every tensor the step holds,
+  std::vector<int> head_round;           // and the type that its normed heads are rounded to before they are rotated
+  std::vector<uint64_t> freq;            // ST_HEAD, ST_HEAD_BWD: turns per position of every rotated pair, times 2^64
   int sum_dtype = DRAGON_F32, round_dtype = DRAGON_F32;
 };
 
@@ -178,12 +181,12 @@ bool norm_and_clip_fit_one_launch(const std::vector<int64_t>& numel, const std::
 size_t scan_scratch_bytes(int64_t rows, int64_t cols);
 constexpr int64_t kMaxAttentionRows = 1 << 30;   // rows of an attention operator's tensors: 32-bit row numbers with room for a tile
 constexpr int kMaxHeadWidth = 128, kMaxRotatedWidth = 256;
-int head_bwd_partials(int64_t rows, int64_t heads, int sm_count);   // rows of partial gain gradients that HeadNorm's gradient leaves
+int head_bwd_partials(int64_t rows, int sm_count);   // rows of partial gain gradients that HeadNorm's gradient leaves
 size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads);
 int attention_bwd_launches(const Step& s);
 int paged_launches(const Step& s, const std::vector<MemRef>& mems, int sm_count);
 size_t paged_scratch_bytes(const Step& s, const std::vector<MemRef>& mems, int sm_count);
-constexpr int kCachesPerLaunch = 8;
+constexpr int kCachesPerLaunch = 8, kHeadsPerLaunch = 4;
 constexpr int kTensorsPerLaunch = 256;   // tensors that one launch of GlobalNorm or ClipByNorm takes in its parameters
 inline int launches_of_tensors(int n) { return (n + kTensorsPerLaunch - 1) / kTensorsPerLaunch; }
 
