@@ -158,15 +158,8 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     if (lane == 0) {
       const int k_steps = (a.r.width + 15) / 16;
       const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_acc = idesc_bf16(128, 16 * k_steps, true);
-      auto product = [&](uint32_t d, uint32_t x, uint32_t y) {      // X Y^T over the head
-        for (int k = 0; k < k_steps; ++k) {
-          const uint32_t off = (k >> 2) * kChunkBytes + (k & 3) * 32;
-          umma_ss(tmem + d, desc_k(x + off), desc_k(y + off), idesc_s, k > 0);
-        }
-      };
-      auto accumulate = [&](uint32_t d, uint32_t p, uint32_t y, bool more) {      // P Y over the tile's rows; P's halves are 64 columns apart
-        for (int k = 0; k < 8; ++k) umma_ts(tmem + d, tmem + p + 64 * (k >> 2) + 8 * (k & 3), desc_mn(y + k * 2048), idesc_acc, more || k > 0);
-      };
+      auto product = [&](uint32_t d, uint32_t x, uint32_t y) { product_over_head<kChunks>(tmem + d, x, y, k_steps, idesc_s); };
+      auto accumulate = [&](uint32_t d, uint32_t p, uint32_t y, bool more) { product_over_rows<64>(tmem + d, tmem + p, y, idesc_acc, more); };
       auto dp_at = [&](int i) { return kDp + (kKeys ? 0 : 128 * (i & 1)); };
       auto issue_s = [&](int i) {
         if (!wait(y1_full + 8 * (i % kSt), (i / kSt) & 1)) return false;

@@ -180,11 +180,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       const int k_steps = (a.r.width + 15) / 16, n_out = 16 * k_steps;
       const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_o = idesc_bf16(128, n_out, true);
       auto product_s = [&](int t, int j) {
-        const uint32_t kt = k_at + (j % kSt) * kTile, qt = q_at + t * kTile;
-        for (int k = 0; k < k_steps; ++k) {
-          const uint32_t off = (k >> 2) * kChunkBytes + (k & 3) * 32;
-          umma_ss(tmem + 128 * t, desc_k(qt + off), desc_k(kt + off), idesc_s, k > 0);
-        }
+        product_over_head<kChunks>(tmem + 128 * t, q_at + t * kTile, k_at + (j % kSt) * kTile, k_steps, idesc_s);
         umma_commit(s_full + 8 * t);
       };
       bool ok = wait(k_full, 0);
@@ -201,8 +197,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         for (int t = 0; t < 2 && ok; ++t) {
           if (!(ok = wait(p_full + 8 * t, j & 1))) break;
           fence_after();
-          for (int k = 0; k < 8; ++k)
-            umma_ts(tmem + 256 + 128 * t, tmem + 128 * t + 8 * k, desc_mn(v_at + s * kTile + k * 2048), idesc_o, j > 0 || k > 0);
+          product_over_rows<32>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, j > 0);
           if (j + 1 < n_tiles) {
             if (t == 0) { if (!(ok = wait(k_full + 8 * ((j + 1) % kSt), ((j + 1) / kSt) & 1))) break; fence_after(); }
             product_s(t, j + 1);

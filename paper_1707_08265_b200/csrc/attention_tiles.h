@@ -78,6 +78,23 @@ __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a_tmem, uint64_t b_
       ::"r"(d), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"((uint32_t)accumulate) : "memory");
 }
 
+// X Y^T over the head's elements, `steps` times 16 of them.  The descriptors of a step differ from the tile's by constants: what the
+// one issuing thread computes between two products is as little as can be (an address computed for each took longer than the product)
+template <int kChunks> __device__ __forceinline__ void product_over_head(uint32_t d, uint32_t x, uint32_t y, int steps, uint32_t idesc) {
+  const uint64_t dx = desc_k(x), dy = desc_k(y);
+#pragma unroll
+  for (int k = 0; k < 4 * kChunks; ++k) {
+    const uint64_t off = (k >> 2) * (kChunkBytes >> 4) + (k & 3) * 2;
+    if (k < steps) umma_ss(d, dx + off, dy + off, idesc, k > 0);
+  }
+}
+// P Y over the 128 rows of the tile Y, P out of TMEM: 16 rows' columns after one another, the second 64 rows' `half` columns on
+template <int kHalf> __device__ __forceinline__ void product_over_rows(uint32_t d, uint32_t p, uint32_t y, uint32_t idesc, bool accumulate) {
+  const uint64_t dy = desc_mn(y);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) umma_ts(d, p + kHalf * (k >> 2) + 8 * (k & 3), dy + 128 * k, idesc, accumulate || k > 0);
+}
+
 // ---- units of work ---------------------------------------------------------------------------
 
 struct Unit {
