@@ -22,8 +22,13 @@ namespace dragon {
 namespace {
 
 constexpr int kBwdThreads = 320;
-constexpr int kBwdStages = 2;
-constexpr size_t bwd_smem(int chunks) { return 1024 + (size_t)(2 + 2 * kBwdStages) * chunks * kChunkBytes + kBwdStages * 1024 + 512; }
+// Stages of the first operand (q, or k), which is held until the end of a round, and of the second (dy, or v).  rows: with two
+// stages of k its next tile came too late (a round 2970 cycles)
+constexpr int bwd_stages1(bool keys, int chunks) { return chunks == 1 ? 4 : keys ? 2 : 3; }
+constexpr int bwd_stages2(int chunks) { return chunks == 1 ? 4 : 2; }
+constexpr size_t bwd_smem(bool keys, int chunks) {
+  return 1024 + (size_t)(2 + bwd_stages1(keys, chunks) + bwd_stages2(chunks)) * chunks * kChunkBytes + (keys ? bwd_stages1(keys, chunks) * 1024 : 0) + 512;
+}
 
 struct BwdArgs {
   RowArgs r;
@@ -36,19 +41,19 @@ template <bool kKeys, int kChunks>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
               const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ BwdArgs a) {
-  constexpr int kSt = kBwdStages;
+  constexpr int kSt1 = bwd_stages1(kKeys, kChunks), kSt2 = bwd_stages2(kChunks);
   constexpr uint32_t kTile = kChunks * kChunkBytes;
   // columns of TMEM
   constexpr uint32_t kS = 0, kDp = 128, kAcc1 = kKeys ? 256 : 384, kAcc2 = 384;      // (rows: the second buffer of dP at 256)
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t x1 = base, x2 = x1 + kTile, y1 = x2 + kTile, y2 = y1 + kSt * kTile;      // the CTA's own tiles, and the stages of those it meets
-  float* stats = reinterpret_cast<float*>(smem_raw + (base - raw) + (2 + 2 * kSt) * kTile);      // keys: [stage][lse, delta][128]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(stats + kSt * 256);
-  const uint32_t x_full = smem_u32(bars), y1_full = x_full + 8, y1_empty = y1_full + 8 * kSt, y2_full = y1_empty + 8 * kSt, y2_empty = y2_full + 8 * kSt;
-  const uint32_t st_full = y2_empty + 8 * kSt, st_empty = st_full + 8 * kSt;
-  const uint32_t s_full = st_empty + 8 * kSt, dp_full = s_full + 8, p_full = dp_full + 16, ds_full = p_full + 8, acc_full = ds_full + 8, drain = acc_full + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 6 * kSt + 7);
+  const uint32_t x1 = base, x2 = x1 + kTile, y1 = x2 + kTile, y2 = y1 + kSt1 * kTile;      // the CTA's own tiles, and the stages of those it meets
+  float* stats = reinterpret_cast<float*>(smem_raw + (base - raw) + (2 + kSt1 + kSt2) * kTile);      // keys: [stage][-lse, -delta][128]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(stats + (kKeys ? kSt1 * 256 : 0));
+  const uint32_t x_full = smem_u32(bars), y1_full = x_full + 8, y1_empty = y1_full + 8 * kSt1, y2_full = y1_empty + 8 * kSt1, y2_empty = y2_full + 8 * kSt2;
+  const uint32_t st_full = y2_empty + 8 * kSt2, st_empty = st_full + 8 * kSt1;
+  const uint32_t s_full = st_empty + 8 * kSt1, dp_full = s_full + 8, p_full = dp_full + 16, ds_full = p_full + 8, acc_full = ds_full + 8, drain = acc_full + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 4 * kSt1 + 2 * kSt2 + 7);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   __shared__ Unit unit;
   __shared__ unsigned again[8];
@@ -61,10 +66,8 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_dy) : "memory");
     mbar_init(x_full, 1);
-    for (int s = 0; s < kSt; ++s) {
-      mbar_init(y1_full + 8 * s, 1); mbar_init(y1_empty + 8 * s, 1); mbar_init(y2_full + 8 * s, 1); mbar_init(y2_empty + 8 * s, 1);
-      mbar_init(st_full + 8 * s, 32); mbar_init(st_empty + 8 * s, 8);
-    }
+    for (int s = 0; s < kSt1; ++s) { mbar_init(y1_full + 8 * s, 1); mbar_init(y1_empty + 8 * s, 1); mbar_init(st_full + 8 * s, 32); mbar_init(st_empty + 8 * s, 8); }
+    for (int s = 0; s < kSt2; ++s) { mbar_init(y2_full + 8 * s, 1); mbar_init(y2_empty + 8 * s, 1); }
     mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(dp_full + 8, 1); mbar_init(p_full, 8); mbar_init(ds_full, 8); mbar_init(acc_full, 1); mbar_init(drain, 1);
     abort_flag[0] = abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -125,8 +128,10 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     __syncwarp();
     bool ok = true;
-    for (int i = 0; i < n && ok; ++i) {
-      const int s = i % kSt, turn = i / kSt, h = kKeys ? head * group + i / tiles : head / group, row = u.a + (t0 + i % tiles) * 128;
+    int h = kKeys ? head * group : head / group, tile = 0;
+    for (int i = 0; i < n && ok; ++i, ++tile) {
+      if (tile == tiles) { tile = 0; ++h; }
+      const int s = i % kSt1, turn = i / kSt1, row = u.a + (t0 + tile) * 128;
       ok = __all_sync(0xffffffffu, wait(y1_empty + 8 * s, (turn & 1) ^ 1));
       if (!ok) break;
       issued1 = i + 1;
@@ -134,24 +139,25 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         mbar_expect_tx(y1_full + 8 * s, kTile);
         for (int c = 0; c < kChunks; ++c) tma_load_3d(y1 + s * kTile + c * kChunkBytes, kKeys ? &tm_q : &tm_k, 64 * c, h, row, y1_full + 8 * s);
       }
-      if (kKeys) {      // lse and delta of the tile's rows; a row behind the sequence's last has probabilities 0
+      if (kKeys) {      // -lse and -delta of the tile's rows; a row behind the sequence's last has probabilities 0
         ok = __all_sync(0xffffffffu, wait(st_empty + 8 * s, (turn & 1) ^ 1));
         if (!ok) break;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int r = (t0 + i % tiles) * 128 + 32 * k + lane;
+          const int r = (t0 + tile) * 128 + 32 * k + lane;
           const size_t at = (size_t)h * a.r.seq.rows + u.a + r;
-          stats[s * 256 + 32 * k + lane] = r < n_rows ? __ldg(a.r.lse + at) : kInf;
-          stats[s * 256 + 128 + 32 * k + lane] = r < n_rows ? __ldg(a.r.delta + at) : 0.f;
+          stats[s * 256 + 32 * k + lane] = r < n_rows ? -__ldg(a.r.lse + at) : -kInf;
+          stats[s * 256 + 128 + 32 * k + lane] = r < n_rows ? -__ldg(a.r.delta + at) : 0.f;
         }
         mbar_arrive(st_full + 8 * s);
       }
-      ok = __all_sync(0xffffffffu, wait(y2_empty + 8 * s, (turn & 1) ^ 1));
+      const int s2 = i % kSt2;
+      ok = __all_sync(0xffffffffu, wait(y2_empty + 8 * s2, ((i / kSt2) & 1) ^ 1));
       if (!ok) break;
       issued2 = i + 1;
       if (lane == 0) {
-        mbar_expect_tx(y2_full + 8 * s, kTile);
-        for (int c = 0; c < kChunks; ++c) tma_load_3d(y2 + s * kTile + c * kChunkBytes, kKeys ? &tm_dy : &tm_v, 64 * c, h, row, y2_full + 8 * s);
+        mbar_expect_tx(y2_full + 8 * s2, kTile);
+        for (int c = 0; c < kChunks; ++c) tma_load_3d(y2 + s2 * kTile + c * kChunkBytes, kKeys ? &tm_dy : &tm_v, 64 * c, h, row, y2_full + 8 * s2);
       }
     }
   } else if (warp == 9) {
@@ -162,28 +168,28 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       auto accumulate = [&](uint32_t d, uint32_t p, uint32_t y, bool more) { product_over_rows<64>(tmem + d, tmem + p, y, idesc_acc, more); };
       auto dp_at = [&](int i) { return kDp + (kKeys ? 0 : 128 * (i & 1)); };
       auto issue_s = [&](int i) {
-        if (!wait(y1_full + 8 * (i % kSt), (i / kSt) & 1)) return false;
+        if (!wait(y1_full + 8 * (i % kSt1), (i / kSt1) & 1)) return false;
         fence_after();
-        product(kS, x1, y1 + (i % kSt) * kTile);
+        product(kS, x1, y1 + (i % kSt1) * kTile);
         umma_commit(s_full);
         return true;
       };
       auto issue_dp = [&](int i) {
-        if (!wait(y2_full + 8 * (i % kSt), (i / kSt) & 1)) return false;
+        if (!wait(y2_full + 8 * (i % kSt2), (i / kSt2) & 1)) return false;
         fence_after();
-        product(dp_at(i), x2, y2 + (i % kSt) * kTile);
+        product(dp_at(i), x2, y2 + (i % kSt2) * kTile);
         umma_commit(dp_full + (kKeys ? 0 : 8 * (i & 1)));
-        if (!kKeys) umma_commit(y2_empty + 8 * (i % kSt));
+        if (!kKeys) umma_commit(y2_empty + 8 * (i % kSt2));
         return true;
       };
       bool ok = wait(x_full, 0) && issue_s(0) && issue_dp(0);
       for (int i = 0; i < n && ok; ++i) {
-        const int s = i % kSt;
+        const int s = i % kSt1, s2 = i % kSt2;
         if (kKeys) {
           if (!(ok = wait(p_full, i & 1))) break;
           fence_after();
-          accumulate(kAcc2, kS, y2 + s * kTile, i > 0);
-          umma_commit(y2_empty + 8 * s);
+          accumulate(kAcc2, kS, y2 + s2 * kTile, i > 0);
+          umma_commit(y2_empty + 8 * s2);
           if (i + 1 < n && !(ok = issue_s(i + 1))) break;
           if (!(ok = wait(ds_full, i & 1))) break;
           fence_after();
@@ -215,9 +221,11 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       lse = a.r.lse[(size_t)head * a.r.seq.rows + u.a + row];
       delta = a.r.delta[(size_t)head * a.r.seq.rows + u.a + row];
     }
+    const Pair factor = pair_of(a.r.scale, a.r.scale);
     bool ok = true;
-    for (int i = 0; i < n; ++i) {
-      const int c0 = (t0 + i % tiles) * 128 + 64 * half;      // the first of this thread's columns
+    for (int i = 0, tile = 0; i < n; ++i, ++tile) {
+      if (tile == tiles) tile = 0;
+      const int c0 = (t0 + tile) * 128 + 64 * half;      // the first of this thread's columns
       // columns [lo, hi) are seen
       int lo, hi;
       if (kKeys) {
@@ -227,9 +235,9 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         hi = (a.r.causal ? min(row + 1, n_rows) : n_rows) - c0;
         lo = a.r.window ? row - a.r.window + 1 - c0 : 0;
       }
-      const float4* st = reinterpret_cast<const float4*>(stats + (i % kSt) * 256 + 64 * half);
+      const float4* st = reinterpret_cast<const float4*>(stats + (i % kSt1) * 256 + 64 * half);
       ok = __all_sync(0xffffffffu, wait(s_full, i & 1));
-      if (ok && kKeys) ok = __all_sync(0xffffffffu, wait(st_full + 8 * (i % kSt), (i / kSt) & 1));
+      if (ok && kKeys) ok = __all_sync(0xffffffffu, wait(st_full + 8 * (i % kSt1), (i / kSt1) & 1));
       if (!ok) break;
       fence_after();
       uint32_t v[64];
@@ -244,12 +252,10 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       }
 #pragma unroll
       for (int c = 0; c < 64; c += 4) {
-        float4 l = make_float4(lse, lse, lse, lse);
+        float4 l = make_float4(-lse, -lse, -lse, -lse);
         if (kKeys) l = st[c / 4];
-        p[c] = exp2_fast(fmaf(__uint_as_float(v[c]), a.r.scale, -l.x));
-        p[c + 1] = exp2_fast(fmaf(__uint_as_float(v[c + 1]), a.r.scale, -l.y));
-        p[c + 2] = exp2_fast(fmaf(__uint_as_float(v[c + 2]), a.r.scale, -l.z));
-        p[c + 3] = exp2_fast(fmaf(__uint_as_float(v[c + 3]), a.r.scale, -l.w));
+        const float2 x = both(fma_pair(pair_of(v[c], v[c + 1]), factor, pair_of(l.x, l.y))), y = both(fma_pair(pair_of(v[c + 2], v[c + 3]), factor, pair_of(l.z, l.w)));
+        p[c] = exp2_fast(x.x); p[c + 1] = exp2_fast(x.y); p[c + 2] = exp2_fast(y.x); p[c + 3] = exp2_fast(y.y);
       }
       if (!__all_sync(0xffffffffu, lo <= 0 && hi >= 64)) {
 #pragma unroll
@@ -273,12 +279,12 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       tmem_ld_wait();
 #pragma unroll
       for (int c = 0; c < 64; c += 4) {
-        float4 d = make_float4(delta, delta, delta, delta);
+        float4 d = make_float4(-delta, -delta, -delta, -delta);
         if (kKeys) d = st[32 + c / 4];
-        const float s0 = p[c] * (__uint_as_float(v[c]) - d.x), s1 = p[c + 1] * (__uint_as_float(v[c + 1]) - d.y);
-        const float s2 = p[c + 2] * (__uint_as_float(v[c + 2]) - d.z), s3 = p[c + 3] * (__uint_as_float(v[c + 3]) - d.w);
-        v[c / 2] = bf16_pair(s0, s1);
-        v[c / 2 + 1] = bf16_pair(s2, s3);
+        const float2 x = both(mul_pair(pair_of(p[c], p[c + 1]), add_pair(pair_of(v[c], v[c + 1]), pair_of(d.x, d.y))));
+        const float2 y = both(mul_pair(pair_of(p[c + 2], p[c + 3]), add_pair(pair_of(v[c + 2], v[c + 3]), pair_of(d.z, d.w))));
+        v[c / 2] = bf16_pair(x.x, x.y);
+        v[c / 2 + 1] = bf16_pair(y.x, y.y);
       }
       tmem_st32(dp, v);
       tmem_st_wait();
@@ -286,7 +292,7 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(ds_full);
-        if (kKeys) mbar_arrive(st_empty + 8 * (i % kSt));
+        if (kKeys) mbar_arrive(st_empty + 8 * (i % kSt1));
       }
     }
     if (ok) {
@@ -334,8 +340,8 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   if (*abort_flag) {      // an unwind: what the producer has handed to the TMA engine lands before the shared memory goes away
     if (threadIdx.x == 256) {
       mbar_wait(x_full, 0, abort_flag + 1);
-      for (int k = std::max(a.drop_first_load ? 1 : 0, issued1 - kSt); k < issued1; ++k) mbar_wait(y1_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
-      for (int k = std::max(0, issued2 - kSt); k < issued2; ++k) mbar_wait(y2_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
+      for (int k = std::max(a.drop_first_load ? 1 : 0, issued1 - kSt1); k < issued1; ++k) mbar_wait(y1_full + 8 * (k % kSt1), (k / kSt1) & 1, abort_flag + 1);
+      for (int k = std::max(0, issued2 - kSt2); k < issued2; ++k) mbar_wait(y2_full + 8 * (k % kSt2), (k / kSt2) & 1, abort_flag + 1);
     }
     __syncthreads();
   }
@@ -362,11 +368,11 @@ __global__ void __launch_bounds__(256) attention_delta(const __grid_constant__ R
 template <bool kKeys, int kChunks> int launch_bwd(const BwdArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& dy, cudaStream_t st) {
   static const char* who = "Attention's gradient";
   static bool set[64] = {};
-  const int rc = allow_smem(reinterpret_cast<const void*>(attention_bwd<kKeys, kChunks>), bwd_smem(kChunks), set, who);
+  const int rc = allow_smem(reinterpret_cast<const void*>(attention_bwd<kKeys, kChunks>), bwd_smem(kKeys, kChunks), set, who);
   if (rc != DRAGON_OK) return rc;
   const long long grid = (long long)a.blocks * (kKeys ? a.r.kv_heads : a.r.heads);
   if (grid > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
-  attention_bwd<kKeys, kChunks><<<(unsigned)grid, kBwdThreads, bwd_smem(kChunks), st>>>(q, k, v, dy, a);
+  attention_bwd<kKeys, kChunks><<<(unsigned)grid, kBwdThreads, bwd_smem(kKeys, kChunks), st>>>(q, k, v, dy, a);
   return launched(who);
 }
 

@@ -49,8 +49,8 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const uint32_t q_at = base, k_at = base + 2 * kTile, v_at = k_at + kSt * kTile;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (base - raw) + (2 + 2 * kSt) * kTile);
   const uint32_t q_full = smem_u32(bars), k_full = q_full + 16, k_empty = k_full + 8 * kSt, v_full = k_empty + 8 * kSt, v_empty = v_full + 8 * kSt;
-  const uint32_t s_full = v_empty + 8 * kSt, p_full = s_full + 16, o_full = p_full + 16, v_clean = o_full + 16, drain = v_clean + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 10 + 4 * kSt);
+  const uint32_t s_full = v_empty + 8 * kSt, p_full = s_full + 16, o_full = p_full + 32, v_clean = o_full + 16, drain = v_clean + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 4 * kSt);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   __shared__ Unit unit;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -62,7 +62,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
-    for (int t = 0; t < 2; ++t) { mbar_init(q_full + 8 * t, 1); mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 8 * t, 4); mbar_init(o_full + 8 * t, 1); }
+    for (int t = 0; t < 2; ++t) { mbar_init(q_full + 8 * t, 1); mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 16 * t, 4); mbar_init(p_full + 16 * t + 8, 4); mbar_init(o_full + 8 * t, 1); }
     for (int s = 0; s < kSt; ++s) { mbar_init(k_full + 8 * s, 1); mbar_init(k_empty + 8 * s, 1); mbar_init(v_full + 8 * s, 1); mbar_init(v_empty + 8 * s, 1); }
     mbar_init(v_clean, 32);
     mbar_init(drain, 1);
@@ -195,9 +195,12 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         ok = wait(v_full + 8 * s, (j / kSt) & 1);
         if (ok && ragged && j == n_tiles - 1) ok = wait(v_clean, 0);
         for (int t = 0; t < 2 && ok; ++t) {
-          if (!(ok = wait(p_full + 8 * t, j & 1))) break;
+          if (!(ok = wait(p_full + 16 * t, j & 1))) break;
           fence_after();
-          product_over_rows<32>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, j > 0);
+          product_over_rows<32, 0, 4>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, j > 0);
+          if (!(ok = wait(p_full + 16 * t + 8, j & 1))) break;
+          fence_after();
+          product_over_rows<32, 4, 8>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, true);
           if (j + 1 < n_tiles) {
             if (t == 0) { if (!(ok = wait(k_full + 8 * ((j + 1) % kSt), ((j + 1) / kSt) & 1))) break; fence_after(); }
             product_s(t, j + 1);
@@ -241,12 +244,14 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
 #pragma unroll
       for (int c = 0; c < 4; ++c) m[c] = __uint_as_float(s[c]);
 #pragma unroll
-      for (int c = 4; c < 128; ++c) m[c & 3] = fmaxf(m[c & 3], __uint_as_float(s[c]));
-      const float most = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+      for (int c = 4; c < 124; c += 2) m[(c >> 1) & 3] = most_of(m[(c >> 1) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+      m[0] = most_of(m[0], __uint_as_float(s[124]), __uint_as_float(s[125]));
+      m[1] = most_of(m[1], __uint_as_float(s[126]), __uint_as_float(s[127]));
+      const float most = most_of(most_of(m[0], m[1], m[2]), m[3], m[3]);      // (a NaN among the scores makes everything of the row NaN)
       if (j == 0) {
         top = most;
       } else {
-        const bool grown = (most - top) * a.r.scale > kRescale;      // (from -inf on: infinite)
+        const bool grown = !((most - top) * a.r.scale <= kRescale) && most != -kInf;      // (from -inf on: infinite; NaN)
         if (__any_sync(0xffffffffu, grown)) {
           const float f = grown ? exp2_fast((top - most) * a.r.scale) : 1.f;
           if (grown) top = most;
@@ -263,25 +268,26 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         }
       }
       const float shift = top == -kInf ? 0.f : top * a.r.scale;
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
+      const Pair factor = pair_of(a.r.scale, a.r.scale), less = pair_of(-shift, -shift);
+      Pair part[2] = {0, 0};
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < 2; ++c) {      // the products of the first 64 keys start while the others are worked on
         uint32_t p[32];
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
-          const float x = exp2_fast(fmaf(__uint_as_float(s[64 * c + 2 * k]), a.r.scale, -shift));
-          const float y = exp2_fast(fmaf(__uint_as_float(s[64 * c + 2 * k + 1]), a.r.scale, -shift));
-          part[(2 * k) & 3] += x;
-          part[(2 * k + 1) & 3] += y;
-          p[k] = bf16_pair(x, y);
+          const float2 x = both(fma_pair(pair_of(s[64 * c + 2 * k], s[64 * c + 2 * k + 1]), factor, less));
+          const float x0 = exp2_fast(x.x), x1 = exp2_fast(x.y);
+          part[k & 1] = add_pair(part[k & 1], pair_of(x0, x1));
+          p[k] = bf16_pair(x0, x1);
         }
         tmem_st32(s_at + 32 * c, p);
+        tmem_st_wait();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * c);
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
-      tmem_st_wait();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_full + 8 * t);
+      const float2 more = both(add_pair(part[0], part[1]));
+      sum += more.x + more.y;
     }
     if (ok && n_tiles > 0) {
       ok = __all_sync(0xffffffffu, wait(o_full + 8 * t, 0));

@@ -52,6 +52,17 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
 // 2^x, results below 2^-126 as 0
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+// two fp32 values in one 64-bit register, and arithmetic on both at once
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair_of(float lo, float hi) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi)); return p; }
+__device__ __forceinline__ Pair pair_of(uint32_t lo, uint32_t hi) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi)); return p; }
+__device__ __forceinline__ float2 both(Pair p) { float2 v; asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p)); return v; }
+__device__ __forceinline__ Pair fma_pair(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ Pair add_pair(Pair a, Pair b) { Pair d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ Pair mul_pair(Pair a, Pair b) { Pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+// the largest of three, NaN if one of them is
+__device__ __forceinline__ float most_of(float a, float b, float c) { float d; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
+
 // rows of a tile along M or N, the head's elements along K: 16 of them are 32 bytes on
 __device__ __forceinline__ uint64_t desc_k(uint32_t addr) { return make_smem_desc(addr); }
 // the head's elements along N, rows of the tile along K: 16 rows are 2048 bytes on, the next 64 elements a chunk
@@ -89,10 +100,10 @@ template <int kChunks> __device__ __forceinline__ void product_over_head(uint32_
   }
 }
 // P Y over the 128 rows of the tile Y, P out of TMEM: 16 rows' columns after one another, the second 64 rows' `half` columns on
-template <int kHalf> __device__ __forceinline__ void product_over_rows(uint32_t d, uint32_t p, uint32_t y, uint32_t idesc, bool accumulate) {
+template <int kHalf, int kFirst = 0, int kLast = 8> __device__ __forceinline__ void product_over_rows(uint32_t d, uint32_t p, uint32_t y, uint32_t idesc, bool accumulate) {
   const uint64_t dy = desc_mn(y);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) umma_ts(d, p + kHalf * (k >> 2) + 8 * (k & 3), dy + 128 * k, idesc, accumulate || k > 0);
+  for (int k = kFirst; k < kLast; ++k) umma_ts(d, p + kHalf * (k >> 2) + 8 * (k & 3), dy + 128 * k, idesc, accumulate || k > 0);
 }
 
 // ---- units of work ---------------------------------------------------------------------------
