@@ -8,9 +8,10 @@
 // (no rounding grows with the position); its top 32 bits go through sincospi in fp32.  They are the same for every head of a
 // row: a CTA computes those of its rows once, into shared memory.
 //
-// Bound: HBM (every element is read and written once).  A warp works on one row at a time: 8 elements a lane, a head in the next
-// power of two of lanes, so that the head's sums are a few shuffles; the lane's angles stay in registers while the warp walks the
-// row's heads.  Tensors of the same rows (queries and keys) are one launch.
+// Bound: HBM (every element is read and written once), and next to it instructions.  A warp works on one row at a time: 8 elements a
+// lane, a head in the next power of two of lanes, so that the head's sums are a few shuffles.  Where pairs are halves apart a lane
+// has 4 elements and their 4 partners.  Gain and angle are multiplied once a row: y = r (a (g c) - b (g' s)), and stay in registers
+// while the warp walks the row's heads.  Tensors of the same rows (queries and keys) are one launch.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -23,11 +24,12 @@
 namespace dragon {
 namespace {
 
+constexpr int kHeadCtas = 2;            // of an SM: persistent, each with its next accesses on the way while it computes
 constexpr int kHeadThreads = 256, kHeadWarps = kHeadThreads / 32;
 constexpr int kHeadRowsMost = kHeadWarps;       // rows of a tile: their angles are computed together
 constexpr int kPairsMost = kMaxRotatedWidth / 2;
 
-enum Pairing { P_NONE, P_NEIGHBOURS, P_LANES, P_ANY };   // where a lane finds the partners of its 8 elements
+enum Pairing { P_NONE, P_NEIGHBOURS, P_HALVES, P_ANY };   // where a lane finds the partners of its 8 elements: nowhere, next to them, in its own other half, anywhere
 
 struct HeadJob {
   const void *x, *gain, *dy;
@@ -64,71 +66,93 @@ __device__ __forceinline__ void fill_angles(const HeadArgs& a, float2 (*cs)[kPla
   }
 }
 
-// the angles of this lane's elements, from e0 of the head on: of its 4 pairs, or of the pairs that its 8 elements belong to.  An
-// element behind dims gets (1, 0); the second of a pair gets minus its sine, so that x' = x c - partner s for both
-template <int kPairing> __device__ __forceinline__ void load_angles(const float2* cs, int e0, int dims, float2* t) {
-  const int half = dims >> 1;
-  if (kPairing == P_NEIGHBOURS) {
-#pragma unroll
-    for (int p = 0; p < 4; ++p) t[p] = (e0 >> 1) + p < half ? cs[place_of((e0 >> 1) + p)] : make_float2(1.f, 0.f);
-  } else if (kPairing != P_NONE) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int at = e0 + e;
-      t[e] = at < dims ? cs[place_of(at < half ? at : at - half)] : make_float2(1.f, 0.f);
-      if (at >= half) t[e].y = -t[e].y;
-    }
+// 4 consecutive elements (of a multiple of 4), as they are in memory
+template <int DT> struct Four;
+template <> struct Four<DRAGON_BF16> {
+  uint2 u;
+  __device__ __forceinline__ void load(const void* p, int, size_t i) { u = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const unsigned short*>(p) + i)); }
+  __device__ __forceinline__ void get(float* v) const { v[0] = bf16_low(u.x); v[1] = bf16_high(u.x); v[2] = bf16_low(u.y); v[3] = bf16_high(u.y); }
+  static __device__ __forceinline__ void store(void* p, int, size_t i, const float* v) {
+    *reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(p) + i) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
   }
-}
+};
+template <> struct Four<DRAGON_F32> {
+  float4 u;
+  __device__ __forceinline__ void load(const void* p, int, size_t i) { u = __ldg(reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + i)); }
+  __device__ __forceinline__ void get(float* v) const { v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; }
+  static __device__ __forceinline__ void store(void* p, int, size_t i, const float* v) { *reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <> struct Four<-1> {
+  float4 u;
+  __device__ __forceinline__ void load(const void* p, int dtype, size_t i) {
+    float v[4];
+    if (dtype == DRAGON_F32) { Four<DRAGON_F32> f; f.load(p, 0, i); f.get(v); }
+    else { Four<DRAGON_BF16> f; f.load(p, 0, i); f.get(v); }
+    u = make_float4(v[0], v[1], v[2], v[3]);
+  }
+  __device__ __forceinline__ void get(float* v) const { v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w; }
+  static __device__ __forceinline__ void store(void* p, int dtype, size_t i, const float* v) {
+    if (dtype == DRAGON_F32) Four<DRAGON_F32>::store(p, 0, i, v);
+    else Four<DRAGON_BF16>::store(p, 0, i, v);
+  }
+};
+// a lane's 8 elements: one access where they are neighbours, two of 4 where they are halves apart
+template <int DT, bool kApart> struct Eight {
+  Raw<DT, 8> r;
+  __device__ __forceinline__ void load(const void* p, int dtype, size_t i, int) { r.load(p, dtype, i); }
+  __device__ __forceinline__ void get(float* v) const { r.get(v); }
+  static __device__ __forceinline__ void store(void* p, int dtype, size_t i, int, const float* v) { Raw<DT, 8> o; o.set(v); o.store(p, dtype, i); }
+};
+template <int DT> struct Eight<DT, true> {
+  Four<DT> a, b;
+  __device__ __forceinline__ void load(const void* p, int dtype, size_t i, int apart) { a.load(p, dtype, i); b.load(p, dtype, i + apart); }
+  __device__ __forceinline__ void get(float* v) const { a.get(v); b.get(v + 4); }
+  static __device__ __forceinline__ void store(void* p, int dtype, size_t i, int apart, const float* v) { Four<DT>::store(p, dtype, i, v); Four<DT>::store(p, dtype, i + apart, v + 4); }
+};
 
-// v: this lane's 8 elements; back: by the negative angle.  buf: 256 floats of this warp (P_ANY)
-template <int kPairing, bool kBack> __device__ __forceinline__ void turn(float* v, const float2* t, int e0, int dims, int lane, float* buf) {
+// element e of a lane's 8, and its partner there (P_NEIGHBOURS, P_HALVES)
+template <int kPairing> __device__ __forceinline__ constexpr int partner_of(int e) { return kPairing == P_HALVES ? e ^ 4 : e ^ 1; }
+
+// The factors of this lane's elements: x'[e] = x[e] own[e] + x[partner] other[e].  Elements behind dims: 1 and 0.  at[e]: their
+// places in the head; back: by the negative angle
+template <int kPairing, bool kBack> __device__ __forceinline__ void load_angles(const float2* cs, const int* at, int dims, float* own, float* other) {
   const int half = dims >> 1;
-  if (kPairing == P_NEIGHBOURS) {
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const float c = t[p].x, s = kBack ? -t[p].y : t[p].y, p0 = v[2 * p], p1 = v[2 * p + 1];
-      v[2 * p] = p0 * c - p1 * s;
-      v[2 * p + 1] = p1 * c + p0 * s;
-    }
-  } else if (kPairing == P_LANES) {      // half a multiple of 8: the partners are the 8 elements of one other lane
-    const int from = e0 < dims ? lane + (e0 < half ? half : -half) / 8 : lane;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float other = __shfl_sync(0xffffffffu, v[e], from);
-      v[e] = v[e] * t[e].x + (kBack ? other : -other) * t[e].y;
-    }
-  } else if (kPairing == P_ANY) {
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) buf[lane * 8 + e] = v[e];
-    __syncwarp();
-    const float* head = buf + lane * 8 - e0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int at = e0 + e;
-      const float other = at < dims ? head[at < half ? at + half : at - half] : 0.f;
-      v[e] = v[e] * t[e].x + (kBack ? other : -other) * t[e].y;
-    }
+  for (int e = 0; e < 8; ++e) {
+    const bool in = at[e] < dims;
+    const int i = kPairing == P_NEIGHBOURS ? at[e] >> 1 : at[e] < half ? at[e] : at[e] - half;
+    const bool first = kPairing == P_NEIGHBOURS ? (e & 1) == 0 : at[e] < half;
+    const float2 t = in ? cs[place_of(i)] : make_float2(1.f, 0.f);
+    own[e] = t.x;
+    other[e] = first != kBack ? -t.y : t.y;
   }
 }
 
 __device__ __forceinline__ float sum_over_lanes(float v, int lanes) {
-  for (int s = lanes >> 1; s; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
+#pragma unroll
+  for (int s = 16; s; s >>= 1)
+    if (lanes > s) v += __shfl_xor_sync(0xffffffffu, v, s);
   return v;
 }
 
-// DT: the type of x, u and y (backwards: x, dy and dx), -1 for a mixture
-template <int DT, int kPairing, bool kBack> __global__ void __launch_bounds__(kHeadThreads) head_kernel(const __grid_constant__ HeadArgs a) {
-  constexpr int kUnroll = kBack ? 2 : 4;
+// DT: the type of x, u and y (backwards: x, dy and dx), -1 for a mixture.  kU: u is written, or rounded before it is rotated
+template <int DT, int kPairing, bool kBack, bool kU> __global__ void __launch_bounds__(kHeadThreads, kHeadCtas) head_kernel(const __grid_constant__ HeadArgs a) {
+  constexpr int kUnroll = (kBack ? 2 : 4) / (DT == DRAGON_BF16 ? 1 : 2);
+  constexpr bool kApart = kPairing == P_HALVES;
   __shared__ float2 cs[kPairing == P_NONE ? 1 : kHeadRowsMost][kPlaces];
   __shared__ float buf[kPairing == P_ANY ? kHeadWarps : 1][256];
   __shared__ float sums[kBack ? kHeadWarps : 1][kMaxRotatedWidth];
   const HeadJob& jb = a.job[blockIdx.y];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (a.status_clear && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status_clear = 0;
-  const int l = lane & (a.lanes - 1), e0 = 8 * l;
-  const bool active = e0 < a.width;
+  const int l = lane & (a.lanes - 1);
+  const bool active = 8 * l < a.width;
+  // this lane's elements: from e0 on, and (P_HALVES) 4 of them `apart` further
+  int e0 = 8 * l, apart = 4;
+  if (kApart && e0 < a.dims) { e0 = 4 * l; apart = a.dims >> 1; }
+  int at_head[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) at_head[e] = e0 + (e & 3) + (e >= 4 ? apart : 0);
   const int per_warp = 32 / a.lanes, sub = lane / a.lanes;      // heads of one warp access
   const int groups = (jb.heads + per_warp - 1) / per_warp;
   const int side = kHeadWarps / a.tile, my_row = warp / side, my_side = warp - my_row * side;      // warps of a row
@@ -137,84 +161,126 @@ template <int DT, int kPairing, bool kBack> __global__ void __launch_bounds__(kH
   float g[8], dg[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) { g[e] = 1.f; dg[e] = 0.f; }
-  if (norm && active) load_any<8>(jb.gain, jb.gt, (size_t)e0, g);
-  for (long long r0 = (long long)blockIdx.x * a.tile; r0 < a.rows; r0 += (long long)gridDim.x * a.tile) {
+  if (norm && active) {
+    Eight<-1, true> r;
+    r.load(jb.gain, jb.gt, e0, apart);
+    r.get(g);
+  }
+  const long long stride = (long long)gridDim.x * a.tile;
+  struct Batch { Eight<DT, kApart> x[kUnroll], d[kUnroll]; };
+  auto head_of = [&](int i0, int k) { return (i0 + k * side) * per_warp + sub; };
+  auto place = [&](long long r0, int head) { return ((size_t)(r0 + my_row) * jb.heads + head) * a.width + e0; };
+  auto fetch = [&](long long r0, int i0, Batch& b) {
+    if (my_row + r0 >= a.rows) return;
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int head = head_of(i0, k);
+      if (active && head < jb.heads) {
+        const size_t at = place(r0, head);
+        if (!kBack || norm) b.x[k].load(jb.x, jb.xt, at, apart);
+        if (kBack) b.d[k].load(jb.dy, jb.dyt, at, apart);
+      }
+    }
+  };
+  Batch now;
+  fetch((long long)blockIdx.x * a.tile, my_side, now);
+  for (long long r0 = (long long)blockIdx.x * a.tile; r0 < a.rows; r0 += stride) {
     const int rows = (int)min((long long)a.tile, a.rows - r0);
-    float2 t[kPairing == P_NONE ? 1 : 8];
+    float own[8], other[8];
     if (kPairing != P_NONE) {
       __syncthreads();
       fill_angles(a, cs, (int)r0, rows);
       __syncthreads();
     }
     if (my_row >= rows) continue;
-    if (kPairing != P_NONE) load_angles<kPairing>(cs[my_row], e0, a.dims, t);
-    const size_t row_at = (size_t)(r0 + my_row) * jb.heads * a.width + e0;
-    for (int i0 = my_side; i0 < groups; i0 += side * kUnroll) {
-      Raw<DT, 8> rx[kUnroll], rd[kUnroll];
-      size_t at[kUnroll];
-      bool ok[kUnroll];
+    if (kPairing != P_NONE) {
+      load_angles<kPairing, kBack>(cs[my_row], at_head, a.dims, own, other);
+      if (!kBack && !kU && kPairing != P_ANY) {      // with the gains: the norm's own multiplication by them is done there
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        const int head = (i0 + k * side) * per_warp + sub;
-        ok[k] = active && head < jb.heads;
-        at[k] = row_at + (size_t)head * a.width;
-        if (ok[k]) {
-          if (!kBack || norm) rx[k].load(jb.x, jb.xt, at[k]);
-          if (kBack) rd[k].load(jb.dy, jb.dyt, at[k]);
-        }
+        for (int e = 0; e < 8; ++e) { own[e] *= g[e]; other[e] *= g[partner_of<kPairing>(e)]; }
       }
+    }
+    for (int i0 = my_side; i0 < groups; i0 += side * kUnroll) {
+      Batch next;
+      const bool last = i0 + side * kUnroll >= groups;
+      fetch(last ? r0 + stride : r0, last ? my_side : i0 + side * kUnroll, next);
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) {
         if (i0 + k * side >= groups) break;       // the whole warp
-        float x[8];
+        const int my_head = head_of(i0, k);
+        const bool ok = active && my_head < jb.heads;
+        const size_t at = place(r0, my_head);
+        float x[8], v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if (ok[k] && (!kBack || norm)) rx[k].get(x);
+        for (int e = 0; e < 8; ++e) x[e] = v[e] = 0.f;
+        if (ok && (!kBack || norm)) now.x[k].get(x);
+        if (kBack && ok) now.d[k].get(v);
         float inv = 1.f;
-        if (!kBack) {
-          if (norm) {
-            float q = 0.f;
+        if (norm) {
+          float q = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q += x[e] * x[e];
-            inv = rsqrtf(sum_over_lanes(q, a.lanes) * inv_width + jb.eps);
+          for (int e = 0; e < 8; ++e) q += x[e] * x[e];
+          inv = rsqrtf(sum_over_lanes(q, a.lanes) * inv_width + jb.eps);
+        }
+        if (!kBack) {
+          if (!kU && (kPairing == P_NEIGHBOURS || kPairing == P_HALVES)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = inv * (x[e] * own[e] + x[partner_of<kPairing>(e)] * other[e]);
+          } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * g[e];
-            if (jb.u && ok[k]) store_any<8>(jb.u, jb.ut, at[k], x);
-            if (jb.round_u) {
+            if (kU && jb.u && ok) Eight<-1, kApart>::store(jb.u, jb.ut, at, apart, x);
+            if (kU && jb.round_u) {
 #pragma unroll
               for (int e = 0; e < 8; ++e) x[e] = bf16_rounded(x[e]);
             }
           }
-          turn<kPairing, false>(x, t, e0, a.dims, lane, buf[kPairing == P_ANY ? warp : 0]);
-          if (jb.y && ok[k]) { Raw<DT, 8> o; o.set(x); o.store(jb.y, jb.yt, at[k]); }
-        } else {
-          float d[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[e] = 0.f;
-          if (ok[k]) rd[k].get(d);
-          turn<kPairing, true>(d, t, e0, a.dims, lane, buf[kPairing == P_ANY ? warp : 0]);
-          if (norm) {
-            float q = 0.f, m = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { q += x[e] * x[e]; m += d[e] * g[e] * x[e]; }
-            inv = rsqrtf(sum_over_lanes(q, a.lanes) * inv_width + jb.eps);
-            const float c = inv * inv * inv * (sum_over_lanes(m, a.lanes) * inv_width);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              dg[e] += d[e] * x[e] * inv;
-              d[e] = inv * d[e] * g[e] - x[e] * c;
-            }
-          }
-          if (jb.y && ok[k]) { Raw<DT, 8> o; o.set(d); o.store(jb.y, jb.yt, at[k]); }
         }
+        float* from = kBack ? v : x;      // what is rotated
+        if (kPairing == P_ANY) {
+          float* b = buf[kPairing == P_ANY ? warp : 0];
+          const int half = a.dims >> 1;
+          __syncwarp();
+#pragma unroll
+          for (int e = 0; e < 8; ++e) b[lane * 8 + e] = from[e];
+          __syncwarp();
+          const float* head = b + lane * 8 - e0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int p = e0 + e;
+            v[e] = from[e] * own[e] + (p < a.dims ? head[p < half ? p + half : p - half] : 0.f) * other[e];
+          }
+        } else if ((kBack || kU) && kPairing != P_NONE) {
+          float w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = from[e] * own[e] + from[partner_of<kPairing>(e)] * other[e];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = w[e];
+        } else if (!kBack && kPairing == P_NONE) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = x[e];
+        }
+        if (kBack && norm) {
+          float m = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m += v[e] * g[e] * x[e];
+          const float c = inv * inv * inv * (sum_over_lanes(m, a.lanes) * inv_width);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            dg[e] += v[e] * x[e] * inv;
+            v[e] = inv * v[e] * g[e] - x[e] * c;
+          }
+        }
+        if (jb.y && ok) Eight<DT, kApart>::store(jb.y, jb.yt, at, apart, v);
       }
+      now = next;
     }
   }
   if (kBack && jb.dgain) {      // the CTA's part of dg: lanes of the same elements, then the warps, in a fixed order
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       for (int s = a.lanes; s < 32; s <<= 1) dg[e] += __shfl_xor_sync(0xffffffffu, dg[e], s);
-      if (lane < a.lanes && active) sums[warp][e0 + e] = dg[e];
+      if (lane < a.lanes && active) sums[warp][at_head[e]] = dg[e];
     }
     __syncthreads();
     for (int c = threadIdx.x; c < a.width; c += kHeadThreads) {
@@ -256,19 +322,19 @@ __global__ void __launch_bounds__(1024) head_finish(const __grid_constant__ Fini
   }
 }
 
-// Rows of a tile: as many as leave four CTAs for every SM
+// Rows of a tile: as many as leave tiles enough for four CTAs on every SM
 int tile_rows(int64_t rows, int sm_count) {
   int t = kHeadRowsMost;
   while (t > 1 && rows < t * (4 * (int64_t)sm_count)) t /= 2;
   return t;
 }
 
-template <bool kBack, int DT> void launch_pairing(const HeadArgs& a, int pairing, dim3 grid, cudaStream_t st) {
+template <int DT, bool kBack, bool kU> void launch_pairing(const HeadArgs& a, int pairing, dim3 grid, cudaStream_t st) {
   switch (pairing) {
-    case P_NONE: head_kernel<DT, P_NONE, kBack><<<grid, kHeadThreads, 0, st>>>(a); break;
-    case P_NEIGHBOURS: head_kernel<DT, P_NEIGHBOURS, kBack><<<grid, kHeadThreads, 0, st>>>(a); break;
-    case P_LANES: head_kernel<DT, P_LANES, kBack><<<grid, kHeadThreads, 0, st>>>(a); break;
-    default: head_kernel<DT, P_ANY, kBack><<<grid, kHeadThreads, 0, st>>>(a);
+    case P_NONE: head_kernel<DT, P_NONE, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a); break;
+    case P_NEIGHBOURS: head_kernel<DT, P_NEIGHBOURS, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a); break;
+    case P_HALVES: head_kernel<DT, P_HALVES, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a); break;
+    default: head_kernel<DT, P_ANY, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a);
   }
 }
 
@@ -281,27 +347,29 @@ template <bool kBack> cudaError_t launch(HeadArgs& a, const Step& s, int jobs, d
     a.dims = (int)n[hn::DIMS];
     a.amplitude = (float)n[hn::AMPLITUDE];
     std::copy(s.freq.begin(), s.freq.end(), a.freq);
-    pairing = n[hn::INTERLEAVED] != 0.0 ? P_NEIGHBOURS : a.dims % 16 == 0 ? P_LANES : P_ANY;
+    pairing = n[hn::INTERLEAVED] != 0.0 ? P_NEIGHBOURS : a.dims % 8 == 0 ? P_HALVES : P_ANY;
   }
-  bool all[2] = {true, true};      // every tensor is f32, is bf16
+  bool all[2] = {true, true}, with_u = false;      // every tensor is f32, is bf16
   for (int j = 0; j < jobs; ++j) {
     const HeadJob& b = a.job[j];
+    with_u |= b.u || b.round_u;
     for (int t = 0; t < 2; ++t) {
       const int type = t ? DRAGON_BF16 : DRAGON_F32;
       all[t] &= (!b.x || b.xt == type) && (!b.y || b.yt == type) && (!kBack || b.dyt == type);
     }
   }
-  if (all[1]) launch_pairing<kBack, DRAGON_BF16>(a, pairing, grid, st);
-  else if (all[0]) launch_pairing<kBack, DRAGON_F32>(a, pairing, grid, st);
-  else launch_pairing<kBack, -1>(a, pairing, grid, st);
+  if (!kBack && with_u) launch_pairing<-1, false, true>(a, pairing, grid, st);
+  else if (all[1]) launch_pairing<DRAGON_BF16, kBack, false>(a, pairing, grid, st);
+  else if (all[0]) launch_pairing<DRAGON_F32, kBack, false>(a, pairing, grid, st);
+  else launch_pairing<-1, kBack, false>(a, pairing, grid, st);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-int head_bwd_partials(int64_t rows, int sm_count) {
+int head_bwd_partials(int64_t rows, int sm_count) {      // the grid, too
   const int tile = tile_rows(rows, sm_count);
-  return (int)std::min<int64_t>((rows + tile - 1) / tile, 4 * (int64_t)sm_count);
+  return (int)std::min<int64_t>((rows + tile - 1) / tile, kHeadCtas * (int64_t)sm_count);
 }
 
 cudaError_t launch_head(const StepRun& r) {
@@ -328,7 +396,7 @@ cudaError_t launch_head(const StepRun& r) {
   a.pos = rotated ? reinterpret_cast<const int*>(r.rd(hd::POS)) : nullptr;
   a.status_clear = r.status_clear;
   a.tile = tile_rows(a.rows, r.sm_count);
-  return launch<false>(a, s, jobs, dim3((unsigned)((a.rows + (int64_t)a.tile - 1) / a.tile), jobs), reinterpret_cast<cudaStream_t>(r.stream));
+  return launch<false>(a, s, jobs, dim3(head_bwd_partials(a.rows, r.sm_count), jobs), reinterpret_cast<cudaStream_t>(r.stream));
 }
 
 cudaError_t launch_head_bwd(const StepRun& r) {
