@@ -8,6 +8,7 @@
 #include <mutex>
 
 #include "attention_util.h"
+#include "device_util.h"
 #include "plan.h"
 #include "tcgen05_util.h"
 
@@ -52,14 +53,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
 // 2^x, results below 2^-126 as 0
 __device__ __forceinline__ float exp2_fast(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
-// two fp32 values in one 64-bit register, and arithmetic on both at once
-typedef unsigned long long Pair;
-__device__ __forceinline__ Pair pair_of(float lo, float hi) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi)); return p; }
-__device__ __forceinline__ Pair pair_of(uint32_t lo, uint32_t hi) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi)); return p; }
-__device__ __forceinline__ float2 both(Pair p) { float2 v; asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p)); return v; }
-__device__ __forceinline__ Pair fma_pair(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
-__device__ __forceinline__ Pair add_pair(Pair a, Pair b) { Pair d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
-__device__ __forceinline__ Pair mul_pair(Pair a, Pair b) { Pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 // the largest of three, NaN if one of them is
 __device__ __forceinline__ float most_of(float a, float b, float c) { float d; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d; }
 

@@ -18,6 +18,15 @@ __device__ __forceinline__ unsigned bf16_pair(float lo, float hi) {
 __device__ __forceinline__ unsigned short bf16_one(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 __device__ __forceinline__ float bf16_rounded(float v) { return bf16_low(bf16_one(v)); }
 
+// two fp32 values in one 64-bit register, and arithmetic on both at once
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair_of(float lo, float hi) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi)); return p; }
+__device__ __forceinline__ Pair pair_of(uint32_t lo, uint32_t hi) { Pair p; asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi)); return p; }
+__device__ __forceinline__ float2 both(Pair p) { float2 v; asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p)); return v; }
+__device__ __forceinline__ Pair fma_pair(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ Pair add_pair(Pair a, Pair b) { Pair d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ Pair mul_pair(Pair a, Pair b) { Pair d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+
 // V consecutive elements (V = 8: 16-byte aligned, 2 or 1) as they are in memory, so that loads can be issued
 // together and converted later.  DT -1: a type known at run time, -2: an absent operand.
 template <int DT, int V> struct Raw;

@@ -55,13 +55,16 @@ __device__ __forceinline__ int place_of(int i) { return (i & 7) * (kPairsMost / 
 constexpr int kPlaces = 8 * (kPairsMost / 8 + 1);
 
 // the angles of `rows` rows from r0 on
-__device__ __forceinline__ void fill_angles(const HeadArgs& a, float2 (*cs)[kPlaces], int r0, int rows) {
+__device__ __forceinline__ void fill_angles(const HeadArgs& a, const unsigned long long* freq, float2 (*cs)[kPlaces], int r0, int rows) {
   const int pairs = a.dims >> 1;
-  for (int i = threadIdx.x; i < rows * pairs; i += kHeadThreads) {
-    const int r = i / pairs, k = i - r * pairs;
-    const unsigned long long turn = (unsigned long long)(long long)__ldg(a.pos + r0 + r) * a.freq[k];
+  int r = threadIdx.x >> 5;      // a warp a row (the rows of a tile are at most as many as the warps)
+  const int side = kHeadWarps / a.tile, part = r / a.tile;
+  r -= part * a.tile;
+  if (r >= rows) return;
+  const unsigned long long pos = (unsigned long long)(long long)__ldg(a.pos + r0 + r);
+  for (int k = (threadIdx.x & 31) + 32 * part; k < pairs; k += 32 * side) {
     float s, c;
-    sincospif((float)(int)(turn >> 32) * 0x1p-31f, &s, &c);
+    sincospif((float)(int)((pos * freq[k]) >> 32) * 0x1p-31f, &s, &c);
     cs[r][place_of(k)] = make_float2(a.amplitude * c, a.amplitude * s);
   }
 }
@@ -110,86 +113,103 @@ template <int DT> struct Eight<DT, true> {
   static __device__ __forceinline__ void store(void* p, int dtype, size_t i, int apart, const float* v) { Four<DT>::store(p, dtype, i, v); Four<DT>::store(p, dtype, i + apart, v + 4); }
 };
 
-// element e of a lane's 8, and its partner there (P_NEIGHBOURS, P_HALVES)
-template <int kPairing> __device__ __forceinline__ constexpr int partner_of(int e) { return kPairing == P_HALVES ? e ^ 4 : e ^ 1; }
-
-// The factors of this lane's elements: x'[e] = x[e] own[e] + x[partner] other[e].  Elements behind dims: 1 and 0.  at[e]: their
+// The factors of this lane's elements, in pairs: x'[e] = x[e] own[e] + x[partner] other[e].  Elements behind dims: 1 and 0.  at[e]: their
 // places in the head; back: by the negative angle
-template <int kPairing, bool kBack> __device__ __forceinline__ void load_angles(const float2* cs, const int* at, int dims, float* own, float* other) {
+template <int kPairing, bool kBack> __device__ __forceinline__ void load_angles(const float2* cs, const int* at, int dims, Pair* own, Pair* other) {
   const int half = dims >> 1;
+  float x[8], y[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const bool in = at[e] < dims;
     const int i = kPairing == P_NEIGHBOURS ? at[e] >> 1 : at[e] < half ? at[e] : at[e] - half;
     const bool first = kPairing == P_NEIGHBOURS ? (e & 1) == 0 : at[e] < half;
     const float2 t = in ? cs[place_of(i)] : make_float2(1.f, 0.f);
-    own[e] = t.x;
-    other[e] = first != kBack ? -t.y : t.y;
+    x[e] = t.x;
+    y[e] = first != kBack ? -t.y : t.y;
   }
+#pragma unroll
+  for (int p = 0; p < 4; ++p) { own[p] = pair_of(x[2 * p], x[2 * p + 1]); other[p] = pair_of(y[2 * p], y[2 * p + 1]); }
 }
+// the partners of pair p of a lane's values (P_NEIGHBOURS, P_HALVES)
+template <int kPairing> __device__ __forceinline__ Pair partners(const Pair* v, int p) {
+  if (kPairing == P_HALVES) return v[p ^ 2];
+  const float2 f = both(v[p]);
+  return pair_of(f.y, f.x);
+}
+__device__ __forceinline__ Pair twice(float v) { return pair_of(v, v); }
+__device__ __forceinline__ float sum_of(Pair a, Pair b) { const float2 s = both(add_pair(a, b)); return s.x + s.y; }
 
-__device__ __forceinline__ float sum_over_lanes(float v, int lanes) {
+template <int kLanes> __device__ __forceinline__ float sum_over_lanes(float v, int lanes) {
 #pragma unroll
   for (int s = 16; s; s >>= 1)
-    if (lanes > s) v += __shfl_xor_sync(0xffffffffu, v, s);
+    if (kLanes ? kLanes > s : lanes > s) v += __shfl_xor_sync(0xffffffffu, v, s);
   return v;
 }
 
-// DT: the type of x, u and y (backwards: x, dy and dx), -1 for a mixture.  kU: u is written, or rounded before it is rotated
-template <int DT, int kPairing, bool kBack, bool kU> __global__ void __launch_bounds__(kHeadThreads, kHeadCtas) head_kernel(const __grid_constant__ HeadArgs a) {
+// DT: the type of x, u and y (backwards: x, dy and dx), -1 for a mixture.  kU: u is written, or rounded before it is rotated.  kLanes: of a
+// head, where every lane of every access has elements (the head's width 8 times a power of two, heads a multiple of those of an
+// access), otherwise 0
+template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void __launch_bounds__(kHeadThreads, kHeadCtas) head_kernel(const __grid_constant__ HeadArgs a) {
   constexpr int kUnroll = (kBack ? 2 : 4) / (DT == DRAGON_BF16 ? 1 : 2);
   constexpr bool kApart = kPairing == P_HALVES;
   __shared__ float2 cs[kPairing == P_NONE ? 1 : kHeadRowsMost][kPlaces];
+  __shared__ unsigned long long freq[kPairing == P_NONE ? 1 : kPairsMost];      // (lanes that index parameters apart wait for one another)
   __shared__ float buf[kPairing == P_ANY ? kHeadWarps : 1][256];
   __shared__ float sums[kBack ? kHeadWarps : 1][kMaxRotatedWidth];
   const HeadJob& jb = a.job[blockIdx.y];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (a.status_clear && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.status_clear = 0;
-  const int l = lane & (a.lanes - 1);
-  const bool active = 8 * l < a.width;
+  if (kPairing != P_NONE && threadIdx.x < a.dims >> 1) freq[threadIdx.x] = a.freq[threadIdx.x];      // (seen behind the tile's first barrier)
+  const int lanes = kLanes ? kLanes : a.lanes, width = kLanes ? 8 * kLanes : a.width, l = lane & (lanes - 1);
+  const bool active = kLanes || 8 * l < width;
   // this lane's elements: from e0 on, and (P_HALVES) 4 of them `apart` further
   int e0 = 8 * l, apart = 4;
   if (kApart && e0 < a.dims) { e0 = 4 * l; apart = a.dims >> 1; }
   int at_head[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) at_head[e] = e0 + (e & 3) + (e >= 4 ? apart : 0);
-  const int per_warp = 32 / a.lanes, sub = lane / a.lanes;      // heads of one warp access
+  const int per_warp = 32 / lanes, sub = lane / lanes;      // heads of one warp access
   const int groups = (jb.heads + per_warp - 1) / per_warp;
   const int side = kHeadWarps / a.tile, my_row = warp / side, my_side = warp - my_row * side;      // warps of a row
-  const float inv_width = 1.f / (float)a.width;
+  const float inv_width = 1.f / (float)width;
   const bool norm = jb.gain != nullptr;
-  float g[8], dg[8];
+  Pair g[4], dg[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) { g[e] = 1.f; dg[e] = 0.f; }
+  for (int p = 0; p < 4; ++p) { g[p] = twice(1.f); dg[p] = 0; }
   if (norm && active) {
     Eight<-1, true> r;
+    float f[8];
     r.load(jb.gain, jb.gt, e0, apart);
-    r.get(g);
+    r.get(f);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) g[p] = pair_of(f[2 * p], f[2 * p + 1]);
   }
   const long long stride = (long long)gridDim.x * a.tile;
   struct Batch { Eight<DT, kApart> x[kUnroll], d[kUnroll]; };
-  auto head_of = [&](int i0, int k) { return (i0 + k * side) * per_warp + sub; };
-  auto place = [&](long long r0, int head) { return ((size_t)(r0 + my_row) * jb.heads + head) * a.width + e0; };
-  auto fetch = [&](long long r0, int i0, Batch& b) {
-    if (my_row + r0 >= a.rows) return;
+  // this lane's first elements of the warp's row of the tile: 32-bit offsets from there to the other heads (a row is at most 2^26 long)
+  auto row_of = [&](long long r0) { return (size_t)(r0 + my_row) * jb.heads * width + sub * width + e0; };
+  auto fetch = [&](size_t row, bool there, int i0, Batch& b) {
+    if (!there) return;
 #pragma unroll
     for (int k = 0; k < kUnroll; ++k) {
-      const int head = head_of(i0, k);
-      if (active && head < jb.heads) {
-        const size_t at = place(r0, head);
+      const int grp = i0 + k * side;
+      if (kLanes ? grp < groups : active && grp * per_warp + sub < jb.heads) {
+        const size_t at = row + (unsigned)(grp * (per_warp * width));
         if (!kBack || norm) b.x[k].load(jb.x, jb.xt, at, apart);
         if (kBack) b.d[k].load(jb.dy, jb.dyt, at, apart);
       }
     }
   };
   Batch now;
-  fetch((long long)blockIdx.x * a.tile, my_side, now);
-  for (long long r0 = (long long)blockIdx.x * a.tile; r0 < a.rows; r0 += stride) {
+  const size_t row_stride = (size_t)stride * jb.heads * width;
+  size_t row = row_of((long long)blockIdx.x * a.tile);
+  fetch(row, (long long)blockIdx.x * a.tile + my_row < a.rows, my_side, now);
+  for (long long r0 = (long long)blockIdx.x * a.tile; r0 < a.rows; r0 += stride, row += row_stride) {
     const int rows = (int)min((long long)a.tile, a.rows - r0);
-    float own[8], other[8];
+    Pair own[4], other[4];
     if (kPairing != P_NONE) {
       __syncthreads();
-      fill_angles(a, cs, (int)r0, rows);
+      fill_angles(a, freq, cs, (int)r0, rows);
       __syncthreads();
     }
     if (my_row >= rows) continue;
@@ -197,81 +217,97 @@ template <int DT, int kPairing, bool kBack, bool kU> __global__ void __launch_bo
       load_angles<kPairing, kBack>(cs[my_row], at_head, a.dims, own, other);
       if (!kBack && !kU && kPairing != P_ANY) {      // with the gains: the norm's own multiplication by them is done there
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { own[e] *= g[e]; other[e] *= g[partner_of<kPairing>(e)]; }
+        for (int p = 0; p < 4; ++p) { own[p] = mul_pair(own[p], g[p]); other[p] = mul_pair(other[p], partners<kPairing>(g, p)); }
       }
     }
     for (int i0 = my_side; i0 < groups; i0 += side * kUnroll) {
       Batch next;
       const bool last = i0 + side * kUnroll >= groups;
-      fetch(last ? r0 + stride : r0, last ? my_side : i0 + side * kUnroll, next);
+      fetch(last ? row + row_stride : row, !last || r0 + stride + my_row < a.rows, last ? my_side : i0 + side * kUnroll, next);
 #pragma unroll
       for (int k = 0; k < kUnroll; ++k) {
         if (i0 + k * side >= groups) break;       // the whole warp
-        const int my_head = head_of(i0, k);
-        const bool ok = active && my_head < jb.heads;
-        const size_t at = place(r0, my_head);
-        float x[8], v[8];
+        const bool ok = kLanes || (active && (i0 + k * side) * per_warp + sub < jb.heads);
+        const size_t at = row + (unsigned)((i0 + k * side) * (per_warp * width));
+        Pair x[4] = {0, 0, 0, 0}, v[4] = {0, 0, 0, 0};
+        float f[8];
+        if (ok && (!kBack || norm)) {
+          now.x[k].get(f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = v[e] = 0.f;
-        if (ok && (!kBack || norm)) now.x[k].get(x);
-        if (kBack && ok) now.d[k].get(v);
+          for (int p = 0; p < 4; ++p) x[p] = pair_of(f[2 * p], f[2 * p + 1]);
+        }
+        if (kBack && ok) {
+          now.d[k].get(f);
+#pragma unroll
+          for (int p = 0; p < 4; ++p) v[p] = pair_of(f[2 * p], f[2 * p + 1]);
+        }
         float inv = 1.f;
         if (norm) {
-          float q = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) q += x[e] * x[e];
-          inv = rsqrtf(sum_over_lanes(q, a.lanes) * inv_width + jb.eps);
+          const float q = sum_of(fma_pair(x[0], x[0], mul_pair(x[1], x[1])), fma_pair(x[2], x[2], mul_pair(x[3], x[3])));
+          inv = rsqrtf(sum_over_lanes<kLanes>(q, lanes) * inv_width + jb.eps);
         }
+        const Pair r = twice(inv);
         if (!kBack) {
           if (!kU && (kPairing == P_NEIGHBOURS || kPairing == P_HALVES)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = inv * (x[e] * own[e] + x[partner_of<kPairing>(e)] * other[e]);
+            for (int p = 0; p < 4; ++p) v[p] = mul_pair(r, fma_pair(x[p], own[p], mul_pair(partners<kPairing>(x, p), other[p])));
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * g[e];
-            if (kU && jb.u && ok) Eight<-1, kApart>::store(jb.u, jb.ut, at, apart, x);
+            for (int p = 0; p < 4; ++p) {
+              x[p] = mul_pair(mul_pair(x[p], r), g[p]);
+              const float2 t = both(x[p]);
+              f[2 * p] = t.x; f[2 * p + 1] = t.y;
+            }
+            if (kU && jb.u && ok) Eight<-1, kApart>::store(jb.u, jb.ut, at, apart, f);
             if (kU && jb.round_u) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] = bf16_rounded(x[e]);
+              for (int p = 0; p < 4; ++p) x[p] = pair_of(bf16_rounded(f[2 * p]), bf16_rounded(f[2 * p + 1]));
             }
           }
         }
-        float* from = kBack ? v : x;      // what is rotated
+        const Pair* from = kBack ? v : x;      // what is rotated
         if (kPairing == P_ANY) {
           float* b = buf[kPairing == P_ANY ? warp : 0];
           const int half = a.dims >> 1;
           __syncwarp();
 #pragma unroll
-          for (int e = 0; e < 8; ++e) b[lane * 8 + e] = from[e];
+          for (int p = 0; p < 4; ++p) *reinterpret_cast<Pair*>(b + lane * 8 + 2 * p) = from[p];
           __syncwarp();
           const float* head = b + lane * 8 - e0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int p = e0 + e;
-            v[e] = from[e] * own[e] + (p < a.dims ? head[p < half ? p + half : p - half] : 0.f) * other[e];
+          for (int p = 0; p < 4; ++p) {
+            float o[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) { const int i = e0 + 2 * p + e; o[e] = i < a.dims ? head[i < half ? i + half : i - half] : 0.f; }
+            v[p] = fma_pair(from[p], own[p], mul_pair(pair_of(o[0], o[1]), other[p]));
           }
         } else if ((kBack || kU) && kPairing != P_NONE) {
-          float w[8];
+          Pair w[4];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = from[e] * own[e] + from[partner_of<kPairing>(e)] * other[e];
+          for (int p = 0; p < 4; ++p) w[p] = fma_pair(from[p], own[p], mul_pair(partners<kPairing>(from, p), other[p]));
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = w[e];
+          for (int p = 0; p < 4; ++p) v[p] = w[p];
         } else if (!kBack && kPairing == P_NONE) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = x[e];
+          for (int p = 0; p < 4; ++p) v[p] = x[p];
         }
         if (kBack && norm) {
-          float m = 0.f;
+          Pair t[4];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) m += v[e] * g[e] * x[e];
-          const float c = inv * inv * inv * (sum_over_lanes(m, a.lanes) * inv_width);
+          for (int p = 0; p < 4; ++p) t[p] = mul_pair(v[p], g[p]);
+          const float m = sum_of(fma_pair(t[0], x[0], mul_pair(t[1], x[1])), fma_pair(t[2], x[2], mul_pair(t[3], x[3])));
+          const Pair c = twice(-inv * inv * inv * (sum_over_lanes<kLanes>(m, lanes) * inv_width));
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            dg[e] += v[e] * x[e] * inv;
-            v[e] = inv * v[e] * g[e] - x[e] * c;
+          for (int p = 0; p < 4; ++p) {
+            dg[p] = fma_pair(v[p], mul_pair(x[p], r), dg[p]);
+            v[p] = fma_pair(t[p], r, mul_pair(x[p], c));
           }
         }
-        if (jb.y && ok) Eight<DT, kApart>::store(jb.y, jb.yt, at, apart, v);
+        if (jb.y && ok) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) { const float2 t = both(v[p]); f[2 * p] = t.x; f[2 * p + 1] = t.y; }
+          Eight<DT, kApart>::store(jb.y, jb.yt, at, apart, f);
+        }
       }
       now = next;
     }
@@ -279,8 +315,9 @@ template <int DT, int kPairing, bool kBack, bool kU> __global__ void __launch_bo
   if (kBack && jb.dgain) {      // the CTA's part of dg: lanes of the same elements, then the warps, in a fixed order
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      for (int s = a.lanes; s < 32; s <<= 1) dg[e] += __shfl_xor_sync(0xffffffffu, dg[e], s);
-      if (lane < a.lanes && active) sums[warp][at_head[e]] = dg[e];
+      float d = e & 1 ? both(dg[e >> 1]).y : both(dg[e >> 1]).x;
+      for (int s = lanes; s < 32; s <<= 1) d += __shfl_xor_sync(0xffffffffu, d, s);
+      if (lane < lanes && active) sums[warp][at_head[e]] = d;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < a.width; c += kHeadThreads) {
@@ -329,12 +366,24 @@ int tile_rows(int64_t rows, int sm_count) {
   return t;
 }
 
-template <int DT, bool kBack, bool kU> void launch_pairing(const HeadArgs& a, int pairing, dim3 grid, cudaStream_t st) {
+template <int DT, int kPairing, bool kBack, bool kU> void launch_lanes(const HeadArgs& a, bool full, dim3 grid, cudaStream_t st) {
+  if constexpr (DT != -1 && kPairing != P_NONE && kPairing != P_ANY) {
+    if (full && a.lanes >= 4) {      // heads of 32, 64, 128 and 256
+      if (a.lanes == 4) head_kernel<DT, kPairing, kBack, kU, 4><<<grid, kHeadThreads, 0, st>>>(a);
+      else if (a.lanes == 8) head_kernel<DT, kPairing, kBack, kU, 8><<<grid, kHeadThreads, 0, st>>>(a);
+      else if (a.lanes == 16) head_kernel<DT, kPairing, kBack, kU, 16><<<grid, kHeadThreads, 0, st>>>(a);
+      else head_kernel<DT, kPairing, kBack, kU, 32><<<grid, kHeadThreads, 0, st>>>(a);
+      return;
+    }
+  }
+  head_kernel<DT, kPairing, kBack, kU, 0><<<grid, kHeadThreads, 0, st>>>(a);
+}
+template <int DT, bool kBack, bool kU> void launch_pairing(const HeadArgs& a, int pairing, bool full, dim3 grid, cudaStream_t st) {
   switch (pairing) {
-    case P_NONE: head_kernel<DT, P_NONE, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a); break;
-    case P_NEIGHBOURS: head_kernel<DT, P_NEIGHBOURS, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a); break;
-    case P_HALVES: head_kernel<DT, P_HALVES, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a); break;
-    default: head_kernel<DT, P_ANY, kBack, kU><<<grid, kHeadThreads, 0, st>>>(a);
+    case P_NONE: launch_lanes<DT, P_NONE, kBack, kU>(a, full, grid, st); break;
+    case P_NEIGHBOURS: launch_lanes<DT, P_NEIGHBOURS, kBack, kU>(a, full, grid, st); break;
+    case P_HALVES: launch_lanes<DT, P_HALVES, kBack, kU>(a, full, grid, st); break;
+    default: launch_lanes<DT, P_ANY, kBack, kU>(a, full, grid, st);
   }
 }
 
@@ -349,19 +398,20 @@ template <bool kBack> cudaError_t launch(HeadArgs& a, const Step& s, int jobs, d
     std::copy(s.freq.begin(), s.freq.end(), a.freq);
     pairing = n[hn::INTERLEAVED] != 0.0 ? P_NEIGHBOURS : a.dims % 8 == 0 ? P_HALVES : P_ANY;
   }
-  bool all[2] = {true, true}, with_u = false;      // every tensor is f32, is bf16
+  bool all[2] = {true, true}, with_u = false, full = a.lanes * 8 == a.width;      // every tensor is f32, is bf16
   for (int j = 0; j < jobs; ++j) {
     const HeadJob& b = a.job[j];
     with_u |= b.u || b.round_u;
+    full &= b.heads % (32 / a.lanes) == 0;
     for (int t = 0; t < 2; ++t) {
       const int type = t ? DRAGON_BF16 : DRAGON_F32;
       all[t] &= (!b.x || b.xt == type) && (!b.y || b.yt == type) && (!kBack || b.dyt == type);
     }
   }
-  if (!kBack && with_u) launch_pairing<-1, false, true>(a, pairing, grid, st);
-  else if (all[1]) launch_pairing<DRAGON_BF16, kBack, false>(a, pairing, grid, st);
-  else if (all[0]) launch_pairing<DRAGON_F32, kBack, false>(a, pairing, grid, st);
-  else launch_pairing<-1, kBack, false>(a, pairing, grid, st);
+  if (!kBack && with_u) launch_pairing<-1, false, true>(a, pairing, full, grid, st);
+  else if (all[1]) launch_pairing<DRAGON_BF16, kBack, false>(a, pairing, full, grid, st);
+  else if (all[0]) launch_pairing<DRAGON_F32, kBack, false>(a, pairing, full, grid, st);
+  else launch_pairing<-1, kBack, false>(a, pairing, full, grid, st);
   return cudaGetLastError();
 }
 
