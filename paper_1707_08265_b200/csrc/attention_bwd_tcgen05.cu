@@ -244,7 +244,8 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       float p[64];
       tmem_ld32(tmem + lanes + kS + 64 * half, v);
       tmem_ld32(tmem + lanes + kS + 64 * half + 32, v + 32);
-      tmem_ld_wait();
+      tmem_loaded32(v);
+      tmem_loaded32(v + 32);
       if (!kKeys) {
         fence_before();
         __syncwarp();
@@ -276,7 +277,8 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       fence_after();
       tmem_ld32(dp, v);
       tmem_ld32(dp + 32, v + 32);
-      tmem_ld_wait();
+      tmem_loaded32(v);
+      tmem_loaded32(v + 32);
 #pragma unroll
       for (int c = 0; c < 64; c += 4) {
         float4 d = make_float4(-delta, -delta, -delta, -delta);
@@ -308,7 +310,7 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
           uint32_t o[16];
           float f[16];
           tmem_ld16(tmem + lanes + acc + c, o);
-          tmem_ld_wait();
+          tmem_loaded16(o);
 #pragma unroll
           for (int k = 0; k < 16; ++k) { f[k] = __uint_as_float(o[k]) * factor; fine &= fabsf(f[k]) < kInf; }
           if (mine && out) {

@@ -234,7 +234,8 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       uint32_t s[128];
 #pragma unroll
       for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
-      tmem_ld_wait();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_loaded32(s + 32 * c);
       const int k0 = (j0 + j) * 128;
       if (!__all_sync(0xffffffffu, lo <= k0 && k0 + 128 <= hi)) {
 #pragma unroll
@@ -260,7 +261,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
           for (int c = 0; c < a.r.width; c += 16) {
             uint32_t o[16];
             tmem_ld16(o_at + c, o);
-            tmem_ld_wait();
+            tmem_loaded16(o);
 #pragma unroll
             for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
             tmem_st16(o_at + c, o);
@@ -302,7 +303,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       for (int c = 0; c < a.r.width; c += 16) {
         uint32_t o[16];
         float v[16];
-        if (n_tiles > 0) { tmem_ld16(o_at + c, o); tmem_ld_wait(); }
+        if (n_tiles > 0) { tmem_ld16(o_at + c, o); tmem_loaded16(o); }
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
           v[k] = n_tiles > 0 ? __uint_as_float(o[k]) * inv : 0.f;
