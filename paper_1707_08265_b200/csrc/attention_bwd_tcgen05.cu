@@ -104,6 +104,7 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const int t0 = first / 128, tiles = (end + 127) / 128 - t0, n = tiles * (kKeys ? group : 1);
 
   if (warp == 9) {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -111,15 +112,15 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  auto wait = [&](uint32_t bar, uint32_t parity) {
-    if (mbar_wait(bar, parity, abort_flag, a.budget)) return true;
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_wait_warp(bar, parity, abort_flag, a.budget)) return true;
     *abort_flag = 1;
     report(a.r.status, DRAGON_ERR_TIMEOUT);
     return false;
   };
   int issued1 = 0, issued2 = 0;
   if (warp == 8) {
-    if (lane == 0) {
+    if (elected()) {
       mbar_expect_tx(x_full, 2 * kTile);
       for (int c = 0; c < kChunks; ++c) {
         tma_load_3d(x1 + c * kChunkBytes, kKeys ? &tm_k : &tm_q, 64 * c, head, u.a + u.row0, x_full);
@@ -132,15 +133,17 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     for (int i = 0; i < n && ok; ++i, ++tile) {
       if (tile == tiles) { tile = 0; ++h; }
       const int s = i % kSt1, turn = i / kSt1, row = u.a + (t0 + tile) * 128;
-      ok = __all_sync(0xffffffffu, wait(y1_empty + 8 * s, (turn & 1) ^ 1));
+      ok = wait_warp(y1_empty + 8 * s, (turn & 1) ^ 1);
       if (!ok) break;
       issued1 = i + 1;
-      if (lane == 0 && !(a.drop_first_load && i == 0)) {      // (failure-detection test: the first stage's signal never comes)
+      const bool leave_out = a.drop_first_load && i == 0;      // (failure-detection test: the first stage's signal never comes)
+      if (elected() && !leave_out) {
         mbar_expect_tx(y1_full + 8 * s, kTile);
         for (int c = 0; c < kChunks; ++c) tma_load_3d(y1 + s * kTile + c * kChunkBytes, kKeys ? &tm_q : &tm_k, 64 * c, h, row, y1_full + 8 * s);
       }
+      __syncwarp();
       if (kKeys) {      // -lse and -delta of the tile's rows; a row behind the sequence's last has probabilities 0
-        ok = __all_sync(0xffffffffu, wait(st_empty + 8 * s, (turn & 1) ^ 1));
+        ok = wait_warp(st_empty + 8 * s, (turn & 1) ^ 1);
         if (!ok) break;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -152,66 +155,70 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         mbar_arrive(st_full + 8 * s);
       }
       const int s2 = i % kSt2;
-      ok = __all_sync(0xffffffffu, wait(y2_empty + 8 * s2, ((i / kSt2) & 1) ^ 1));
+      ok = wait_warp(y2_empty + 8 * s2, ((i / kSt2) & 1) ^ 1);
       if (!ok) break;
       issued2 = i + 1;
-      if (lane == 0) {
+      if (elected()) {
         mbar_expect_tx(y2_full + 8 * s2, kTile);
         for (int c = 0; c < kChunks; ++c) tma_load_3d(y2 + s2 * kTile + c * kChunkBytes, kKeys ? &tm_dy : &tm_v, 64 * c, h, row, y2_full + 8 * s2);
       }
+      __syncwarp();
     }
   } else if (warp == 9) {
-    if (lane == 0) {
-      const int k_steps = (a.r.width + 15) / 16;
-      const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_acc = idesc_bf16(128, 16 * k_steps, true);
-      auto product = [&](uint32_t d, uint32_t x, uint32_t y) { product_over_head<kChunks>(tmem + d, x, y, k_steps, idesc_s); };
-      auto accumulate = [&](uint32_t d, uint32_t p, uint32_t y, bool more) { product_over_rows<64>(tmem + d, tmem + p, y, idesc_acc, more); };
-      auto dp_at = [&](int i) { return kDp + (kKeys ? 0 : 128 * (i & 1)); };
-      auto issue_s = [&](int i) {
-        if (!wait(y1_full + 8 * (i % kSt1), (i / kSt1) & 1)) return false;
-        fence_after();
-        product(kS, x1, y1 + (i % kSt1) * kTile);
+    const int k_steps = (a.r.width + 15) / 16;
+    const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_acc = idesc_bf16(128, 16 * k_steps, true);
+    auto commit = [&](uint32_t bar) { if (elected()) umma_commit(bar); __syncwarp(); };
+    auto dp_at = [&](int i) { return kDp + (kKeys ? 0 : 128 * (i & 1)); };
+    auto issue_s = [&](int i) {
+      if (!wait_warp(y1_full + 8 * (i % kSt1), (i / kSt1) & 1)) return false;
+      fence_after();
+      if (elected()) {
+        product_over_head<kChunks>(tmem + kS, x1, y1 + (i % kSt1) * kTile, k_steps, idesc_s);
         umma_commit(s_full);
-        return true;
-      };
-      auto issue_dp = [&](int i) {
-        if (!wait(y2_full + 8 * (i % kSt2), (i / kSt2) & 1)) return false;
-        fence_after();
-        product(dp_at(i), x2, y2 + (i % kSt2) * kTile);
+      }
+      __syncwarp();
+      return true;
+    };
+    auto issue_dp = [&](int i) {
+      if (!wait_warp(y2_full + 8 * (i % kSt2), (i / kSt2) & 1)) return false;
+      fence_after();
+      if (elected()) {
+        product_over_head<kChunks>(tmem + dp_at(i), x2, y2 + (i % kSt2) * kTile, k_steps, idesc_s);
         umma_commit(dp_full + (kKeys ? 0 : 8 * (i & 1)));
         if (!kKeys) umma_commit(y2_empty + 8 * (i % kSt2));
-        return true;
-      };
-      bool ok = wait(x_full, 0) && issue_s(0) && issue_dp(0);
-      for (int i = 0; i < n && ok; ++i) {
-        const int s = i % kSt1, s2 = i % kSt2;
-        if (kKeys) {
-          if (!(ok = wait(p_full, i & 1))) break;
-          fence_after();
-          accumulate(kAcc2, kS, y2 + s2 * kTile, i > 0);
-          umma_commit(y2_empty + 8 * s2);
-          if (i + 1 < n && !(ok = issue_s(i + 1))) break;
-          if (!(ok = wait(ds_full, i & 1))) break;
-          fence_after();
-          accumulate(kAcc1, kDp, y1 + s * kTile, i > 0);
-          umma_commit(y1_empty + 8 * s);
-          if (i + 1 < n && !(ok = issue_dp(i + 1))) break;
-        } else {
-          if (i + 1 < n) {
-            if (!(ok = wait(p_full, i & 1))) break;      // S has been read
-            fence_after();
-            if (!(ok = issue_s(i + 1) && issue_dp(i + 1))) break;
-          }
-          if (!(ok = wait(ds_full, i & 1))) break;
-          fence_after();
-          accumulate(kAcc1, dp_at(i), y1 + s * kTile, i > 0);
-          umma_commit(y1_empty + 8 * s);
-        }
       }
-      if (ok) umma_commit(acc_full);
-      if (*abort_flag) { umma_commit(drain); mbar_wait(drain, 0, abort_flag + 1); }
+      __syncwarp();
+      return true;
+    };
+    auto accumulate = [&](uint32_t d, uint32_t p, uint32_t y, bool more, uint32_t empty) {
+      fence_after();
+      if (elected()) {
+        product_over_rows<64>(tmem + d, tmem + p, y, idesc_acc, more);
+        umma_commit(empty);
+      }
+      __syncwarp();
+    };
+    bool ok = wait_warp(x_full, 0) && issue_s(0) && issue_dp(0);
+    for (int i = 0; i < n && ok; ++i) {
+      const int s = i % kSt1, s2 = i % kSt2;
+      if (kKeys) {
+        if (!(ok = wait_warp(p_full, i & 1))) break;
+        accumulate(kAcc2, kS, y2 + s2 * kTile, i > 0, y2_empty + 8 * s2);
+        if (i + 1 < n && !(ok = issue_s(i + 1))) break;
+        if (!(ok = wait_warp(ds_full, i & 1))) break;
+        accumulate(kAcc1, kDp, y1 + s * kTile, i > 0, y1_empty + 8 * s);
+        if (i + 1 < n && !(ok = issue_dp(i + 1))) break;
+      } else {
+        if (i + 1 < n) {
+          if (!(ok = wait_warp(p_full, i & 1))) break;      // S has been read
+          fence_after();
+          if (!(ok = issue_s(i + 1) && issue_dp(i + 1))) break;
+        }
+        if (!(ok = wait_warp(ds_full, i & 1))) break;
+        accumulate(kAcc1, dp_at(i), y1 + s * kTile, i > 0, y1_empty + 8 * s);
+      }
     }
-    __syncwarp();
+    if (ok) commit(acc_full);
   } else {
     const int e = (warp & 3) * 32 + lane, half = warp >> 2, row = u.row0 + e;      // own row of the sequence (a key, or a query)
     const bool mine = row < n_rows;
@@ -236,20 +243,20 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         lo = a.r.window ? row - a.r.window + 1 - c0 : 0;
       }
       const float4* st = reinterpret_cast<const float4*>(stats + (i % kSt1) * 256 + 64 * half);
-      ok = __all_sync(0xffffffffu, wait(s_full, i & 1));
-      if (ok && kKeys) ok = __all_sync(0xffffffffu, wait(st_full + 8 * (i % kSt1), (i / kSt1) & 1));
+      ok = wait_warp(s_full, i & 1);
+      if (ok && kKeys) ok = wait_warp(st_full + 8 * (i % kSt1), (i / kSt1) & 1);
       if (!ok) break;
       fence_after();
       uint32_t v[64];
       float p[64];
-      tmem_ld32(tmem + lanes + kS + 64 * half, v);
-      tmem_ld32(tmem + lanes + kS + 64 * half + 32, v + 32);
+      tmem_load32(tmem + lanes + kS + 64 * half, v);
+      tmem_load32(tmem + lanes + kS + 64 * half + 32, v + 32);
       tmem_loaded32(v);
       tmem_loaded32(v + 32);
       if (!kKeys) {
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full);
+        mbar_arrive_if(p_full, lane == 0);
       }
 #pragma unroll
       for (int c = 0; c < 64; c += 4) {
@@ -269,14 +276,14 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         tmem_st_wait();
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full);
+        mbar_arrive_if(p_full, lane == 0);
       }
       const uint32_t dp = tmem + lanes + kDp + (kKeys ? 0 : 128 * (i & 1)) + 64 * half;
-      ok = __all_sync(0xffffffffu, wait(dp_full + (kKeys ? 0 : 8 * (i & 1)), (kKeys ? i : i >> 1) & 1));
+      ok = wait_warp(dp_full + (kKeys ? 0 : 8 * (i & 1)), (kKeys ? i : i >> 1) & 1);
       if (!ok) break;
       fence_after();
-      tmem_ld32(dp, v);
-      tmem_ld32(dp + 32, v + 32);
+      tmem_load32(dp, v);
+      tmem_load32(dp + 32, v + 32);
       tmem_loaded32(v);
       tmem_loaded32(v + 32);
 #pragma unroll
@@ -292,13 +299,11 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       tmem_st_wait();
       fence_before();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(ds_full);
-        if (kKeys) mbar_arrive(st_empty + 8 * (i % kSt1));
-      }
+      mbar_arrive_if(ds_full, lane == 0);
+      if (kKeys) mbar_arrive_if(st_empty + 8 * (i % kSt1), lane == 0);
     }
     if (ok) {
-      ok = __all_sync(0xffffffffu, wait(acc_full, 0));
+      ok = wait_warp(acc_full, 0);
       fence_after();
     }
     bool fine = true;
@@ -329,6 +334,7 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     // rows that are not finite: again, after both halves have been written (every warp comes here, after an unwind too)
     const unsigned bad = __ballot_sync(0xffffffffu, mine && !fine);
     if (lane == 0) again[warp] = bad;
+    __syncwarp();
     asm volatile("bar.sync 1, 256;" ::: "memory");
     if (half == 0)
       for (unsigned b = again[warp] | again[warp + 4]; b; b &= b - 1) {
@@ -339,7 +345,12 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   }
   fence_before();
   __syncthreads();
-  if (*abort_flag) {      // an unwind: what the producer has handed to the TMA engine lands before the shared memory goes away
+  if (*abort_flag) {      // an unwind: copies and products that have been asked for end before their memory goes away
+    if (warp == 9) {
+      if (elected()) umma_commit(drain);
+      __syncwarp();
+      mbar_wait_warp(drain, 0, abort_flag + 1, kWaitBudgetCycles);
+    }
     if (threadIdx.x == 256) {
       mbar_wait(x_full, 0, abort_flag + 1);
       for (int k = std::max(a.drop_first_load ? 1 : 0, issued1 - kSt1); k < issued1; ++k) mbar_wait(y1_full + 8 * (k % kSt1), (k / kSt1) & 1, abort_flag + 1);
@@ -347,6 +358,7 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     __syncthreads();
   }
+  __syncwarp();
   if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 

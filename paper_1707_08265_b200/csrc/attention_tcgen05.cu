@@ -113,6 +113,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const bool ragged = u.keys - (j0 + n_tiles - 1) * 128 < 128;      // the last tile has rows behind the sequence's last key
 
   if (warp == 9) {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -120,15 +121,15 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  auto wait = [&](uint32_t bar, uint32_t parity) {
-    if (mbar_wait(bar, parity, abort_flag, a.budget)) return true;
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) {
+    if (mbar_wait_warp(bar, parity, abort_flag, a.budget)) return true;
     *abort_flag = 1;
     report(a.r.status, DRAGON_ERR_TIMEOUT);
     return false;
   };
   int issued_k = 0, issued_v = 0;
   if (warp == 8) {
-    if (lane == 0 && n_tiles > 0) {
+    if (n_tiles > 0 && elected()) {
       for (int t = 0; t < 2; ++t) {
         mbar_expect_tx(q_full + 8 * t, kTile);
         for (int c = 0; c < kChunks; ++c)
@@ -142,24 +143,29 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       for (int which = 0; which < 2; ++which) {
         const CUtensorMap* tm = which ? &tm_v : &tm_k;
         const uint32_t full = (which ? v_full : k_full) + 8 * s, dst = (which ? v_at : k_at) + s * kTile;
-        ok = __all_sync(0xffffffffu, wait((which ? v_empty : k_empty) + 8 * s, (turn & 1) ^ 1));
+        ok = wait_warp((which ? v_empty : k_empty) + 8 * s, (turn & 1) ^ 1);
         if (!ok) break;
         if (which) issued_v = j + 1; else issued_k = j + 1;
         if (a.drop_first_load && j == 0 && !which) continue;      // failure-detection test: this stage's signal never comes
-        if (lane == 0) mbar_expect_tx(full, kTile);
-        __syncwarp();
         if (!kPaged) {
-          if (lane < kChunks) tma_load_3d(dst + lane * kChunkBytes, tm, 64 * lane, kvh, u.a + (j0 + j) * 128, full);
+          if (elected()) {
+            mbar_expect_tx(full, kTile);
+            for (int c = 0; c < kChunks; ++c) tma_load_3d(dst + c * kChunkBytes, tm, 64 * c, kvh, u.a + (j0 + j) * 128, full);
+          }
+          __syncwarp();
         } else {
           const int page = 1 << a.r.pages.shift, box = min(page, 128), at = (j0 + j) * 128 + lane * box;
-          if (lane < 128 / box) {
-            int row = a.r.pages.pool << a.r.pages.shift;          // behind the cache: zeros
-            if (at < u.keys) {
-              const int number = a.r.pages.page_of(u.seq, at);
-              if (a.r.pages.in_pool(number)) row = (number << a.r.pages.shift) + (at & (page - 1));
-              else report(a.r.status, DRAGON_ERR_INVALID_ARG);
+          const bool mine = lane < 128 / box, there = mine && at < u.keys;
+          const int number = there ? a.r.pages.page_of(u.seq, at) : -1, none = a.r.pages.pool << a.r.pages.shift;      // behind the cache: zeros
+          const int row = a.r.pages.in_pool(number) ? (number << a.r.pages.shift) + (at & (page - 1)) : none;
+          if (__any_sync(0xffffffffu, there && row == none)) report(a.r.status, DRAGON_ERR_INVALID_ARG);
+          for (int p = 0; p < 128 / box; ++p) {      // (each lane has looked up a page; one lane issues all copies)
+            const int from = __shfl_sync(0xffffffffu, row, p);
+            if (elected()) {
+              if (p == 0) mbar_expect_tx(full, kTile);
+              for (int c = 0; c < kChunks; ++c) tma_load_3d(dst + c * kChunkBytes + p * box * 128, tm, 64 * c, kvh, from, full);
             }
-            for (int c = 0; c < kChunks; ++c) tma_load_3d(dst + c * kChunkBytes + lane * box * 128, tm, 64 * c, kvh, row, full);
+            __syncwarp();
           }
         }
       }
@@ -167,7 +173,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     if (ok && ragged && n_tiles > 0) {
       // what stands behind the sequence's last key (other sequences, a page's unused rows) is not to meet a probability of 0
       const int j = n_tiles - 1, keep = u.keys - (j0 + j) * 128;
-      if (__all_sync(0xffffffffu, wait(v_full + 8 * (j % kSt), (j / kSt) & 1))) {
+      if (wait_warp(v_full + 8 * (j % kSt), (j / kSt) & 1)) {
         unsigned char* tile = smem_raw + (v_at - raw) + (j % kSt) * kTile;
         for (int c = 0; c < kChunks; ++c)
           for (int i = lane; i < (128 - keep) * 8; i += 32) *reinterpret_cast<uint4*>(tile + c * kChunkBytes + keep * 128 + 16 * i) = make_uint4(0, 0, 0, 0);
@@ -176,46 +182,50 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
       }
     }
   } else if (warp == 9) {
-    if (lane == 0 && n_tiles > 0) {
+    if (n_tiles > 0) {
       const int k_steps = (a.r.width + 15) / 16, n_out = 16 * k_steps;
       const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_o = idesc_bf16(128, n_out, true);
+      auto commit = [&](uint32_t bar) { if (elected()) umma_commit(bar); __syncwarp(); };
       auto product_s = [&](int t, int j) {
-        product_over_head<kChunks>(tmem + 128 * t, q_at + t * kTile, k_at + (j % kSt) * kTile, k_steps, idesc_s);
-        umma_commit(s_full + 8 * t);
-      };
-      bool ok = wait(k_full, 0);
-      for (int t = 0; t < 2 && ok; ++t) {
-        ok = wait(q_full + 8 * t, 0);
         fence_after();
+        if (elected()) {
+          product_over_head<kChunks>(tmem + 128 * t, q_at + t * kTile, k_at + (j % kSt) * kTile, k_steps, idesc_s);
+          umma_commit(s_full + 8 * t);
+        }
+        __syncwarp();
+      };
+      bool ok = wait_warp(k_full, 0);
+      for (int t = 0; t < 2 && ok; ++t) {
+        ok = wait_warp(q_full + 8 * t, 0);
         if (ok) product_s(t, 0);
       }
-      if (ok) umma_commit(k_empty);
+      if (ok) commit(k_empty);
       for (int j = 0; j < n_tiles && ok; ++j) {
         const int s = j % kSt;
-        ok = wait(v_full + 8 * s, (j / kSt) & 1);
-        if (ok && ragged && j == n_tiles - 1) ok = wait(v_clean, 0);
+        ok = wait_warp(v_full + 8 * s, (j / kSt) & 1);
+        if (ok && ragged && j == n_tiles - 1) ok = wait_warp(v_clean, 0);
         for (int t = 0; t < 2 && ok; ++t) {
-          if (!(ok = wait(p_full + 16 * t, j & 1))) break;
+          if (!(ok = wait_warp(p_full + 16 * t, j & 1))) break;
           fence_after();
-          product_over_rows<32, 0, 4>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, j > 0);
-          if (!(ok = wait(p_full + 16 * t + 8, j & 1))) break;
+          if (elected()) product_over_rows<32, 0, 4>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, j > 0);
+          __syncwarp();
+          if (!(ok = wait_warp(p_full + 16 * t + 8, j & 1))) break;
           fence_after();
-          product_over_rows<32, 4, 8>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, true);
+          if (elected()) product_over_rows<32, 4, 8>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, true);
+          __syncwarp();
           if (j + 1 < n_tiles) {
-            if (t == 0) { if (!(ok = wait(k_full + 8 * ((j + 1) % kSt), ((j + 1) / kSt) & 1))) break; fence_after(); }
+            if (t == 0 && !(ok = wait_warp(k_full + 8 * ((j + 1) % kSt), ((j + 1) / kSt) & 1))) break;
             product_s(t, j + 1);
           } else {
-            umma_commit(o_full + 8 * t);
+            commit(o_full + 8 * t);
           }
         }
         if (ok) {
-          umma_commit(v_empty + 8 * s);
-          if (j + 1 < n_tiles) umma_commit(k_empty + 8 * ((j + 1) % kSt));
+          commit(v_empty + 8 * s);
+          if (j + 1 < n_tiles) commit(k_empty + 8 * ((j + 1) % kSt));
         }
       }
-      if (*abort_flag) { umma_commit(drain); mbar_wait(drain, 0, abort_flag + 1); }
     }
-    __syncwarp();
   } else {
     const int t = warp >> 2, e = (warp & 3) * 32 + lane;
     const int head = a.by_heads ? head0 + t : head0 + (e & (pack - 1));
@@ -228,12 +238,12 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     float top = -kInf, sum = 0.f;
     bool ok = true;
     for (int j = 0; j < n_tiles; ++j) {
-      ok = __all_sync(0xffffffffu, wait(s_full + 8 * t, j & 1));
+      ok = wait_warp(s_full + 8 * t, j & 1);
       if (!ok) break;
       fence_after();
       uint32_t s[128];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
+      for (int c = 0; c < 4; ++c) tmem_load32(s_at + 32 * c, s + 32 * c);
 #pragma unroll
       for (int c = 0; c < 4; ++c) tmem_loaded32(s + 32 * c);
       const int k0 = (j0 + j) * 128;
@@ -285,13 +295,13 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         tmem_st_wait();
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 16 * t + 8 * c);
+        mbar_arrive_if(p_full + 16 * t + 8 * c, lane == 0);
       }
       const float2 more = both(add_pair(part[0], part[1]));
       sum += more.x + more.y;
     }
     if (ok && n_tiles > 0) {
-      ok = __all_sync(0xffffffffu, wait(o_full + 8 * t, 0));
+      ok = wait_warp(o_full + 8 * t, 0);
       fence_after();
     }
     if (ok) {
@@ -332,7 +342,12 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   }
   fence_before();
   __syncthreads();
-  if (*abort_flag) {      // an unwind: what the producer has handed to the TMA engine lands before the shared memory goes away
+  if (*abort_flag) {      // an unwind: copies and products that have been asked for end before their memory goes away
+    if (warp == 9) {
+      if (elected()) umma_commit(drain);
+      __syncwarp();
+      mbar_wait_warp(drain, 0, abort_flag + 1, kWaitBudgetCycles);
+    }
     if (threadIdx.x == 256) {
       for (int t = 0; t < 2 && n_tiles > 0; ++t) mbar_wait(q_full + 8 * t, 0, abort_flag + 1);
       for (int k = std::max(a.drop_first_load ? 1 : 0, issued_k - kSt); k < issued_k; ++k) mbar_wait(k_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
@@ -340,6 +355,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     __syncthreads();
   }
+  __syncwarp();
   if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
