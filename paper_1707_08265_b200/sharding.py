@@ -40,15 +40,15 @@ def _refuse_mixed_rows(desc, extent):
     for op in desc["ops"]:
         cut = [_has_extent(desc, t, extent) for t in op["in"]]
         result = any(_has_extent(desc, t, extent) for t in op["out"])
-        if op["type"] == "RMSNorm":
+        if op["type"] in ("RMSNorm", "HeadNorm"):
             ok = len(desc["tensors"][op["in"][0]]["shape"]) == 2 and not cut[1] if any(cut) else True
         elif op["type"] == "BlockScale":
             ok = cut[0] == result and not (cut[0] and op.get("attrs", [1])[0] != 1)
-        elif op["type"] == "Quantize":
+        elif op["type"] in ("Quantize", "Rotate"):
             ok = cut[0] == cut[1]
         elif op["type"] == "ScaledInnerProduct":
             ok = cut[0] == cut[1] and not cut[2] and not cut[3]
-        elif op["type"] in ("GlobalNorm", "GatedScan"):
+        elif op["type"] in ("GlobalNorm", "GatedScan", "Attention", "CacheWrite", "PagedAttention"):
             ok = not any(cut)
         elif op["type"] == "ClipByNorm":
             ok = True

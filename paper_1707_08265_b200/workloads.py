@@ -17,6 +17,9 @@ Workloads (sizes are arguments so that tests can shrink them):
                       SoftmaxCrossEntropy, with gradients for every weight (a language model's layer and its loss)
   recurrent_step      the same layer one row per sequence with its weights in e4m3 (RMSNorm with 8-bit output,
                       ScaledInnerProduct, GatedScan from fed states): a decoding step
+  attention_layer     RMSNorm / InnerProduct / HeadNorm / Rotate / Attention / InnerProduct with a residual stream, RMSNorm,
+                      InnerProduct, SoftmaxCrossEntropy, with gradients for every weight
+  attention_step      the same layer over a paged cache (CacheWrite, PagedAttention): single tokens, or chunks of new ones
   clipped_updater     W' = W - lr * clipped gradient for several weights under one global norm
 """
 import numpy as np
@@ -292,6 +295,70 @@ def recurrent_step(seqs, width, inner):
     ids["new_states"] = g.op("GatedScan", [f, x, ids["states"]], "new_states", [seqs, inner], attrs=[seqs])
     o = product(ids["new_states"], "h")("Wo", "o", "f32")
     ids["r2"] = g.op("Add", [ids["r"], o], "r2", [seqs, width], "bf16")
+    return g, ids
+
+
+def _queries_keys_values(g, ids, rows, width, heads, kv_heads, head_width, interleaved):
+    """y = RMSNorm(r; g1) and its products; queries and keys normalised head by head and turned by their positions."""
+    ids["r"] = g.tensor("r", [rows, width], "bf16")
+    for n, heads_of in (("Wq", heads), ("Wk", kv_heads), ("Wv", kv_heads)):
+        ids[n] = g.tensor(n, [heads_of * head_width, width], "bf16")
+    ids["Wo"] = g.tensor("Wo", [width, heads * head_width], "bf16")
+    ids["g1"], ids["gq"], ids["gk"] = g.tensor("gain1", [width]), g.tensor("gain_q", [head_width]), g.tensor("gain_k", [head_width])
+    ids["pos"] = g.tensor("pos", [rows], "i32")
+    y = g.op("RMSNorm", [ids["r"], ids["g1"]], "y", [rows, width], "bf16")
+    q, k, v = (g.op("InnerProduct", [y, ids["W" + n]], n, [rows, g.shape(ids["W" + n])[0]], "bf16") for n in "qkv")
+
+    def turned(x, gain, name, count):
+        u = g.op("HeadNorm", [x, gain], name + "_normed", g.shape(x))
+        return g.op("Rotate", [u, ids["pos"]], name + "_turned", g.shape(x), "bf16", attrs=[count, head_width, interleaved])
+
+    return turned(q, ids["gq"], "q", heads), turned(k, ids["gk"], "k", kv_heads), v
+
+
+def attention_layer(rows, width, heads, kv_heads, head_width, vocab, sequences=1, starts=0, window=0, interleaved=0):
+    """One layer over ``rows`` rows, those of ``sequences`` equally long sequences or (starts) of that many packed ones, and the loss:
+      y = RMSNorm(r; g1),  q, k, v = y Wq^T, y Wk^T, y Wv^T,  a = Attention(Rotate(HeadNorm(q)), Rotate(HeadNorm(k)), v),
+      r2 = r + a Wo^T,  z = RMSNorm(r2; g2) We^T,  loss(z, labels)
+    r: the residual stream, bf16 [rows, width]; pos: every row's position.  Returns (graph, ids); ids["grads"]: gradients of ids["weights"]."""
+    g, ids = GraphDesc(), {}
+    q, k, v = _queries_keys_values(g, ids, rows, width, heads, kv_heads, head_width, interleaved)
+    ids["We"], ids["g2"], ids["labels"] = g.tensor("We", [vocab, width], "bf16"), g.tensor("gain2", [width]), g.tensor("labels", [rows], "i32")
+    ins = [q, k, v]
+    if starts:
+        ids["starts"] = g.tensor("starts", [starts + 1], "i32")
+        ins.append(ids["starts"])
+    a = g.op("Attention", ins, "a", [rows, heads * head_width], "bf16", attrs=[heads, kv_heads, 1, window, 0.0, sequences])
+    o = g.op("InnerProduct", [a, ids["Wo"]], "o", [rows, width])
+    ids["r2"] = g.op("Add", [o, ids["r"]], "r2", [rows, width], "bf16")
+    y2 = g.op("RMSNorm", [ids["r2"], ids["g2"]], "y2", [rows, width], "bf16")
+    z = g.op("InnerProduct", [y2, ids["We"]], "z", [rows, vocab])
+    ids["loss"] = g.op("SoftmaxCrossEntropy", [z, ids["labels"]], "loss", [])
+    ids["weights"] = [ids[n] for n in ("Wq", "Wk", "Wv", "Wo", "We", "g1", "gq", "gk", "g2")]
+    ids["grads"] = g.grad([ids["loss"]], ids["weights"])
+    return g, ids
+
+
+def attention_step(rows, sequences, width, heads, kv_heads, head_width, page, most_pages, pool, window=0, interleaved=0):
+    """The layer for ``rows`` new tokens of ``sequences`` sequences (one each, or those that starts gives) over a cache of ``pool``
+    pages of ``page`` rows: the new keys and values go into the cache (ids["new_keys"], ids["new_values"]: fetched into the memory
+    of keys and values they are written in place), the queries meet all that stands in it.  lengths counts the new tokens."""
+    g, ids = GraphDesc(), {}
+    cols = kv_heads * head_width
+    q, k, v = _queries_keys_values(g, ids, rows, width, heads, kv_heads, head_width, interleaved)
+    for n in ("keys", "values"):
+        ids[n] = g.tensor(n, [pool * page, cols], "bf16")
+    ids["pages"], ids["lengths"] = g.tensor("pages", [sequences, most_pages], "i32"), g.tensor("lengths", [sequences], "i32")
+    table = [ids["pages"], ids["lengths"]]
+    if rows != sequences:
+        ids["starts"] = g.tensor("starts", [sequences + 1], "i32")
+        table.append(ids["starts"])
+    for n, new in (("keys", k), ("values", v)):
+        ids["new_" + n] = g.op("CacheWrite", [ids[n], new] + table, "new_" + n, [pool * page, cols], "bf16", attrs=[page])
+    a = g.op("PagedAttention", [q, ids["new_keys"], ids["new_values"]] + table, "a", [rows, heads * head_width], "bf16",
+             attrs=[heads, kv_heads, page, window, 0.0])
+    o = g.op("InnerProduct", [a, ids["Wo"]], "o", [rows, width])
+    ids["r2"] = g.op("Add", [o, ids["r"]], "r2", [rows, width], "bf16")
     return g, ids
 
 
