@@ -37,6 +37,7 @@ int launch_attention(const StepRun& r) {
   RowArgs a = row_args(r);
   a.out = r.wr(at::Y); a.ot = r.wr_type(at::Y);
   a.lse = reinterpret_cast<float*>(r.wr(at::LSE));
+  if (r.s.wr.size() > at::REST) a.rest = reinterpret_cast<unsigned short*>(r.wr(at::REST));
   return launch_attention_forward(a, false, a.seq.rows, 0, reinterpret_cast<cudaStream_t>(r.stream), "Attention");
 }
 
@@ -44,6 +45,7 @@ int launch_attention_bwd(const StepRun& r) {
   RowArgs a = row_args(r);
   a.y = r.rd(at::Y_IN); a.yt = r.rd_type(at::Y_IN);
   a.lse = reinterpret_cast<float*>(r.rd(at::LSE_IN));
+  a.rest = reinterpret_cast<unsigned short*>(r.rd(at::REST_IN));
   a.dy = reinterpret_cast<const unsigned short*>(r.rd(at::DY));
   a.out = r.wr(at::DQ); a.ot = r.wr_type(at::DQ);
   a.dk = r.wr(at::DK); a.dkt = r.wr_type(at::DK);

@@ -17,6 +17,7 @@ struct RowArgs {
   const void* y;            // backwards: the forward result
   void* out;                // y, or dq
   void *dk, *dv;
+  unsigned short* rest;     // what y's rounding to bf16 left out (nullptr: not wanted)
   float* lse;
   float* delta;
   int yt, ot, dkt, dvt;
@@ -41,6 +42,9 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int s = 16; s; s >>= 1) v += __shfl_xor_sync(0xffffffffu, v, s);
   return v;
 }
+
+// what rounding to bf16 leaves out of v
+__device__ __forceinline__ float behind_bf16(float v) { return v - __bfloat162float(__float2bfloat16_rn(v)); }
 
 // first and last + 1 of the keys that the row at position i of its sequence (of n rows) sees
 __device__ __forceinline__ void seen_by(const RowArgs& a, int i, int n, int* first, int* last) {
@@ -95,6 +99,8 @@ template <bool kPaged> __device__ __noinline__ void attend_row(const RowArgs& a,
   const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a NaN stays one)
 #pragma unroll
   for (int e = 0; e < 4; ++e) if (a.out && lane + 32 * e < a.width) put(a.out, a.ot, base + lane + 32 * e, acc[e] * inv);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) if (a.rest && lane + 32 * e < a.width) put(a.rest, DRAGON_BF16, base + lane + 32 * e, behind_bf16(acc[e] * inv));
   if (a.lse && lane == 0) a.lse[(size_t)h * a.seq.rows + row] = sum == 0.f ? kInf : top + log2f(sum);
 }
 

@@ -329,6 +329,12 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
           store_any<8>(a.r.out, a.r.ot, at + c, v);
           if (c + 8 < a.r.width) store_any<8>(a.r.out, a.r.ot, at + c + 8, v + 8);
         }
+        if (!kPaged && mine && a.r.rest) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = behind_bf16(v[k]);
+          store_any<8>(a.r.rest, DRAGON_BF16, at + c, v);
+          if (c + 8 < a.r.width) store_any<8>(a.r.rest, DRAGON_BF16, at + c + 8, v + 8);
+        }
       }
       if (kPaged && a.r.splits > 1) {      // (where the parts are put together a row that is not finite is computed again)
         if (mine) a.r.part_lse[((size_t)blockIdx.y * a.r.seq.rows + row) * a.r.heads + head] = sum == 0.f ? -kInf : top * a.r.scale + log2f(sum);

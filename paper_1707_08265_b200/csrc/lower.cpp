@@ -666,11 +666,16 @@ struct Lowerer {
         break;
       }
       case DRAGON_OP_ATTENTION: {
+        // what a bf16 result's rounding left out goes along: delta = sum(dy y) is subtracted from values that are close to it
+        if (g.tensors[o].dtype == DRAGON_BF16 && items[attn_item[r.op]].wr.size() == at::REST) {
+          const int mRest = new_mem(MEM_WORK, -1, DRAGON_BF16, g.tensors[o].shape);
+          items[attn_item[r.op]].wr.push_back(mRest);
+        }
         const Item fwd = items[attn_item[r.op]];
         const int mdY = materialise(dy, DRAGON_BF16, DRAGON_BF16);
         int md[3];
         for (int p = 0; p < 3; ++p) md[p] = want[p] ? grad_mem(s, op.in[p]) : -1;
-        const int i = add_item(IT_ATTN_BWD, {fwd.rd[at::Q], fwd.rd[at::K], fwd.rd[at::V], fwd.rd[at::STARTS], fwd.wr[at::Y], fwd.wr[at::LSE], mdY}, {md[0], md[1], md[2]}, 0.0);
+        const int i = add_item(IT_ATTN_BWD, {fwd.rd[at::Q], fwd.rd[at::K], fwd.rd[at::V], fwd.rd[at::STARTS], fwd.wr[at::Y], fwd.wr[at::LSE], mdY, fwd.wr.size() > at::REST ? fwd.wr[at::REST] : -1}, {md[0], md[1], md[2]}, 0.0);
         items[i].num = op.num;
         for (int p = 0; p < 3; ++p)
           if (want[p]) add(p, new_val(VK_MEM, g.tensors[op.in[p]].shape, md[p]));

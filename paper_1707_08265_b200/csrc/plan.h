@@ -89,8 +89,9 @@ namespace sc { enum { GATE, X, H0, RESET, DH, CARRY_IN }; enum { H, CARRY }; enu
 namespace hd { enum { X, GAIN, POS, READS }; enum { U, Y, WRITES }; }      // (a step may hold several: READS operands and WRITES results each)
 namespace hb { enum { X, GAIN, POS, DY, READS }; enum { DX, DGAIN, WRITES }; }
 namespace hn { enum { EPS, WIDTH, DIMS, INTERLEAVED, BASE, FACTOR, LOW, HIGH, ORIGINAL, AMPLITUDE, COUNT }; }
-// IT_ATTN, IT_ATTN_BWD: lse [heads, T] is log2 of every row's sum of exponentials (scaled), +inf for a row that sees nothing
-namespace at { enum { Q, K, V, STARTS, Y_IN, LSE_IN, DY }; enum { Y, LSE }; enum { DQ, DK, DV }; }
+// IT_ATTN, IT_ATTN_BWD: lse [heads, T] is log2 of every row's sum of exponentials (scaled), +inf for a row that sees nothing;
+// rest (where y is bf16 and a gradient is computed): what y's rounding left out, bf16
+namespace at { enum { Q, K, V, STARTS, Y_IN, LSE_IN, DY, REST_IN }; enum { Y, LSE, REST }; enum { DQ, DK, DV }; }
 namespace an { enum { HEADS, KV_HEADS, CAUSAL, WINDOW, SCALE, SEQUENCES }; }
 namespace cw { enum { PAGES, LENGTHS, STARTS, CACHE, ROWS }; }                    // IT_CACHE_WRITE: rd = table, then cache and rows of each; wr = the new caches
 namespace pa { enum { Q, K, V, PAGES, LENGTHS, STARTS }; enum { Y }; }            // IT_PAGED
