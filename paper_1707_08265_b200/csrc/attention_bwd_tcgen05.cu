@@ -4,8 +4,8 @@
 //   p = exp2(scale' q k^T - lse), dp = dy v^T, ds = p (dp - delta), delta = sum(dy y) of a row
 //   dv = p^T dy, dk = scale ds^T q (over the query heads that share the key head), dq = scale ds k
 //
-// Two kernels, so that every sum has one owner and its order is fixed (no atomics); q k^T and dy v^T are computed in both (7 products
-// of a tile where one pass needs 5):
+// Two kinds of CTA, so that every sum has one owner and its order is fixed (no atomics); q k^T and dy v^T are computed by both (7
+// products of a tile where one pass needs 5):
 //   keys:  a CTA has 128 keys of a key head and meets every tile of queries that sees them, of every head of the group.  It
 //          computes S^T = K Q^T and dP^T = V dY^T, so that P^T and dS^T lie in TMEM as the A operands of dV += P^T dY and
 //          dK += dS^T Q (dY and Q as they lie in memory, MN-major).
@@ -13,6 +13,7 @@
 // One tile pair is 128 x 128; two warps share a row (64 columns each).  The products are issued in an order in which the tensor
 // unit has work while the threads compute: keys: dV(i), S(i+1), dK(i), dP(i+1); rows: S(i+1), dP(i+1), dQ(i) (dP has two buffers).
 // Warps: 0..7 mathematics, 8 TMA, 9 MMA.  Every wait is bounded.
+// Both kinds are one launch, keys first: theirs are the longest (all heads of a group), and the rows' fill the SMs that run out of them.
 #include <algorithm>
 
 #include "attention_rows.h"
@@ -33,14 +34,13 @@ constexpr size_t bwd_smem(bool keys, int chunks) {
 struct BwdArgs {
   RowArgs r;
   int blocks, each_blocks;
+  int key_ctas;             // the first CTAs have keys, the others rows
   long long budget;
   int drop_first_load;
 };
 
 template <bool kKeys, int kChunks>
-__global__ void __launch_bounds__(kBwdThreads, 1)
-attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-              const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ BwdArgs a) {
+__device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CUtensorMap& tm_dy, const BwdArgs& a, int cta) {
   constexpr int kSt1 = bwd_stages1(kKeys, kChunks), kSt2 = bwd_stages2(kChunks);
   constexpr uint32_t kTile = kChunks * kChunkBytes;
   // columns of TMEM
@@ -58,7 +58,7 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   __shared__ Unit unit;
   __shared__ unsigned again[8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.r.heads / a.r.kv_heads;
-  const int n_heads = kKeys ? a.r.kv_heads : a.r.heads, head = blockIdx.x % n_heads;
+  const int n_heads = kKeys ? a.r.kv_heads : a.r.heads, head = cta % n_heads;
 
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
@@ -74,12 +74,13 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   }
   if (warp == 0) {
     Unit u;
-    find_unit(a.r.seq, a.blocks, a.each_blocks, blockIdx.x / n_heads, 128, &u, lane);
+    find_unit(a.r.seq, a.blocks, a.each_blocks, cta / n_heads, 128, &u, lane);
     if (u.seq >= 0 && kKeys && a.r.causal) u.row0 = (u.b - u.a - 1) / 128 * 128 - u.row0;      // the first keys are seen by most rows
     if (lane == 0) unit = u;
   }
   __syncthreads();
   const Unit u = unit;
+  after_the_launch_before();
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares)
@@ -362,9 +363,19 @@ attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
+template <int kChunks>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attention_bwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+              const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ BwdArgs a) {
+  if ((int)blockIdx.x < a.key_ctas) bwd_cta<true, kChunks>(tm_q, tm_k, tm_v, tm_dy, a, blockIdx.x);
+  else bwd_cta<false, kChunks>(tm_q, tm_k, tm_v, tm_dy, a, blockIdx.x - a.key_ctas);
+}
+
 // delta = sum(dy y) of every row and head, y with what its rounding left out: in a row that sees few keys dp - delta is small, and
 // with the rounded y alone dq and dk of short sequences were off by 0.0030 of their norm, not 0.0024.  A head in the next power of two of lanes, 8 elements a lane
 __global__ void __launch_bounds__(256) attention_delta(const __grid_constant__ RowArgs a, int lanes) {
+  next_launch_may_come();
+  after_the_launch_before();
   if (blockIdx.x == 0 && threadIdx.x == 0 && a.status_clear) *a.status_clear = 0;
   const int lane = threadIdx.x & 31, l = lane & (lanes - 1);
   const long long i = ((long long)blockIdx.x * 8 + (threadIdx.x >> 5)) * (32 / lanes) + lane / lanes, n = (long long)a.seq.rows * a.heads;      // row by row, head by head
@@ -385,21 +396,20 @@ __global__ void __launch_bounds__(256) attention_delta(const __grid_constant__ R
   if (i < n && l == 0) a.delta[(size_t)(i % a.heads) * a.seq.rows + i / a.heads] = sum;
 }
 
-template <bool kKeys, int kChunks> int launch_bwd(const BwdArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& dy, cudaStream_t st) {
+template <int kChunks> int launch_bwd(const BwdArgs& a, long long ctas, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& dy, cudaStream_t st) {
   static const char* who = "Attention's gradient";
   static bool set[64] = {};
-  const int rc = allow_smem(reinterpret_cast<const void*>(attention_bwd<kKeys, kChunks>), bwd_smem(kKeys, kChunks), set, who);
+  constexpr size_t bytes = std::max(bwd_smem(true, kChunks), bwd_smem(false, kChunks));
+  const int rc = allow_smem(reinterpret_cast<const void*>(attention_bwd<kChunks>), bytes, set, who);
   if (rc != DRAGON_OK) return rc;
-  const long long grid = (long long)a.blocks * (kKeys ? a.r.kv_heads : a.r.heads);
-  if (grid > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
-  attention_bwd<kKeys, kChunks><<<(unsigned)grid, kBwdThreads, bwd_smem(kKeys, kChunks), st>>>(q, k, v, dy, a);
-  return launched(who);
+  if (ctas > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
+  return launch_behind(attention_bwd<kChunks>, dim3((unsigned)ctas), dim3(kBwdThreads), bytes, st, who, q, k, v, dy, a);
 }
 
 }  // namespace
 
 size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads) { return (size_t)(rows * heads) * sizeof(float); }
-int attention_bwd_launches(const Step& s) { return 1 + (s.wr[at::DQ] >= 0) + (s.wr[at::DK] >= 0 || s.wr[at::DV] >= 0); }
+int attention_bwd_launches(const Step& s) { return 1 + (s.wr[at::DQ] >= 0 || s.wr[at::DK] >= 0 || s.wr[at::DV] >= 0); }
 
 int launch_attention_backward(const RowArgs& rows, cudaStream_t st) {
   BwdArgs a = {};
@@ -415,11 +425,10 @@ int launch_attention_backward(const RowArgs& rows, cudaStream_t st) {
   int lanes = 1;
   while (lanes * 8 < rows.width) lanes *= 2;
   const long long warps = ((long long)rows.seq.rows * rows.heads * lanes + 31) / 32;
-  attention_delta<<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(rows, lanes);
-  int rc = launched("Attention's gradient");
-  const bool wide = rows.width > 64;
-  if (rc == DRAGON_OK && rows.out) rc = wide ? launch_bwd<false, 2>(a, q, k, v, dy, st) : launch_bwd<false, 1>(a, q, k, v, dy, st);
-  if (rc == DRAGON_OK && (rows.dk || rows.dv)) rc = wide ? launch_bwd<true, 2>(a, q, k, v, dy, st) : launch_bwd<true, 1>(a, q, k, v, dy, st);
+  int rc = launch_behind(attention_delta, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, "Attention's gradient", rows, lanes);
+  const long long key_ctas = rows.dk || rows.dv ? (long long)a.blocks * rows.kv_heads : 0, ctas = key_ctas + (rows.out ? (long long)a.blocks * rows.heads : 0);
+  a.key_ctas = (int)std::min(key_ctas, 0x7fffffffLL);
+  if (rc == DRAGON_OK && ctas) rc = rows.width > 64 ? launch_bwd<2>(a, ctas, q, k, v, dy, st) : launch_bwd<1>(a, ctas, q, k, v, dy, st);
   return rc;
 }
 

@@ -178,9 +178,34 @@ __device__ __noinline__ void dkv_of_row(const RowArgs& a, int kvh, int row, int 
     }
 }
 
+// Launches of one operator behind one another: a kernel's CTAs may be there, and prepare what needs no results, before the launch in
+// front has ended (a launch of 2 to 3 us is hidden that way).  Each launch lets the next one come as soon as all of its CTAs run,
+// and each thread waits for the end of the launch before (which has waited for the one before it) ahead of its first access to memory
+// that a kernel writes.
+__device__ __forceinline__ void next_launch_may_come() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void after_the_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 int launched(const char* who) {
   const cudaError_t e = cudaGetLastError();
   if (e == cudaSuccess) return DRAGON_OK;
+  set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
+  return DRAGON_ERR_CUDA;
+}
+
+template <typename... P, typename... A> int launch_behind(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, const char* who, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  if (e == cudaSuccess) return launched(who);
+  cudaGetLastError();
   set_error("%s: launch failed: %s", who, cudaGetErrorString(e));
   return DRAGON_ERR_CUDA;
 }

@@ -53,6 +53,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 4 * kSt);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   __shared__ Unit unit;
+  if (kPaged) after_the_launch_before();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pack = 1 << a.pack_shift, tile_rows = 128 >> a.pack_shift, block_rows = a.by_heads ? 128 : 2 * tile_rows;      // rows: of the sequence
   const int column = blockIdx.x % a.columns, group = a.r.heads / a.r.kv_heads, heads_here = a.by_heads ? 2 : pack;
@@ -88,6 +89,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   }
   __syncthreads();
   const Unit u = unit;
+  next_launch_may_come();
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
     if (a.r.splits > 1) return;      // (where the parts are put together)
     const int wide = heads_here * a.r.width;
@@ -371,7 +373,9 @@ template <bool kPaged, int kChunks> int launch_fwd(const FwdArgs& a, const CUten
   if (rc != DRAGON_OK) return rc;
   const long long grid = (long long)a.blocks * a.columns;
   if (grid > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
-  attention_fwd<kPaged, kChunks><<<dim3((unsigned)grid, a.r.splits), kFwdThreads, fwd_smem(kChunks), st>>>(q, k, v, a);
+  const dim3 ctas((unsigned)grid, a.r.splits);
+  if (kPaged) return launch_behind(attention_fwd<kPaged, kChunks>, ctas, dim3(kFwdThreads), fwd_smem(kChunks), st, who, q, k, v, a);
+  attention_fwd<kPaged, kChunks><<<ctas, kFwdThreads, fwd_smem(kChunks), st>>>(q, k, v, a);
   return launched(who);
 }
 

@@ -36,6 +36,7 @@ struct WriteArgs {
 };
 
 __global__ void __launch_bounds__(32 * kWriteWarps) cache_write(const __grid_constant__ WriteArgs a) {
+  next_launch_may_come();
   if (blockIdx.x == 0 && blockIdx.y == 0) {
     if (threadIdx.x == 0 && a.status_clear) *a.status_clear = 0;
     if (!a.seq.in_order()) report(a.status, DRAGON_ERR_INVALID_ARG);
@@ -92,6 +93,8 @@ template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps) 
   extern __shared__ __align__(16) unsigned char smem_few[];
   __shared__ float warp_top[kFewWarps][kRows], warp_sum_of[kFewWarps][kRows];
   __shared__ int row_bad[kRows];
+  next_launch_may_come();
+  after_the_launch_before();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int split = blockIdx.x % a.splits, column = blockIdx.x / a.splits % columns, s = blockIdx.x / a.splits / columns;
   const int kvh = column % a.kv_heads, tile = column / a.kv_heads, group = a.heads / a.kv_heads;
@@ -304,6 +307,7 @@ template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps) 
 // parts, 4 elements a lane.  by_sequence: only rows of sequences of few rows (the others have no parts).
 __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArgs a, int few, int few_splits, int tile_splits, int ways, int by_sequence) {
   __shared__ float sums[8][132];
+  after_the_launch_before();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = warp & (ways - 1), group = a.heads / a.kv_heads;
   const long long item = ((long long)blockIdx.x * 8 + warp) / ways;
   int row, head, s, splits = 0;
@@ -423,9 +427,9 @@ template <int kSteps> int launch_few(const RowArgs& a, const PagedPlan& p, int m
   const int columns = a.kv_heads * ((most_rows + p.few_rows - 1) / p.few_rows);
   const long long grid = (long long)p.few_splits * columns * a.seq.count;
   if (grid > 0x7fffffffLL) { set_error("PagedAttention: too many sequences and heads"); return DRAGON_ERR_UNSUPPORTED; }
-  if (wide) paged_few<kSteps, 2><<<(unsigned)grid, 32 * kFewWarps, bytes, st>>>(a, p.most_few, columns);
-  else paged_few<kSteps, 1><<<(unsigned)grid, 32 * kFewWarps, bytes, st>>>(a, p.most_few, columns);
-  return launched("PagedAttention");
+  const dim3 ctas((unsigned)grid), threads(32 * kFewWarps);
+  return wide ? launch_behind(paged_few<kSteps, 2>, ctas, threads, bytes, st, "PagedAttention", a, p.most_few, columns)
+              : launch_behind(paged_few<kSteps, 1>, ctas, threads, bytes, st, "PagedAttention", a, p.most_few, columns);
 }
 
 }  // namespace
@@ -517,8 +521,7 @@ int launch_paged_attention(const StepRun& r) {
     const bool by_sequence = a.seq.starts && p.tiles && p.tile_splits == 1;
     const int ways = std::max(p.few_splits, p.tile_splits) > 8 ? 8 : 1;
     const long long items = by_sequence ? (long long)a.seq.count * a.kv_heads * p.most_few : (long long)a.seq.rows * a.heads;
-    paged_join<<<(unsigned)((items * ways + 7) / 8), 256, 0, st>>>(a, p.most_few, p.few_splits, p.tile_splits, ways, by_sequence);
-    rc = launched("PagedAttention");
+    rc = launch_behind(paged_join, dim3((unsigned)((items * ways + 7) / 8)), dim3(256), 0, st, "PagedAttention", a, p.most_few, p.few_splits, p.tile_splits, ways, (int)by_sequence);
   }
   return rc;
 }
