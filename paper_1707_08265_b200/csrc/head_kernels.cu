@@ -54,14 +54,10 @@ struct HeadArgs {
 __device__ __forceinline__ int place_of(int i) { return (i & 7) * (kPairsMost / 8 + 1) + (i >> 3); }
 constexpr int kPlaces = 8 * (kPairsMost / 8 + 1);
 
-// the angles of `rows` rows from r0 on
-__device__ __forceinline__ void fill_angles(const HeadArgs& a, const unsigned long long* freq, float2 (*cs)[kPlaces], int r0, int rows) {
+// the angles of a tile: a warp a row (its rows are at most as many as the warps), or several warps a row; position: of the warp's row
+__device__ __forceinline__ void fill_angles(const HeadArgs& a, const unsigned long long* freq, float2 (*cs)[kPlaces], int position, int r, int part, int side) {
   const int pairs = a.dims >> 1;
-  int r = threadIdx.x >> 5;      // a warp a row (the rows of a tile are at most as many as the warps)
-  const int side = kHeadWarps / a.tile, part = r / a.tile;
-  r -= part * a.tile;
-  if (r >= rows) return;
-  const unsigned long long pos = (unsigned long long)(long long)__ldg(a.pos + r0 + r);
+  const unsigned long long pos = (unsigned long long)(long long)position;
   for (int k = (threadIdx.x & 31) + 32 * part; k < pairs; k += 32 * side) {
     float s, c;
     sincospif((float)(int)((pos * freq[k]) >> 32) * 0x1p-31f, &s, &c);
@@ -201,6 +197,10 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
     }
   };
   Batch now;
+  // the row whose angles this warp computes, and its position, known a tile ahead
+  const int angle_row = warp & (a.tile - 1), angle_part = warp / a.tile;
+  auto position_of = [&](long long r0) { return kPairing != P_NONE && r0 + angle_row < a.rows ? __ldg(a.pos + r0 + angle_row) : 0; };
+  int position = position_of((long long)blockIdx.x * a.tile);
   const size_t row_stride = (size_t)stride * jb.heads * width;
   size_t row = row_of((long long)blockIdx.x * a.tile);
   fetch(row, (long long)blockIdx.x * a.tile + my_row < a.rows, my_side, now);
@@ -209,7 +209,8 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
     Pair own[4], other[4];
     if (kPairing != P_NONE) {
       __syncthreads();
-      fill_angles(a, freq, cs, (int)r0, rows);
+      if (angle_row < rows) fill_angles(a, freq, cs, position, angle_row, angle_part, side);
+      position = position_of(r0 + stride);
       __syncthreads();
     }
     if (my_row >= rows) continue;
@@ -359,10 +360,25 @@ __global__ void __launch_bounds__(1024) head_finish(const __grid_constant__ Fini
   }
 }
 
-// Rows of a tile: as many as leave tiles enough for four CTAs on every SM
-int tile_rows(int64_t rows, int sm_count) {
+// Rows of a tile: as many as leave tiles enough for four CTAs on every SM, and so many that each warp of a row has an access to make
+// (964 rows of one head with gradients: 34 us with tiles of one row, of whose eight warps seven had nothing to do, 14.5 with eight rows)
+int tile_rows(int64_t rows, int accesses, int sm_count) {
   int t = kHeadRowsMost;
-  while (t > 1 && rows < t * (4 * (int64_t)sm_count)) t /= 2;
+  while (t > 1 && rows < t * (4 * (int64_t)sm_count) && accesses >= 2 * kHeadWarps / t) t /= 2;
+  return t;
+}
+struct HeadTiles { int tile, grid; };
+// x: where a job's operand of [rows, heads * width] stands among its `reads`
+HeadTiles head_tiles(const Step& s, const std::vector<MemRef>& mems, int x, int reads, int sm_count) {
+  const int width = (int)s.num[hn::WIDTH];
+  int lanes = 1;
+  while (lanes * 8 < width) lanes *= 2;
+  int64_t accesses = 1;
+  for (size_t at = x; at < s.rd.size(); at += reads) accesses = std::max(accesses, (mems[s.rd[at]].shape.d[1] / width * lanes + 31) / 32);
+  const int64_t rows = mems[s.rd[x]].shape.d[0];
+  HeadTiles t;
+  t.tile = tile_rows(rows, (int)std::min<int64_t>(accesses, kHeadWarps), sm_count);
+  t.grid = (int)std::min<int64_t>((rows + t.tile - 1) / t.tile, kHeadCtas * (int64_t)sm_count);
   return t;
 }
 
@@ -417,10 +433,7 @@ template <bool kBack> cudaError_t launch(HeadArgs& a, const Step& s, int jobs, d
 
 }  // namespace
 
-int head_bwd_partials(int64_t rows, int sm_count) {      // the grid, too
-  const int tile = tile_rows(rows, sm_count);
-  return (int)std::min<int64_t>((rows + tile - 1) / tile, kHeadCtas * (int64_t)sm_count);
-}
+int head_bwd_partials(const Step& s, const std::vector<MemRef>& mems, int sm_count) { return head_tiles(s, mems, hb::DY, hb::READS, sm_count).grid; }
 
 cudaError_t launch_head(const StepRun& r) {
   const Step& s = r.s;
@@ -445,8 +458,9 @@ cudaError_t launch_head(const StepRun& r) {
   }
   a.pos = rotated ? reinterpret_cast<const int*>(r.rd(hd::POS)) : nullptr;
   a.status_clear = r.status_clear;
-  a.tile = tile_rows(a.rows, r.sm_count);
-  return launch<false>(a, s, jobs, dim3(head_bwd_partials(a.rows, r.sm_count), jobs), reinterpret_cast<cudaStream_t>(r.stream));
+  const HeadTiles t = head_tiles(s, r.mems, hd::X, hd::READS, r.sm_count);
+  a.tile = t.tile;
+  return launch<false>(a, s, jobs, dim3(t.grid, jobs), reinterpret_cast<cudaStream_t>(r.stream));
 }
 
 cudaError_t launch_head_bwd(const StepRun& r) {
@@ -456,7 +470,9 @@ cudaError_t launch_head_bwd(const StepRun& r) {
   FinishArgs f = {};
   a.width = f.width = (int)s.num[hn::WIDTH];
   a.rows = (int)sh.d[0];
-  const int jobs = (int)s.rd.size() / hb::READS, grid = head_bwd_partials(a.rows, r.sm_count);
+  const int jobs = (int)s.rd.size() / hb::READS;
+  const HeadTiles t = head_tiles(s, r.mems, hb::DY, hb::READS, r.sm_count);
+  const int grid = t.grid;
   int sums = 0;
   for (int j = 0; j < jobs; ++j) {
     HeadJob& b = a.job[j];
@@ -476,7 +492,7 @@ cudaError_t launch_head_bwd(const StepRun& r) {
   }
   a.pos = reinterpret_cast<const int*>(r.rd(hb::POS));
   a.status_clear = r.status_clear;
-  a.tile = tile_rows(a.rows, r.sm_count);
+  a.tile = t.tile;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
   const cudaError_t e = launch<true>(a, s, jobs, dim3(grid, jobs), st);
   if (e != cudaSuccess || !sums) return e;

@@ -1373,8 +1373,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
     }
     if ((st.kind == ST_HEAD || st.kind == ST_HEAD_BWD) && st.rd[hd::POS] >= 0) st.freq = rotation_table(st.num);
     if (st.kind == ST_HEAD_BWD) {
-      const Shape& sh = mems[st.rd[hb::DY]].shape;
-      st.n_colpart = head_bwd_partials(sh.d[0], sm_count);
+      st.n_colpart = head_bwd_partials(st, mems, sm_count);
       st.colpart_off = take(st.head_eps.size() * st.n_colpart * (size_t)st.num[hn::WIDTH] * sizeof(float));
     }
     if (st.kind == ST_ATTN_BWD) st.scratch_off = take(attention_bwd_scratch_bytes(mems[st.rd[at::Q]].shape.d[0], (int64_t)st.num[an::HEADS]));

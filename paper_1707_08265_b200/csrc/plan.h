@@ -182,7 +182,7 @@ bool norm_and_clip_fit_one_launch(const std::vector<int64_t>& numel, const std::
 size_t scan_scratch_bytes(int64_t rows, int64_t cols);
 constexpr int64_t kMaxAttentionRows = 1 << 30;   // rows of an attention operator's tensors: 32-bit row numbers with room for a tile
 constexpr int kMaxHeadWidth = 128, kMaxRotatedWidth = 256;
-int head_bwd_partials(int64_t rows, int sm_count);   // rows of partial gain gradients that HeadNorm's gradient leaves
+int head_bwd_partials(const Step& s, const std::vector<MemRef>& mems, int sm_count);   // rows of partial gain gradients that HeadNorm's gradient leaves
 size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads);
 int attention_bwd_launches(const Step& s);
 int paged_launches(const Step& s, const std::vector<MemRef>& mems, int sm_count);
