@@ -10,6 +10,8 @@
 //          computes S^T = K Q^T and dP^T = V dY^T, so that P^T and dS^T lie in TMEM as the A operands of dV += P^T dY and
 //          dK += dS^T Q (dY and Q as they lie in memory, MN-major).
 //   rows:  a CTA has 128 rows of a head and meets their keys: S = Q K^T, dP = dY V^T, dQ += dS K.
+// Where the heads of a group are a power of two a tile of queries has all of them, for 128 / group neighbouring rows of the sequence:
+// short sequences fill it (14 sequences of 28 rows, 8 heads a group: 54 us forwards and backwards with tiles of one head, 31 so).
 // One tile pair is 128 x 128; two warps share a row (64 columns each).  The products are issued in an order in which the tensor
 // unit has work while the threads compute: keys: dV(i), S(i+1), dK(i), dP(i+1); rows: S(i+1), dP(i+1), dQ(i) (dP has two buffers).
 // Warps: 0..7 mathematics, 8 TMA, 9 MMA.  Every wait is bounded.
@@ -33,7 +35,8 @@ constexpr size_t bwd_smem(bool keys, int chunks) {
 
 struct BwdArgs {
   RowArgs r;
-  int blocks, each_blocks;
+  int pack_shift;           // log2 of the heads in a tile of queries
+  int blocks[2], each_blocks[2];      // of rows, of keys
   int key_ctas;             // the first CTAs have keys, the others rows
   long long budget;
   int drop_first_load;
@@ -58,7 +61,9 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   __shared__ Unit unit;
   __shared__ unsigned again[8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.r.heads / a.r.kv_heads;
-  const int n_heads = kKeys ? a.r.kv_heads : a.r.heads, head = cta % n_heads;
+  const int shift = a.pack_shift, pack = 1 << shift, tile_rows = 128 >> shift;      // rows of the sequence in a tile of queries
+  const int own_rows = kKeys ? 128 : tile_rows, own_heads = kKeys ? 1 : pack, n_heads = kKeys ? a.r.kv_heads : a.r.heads;
+  const int columns = n_heads / own_heads, head0 = cta % columns * own_heads;      // the first of the CTA's heads
 
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
@@ -74,7 +79,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   }
   if (warp == 0) {
     Unit u;
-    find_unit(a.r.seq, a.blocks, a.each_blocks, cta / n_heads, 128, &u, lane);
+    find_unit(a.r.seq, a.blocks[kKeys], a.each_blocks[kKeys], cta / columns, own_rows, &u, lane);
     if (u.seq >= 0 && kKeys && a.r.causal) u.row0 = (u.b - u.a - 1) / 128 * 128 - u.row0;      // the first keys are seen by most rows
     if (lane == 0) unit = u;
   }
@@ -84,15 +89,15 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares)
-      for (int c = 8 * threadIdx.x; c < a.r.width; c += 8 * kBwdThreads) {
-        const size_t at = ((size_t)row * n_heads + head) * a.r.width + c;
+      for (int c = 8 * threadIdx.x; c < own_heads * a.r.width; c += 8 * kBwdThreads) {
+        const size_t at = ((size_t)row * n_heads + head0) * a.r.width + c;
         if (kKeys && a.r.dk) store_any<8>(a.r.dk, a.r.dkt, at, zero);
         if (kKeys && a.r.dv) store_any<8>(a.r.dv, a.r.dvt, at, zero);
         if (!kKeys) store_any<8>(a.r.out, a.r.ot, at, zero);
       }
     return;
   }
-  const int n_rows = u.b - u.a, last = min(u.row0 + 128, n_rows) - 1;      // own rows: row0 .. last
+  const int n_rows = u.b - u.a, last = min(u.row0 + own_rows, n_rows) - 1;      // own rows: row0 .. last
   // the tiles it meets: keys: rows that see any of the own keys; rows: keys that any of the own rows sees
   int first = 0, end = n_rows;
   if (kKeys) {
@@ -102,7 +107,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     if (a.r.causal) end = last + 1;
     if (a.r.window) first = max(0, u.row0 - a.r.window + 1);
   }
-  const int t0 = first / 128, tiles = (end + 127) / 128 - t0, n = tiles * (kKeys ? group : 1);
+  const int met_rows = kKeys ? tile_rows : 128, t0 = first / met_rows, tiles = (end + met_rows - 1) / met_rows - t0, n = tiles * (kKeys ? group >> shift : 1);
 
   if (warp == 9) {
     __syncwarp();
@@ -124,16 +129,16 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     if (elected()) {
       mbar_expect_tx(x_full, 2 * kTile);
       for (int c = 0; c < kChunks; ++c) {
-        tma_load_3d(x1 + c * kChunkBytes, kKeys ? &tm_k : &tm_q, 64 * c, head, u.a + u.row0, x_full);
-        tma_load_3d(x2 + c * kChunkBytes, kKeys ? &tm_v : &tm_dy, 64 * c, head, u.a + u.row0, x_full);
+        tma_load_3d(x1 + c * kChunkBytes, kKeys ? &tm_k : &tm_q, 64 * c, head0, u.a + u.row0, x_full);
+        tma_load_3d(x2 + c * kChunkBytes, kKeys ? &tm_v : &tm_dy, 64 * c, head0, u.a + u.row0, x_full);
       }
     }
     __syncwarp();
     bool ok = true;
-    int h = kKeys ? head * group : head / group, tile = 0;
+    int h = kKeys ? head0 * group : head0 / group, tile = 0;
     for (int i = 0; i < n && ok; ++i, ++tile) {
       if (tile == tiles) { tile = 0; ++h; }
-      const int s = i % kSt1, turn = i / kSt1, row = u.a + (t0 + tile) * 128;
+      const int s = i % kSt1, turn = i / kSt1, row = u.a + (t0 + tile) * met_rows;
       ok = wait_warp(y1_empty + 8 * s, (turn & 1) ^ 1);
       if (!ok) break;
       issued1 = i + 1;
@@ -148,8 +153,8 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
         if (!ok) break;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int r = (t0 + tile) * 128 + 32 * k + lane;
-          const size_t at = (size_t)h * a.r.seq.rows + u.a + r;
+          const int r = (t0 + tile) * tile_rows + ((32 * k + lane) >> shift);
+          const size_t at = (size_t)(h + (lane & (pack - 1) & 31) + (32 * k & (pack - 1))) * a.r.seq.rows + u.a + r;
           stats[s * 256 + 32 * k + lane] = r < n_rows ? -__ldg(a.r.lse + at) : -kInf;
           stats[s * 256 + 128 + 32 * k + lane] = r < n_rows ? -__ldg(a.r.delta + at) : 0.f;
         }
@@ -221,7 +226,8 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     }
     if (ok) commit(acc_full);
   } else {
-    const int e = (warp & 3) * 32 + lane, half = warp >> 2, row = u.row0 + e;      // own row of the sequence (a key, or a query)
+    const int e = (warp & 3) * 32 + lane, half = warp >> 2;
+    const int row = u.row0 + (kKeys ? e : e >> shift), head = head0 + (kKeys ? 0 : e & (pack - 1));      // own row of the sequence (a key, or a query)
     const bool mine = row < n_rows;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     float lse = kInf, delta = 0.f;
@@ -233,12 +239,12 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     bool ok = true;
     for (int i = 0, tile = 0; i < n; ++i, ++tile) {
       if (tile == tiles) tile = 0;
-      const int c0 = (t0 + tile) * 128 + 64 * half;      // the first of this thread's columns
+      const int r0 = (t0 + tile) * met_rows, c0 = r0 + 64 * half;      // the tile's first row; (rows) this thread's first column
       // columns [lo, hi) are seen
       int lo, hi;
       if (kKeys) {
-        lo = a.r.causal ? row - c0 : 0;
-        hi = a.r.window ? (int)min(64LL, (long long)row + a.r.window - c0) : 64;
+        lo = a.r.causal ? (min(max(row - r0, 0), tile_rows) << shift) - 64 * half : 0;
+        hi = a.r.window ? ((int)min((long long)tile_rows, max(0LL, (long long)row + a.r.window - r0)) << shift) - 64 * half : 64;
       } else {
         hi = (a.r.causal ? min(row + 1, n_rows) : n_rows) - c0;
         lo = a.r.window ? row - a.r.window + 1 - c0 : 0;
@@ -339,9 +345,9 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     asm volatile("bar.sync 1, 256;" ::: "memory");
     if (half == 0)
       for (unsigned b = again[warp] | again[warp + 4]; b; b &= b - 1) {
-        const int r = u.a + u.row0 + (warp & 3) * 32 + __ffs(b) - 1;
-        if (kKeys) dkv_of_row(a.r, head, r, lane);
-        else dq_of_row(a.r, head, r, lane);
+        const int r = (warp & 3) * 32 + __ffs(b) - 1, first_row = u.a + u.row0;
+        if (kKeys) dkv_of_row(a.r, head0, first_row + r, lane);
+        else dq_of_row(a.r, head0 + (r & (pack - 1)), first_row + (r >> shift), lane);
       }
   }
   fence_before();
@@ -414,11 +420,15 @@ int attention_bwd_launches(const Step& s) { return 1 + (s.wr[at::DQ] >= 0 || s.w
 int launch_attention_backward(const RowArgs& rows, cudaStream_t st) {
   BwdArgs a = {};
   a.r = rows;
-  count_blocks(rows.seq, 128, &a.blocks, &a.each_blocks);
+  const int group = rows.heads / rows.kv_heads;
+  while (packs(group) && 1 << a.pack_shift < group) ++a.pack_shift;
+  const int tile_rows = 128 >> a.pack_shift, pack = 1 << a.pack_shift;
+  count_blocks(rows.seq, tile_rows, &a.blocks[0], &a.each_blocks[0]);
+  count_blocks(rows.seq, 128, &a.blocks[1], &a.each_blocks[1]);
   wait_settings("DRAGON_ATTENTION", &a.budget, &a.drop_first_load);
   CUtensorMap q, k, v, dy;
-  if (!head_map(&q, rows.q, rows.seq.rows, rows.heads, rows.width, 128) || !head_map(&k, rows.k, rows.seq.rows, rows.kv_heads, rows.width, 128) ||
-      !head_map(&v, rows.v, rows.seq.rows, rows.kv_heads, rows.width, 128) || !head_map(&dy, rows.dy, rows.seq.rows, rows.heads, rows.width, 128)) {
+  if (!head_map(&q, rows.q, rows.seq.rows, rows.heads, rows.width, tile_rows, pack) || !head_map(&k, rows.k, rows.seq.rows, rows.kv_heads, rows.width, 128) ||
+      !head_map(&v, rows.v, rows.seq.rows, rows.kv_heads, rows.width, 128) || !head_map(&dy, rows.dy, rows.seq.rows, rows.heads, rows.width, tile_rows, pack)) {
     set_error("Attention's gradient: cannot encode the TMA descriptors (no CUDA driver?)");
     return DRAGON_ERR_CUDA;
   }
@@ -426,7 +436,7 @@ int launch_attention_backward(const RowArgs& rows, cudaStream_t st) {
   while (lanes * 8 < rows.width) lanes *= 2;
   const long long warps = ((long long)rows.seq.rows * rows.heads * lanes + 31) / 32;
   int rc = launch_behind(attention_delta, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, "Attention's gradient", rows, lanes);
-  const long long key_ctas = rows.dk || rows.dv ? (long long)a.blocks * rows.kv_heads : 0, ctas = key_ctas + (rows.out ? (long long)a.blocks * rows.heads : 0);
+  const long long key_ctas = rows.dk || rows.dv ? (long long)a.blocks[1] * rows.kv_heads : 0, ctas = key_ctas + (rows.out ? (long long)a.blocks[0] * (rows.heads / pack) : 0);
   a.key_ctas = (int)std::min(key_ctas, 0x7fffffffLL);
   if (rc == DRAGON_OK && ctas) rc = rows.width > 64 ? launch_bwd<2>(a, ctas, q, k, v, dy, st) : launch_bwd<1>(a, ctas, q, k, v, dy, st);
   return rc;

@@ -381,9 +381,6 @@ template <bool kPaged, int kChunks> int launch_fwd(const FwdArgs& a, const CUten
 
 }  // namespace
 
-// whether a tile holds all heads of a group
-static bool packs(int group) { return (group & (group - 1)) == 0 && group <= 128; }
-
 // units of work that the kernel has at least room for, without splits
 int64_t attention_units(int64_t rows, int64_t sequences, int heads, int kv_heads) {
   const int group = heads / kv_heads;

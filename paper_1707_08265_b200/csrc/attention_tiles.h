@@ -205,6 +205,9 @@ bool head_map(CUtensorMap* map, const void* ptr, int64_t rows, int heads, int wi
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// whether a tile of queries holds all heads of a group
+bool packs(int group) { return (group & (group - 1)) == 0 && group <= 128; }
+
 // blocks of rows that a grid needs room for, and those of a sequence where all are equally long
 void count_blocks(const Sequences& q, int block_rows, int* blocks, int* each_blocks) {
   *each_blocks = q.starts ? 0 : (q.each + block_rows - 1) / block_rows;
