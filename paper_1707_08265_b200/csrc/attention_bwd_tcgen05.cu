@@ -55,8 +55,8 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   uint64_t* bars = reinterpret_cast<uint64_t*>(stats + (kKeys ? kSt1 * 256 : 0));
   const uint32_t x_full = smem_u32(bars), y1_full = x_full + 8, y1_empty = y1_full + 8 * kSt1, y2_full = y1_empty + 8 * kSt1, y2_empty = y2_full + 8 * kSt2;
   const uint32_t st_full = y2_empty + 8 * kSt2, st_empty = st_full + 8 * kSt1;
-  const uint32_t s_full = st_empty + 8 * kSt1, dp_full = s_full + 8, p_full = dp_full + 16, ds_full = p_full + 8, acc_full = ds_full + 8, drain = acc_full + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 4 * kSt1 + 2 * kSt2 + 7);
+  const uint32_t s_full = st_empty + 8 * kSt1, dp_full = s_full + 8, p_full = dp_full + 16, ds_full = p_full + 8, acc_full = ds_full + 16, drain = acc_full + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 4 * kSt1 + 2 * kSt2 + 8);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   __shared__ Unit unit;
   __shared__ unsigned again[8];
@@ -73,7 +73,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     mbar_init(x_full, 1);
     for (int s = 0; s < kSt1; ++s) { mbar_init(y1_full + 8 * s, 1); mbar_init(y1_empty + 8 * s, 1); mbar_init(st_full + 8 * s, 32); mbar_init(st_empty + 8 * s, 8); }
     for (int s = 0; s < kSt2; ++s) { mbar_init(y2_full + 8 * s, 1); mbar_init(y2_empty + 8 * s, 1); }
-    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(dp_full + 8, 1); mbar_init(p_full, 8); mbar_init(ds_full, 8); mbar_init(acc_full, 1); mbar_init(drain, 1);
+    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(dp_full + 8, 1); mbar_init(p_full, 8); mbar_init(ds_full, 8); mbar_init(ds_full + 8, 8); mbar_init(acc_full, 1); mbar_init(drain, 1);
     abort_flag[0] = abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -220,7 +220,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
           fence_after();
           if (!(ok = issue_s(i + 1) && issue_dp(i + 1))) break;
         }
-        if (!(ok = wait_warp(ds_full, i & 1))) break;
+        if (!(ok = wait_warp(ds_full + 8 * (i & 1), (i >> 1) & 1))) break;
         accumulate(kAcc1, dp_at(i), y1 + s * kTile, i > 0, y1_empty + 8 * s);
       }
     }
@@ -306,7 +306,9 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
       tmem_st_wait();
       fence_before();
       __syncwarp();
-      mbar_arrive_if(ds_full, lane == 0);
+      // (rows: S and dP of the next round are there by now, so a warp can be here again before another one has come here for this round:
+      // two barriers, in turn)
+      mbar_arrive_if(ds_full + (kKeys ? 0 : 8 * (i & 1)), lane == 0);
       if (kKeys) mbar_arrive_if(st_empty + 8 * (i % kSt1), lane == 0);
     }
     if (ok) {
