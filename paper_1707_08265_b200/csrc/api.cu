@@ -627,7 +627,7 @@ int dragon_function_num_launches(const dragon_function_t* f) {
       for (size_t k = hb::DGAIN; k < st.wr.size(); k += hb::WRITES) sums |= st.wr[k] >= 0;
       n += 1 + sums;
     }
-    else if (st.kind == ST_ATTN_BWD) n += attention_bwd_launches(st);
+    else if (st.kind == ST_ATTN || st.kind == ST_ATTN_BWD) n += attention_launches(st, f->plan.mems, f->plan.sm_count);
     else if (st.kind == ST_PAGED) n += paged_launches(st, f->plan.mems, f->plan.sm_count);
     else if (st.kind != ST_COPY) n += 1 + (st.mF >= 0 ? 1 : 0);
   }

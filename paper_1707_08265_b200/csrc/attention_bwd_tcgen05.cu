@@ -63,6 +63,9 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.r.heads / a.r.kv_heads;
   const int shift = a.pack_shift, pack = 1 << shift, tile_rows = 128 >> shift;      // rows of the sequence in a tile of queries
   const int own_rows = kKeys ? 128 : tile_rows, own_heads = kKeys ? 1 : pack, n_heads = kKeys ? a.r.kv_heads : a.r.heads;
+  const int splits = kKeys ? a.r.key_splits : a.r.splits;
+  int part = 0;
+  if (splits > 1) { part = cta % splits; cta /= splits; }      // (divisions that most calls do without)
   const int columns = n_heads / own_heads, head0 = cta % columns * own_heads;      // the first of the CTA's heads
 
   if (threadIdx.x == 0) {
@@ -85,6 +88,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   }
   __syncthreads();
   const Unit u = unit;
+  next_launch_may_come();
   after_the_launch_before();
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -107,7 +111,27 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     if (a.r.causal) end = last + 1;
     if (a.r.window) first = max(0, u.row0 - a.r.window + 1);
   }
-  const int met_rows = kKeys ? tile_rows : 128, t0 = first / met_rows, tiles = (end + met_rows - 1) / met_rows - t0, n = tiles * (kKeys ? group >> shift : 1);
+  const int met_rows = kKeys ? tile_rows : 128, t0 = first / met_rows, tiles = (end + met_rows - 1) / met_rows - t0, all = tiles * (kKeys ? group >> shift : 1);
+  int skip = 0, n = all, h_skip = 0, tile_skip = 0;      // this CTA's part of them
+  if (splits > 1) {
+    const int each = (all + splits - 1) / splits;
+    skip = min(all, part * each);
+    n = min(each, all - skip);
+    h_skip = skip / tiles;
+    tile_skip = skip - h_skip * tiles;
+  }
+  float* const to = splits > 1 ? (kKeys ? a.r.part_k : a.r.part) + (size_t)part * a.r.seq.rows * n_heads * a.r.width : nullptr;
+  float* const to_v = splits > 1 && kKeys ? a.r.part_v + (size_t)part * a.r.seq.rows * n_heads * a.r.width : nullptr;
+  if (n == 0) {      // (more parts than tiles)
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int wide = own_heads * a.r.width;
+    for (int i = 8 * threadIdx.x; i < (last - u.row0 + 1) * wide; i += 8 * kBwdThreads) {
+      const size_t at = ((size_t)(u.a + u.row0 + i / wide) * n_heads + head0) * a.r.width + i % wide;
+      store_any<8>(to, DRAGON_F32, at, zero);
+      if (kKeys) store_any<8>(to_v, DRAGON_F32, at, zero);
+    }
+    return;
+  }
 
   if (warp == 9) {
     __syncwarp();
@@ -135,7 +159,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     }
     __syncwarp();
     bool ok = true;
-    int h = kKeys ? head0 * group : head0 / group, tile = 0;
+    int h = kKeys ? head0 * group + h_skip : head0 / group, tile = tile_skip;
     for (int i = 0; i < n && ok; ++i, ++tile) {
       if (tile == tiles) { tile = 0; ++h; }
       const int s = i % kSt1, turn = i / kSt1, row = u.a + (t0 + tile) * met_rows;
@@ -237,7 +261,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     }
     const Pair factor = pair_of(a.r.scale, a.r.scale);
     bool ok = true;
-    for (int i = 0, tile = 0; i < n; ++i, ++tile) {
+    for (int i = 0, tile = tile_skip; i < n; ++i, ++tile) {
       if (tile == tiles) tile = 0;
       const int r0 = (t0 + tile) * met_rows, c0 = r0 + 64 * half;      // the tile's first row; (rows) this thread's first column
       // columns [lo, hi) are seen
@@ -333,12 +357,14 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
           }
         }
       };
+      const bool parts = splits > 1;
       if (kKeys) {
-        write(kAcc1, a.r.dk, a.r.dkt, a.r.raw_scale);
-        write(kAcc2, a.r.dv, a.r.dvt, 1.f);
+        write(kAcc1, parts ? to : a.r.dk, parts ? DRAGON_F32 : a.r.dkt, a.r.raw_scale);
+        write(kAcc2, parts ? to_v : a.r.dv, parts ? DRAGON_F32 : a.r.dvt, 1.f);
       } else {
-        write(kAcc1, a.r.out, a.r.ot, a.r.raw_scale);
+        write(kAcc1, parts ? to : a.r.out, parts ? DRAGON_F32 : a.r.ot, a.r.raw_scale);
       }
+      fine |= parts;      // (where the parts are added up a row that is not finite is computed again)
     }
     // rows that are not finite: again, after both halves have been written (every warp comes here, after an unwind too)
     const unsigned bad = __ballot_sync(0xffffffffu, mine && !fine);
@@ -416,8 +442,13 @@ template <int kChunks> int launch_bwd(const BwdArgs& a, long long ctas, const CU
 
 }  // namespace
 
-size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads) { return (size_t)(rows * heads) * sizeof(float); }
-int attention_bwd_launches(const Step& s) { return 1 + (s.wr[at::DQ] >= 0 || s.wr[at::DK] >= 0 || s.wr[at::DV] >= 0); }
+// CTAs of both kinds that there are at least, without splits, and the rows of a sequence in a tile of queries
+void attention_bwd_units(int64_t rows, int64_t sequences, int heads, int kv_heads, int64_t* row_units, int64_t* key_units, int* tile_rows) {
+  const int group = heads / kv_heads, pack = packs(group) ? group : 1;
+  *tile_rows = 128 / pack;
+  *row_units = std::max<int64_t>(sequences, (rows + *tile_rows - 1) / *tile_rows) * (heads / pack);
+  *key_units = std::max<int64_t>(sequences, (rows + 127) / 128) * kv_heads;
+}
 
 int launch_attention_backward(const RowArgs& rows, cudaStream_t st) {
   BwdArgs a = {};
@@ -438,7 +469,8 @@ int launch_attention_backward(const RowArgs& rows, cudaStream_t st) {
   while (lanes * 8 < rows.width) lanes *= 2;
   const long long warps = ((long long)rows.seq.rows * rows.heads * lanes + 31) / 32;
   int rc = launch_behind(attention_delta, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, "Attention's gradient", rows, lanes);
-  const long long key_ctas = rows.dk || rows.dv ? (long long)a.blocks[1] * rows.kv_heads : 0, ctas = key_ctas + (rows.out ? (long long)a.blocks[0] * (rows.heads / pack) : 0);
+  const long long key_ctas = rows.dk || rows.dv ? (long long)a.blocks[1] * rows.kv_heads * rows.key_splits : 0;
+  const long long ctas = key_ctas + (rows.out ? (long long)a.blocks[0] * (rows.heads / pack) * rows.splits : 0);
   a.key_ctas = (int)std::min(key_ctas, 0x7fffffffLL);
   if (rc == DRAGON_OK && ctas) rc = rows.width > 64 ? launch_bwd<2>(a, ctas, q, k, v, dy, st) : launch_bwd<1>(a, ctas, q, k, v, dy, st);
   return rc;

@@ -26,9 +26,10 @@ struct RowArgs {
   float raw_scale;
   Sequences seq;
   Pages pages;
-  // keys of a sequence split over `splits` CTAs: every part's result and the log2 of its sum (-inf: no keys), [split][row][head]
-  int splits;
-  float *part, *part_lse;
+  // what a CTA meets split over `splits` CTAs.  Forwards: every part's result and the log2 of its sum (-inf: no keys), [split][row][head];
+  // backwards: every part's dq, and with key_splits dk and dv, which are added up
+  int splits, key_splits;
+  float *part, *part_lse, *part_k, *part_v;
   int* status;
   int* status_clear;
 };

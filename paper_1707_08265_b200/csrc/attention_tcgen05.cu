@@ -11,7 +11,8 @@
 // While the softmax threads of one tile work, the tensor unit works for the other.  m only moves when a row's maximum has grown
 // by more than 2^8 (P_t and the sum then stay below 2^8 times their scale, far inside bf16 and fp32): O_t in TMEM is rescaled
 // that seldom that the softmax threads do it themselves.  S_t of the next keys is issued behind O_t's product, so a completed
-// S_t says that O_t may be touched.  A paged cache's keys can be split over several CTAs (few rows, long contexts).
+// S_t says that O_t may be touched.  Where there are few units of work (few rows or heads, long contexts) the keys of one are split over
+// several CTAs.
 // Warps: 0..3 and 4..7 softmax of tile 0 and 1 (a warp its TMEM lanes), 8 TMA, 9 MMA.  Every wait is bounded.
 #include <algorithm>
 #include <cstdlib>
@@ -91,7 +92,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const Unit u = unit;
   next_launch_may_come();
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
-    if (a.r.splits > 1) return;      // (where the parts are put together)
+    if (kPaged && a.r.splits > 1) return;      // (where the parts are put together)
     const int wide = heads_here * a.r.width;
     for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -107,7 +108,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const int key_end = a.r.causal ? max(0, min(u.keys, u.first_pos + last_row + 1)) : u.keys;
   const int key_begin = a.r.window ? max(0, u.first_pos + u.row0 - a.r.window + 1) : 0;
   int j0 = key_begin / 128, n_tiles = key_end > key_begin ? (key_end + 127) / 128 - j0 : 0;
-  if (kPaged && a.r.splits > 1) {
+  if (a.r.splits > 1) {
     const int each = (n_tiles + a.r.splits - 1) / a.r.splits, skip = min(n_tiles, (int)blockIdx.y * each);
     j0 += skip;
     n_tiles = min(each, n_tiles - skip);
@@ -321,7 +322,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
           v[k] = n_tiles > 0 ? __uint_as_float(o[k]) * inv : 0.f;
           fine &= fabsf(v[k]) < kInf;
         }
-        if (kPaged && a.r.splits > 1) {
+        if (a.r.splits > 1) {
           float* to = a.r.part + ((size_t)blockIdx.y * a.r.seq.rows * a.r.heads * a.r.width + at + c);
           if (mine && n_tiles > 0) {
             store_any<8>(to, DRAGON_F32, 0, v);
@@ -331,18 +332,18 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
           store_any<8>(a.r.out, a.r.ot, at + c, v);
           if (c + 8 < a.r.width) store_any<8>(a.r.out, a.r.ot, at + c + 8, v + 8);
         }
-        if (!kPaged && mine && a.r.rest) {
+        if (!kPaged && a.r.splits == 1 && mine && a.r.rest) {
 #pragma unroll
           for (int k = 0; k < 16; ++k) v[k] = behind_bf16(v[k]);
           store_any<8>(a.r.rest, DRAGON_BF16, at + c, v);
           if (c + 8 < a.r.width) store_any<8>(a.r.rest, DRAGON_BF16, at + c + 8, v + 8);
         }
       }
-      if (kPaged && a.r.splits > 1) {      // (where the parts are put together a row that is not finite is computed again)
+      if (a.r.splits > 1) {      // (where the parts are put together a row that is not finite is computed again)
         if (mine) a.r.part_lse[((size_t)blockIdx.y * a.r.seq.rows + row) * a.r.heads + head] = sum == 0.f ? -kInf : top * a.r.scale + log2f(sum);
         fine = true;
       }
-      if (mine && a.r.lse) a.r.lse[(size_t)head * a.r.seq.rows + row] = sum == 0.f ? kInf : top * a.r.scale + log2f(sum);
+      if (!kPaged && a.r.splits == 1 && mine && a.r.lse) a.r.lse[(size_t)head * a.r.seq.rows + row] = sum == 0.f ? kInf : top * a.r.scale + log2f(sum);
       __syncwarp();
       for (unsigned again = __ballot_sync(0xffffffffu, mine && !fine); again; again &= again - 1)
         attend_row<kPaged>(a.r, __shfl_sync(0xffffffffu, head, __ffs(again) - 1), __shfl_sync(0xffffffffu, row, __ffs(again) - 1), lane);

@@ -1376,7 +1376,7 @@ static int lower_with_cuts(const Graph& g, const PruneResult& pr, const std::vec
       st.n_colpart = head_bwd_partials(st, mems, sm_count);
       st.colpart_off = take(st.head_eps.size() * st.n_colpart * (size_t)st.num[hn::WIDTH] * sizeof(float));
     }
-    if (st.kind == ST_ATTN_BWD) st.scratch_off = take(attention_bwd_scratch_bytes(mems[st.rd[at::Q]].shape.d[0], (int64_t)st.num[an::HEADS]));
+    if (st.kind == ST_ATTN || st.kind == ST_ATTN_BWD) st.scratch_off = take(attention_scratch_bytes(st, mems, sm_count));
     if (st.kind == ST_PAGED) st.scratch_off = take(paged_scratch_bytes(st, mems, sm_count));
     if (st.kind == ST_GNORM || st.kind == ST_NORM_CLIP) st.scratch_off = take(global_norm_scratch_bytes((int)st.rd.size(), sm_count));
     if (st.kind == ST_SCAN || st.kind == ST_SCAN_BWD) {

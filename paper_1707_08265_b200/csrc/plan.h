@@ -183,8 +183,8 @@ size_t scan_scratch_bytes(int64_t rows, int64_t cols);
 constexpr int64_t kMaxAttentionRows = 1 << 30;   // rows of an attention operator's tensors: 32-bit row numbers with room for a tile
 constexpr int kMaxHeadWidth = 128, kMaxRotatedWidth = 256;
 int head_bwd_partials(const Step& s, const std::vector<MemRef>& mems, int sm_count);   // rows of partial gain gradients that HeadNorm's gradient leaves
-size_t attention_bwd_scratch_bytes(int64_t rows, int64_t heads);
-int attention_bwd_launches(const Step& s);
+size_t attention_scratch_bytes(const Step& s, const std::vector<MemRef>& mems, int sm_count);      // forwards or backwards
+int attention_launches(const Step& s, const std::vector<MemRef>& mems, int sm_count);
 int paged_launches(const Step& s, const std::vector<MemRef>& mems, int sm_count);
 size_t paged_scratch_bytes(const Step& s, const std::vector<MemRef>& mems, int sm_count);
 constexpr int kCachesPerLaunch = 8, kHeadsPerLaunch = 4;

@@ -203,3 +203,13 @@ def test_attention_plan():
     # only the wanted gradients
     g, ids, inputs, outputs = attention_graph(64, 4, 2, 32, grad=True)
     assert "attention_bwd" in B.Graph.from_desc(g.desc).function(inputs, outputs[1:2]).describe()
+
+
+def test_work_of_few_ctas_is_split():
+    """Forward, row sums and gradient are a launch each; one more where the parts of a forward, or of a gradient, are put together."""
+    def launches(*args, **kw):
+        g, _, inputs, outputs = attention_graph(*args, grad=True, **kw)
+        return B.Graph.from_desc(g.desc).function(inputs, outputs).num_launches()
+
+    assert launches(3001, 1, 1, 32) == 5 and launches(2500, 1, 1, 96, window=700) == 4
+    assert launches(16384, 8, 2, 128) == 3 and launches(1, 1, 1, 8) == 3 and launches(8192, 32, 8, 128, sequences=4) == 3
