@@ -68,7 +68,8 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   if (splits > 1) { part = cta % splits; cta /= splits; }      // (divisions that most calls do without)
   const int columns = n_heads / own_heads, head0 = cta % columns * own_heads;      // the first of the CTA's heads
 
-  if (threadIdx.x == 0) {
+  // three warps side by side: barriers, the unit of work, TMEM
+  if (warp == 1 && elected()) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
@@ -86,8 +87,20 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     if (u.seq >= 0 && kKeys && a.r.causal) u.row0 = (u.b - u.a - 1) / 128 * 128 - u.row0;      // the first keys are seen by most rows
     if (lane == 0) unit = u;
   }
+  if (warp == 9) {
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
   __syncthreads();
+  fence_after();
   const Unit u = unit;
+  const uint32_t tmem = *tmem_slot;
+  auto give_tmem_back = [&]() {
+    __syncwarp();
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  };
   next_launch_may_come();
   after_the_launch_before();
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
@@ -99,6 +112,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
         if (kKeys && a.r.dv) store_any<8>(a.r.dv, a.r.dvt, at, zero);
         if (!kKeys) store_any<8>(a.r.out, a.r.ot, at, zero);
       }
+    give_tmem_back();
     return;
   }
   const int n_rows = u.b - u.a, last = min(u.row0 + own_rows, n_rows) - 1;      // own rows: row0 .. last
@@ -130,18 +144,10 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
       store_any<8>(to, DRAGON_F32, at, zero);
       if (kKeys) store_any<8>(to_v, DRAGON_F32, at, zero);
     }
+    give_tmem_back();
     return;
   }
 
-  if (warp == 9) {
-    __syncwarp();
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  const uint32_t tmem = *tmem_slot;
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {
     if (mbar_wait_warp(bar, parity, abort_flag, a.budget)) return true;
     *abort_flag = 1;
@@ -393,8 +399,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     }
     __syncthreads();
   }
-  __syncwarp();
-  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  give_tmem_back();
 }
 
 template <int kChunks>

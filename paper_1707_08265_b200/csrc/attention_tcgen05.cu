@@ -60,7 +60,8 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const int column = blockIdx.x % a.columns, group = a.r.heads / a.r.kv_heads, heads_here = a.by_heads ? 2 : pack;
   const int head0 = column * heads_here, kvh = head0 / group;
 
-  if (threadIdx.x == 0) {
+  // three warps side by side: barriers, the unit of work, TMEM
+  if (warp == 1 && elected()) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
@@ -88,21 +89,34 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     if (lane == 0) unit = u;
   }
+  if (warp == 9) {
+    __syncwarp();
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
   __syncthreads();
+  fence_after();
   const Unit u = unit;
+  const uint32_t tmem = *tmem_slot;
+  auto give_tmem_back = [&]() {
+    __syncwarp();
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  };
   next_launch_may_come();
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
-    if (kPaged && a.r.splits > 1) return;      // (where the parts are put together)
+    if (kPaged && a.r.splits > 1) { give_tmem_back(); return; }      // (where the parts are put together)
     const int wide = heads_here * a.r.width;
     for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (a.r.out) for (int c = 8 * threadIdx.x; c < wide; c += 8 * kFwdThreads) store_any<8>(a.r.out, a.r.ot, ((size_t)row * a.r.heads + head0) * a.r.width + c, zero);
       if (a.r.lse && threadIdx.x < heads_here) a.r.lse[(size_t)(head0 + threadIdx.x) * a.r.seq.rows + row] = kInf;
     }
+    give_tmem_back();
     return;
   }
   const int n_rows = u.b - u.a;
-  if (kPaged && n_rows * group <= a.few) return;
+  if (kPaged && n_rows * group <= a.few) { give_tmem_back(); return; }
   // the tiles of keys that any row of the unit sees
   const int last_row = min(u.row0 + block_rows, n_rows) - 1;      // (row0 < n_rows)
   const int key_end = a.r.causal ? max(0, min(u.keys, u.first_pos + last_row + 1)) : u.keys;
@@ -115,15 +129,6 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   }
   const bool ragged = u.keys - (j0 + n_tiles - 1) * 128 < 128;      // the last tile has rows behind the sequence's last key
 
-  if (warp == 9) {
-    __syncwarp();
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  fence_before();
-  __syncthreads();
-  fence_after();
-  const uint32_t tmem = *tmem_slot;
   auto wait_warp = [&](uint32_t bar, uint32_t parity) {
     if (mbar_wait_warp(bar, parity, abort_flag, a.budget)) return true;
     *abort_flag = 1;
@@ -364,8 +369,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     __syncthreads();
   }
-  __syncwarp();
-  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  give_tmem_back();
 }
 
 template <bool kPaged, int kChunks> int launch_fwd(const FwdArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t st, const char* who) {
