@@ -21,8 +21,7 @@ int64_t attention_units(int64_t rows, int64_t sequences, int heads, int kv_heads
 namespace {
 
 constexpr int kWriteWarps = 8;
-constexpr int kPartsMost = 64;        // parts of a sequence's keys
-constexpr int kFewCtas = 8;           // CTAs of the kernel for few rows aimed at, for every SM (two at once)
+constexpr int kPartsMost = 128;       // parts of a sequence's keys
 
 struct WriteArgs {
   const uint4* rows[kCachesPerLaunch];
@@ -68,9 +67,15 @@ __global__ void __launch_bounds__(32 * kWriteWarps) cache_write(const __grid_con
 
 // ---- few rows ------------------------------------------------------------------------------------
 
-constexpr int kFewWarps = 4, kFewStages = 3, kFewMost = 32;      // kFewMost: rows (times heads of a group) of a sequence
+constexpr int kFewWarps = 4, kFewStages = 2, kFewMost = 32;      // kFewMost: rows (times heads of a group) of a sequence
 constexpr int few_pitch(int steps) { return steps * 32 + 16; }      // bytes of a key in a stage: an odd number of 16, for ldmatrix
 constexpr int few_smem(int steps, int m) { return std::max(kFewWarps * kFewStages * 2 * 16 * few_pitch(steps), kFewWarps * 16 * m * (16 * steps + 4) * 4) + 16; }
+
+// CTAs of it that an SM holds, by shared memory and registers.  Two stages and a CTA more were faster than three stages (64 sequences of
+// 4000 tokens 160 -> 148 us)
+constexpr int few_resident(int steps, int m) {
+  return std::min(227 * 1024 / (few_smem(steps, m) + 2048), m == 1 ? 5 : steps <= 2 ? 4 : steps <= 4 ? 3 : 2);
+}
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool real) {      // zeros where it is not real
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0) : "memory");
@@ -88,7 +93,7 @@ __device__ __forceinline__ void mma16(float* c, const uint32_t* a, uint32_t b0, 
 __device__ __forceinline__ float exp2_of(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // kSteps: 16 elements of the head each; kM: 16 rows each
-template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps) paged_few(const __grid_constant__ RowArgs a, int few, int columns) {
+template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps, few_resident(kSteps, kM)) paged_few(const __grid_constant__ RowArgs a, int few, int columns) {
   constexpr int kPitch = few_pitch(kSteps), kRows = 16 * kM, kStage = 2 * 16 * kPitch, kOut = 16 * kSteps + 4;
   extern __shared__ __align__(16) unsigned char smem_few[];
   __shared__ float warp_top[kFewWarps][kRows], warp_sum_of[kFewWarps][kRows];
@@ -395,7 +400,7 @@ int parts_of(int64_t units, int64_t room, int64_t ctas, int64_t least) {
   return (int)std::max<int64_t>(1, std::min({(ctas + units - 1) / units, (room + least - 1) / least, (int64_t)kPartsMost}));
 }
 
-PagedPlan plan_paged(int64_t rows, int64_t sequences, bool starts, int64_t room, int heads, int kv_heads, int sm_count) {
+PagedPlan plan_paged(int64_t rows, int64_t sequences, bool starts, int64_t room, int heads, int kv_heads, int width, int sm_count) {
   PagedPlan p = {};
   const int group = heads / kv_heads;
   const int64_t each = rows / sequences * group;      // without starts: rows x group of every sequence
@@ -406,7 +411,10 @@ PagedPlan plan_paged(int64_t rows, int64_t sequences, bool starts, int64_t room,
   p.tiles = starts ? rows * group > p.most_few || !p.few : !p.few;
   if (!p.few) p.most_few = 0;
   p.few_rows = p.most_few > 16 && (starts || each > 16) ? 32 : 16;
-  p.few_splits = p.few ? parts_of(sequences * kv_heads, room, kFewCtas * sm_count, 256) : 1;
+  // few rows: as many parts as the GPU holds at once (one sequence of 100000 tokens: 88 us with 512 CTAs, 79 with the 440 that are there
+  // together); with more sequences than that, whose lengths differ, parts of which some eight CTAs an SM come
+  const int64_t units = sequences * kv_heads, slots = few_resident((width + 31) / 32 * 2, p.few_rows / 16) * (int64_t)sm_count;
+  p.few_splits = p.few ? parts_of(units, room, units <= slots ? slots / units * units : 8 * (int64_t)sm_count, 256) : 1;
   p.tile_splits = p.tiles ? parts_of(attention_units(rows, sequences, heads, kv_heads), room, sm_count, 512) : 1;
   p.join = starts ? p.few_splits > 1 || p.tile_splits > 1 || !p.tiles : p.few_splits > 1 || p.tile_splits > 1;
   return p;
@@ -414,7 +422,7 @@ PagedPlan plan_paged(int64_t rows, int64_t sequences, bool starts, int64_t room,
 PagedPlan plan_of(const Step& s, const std::vector<MemRef>& mems, int sm_count) {
   const Shape &q = mems[s.rd[pa::Q]].shape, &pages = mems[s.rd[pa::PAGES]].shape;
   return plan_paged(q.d[0], pages.d[0], s.rd[pa::STARTS] >= 0, std::min<int64_t>(pages.d[1] * (int64_t)s.num[pn::PAGE], 0x7fffffff), (int)s.num[pn::HEADS],
-                    (int)s.num[pn::KV_HEADS], sm_count);
+                    (int)s.num[pn::KV_HEADS], (int)(q.d[1] / (int64_t)s.num[pn::HEADS]), sm_count);
 }
 
 template <int kSteps> int launch_few(const RowArgs& a, const PagedPlan& p, int most_rows, cudaStream_t st) {
