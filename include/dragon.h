@@ -122,7 +122,8 @@ enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2, DRAGON_F8E4M3 = 3 };
  *                          position (padding in front) writes nothing; nor does a position behind P pages or a page
  *                          number outside of the pool, which set the function status to DRAGON_ERR_INVALID_ARG.  Fetching
  *                          cache' into the very memory that was fed as cache (dragon_function_can_alias) writes the rows
- *                          in place; otherwise the cache is copied first.
+ *                          in place; otherwise the cache is copied first.  New rows have places of their own: of two with the
+ *                          same place either's elements may be kept.
  *   PAGED_ATTENTION(q, kcache, vcache, pages, lengths [, starts]) attrs {heads, kv_heads = heads, page, window = 0, scale = 0}
  *                          q [T, heads*D], kcache, vcache bf16 [pages_in_pool * page, kv_heads*D] that hold every token,
  *                          the new ones too; the table as for CACHE_WRITE; y like q.  The row at position p sees positions

@@ -1,6 +1,7 @@
 // Attention one row at a time: a warp computes a row of a head from the keys it sees and nothing else.  The tensor-core kernels
 // multiply whole tiles, so that a masked key's infinities and NaN reach a row as 0 x inf; a row whose result is not finite is
-// computed again here, which gives what the formula gives.
+// computed again here, which gives what the formula gives.  (Where everything is NaN, as in a training run that has come apart, it
+// ends at the first key.)
 #pragma once
 #include <cuda_runtime.h>
 
@@ -96,6 +97,7 @@ template <bool kPaged> __device__ __noinline__ void attend_row(const RowArgs& a,
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] = acc[e] * f + (ok && lane + 32 * e < a.width ? p * at(a.v, kb + lane + 32 * e) : 0.f);
     top = now;
+    if (sum != sum) break;      // NaN from here on whatever follows
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;      // (a NaN stays one)
 #pragma unroll
@@ -135,6 +137,7 @@ __device__ __noinline__ void dq_of_row(const RowArgs& a, int h, int row, int lan
     const float p = exp2f(warp_sum(x) * a.scale - lse), ds = p * (warp_sum(dp) - delta) * a.raw_scale;
 #pragma unroll
     for (int e = 0; e < 4; ++e) dq[e] += ds * k[e];
+    if (ds != ds) break;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) if (a.out && lane + 32 * e < a.width) put(a.out, a.ot, base + lane + 32 * e, dq[e]);
@@ -155,8 +158,9 @@ __device__ __noinline__ void dkv_of_row(const RowArgs& a, int kvh, int row, int 
   int r0 = 0, r1 = 0;
   if (s >= 0) a.seq.rows_of(s, &r0, &r1);
   const int j = row - r0, n = r1 - r0, i0 = a.causal ? j : 0, i1 = a.window ? min(n, j + a.window) : n;
-  for (int h = kvh * group; s >= 0 && h < (kvh + 1) * group; ++h)
-    for (int i = i0; i < i1; ++i) {
+  bool open = s >= 0;      // until everything is NaN
+  for (int h = kvh * group; open && h < (kvh + 1) * group; ++h)
+    for (int i = i0; open && i < i1; ++i) {
       const size_t base = (size_t)(r0 + i) * a.heads * a.width + (size_t)h * a.width, st = (size_t)h * a.seq.rows + r0 + i;
       float x = 0.f, dp = 0.f, q[4], d[4];
 #pragma unroll
@@ -170,6 +174,7 @@ __device__ __noinline__ void dkv_of_row(const RowArgs& a, int kvh, int row, int 
       const float p = exp2f(warp_sum(x) * a.scale - a.lse[st]), ds = p * (warp_sum(dp) - a.delta[st]) * a.raw_scale;
 #pragma unroll
       for (int e = 0; e < 4; ++e) { dk[e] += ds * q[e]; dv[e] += p * d[e]; }
+      open = p == p;
     }
 #pragma unroll
   for (int e = 0; e < 4; ++e)

@@ -305,3 +305,21 @@ def test_a_cache_beyond_32_bits(new):
     for c, w in ((kc, want[1]), (vc, want[2])):
         for j, at in enumerate(numbers):
             assert np.array_equal(c[at * page:(at + 1) * page].double().cpu().numpy(), w[j * page:(j + 1) * page])
+
+
+def test_everything_nan_ends_soon():
+    """A training run that has come apart: every row is computed by itself, and ends at its first key.  (Every row over all of its keys would
+    take some seconds here.)"""
+    import torch
+    g, ids, inputs, outputs = attention_graph(32768, 8, 2, 128, grad=True)
+    dev = [torch.full(g.shape(t), float("nan"), dtype=torch.bfloat16, device="cuda") for t in inputs]
+    outs = [torch.zeros(g.shape(t), dtype=torch.bfloat16, device="cuda") for t in outputs]
+    f = B.Graph.from_desc(g.desc).function(inputs, outputs)
+    f.run_torch(dev, outs)
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    f.run_torch(dev, outs)
+    end.record()
+    torch.cuda.synchronize()
+    assert f.status() == 0 and all(bool(torch.isnan(o).all()) for o in outs)
+    assert start.elapsed_time(end) < 200
