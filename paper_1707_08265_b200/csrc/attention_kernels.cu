@@ -7,7 +7,7 @@
 #include "attention_rows.h"
 
 namespace dragon {
-int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, cudaStream_t st, const char* who);
+int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, int sm_count, cudaStream_t st, const char* who);
 int launch_attention_backward(const RowArgs& rows, cudaStream_t st);
 int64_t attention_units(int64_t rows, int64_t sequences, int heads, int kv_heads);
 void attention_bwd_units(int64_t rows, int64_t sequences, int heads, int kv_heads, int64_t* row_units, int64_t* key_units, int* tile_rows);
@@ -173,7 +173,7 @@ int launch_attention(const StepRun& r) {
   a.part_lse = a.part + (size_t)a.splits * a.seq.rows * a.heads * a.width;
   if (r.s.wr.size() > at::REST) a.rest = reinterpret_cast<unsigned short*>(r.wr(at::REST));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(r.stream);
-  const int rc = launch_attention_forward(a, false, a.seq.rows, 0, st, "Attention");
+  const int rc = launch_attention_forward(a, false, a.seq.rows, 0, r.sm_count, st, "Attention");
   if (rc != DRAGON_OK || a.splits == 1) return rc;
   const long long items = (long long)a.seq.rows * a.heads;
   return launch_behind(attention_join, dim3((unsigned)((items + 7) / 8)), dim3(256), 0, st, "Attention", a);

@@ -1,19 +1,19 @@
 // Attention's forward pass on the tensor cores: y = softmax(scale q k^T) v over packed sequences or over a paged cache.
 // Hand-written for sm_100a.
 //
-// A CTA works on two tiles of 128 query rows that see the same keys: where the heads of a group are a power of two, all of them
-// for 128 / group neighbouring rows of the sequence in each tile; otherwise the same 128 rows of two heads of a group, or 256 rows
+// A CTA works on one or two tiles of 128 query rows that see the same keys: where the heads of a group are a power of two, all of them
+// for 128 / group neighbouring rows of the sequence in each tile; otherwise the same 128 rows of two heads of a group, or rows
 // of one head.  Keys and values pass once, 128 at a time:
 //   S_t = Q_t K^T              tcgen05.mma, both operands in shared memory (TMA, 128-byte swizzle), S_t in TMEM
 //   P_t = exp2(scale' S_t - m) one thread a row: the running maximum m and sum stay in its registers; P_t goes back over S_t as
 //                              bf16 (its sum is taken in fp32 before the rounding)
 //   O_t += P_t V               tcgen05.mma with P_t as the A operand out of TMEM, V as it lies in memory (MN-major)
-// While the softmax threads of one tile work, the tensor unit works for the other.  m only moves when a row's maximum has grown
+// While the softmax threads of one tile work, the tensor unit works for the other (of the CTA, or of the SM's other CTA).  m only moves when a row's maximum has grown
 // by more than 2^8 (P_t and the sum then stay below 2^8 times their scale, far inside bf16 and fp32): O_t in TMEM is rescaled
 // that seldom that the softmax threads do it themselves.  S_t of the next keys is issued behind O_t's product, so a completed
 // S_t says that O_t may be touched.  Where there are few units of work (few rows or heads, long contexts) the keys of one are split over
 // several CTAs.
-// Warps: 0..3 and 4..7 softmax of tile 0 and 1 (a warp its TMEM lanes), 8 TMA, 9 MMA.  Every wait is bounded.
+// Warps: four softmax warps a tile (a warp its TMEM lanes), then TMA, MMA.  Every wait is bounded.
 #include <algorithm>
 #include <cstdlib>
 
@@ -23,9 +23,9 @@
 namespace dragon {
 namespace {
 
-constexpr int kFwdThreads = 320;
-constexpr int fwd_stages(int chunks) { return chunks == 1 ? 4 : 2; }                          // of K and of V each
-constexpr size_t fwd_smem(int chunks) { return 1024 + (size_t)(2 + 2 * fwd_stages(chunks)) * chunks * kChunkBytes + 512; }
+constexpr int fwd_threads(int tiles) { return 128 * tiles + 64; }
+constexpr int fwd_stages(int tiles, int chunks) { return tiles * (chunks == 1 ? 2 : 1); }      // of K and of V each
+constexpr size_t fwd_smem(int tiles, int chunks) { return 1024 + (size_t)(tiles + 2 * fwd_stages(tiles, chunks)) * chunks * kChunkBytes + 512; }
 constexpr float kRescale = 8.f;
 
 struct FwdArgs {
@@ -40,15 +40,15 @@ struct FwdArgs {
   int drop_first_load;
 };
 
-template <bool kPaged, int kChunks>
-__global__ void __launch_bounds__(kFwdThreads, 1)
+template <bool kPaged, int kTiles, int kChunks>
+__global__ void __launch_bounds__(fwd_threads(kTiles), 3 - kTiles)
 attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ FwdArgs a) {
-  constexpr int kSt = fwd_stages(kChunks);
+  constexpr int kSt = fwd_stages(kTiles, kChunks), kTmaWarp = 4 * kTiles, kMmaWarp = kTmaWarp + 1;
   constexpr uint32_t kTile = kChunks * kChunkBytes;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t q_at = base, k_at = base + 2 * kTile, v_at = k_at + kSt * kTile;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (base - raw) + (2 + 2 * kSt) * kTile);
+  const uint32_t q_at = base, k_at = base + kTiles * kTile, v_at = k_at + kSt * kTile;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_raw + (base - raw) + (kTiles + 2 * kSt) * kTile);
   const uint32_t q_full = smem_u32(bars), k_full = q_full + 16, k_empty = k_full + 8 * kSt, v_full = k_empty + 8 * kSt, v_empty = v_full + 8 * kSt;
   const uint32_t s_full = v_empty + 8 * kSt, p_full = s_full + 16, o_full = p_full + 32, v_clean = o_full + 16, drain = v_clean + 8;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 4 * kSt);
@@ -56,7 +56,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   __shared__ Unit unit;
   if (kPaged) after_the_launch_before();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int pack = 1 << a.pack_shift, tile_rows = 128 >> a.pack_shift, block_rows = a.by_heads ? 128 : 2 * tile_rows;      // rows: of the sequence
+  const int pack = 1 << a.pack_shift, tile_rows = 128 >> a.pack_shift, block_rows = a.by_heads ? 128 : kTiles * tile_rows;      // rows: of the sequence
   const int column = blockIdx.x % a.columns, group = a.r.heads / a.r.kv_heads, heads_here = a.by_heads ? 2 : pack;
   const int head0 = column * heads_here, kvh = head0 / group;
 
@@ -65,7 +65,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_v) : "memory");
-    for (int t = 0; t < 2; ++t) { mbar_init(q_full + 8 * t, 1); mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 16 * t, 4); mbar_init(p_full + 16 * t + 8, 4); mbar_init(o_full + 8 * t, 1); }
+    for (int t = 0; t < kTiles; ++t) { mbar_init(q_full + 8 * t, 1); mbar_init(s_full + 8 * t, 1); mbar_init(p_full + 16 * t, 4); mbar_init(p_full + 16 * t + 8, 4); mbar_init(o_full + 8 * t, 1); }
     for (int s = 0; s < kSt; ++s) { mbar_init(k_full + 8 * s, 1); mbar_init(k_empty + 8 * s, 1); mbar_init(v_full + 8 * s, 1); mbar_init(v_empty + 8 * s, 1); }
     mbar_init(v_clean, 32);
     mbar_init(drain, 1);
@@ -89,9 +89,9 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     if (lane == 0) unit = u;
   }
-  if (warp == 9) {
+  if (warp == kMmaWarp) {
     __syncwarp();
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(256u * kTiles) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_before();
@@ -101,7 +101,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   const uint32_t tmem = *tmem_slot;
   auto give_tmem_back = [&]() {
     __syncwarp();
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u * kTiles) : "memory");
   };
   next_launch_may_come();
   if (u.seq < 0) {      // rows of no sequence: zeros, shared out among the units that are left over
@@ -109,7 +109,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const int wide = heads_here * a.r.width;
     for (int i = u.spare, row; (row = row_of_none(a.r.seq, i)) >= 0; i += u.spares) {
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (a.r.out) for (int c = 8 * threadIdx.x; c < wide; c += 8 * kFwdThreads) store_any<8>(a.r.out, a.r.ot, ((size_t)row * a.r.heads + head0) * a.r.width + c, zero);
+      if (a.r.out) for (int c = 8 * threadIdx.x; c < wide; c += 8 * fwd_threads(kTiles)) store_any<8>(a.r.out, a.r.ot, ((size_t)row * a.r.heads + head0) * a.r.width + c, zero);
       if (a.r.lse && threadIdx.x < heads_here) a.r.lse[(size_t)(head0 + threadIdx.x) * a.r.seq.rows + row] = kInf;
     }
     give_tmem_back();
@@ -136,9 +136,9 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     return false;
   };
   int issued_k = 0, issued_v = 0;
-  if (warp == 8) {
+  if (warp == kTmaWarp) {
     if (n_tiles > 0 && elected()) {
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < kTiles; ++t) {
         mbar_expect_tx(q_full + 8 * t, kTile);
         for (int c = 0; c < kChunks; ++c)
           tma_load_3d(q_at + t * kTile + c * kChunkBytes, &tm_q, 64 * c, a.by_heads ? head0 + t : head0, u.a + u.row0 + (a.by_heads ? 0 : tile_rows * t), q_full + 8 * t);
@@ -189,7 +189,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         mbar_arrive(v_clean);
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == kMmaWarp) {
     if (n_tiles > 0) {
       const int k_steps = (a.r.width + 15) / 16, n_out = 16 * k_steps;
       const uint32_t idesc_s = idesc_bf16(128, 128, false), idesc_o = idesc_bf16(128, n_out, true);
@@ -203,7 +203,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         __syncwarp();
       };
       bool ok = wait_warp(k_full, 0);
-      for (int t = 0; t < 2 && ok; ++t) {
+      for (int t = 0; t < kTiles && ok; ++t) {
         ok = wait_warp(q_full + 8 * t, 0);
         if (ok) product_s(t, 0);
       }
@@ -212,14 +212,17 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         const int s = j % kSt;
         ok = wait_warp(v_full + 8 * s, (j / kSt) & 1);
         if (ok && ragged && j == n_tiles - 1) ok = wait_warp(v_clean, 0);
-        for (int t = 0; t < 2 && ok; ++t) {
+        for (int t = 0; t < kTiles && ok; ++t) {
           if (!(ok = wait_warp(p_full + 16 * t, j & 1))) break;
           fence_after();
-          if (elected()) product_over_rows<32, 0, 4>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, j > 0);
+          if (elected()) product_over_rows<32, 0, 4>(tmem + 128 * (kTiles + t), tmem + 128 * t, v_at + s * kTile, idesc_o, j > 0);
           __syncwarp();
           if (!(ok = wait_warp(p_full + 16 * t + 8, j & 1))) break;
           fence_after();
-          if (elected()) product_over_rows<32, 4, 8>(tmem + 256 + 128 * t, tmem + 128 * t, v_at + s * kTile, idesc_o, true);
+          if (elected()) {
+            product_over_rows<32, 4, 8>(tmem + 128 * (kTiles + t), tmem + 128 * t, v_at + s * kTile, idesc_o, true);
+            if (t == kTiles - 1) umma_commit(v_empty + 8 * s);
+          }
           __syncwarp();
           if (j + 1 < n_tiles) {
             if (t == 0 && !(ok = wait_warp(k_full + 8 * ((j + 1) % kSt), ((j + 1) / kSt) & 1))) break;
@@ -228,10 +231,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             commit(o_full + 8 * t);
           }
         }
-        if (ok) {
-          commit(v_empty + 8 * s);
-          if (j + 1 < n_tiles) commit(k_empty + 8 * ((j + 1) % kSt));
-        }
+        if (ok && j + 1 < n_tiles) commit(k_empty + 8 * ((j + 1) % kSt));
       }
     }
   } else {
@@ -242,7 +242,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const bool mine = i < n_rows;
     // the keys that the row sees
     const int hi = !mine ? 0 : a.r.causal ? min(pos + 1, u.keys) : u.keys, lo = a.r.window ? max(0, pos - a.r.window + 1) : 0;
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + 256 + 128 * t;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + lanes + 128 * t, o_at = tmem + lanes + 128 * (kTiles + t);
     float top = -kInf, sum = 0.f;
     bool ok = true;
     for (int j = 0; j < n_tiles; ++j) {
@@ -357,13 +357,13 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   fence_before();
   __syncthreads();
   if (*abort_flag) {      // an unwind: copies and products that have been asked for end before their memory goes away
-    if (warp == 9) {
+    if (warp == kMmaWarp) {
       if (elected()) umma_commit(drain);
       __syncwarp();
       mbar_wait_warp(drain, 0, abort_flag + 1, kWaitBudgetCycles);
     }
-    if (threadIdx.x == 256) {
-      for (int t = 0; t < 2 && n_tiles > 0; ++t) mbar_wait(q_full + 8 * t, 0, abort_flag + 1);
+    if (threadIdx.x == 32 * kTmaWarp) {
+      for (int t = 0; t < kTiles && n_tiles > 0; ++t) mbar_wait(q_full + 8 * t, 0, abort_flag + 1);
       for (int k = std::max(a.drop_first_load ? 1 : 0, issued_k - kSt); k < issued_k; ++k) mbar_wait(k_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
       for (int k = std::max(0, issued_v - kSt); k < issued_v; ++k) mbar_wait(v_full + 8 * (k % kSt), (k / kSt) & 1, abort_flag + 1);
     }
@@ -372,15 +372,17 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
   give_tmem_back();
 }
 
-template <bool kPaged, int kChunks> int launch_fwd(const FwdArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t st, const char* who) {
+template <bool kPaged, int kTiles, int kChunks> int launch_fwd(const FwdArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t st, const char* who) {
   static bool set[64] = {};
-  const int rc = allow_smem(reinterpret_cast<const void*>(attention_fwd<kPaged, kChunks>), fwd_smem(kChunks), set, who);
+  const auto kernel = attention_fwd<kPaged, kTiles, kChunks>;
+  constexpr size_t bytes = fwd_smem(kTiles, kChunks);
+  const int rc = allow_smem(reinterpret_cast<const void*>(kernel), bytes, set, who);
   if (rc != DRAGON_OK) return rc;
   const long long grid = (long long)a.blocks * a.columns;
   if (grid > 0x7fffffffLL) { set_error("%s: too many blocks of rows", who); return DRAGON_ERR_UNSUPPORTED; }
-  const dim3 ctas((unsigned)grid, a.r.splits);
-  if (kPaged) return launch_behind(attention_fwd<kPaged, kChunks>, ctas, dim3(kFwdThreads), fwd_smem(kChunks), st, who, q, k, v, a);
-  attention_fwd<kPaged, kChunks><<<ctas, kFwdThreads, fwd_smem(kChunks), st>>>(q, k, v, a);
+  const dim3 ctas((unsigned)grid, a.r.splits), threads(fwd_threads(kTiles));
+  if (kPaged) return launch_behind(kernel, ctas, threads, bytes, st, who, q, k, v, a);
+  kernel<<<ctas, threads, bytes, st>>>(q, k, v, a);
   return launched(who);
 }
 
@@ -393,16 +395,34 @@ int64_t attention_units(int64_t rows, int64_t sequences, int heads, int kv_heads
   return std::max<int64_t>(sequences, (rows + block - 1) / block) * (packs(group) ? kv_heads : group % 2 == 0 ? heads / 2 : heads);
 }
 
+// Tiles of a CTA: one, with two CTAs on an SM, or two that share the copies of keys and values.  Two CTAs overlap start and end of one
+// with the other's work, and their units are half as long; heads of 64 and less: always (1 x 16384 rows, 8 heads of 64: 415 us with two
+// tiles, 392 with one).  With wider heads there is room for one stage of keys and values only: two tiles (16384 rows, 8 heads on 2 of
+// 128: 420 us, 445 with one), but where a unit meets few keys (1 x 12001, window 1024, heads of 96: 57 us with two tiles, 51 with one), where
+// a causal call has units for less than two rounds of the GPU (7807 rows, 8 heads: 161 and 144), or the second tile had no rows (15 new rows
+// of 14 sequences of 4200, 9 heads on 3: 102 and 68).
+static int tiles_of(const RowArgs& r, bool paged, int sm_count) {
+  if (r.width <= 64) return 1;
+  const int group = r.heads / r.kv_heads, count = std::max(1, r.seq.count);
+  const int64_t each = (r.seq.rows + count - 1) / count, room = paged ? std::min<int64_t>((int64_t)r.pages.most << r.pages.shift, 0x7fffffff) : each;
+  const bool falling = r.causal && !r.window && !paged;
+  const int64_t pairs = ((r.window ? std::min<int64_t>(room, (int64_t)r.window + 128) : room) + 127) / 128;
+  if (each * (packs(group) ? group : 1) <= 128 || pairs <= (falling ? 32 : 16)) return 1;
+  return falling && attention_units(r.seq.rows, count, r.heads, r.kv_heads) < 2 * (int64_t)sm_count ? 1 : 2;
+}
+
 // rows: what the row functions need as well; key_rows: rows of k and v in memory; few: rows x group of a sequence up to which another kernel has it
-int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, cudaStream_t st, const char* who) {
+int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, int sm_count, cudaStream_t st, const char* who) {
   FwdArgs a = {};
   a.r = rows;
   const int group = rows.heads / rows.kv_heads;
   const bool packed = packs(group);
   while (packed && (1 << a.pack_shift) < group) ++a.pack_shift;
-  a.by_heads = !packed && group % 2 == 0;
+  const bool wide = rows.width > 64;
+  const int tiles = tiles_of(rows, paged, sm_count);
+  a.by_heads = tiles == 2 && !packed && group % 2 == 0;
   a.columns = packed ? rows.kv_heads : a.by_heads ? rows.heads / 2 : rows.heads;
-  const int block = a.by_heads ? 128 : 256 >> a.pack_shift;
+  const int block = a.by_heads ? 128 : 128 * tiles >> a.pack_shift;
   count_blocks(rows.seq, block, &a.blocks, &a.each_blocks);
   a.few = few;
   wait_settings("DRAGON_ATTENTION", &a.budget, &a.drop_first_load);
@@ -413,9 +433,12 @@ int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, 
     set_error("%s: cannot encode the TMA descriptors (no CUDA driver?)", who);
     return DRAGON_ERR_CUDA;
   }
-  const bool wide = rows.width > 64;
-  return paged ? (wide ? launch_fwd<true, 2>(a, q, k, v, st, who) : launch_fwd<true, 1>(a, q, k, v, st, who))
-               : (wide ? launch_fwd<false, 2>(a, q, k, v, st, who) : launch_fwd<false, 1>(a, q, k, v, st, who));
+  const auto launch = [&](auto t, auto c) {
+    return paged ? launch_fwd<true, t, c>(a, q, k, v, st, who) : launch_fwd<false, t, c>(a, q, k, v, st, who);
+  };
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 2> two;
+  return !wide ? launch(one, one) : tiles == 1 ? launch(one, two) : launch(two, two);
 }
 
 }  // namespace dragon

@@ -16,7 +16,7 @@
 #include "attention_tiles.h"
 
 namespace dragon {
-int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, cudaStream_t st, const char* who);
+int launch_attention_forward(const RowArgs& rows, bool paged, int64_t key_rows, int few, int sm_count, cudaStream_t st, const char* who);
 int64_t attention_units(int64_t rows, int64_t sequences, int heads, int kv_heads);
 namespace {
 
@@ -523,7 +523,7 @@ int launch_paged_attention(const StepRun& r) {
   }
   if (rc == DRAGON_OK && p.tiles) {
     a.splits = p.tile_splits;
-    rc = launch_attention_forward(a, true, r.mems[r.s.rd[pa::K]].shape.d[0], p.most_few, st, "PagedAttention");
+    rc = launch_attention_forward(a, true, r.mems[r.s.rd[pa::K]].shape.d[0], p.most_few, r.sm_count, st, "PagedAttention");
   }
   if (rc == DRAGON_OK && p.join) {
     const bool by_sequence = a.seq.starts && p.tiles && p.tile_splits == 1;
