@@ -15,7 +15,7 @@
 // One tile pair is 128 x 128; two warps share a row (64 columns each).  The products are issued in an order in which the tensor
 // unit has work while the threads compute: keys: dV(i), S(i+1), dK(i), dP(i+1); rows: S(i+1), dP(i+1), dQ(i) (dP has two buffers).
 // Warps: 0..7 mathematics, 8 TMA, 9 MMA.  Every wait is bounded.
-// Bound: keys, a round has 2048 cycles of products and takes 3245; rows, 1536 and 2288; what is left over is one product waiting for the
+// Bound: keys, a round has 2048 cycles of products and takes about 3200 (3245 before the products of half of P^T started early); rows, 1536 and 2288; what is left over is one product waiting for the
 // threads' results of another.  16384 causal rows, 8 heads on 2 of 128: 1410 us, 0.97 PFLOP/s of the formula's five products (1.36 of the
 // seven).
 // Both kinds are one launch, keys first: theirs are the longest (all heads of a group), and the rows' fill the SMs that run out of them.
@@ -58,8 +58,8 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   uint64_t* bars = reinterpret_cast<uint64_t*>(stats + (kKeys ? kSt1 * 256 : 0));
   const uint32_t x_full = smem_u32(bars), y1_full = x_full + 8, y1_empty = y1_full + 8 * kSt1, y2_full = y1_empty + 8 * kSt1, y2_empty = y2_full + 8 * kSt2;
   const uint32_t st_full = y2_empty + 8 * kSt2, st_empty = st_full + 8 * kSt1;
-  const uint32_t s_full = st_empty + 8 * kSt1, dp_full = s_full + 8, p_full = dp_full + 16, ds_full = p_full + 8, acc_full = ds_full + 16, drain = acc_full + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 4 * kSt1 + 2 * kSt2 + 8);
+  const uint32_t s_full = st_empty + 8 * kSt1, dp_full = s_full + 8, p_full = dp_full + 16, ds_full = p_full + 16, acc_full = ds_full + 16, drain = acc_full + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 4 * kSt1 + 2 * kSt2 + 9);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   __shared__ Unit unit;
   __shared__ unsigned again[8];
@@ -80,7 +80,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     mbar_init(x_full, 1);
     for (int s = 0; s < kSt1; ++s) { mbar_init(y1_full + 8 * s, 1); mbar_init(y1_empty + 8 * s, 1); mbar_init(st_full + 8 * s, 32); mbar_init(st_empty + 8 * s, 8); }
     for (int s = 0; s < kSt2; ++s) { mbar_init(y2_full + 8 * s, 1); mbar_init(y2_empty + 8 * s, 1); }
-    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(dp_full + 8, 1); mbar_init(p_full, 8); mbar_init(ds_full, 8); mbar_init(ds_full + 8, 8); mbar_init(acc_full, 1); mbar_init(drain, 1);
+    mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(dp_full + 8, 1); mbar_init(p_full, 8); mbar_init(p_full + 8, 8); mbar_init(ds_full, 8); mbar_init(ds_full + 8, 8); mbar_init(acc_full, 1); mbar_init(drain, 1);
     abort_flag[0] = abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -241,8 +241,22 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
     for (int i = 0; i < n && ok; ++i) {
       const int s = i % kSt1, s2 = i % kSt2;
       if (kKeys) {
+        // rows 0..31 and 64..95 of the tile, then the others
         if (!(ok = wait_warp(p_full, i & 1))) break;
-        accumulate(kAcc2, kS, y2 + s2 * kTile, i > 0, y2_empty + 8 * s2);
+        fence_after();
+        if (elected()) {
+          product_over_rows<64, 0, 2>(tmem + kAcc2, tmem + kS, y2 + s2 * kTile, idesc_acc, i > 0);
+          product_over_rows<64, 4, 6>(tmem + kAcc2, tmem + kS, y2 + s2 * kTile, idesc_acc, true);
+        }
+        __syncwarp();
+        if (!(ok = wait_warp(p_full + 8, i & 1))) break;
+        fence_after();
+        if (elected()) {
+          product_over_rows<64, 2, 4>(tmem + kAcc2, tmem + kS, y2 + s2 * kTile, idesc_acc, true);
+          product_over_rows<64, 6, 8>(tmem + kAcc2, tmem + kS, y2 + s2 * kTile, idesc_acc, true);
+          umma_commit(y2_empty + 8 * s2);
+        }
+        __syncwarp();
         if (i + 1 < n && !(ok = issue_s(i + 1))) break;
         if (!(ok = wait_warp(ds_full, i & 1))) break;
         accumulate(kAcc1, kDp, y1 + s * kTile, i > 0, y1_empty + 8 * s);
@@ -287,55 +301,68 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
       if (ok && kKeys) ok = wait_warp(st_full + 8 * (i % kSt1), (i / kSt1) & 1);
       if (!ok) break;
       fence_after();
+      // 32 columns at a time: the next ones are on their way out of TMEM, and results into it, while these are worked on
+      const bool all_seen = __all_sync(0xffffffffu, lo <= 0 && hi >= 64);
+      const uint32_t s_at = tmem + lanes + kS + 64 * half;
       uint32_t v[64];
       float p[64];
-      tmem_load32(tmem + lanes + kS + 64 * half, v);
-      tmem_load32(tmem + lanes + kS + 64 * half + 32, v + 32);
-      tmem_loaded32(v);
-      tmem_loaded32(v + 32);
-      if (!kKeys) {
+      tmem_load32(s_at, v);
+      if (kKeys) tmem_loaded32(v);
+      tmem_load32(s_at + 32, v + 32);
+      if (!kKeys) {      // (the next S may be written as soon as this one has been read)
+        tmem_loaded32(v);
+        tmem_loaded32(v + 32);
         fence_before();
         __syncwarp();
         mbar_arrive_if(p_full, lane == 0);
       }
 #pragma unroll
-      for (int c = 0; c < 64; c += 4) {
-        float4 l = make_float4(-lse, -lse, -lse, -lse);
-        if (kKeys) l = st[c / 4];
-        const float2 x = both(fma_pair(pair_of(v[c], v[c + 1]), factor, pair_of(l.x, l.y))), y = both(fma_pair(pair_of(v[c + 2], v[c + 3]), factor, pair_of(l.z, l.w)));
-        p[c] = exp2_fast(x.x); p[c + 1] = exp2_fast(x.y); p[c + 2] = exp2_fast(y.x); p[c + 3] = exp2_fast(y.y);
-      }
-      if (!__all_sync(0xffffffffu, lo <= 0 && hi >= 64)) {
+      for (int h = 0; h < 64; h += 32) {
+        if (kKeys && h) tmem_loaded32(v + 32);
 #pragma unroll
-        for (int c = 0; c < 64; ++c) if (c < lo || c >= hi) p[c] = 0.f;
-      }
-      if (kKeys) {
+        for (int c = h; c < h + 32; c += 4) {
+          float4 l = make_float4(-lse, -lse, -lse, -lse);
+          if (kKeys) l = st[c / 4];
+          const float2 x = both(fma_pair(pair_of(v[c], v[c + 1]), factor, pair_of(l.x, l.y))), y = both(fma_pair(pair_of(v[c + 2], v[c + 3]), factor, pair_of(l.z, l.w)));
+          p[c] = exp2_fast(x.x); p[c + 1] = exp2_fast(x.y); p[c + 2] = exp2_fast(y.x); p[c + 3] = exp2_fast(y.y);
+        }
+        if (!all_seen) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) v[c] = bf16_pair(p[2 * c], p[2 * c + 1]);
-        tmem_st32(tmem + lanes + kS + 64 * half, v);
-        tmem_st_wait();
-        fence_before();
-        __syncwarp();
-        mbar_arrive_if(p_full, lane == 0);
+          for (int c = h; c < h + 32; ++c) if (c < lo || c >= hi) p[c] = 0.f;
+        }
+        if (kKeys) {
+          uint32_t w[16];
+#pragma unroll
+          for (int c = 0; c < 16; ++c) w[c] = bf16_pair(p[h + 2 * c], p[h + 2 * c + 1]);
+          tmem_st16(s_at + h / 2, w);
+          tmem_st_wait();
+          fence_before();
+          __syncwarp();
+          mbar_arrive_if(p_full + h / 4, lane == 0);      // (the products of the first half start while the second is worked on)
+        }
       }
       const uint32_t dp = tmem + lanes + kDp + (kKeys ? 0 : 128 * (i & 1)) + 64 * half;
       ok = wait_warp(dp_full + (kKeys ? 0 : 8 * (i & 1)), (kKeys ? i : i >> 1) & 1);
       if (!ok) break;
       fence_after();
       tmem_load32(dp, v);
-      tmem_load32(dp + 32, v + 32);
       tmem_loaded32(v);
-      tmem_loaded32(v + 32);
+      tmem_load32(dp + 32, v + 32);
 #pragma unroll
-      for (int c = 0; c < 64; c += 4) {
-        float4 d = make_float4(-delta, -delta, -delta, -delta);
-        if (kKeys) d = st[32 + c / 4];
-        const float2 x = both(mul_pair(pair_of(p[c], p[c + 1]), add_pair(pair_of(v[c], v[c + 1]), pair_of(d.x, d.y))));
-        const float2 y = both(mul_pair(pair_of(p[c + 2], p[c + 3]), add_pair(pair_of(v[c + 2], v[c + 3]), pair_of(d.z, d.w))));
-        v[c / 2] = bf16_pair(x.x, x.y);
-        v[c / 2 + 1] = bf16_pair(y.x, y.y);
+      for (int h = 0; h < 64; h += 32) {
+        if (h) tmem_loaded32(v + 32);
+        uint32_t w[16];
+#pragma unroll
+        for (int c = h; c < h + 32; c += 4) {
+          float4 d = make_float4(-delta, -delta, -delta, -delta);
+          if (kKeys) d = st[32 + c / 4];
+          const float2 x = both(mul_pair(pair_of(p[c], p[c + 1]), add_pair(pair_of(v[c], v[c + 1]), pair_of(d.x, d.y))));
+          const float2 y = both(mul_pair(pair_of(p[c + 2], p[c + 3]), add_pair(pair_of(v[c + 2], v[c + 3]), pair_of(d.z, d.w))));
+          w[(c - h) / 2] = bf16_pair(x.x, x.y);
+          w[(c - h) / 2 + 1] = bf16_pair(y.x, y.y);
+        }
+        tmem_st16(dp + h / 2, w);
       }
-      tmem_st32(dp, v);
       tmem_st_wait();
       fence_before();
       __syncwarp();
