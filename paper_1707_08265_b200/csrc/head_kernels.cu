@@ -247,6 +247,7 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
         if (norm) {
           const float q = sum_of(fma_pair(x[0], x[0], mul_pair(x[1], x[1])), fma_pair(x[2], x[2], mul_pair(x[3], x[3])));
           inv = rsqrtf(sum_over_lanes<kLanes>(q, lanes) * inv_width + jb.eps);
+          if (kBack && !ok) inv = 0.f;      // (lanes without a head: an infinite root times their zeros would go into dg)
         }
         const Pair r = twice(inv);
         if (!kBack) {
