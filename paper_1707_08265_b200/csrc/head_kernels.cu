@@ -2,7 +2,7 @@
 //
 //   u = x / sqrt(mean(x^2) + eps) * g;  y = amplitude (a cos t - b sin t, b cos t + a sin t) over pairs (a, b) of u's first dims
 //   elements, t = position * f_i.  Backwards, with d = the rotation by -t of dy:
-//   dg = sum over rows and heads of d x r,  dx = r (d g) - x r^3 mean(d g x),  r = 1 / sqrt(mean(x^2) + eps).
+//   dg = sum over rows and heads of d x r,  dx = r (d g - x r mean(d g x r)),  r = 1 / sqrt(mean(x^2) + eps).
 //
 // Angles: f_i / 2 pi is kept as a 64-bit fraction of a turn, so position * f_i modulo one turn is one wrapping integer product
 // (no rounding grows with the position); its top 32 bits go through sincospi in fp32.  They are the same for every head of a
@@ -295,15 +295,16 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
           for (int p = 0; p < 4; ++p) v[p] = x[p];
         }
         if (kBack && norm) {
-          Pair t[4];
+          // on the normalised values u = x r: no power of r above the first, which alone may leave fp32's range (heads of 1e13 and more)
+          Pair t[4], u[4];
 #pragma unroll
-          for (int p = 0; p < 4; ++p) t[p] = mul_pair(v[p], g[p]);
-          const float m = sum_of(fma_pair(t[0], x[0], mul_pair(t[1], x[1])), fma_pair(t[2], x[2], mul_pair(t[3], x[3])));
-          const Pair c = twice(-inv * inv * inv * (sum_over_lanes<kLanes>(m, lanes) * inv_width));
+          for (int p = 0; p < 4; ++p) { t[p] = mul_pair(v[p], g[p]); u[p] = mul_pair(x[p], r); }
+          const float m = sum_of(fma_pair(t[0], u[0], mul_pair(t[1], u[1])), fma_pair(t[2], u[2], mul_pair(t[3], u[3])));
+          const Pair c = twice(-sum_over_lanes<kLanes>(m, lanes) * inv_width);
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
-            dg[p] = fma_pair(v[p], mul_pair(x[p], r), dg[p]);
-            v[p] = fma_pair(t[p], r, mul_pair(x[p], c));
+            dg[p] = fma_pair(v[p], u[p], dg[p]);
+            v[p] = mul_pair(r, fma_pair(u[p], c, t[p]));
           }
         }
         if (jb.y && ok) {

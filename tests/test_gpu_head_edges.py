@@ -1,4 +1,4 @@
-"""HeadNorm and Rotate where they could go wrong: no eps."""
+"""HeadNorm and Rotate where they could go wrong: no eps, very large and very small heads."""
 import pytest
 
 from attention_cases import head_bounds, head_feeds, within
@@ -45,3 +45,11 @@ def check(g, inputs, outputs, feeds, size=1.0):
 def test_no_eps(heads, width, rotate, eps):
     g, inputs, outputs = norm_graph(70, heads, width, eps, rotate=rotate)
     check(g, inputs, outputs, head_feeds(g, inputs, heads + width))
+
+
+@pytest.mark.parametrize("size", [2.0 ** 53, 2.0 ** 44, 2.0 ** -53, 2.0 ** -44])
+@pytest.mark.parametrize("heads,width,rotate,x", [(3, 64, True, "f32"), (2, 128, True, "bf16"), (5, 72, False, "f32"), (8, 32, False, "bf16")])
+def test_heads_far_from_one(size, heads, width, rotate, x):
+    """Squares of up to 2^112 and down to 2^-112: in range, and so is every factor of the formula; the cube of the root is not."""
+    g, inputs, outputs = norm_graph(33, heads, width, 0.0, x=x, y="f32", rotate=rotate)
+    check(g, inputs, outputs, head_feeds(g, inputs, heads + width), size)
