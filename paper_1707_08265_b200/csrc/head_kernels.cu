@@ -149,6 +149,7 @@ template <int kLanes> __device__ __forceinline__ float sum_over_lanes(float v, i
 template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void __launch_bounds__(kHeadThreads, kHeadCtas) head_kernel(const __grid_constant__ HeadArgs a) {
   constexpr int kUnroll = (kBack ? 2 : 4) / (DT == DRAGON_BF16 ? 1 : 2);
   constexpr bool kApart = kPairing == P_HALVES;
+  constexpr bool scaled_there = !kBack && !kU && (kPairing == P_NEIGHBOURS || kPairing == P_HALVES);      // gains go with the angles
   __shared__ float2 cs[kPairing == P_NONE ? 1 : kHeadRowsMost][kPlaces];
   __shared__ unsigned long long freq[kPairing == P_NONE ? 1 : kPairsMost];      // (lanes that index parameters apart wait for one another)
   __shared__ float buf[kPairing == P_ANY ? kHeadWarps : 1][256];
@@ -217,7 +218,7 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
     if (my_row >= rows) continue;
     if (kPairing != P_NONE) {
       load_angles<kPairing, kBack>(cs[my_row], at_head, a.dims, own, other);
-      if (!kBack && !kU && kPairing != P_ANY) {      // with the gains: the norm's own multiplication by them is done there
+      if (scaled_there) {      // with the gains: the norm's own multiplication by them is done there
 #pragma unroll
         for (int p = 0; p < 4; ++p) { own[p] = mul_pair(own[p], g[p]); other[p] = mul_pair(other[p], partners<kPairing>(g, p)); }
       }
@@ -251,7 +252,7 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
         }
         const Pair r = twice(inv);
         if (!kBack) {
-          if (!kU && (kPairing == P_NEIGHBOURS || kPairing == P_HALVES)) {
+          if (scaled_there) {
 #pragma unroll
             for (int p = 0; p < 4; ++p) v[p] = mul_pair(r, fma_pair(x[p], own[p], mul_pair(partners<kPairing>(x, p), other[p])));
           } else {
@@ -269,6 +270,7 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
           }
         }
         const Pair* from = kBack ? v : x;      // what is rotated
+        const Pair kept[4] = {v[0], v[1], v[2], v[3]};
         if (kPairing == P_ANY) {
           float* b = buf[kPairing == P_ANY ? warp : 0];
           const int half = a.dims >> 1;
@@ -293,6 +295,11 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
         } else if (!kBack && kPairing == P_NONE) {
 #pragma unroll
           for (int p = 0; p < 4; ++p) v[p] = x[p];
+        }
+        if (kPairing != P_NONE && a.dims < width) {      // elements behind dims are copied: not even 0 times another one goes into them
+#pragma unroll
+          for (int p = 0; p < 4; ++p)
+            if (at_head[2 * p] >= a.dims) v[p] = kBack ? kept[p] : scaled_there ? mul_pair(r, mul_pair(x[p], own[p])) : x[p];
         }
         if (kBack && norm) {
           // on the normalised values u = x r: no power of r above the first, which alone may leave fp32's range (heads of 1e13 and more)

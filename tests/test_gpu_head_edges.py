@@ -1,4 +1,6 @@
-"""HeadNorm and Rotate where they could go wrong: no eps, very large and very small heads."""
+"""HeadNorm and Rotate where they could go wrong: no eps, very large and very small heads, values that are not finite behind
+the rotated elements."""
+import numpy as np
 import pytest
 
 from attention_cases import head_bounds, head_feeds, within
@@ -53,3 +55,70 @@ def test_heads_far_from_one(size, heads, width, rotate, x):
     """Squares of up to 2^112 and down to 2^-112: in range, and so is every factor of the formula; the cube of the root is not."""
     g, inputs, outputs = norm_graph(33, heads, width, 0.0, x=x, y="f32", rotate=rotate)
     check(g, inputs, outputs, head_feeds(g, inputs, heads + width), size)
+
+
+def same_bits(a, b):
+    return np.array_equal(a, b) and np.array_equal(np.signbit(a), np.signbit(b))
+
+
+def copied_graph(rows, heads, width, dims, interleaved, norm, dt, grad=True):
+    g = wl.GraphDesc()
+    shape = [rows, heads * width]
+    x, pos = g.tensor("x", shape, dt), g.tensor("pos", [rows], "i32")
+    inputs, last = [x, pos], x
+    if norm:
+        gain = g.tensor("gain", [width])
+        inputs.append(gain)
+        last = g.op("HeadNorm", [x, gain], "u", shape, norm, attrs=[1e-5])
+    y = g.op("Rotate", [last, pos], "y", shape, dt, attrs=[heads, dims, interleaved])
+    if not grad:
+        return g, inputs, [y]
+    dy = g.tensor("dy", shape, dt)
+    inputs.append(dy)
+    return g, inputs, [y] + g.grad([g.op("Mul", [y, dy], "along")], [x], [dt])
+
+
+# halves of 8 elements' lanes and others, neighbours, widths known when the kernel is compiled and others
+COPIED = [(2, 64, 48, 0), (2, 64, 44, 0), (2, 64, 48, 1), (4, 128, 32, 0), (4, 128, 30, 1), (3, 40, 20, 0), (3, 40, 16, 0), (1, 256, 2, 1), (5, 80, 8, 0)]
+
+
+@pytest.mark.parametrize("heads,width,dims,interleaved", COPIED)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_elements_behind_the_rotated_ones_are_copied(heads, width, dims, interleaved, dt, bad):
+    """Whatever stands there: every other element keeps its bits, forwards and in the gradient."""
+    g, inputs, outputs = copied_graph(19, heads, width, dims, interleaved, None, dt)
+    feeds = head_feeds(g, inputs, width + dims)
+    for k in (0, 2):
+        feeds[k].reshape(19, heads, width)[:, :, -1] = -0.0
+    clean, _ = run_gpu(g.desc, inputs, outputs, feeds)
+    behind = np.zeros((19, heads, width), bool)
+    behind[:, :, dims:] = True
+    behind = behind.reshape(19, -1)
+    for k, a in zip((0, 2), clean):
+        assert same_bits(a[behind], feeds[k][behind])
+    at = np.zeros((19, heads, width), bool)
+    at[3, 0, dims] = at[4, heads - 1, width - 3] = at[18, 0, width - 2] = True
+    at = at.reshape(19, -1)
+    dirty = [f.copy() for f in feeds]
+    dirty[0][at] = dirty[2][at] = bad
+    got, _ = run_gpu(g.desc, inputs, outputs, dirty)
+    for a, c in zip(got, clean):
+        assert same_bits(a[~at], c[~at])
+        assert np.isnan(a[at]).all() if np.isnan(bad) else (a[at] == bad).all()
+
+
+@pytest.mark.parametrize("heads,width,dims,interleaved", COPIED)
+@pytest.mark.parametrize("u", ["f32", "bf16"])
+def test_an_infinity_behind_the_rotated_elements_of_a_normed_head(heads, width, dims, interleaved, u):
+    """The head's root mean square is infinite then: the element itself is NaN, the others of the head are 0."""
+    g, inputs, outputs = copied_graph(9, heads, width, dims, interleaved, u, "f32", grad=False)
+    feeds = head_feeds(g, inputs, width + dims)
+    clean, _ = run_gpu(g.desc, inputs, outputs, feeds)
+    feeds[0].reshape(9, heads, width)[4, heads - 1, width - 2] = np.inf
+    got, _ = run_gpu(g.desc, inputs, outputs, feeds)
+    a, c = (t.reshape(9, heads, width) for t in (got[0], clean[0]))
+    head = np.zeros((9, heads), bool)
+    head[4, heads - 1] = True
+    assert same_bits(a[~head], c[~head])
+    assert np.isnan(a[4, heads - 1, width - 2]) and (np.delete(a[4, heads - 1], width - 2) == 0).all()
