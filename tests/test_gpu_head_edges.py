@@ -1,5 +1,5 @@
 """HeadNorm and Rotate where they could go wrong: no eps, very large and very small heads, values that are not finite behind
-the rotated elements."""
+the rotated elements, norms without a rotation behind them."""
 import numpy as np
 import pytest
 
@@ -55,6 +55,32 @@ def test_heads_far_from_one(size, heads, width, rotate, x):
     """Squares of up to 2^112 and down to 2^-112: in range, and so is every factor of the formula; the cube of the root is not."""
     g, inputs, outputs = norm_graph(33, heads, width, 0.0, x=x, y="f32", rotate=rotate)
     check(g, inputs, outputs, head_feeds(g, inputs, heads + width), size)
+
+
+@pytest.mark.parametrize("heads,width,x,y", [(1, 64, "bf16", "bf16"), (3, 64, "f32", "f32"), (6, 80, "bf16", "bf16"), (32, 128, "bf16", "bf16"), (5, 256, "f32", "bf16"), (7, 8, "bf16", "f32")])
+@pytest.mark.parametrize("rows", [1, 333])
+def test_a_norm_alone_with_gradients(heads, width, x, y, rows):
+    g, inputs, outputs = norm_graph(rows, heads, width, 1e-5, x=x, y=y, rotate=False)
+    check(g, inputs, outputs, head_feeds(g, inputs, heads + rows))
+
+
+def test_a_norm_that_a_rotation_and_something_else_read():
+    """Its gradient is a sum: the rotation backwards and the norm backwards are passes of their own."""
+    g = wl.GraphDesc()
+    shape = [50, 3 * 40]
+    x, gain, pos, dy, du = g.tensor("x", shape), g.tensor("gain", [40]), g.tensor("pos", [50], "i32"), g.tensor("dy", shape), g.tensor("du", shape)
+    u = g.op("HeadNorm", [x, gain], "u", shape, "f32", attrs=[1e-5])
+    y = g.op("Rotate", [u, pos], "y", shape, "f32", attrs=[3, 40])
+    grads = g.grad([g.op("Mul", [y, dy], "along_y"), g.op("Mul", [u, du], "along_u")], [x, gain])
+    inputs, outputs = [x, gain, pos, dy, du], [u, y] + grads
+    feeds = head_feeds(g, inputs, 7)
+    got, _ = run_gpu(g.desc, inputs, outputs, feeds)
+    want = interp.run_function(g.desc, inputs, outputs, feeds)
+    # a gradient of the norm of magnitude sqrt(2) |dy| + |du| at most: the bound for a dy of twice their sum
+    h, h_in, h_out = norm_graph(50, 3, 40, 1e-5)
+    b = head_bounds(h, h_in, h_out, feeds[:3] + [2 * (np.abs(feeds[3]) + np.abs(feeds[4]))])
+    for n, a, w in zip(("u", "y", "dx", "dgain"), got, want):
+        assert within(a, w, b[n], "f32") <= 1, n
 
 
 def same_bits(a, b):
