@@ -31,6 +31,10 @@ struct RowArgs {
   // backwards: every part's dq, and with key_splits dk and dv, which are added up
   int splits, key_splits;
   float *part, *part_lse, *part_k, *part_v;
+  // PagedAttention's few rows: results of a split, and where slots is not 0 so many of every sequence and key head (new row x group +
+  // head of the group) instead of [row][head]: with starts there may be many rows, of which only those of short sequences have parts
+  long long part_items;
+  int slots;
   int* status;
   int* status_clear;
 };

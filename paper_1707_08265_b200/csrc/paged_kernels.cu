@@ -93,6 +93,11 @@ __device__ __forceinline__ void mma16(float* c, const uint32_t* a, uint32_t b0, 
 }
 __device__ __forceinline__ float exp2_of(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+// where a part of few rows stands among those of its split; r: new row of the sequence x group + head of the group
+__device__ __forceinline__ size_t few_item(const RowArgs& a, int s, int kvh, int r, int row, int head) {
+  return a.slots ? ((size_t)s * a.kv_heads + kvh) * a.slots + r : (size_t)row * a.heads + head;
+}
+
 // kSteps: 16 elements of the head each; kM: 16 rows each
 template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps, few_resident(kSteps, kM)) paged_few(const __grid_constant__ RowArgs a, int few, int columns) {
   constexpr int kPitch = few_pitch(kSteps), kRows = 16 * kM, kStage = 2 * 16 * kPitch, kOut = 16 * kSteps + 4;
@@ -296,8 +301,9 @@ template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps, 
     const int row = r0 + (first + r) / group, head = kvh * group + (first + r) % group;
     const size_t at = ((size_t)row * a.heads + head) * a.width + c;
     if (parts) {
-      if (my1 > my0) store_any<8>(a.part + (size_t)split * a.seq.rows * a.heads * a.width, DRAGON_F32, at, v);
-      if (c == 0) a.part_lse[((size_t)split * a.seq.rows + row) * a.heads + head] = l == 0.f ? -kInf : most * a.scale + log2f(l);
+      const size_t item = split * (size_t)a.part_items + few_item(a, s, kvh, first + r, row, head);
+      if (my1 > my0) store_any<8>(a.part, DRAGON_F32, item * a.width + c, v);
+      if (c == 0) a.part_lse[item] = l == 0.f ? -kInf : most * a.scale + log2f(l);
     } else {
       store_any<8>(a.out, a.ot, at, v);
       if (!fine) row_bad[r] = 1;
@@ -311,12 +317,15 @@ template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps, 
 
 // The parts of every row put together; rows of no sequence get zeros.  A row and head for `ways` warps (1 or 8), which share its
 // parts, 4 elements a lane.  by_sequence: only rows of sequences of few rows (the others have no parts).
-__global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArgs a, int few, int few_splits, int tile_splits, int ways, int by_sequence) {
+__global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArgs a, const float* tile_part, const float* tile_lse, int few, int few_splits, int tile_splits,
+                                                  int ways, int by_sequence) {
   __shared__ float sums[8][132];
   after_the_launch_before();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, way = warp & (ways - 1), group = a.heads / a.kv_heads;
   const long long item = ((long long)blockIdx.x * 8 + warp) / ways;
   int row, head, s, splits = 0;
+  const float *part = a.part, *lse = a.part_lse;
+  size_t from = 0, stride = a.part_items;      // its first part, and from one to the next
   if (by_sequence) {
     const int slots = a.kv_heads * few, slot = (int)(item % slots), r = slot % few;
     s = (int)(item / slots);
@@ -327,6 +336,7 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
     row = r0 + r / group;
     head = slot / few * group + r % group;
     splits = few_splits;
+    from = few_item(a, s, slot / few, r, row, head);
   } else {
     if (item >= (long long)a.seq.rows * a.heads) return;
     row = (int)(item / a.heads);
@@ -335,13 +345,21 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
     if (s >= 0) {
       int r0, r1;
       a.seq.rows_of(s, &r0, &r1);
-      splits = (r1 - r0) * group <= few ? few_splits : tile_splits;
+      const bool is_few = (r1 - r0) * group <= few;
+      splits = is_few ? few_splits : tile_splits;
       if (splits == 1) return;      // written already
+      if (is_few) {
+        from = few_item(a, s, head / group, (row - r0) * group + head % group, row, head);
+      } else {
+        from = (size_t)row * a.heads + head;
+        stride = (size_t)a.seq.rows * a.heads;
+        part = tile_part;
+        lse = tile_lse;
+      }
     }
   }
-  const size_t i = (size_t)row * a.heads + head, stride = (size_t)a.seq.rows * a.heads;
   float most = -kInf;
-  for (int p = lane; p < splits; p += 32) most = fmaxf(most, a.part_lse[p * stride + i]);
+  for (int p = lane; p < splits; p += 32) most = fmaxf(most, lse[p * stride + from]);
 #pragma unroll
   for (int k = 16; k; k >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, k));
   const float shift = most == -kInf ? 0.f : most;
@@ -352,10 +370,10 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int p = p0 + k * ways;
-      const float l = p < splits ? a.part_lse[p * stride + i] : -kInf;
+      const float l = p < splits ? lse[p * stride + from] : -kInf;
       w[k] = exp2f(l - shift);
       x[k] = make_float4(0.f, 0.f, 0.f, 0.f);      // (no keys: nothing was written)
-      if (l != -kInf && 4 * lane < a.width) x[k] = *reinterpret_cast<const float4*>(a.part + (p * stride + i) * a.width + 4 * lane);
+      if (l != -kInf && 4 * lane < a.width) x[k] = *reinterpret_cast<const float4*>(part + (p * stride + from) * a.width + 4 * lane);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -381,7 +399,7 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
   for (int e = 0; e < 4; ++e) { v[e] *= inv; fine &= fabsf(v[e]) < kInf; }
   if (!__all_sync(0xffffffffu, fine)) { attend_row<true>(a, head, row, lane); return; }
   if (4 * lane < a.width) {
-    const size_t at = i * a.width + 4 * lane;
+    const size_t at = ((size_t)row * a.heads + head) * a.width + 4 * lane;
     if (a.ot == DRAGON_F32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
     else *reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(a.out) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
   }
@@ -394,6 +412,10 @@ struct PagedPlan {
   int most_few;                       // rows x group of a sequence that the kernel for few rows takes
   int few_rows;                       // of one CTA
   int few_splits, tile_splits;
+  int slots;                          // numbering of the few rows' parts (RowArgs), and how many of a split
+  int64_t few_items;
+  // the workspace in floats: log sums and results of the few rows' parts, then of the tiles'
+  int64_t few_lse, few_part, tile_lse, tile_part, floats;
 };
 
 // Parts: as many as bring the CTAs to `waves` times what the GPU holds at once, of at least `least` keys each
@@ -418,6 +440,14 @@ PagedPlan plan_paged(int64_t rows, int64_t sequences, bool starts, int64_t room,
   p.few_splits = p.few ? parts_of(units, room, units <= slots ? slots / units * units : 8 * (int64_t)sm_count, 256) : 1;
   p.tile_splits = p.tiles ? parts_of(attention_units(rows, sequences, heads, kv_heads), room, sm_count, 512) : 1;
   p.join = starts ? p.few_splits > 1 || p.tile_splits > 1 || !p.tiles : p.few_splits > 1 || p.tile_splits > 1;
+  // (numbered by rows with 64 sequences of single new rows, by slots with a chunk of 16384 rows, 64 heads on 8: 8.5 MB where all rows would take 29.8 GB)
+  const int64_t most = std::min<int64_t>(p.most_few, starts ? rows * group : each), by_slots = sequences * kv_heads * most;
+  p.slots = by_slots < rows * heads ? (int)most : 0;
+  p.few_items = p.slots ? by_slots : rows * heads;
+  auto take = [&](int64_t floats) { const int64_t at = p.floats; p.floats += (floats + 63) & ~(int64_t)63; return at; };
+  const int64_t few = p.few_splits > 1 ? p.few_splits * p.few_items : 0, tile = p.tile_splits > 1 ? p.tile_splits * rows * heads : 0;
+  p.few_lse = take(few); p.few_part = take(few * width);
+  p.tile_lse = take(tile); p.tile_part = take(tile * width);
   return p;
 }
 PagedPlan plan_of(const Step& s, const std::vector<MemRef>& mems, int sm_count) {
@@ -483,10 +513,7 @@ int paged_launches(const Step& s, const std::vector<MemRef>& mems, int sm_count)
   return p.few + p.tiles + p.join;
 }
 size_t paged_scratch_bytes(const Step& s, const std::vector<MemRef>& mems, int sm_count) {
-  const PagedPlan p = plan_of(s, mems, sm_count);
-  const Shape& q = mems[s.rd[pa::Q]].shape;
-  const int64_t parts = std::max(p.few_splits, p.tile_splits);
-  return parts > 1 ? (size_t)(parts * q.d[0] * (q.d[1] + (int64_t)s.num[pn::HEADS])) * sizeof(float) + 256 : 0;
+  return plan_of(s, mems, sm_count).floats * sizeof(float);
 }
 
 int launch_paged_attention(const StepRun& r) {
@@ -512,25 +539,31 @@ int launch_paged_attention(const StepRun& r) {
   a.pages.pool = (int)(r.mems[r.s.rd[pa::K]].shape.d[0] >> a.pages.shift);
   a.status = r.status;
   a.status_clear = r.status_clear;
-  a.part_lse = reinterpret_cast<float*>(r.ws + r.s.scratch_off);
-  a.part = a.part_lse + (((int64_t)std::max(p.few_splits, p.tile_splits) * a.seq.rows * a.heads + 63) & ~(int64_t)63);
+  float* const ws = reinterpret_cast<float*>(r.ws + r.s.scratch_off);
   int rc = DRAGON_OK;
   if (p.few) {
     a.splits = p.few_splits;
+    a.part_lse = ws + p.few_lse;
+    a.part = ws + p.few_part;
+    a.part_items = p.few_items;
+    a.slots = p.slots;
     const int most_rows = std::min<int64_t>(p.most_few, a.seq.starts ? (int64_t)a.seq.rows * (a.heads / a.kv_heads) : (int64_t)a.seq.each * (a.heads / a.kv_heads));
     const int steps = (a.width + 15) / 16;
     rc = steps <= 2 ? launch_few<2>(a, p, most_rows, st) : steps <= 4 ? launch_few<4>(a, p, most_rows, st) : steps <= 6 ? launch_few<6>(a, p, most_rows, st)
                                                                                                           : launch_few<8>(a, p, most_rows, st);
   }
   if (rc == DRAGON_OK && p.tiles) {
-    a.splits = p.tile_splits;
-    rc = launch_attention_forward(a, true, r.mems[r.s.rd[pa::K]].shape.d[0], p.most_few, r.sm_count, st, "PagedAttention");
+    RowArgs t = a;
+    t.splits = p.tile_splits;
+    t.part_lse = ws + p.tile_lse;
+    t.part = ws + p.tile_part;
+    rc = launch_attention_forward(t, true, r.mems[r.s.rd[pa::K]].shape.d[0], p.most_few, r.sm_count, st, "PagedAttention");
   }
   if (rc == DRAGON_OK && p.join) {
     const bool by_sequence = a.seq.starts && p.tiles && p.tile_splits == 1;
     const int ways = std::max(p.few_splits, p.tile_splits) > 8 ? 8 : 1;
     const long long items = by_sequence ? (long long)a.seq.count * a.kv_heads * p.most_few : (long long)a.seq.rows * a.heads;
-    rc = launch_behind(paged_join, dim3((unsigned)((items * ways + 7) / 8)), dim3(256), 0, st, "PagedAttention", a, p.most_few, p.few_splits, p.tile_splits, ways, (int)by_sequence);
+    rc = launch_behind(paged_join, dim3((unsigned)((items * ways + 7) / 8)), dim3(256), 0, st, "PagedAttention", a, (const float*)(ws + p.tile_part), (const float*)(ws + p.tile_lse), p.most_few, p.few_splits, p.tile_splits, ways, (int)by_sequence);
   }
   return rc;
 }
