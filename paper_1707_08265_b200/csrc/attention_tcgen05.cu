@@ -118,7 +118,7 @@ attention_fwd(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     return;
   }
   const int n_rows = u.b - u.a;
-  if (kPaged && n_rows * group <= a.few) { give_tmem_back(); return; }
+  if (kPaged && has_few_rows(n_rows, group, a.few)) { give_tmem_back(); return; }
   // the tiles of keys that any row of the unit sees
   const int last_row = min(u.row0 + block_rows, n_rows) - 1;      // (row0 < n_rows)
   const int key_end = a.r.causal ? max(0, min(u.keys, u.first_pos + last_row + 1)) : u.keys;

@@ -113,8 +113,9 @@ template <int kSteps, int kM> __global__ void __launch_bounds__(32 * kFewWarps, 
   if (blockIdx.x == 0 && !a.seq.in_order()) report(a.status, DRAGON_ERR_INVALID_ARG);
   int r0, r1;
   a.seq.rows_of(s, &r0, &r1);
+  if (!has_few_rows(r1 - r0, group, few)) return;
   const int rows = (r1 - r0) * group, first = tile * kRows;      // row r: new token r / group, head r % group of the group
-  if (rows > few || first >= rows) return;
+  if (first >= rows) return;
   bool fits;
   const int tokens = a.pages.tokens(s, &fits), base = tokens - (r1 - r0);
   if (!fits && threadIdx.x == 0) report(a.status, DRAGON_ERR_INVALID_ARG);
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
     if (s >= a.seq.count) return;
     int r0, r1;
     a.seq.rows_of(s, &r0, &r1);
-    if ((r1 - r0) * group > few || r >= (r1 - r0) * group) return;
+    if (!has_few_rows(r1 - r0, group, few) || r >= (r1 - r0) * group) return;
     row = r0 + r / group;
     head = slot / few * group + r % group;
     splits = few_splits;
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
     if (s >= 0) {
       int r0, r1;
       a.seq.rows_of(s, &r0, &r1);
-      const bool is_few = (r1 - r0) * group <= few;
+      const bool is_few = has_few_rows(r1 - r0, group, few);
       splits = is_few ? few_splits : tile_splits;
       if (splits == 1) return;      // written already
       if (is_few) {
