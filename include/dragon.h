@@ -128,7 +128,9 @@ enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2, DRAGON_F8E4M3 = 3 };
  *                          q [T, heads*D], kcache, vcache bf16 [pages_in_pool * page, kv_heads*D] that hold every token,
  *                          the new ones too; the table as for CACHE_WRITE; y like q.  The row at position p sees positions
  *                          0 .. p (window > 0: the last `window` of them); one at a negative position, or of no sequence,
- *                          gets 0.  Pages outside of the pool count as zeros and set the status, as above.
+ *                          gets 0.  Pages outside of the pool count as zeros and set the status, as above; a length behind P pages, or
+ *                          above 2^31 - 256, counts as that many and sets it too.  Probabilities are rounded to bf16 for their
+ *                          product, as ATTENTION's are; statistics and sums are fp32.
  * RMS_NORM, GATED_SCAN, HEAD_NORM, ROTATE and ATTENTION have gradients (with respect to h, g; gate, x, h0; x, g; x; q, k, v).  A
  * gradient chain through BLOCK_SCALE, QUANTIZE, SCALED_INNER_PRODUCT, GLOBAL_NORM, CLIP_BY_NORM, CACHE_WRITE or PAGED_ATTENTION is
  * DRAGON_ERR_UNSUPPORTED at dragon_function.

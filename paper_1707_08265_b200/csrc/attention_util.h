@@ -39,15 +39,17 @@ struct Sequences {
   }
 };
 
+constexpr int kMostTokens = 0x7fffff00;      // of a sequence: positions, and the end of their last tile, stay within 32 bits
+
 // The pages of a cache: token p of sequence s is row pages[s][p / page] * page + p % page
 struct Pages {
   const int* pages;           // [sequences][most]
   const int* lengths;         // tokens of every sequence
   int most, shift, pool;      // page = 1 << shift rows; pool: pages there are
-  // tokens that the table has room for, of those that sequence s says it has
+  // tokens that the table has room for (and positions in 32 bits), of those that sequence s says it has
   __device__ __forceinline__ int tokens(int s, bool* fits) const {
     const int n = max(__ldg(lengths + s), 0);
-    const long long room = (long long)most << shift;
+    const long long room = min((long long)most << shift, (long long)kMostTokens);
     *fits = n <= room;
     return (int)min((long long)n, room);
   }
