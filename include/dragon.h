@@ -108,7 +108,8 @@ enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2, DRAGON_F8E4M3 = 3 };
  *                          q [T, heads*D], k, v [T, kv_heads*D], y like q; D a multiple of 8, at most 128.  Every row i of
  *                          a query head sees the rows j of its sequence (causal: j <= i; window > 0, causal only:
  *                          i - j < window) in key head h / (heads / kv_heads):
- *                          y = sum_j softmax_j(scale q_i . k_j) v_j, scale 1/sqrt(D) where it is given as 0.  The rows are
+ *                          y = sum_j softmax_j(scale q_i . k_j) v_j, scale 1/sqrt(D) where it is given as 0 (otherwise
+ *                          positive, and times log2 e within fp32).  The rows are
  *                          `sequences` sequences of equal length, or sequence s has rows starts[s] .. starts[s+1] - 1
  *                          (starts int32 [S+1], ascending; sequences may be empty; rows of no sequence get 0 and pass no
  *                          gradient; starts out of range are cut to it, and they and starts out of order set the function

@@ -103,6 +103,12 @@ int check_table(const Graph& g, const char* who, const dragon_id* in, int n_in, 
   return DRAGON_OK;
 }
 
+// attention's scale: 0 (1/sqrt(D)), or one whose product with log2(e), by which the kernels multiply scores, fp32 holds
+bool valid_scale(double scale) {
+  const float s = (float)(scale * 1.4426950408889634);
+  return scale == 0.0 || (s > 0.0f && s <= std::numeric_limits<float>::max());
+}
+
 bool valid_page(double page) { return whole(page, 16.0, 1 << 20) && ((int64_t)page & ((int64_t)page - 1)) == 0; }
 
 int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, double attr, std::vector<double>* num, Shape* out) {
@@ -259,8 +265,8 @@ int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, double 
       std::vector<double>& n = *num;
       if (n[1] == 0.0) n[1] = n[0];
       if (!whole(n[0], 1.0, 65535.0) || !whole(n[1], 1.0, n[0]) || (int64_t)n[0] % (int64_t)n[1] || !whole(n[2], 0.0, 1.0) || !whole(n[3], 0.0, 1 << 30) ||
-          (n[3] > 0.0 && n[2] == 0.0) || n[4] < 0.0 || !((float)n[4] <= std::numeric_limits<float>::max()) || !whole(n[5], 1.0, 2147483647.0) || (n_in == 4 && n[5] != 1.0)) {
-        set_error("Attention: heads a multiple of kv_heads, causal 0 or 1, a window only where causal, scale at least 0, sequences only without starts");
+          (n[3] > 0.0 && n[2] == 0.0) || !valid_scale(n[4]) || !whole(n[5], 1.0, 2147483647.0) || (n_in == 4 && n[5] != 1.0)) {
+        set_error("Attention: heads a multiple of kv_heads, causal 0 or 1, a window only where causal, scale 0 or positive in fp32, sequences only without starts");
         return DRAGON_ERR_INVALID_ARG;
       }
       if (q.rank != 2 || k.rank != 2 || v != k || k.d[0] != q.d[0] || q.d[1] % (int64_t)n[0] || k.d[1] != q.d[1] / (int64_t)n[0] * (int64_t)n[1] || q.d[0] % (int64_t)n[5]) {
@@ -298,9 +304,8 @@ int infer_shape(const Graph& g, int type, const dragon_id* in, int n_in, double 
       const Shape &q = T(0).shape, &k = T(1).shape, &v = T(2).shape;
       std::vector<double>& n = *num;
       if (n[1] == 0.0) n[1] = n[0];
-      if (!whole(n[0], 1.0, 65535.0) || !whole(n[1], 1.0, n[0]) || (int64_t)n[0] % (int64_t)n[1] || !valid_page(n[2]) || !whole(n[3], 0.0, 1 << 30) || n[4] < 0.0 ||
-          !((float)n[4] <= std::numeric_limits<float>::max())) {
-        set_error("PagedAttention: heads a multiple of kv_heads, page a power of two of 16 or more, window and scale at least 0");
+      if (!whole(n[0], 1.0, 65535.0) || !whole(n[1], 1.0, n[0]) || (int64_t)n[0] % (int64_t)n[1] || !valid_page(n[2]) || !whole(n[3], 0.0, 1 << 30) || !valid_scale(n[4])) {
+        set_error("PagedAttention: heads a multiple of kv_heads, page a power of two of 16 or more, window at least 0, scale 0 or positive in fp32");
         return DRAGON_ERR_INVALID_ARG;
       }
       if (q.rank != 2 || k.rank != 2 || v != k || q.d[1] % (int64_t)n[0] || k.d[1] != q.d[1] / (int64_t)n[0] * (int64_t)n[1] || k.d[0] % (int64_t)n[2]) {
