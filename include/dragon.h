@@ -109,12 +109,12 @@ enum { DRAGON_F32 = 0, DRAGON_BF16 = 1, DRAGON_I32 = 2, DRAGON_F8E4M3 = 3 };
  *                          a query head sees the rows j of its sequence (causal: j <= i; window > 0, causal only:
  *                          i - j < window) in key head h / (heads / kv_heads):
  *                          y = sum_j softmax_j(scale q_i . k_j) v_j, scale 1/sqrt(D) where it is given as 0 (otherwise
- *                          positive, and times log2 e within fp32).  The rows are
- *                          `sequences` sequences of equal length, or sequence s has rows starts[s] .. starts[s+1] - 1
- *                          (starts int32 [S+1], ascending; sequences may be empty; rows of no sequence get 0 and pass no
- *                          gradient; starts out of range are cut to it, and they and starts out of order set the function
- *                          status to DRAGON_ERR_INVALID_ARG: out of order some rows may be left unwritten).  Operands are consumed as bf16, probabilities are rounded to bf16 for
- *                          their product; statistics and sums are fp32.
+ *                          positive, and times log2 e within fp32); 0 where all scores are -inf.  The rows are `sequences`
+ *                          sequences of equal length, or sequence s has rows starts[s] .. starts[s+1] - 1 (starts int32
+ *                          [S+1], ascending; sequences may be empty; rows of no sequence get 0 and pass no gradient; starts
+ *                          out of range are cut to it, and they and starts out of order set the function status to
+ *                          DRAGON_ERR_INVALID_ARG: out of order some rows may be left unwritten).  Operands are consumed as
+ *                          bf16, probabilities are rounded to bf16 for their product; statistics and sums are fp32.
  *   CACHE_WRITE(cache, rows, pages, lengths [, starts]) attrs {page}   cache' = the cache with the rows of new tokens in their
  *                          places.  cache [pages_in_pool * page, C], rows [T, C], the same type (f32 or bf16), C a multiple of 8; page a power of
  *                          two of 16 or more; pages int32 [S, P], lengths int32 [S].  Sequence s has lengths[s] tokens, its

@@ -156,6 +156,14 @@ def sequence_rows(rows, sequences, starts):
     return [(int(a), int(b)) for a, b in zip(starts[:-1], starts[1:])]
 
 
+def _softmax(x):
+    """Over the last axis; zeros where all scores are -inf."""
+    top = x.max(axis=-1, keepdims=True)
+    e = np.exp(x - np.where(top == -np.inf, 0, top))
+    total = e.sum(axis=-1, keepdims=True)
+    return e / np.where(total == 0, 1, total)
+
+
 def attention_parts(op, ins, bf16=True):
     """For every sequence and query head: (rows, columns of the head, columns of its key head, probabilities, scale)."""
     heads, kv_heads, causal, window, scale, sequences = _numbers(op, [1, 0, 1, 0, 0.0, 1])
@@ -173,8 +181,7 @@ def attention_parts(op, ins, bf16=True):
         for h in range(heads):
             mine, theirs = slice(h * width, (h + 1) * width), slice(h // (heads // kv_heads) * width, (h // (heads // kv_heads) + 1) * width)
             x = np.where(seen, scale * (q[a:b, mine] @ k[a:b, theirs].T), -np.inf)
-            e = np.exp(x - x.max(axis=1, keepdims=True)) if b > a else x
-            yield slice(a, b), mine, theirs, e / e.sum(axis=1, keepdims=True), scale
+            yield slice(a, b), mine, theirs, _softmax(x) if b > a else x, scale
 
 
 def cache_places(page, rows, pool, pages, lengths, starts):
@@ -203,8 +210,7 @@ def paged_parts(op, ins):
         for h in range(heads):
             mine, theirs = slice(h * width, (h + 1) * width), slice(h // (heads // kv_heads) * width, (h // (heads // kv_heads) + 1) * width)
             x = scale * (kc[at, theirs] @ q[r, mine])
-            e = np.exp(x - x.max())
-            yield r, mine, theirs, at, e / e.sum()
+            yield r, mine, theirs, at, _softmax(x)
 
 
 def _forward(op, ins, dtype, bf16_contraction=True):
