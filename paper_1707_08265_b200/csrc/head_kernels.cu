@@ -283,8 +283,8 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
           for (int p = 0; p < 4; ++p) {
             float o[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) { const int i = e0 + 2 * p + e; o[e] = i < a.dims ? head[i < half ? i + half : i - half] : 0.f; }
-            v[p] = fma_pair(from[p], own[p], mul_pair(pair_of(o[0], o[1]), other[p]));
+            for (int e = 0; e < 2; ++e) { const int i = e0 + 2 * p + e; o[e] = head[i < half ? i + half : i - half]; }
+            v[p] = e0 + 2 * p < a.dims ? fma_pair(from[p], own[p], mul_pair(pair_of(o[0], o[1]), other[p])) : from[p];
           }
         } else if ((kBack || kU) && kPairing != P_NONE) {
           Pair w[4];
@@ -296,7 +296,8 @@ template <int DT, int kPairing, bool kBack, bool kU, int kLanes> __global__ void
 #pragma unroll
           for (int p = 0; p < 4; ++p) v[p] = x[p];
         }
-        if (kPairing != P_NONE && a.dims < width) {      // elements behind dims are copied: not even 0 times another one goes into them
+        // elements behind dims (whole pairs) are copied: not even 0 times another one goes into them
+        if ((kPairing == P_NEIGHBOURS || kPairing == P_HALVES) && a.dims < width) {
 #pragma unroll
           for (int p = 0; p < 4; ++p)
             if (at_head[2 * p] >= a.dims) v[p] = kBack ? kept[p] : scaled_there ? mul_pair(r, mul_pair(x[p], own[p])) : x[p];
