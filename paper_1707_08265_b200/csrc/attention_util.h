@@ -58,7 +58,7 @@ struct Pages {
 };
 
 // whether a sequence of n new rows has at most `few` of them times the heads of a group (the product itself may pass 32 bits)
-__device__ __forceinline__ bool has_few_rows(int n, int group, int few) { return n <= few / group; }
+__device__ __forceinline__ bool has_few_rows(int n, int group, int few) { return (long long)n * group <= few; }
 
 __device__ __forceinline__ void report(int* status, int code) { atomicExch(status, code); }
 

@@ -365,21 +365,26 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
   for (int k = 16; k; k >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, k));
   const float shift = most == -kInf ? 0.f : most;
   float total = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  // loads without a condition, so that they are on their way together; what a part without keys left (it wrote nothing) is not taken
+  const bool in = 4 * lane < a.width;
+  lse += from;
+  part += from * a.width + (in ? 4 * lane : 0);
+  const size_t step = stride * a.width;
   for (int p0 = way; p0 < splits; p0 += 4 * ways) {
-    float w[4];
+    float l[4];
     float4 x[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int p = p0 + k * ways;
-      const float l = p < splits ? lse[p * stride + from] : -kInf;
-      w[k] = exp2f(l - shift);
-      x[k] = make_float4(0.f, 0.f, 0.f, 0.f);      // (no keys: nothing was written)
-      if (l != -kInf && 4 * lane < a.width) x[k] = *reinterpret_cast<const float4*>(part + (p * stride + from) * a.width + 4 * lane);
+      const int p = min(p0 + k * ways, splits - 1);
+      l[k] = lse[p * stride];
+      x[k] = *reinterpret_cast<const float4*>(part + p * step);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      total += w[k];
-      v[0] += w[k] * x[k].x; v[1] += w[k] * x[k].y; v[2] += w[k] * x[k].z; v[3] += w[k] * x[k].w;
+      if (p0 + k * ways >= splits || l[k] == -kInf) continue;
+      const float w = exp2f(l[k] - shift);
+      total += w;
+      v[0] += w * x[k].x; v[1] += w * x[k].y; v[2] += w * x[k].z; v[3] += w * x[k].w;
     }
   }
   if (ways > 1) {      // (the CTA has one row and head: it came here as a whole)
@@ -399,7 +404,7 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
 #pragma unroll
   for (int e = 0; e < 4; ++e) { v[e] *= inv; fine &= fabsf(v[e]) < kInf; }
   if (!__all_sync(0xffffffffu, fine)) { attend_row<true>(a, head, row, lane); return; }
-  if (4 * lane < a.width) {
+  if (in) {
     const size_t at = ((size_t)row * a.heads + head) * a.width + 4 * lane;
     if (a.ot == DRAGON_F32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
     else *reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(a.out) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
