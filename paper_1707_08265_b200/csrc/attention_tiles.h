@@ -149,12 +149,11 @@ struct Unit {
   int spare, spares;    // seq < 0: which of how many units that have the rows of none (spare as large as the rows: not one of them)
 };
 
+// Up to so many packed sequences are walked over, more are searched: 64 of up to 100 rows with gradients take 37.2 us walked over and 43.0
+// searched (units without rows stand among the others then), 128 of up to 300 rows 221 and 215, 600 of up to 300 rows 1243 and 939
+constexpr int kWalked = 64;
 // Which block of rows this unit has: blocks of a sequence from its end (those that see most keys go first)
 // (blocks: those that the grid has room for, each_blocks: of a sequence, where all are equally long, 0: starts; block_rows: a power of two)
-// With starts, sequence s has the units from starts[s] / block_rows + s on: the numbers ascend, leave every sequence room for its blocks
-// and come from starts alone, so that a unit finds its sequence in a search of 32 probes a turn (one turn up to 32 sequences; a walk
-// over all of them in every CTA took 46.3 ms for 16384 rows in as many sequences with gradients, the search takes 3.3).  A unit behind its
-// sequence's last block has nothing to do; those in front of the first sequence and behind the last have the rows of none.
 __device__ __forceinline__ void find_unit(const Sequences& q, int blocks, int each_blocks, int unit, int block_rows, Unit* u, int lane) {
   u->seq = -1;
   if (each_blocks) {
@@ -164,6 +163,35 @@ __device__ __forceinline__ void find_unit(const Sequences& q, int blocks, int ea
     u->row0 = (each_blocks - 1 - unit / q.count) * block_rows;
     return;
   }
+  if (q.count <= kWalked) {      // blocks counted from the first sequence on, 32 sequences at a time: units without rows are all behind the others
+    int before = 0;
+    for (int s0 = 0; s0 < q.count; s0 += 32) {
+      int x = 0, y = 0;
+      if (s0 + lane < q.count) q.rows_of(s0 + lane, &x, &y);
+      const int n = (y - x + block_rows - 1) / block_rows;
+      int sum = n;
+#pragma unroll
+      for (int k = 1; k < 32; k <<= 1) { const int t = __shfl_up_sync(0xffffffffu, sum, k); if (lane >= k) sum += t; }
+      const int local = unit - before;
+      const unsigned hit = __ballot_sync(0xffffffffu, local >= sum - n && local < sum);
+      if (hit) {
+        const int w = __ffs(hit) - 1;
+        u->seq = s0 + w;
+        u->a = __shfl_sync(0xffffffffu, x, w);
+        u->b = __shfl_sync(0xffffffffu, y, w);
+        u->row0 = (__shfl_sync(0xffffffffu, sum, w) - 1 - local) * block_rows;
+        return;
+      }
+      before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    u->spare = unit - before;
+    u->spares = blocks - before;
+    return;
+  }
+  // Sequence s has the units from starts[s] / block_rows + s on: the numbers ascend, leave every sequence room for its blocks and come from
+  // starts alone, so that a unit finds its sequence in a search of 32 probes a turn (a walk over all of them in every CTA took 46.3 ms
+  // for 16384 rows in as many sequences with gradients, the search takes 3.3).  A unit behind its sequence's last block has nothing
+  // to do; those in front of the first sequence and behind the last have the rows of none.
   const int shift = 31 - __clz(block_rows);
   auto start = [&](int s) { return min(max(__ldg(q.starts + s), 0), q.rows); };
   int s = -1, step = 1;      // s: the last sequence whose units begin here or before
@@ -217,7 +245,7 @@ bool packs(int group) { return (group & (group - 1)) == 0 && group <= 128; }
 // blocks of rows that a grid needs room for, and those of a sequence where all are equally long
 void count_blocks(const Sequences& q, int block_rows, int* blocks, int* each_blocks) {
   *each_blocks = q.starts ? 0 : (q.each + block_rows - 1) / block_rows;
-  *blocks = q.starts ? (q.rows + block_rows - 1) / block_rows + q.count + 1 : *each_blocks * q.count;      // (one at least behind the last sequence's)
+  *blocks = q.starts ? (q.rows + block_rows - 1) / block_rows + q.count + (q.count > kWalked) : *each_blocks * q.count;      // (one at least for rows of none)
 }
 
 // a kernel's dynamic shared memory, once per device (set: one flag a device)
