@@ -15,9 +15,9 @@
 // One tile pair is 128 x 128; two warps share a row (64 columns each).  The products are issued in an order in which the tensor
 // unit has work while the threads compute: keys: dV(i), S(i+1), dK(i), dP(i+1); rows: S(i+1), dP(i+1), dQ(i) (dP has two buffers).
 // Warps: 0..7 mathematics, 8 TMA, 9 MMA.  Every wait is bounded.
-// Bound: keys, a round has 2048 cycles of products and takes about 3200 (3245 before the products of half of P^T started early); rows, 1536 and 2288; what is left over is one product waiting for the
-// threads' results of another.  16384 causal rows, 8 heads on 2 of 128: 1410 us, 0.97 PFLOP/s of the formula's five products (1.36 of the
-// seven).
+// Bound: keys, a round has 2048 cycles of products and took 3245, about 3200 by the launch's time since the products of half of P^T start
+// early; rows, 1536 and 2288; what is left over is one product waiting for the threads' results of another.  16384 causal rows, 8 heads on
+// 2 of 128: 1395 us on a cool GPU, 0.99 PFLOP/s of the formula's five products (1.38 of the seven), some 15 % more under its power limit.
 // Both kinds are one launch, keys first: theirs are the longest (all heads of a group), and the rows' fill the SMs that run out of them.
 #include <algorithm>
 

@@ -10,7 +10,8 @@
 //   O_t += P_t V               tcgen05.mma with P_t as the A operand out of TMEM, V as it lies in memory (MN-major)
 // While the softmax threads of one tile work, the tensor unit works for the other (of the CTA, or of the SM's other CTA).
 // Bound: exponentials and products alike.  A round (two tiles against 128 keys, heads of 128) has 2048 cycles of each and takes 3200; a
-// CTA's start and end another 14000.  16384 causal rows, 8 heads on 2 of 128: 420 us, 1.31 PFLOP/s.  m only moves when a row's maximum has grown
+// CTA's start and end another 14000.  16384 causal rows, 8 heads on 2 of 128: 420 us, 1.31 PFLOP/s on a cool GPU (with gradients, one after
+// another under the power limit, all launches take some 15 % more).  m only moves when a row's maximum has grown
 // by more than 2^8 (P_t and the sum then stay below 2^8 times their scale, far inside bf16 and fp32): O_t in TMEM is rescaled
 // that seldom that the softmax threads do it themselves.  S_t of the next keys is issued behind O_t's product, so a completed
 // S_t says that O_t may be touched.  Where there are few units of work (few rows or heads, long contexts) the keys of one are split over

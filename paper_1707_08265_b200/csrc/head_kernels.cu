@@ -8,8 +8,8 @@
 // (no rounding grows with the position); its top 32 bits go through sincospi in fp32.  They are the same for every head of a
 // row: a CTA computes those of its rows once, into shared memory.
 //
-// Bound: HBM (every element is read and written once), and next to it instructions (8192 rows, 32 + 8 heads of 128 in bf16: forward 35 us,
-// 4.8 TB/s, gradient 61, 4.1, with 0.55 and 0.62 of the issue slots; three CTAs an SM spill: 99 us for both become 145).  A warp works on one row at a time: 8 elements a
+// Bound: HBM (every element is read and written once), and next to it instructions (8192 rows, 32 + 8 heads of 128 in bf16: forward 36 us,
+// 4.7 TB/s, gradient 59, 4.2, with 0.55 and 0.60 of the issue slots; three CTAs an SM spill: 99 us for both become 145).  A warp works on one row at a time: 8 elements a
 // lane, a head in the next power of two of lanes, so that the head's sums are a few shuffles.  Where pairs are halves apart a lane
 // has 4 elements and their 4 partners.  Gain and angle are multiplied once a row: y = r (a (g c) - b (g' s)), and stay in registers
 // while the warp walks the row's heads.  Tensors of the same rows (queries and keys) are one launch.

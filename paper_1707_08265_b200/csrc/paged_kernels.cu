@@ -6,7 +6,7 @@
 // SMs have some.  The keys of a sequence and key head are split over CTAs; in a CTA each of four warps walks its own groups of 16
 // keys through its own ring of stages (cp.async; no barrier between warps), with mma.sync products of 16 rows and an online
 // softmax in registers (a tile of tcgen05 would have 128 rows, of which 8 were real).  A group of 16 keys lies in one page.
-// One sequence of 100000 tokens, 32 heads on 8 of 128: 67 us, 5.8 TB/s.
+// One sequence of 95225 tokens, 32 heads on 8 of 128: 67 us, 5.8 TB/s (this kernel alone; the whole step 75 to 79).
 // What the warps and the CTAs have is put together by their maxima, in a fixed order.  Sequences with more rows go to the
 // tensor-core kernel for tiles (attention_tcgen05.cu), whose keys are split likewise.
 #include <cuda_runtime.h>
@@ -73,7 +73,7 @@ constexpr int few_pitch(int steps) { return steps * 32 + 16; }      // bytes of 
 constexpr int few_smem(int steps, int m) { return std::max(kFewWarps * kFewStages * 2 * 16 * few_pitch(steps), kFewWarps * 16 * m * (16 * steps + 4) * 4) + 16; }
 
 // CTAs of it that an SM holds, by shared memory and registers.  Two stages and a CTA more were faster than three stages (64 sequences of
-// 4000 tokens 160 -> 148 us)
+// 2000 to 4000 tokens 160 -> 148 us)
 constexpr int few_resident(int steps, int m) {
   return std::min(227 * 1024 / (few_smem(steps, m) + 2048), m == 1 ? 5 : steps <= 2 ? 4 : steps <= 4 ? 3 : 2);
 }
@@ -440,7 +440,7 @@ PagedPlan plan_paged(int64_t rows, int64_t sequences, bool starts, int64_t room,
   p.tiles = starts ? rows * group > p.most_few || !p.few : !p.few;
   if (!p.few) p.most_few = 0;
   p.few_rows = p.most_few > 16 && (starts || each > 16) ? 32 : 16;
-  // few rows: as many parts as the GPU holds at once (one sequence of 100000 tokens: 88 us with 512 CTAs, 79 with the 440 that are there
+  // few rows: as many parts as the GPU holds at once (one sequence of 95225 tokens, the whole step: 88 us with 512 CTAs, 79 with the 440 that are there
   // together); with more sequences than that, whose lengths differ, parts of which some eight CTAs an SM come
   const int64_t units = sequences * kv_heads, slots = few_resident((width + 31) / 32 * 2, p.few_rows / 16) * (int64_t)sm_count;
   p.few_splits = p.few ? parts_of(units, room, units <= slots ? slots / units * units : 8 * (int64_t)sm_count, 256) : 1;

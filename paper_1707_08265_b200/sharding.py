@@ -11,9 +11,9 @@ Which axis, for the five workloads:
   * the MLP (workload 4): the batch; weights and biases are replicated; the loss is a mean over the batch and
     every gradient descends from it, so a rank's results are weighted by its share of the batch and added
     -> all-reduce(sum) of loss, dW1, db1, dW2, db2 after scaling by rows_of_rank / rows.
-Of the language-model operators those that work on each row by itself run on shards of rows (RMSNorm, scales of 1 x 128
-blocks and Quantize in them, the rows of X in ScaledInnerProduct, ClipByNorm by a norm that every rank has); what mixes rows
-(GatedScan, scales of 128 x 128 blocks, GlobalNorm) is refused with a ValueError, and so is a result that only holds one
+Of the language-model operators those that work on each row by itself run on shards of rows (RMSNorm, HeadNorm, Rotate, scales
+of 1 x 128 blocks and Quantize in them, the rows of X in ScaledInnerProduct, ClipByNorm by a norm that every rank has); what mixes
+rows (GatedScan, Attention, CacheWrite, PagedAttention, scales of 128 x 128 blocks, GlobalNorm) is refused with a ValueError, and so is a result that only holds one
 rank's part going into any of them.
 Remote data always lands in local memory (the all-reduce's output) before any kernel reads it.
 """
