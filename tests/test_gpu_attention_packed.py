@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from attention_cases import attention_bounds, attention_feeds, attention_graph, paged_bounds, paged_feeds, paged_graph, within
-from lm_cases import run_gpu
+from lm_cases import run_gpu, to_gpu
 from oracle import interp
 from paper_1707_08265_b200 import binding as B
 
@@ -71,3 +71,27 @@ def test_as_many_sequences_as_rows():
     for d, x in ((outs[1], dev[1]), (outs[2], dev[0])):
         assert bool((d.float().view(rows, 2, 64).abs() <= 128 * 2.0 ** -24 * 0.125 * size * x.float().view(rows, 2, 64).abs() * (1 + 2.0 ** -6) + 1e-30).all())
     assert start.elapsed_time(end) < 40
+
+
+@pytest.mark.parametrize("sequences", [40, 200])
+def test_many_starts_out_of_order_are_reported(sequences):
+    """No access leaves the tensors whatever stands in starts, and the next run with good ones is right."""
+    import torch
+    rows, rng = 700, np.random.default_rng(sequences)
+    good = np.sort(rng.integers(0, rows + 1, sequences + 1))
+    g, ids, inputs, outputs = attention_graph(rows, 4, 2, 64, starts=sequences, grad=True)
+    feeds = attention_feeds(g, inputs, sequences, good)
+    f = B.Graph.from_desc(g.desc).function(inputs, outputs)
+    dev = [to_gpu(a, g.desc["tensors"][t]["dtype"]) for a, t in zip(feeds, inputs)]
+    raw = [torch.full((rows * g.shape(t)[1] + 64,), 7.0, dtype=torch.bfloat16, device="cuda") for t in outputs]
+    outs = [b[:-64].view(rows, -1) for b in raw]
+    for bad in (rng.permutation(good), good[::-1].copy(), rng.integers(-2 ** 31, 2 ** 31, sequences + 1), np.where(np.arange(sequences + 1) % 2, 0, rows)):
+        dev[3].copy_(torch.from_numpy(bad.astype(np.int32)))
+        f.run_torch(dev, outs)
+        assert f.status() == B.ERR_INVALID_ARG and all(bool((b[-64:] == 7).all()) for b in raw)
+    dev[3].copy_(torch.from_numpy(good.astype(np.int32)))
+    f.run_torch(dev, outs)
+    assert f.status() == 0
+    want, bounds = interp.run_function(g.desc, inputs, outputs, feeds), attention_bounds(g, inputs, outputs, feeds)
+    for n, a, b in zip(("y", "dq", "dk", "dv"), outs, want):
+        assert within(a.double().cpu().numpy(), b, bounds[n], "bf16") <= 1, n
