@@ -62,7 +62,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 1 + 4 * kSt1 + 2 * kSt2 + 9);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   __shared__ Unit unit;
-  __shared__ unsigned again[8];
+  __shared__ unsigned again[2][8];      // rows of a warp whose dk or dq, and whose dv, is not finite
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = a.r.heads / a.r.kv_heads;
   const int shift = a.pack_shift, pack = 1 << shift, tile_rows = 128 >> shift;      // rows of the sequence in a tile of queries
   const int own_rows = kKeys ? 128 : tile_rows, own_heads = kKeys ? 1 : pack, n_heads = kKeys ? a.r.kv_heads : a.r.heads;
@@ -375,10 +375,10 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
       ok = wait_warp(acc_full, 0);
       fence_after();
     }
-    bool fine = true;
+    bool fine[2] = {true, true};
     if (ok) {      // a warp writes half of the head's elements
       const size_t at = ((size_t)(u.a + row) * n_heads + head) * a.r.width;
-      auto write = [&](uint32_t acc, void* out, int type, float factor) {
+      auto write = [&](uint32_t acc, void* out, int type, float factor, bool* fine) {
 #pragma unroll 1
         for (int c = 32 * kChunks * half; c < min(a.r.width, 32 * kChunks * (half + 1)); c += 16) {
           uint32_t o[16];
@@ -386,7 +386,7 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
           tmem_ld16(tmem + lanes + acc + c, o);
           tmem_loaded16(o);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) { f[k] = __uint_as_float(o[k]) * factor; fine &= fabsf(f[k]) < kInf; }
+          for (int k = 0; k < 16; ++k) { f[k] = __uint_as_float(o[k]) * factor; *fine &= fabsf(f[k]) < kInf; }
           if (mine && out) {
             store_any<8>(out, type, at + c, f);
             if (c + 8 < a.r.width) store_any<8>(out, type, at + c + 8, f + 8);
@@ -395,24 +395,33 @@ __device__ __forceinline__ void bwd_cta(const CUtensorMap& tm_q, const CUtensorM
       };
       const bool parts = splits > 1;
       if (kKeys) {
-        write(kAcc1, parts ? to : a.r.dk, parts ? DRAGON_F32 : a.r.dkt, a.r.raw_scale);
-        write(kAcc2, parts ? to_v : a.r.dv, parts ? DRAGON_F32 : a.r.dvt, 1.f);
+        write(kAcc1, parts ? to : a.r.dk, parts ? DRAGON_F32 : a.r.dkt, a.r.raw_scale, fine);
+        write(kAcc2, parts ? to_v : a.r.dv, parts ? DRAGON_F32 : a.r.dvt, 1.f, fine + 1);
       } else {
-        write(kAcc1, parts ? to : a.r.out, parts ? DRAGON_F32 : a.r.ot, a.r.raw_scale);
+        write(kAcc1, parts ? to : a.r.out, parts ? DRAGON_F32 : a.r.ot, a.r.raw_scale, fine);
       }
-      fine |= parts;      // (where the parts are added up a row that is not finite is computed again)
+      fine[0] |= parts || (kKeys && !a.r.dk);      // (where the parts are added up a row that is not finite is computed again)
+      fine[1] |= parts || !kKeys || !a.r.dv;
     }
     // rows that are not finite: again, after both halves have been written (every warp comes here, after an unwind too)
-    const unsigned bad = __ballot_sync(0xffffffffu, mine && !fine);
-    if (lane == 0) again[warp] = bad;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const unsigned bad = __ballot_sync(0xffffffffu, mine && !fine[k]);
+      if (lane == 0) again[k][warp] = bad;
+    }
     __syncwarp();
     asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (half == 0)
-      for (unsigned b = again[warp] | again[warp + 4]; b; b &= b - 1) {
+    {      // the two warps of 32 rows take turns
+      const unsigned bad1 = again[0][warp & 3] | again[0][(warp & 3) + 4], bad2 = again[1][warp & 3] | again[1][(warp & 3) + 4];
+      int turn = 0;
+      for (unsigned b = bad1 | bad2; b; b &= b - 1) {
+        if ((turn++ & 1) != half) continue;
         const int r = (warp & 3) * 32 + __ffs(b) - 1, first_row = u.a + u.row0;
-        if (kKeys) dkv_of_row(a.r, head0, first_row + r, lane);
+        const unsigned bit = b & (0u - b);
+        if (kKeys) dkv_of_row(a.r, head0, first_row + r, lane, bad1 & bit, bad2 & bit);
         else dq_of_row(a.r, head0 + (r & (pack - 1)), first_row + (r >> shift), lane);
       }
+    }
   }
   fence_before();
   __syncthreads();

@@ -82,14 +82,16 @@ __global__ void __launch_bounds__(256) attention_join(const __grid_constant__ Ro
   bool fine = fabsf(total) < kInf;
 #pragma unroll
   for (int e = 0; e < 4; ++e) { v[e] *= inv; fine &= fabsf(v[e]) < kInf; }
-  if (!__all_sync(0xffffffffu, fine)) { attend_row<false>(a, head, row, lane); return; }
   if (a.lse && lane == 0) a.lse[(size_t)head * a.seq.rows + row] = total == 0.f ? kInf : shift + log2f(total);
-  if (!in) return;
   const size_t at = item * a.width + 4 * lane;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    if (a.out) put(a.out, a.ot, at + e, v[e]);
-    if (a.rest) put(a.rest, DRAGON_BF16, at + e, behind_bf16(v[e]));
+    if (a.out && in) put(a.out, a.ot, at + e, v[e]);
+    if (a.rest && in) put(a.rest, DRAGON_BF16, at + e, behind_bf16(v[e]));
+  }
+  if (!__all_sync(0xffffffffu, fine)) {
+    __syncwarp();
+    attend_row<false>(a, head, row, lane);
   }
 }
 
@@ -115,19 +117,17 @@ __global__ void __launch_bounds__(256) attention_bwd_join(const __grid_constant_
     return fabsf(v[0]) < kInf && fabsf(v[1]) < kInf && fabsf(v[2]) < kInf && fabsf(v[3]) < kInf;
   };
   float v[4], w[4];
-  const bool fine = !keys ? sum(a.part, a.splits, v) : (!a.dk || sum(a.part_k, a.key_splits, v)) & (!a.dv || sum(a.part_v, a.key_splits, w));
-  if (!__all_sync(0xffffffffu, fine)) {
-    if (keys) dkv_of_row(a, head, row, lane);
-    else dq_of_row(a, head, row, lane);
-    return;
-  }
-  if (!in) return;
+  const bool fine = __all_sync(0xffffffffu, !keys ? sum(a.part, a.splits, v) : !a.dk || sum(a.part_k, a.key_splits, v));
+  const bool fine_v = __all_sync(0xffffffffu, !keys || !a.dv || sum(a.part_v, a.key_splits, w));
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 4 && in; ++e) {
     if (!keys) put(a.out, a.ot, at + e, v[e]);
     if (keys && a.dk) put(a.dk, a.dkt, at + e, v[e]);
     if (keys && a.dv) put(a.dv, a.dvt, at + e, w[e]);
   }
+  __syncwarp();
+  if (keys && !(fine && fine_v)) dkv_of_row(a, head, row, lane, !fine, !fine_v);
+  else if (!fine) dq_of_row(a, head, row, lane);
 }
 
 RowArgs row_args(const StepRun& r) {

@@ -403,11 +403,14 @@ __global__ void __launch_bounds__(256) paged_join(const __grid_constant__ RowArg
   bool fine = fabsf(total) < kInf;
 #pragma unroll
   for (int e = 0; e < 4; ++e) { v[e] *= inv; fine &= fabsf(v[e]) < kInf; }
-  if (!__all_sync(0xffffffffu, fine)) { attend_row<true>(a, head, row, lane); return; }
   if (in) {
     const size_t at = ((size_t)row * a.heads + head) * a.width + 4 * lane;
     if (a.ot == DRAGON_F32) *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
     else *reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(a.out) + at) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+  }
+  if (!__all_sync(0xffffffffu, fine)) {
+    __syncwarp();
+    attend_row<true>(a, head, row, lane);
   }
 }
 
